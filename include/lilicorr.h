@@ -318,6 +318,64 @@ lilicorr_status_t lilicorr_select_block_walk(const lilicorr_head* head, int B, c
                                              int32_t* tokens, void* ws, size_t ws_bytes,
                                              cudaStream_t stream);
 
+/* Beam search. Not from the paper: a program that drafts or decodes several continuations
+ * (beams) of a request picks over (beam, token) where lilicorr_topk_lse picks over tokens, and
+ * moves the beams' caches accordingly. `requests` R, `beams` W per request (1 <= W <=
+ * LILICORR_MAX_BEAMS), n continuations kept (1 <= n <= LILICORR_MAX_K).
+ *   scores [R, W] fp32   running log-probability of each beam; -inf: there is no such beam
+ *   done   [R, W] bytes  not 0: the beam has ended (may be NULL: none has)
+ *   end_id               the token that ends a beam, or -1 (only where done is NULL)
+ * A live beam w offers each of its tokens v at total = scores[w] + logp(v | w); a beam that is done
+ * offers the one candidate (end_id, scores[w]), and nothing else about it is read. Totals are formed
+ * and compared in 64 bits; equal totals order by lower beam, in a beam by the candidates' order. A
+ * candidate of total -inf (a banned token) is never kept. Outputs, best first:
+ *   tokens, parents [R, n] int32   token and beam of each kept candidate; -1 where there are fewer
+ *   next_scores     [R, n] fp32    the total, rounded once; -inf where there are fewer
+ *   next_done       [R, n] bytes   1 where the parent was done or the token is end_id (may be NULL)
+ * so outputs are inputs of the next step, -inf and -1 included. Outputs must not overlap inputs. A
+ * NaN or +inf score or log-probability, and a live beam whose normaliser is not finite (NaN or +inf
+ * logits, or only -inf), set LILICORR_ERR_NONFINITE; such a candidate, or beam, is not kept. */
+#define LILICORR_MAX_BEAMS 64
+
+/* From logits [R, W, V] (F32 or BF16), one pass over the rows of live beams:
+ * logp(v | w) = logits[w, v] - log sum_u exp(logits[w, u]), in a beam equal logits by lower id.
+ * n <= W * V, R * W <= 65535. ws: zero-filled once, at least
+ * lilicorr_beam_select_workspace_bytes(R, W, V, n) bytes (0: unsupported shape); its first word is
+ * the device status. */
+size_t lilicorr_beam_select_workspace_bytes(int requests, int beams, int V, int n);
+lilicorr_status_t lilicorr_beam_select(const void* logits, lilicorr_dtype_t dtype, int requests,
+                                       int beams, int V, int n, const float* scores,
+                                       const uint8_t* done, int32_t end_id, int32_t* tokens,
+                                       int32_t* parents, float* next_scores, uint8_t* next_done,
+                                       void* ws, size_t ws_bytes, cudaStream_t stream);
+
+/* From candidate lists ids, logp [R, W, K] (lilicorr_topk_lse, lilicorr_lm_head_topk or merged
+ * vocabulary shards; any order, in a beam equal totals by position): the exact beam search step
+ * where K >= min(n, V). 1 <= K <= LILICORR_MAX_K, n <= W * K. status: a device uint32 word (may be
+ * NULL) that receives LILICORR_ERR_NONFINITE. */
+lilicorr_status_t lilicorr_beam_merge(const int32_t* ids, const float* logp, int requests, int beams,
+                                      int K, int n, const float* scores, const uint8_t* done,
+                                      int32_t end_id, int32_t* tokens, int32_t* parents,
+                                      float* next_scores, uint8_t* next_done, uint32_t* status,
+                                      cudaStream_t stream);
+
+/* The beams' states moved, in place, to the beams that continue them: for each of the n_states
+ * arrays (caches of layers, keys and values: device pointers in the host array host_states), each
+ * request r and position p < lengths[r],
+ *   state[r, w, p, h, :] = (state before the call)[r, parents[r, w], p, h, :].
+ * An array is [requests, beams, positions, heads] rows of row_bytes contiguous bytes, the strides in
+ * bytes and the same for all arrays (which must not overlap one another, nor an array itself).
+ *   parents [R, W] int32 device; a value outside [0, W) leaves that beam as it is
+ *   lengths [R] int32 device, at most `positions` of them are moved; NULL: all positions
+ * No alignment is asked for; rows and strides that are multiples of 16 bytes are fastest. positions *
+ * heads * row_bytes below 2^35, fewer for narrower vectors. */
+lilicorr_status_t lilicorr_beam_reorder(void* const* host_states, int n_states, int requests,
+                                        int beams, int positions, int heads, size_t row_bytes,
+                                        int64_t stride_request, int64_t stride_beam,
+                                        int64_t stride_position, int64_t stride_head,
+                                        const int32_t* parents, const int32_t* lengths,
+                                        cudaStream_t stream);
+
 /* Device view of a select_block workspace after the call, for inspection:
  * pointers into ws of the intermediates of the last call (ids [B,L,K] int32,
  * logp [B,L,K] fp32, lse [B,L] fp32, anchor [B,K] fp32, pair [B,L-1,K,K] fp32,

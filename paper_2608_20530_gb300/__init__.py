@@ -7,7 +7,8 @@ library is missing, every call raises.
 
 Names follow the C ABI: ``topk_lse``, ``embed_in_out``, ``pair_scores``,
 ``greedy_walk``, ``select_block``, plus ``Head`` (an uploaded scoring head) and
-``Workspace`` (caller-owned scratch).
+``Workspace`` (caller-owned scratch); for several continuations of a request (beams, drafted
+blocks) ``beam_select``, ``beam_merge`` and ``beam_reorder``.
 """
 from __future__ import annotations
 
@@ -78,6 +79,13 @@ _SIGS = {
     "lilicorr_topk_lse_partial": (_I, [_P, _I, _I, _I, _I, _I, _P, _P, _S, _P]),
     "lilicorr_topk_lse_merge": (_I, [_P, _I, _I, _I, _P, _P, _P, _P, _P]),
     "lilicorr_topk_lse_noalloc": (_I, [_P, _I, _I, _I, _I, _P, _P, _P, _P]),
+    "lilicorr_beam_select_workspace_bytes": (_S, [_I, _I, _I, _I]),
+    "lilicorr_beam_select": (_I, [_P, _I, _I, _I, _I, _I, _P, _P, ctypes.c_int32, _P, _P, _P, _P, _P,
+                                  _S, _P]),
+    "lilicorr_beam_merge": (_I, [_P, _P, _I, _I, _I, _I, _P, _P, ctypes.c_int32, _P, _P, _P, _P, _P,
+                                 _P]),
+    "lilicorr_beam_reorder": (_I, [ctypes.POINTER(_P), _I, _I, _I, _I, _I, _S] +
+                              [ctypes.c_int64] * 4 + [_P, _P, _P]),
     "lilicorr_test_linear": (_I, [_P, _I, _I, _P, _I, _I, _P, _I, _I, _I, _I, _I, _P, _P, _I, _I,
                                   _P, _P]),
     "lilicorr_test_linear_timeout": (_I, [_P, _P, _P, _I, _I, _I, ctypes.c_longlong, _P, _P]),
@@ -121,6 +129,18 @@ def _dev(t: torch.Tensor, name: str) -> torch.Tensor:
         raise ValueError(f"{name} must be a CUDA tensor")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
+    return t
+
+
+def _here(t: torch.Tensor, name: str, dtype: Optional[torch.dtype] = None,
+          shape: Optional[Tuple[int, ...]] = None) -> torch.Tensor:
+    """``t`` on the current device, of that type and shape (strides are the caller's matter)."""
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} must be a CUDA tensor on the current device")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     return t
 
 
@@ -482,6 +502,106 @@ def select_block(head: Head, logits: torch.Tensor, hidden: torch.Tensor, target:
                                                 target.data_ptr(), WALKS[walk], tokens.data_ptr(),
                                                 ws.ptr, ws.nbytes, _stream()), "select_block_walk")
     return tokens
+
+
+# --------------------------------------------------------------------------- beams
+def _beam_args(scores: torch.Tensor, done: Optional[torch.Tensor], R: int, W: int, n: int):
+    _dev(_here(scores, "scores", torch.float32, (R, W)), "scores")
+    if done is not None:
+        if done.dtype not in (torch.bool, torch.uint8):
+            raise ValueError("done must be bool or uint8")
+        _dev(_here(done, "done", None, (R, W)), "done")
+    dev = scores.device
+    n = max(int(n), 0)
+    return (torch.empty((R, n), dtype=torch.int32, device=dev),
+            torch.empty((R, n), dtype=torch.int32, device=dev),
+            torch.empty((R, n), dtype=torch.float32, device=dev),
+            torch.empty((R, n), dtype=torch.bool, device=dev))
+
+
+def beam_select_workspace_bytes(requests: int, beams: int, V: int, n: int) -> int:
+    """Bytes of the workspace that beam_select needs (0: unsupported shape)."""
+    return int(lib().lilicorr_beam_select_workspace_bytes(requests, beams, V, n))
+
+
+def beam_select(logits: torch.Tensor, scores: torch.Tensor, n: int,
+                done: Optional[torch.Tensor] = None, end_id: int = -1,
+                ws: Optional[Workspace] = None):
+    """The n best continuations of each request over its beams and the vocabulary: logits
+    [R, W, V] (fp32 or bf16) and running scores [R, W] fp32 -> (tokens [R, n] int32, parents [R, n]
+    int32, scores [R, n] fp32, done [R, n] bool), best first. A score of -inf is an absent beam;
+    beams that are ``done`` [R, W] keep their score and offer ``end_id`` (see lilicorr.h)."""
+    if logits.dim() != 3:
+        raise ValueError("logits must be [requests, beams, V]")
+    _dev(_here(logits, "logits"), "logits")
+    R, W, V = logits.shape
+    out = _beam_args(scores, done, R, W, n)
+    if ws is None:
+        ws = Workspace(beam_select_workspace_bytes(R, W, V, n), logits.device)
+    _check(lib().lilicorr_beam_select(logits.data_ptr(), _dtype_code(logits), R, W, V, int(n),
+                                      scores.data_ptr(), _ptr(done), int(end_id),
+                                      *(t.data_ptr() for t in out), ws.ptr, ws.nbytes, _stream()),
+           "beam_select")
+    return out
+
+
+def beam_merge(ids: torch.Tensor, logp: torch.Tensor, scores: torch.Tensor, n: int,
+               done: Optional[torch.Tensor] = None, end_id: int = -1,
+               status: Optional[torch.Tensor] = None):
+    """beam_select from candidate lists ids [R, W, K] int32, logp [R, W, K] fp32 (of topk_lse,
+    lm_head_topk or topk_lse_merge): the exact beam search step where K >= min(n, V)."""
+    if ids.dim() != 3:
+        raise ValueError("ids must be [requests, beams, K]")
+    R, W, K = ids.shape
+    _dev(_here(ids, "ids", torch.int32), "ids")
+    _dev(_here(logp, "logp", torch.float32, (R, W, K)), "logp")
+    out = _beam_args(scores, done, R, W, n)
+    _check(lib().lilicorr_beam_merge(ids.data_ptr(), logp.data_ptr(), R, W, K, int(n),
+                                     scores.data_ptr(), _ptr(done), int(end_id),
+                                     *(t.data_ptr() for t in out), _ptr(status), _stream()),
+           "beam_merge")
+    return out
+
+
+def _state_layout(t: torch.Tensor, R: int, W: int, name: str):
+    """(positions, heads, row bytes, the four strides in bytes) of a state [R, W, positions, ...]:
+    trailing dimensions dense, but that the fourth of five may have any stride."""
+    if t.dim() < 3 or t.shape[0] != R or t.shape[1] != W:
+        raise ValueError(f"{name} must be [requests, beams, positions, ...]")
+    es = t.element_size()
+    heads, s_head, tail = 1, 0, list(range(3, t.dim()))
+    if t.dim() == 5:
+        heads, s_head, tail = t.shape[3], t.stride(3) * es, [4]
+    row = es
+    for i in reversed(tail):
+        if t.shape[i] > 1 and t.stride(i) * es != row:
+            raise ValueError(f"{name}: the dimensions behind the positions must be dense")
+        row *= t.shape[i]
+    return (t.shape[2], heads, row, t.stride(0) * es, t.stride(1) * es, t.stride(2) * es, s_head)
+
+
+def beam_reorder(states, parents: torch.Tensor, lengths: Optional[torch.Tensor] = None):
+    """Move the beams' states, in place, to the beams that continue them: for each tensor
+    [R, W, positions, ...] of ``states`` (one or a sequence, e.g. the layers' key and value caches)
+    state[r, w, :lengths[r]] = state[r, parents[r, w], :lengths[r]] as it was before the call.
+    parents [R, W] int32 (outside [0, W): the beam stays), lengths [R] int32 (None: all). Tensors may
+    be strided views ([R, W, positions, heads, d] of any layout with dense d). Returns ``states``."""
+    tensors = [states] if isinstance(states, torch.Tensor) else list(states)
+    if parents.dim() != 2:
+        raise ValueError("parents must be [requests, beams]")
+    R, W = parents.shape
+    _dev(_here(parents, "parents", torch.int32), "parents")
+    if lengths is not None:
+        _dev(_here(lengths, "lengths", torch.int32, (R,)), "lengths")
+    groups: Dict[tuple, list] = {}
+    for i, t in enumerate(tensors):
+        _here(t, f"states[{i}]")
+        groups.setdefault(_state_layout(t, R, W, f"states[{i}]"), []).append(t.data_ptr())
+    for (positions, heads, row, *strides), ptrs in groups.items():
+        _check(lib().lilicorr_beam_reorder((_P * len(ptrs))(*ptrs), len(ptrs), R, W, positions, heads,
+                                           row, *strides, parents.data_ptr(), _ptr(lengths),
+                                           _stream()), "beam_reorder")
+    return states
 
 
 def test_linear(A: torch.Tensor, W: torch.Tensor, out_dtype=torch.float32, bias=None,
