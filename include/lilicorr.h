@@ -376,6 +376,41 @@ lilicorr_status_t lilicorr_beam_reorder(void* const* host_states, int n_states, 
                                         const int32_t* parents, const int32_t* lengths,
                                         cudaStream_t stream);
 
+/* Attention of sequences that share a prefix. Not from the paper: the pass in which the target
+ * verifies several drafted blocks of a request (the greedy walk's and the best path's, say), or in
+ * which the beams of a request take their next step. N = groups * beams sequences, sequence n of
+ * group n / beams; a group's sequences share the keys and values of its prefix, which are read once
+ * for all of them, and each has its own behind it, the T = tokens newest included:
+ *   out[n, t, h] = sum_j softmax_j(scale q[n, t, h] . key_j) value_j
+ * over the prefix's positions j < prefix_len[n / beams] and the own positions j < seq_len[n] - (T -
+ * 1 - t), key head h / (q_heads / kv_heads); lse[n, t, h] = log sum_j exp(scale q . key_j). A row
+ * that sees no key gets out 0 and lse -inf. Lengths are clipped to [0, capacity], but seq_len[n] < 0
+ * says that there is no sequence n: its rows of out and lse are left as they were. What a cache holds
+ * behind its length is not looked at (NaN included); what it holds before it has to be finite.
+ *   q, out [N, T, q_heads, head_dim]; prefix_k, prefix_v [groups, prefix_capacity, kv_heads,
+ *   head_dim]; k, v [N, own_capacity, kv_heads, head_dim], all of dtype, each with its strides in
+ *   elements (the last dimension is dense), 16-byte aligned, strides multiples of 16 bytes and not
+ *   negative; lse [N, T, q_heads] fp32; prefix_len [groups], seq_len [N] int32 on the device
+ * head_dim a multiple of 8 up to 128, q_heads a multiple of kv_heads, capacities from 0 (then the
+ * pointers of that side may be NULL) to 2^30. F32 runs in fp32 throughout; BF16 takes bf16 products
+ * with fp32 accumulation, softmax and sums in fp32. ws: zero-filled once, at least
+ * lilicorr_prefix_attention_workspace_bytes(desc) bytes (0: unsupported); its first word is the
+ * device status. */
+typedef struct {
+  int groups, beams, tokens, q_heads, kv_heads, head_dim, prefix_capacity, own_capacity;
+  lilicorr_dtype_t dtype;
+  float scale;
+  int64_t q_stride[3], out_stride[3];                /* sequence, token, head */
+  int64_t prefix_k_stride[3], prefix_v_stride[3];    /* group, position, head */
+  int64_t k_stride[3], v_stride[3];                  /* sequence, position, head */
+} lilicorr_prefix_attention_desc;
+size_t lilicorr_prefix_attention_workspace_bytes(const lilicorr_prefix_attention_desc* desc);
+lilicorr_status_t lilicorr_prefix_attention(const lilicorr_prefix_attention_desc* desc, const void* q,
+                                            const void* prefix_k, const void* prefix_v,
+                                            const int32_t* prefix_len, const void* k, const void* v,
+                                            const int32_t* seq_len, void* out, float* lse, void* ws,
+                                            size_t ws_bytes, cudaStream_t stream);
+
 /* Device view of a select_block workspace after the call, for inspection:
  * pointers into ws of the intermediates of the last call (ids [B,L,K] int32,
  * logp [B,L,K] fp32, lse [B,L] fp32, anchor [B,K] fp32, pair [B,L-1,K,K] fp32,

@@ -8,7 +8,7 @@ library is missing, every call raises.
 Names follow the C ABI: ``topk_lse``, ``embed_in_out``, ``pair_scores``,
 ``greedy_walk``, ``select_block``, plus ``Head`` (an uploaded scoring head) and
 ``Workspace`` (caller-owned scratch); for several continuations of a request (beams, drafted
-blocks) ``beam_select``, ``beam_merge`` and ``beam_reorder``.
+blocks) ``beam_select``, ``beam_merge``, ``beam_reorder`` and ``prefix_attention``.
 """
 from __future__ import annotations
 
@@ -40,6 +40,15 @@ class HeadDesc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int) for n in
                 ("H", "D", "d", "n_heads", "ffn", "n_layers", "L", "K", "V", "n_tgt")] + \
                [("dtype", ctypes.c_int)]
+
+
+class PrefixAttentionDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in
+                ("groups", "beams", "tokens", "q_heads", "kv_heads", "head_dim", "prefix_capacity",
+                 "own_capacity", "dtype")] + [("scale", ctypes.c_float)] + \
+               [(n, ctypes.c_int64 * 3) for n in
+                ("q_stride", "out_stride", "prefix_k_stride", "prefix_v_stride", "k_stride",
+                 "v_stride")]
 
 
 _LIB: Optional[ctypes.CDLL] = None
@@ -86,6 +95,8 @@ _SIGS = {
                                  _P]),
     "lilicorr_beam_reorder": (_I, [ctypes.POINTER(_P), _I, _I, _I, _I, _I, _S] +
                               [ctypes.c_int64] * 4 + [_P, _P, _P]),
+    "lilicorr_prefix_attention_workspace_bytes": (_S, [ctypes.POINTER(PrefixAttentionDesc)]),
+    "lilicorr_prefix_attention": (_I, [ctypes.POINTER(PrefixAttentionDesc)] + [_P] * 10 + [_S, _P]),
     "lilicorr_test_linear": (_I, [_P, _I, _I, _P, _I, _I, _P, _I, _I, _I, _I, _I, _P, _P, _I, _I,
                                   _P, _P]),
     "lilicorr_test_linear_timeout": (_I, [_P, _P, _P, _I, _I, _I, ctypes.c_longlong, _P, _P]),
@@ -602,6 +613,67 @@ def beam_reorder(states, parents: torch.Tensor, lengths: Optional[torch.Tensor] 
                                            row, *strides, parents.data_ptr(), _ptr(lengths),
                                            _stream()), "beam_reorder")
     return states
+
+
+# --------------------------------------------------------------------------- shared prefixes
+def _attention_desc(q: torch.Tensor, prefix_k: torch.Tensor, k: torch.Tensor,
+                    scale: Optional[float]) -> PrefixAttentionDesc:
+    if q.dim() != 4 or prefix_k.dim() != 4 or k.dim() != 4:
+        raise ValueError("q is [N, T, q_heads, d], caches are [groups or N, capacity, kv_heads, d]")
+    N, T, Hq, d = q.shape
+    G, P, Hkv, _ = prefix_k.shape
+    if N % max(G, 1) or (G == 0 and N):
+        raise ValueError(f"{N} sequences do not divide into {G} groups")
+    x = PrefixAttentionDesc(G, N // G if G else 1, T, Hq, Hkv, d, P, k.shape[1], _dtype_code(q),
+                            d ** -0.5 if scale is None and d else float(scale or 0.0))
+    return x
+
+
+def prefix_attention_workspace_bytes(q: torch.Tensor, prefix_k: torch.Tensor, k: torch.Tensor) -> int:
+    """Bytes of the workspace that prefix_attention needs for tensors of these shapes."""
+    return int(lib().lilicorr_prefix_attention_workspace_bytes(
+        ctypes.byref(_attention_desc(q, prefix_k, k, 1.0))))
+
+
+def prefix_attention(q: torch.Tensor, prefix_k: torch.Tensor, prefix_v: torch.Tensor, k: torch.Tensor,
+                     v: torch.Tensor, prefix_len: torch.Tensor, seq_len: torch.Tensor,
+                     scale: Optional[float] = None, ws: Optional[Workspace] = None,
+                     out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None):
+    """Attention of N sequences, each group of N / G of them behind one prefix that is read once for
+    all: q [N, T, q_heads, d] (the T newest tokens of each), prefix_k, prefix_v [G, P, kv_heads, d]
+    of which prefix_len [G] positions are held, k, v [N, S, kv_heads, d] of which seq_len [N] are, the
+    T newest included (causal among them) -> (out like q, lse [N, T, q_heads] fp32). fp32 or bf16, any
+    strides that keep 16-byte rows. seq_len < 0: no such sequence, its rows of ``out`` and ``lse``
+    stay as they are. scale defaults to 1 / sqrt(d)."""
+    x = _attention_desc(q, prefix_k, k, scale)
+    N, T, Hq, d = q.shape
+    G, P, Hkv, _ = prefix_k.shape
+    S = k.shape[1]
+    if out is None:
+        out = torch.empty((N, T, Hq, d), dtype=q.dtype, device=q.device)
+    if lse is None:
+        lse = torch.empty((N, T, Hq), dtype=torch.float32, device=q.device)
+    for t, name, shape, strides in ((q, "q", (N, T, Hq, d), x.q_stride),
+                                    (out, "out", (N, T, Hq, d), x.out_stride),
+                                    (prefix_k, "prefix_k", (G, P, Hkv, d), x.prefix_k_stride),
+                                    (prefix_v, "prefix_v", (G, P, Hkv, d), x.prefix_v_stride),
+                                    (k, "k", (N, S, Hkv, d), x.k_stride),
+                                    (v, "v", (N, S, Hkv, d), x.v_stride)):
+        _here(t, name, q.dtype, shape)
+        if t.numel() and d > 1 and t.stride(3) != 1:
+            raise ValueError(f"{name}: the last dimension must be dense")
+        strides[:] = t.stride()[:3]
+    _dev(_here(lse, "lse", torch.float32, (N, T, Hq)), "lse")
+    _dev(_here(prefix_len, "prefix_len", torch.int32, (G,)), "prefix_len")
+    _dev(_here(seq_len, "seq_len", torch.int32, (N,)), "seq_len")
+    if ws is None:
+        ws = Workspace(int(lib().lilicorr_prefix_attention_workspace_bytes(ctypes.byref(x))), q.device)
+    _check(lib().lilicorr_prefix_attention(ctypes.byref(x), q.data_ptr(), prefix_k.data_ptr(),
+                                           prefix_v.data_ptr(), prefix_len.data_ptr(), k.data_ptr(),
+                                           v.data_ptr(), seq_len.data_ptr(), out.data_ptr(),
+                                           lse.data_ptr(), ws.ptr, ws.nbytes, _stream()),
+           "prefix_attention")
+    return out, lse
 
 
 def test_linear(A: torch.Tensor, W: torch.Tensor, out_dtype=torch.float32, bias=None,

@@ -1,0 +1,619 @@
+// Attention of sequences that share a prefix: beams of a request, or drafted blocks under
+// verification, each with a short cache of its own behind the request's.
+//
+//   out = sum_j softmax_j(scale q . k_j) v_j  over the prefix's keys and the sequence's own
+//
+// The softmax over the two key sets splits: with (m, l, o) = (max s, sum 2^(s - m), sum 2^(s - m) v)
+// of each piece of the keys, the whole is sum 2^(m_i - M) o_i / sum 2^(m_i - M) l_i, M = max m_i. So
+// the rows of ALL sequences of a group meet the prefix as one product (its keys are read once for
+// all), each sequence's own keys are a second, and one pass joins the pieces. Scores, maxima, sums and
+// o are fp32; on bf16 inputs the probabilities are rounded to bf16 for the second product (half a
+// step 2^-9 of each term, of either sign, below the output's own rounding), their sum is of the
+// unrounded ones.
+#include "prefix_attention.cuh"
+
+namespace lilicorr {
+
+namespace {
+
+constexpr int PM_THREADS = 128;
+constexpr int PM_KT = 64;                // keys per stage
+constexpr int PM_STAGES = 3;
+
+__device__ __forceinline__ uint32_t sm_addr(const void* p) {
+  return static_cast<uint32_t>(__cvta_generic_to_shared(p));
+}
+__device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr));
+}
+__device__ __forceinline__ void ldsm4_t(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr));
+}
+__device__ __forceinline__ void mma_16x8x16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0,
+                                            uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, "
+      "{%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// 16 bytes to shared memory, zeros where `live` is false (the source is not read then)
+__device__ __forceinline__ void copy16(void* dst, const void* src, bool live) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(sm_addr(dst)), "l"(src),
+               "r"(live ? 16 : 0)
+               : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+// Stage keys [key0, key0 + KT) of one (group or sequence, head): rows of `row_bytes` live bytes in
+// smem rows of ld bytes, zeros past `held` keys and past the head's width, so that whatever the cache
+// holds behind its last token (NaN too) meets its zero probability as a zero.
+template <int KT, int PIECES, int NT>
+__device__ __forceinline__ void stage_rows(unsigned char* dst, const unsigned char* src, int64_t s_pos,
+                                           int ld, int key0, int held, int pieces, int tid) {
+#pragma unroll 4
+  for (int i = tid; i < KT * PIECES; i += NT) {
+    const int j = i / PIECES, p = i % PIECES;
+    const bool live = key0 + j < held && p < pieces;
+    copy16(dst + j * ld + p * 16, live ? src + (int64_t)(key0 + j) * s_pos + p * 16 : src, live);
+  }
+}
+
+// bf16: four warps, RB of the four over 16 query rows each, the other 4 / RB over the keys of a stage
+// (warp-level products; the pieces of the keys meet in shared memory at the end).
+template <int DP, int RB>
+__global__ void __launch_bounds__(PM_THREADS)
+pa_mma_kernel(const PaArgs a, const PaKeys kk, int rows, int blocks) {
+  pdl_wait();
+  constexpr int LD = (DP + 8) * 2;                  // bytes of a staged row
+  constexpr int PH = 4 / RB, KW = PM_KT / PH;       // key phases, keys per warp and stage
+  constexpr int KS = DP / 16, NB = KW / 8, OB = DP / 8;
+  extern __shared__ __align__(16) unsigned char sm[];
+  constexpr int STAGE = 2 * PM_KT * LD;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int rb = warp % RB, ph = warp / RB;
+
+  int x = blockIdx.x;
+  const int block = x % blocks; x /= blocks;
+  const int hk = x % a.Hkv; x /= a.Hkv;
+  const int b = x % (kk.own ? a.G * a.W : a.G);
+  const int split = x / (kk.own ? a.G * a.W : a.G);
+  const int held = min(max(kk.len[b], 0), kk.capacity);
+  int k0, k1;
+  pa_piece(held, kk.splits, split, k0, k1);
+  const int r0 = block * 16 * RB;
+  const int slot = kk.slot0 + split;
+  if (k0 >= k1) {
+    for (int r = r0 + tid; r < min(rows, r0 + 16 * RB); r += PM_THREADS)
+      a.ml[(size_t)slot * a.rows() + pa_index(a, pa_row(a, kk.own, b, hk, r))] =
+          make_float2(-INFINITY, 0.f);
+    return;
+  }
+  const unsigned char* kp = static_cast<const unsigned char*>(kk.k) +
+                            2 * ((int64_t)b * kk.k_s[0] + (int64_t)hk * kk.k_s[2]);
+  const unsigned char* vp = static_cast<const unsigned char*>(kk.v) +
+                            2 * ((int64_t)b * kk.v_s[0] + (int64_t)hk * kk.v_s[2]);
+  const int pieces = a.d / 8, tiles = (k1 - k0 + PM_KT - 1) / PM_KT;
+  auto stage = [&](int t) {
+    unsigned char* s = sm + (t % PM_STAGES) * STAGE;
+    if (t < tiles) {
+      stage_rows<PM_KT, DP / 8, PM_THREADS>(s, kp, kk.k_s[1] * 2, LD, k0 + t * PM_KT, k1, pieces, tid);
+      stage_rows<PM_KT, DP / 8, PM_THREADS>(s + PM_KT * LD, vp, kk.v_s[1] * 2, LD, k0 + t * PM_KT, k1,
+                                            pieces, tid);
+    }
+    copy_commit();
+  };
+  // the queries pass through the last stage's space
+  unsigned char* sq = sm + (PM_STAGES - 1) * STAGE;
+  for (int i = tid; i < 16 * RB * (DP / 8); i += PM_THREADS) {
+    const int r = r0 + i / (DP / 8), p = i % (DP / 8);
+    const bool live = r < rows && p < pieces;
+    const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q);
+    if (live) {
+      const PaRow w = pa_row(a, kk.own, b, hk, r);
+      src += (int64_t)w.n * a.q_s[0] + (int64_t)w.t * a.q_s[1] + (int64_t)w.h * a.q_s[2] + p * 8;
+    }
+    copy16(sq + (i / (DP / 8)) * LD + p * 16, src, live);
+  }
+  copy_commit();
+#pragma unroll
+  for (int t = 0; t < PM_STAGES - 1; ++t) stage(t);
+  copy_wait<PM_STAGES - 1>();
+  __syncthreads();
+  uint32_t qa[KS][4];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks)
+    ldsm4(sm_addr(sq + (rb * 16 + (lane & 15)) * LD + (ks * 16 + (lane >> 4) * 8) * 2), qa[ks]);
+
+  // the two query rows of this thread, and how many keys each may see
+  const int g = lane >> 2, c = lane & 3;
+  int lim0 = k1, lim1 = k1;
+  if (kk.own) {
+    const int t0 = (r0 + rb * 16 + g) / a.rep, t1 = (r0 + rb * 16 + g + 8) / a.rep;
+    lim0 = min(k1, held - (a.T - 1 - t0));
+    lim1 = min(k1, held - (a.T - 1 - t1));
+  }
+  float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
+  float o[OB][4];
+#pragma unroll
+  for (int i = 0; i < OB; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+
+  for (int t = 0; t < tiles; ++t) {
+    copy_wait<PM_STAGES - 2>();
+    __syncthreads();                               // tile t landed; tile t - 1's space is free
+    stage(t + PM_STAGES - 1);
+    const unsigned char* sk = sm + (t % PM_STAGES) * STAGE + ph * KW * LD;
+    const unsigned char* sv = sk + PM_KT * LD;
+    const int key0 = k0 + t * PM_KT + ph * KW;
+    float s[NB][4];
+#pragma unroll
+    for (int i = 0; i < NB; ++i) s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int nb = 0; nb < NB; nb += 2) {
+        uint32_t bf[4];
+        const int key = nb * 8 + (lane & 7) + ((lane >> 4) << 3);
+        ldsm4(sm_addr(sk + key * LD + (ks * 16 + ((lane >> 3) & 1) * 8) * 2), bf);
+        mma_16x8x16(s[nb], qa[ks], bf[0], bf[1]);
+        mma_16x8x16(s[nb + 1], qa[ks], bf[2], bf[3]);
+      }
+    float b0 = -INFINITY, b1 = -INFINITY;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int key = key0 + nb * 8 + 2 * c + e;
+        s[nb][e] = key < lim0 ? s[nb][e] * a.scale_log2 : -INFINITY;
+        s[nb][2 + e] = key < lim1 ? s[nb][2 + e] * a.scale_log2 : -INFINITY;
+        b0 = fmaxf(b0, s[nb][e]);
+        b1 = fmaxf(b1, s[nb][2 + e]);
+      }
+    b0 = fmaxf(b0, __shfl_xor_sync(0xffffffffu, b0, 1));
+    b0 = fmaxf(b0, __shfl_xor_sync(0xffffffffu, b0, 2));
+    b1 = fmaxf(b1, __shfl_xor_sync(0xffffffffu, b1, 1));
+    b1 = fmaxf(b1, __shfl_xor_sync(0xffffffffu, b1, 2));
+    const float n0 = fmaxf(m0, b0), n1 = fmaxf(m1, b1);
+    // a row that has seen no key yet keeps maximum -inf; its terms are taken against 0
+    const float u0 = n0 == -INFINITY ? 0.f : n0, u1 = n1 == -INFINITY ? 0.f : n1;
+    const float c0 = pa_ex2(m0 - u0), c1 = pa_ex2(m1 - u1);
+    m0 = n0;
+    m1 = n1;
+    l0 *= c0;
+    l1 *= c1;
+#pragma unroll
+    for (int i = 0; i < OB; ++i) {
+      o[i][0] *= c0; o[i][1] *= c0;
+      o[i][2] *= c1; o[i][3] *= c1;
+    }
+    uint32_t pa[NB / 2][4];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      const float p0 = pa_ex2(s[nb][0] - u0), p1 = pa_ex2(s[nb][1] - u0);
+      const float p2 = pa_ex2(s[nb][2] - u1), p3 = pa_ex2(s[nb][3] - u1);
+      l0 += p0 + p1;
+      l1 += p2 + p3;
+      pa[nb >> 1][(nb & 1) * 2] = bf16_pack2(p0, p1);
+      pa[nb >> 1][(nb & 1) * 2 + 1] = bf16_pack2(p2, p3);
+    }
+#pragma unroll
+    for (int ks = 0; ks < NB / 2; ++ks)
+#pragma unroll
+      for (int ob = 0; ob < OB; ob += 2) {
+        uint32_t vf[4];
+        const int key = ks * 16 + (lane & 7) + ((lane >> 3) & 1) * 8;
+        ldsm4_t(sm_addr(sv + key * LD + (ob * 8 + (lane >> 4) * 8) * 2), vf);
+        mma_16x8x16(o[ob], pa[ks], vf[0], vf[1]);
+        mma_16x8x16(o[ob + 1], pa[ks], vf[2], vf[3]);
+      }
+  }
+  l0 += __shfl_xor_sync(0xffffffffu, l0, 1);
+  l0 += __shfl_xor_sync(0xffffffffu, l0, 2);
+  l1 += __shfl_xor_sync(0xffffffffu, l1, 1);
+  l1 += __shfl_xor_sync(0xffffffffu, l1, 2);
+
+  // join the key phases of each row: phase ph > 0 leaves its state in shared memory
+  if constexpr (PH > 1) {
+    copy_wait<0>();
+    __syncthreads();
+    float* xo = reinterpret_cast<float*>(sm);
+    constexpr int XL = DP + 4;
+    float* xm = xo + (size_t)(PH - 1) * RB * 16 * XL;
+    if (ph > 0) {
+      const int row = ((ph - 1) * RB + rb) * 16 + g;
+      if (c == 0) {
+        xm[2 * row] = m0; xm[2 * row + 1] = l0;
+        xm[2 * (row + 8)] = m1; xm[2 * (row + 8) + 1] = l1;
+      }
+#pragma unroll
+      for (int i = 0; i < OB; ++i) {
+        *reinterpret_cast<float2*>(xo + (size_t)row * XL + i * 8 + 2 * c) = make_float2(o[i][0], o[i][1]);
+        *reinterpret_cast<float2*>(xo + (size_t)(row + 8) * XL + i * 8 + 2 * c) =
+            make_float2(o[i][2], o[i][3]);
+      }
+    }
+    __syncthreads();
+    if (ph > 0) return;
+#pragma unroll
+    for (int p = 0; p < PH - 1; ++p) {
+      const int row = (p * RB + rb) * 16 + g;
+      const float pm0 = xm[2 * row], pl0 = xm[2 * row + 1];
+      const float pm1 = xm[2 * (row + 8)], pl1 = xm[2 * (row + 8) + 1];
+      const float n0 = fmaxf(m0, pm0), n1 = fmaxf(m1, pm1);
+      const float u0 = n0 == -INFINITY ? 0.f : n0, u1 = n1 == -INFINITY ? 0.f : n1;
+      const float c0 = pa_ex2(m0 - u0), c1 = pa_ex2(m1 - u1);
+      const float e0 = pa_ex2(pm0 - u0), e1 = pa_ex2(pm1 - u1);
+      m0 = n0; m1 = n1;
+      l0 = l0 * c0 + pl0 * e0;
+      l1 = l1 * c1 + pl1 * e1;
+#pragma unroll
+      for (int i = 0; i < OB; ++i) {
+        const float2 q0 = *reinterpret_cast<const float2*>(xo + (size_t)row * XL + i * 8 + 2 * c);
+        const float2 q1 = *reinterpret_cast<const float2*>(xo + (size_t)(row + 8) * XL + i * 8 + 2 * c);
+        o[i][0] = o[i][0] * c0 + q0.x * e0;
+        o[i][1] = o[i][1] * c0 + q0.y * e0;
+        o[i][2] = o[i][2] * c1 + q1.x * e1;
+        o[i][3] = o[i][3] * c1 + q1.y * e1;
+      }
+    }
+  }
+  const int ra = r0 + rb * 16 + g;
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    const int r = ra + half * 8;
+    if (r >= rows) continue;
+    const size_t at = (size_t)slot * a.rows() + pa_index(a, pa_row(a, kk.own, b, hk, r));
+    if (c == 0) a.ml[at] = half ? make_float2(m1, l1) : make_float2(m0, l0);
+#pragma unroll
+    for (int i = 0; i < OB; ++i)
+      if (i * 8 < a.d)
+        *reinterpret_cast<float2*>(a.po + at * a.d + i * 8 + 2 * c) =
+            half ? make_float2(o[i][2], o[i][3]) : make_float2(o[i][0], o[i][1]);
+  }
+}
+
+// fp32 on the CUDA cores: each of four warps owns four query rows, a lane a key of the stage's 32 for
+// the scores and four columns of V for the sums.
+constexpr int PS_THREADS = 128;
+constexpr int PS_ROWS = 16;
+constexpr int PS_KT = 32;
+constexpr int PS_STAGES = 2;
+
+template <int DP>
+__global__ void __launch_bounds__(PS_THREADS)
+pa_simt_kernel(const PaArgs a, const PaKeys kk, int rows, int blocks) {
+  pdl_wait();
+  constexpr int LD = (DP + 4) * 4;
+  constexpr int STAGE = 2 * PS_KT * LD;
+  extern __shared__ __align__(16) unsigned char sm[];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  int x = blockIdx.x;
+  const int block = x % blocks; x /= blocks;
+  const int hk = x % a.Hkv; x /= a.Hkv;
+  const int b = x % (kk.own ? a.G * a.W : a.G);
+  const int split = x / (kk.own ? a.G * a.W : a.G);
+  const int held = min(max(kk.len[b], 0), kk.capacity);
+  int k0, k1;
+  pa_piece(held, kk.splits, split, k0, k1);
+  const int r0 = block * PS_ROWS;
+  const int slot = kk.slot0 + split;
+  if (k0 >= k1) {
+    for (int r = r0 + tid; r < min(rows, r0 + PS_ROWS); r += PS_THREADS)
+      a.ml[(size_t)slot * a.rows() + pa_index(a, pa_row(a, kk.own, b, hk, r))] =
+          make_float2(-INFINITY, 0.f);
+    return;
+  }
+  const unsigned char* kp = static_cast<const unsigned char*>(kk.k) +
+                            4 * ((int64_t)b * kk.k_s[0] + (int64_t)hk * kk.k_s[2]);
+  const unsigned char* vp = static_cast<const unsigned char*>(kk.v) +
+                            4 * ((int64_t)b * kk.v_s[0] + (int64_t)hk * kk.v_s[2]);
+  const int pieces = a.d / 4, tiles = (k1 - k0 + PS_KT - 1) / PS_KT;
+  float* sq = reinterpret_cast<float*>(sm + PS_STAGES * STAGE);          // [16][DP]
+  auto stage = [&](int t) {
+    unsigned char* s = sm + (t % PS_STAGES) * STAGE;
+    if (t < tiles) {
+      stage_rows<PS_KT, DP / 4, PS_THREADS>(s, kp, kk.k_s[1] * 4, LD, k0 + t * PS_KT, k1, pieces, tid);
+      stage_rows<PS_KT, DP / 4, PS_THREADS>(s + PS_KT * LD, vp, kk.v_s[1] * 4, LD, k0 + t * PS_KT, k1,
+                                            pieces, tid);
+    }
+    copy_commit();
+  };
+  for (int i = tid; i < PS_ROWS * (DP / 4); i += PS_THREADS) {
+    const int r = r0 + i / (DP / 4), p = i % (DP / 4);
+    const bool live = r < rows && p < pieces;
+    const float* src = static_cast<const float*>(a.q);
+    if (live) {
+      const PaRow w = pa_row(a, kk.own, b, hk, r);
+      src += (int64_t)w.n * a.q_s[0] + (int64_t)w.t * a.q_s[1] + (int64_t)w.h * a.q_s[2] + p * 4;
+    }
+    copy16(sq + i * 4, src, live);
+  }
+  stage(0);
+  const int rw = r0 + warp * 4;                   // this warp's first row
+  int lim[4];
+  float m[4], l[4];
+  float4 o[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    lim[i] = kk.own ? min(k1, held - (a.T - 1 - (rw + i) / a.rep)) : k1;
+    m[i] = -INFINITY;
+    l[i] = 0.f;
+    o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  for (int t = 0; t < tiles; ++t) {
+    copy_wait<0>();
+    __syncthreads();
+    stage(t + 1);
+    if (rw >= rows) continue;
+    const unsigned char* sk = sm + (t % PS_STAGES) * STAGE;
+    const unsigned char* sv = sk + PS_KT * LD;
+    const int key = k0 + t * PS_KT + lane;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int p = 0; p < DP / 4; ++p) {
+      const float4 kv = *reinterpret_cast<const float4*>(sk + lane * LD + p * 16);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        s[i] = dot4(*reinterpret_cast<const float4*>(sq + (warp * 4 + i) * DP + p * 4), kv, s[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      s[i] = key < lim[i] ? s[i] * a.scale_log2 : -INFINITY;
+      const float n = fmaxf(m[i], warp_max(s[i]));
+      const float u = n == -INFINITY ? 0.f : n;
+      const float f = pa_ex2(m[i] - u);
+      m[i] = n;
+      s[i] = pa_ex2(s[i] - u);
+      l[i] = l[i] * f + s[i];                     // this lane's share of the sum
+      o[i].x *= f; o[i].y *= f; o[i].z *= f; o[i].w *= f;
+    }
+#pragma unroll 8
+    for (int j = 0; j < PS_KT; ++j) {
+      const float4 v = *reinterpret_cast<const float4*>(sv + j * LD + (lane % (DP / 4)) * 16);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float p = __shfl_sync(0xffffffffu, s[i], j);
+        o[i].x = fmaf(p, v.x, o[i].x);
+        o[i].y = fmaf(p, v.y, o[i].y);
+        o[i].z = fmaf(p, v.z, o[i].z);
+        o[i].w = fmaf(p, v.w, o[i].w);
+      }
+    }
+  }
+  if (rw >= rows) return;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float sum = warp_sum(l[i]);
+    if (rw + i >= rows) continue;
+    const size_t at = (size_t)slot * a.rows() + pa_index(a, pa_row(a, kk.own, b, hk, rw + i));
+    if (lane == 0) a.ml[at] = make_float2(m[i], sum);
+    if (lane < DP / 4 && lane * 4 < a.d) *reinterpret_cast<float4*>(a.po + at * a.d + lane * 4) = o[i];
+  }
+}
+
+// Join a row's pieces: one warp a row, four columns a lane.
+template <typename T>
+__global__ void __launch_bounds__(128)
+pa_combine_kernel(const PaArgs a) {
+  pdl_wait();
+  const int lane = threadIdx.x & 31;
+  const size_t rows = a.rows();
+  const size_t row = (size_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+  if (row >= rows) return;
+  const int h = (int)(row % a.Hq);
+  const size_t nt = row / a.Hq;
+  const int t = (int)(nt % a.T), n = (int)(nt / a.T);
+  if (a.seq_len[n] < 0) return;                   // no such sequence: its rows stay as they are
+  float M = -INFINITY;
+  for (int s = lane; s < a.slots; s += 32) M = fmaxf(M, a.ml[s * rows + row].x);
+  M = warp_max(M);
+  const float u = M == -INFINITY ? 0.f : M;
+  float L = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int s0 = 0; s0 < a.slots; s0 += 32) {
+    const float2 ml = s0 + lane < a.slots ? a.ml[(s0 + lane) * rows + row] : make_float2(-INFINITY, 0.f);
+    const float f = ml.x == -INFINITY ? 0.f : pa_ex2(ml.x - u);
+    L += f * ml.y;
+    for (int j = 0; j < min(32, a.slots - s0); ++j) {
+      const float w = __shfl_sync(0xffffffffu, f, j);
+      const float mx = __shfl_sync(0xffffffffu, ml.x, j);
+      if (mx == -INFINITY || lane * 4 >= a.d) continue;    // no keys: nothing was written
+      const float4 p = *reinterpret_cast<const float4*>(a.po + ((s0 + j) * rows + row) * a.d + lane * 4);
+      o.x = fmaf(w, p.x, o.x);
+      o.y = fmaf(w, p.y, o.y);
+      o.z = fmaf(w, p.z, o.z);
+      o.w = fmaf(w, p.w, o.w);
+    }
+  }
+  L = warp_sum(L);
+  const float inv = L > 0.f ? 1.0f / L : (M == -INFINITY ? 0.f : L);
+  T* out = static_cast<T*>(a.out) + (int64_t)n * a.o_s[0] + (int64_t)t * a.o_s[1] + (int64_t)h * a.o_s[2];
+  if (lane * 4 < a.d) {
+    o.x *= inv; o.y *= inv; o.z *= inv; o.w *= inv;
+    if constexpr (sizeof(T) == 4)
+      *reinterpret_cast<float4*>(out + lane * 4) = o;
+    else
+      *reinterpret_cast<uint2*>(out + lane * 4) = make_uint2(bf16_pack2(o.x, o.y), bf16_pack2(o.z, o.w));
+  }
+  if (lane == 0) a.lse[row] = M == -INFINITY ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+}
+
+int key_sets(const PaArgs& a, const PaKeys& k) { return k.own ? a.G * a.W : a.G; }
+int key_rows(const PaArgs& a, const PaKeys& k) { return (k.own ? 1 : a.W) * a.T * a.rep; }
+
+template <int DP, int RB>
+lilicorr_status_t launch_mma(const PaArgs& a, const PaKeys& k, cudaStream_t st) {
+  static bool configured[64] = {false};
+  LL_TRY(allow_max_dynamic_smem(pa_mma_kernel<DP, RB>, configured));
+  const int rows = key_rows(a, k), blocks = ceil_div(rows, 16 * RB);
+  const size_t smem = (size_t)PM_STAGES * 2 * PM_KT * (DP + 8) * 2;
+  const size_t grid = (size_t)key_sets(a, k) * a.Hkv * blocks * k.splits;
+  if (grid > 0x7FFFFFFFull) return LILICORR_ERR_SHAPE;
+  return launch_k(pa_mma_kernel<DP, RB>, (unsigned)grid, PM_THREADS, smem, st, a, k, rows, blocks);
+}
+
+template <int DP>
+lilicorr_status_t launch_simt(const PaArgs& a, const PaKeys& k, cudaStream_t st) {
+  static bool configured[64] = {false};
+  LL_TRY(allow_max_dynamic_smem(pa_simt_kernel<DP>, configured));
+  const int rows = key_rows(a, k), blocks = ceil_div(rows, PS_ROWS);
+  const size_t smem = (size_t)PS_STAGES * 2 * PS_KT * (DP + 4) * 4 + PS_ROWS * DP * 4;
+  const size_t grid = (size_t)key_sets(a, k) * a.Hkv * blocks * k.splits;
+  if (grid > 0x7FFFFFFFull) return LILICORR_ERR_SHAPE;
+  return launch_k(pa_simt_kernel<DP>, (unsigned)grid, PS_THREADS, smem, st, a, k, rows, blocks);
+}
+
+}  // namespace
+
+lilicorr_status_t launch_pa_mma(const PaArgs& a, const PaKeys& k, cudaStream_t st) {
+  const int rows = key_rows(a, k);
+  if (a.d <= 64) {
+    if (rows <= 16) return launch_mma<64, 1>(a, k, st);
+    if (rows <= 32) return launch_mma<64, 2>(a, k, st);
+    return launch_mma<64, 4>(a, k, st);
+  }
+  if (rows <= 16) return launch_mma<128, 1>(a, k, st);
+  if (rows <= 32) return launch_mma<128, 2>(a, k, st);
+  return launch_mma<128, 4>(a, k, st);
+}
+
+lilicorr_status_t launch_pa_simt(const PaArgs& a, const PaKeys& k, cudaStream_t st) {
+  return a.d <= 64 ? launch_simt<64>(a, k, st) : launch_simt<128>(a, k, st);
+}
+
+lilicorr_status_t launch_pa_combine(const PaArgs& a, lilicorr_dtype_t dt, cudaStream_t st) {
+  const size_t grid = (a.rows() + 3) / 4;
+  if (dt == LILICORR_BF16) return launch_k(pa_combine_kernel<__nv_bfloat16>, (unsigned)grid, 128, 0, st, a);
+  return launch_k(pa_combine_kernel<float>, (unsigned)grid, 128, 0, st, a);
+}
+
+// ---------------------------------------------------------------------------- the call
+namespace {
+
+struct PaPlan {
+  int psplits, ssplits;
+  size_t rows, ml_off, po_off, total;
+};
+
+bool stride_ok(const int64_t (&s)[3], const int (&extent)[3], int per16) {
+  for (int i = 0; i < 3; ++i)
+    if (extent[i] > 1 && (s[i] < 0 || s[i] % per16 || s[i] > (1ll << 40))) return false;
+  return true;
+}
+
+bool pa_plan(const lilicorr_prefix_attention_desc* d, PaPlan* p) {
+  if (!d || (d->dtype != LILICORR_F32 && d->dtype != LILICORR_BF16)) return false;
+  if (d->groups < 0 || d->beams < 1 || d->tokens < 1 || d->q_heads < 1 || d->kv_heads < 1) return false;
+  if (d->q_heads % d->kv_heads || d->head_dim < 8 || d->head_dim > 128 || d->head_dim % 8) return false;
+  if (d->prefix_capacity < 0 || d->own_capacity < 0) return false;
+  if (d->prefix_capacity > (1 << 30) || d->own_capacity > (1 << 30)) return false;
+  const double rows = (double)d->groups * d->beams * d->tokens * d->q_heads;
+  if (rows >= 2147483648.0 || (double)d->groups * d->beams * d->kv_heads >= 2147483648.0) return false;
+  const int sms = num_sms();
+  const int rep = d->q_heads / d->kv_heads;
+  // pieces of a key range: about four CTAs an SM over all ranges, none below 256 keys
+  auto pieces = [&](long long ranges, int cap) {
+    const long long want = ranges > 0 ? (4ll * sms + ranges - 1) / ranges : 1;
+    const long long most = (cap + 255) / 256;
+    long long n = want < most ? want : most;
+    return (int)(n < 1 ? 1 : n > 128 ? 128 : n);
+  };
+  const long long prow = (long long)d->beams * d->tokens * rep;
+  p->psplits = d->prefix_capacity
+                   ? pieces((long long)d->groups * d->kv_heads * ((prow + 63) / 64), d->prefix_capacity)
+                   : 0;
+  p->ssplits = d->own_capacity ? pieces((long long)d->groups * d->beams * d->kv_heads, d->own_capacity) : 0;
+  p->rows = (size_t)rows;
+  const size_t slots = (size_t)p->psplits + p->ssplits;
+  p->ml_off = 256;
+  p->po_off = p->ml_off + align_up(slots * p->rows * sizeof(float2), 256);
+  p->total = p->po_off + align_up(slots * p->rows * d->head_dim * sizeof(float), 256);
+  return true;
+}
+
+}  // namespace
+}  // namespace lilicorr
+
+using namespace lilicorr;
+
+extern "C" {
+
+size_t lilicorr_prefix_attention_workspace_bytes(const lilicorr_prefix_attention_desc* desc) {
+  PaPlan p;
+  return pa_plan(desc, &p) ? p.total : 0;
+}
+
+lilicorr_status_t lilicorr_prefix_attention(const lilicorr_prefix_attention_desc* desc, const void* q,
+                                            const void* prefix_k, const void* prefix_v,
+                                            const int32_t* prefix_len, const void* k, const void* v,
+                                            const int32_t* seq_len, void* out, float* lse, void* ws,
+                                            size_t ws_bytes, cudaStream_t stream) {
+  if (!desc) return LILICORR_ERR_ARG;
+  if (desc->dtype != LILICORR_F32 && desc->dtype != LILICORR_BF16) return LILICORR_ERR_DTYPE;
+  PaPlan p;
+  if (!pa_plan(desc, &p)) return LILICORR_ERR_SHAPE;
+  if (!(desc->scale > 0.f) || !(desc->scale < INFINITY)) return LILICORR_ERR_ARG;
+  if (desc->groups == 0) return LILICORR_OK;
+  const bool has_p = desc->prefix_capacity > 0, has_s = desc->own_capacity > 0;
+  if (!q || !out || !lse || !ws || !seq_len) return LILICORR_ERR_ARG;
+  if (has_p && (!prefix_k || !prefix_v || !prefix_len)) return LILICORR_ERR_ARG;
+  if (has_s && (!k || !v)) return LILICORR_ERR_ARG;
+  if (!aligned16(q) || !aligned16(out) || !aligned16(ws)) return LILICORR_ERR_ARG;
+  if (has_p && (!aligned16(prefix_k) || !aligned16(prefix_v))) return LILICORR_ERR_ARG;
+  if (has_s && (!aligned16(k) || !aligned16(v))) return LILICORR_ERR_ARG;
+  const int N = desc->groups * desc->beams, per16 = desc->dtype == LILICORR_BF16 ? 8 : 4;
+  const int rows_e[3] = {N, desc->tokens, desc->q_heads};
+  const int pre_e[3] = {desc->groups, desc->prefix_capacity, desc->kv_heads};
+  const int own_e[3] = {N, desc->own_capacity, desc->kv_heads};
+  if (!stride_ok(desc->q_stride, rows_e, per16) || !stride_ok(desc->out_stride, rows_e, per16) ||
+      (has_p && (!stride_ok(desc->prefix_k_stride, pre_e, per16) ||
+                 !stride_ok(desc->prefix_v_stride, pre_e, per16))) ||
+      (has_s && (!stride_ok(desc->k_stride, own_e, per16) || !stride_ok(desc->v_stride, own_e, per16))))
+    return LILICORR_ERR_ARG;
+  if (ws_bytes < p.total) return LILICORR_ERR_WORKSPACE;
+
+  unsigned char* w = static_cast<unsigned char*>(ws);
+  PaArgs a;
+  memset(&a, 0, sizeof(a));
+  a.q = q;
+  a.out = out;
+  a.lse = lse;
+  a.seq_len = seq_len;
+  a.G = desc->groups; a.W = desc->beams; a.T = desc->tokens;
+  a.Hq = desc->q_heads; a.Hkv = desc->kv_heads; a.rep = desc->q_heads / desc->kv_heads;
+  a.d = desc->head_dim;
+  a.scale_log2 = desc->scale * PA_LOG2E;
+  a.slots = p.psplits + p.ssplits;
+  a.status = reinterpret_cast<uint32_t*>(w);
+  a.ml = reinterpret_cast<float2*>(w + p.ml_off);
+  a.po = reinterpret_cast<float*>(w + p.po_off);
+  PaKeys pre, own;
+  memset(&pre, 0, sizeof(pre));
+  memset(&own, 0, sizeof(own));
+  for (int i = 0; i < 3; ++i) {                    // a dimension of one has no stride to speak of
+    a.q_s[i] = rows_e[i] > 1 ? desc->q_stride[i] : 0;
+    a.o_s[i] = rows_e[i] > 1 ? desc->out_stride[i] : 0;
+    pre.k_s[i] = pre_e[i] > 1 ? desc->prefix_k_stride[i] : 0;
+    pre.v_s[i] = pre_e[i] > 1 ? desc->prefix_v_stride[i] : 0;
+    own.k_s[i] = own_e[i] > 1 ? desc->k_stride[i] : 0;
+    own.v_s[i] = own_e[i] > 1 ? desc->v_stride[i] : 0;
+  }
+  pre.k = prefix_k; pre.v = prefix_v; pre.len = prefix_len;
+  pre.capacity = desc->prefix_capacity; pre.splits = p.psplits; pre.slot0 = 0; pre.own = 0;
+  own.k = k; own.v = v; own.len = seq_len;
+  own.capacity = desc->own_capacity; own.splits = p.ssplits; own.slot0 = p.psplits; own.own = 1;
+  const bool bf = desc->dtype == LILICORR_BF16;
+  if (has_p) LL_TRY(bf ? launch_pa_mma(a, pre, stream) : launch_pa_simt(a, pre, stream));
+  if (has_s) LL_TRY(bf ? launch_pa_mma(a, own, stream) : launch_pa_simt(a, own, stream));
+  return launch_pa_combine(a, desc->dtype, stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,68 @@
+// Attention of sequences that share their request's prefix: what its kernels have in common.
+#pragma once
+
+#include "internal.cuh"
+
+namespace lilicorr {
+
+// One side of the keys: the prefix of each group (shared by its sequences), or each sequence's own.
+struct PaKeys {
+  const void* k;
+  const void* v;
+  int64_t k_s[3], v_s[3];      // strides in elements: group or sequence, position, head
+  const int32_t* len;          // [groups] or [sequences]
+  int capacity;
+  int splits;                  // pieces that each key range is cut into
+  int slot0;                   // first partial slot
+  int own;                     // 0: prefix, 1: the sequences' own keys (causal over the T tokens)
+};
+
+struct PaArgs {
+  const void* q;
+  int64_t q_s[3];              // sequence, token, head
+  void* out;
+  int64_t o_s[3];
+  float* lse;                  // [N, T, Hq]
+  const int32_t* seq_len;      // [N]
+  int G, W, T, Hq, Hkv, rep, d;
+  float scale_log2;            // scale * log2(e): scores in log2 units
+  int slots;                   // partial results per row
+  float2* ml;                  // [slots][rows] (maximum, sum of 2^(s - maximum)); maximum -inf: none
+  float* po;                   // [slots][rows][d] sums of 2^(s - maximum) V
+  uint32_t* status;
+  __device__ __host__ size_t rows() const { return (size_t)G * W * T * Hq; }
+};
+
+constexpr float PA_LOG2E = 1.4426950408889634f;
+
+// Rows that share a key range: (sequence of the group, token, query head of the key head), in that
+// order. Row r of (group or sequence b, key head h) as (sequence, token, query head).
+struct PaRow { int n, t, h; };
+__device__ __forceinline__ PaRow pa_row(const PaArgs& a, int own, int b, int hk, int r) {
+  const int per = a.T * a.rep, w = own ? 0 : r / per, in = own ? r : r - w * per;
+  PaRow x;
+  x.n = own ? b : b * a.W + w;
+  x.t = in / a.rep;
+  x.h = hk * a.rep + (in - x.t * a.rep);
+  return x;
+}
+__device__ __forceinline__ size_t pa_index(const PaArgs& a, const PaRow& x) {
+  return ((size_t)x.n * a.T + x.t) * a.Hq + x.h;
+}
+// Piece `split` of a key range of length len: [k0, k1), starts at multiples of 64.
+__device__ __forceinline__ void pa_piece(int len, int splits, int split, int& k0, int& k1) {
+  const int chunk = ((len + splits - 1) / splits + 63) / 64 * 64;
+  k0 = min((long long)len, (long long)split * chunk);
+  k1 = min((long long)len, (long long)k0 + chunk);
+}
+__device__ __forceinline__ float pa_ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+lilicorr_status_t launch_pa_mma(const PaArgs& a, const PaKeys& k, cudaStream_t st);
+lilicorr_status_t launch_pa_simt(const PaArgs& a, const PaKeys& k, cudaStream_t st);
+lilicorr_status_t launch_pa_combine(const PaArgs& a, lilicorr_dtype_t dt, cudaStream_t st);
+
+}  // namespace lilicorr
