@@ -14,6 +14,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Dict, Mapping, Optional, Sequence, Tuple
 
 import numpy as np
@@ -95,8 +96,8 @@ _SIGS = {
                                  _P]),
     "lilicorr_beam_reorder": (_I, [ctypes.POINTER(_P), _I, _I, _I, _I, _I, _S] +
                               [ctypes.c_int64] * 4 + [_P, _P, _P]),
-    "lilicorr_prefix_attention_workspace_bytes": (_S, [ctypes.POINTER(PrefixAttentionDesc)]),
-    "lilicorr_prefix_attention": (_I, [ctypes.POINTER(PrefixAttentionDesc)] + [_P] * 10 + [_S, _P]),
+    "lilicorr_prefix_attention_workspace_bytes": (_S, [_P]),
+    "lilicorr_prefix_attention": (_I, [_P] * 11 + [_S, _P]),
     "lilicorr_test_linear": (_I, [_P, _I, _I, _P, _I, _I, _P, _I, _I, _I, _I, _I, _P, _P, _I, _I,
                                   _P, _P]),
     "lilicorr_test_linear_timeout": (_I, [_P, _P, _P, _I, _I, _I, ctypes.c_longlong, _P, _P]),
@@ -127,7 +128,15 @@ def _check(status: int, where: str) -> None:
         raise LilicorrError(status, where)
 
 
+try:                               # the current stream's handle without a Stream object (0.1 us, not 2.9)
+    _raw_stream = torch._C._cuda_getCurrentRawStream
+except AttributeError:             # a torch built without CUDA, or without this entry
+    _raw_stream = None
+
+
 def _stream() -> int:
+    if _raw_stream is not None:
+        return _raw_stream(torch.cuda.current_device())
     return torch.cuda.current_stream().cuda_stream
 
 
@@ -143,15 +152,17 @@ def _dev(t: torch.Tensor, name: str) -> torch.Tensor:
     return t
 
 
-def _here(t: torch.Tensor, name: str, dtype: Optional[torch.dtype] = None,
-          shape: Optional[Tuple[int, ...]] = None) -> torch.Tensor:
-    """``t`` on the current device, of that type and shape (strides are the caller's matter)."""
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+def _here(t: torch.Tensor, name: str, dev: int, dtype: Optional[torch.dtype] = None,
+          shape: Optional[Tuple[int, ...]] = None, dense: bool = False) -> torch.Tensor:
+    """``t`` on the current device ``dev``, of that type and shape, contiguous if ``dense``."""
+    if t.get_device() != dev:
         raise ValueError(f"{name} must be a CUDA tensor on the current device")
-    if dtype is not None and t.dtype != dtype:
+    if dtype is not None and t.dtype is not dtype:
         raise ValueError(f"{name} must be {dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if dense and not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
     return t
 
 
@@ -516,18 +527,17 @@ def select_block(head: Head, logits: torch.Tensor, hidden: torch.Tensor, target:
 
 
 # --------------------------------------------------------------------------- beams
-def _beam_args(scores: torch.Tensor, done: Optional[torch.Tensor], R: int, W: int, n: int):
-    _dev(_here(scores, "scores", torch.float32, (R, W)), "scores")
+def _beam_args(dev: int, scores: torch.Tensor, done: Optional[torch.Tensor], R: int, W: int, n: int):
+    _here(scores, "scores", dev, torch.float32, (R, W), True)
     if done is not None:
-        if done.dtype not in (torch.bool, torch.uint8):
+        if done.dtype is not torch.bool and done.dtype is not torch.uint8:
             raise ValueError("done must be bool or uint8")
-        _dev(_here(done, "done", None, (R, W)), "done")
-    dev = scores.device
-    n = max(int(n), 0)
-    return (torch.empty((R, n), dtype=torch.int32, device=dev),
-            torch.empty((R, n), dtype=torch.int32, device=dev),
-            torch.empty((R, n), dtype=torch.float32, device=dev),
-            torch.empty((R, n), dtype=torch.bool, device=dev))
+        _here(done, "done", dev, None, (R, W), True)
+    shape, on = (R, max(n, 0)), scores.device
+    return (torch.empty(shape, dtype=torch.int32, device=on),
+            torch.empty(shape, dtype=torch.int32, device=on),
+            torch.empty(shape, dtype=torch.float32, device=on),
+            torch.empty(shape, dtype=torch.bool, device=on))
 
 
 def beam_select_workspace_bytes(requests: int, beams: int, V: int, n: int) -> int:
@@ -544,15 +554,17 @@ def beam_select(logits: torch.Tensor, scores: torch.Tensor, n: int,
     beams that are ``done`` [R, W] keep their score and offer ``end_id`` (see lilicorr.h)."""
     if logits.dim() != 3:
         raise ValueError("logits must be [requests, beams, V]")
-    _dev(_here(logits, "logits"), "logits")
+    dev = torch.cuda.current_device()
+    _here(logits, "logits", dev, dense=True)
     R, W, V = logits.shape
-    out = _beam_args(scores, done, R, W, n)
+    n = int(n)
+    tokens, parents, best, over = out = _beam_args(dev, scores, done, R, W, n)
     if ws is None:
         ws = Workspace(beam_select_workspace_bytes(R, W, V, n), logits.device)
-    _check(lib().lilicorr_beam_select(logits.data_ptr(), _dtype_code(logits), R, W, V, int(n),
-                                      scores.data_ptr(), _ptr(done), int(end_id),
-                                      *(t.data_ptr() for t in out), ws.ptr, ws.nbytes, _stream()),
-           "beam_select")
+    _check(lib().lilicorr_beam_select(logits.data_ptr(), _dtype_code(logits), R, W, V, n,
+                                      scores.data_ptr(), _ptr(done), end_id, tokens.data_ptr(),
+                                      parents.data_ptr(), best.data_ptr(), over.data_ptr(), ws.ptr,
+                                      ws.nbytes, _stream()), "beam_select")
     return out
 
 
@@ -563,13 +575,17 @@ def beam_merge(ids: torch.Tensor, logp: torch.Tensor, scores: torch.Tensor, n: i
     lm_head_topk or topk_lse_merge): the exact beam search step where K >= min(n, V)."""
     if ids.dim() != 3:
         raise ValueError("ids must be [requests, beams, K]")
-    R, W, K = ids.shape
-    _dev(_here(ids, "ids", torch.int32), "ids")
-    _dev(_here(logp, "logp", torch.float32, (R, W, K)), "logp")
-    out = _beam_args(scores, done, R, W, n)
-    _check(lib().lilicorr_beam_merge(ids.data_ptr(), logp.data_ptr(), R, W, K, int(n),
-                                     scores.data_ptr(), _ptr(done), int(end_id),
-                                     *(t.data_ptr() for t in out), _ptr(status), _stream()),
+    dev = torch.cuda.current_device()
+    R, W, K = shape = ids.shape
+    n = int(n)
+    _here(ids, "ids", dev, torch.int32, None, True)
+    _here(logp, "logp", dev, torch.float32, shape, True)
+    if status is not None:
+        _here(status, "status", dev)
+    tokens, parents, best, over = out = _beam_args(dev, scores, done, R, W, n)
+    _check(lib().lilicorr_beam_merge(ids.data_ptr(), logp.data_ptr(), R, W, K, n, scores.data_ptr(),
+                                     _ptr(done), end_id, tokens.data_ptr(), parents.data_ptr(),
+                                     best.data_ptr(), over.data_ptr(), _ptr(status), _stream()),
            "beam_merge")
     return out
 
@@ -601,13 +617,20 @@ def beam_reorder(states, parents: torch.Tensor, lengths: Optional[torch.Tensor] 
     if parents.dim() != 2:
         raise ValueError("parents must be [requests, beams]")
     R, W = parents.shape
-    _dev(_here(parents, "parents", torch.int32), "parents")
+    dev = torch.cuda.current_device()
+    _here(parents, "parents", dev, torch.int32, None, True)
     if lengths is not None:
-        _dev(_here(lengths, "lengths", torch.int32, (R,)), "lengths")
+        _here(lengths, "lengths", dev, torch.int32, (R,), True)
+    # arrays of one layout go together
     groups: Dict[tuple, list] = {}
+    layouts: Dict[tuple, tuple] = {}
     for i, t in enumerate(tensors):
-        _here(t, f"states[{i}]")
-        groups.setdefault(_state_layout(t, R, W, f"states[{i}]"), []).append(t.data_ptr())
+        _here(t, f"states[{i}]", dev)
+        key = (t.shape, t.stride(), t.dtype)
+        layout = layouts.get(key)
+        if layout is None:
+            layout = layouts[key] = _state_layout(t, R, W, f"states[{i}]")
+        groups.setdefault(layout, []).append(t.data_ptr())
     for (positions, heads, row, *strides), ptrs in groups.items():
         _check(lib().lilicorr_beam_reorder((_P * len(ptrs))(*ptrs), len(ptrs), R, W, positions, heads,
                                            row, *strides, parents.data_ptr(), _ptr(lengths),
@@ -616,23 +639,25 @@ def beam_reorder(states, parents: torch.Tensor, lengths: Optional[torch.Tensor] 
 
 
 # --------------------------------------------------------------------------- shared prefixes
-def _attention_desc(q: torch.Tensor, prefix_k: torch.Tensor, k: torch.Tensor,
-                    scale: Optional[float]) -> PrefixAttentionDesc:
+_PA_DESC = struct.Struct("9if18q")          # the layout of lilicorr_prefix_attention_desc
+_NO_STRIDES = (0,) * 18
+
+
+def _attention_desc(q: torch.Tensor, prefix_k: torch.Tensor, k: torch.Tensor, scale: float,
+                    strides=_NO_STRIDES) -> bytes:
     if q.dim() != 4 or prefix_k.dim() != 4 or k.dim() != 4:
         raise ValueError("q is [N, T, q_heads, d], caches are [groups or N, capacity, kv_heads, d]")
     N, T, Hq, d = q.shape
     G, P, Hkv, _ = prefix_k.shape
     if N % max(G, 1) or (G == 0 and N):
         raise ValueError(f"{N} sequences do not divide into {G} groups")
-    x = PrefixAttentionDesc(G, N // G if G else 1, T, Hq, Hkv, d, P, k.shape[1], _dtype_code(q),
-                            d ** -0.5 if scale is None and d else float(scale or 0.0))
-    return x
+    return _PA_DESC.pack(G, N // G if G else 1, T, Hq, Hkv, d, P, k.shape[1], _dtype_code(q), scale,
+                         *strides)
 
 
 def prefix_attention_workspace_bytes(q: torch.Tensor, prefix_k: torch.Tensor, k: torch.Tensor) -> int:
     """Bytes of the workspace that prefix_attention needs for tensors of these shapes."""
-    return int(lib().lilicorr_prefix_attention_workspace_bytes(
-        ctypes.byref(_attention_desc(q, prefix_k, k, 1.0))))
+    return int(lib().lilicorr_prefix_attention_workspace_bytes(_attention_desc(q, prefix_k, k, 1.0)))
 
 
 def prefix_attention(q: torch.Tensor, prefix_k: torch.Tensor, prefix_v: torch.Tensor, k: torch.Tensor,
@@ -645,30 +670,33 @@ def prefix_attention(q: torch.Tensor, prefix_k: torch.Tensor, prefix_v: torch.Te
     T newest included (causal among them) -> (out like q, lse [N, T, q_heads] fp32). fp32 or bf16, any
     strides that keep 16-byte rows. seq_len < 0: no such sequence, its rows of ``out`` and ``lse``
     stay as they are. scale defaults to 1 / sqrt(d)."""
-    x = _attention_desc(q, prefix_k, k, scale)
-    N, T, Hq, d = q.shape
-    G, P, Hkv, _ = prefix_k.shape
-    S = k.shape[1]
+    if q.dim() != 4 or prefix_k.dim() != 4 or k.dim() != 4:
+        raise ValueError("q is [N, T, q_heads, d], caches are [groups or N, capacity, kv_heads, d]")
+    dev, dt = torch.cuda.current_device(), q.dtype
+    N, T, Hq, d = qs = q.shape
+    G, P, Hkv, _ = ps = prefix_k.shape
+    ks = k.shape
+    if ks[0] != N or ks[2] != Hkv or ks[3] != d or ps[3] != d:
+        raise ValueError(f"caches {tuple(ps)} and {tuple(ks)} do not go with q {tuple(qs)}")
     if out is None:
-        out = torch.empty((N, T, Hq, d), dtype=q.dtype, device=q.device)
+        out = torch.empty(qs, dtype=dt, device=q.device)
     if lse is None:
         lse = torch.empty((N, T, Hq), dtype=torch.float32, device=q.device)
-    for t, name, shape, strides in ((q, "q", (N, T, Hq, d), x.q_stride),
-                                    (out, "out", (N, T, Hq, d), x.out_stride),
-                                    (prefix_k, "prefix_k", (G, P, Hkv, d), x.prefix_k_stride),
-                                    (prefix_v, "prefix_v", (G, P, Hkv, d), x.prefix_v_stride),
-                                    (k, "k", (N, S, Hkv, d), x.k_stride),
-                                    (v, "v", (N, S, Hkv, d), x.v_stride)):
-        _here(t, name, q.dtype, shape)
-        if t.numel() and d > 1 and t.stride(3) != 1:
+    strides: list = []
+    for t, name, shape in ((q, "q", qs), (out, "out", qs), (prefix_k, "prefix_k", ps),
+                           (prefix_v, "prefix_v", ps), (k, "k", ks), (v, "v", ks)):
+        _here(t, name, dev, dt, shape)
+        a, b, c, one = t.stride()
+        if one != 1 and d > 1 and t.numel():
             raise ValueError(f"{name}: the last dimension must be dense")
-        strides[:] = t.stride()[:3]
-    _dev(_here(lse, "lse", torch.float32, (N, T, Hq)), "lse")
-    _dev(_here(prefix_len, "prefix_len", torch.int32, (G,)), "prefix_len")
-    _dev(_here(seq_len, "seq_len", torch.int32, (N,)), "seq_len")
+        strides += (a, b, c)
+    _here(lse, "lse", dev, torch.float32, (N, T, Hq), True)
+    _here(prefix_len, "prefix_len", dev, torch.int32, (G,), True)
+    _here(seq_len, "seq_len", dev, torch.int32, (N,), True)
+    desc = _attention_desc(q, prefix_k, k, scale if scale is not None else max(d, 1) ** -0.5, strides)
     if ws is None:
-        ws = Workspace(int(lib().lilicorr_prefix_attention_workspace_bytes(ctypes.byref(x))), q.device)
-    _check(lib().lilicorr_prefix_attention(ctypes.byref(x), q.data_ptr(), prefix_k.data_ptr(),
+        ws = Workspace(int(lib().lilicorr_prefix_attention_workspace_bytes(desc)), q.device)
+    _check(lib().lilicorr_prefix_attention(desc, q.data_ptr(), prefix_k.data_ptr(),
                                            prefix_v.data_ptr(), prefix_len.data_ptr(), k.data_ptr(),
                                            v.data_ptr(), seq_len.data_ptr(), out.data_ptr(),
                                            lse.data_ptr(), ws.ptr, ws.nbytes, _stream()),

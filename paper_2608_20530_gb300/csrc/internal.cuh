@@ -260,14 +260,6 @@ lilicorr_status_t launch_topk_lse(const void* logits, lilicorr_dtype_t dt, int r
                                   void* partial_out = nullptr, int32_t id_offset = 0);
 // bytes of one row's partial record: max, sum, K values, K ids
 __host__ __device__ constexpr size_t topk_partial_bytes(int K) { return 8 + 8 * (size_t)K; }
-// Beams (beam.cu): the top-K pass over the rows of live beams, its normalisers in 64 bits, one
-// record a live row: lse (double), K values, K ids (-1: none). ws: beam_rows_ws_bytes, zero-filled
-// once.
-__host__ __device__ constexpr size_t beam_record_bytes(int K) { return 8 + 8 * (size_t)K; }
-size_t beam_rows_ws_bytes(int rows, int V, int K, lilicorr_dtype_t dt);
-lilicorr_status_t launch_beam_rows(const void* logits, lilicorr_dtype_t dt, int rows, int V, int K,
-                                   const float* scores, const uint8_t* done, void* records,
-                                   uint32_t* status, void* ws, cudaStream_t st);
 // the merge holds P*K keys (and as many survivors) in shared memory
 constexpr int TOPK_MERGE_KEYS_MAX = 8192;
 

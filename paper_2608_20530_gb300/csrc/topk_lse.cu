@@ -26,7 +26,6 @@
 //     row the last CTA to finish (atomic ticket, no waiting) merges the splits'
 //     partial (max, sum, top-K) records and writes ids, logp and lse.
 #include <mutex>
-#include <type_traits>
 
 #include "internal.cuh"
 
@@ -141,68 +140,8 @@ __device__ void cta_select(const uint64_t* groups, int ngroups, int stride, int 
   csync<NT>();
 }
 
-// A thread's running sum of exponentials. Lse is (max, sum of exp below it) in fp32. LseWide is
-// for sums that are compared with another row's (beams): its reference is a whole power of two, so
-// that a rescale is exact, the exponents' arguments x log2(e) - e carry log2(e) in two parts, and
-// the sum a compensation term; what is left is the rounding of each term (relative 2^-22 or so, of
-// either sign), 1e-8 of the sum over a vocabulary.
-struct Lse {
-  static constexpr bool WIDE = false;
-  float m = -INFINITY, s = 0.f;
-};
-struct LseWide {
-  static constexpr bool WIDE = true;
-  float m = -INFINITY;                  // the largest value seen
-  float s = 0.f, c = 0.f;               // the sum in units of 2^e, and what its additions lost
-  float e = -INFINITY;                  // ceil(m log2(e))
-};
-// log2(e) - LOG2E
-constexpr float LOG2E_LO = 1.92596299e-8f;
-
-// 2^d of a whole number d <= 0 (0 below the normal range and for -inf)
-__device__ __forceinline__ float pow2_whole(float d) {
-  return d < -126.f ? 0.f : __int_as_float((127 + (int)d) << 23);
-}
-__device__ __forceinline__ void wide_raise(LseWide& a, float vmax) {
-  a.m = vmax;
-  const float e = ceilf(vmax * LOG2E);
-  if (e > a.e) {
-    const float f = a.e == -INFINITY ? 0.f : pow2_whole(a.e - e);
-    a.s *= f;
-    a.c *= f;
-    a.e = e;
-  }
-}
-__device__ __forceinline__ void wide_add(LseWide& a, float b) {
-  const float t = a.s + b, bb = t - a.s;
-  a.c += (a.s - (t - bb)) + (b - bb);
-  a.s = t;
-}
-// The exponent that arguments are taken against: 0 while only -inf (or NaN) was seen, so that
-// -inf adds 0 and NaN stays NaN.
-__device__ __forceinline__ float wide_ref(float e) { return e == -INFINITY ? 0.f : e; }
-// The warp's sum in units of 2^E, E the lanes' largest exponent (returned in e_out), in 64 bits.
-// Lanes without one (e -inf) hold 0, or NaN if they met NaN.
-__device__ __forceinline__ double wide_warp_sum(float e, double s, float& e_out) {
-  e_out = warp_max(e);
-  double v = e == -INFINITY ? s : s * (double)pow2_whole(e - e_out);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(FULL, v, o);
-  return v;
-}
-
 template <int N>
-__device__ __forceinline__ float lse_update(LseWide& a, const float (&x)[N], bool valid) {
-  static_assert(N == 1, "one value at a time");
-  if (!valid) return -INFINITY;
-  if (x[0] > a.m) wide_raise(a, x[0]);
-  wide_add(a, ex2(fmaf(x[0], LOG2E_LO, fmaf(x[0], LOG2E, -wide_ref(a.e)))));
-  return x[0];
-}
-
-template <int N>
-__device__ __forceinline__ float lse_update(Lse& a, const float (&x)[N], bool valid) {
-  float &m = a.m, &s = a.s;
+__device__ __forceinline__ float lse_update(float& m, float& s, const float (&x)[N], bool valid) {
   float vmax = x[0];
 #pragma unroll
   for (int j = 1; j < N; ++j) vmax = fmaxf(vmax, x[j]);
@@ -410,21 +349,16 @@ __device__ __forceinline__ void load_batch(const uint4* __restrict__ vp, int it,
 
 // The sum of exp(x - m) over one 16-byte vector, added into two packed accumulators (the
 // values are unpacked pair by pair, so the raw words stay the only copy in registers).
-// WIDE: the arguments as LseWide takes them.
-template <typename T, bool WIDE>
+template <typename T>
 __device__ __forceinline__ void exp_vec(const uint4& r, uint64_t l2, uint64_t nm, uint64_t& a0,
                                         uint64_t& a1) {
   const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-  auto arg = [&](uint64_t x) {
-    const uint64_t t = fma2(x, l2, nm);
-    if constexpr (WIDE) return fma2(x, pack2(LOG2E_LO, LOG2E_LO), t);
-    else return t;
-  };
   if constexpr (sizeof(T) == 2) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       float t0, t1;
-      unpack2(arg(pack2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u))), t0, t1);
+      unpack2(fma2(pack2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u)), l2, nm),
+              t0, t1);
       const uint64_t e = pack2(ex2(t0), ex2(t1));
       if (i & 1) a1 = add2(a1, e); else a0 = add2(a0, e);
     }
@@ -432,7 +366,7 @@ __device__ __forceinline__ void exp_vec(const uint4& r, uint64_t l2, uint64_t nm
 #pragma unroll
     for (int i = 0; i < 4; i += 2) {
       float t0, t1;
-      unpack2(arg(pack2(__uint_as_float(w[i]), __uint_as_float(w[i + 1]))), t0, t1);
+      unpack2(fma2(pack2(__uint_as_float(w[i]), __uint_as_float(w[i + 1])), l2, nm), t0, t1);
       const uint64_t e = pack2(ex2(t0), ex2(t1));
       if ((i >> 1) & 1) a1 = add2(a1, e); else a0 = add2(a0, e);
     }
@@ -442,12 +376,11 @@ __device__ __forceinline__ void exp_vec(const uint4& r, uint64_t l2, uint64_t nm
 // Reduce one loaded batch: the online (max, sum exp) with one rescale check per batch, then
 // the candidates, which the warp looks at only if some lane's batch maximum reaches the
 // bound. s_wtop[warp]: the warps' published r-th largest lane maxima (r = ceil(K / warps)).
-template <typename T, int NT, int U, bool CHECK, class Acc>
+template <typename T, int NT, int U, bool CHECK>
 __device__ __forceinline__ void process_batch(const uint4 (&raw)[U], int it, int v_lo,
                                               int v_end, uint32_t id_base, int K, int tid, int lane,
-                                              Acc& acc, WarpCand& w,
+                                              float& m, float& s, WarpCand& w,
                                               uint32_t* s_cta_thr, float* s_wtop) {
-  float &m = acc.m, &s = acc.s;
   constexpr int VEC = Vec<T>::N;
   float vmx[U];
   float bmax = -INFINITY;
@@ -458,26 +391,19 @@ __device__ __forceinline__ void process_batch(const uint4 (&raw)[U], int it, int
   }
   // online log-sum-exp, one rescale per batch (rarely taken after the first batches)
   if (bmax > m) {
-    if constexpr (Acc::WIDE) {
-      wide_raise(acc, bmax);
-    } else {
-      s *= ex2((m - bmax) * LOG2E);
-      m = bmax;
-    }
+    s *= ex2((m - bmax) * LOG2E);
+    m = bmax;
   }
-  if (Acc::WIDE || m != -INFINITY) {
-    float ml;
-    if constexpr (Acc::WIDE) ml = wide_ref(acc.e);
-    else ml = m * LOG2E;
+  if (m != -INFINITY) {
+    const float ml = m * LOG2E;
     const uint64_t l2 = pack2(LOG2E, LOG2E), nm = pack2(-ml, -ml);
     uint64_t a0 = pack2(0.f, 0.f), a1 = a0;
 #pragma unroll
-    for (int u = 0; u < U; ++u) exp_vec<T, Acc::WIDE>(raw[u], l2, nm, a0, a1);
+    for (int u = 0; u < U; ++u) exp_vec<T>(raw[u], l2, nm, a0, a1);
     float p0, p1, p2, p3;
     unpack2(a0, p0, p1);
     unpack2(a1, p2, p3);
-    if constexpr (Acc::WIDE) wide_add(acc, (p0 + p1) + (p2 + p3));
-    else s += (p0 + p1) + (p2 + p3);
+    s += (p0 + p1) + (p2 + p3);
   }
   // candidates: only when some lane's batch maximum reaches the current filter
   w.thr = fmaxf(w.thr, unord32(*(volatile uint32_t*)s_cta_thr));
@@ -525,10 +451,11 @@ __device__ __forceinline__ void process_batch(const uint4 (&raw)[U], int it, int
 // Stream vectors [v_begin, v_end) through process_batch with the next batch's loads in
 // flight while the current one is reduced; full batches in the loop, the ragged last one
 // after it.
-template <typename T, int NT, int U, class Acc>
+template <typename T, int NT, int U>
 __device__ __forceinline__ void stream_chunk(const uint4* __restrict__ vp, int v_begin, int v_end,
-                                             uint32_t id_base, int K, int tid, int lane, Acc& acc,
-                                             WarpCand& w, uint32_t* s_cta_thr, float* s_wtop) {
+                                             uint32_t id_base, int K, int tid, int lane, float& m,
+                                             float& s, WarpCand& w, uint32_t* s_cta_thr,
+                                             float* s_wtop) {
   constexpr int STEP = U * NT;
   const int full_end = v_begin + (v_end - v_begin) / STEP * STEP;
   uint4 cur[U], nxt[U];
@@ -536,38 +463,33 @@ __device__ __forceinline__ void stream_chunk(const uint4* __restrict__ vp, int v
 #pragma unroll 1
   for (int it = v_begin; it < full_end; it += STEP) {
     if (it + STEP < full_end) load_batch<T, NT, U, false>(vp, it + STEP, v_end, tid, nxt);
-    process_batch<T, NT, U, false>(cur, it, it, v_end, id_base, K, tid, lane, acc, w, s_cta_thr,
+    process_batch<T, NT, U, false>(cur, it, it, v_end, id_base, K, tid, lane, m, s, w, s_cta_thr,
                                    s_wtop);
 #pragma unroll
     for (int u = 0; u < U; ++u) cur[u] = nxt[u];
   }
   if (full_end < v_end) {
     load_batch<T, NT, U, true>(vp, full_end, v_end, tid, cur);
-    process_batch<T, NT, U, true>(cur, full_end, full_end, v_end, id_base, K, tid, lane, acc, w,
+    process_batch<T, NT, U, true>(cur, full_end, full_end, v_end, id_base, K, tid, lane, m, s, w,
                                   s_cta_thr, s_wtop);
   }
 }
 
 // Elements [e_begin, e_end) of row rp, one per lane (the few outside the 16-byte vectors).
-template <typename T, class Acc>
+template <typename T>
 __device__ __forceinline__ void scalar_part(const T* rp, int e_begin, int e_end, int K, int lane,
-                                            Acc& acc, WarpCand& w) {
+                                            float& m, float& s, WarpCand& w) {
   for (int base = e_begin; base < e_end; base += 32) {
     const int e = base + lane;
     const bool valid = e < e_end;
     float x[1] = {valid ? Vec<T>::scalar(rp, e) : -INFINITY};
-    lse_update<1>(acc, x, valid);
+    lse_update<1>(m, s, x, valid);
     warp_append<1>(w, x, (uint32_t)(valid ? e : 0), valid, K, lane);
   }
 }
 
 struct Rec {            // partial record of one (row, split)
   float m, s;
-  uint64_t keys[1];     // [K]
-};
-struct WideRec {        // the same of a wide sum: s in units of 2^e
-  double s;
-  float e;
   uint64_t keys[1];     // [K]
 };
 
@@ -577,15 +499,6 @@ struct WideRec {        // the same of a wide sum: s in units of 2^e
 struct PartialOut {
   unsigned char* rec;       // [rows][partial_bytes(K)], or null for the final outputs
   int32_t id_offset;
-};
-
-// Beams: which rows are live (score above -inf, not done; the others are not read and write
-// nothing), and a record per live row: its log-normaliser in 64 bits, then the values and ids of
-// its K largest logits (id -1: none).
-struct BeamOut {
-  unsigned char* rec;       // [rows][beam_record_bytes(K)]
-  const float* scores;      // [rows]
-  const uint8_t* done;      // [rows], may be null
 };
 
 // Warp 0 of the CTA that completes row `row`: (m, s) of the row, its top-K keys in s_top.
@@ -616,23 +529,6 @@ __device__ __forceinline__ void write_row(int row, int K, float m, float s, cons
   }
 }
 
-// Warp 0 of the CTA that completes a beam's row: the sum s in units of 2^e, the top-K keys.
-__device__ __forceinline__ void write_beam_row(int row, int K, float e, double s,
-                                               const uint64_t* s_top, const BeamOut& bout,
-                                               uint32_t* status, int lane) {
-  unsigned char* r = bout.rec + (size_t)row * beam_record_bytes(K);
-  if (lane == 0) {
-    const double l = (double)e * 0.69314718055994530942 + log(s);
-    *reinterpret_cast<double*>(r) = l;
-    if (!isfinite(l)) set_status(status, LILICORR_ERR_NONFINITE);
-  }
-  if (lane < K) {
-    const uint64_t k = s_top[lane];
-    reinterpret_cast<float*>(r + 8)[lane] = k ? key_value(k) : -INFINITY;
-    reinterpret_cast<int32_t*>(r + 8)[K + lane] = k ? key_id(k) : -1;
-  }
-}
-
 // Shared memory of one CTA's row reduction.
 template <int NW>
 struct TkShared {
@@ -643,7 +539,6 @@ struct TkShared {
   uint64_t top[LILICORR_MAX_K];
   uint64_t bound;
   float m[NW], s[NW];
-  double sd[NW];                        // the warps' wide sums (their exponents in m)
   float wtop[NW];                       // the warps' r-th largest lane maxima
   uint32_t cta_thr;                     // CTA-wide value bound (order image)
   int last, count;
@@ -654,29 +549,23 @@ struct TkShared {
 // (its only piece) or the piece's partial record and a ticket. The CTA that takes the
 // row's last ticket (atomic, no waiting) merges the `npieces` records (row_recs,
 // rec_bytes apart) and writes the row.
-template <int NT, class Acc, class Out>
-__device__ void finish_piece(TkShared<NT / 32>& sh, WarpCand& w, const Acc& acc, int row, int K,
+template <int NT>
+__device__ void finish_piece(TkShared<NT / 32>& sh, WarpCand& w, float m, float s, int row, int K,
                              int npieces, int piece, unsigned char* row_recs, size_t rec_bytes,
-                             uint32_t* counters, const Out& pout, int32_t* ids,
+                             uint32_t* counters, const PartialOut& pout, int32_t* ids,
                              float* logp, float* lse, uint32_t* status) {
   constexpr int NW = NT / 32;
-  constexpr bool WIDE = Acc::WIDE;
-  using Record = std::conditional_t<WIDE, WideRec, Rec>;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   // (max, sum) of the warp, then of the CTA
+  const float wm = warp_max(m);
+  float ws = (m == -INFINITY) ? 0.f : s * ex2((m - wm) * LOG2E);
+  ws = warp_sum(ws);
   const float pb = publish_bound(w, K);
-  if constexpr (WIDE) {
-    float we;
-    const double wsum = wide_warp_sum(acc.e, (double)acc.s + (double)acc.c, we);
-    if (lane == 0) { sh.m[warp] = we; sh.sd[warp] = wsum; }
-  } else {
-    const float m = acc.m, s = acc.s;
-    const float wm = warp_max(m);
-    float ws = (m == -INFINITY) ? 0.f : s * ex2((m - wm) * LOG2E);
-    ws = warp_sum(ws);
-    if (lane == 0) { sh.m[warp] = wm; sh.s[warp] = ws; }
+  if (lane == 0) {
+    sh.m[warp] = wm;
+    sh.s[warp] = ws;
+    atomicMax(&sh.cta_thr, ord32(pb));
   }
-  if (lane == 0) atomicMax(&sh.cta_thr, ord32(pb));
   // CTA top-K: keys of every warp's buffer at or above the CTA-wide bound, rank-counted
   // (the bound never exceeds the CTA's K-th value, so the K largest keys all survive)
   if (tid == 0) sh.count = 0;
@@ -707,33 +596,21 @@ __device__ void finish_piece(TkShared<NT / 32>& sh, WarpCand& w, const Acc& acc,
   }
 
   float cm = -INFINITY, cs = 0.f;
-  double csd = 0.0;
   if (warp == 0) {
     const float pm = lane < NW ? sh.m[lane] : -INFINITY;
-    if constexpr (WIDE) {
-      csd = wide_warp_sum(pm, lane < NW ? sh.sd[lane] : 0.0, cm);
-    } else {
-      const float ps = lane < NW ? sh.s[lane] : 0.f;
-      cm = warp_max(pm);
-      cs = warp_sum(pm == -INFINITY ? 0.f : ps * ex2((pm - cm) * LOG2E));
-    }
+    const float ps = lane < NW ? sh.s[lane] : 0.f;
+    cm = warp_max(pm);
+    cs = warp_sum(pm == -INFINITY ? 0.f : ps * ex2((pm - cm) * LOG2E));
   }
   if (npieces == 1) {
-    if (warp == 0) {
-      if constexpr (WIDE) write_beam_row(row, K, cm, csd, sh.top, pout, status, lane);
-      else write_row(row, K, cm, cs, sh.top, pout, ids, logp, lse, status, lane);
-    }
+    if (warp == 0) write_row(row, K, cm, cs, sh.top, pout, ids, logp, lse, status, lane);
     return;
   }
 
   // publish this piece's record, then take a ticket
-  Record* rec = reinterpret_cast<Record*>(row_recs + (size_t)piece * rec_bytes);
+  Rec* rec = reinterpret_cast<Rec*>(row_recs + (size_t)piece * rec_bytes);
   if (warp == 0) {
-    if constexpr (WIDE) {
-      if (lane == 0) { rec->e = cm; rec->s = csd; }
-    } else {
-      if (lane == 0) { rec->m = cm; rec->s = cs; }
-    }
+    if (lane == 0) { rec->m = cm; rec->s = cs; }
     if (lane < K) rec->keys[lane] = sh.top[lane];
     __threadfence();
   }
@@ -749,56 +626,35 @@ __device__ void finish_piece(TkShared<NT / 32>& sh, WarpCand& w, const Acc& acc,
   // last CTA of the row: merge all pieces (their lists staged in shared memory)
   const int n = npieces * K;
   for (int i = tid; i < n; i += NT) {
-    const Record* r = reinterpret_cast<const Record*>(row_recs + (size_t)(i / K) * rec_bytes);
+    const Rec* r = reinterpret_cast<const Rec*>(row_recs + (size_t)(i / K) * rec_bytes);
     sh.keys[i] = __ldcg(reinterpret_cast<const unsigned long long*>(&r->keys[i % K]));
   }
   csync<NT>();
   cta_select<NT>(sh.keys, npieces, K, K, sh.merge, &sh.count, &sh.bound, sh.top);
   if (warp == 0) {
-    if (lane == 0) counters[row] = 0u;             // leave the workspace reusable
-    if constexpr (WIDE) {
-      float pe = -INFINITY, ge;
-      double ps = 0.0;
-      for (int i = lane; i < npieces; i += 32) {
-        const WideRec* r = reinterpret_cast<const WideRec*>(row_recs + (size_t)i * rec_bytes);
-        const float re = __ldcg(&r->e);
-        const double rs = __ldcg(&r->s);
-        if (re == -INFINITY) {
-          ps += rs;                                    // 0, or NaN
-          continue;
-        }
-        const float big = fmaxf(pe, re);
-        ps = (pe == -INFINITY ? ps : ps * (double)pow2_whole(pe - big)) +
-             rs * (double)pow2_whole(re - big);
-        pe = big;
-      }
-      const double gs = wide_warp_sum(pe, ps, ge);
-      write_beam_row(row, K, ge, gs, sh.top, pout, status, lane);
-    } else {
-      float pm = -INFINITY, ps = 0.f;
-      for (int i = lane; i < npieces; i += 32) {
-        const Rec* r = reinterpret_cast<const Rec*>(row_recs + (size_t)i * rec_bytes);
-        const float rm = __ldcg(&r->m), rs = __ldcg(&r->s);
-        if (rm == -INFINITY) continue;
-        if (rm > pm) { ps = ps * ex2((pm - rm) * LOG2E) + rs; pm = rm; }
-        else ps += rs * ex2((rm - pm) * LOG2E);
-      }
-      const float gm = warp_max(pm);
-      const float gs = warp_sum(pm == -INFINITY ? 0.f : ps * ex2((pm - gm) * LOG2E));
-      write_row(row, K, gm, gs, sh.top, pout, ids, logp, lse, status, lane);
+    float pm = -INFINITY, ps = 0.f;
+    for (int i = lane; i < npieces; i += 32) {
+      const Rec* r = reinterpret_cast<const Rec*>(row_recs + (size_t)i * rec_bytes);
+      const float rm = __ldcg(&r->m), rs = __ldcg(&r->s);
+      if (rm == -INFINITY) continue;
+      if (rm > pm) { ps = ps * ex2((pm - rm) * LOG2E) + rs; pm = rm; }
+      else ps += rs * ex2((rm - pm) * LOG2E);
     }
+    const float gm = warp_max(pm);
+    const float gs = warp_sum(pm == -INFINITY ? 0.f : ps * ex2((pm - gm) * LOG2E));
+    if (lane == 0) counters[row] = 0u;             // leave the workspace reusable
+    write_row(row, K, gm, gs, sh.top, pout, ids, logp, lse, status, lane);
   }
 }
 
 // U vectors per thread per batch: 4 with up to 1024 / NT CTAs per SM (64 registers), 8 for
 // the split plan of few rows (at most two CTAs per SM; more bytes in flight per thread).
-// Acc, Out: Lse and PartialOut, or LseWide and BeamOut for the rows of beams.
-template <typename T, int NT, int U, class Acc, class Out>
+template <typename T, int NT, int U>
 __global__ void __launch_bounds__(NT, (U > 4 ? 512 : 1024) / NT)
 topk_lse_kernel(const T* __restrict__ logits, int V, int K, int splits, int chunk_vecs,
                 size_t rec_bytes, int32_t* __restrict__ ids, float* __restrict__ logp,
                 float* __restrict__ lse, uint32_t* status, uint32_t* counters,
-                unsigned char* partials, Out pout) {
+                unsigned char* partials, PartialOut pout) {
   pdl_wait();
   constexpr int VEC = Vec<T>::N;
   constexpr int NW = NT / 32;
@@ -807,10 +663,6 @@ topk_lse_kernel(const T* __restrict__ logits, int V, int K, int splits, int chun
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int split = blockIdx.x;
   const int row = blockIdx.y;
-  if constexpr (Acc::WIDE) {
-    // a beam that is done or absent: its logits are never read (the same for the whole row)
-    if (!(pout.scores[row] > -INFINITY) || (pout.done && pout.done[row])) return;
-  }
   const T* rp = logits + (size_t)row * V;
 
   // vector-aligned region of this row: [e0, e0 + nvec * VEC)
@@ -830,20 +682,20 @@ topk_lse_kernel(const T* __restrict__ logits, int V, int K, int splits, int chun
   if (tid < NW) sh.wtop[tid] = -INFINITY;
   __syncthreads();
 
-  Acc acc;
+  float m = -INFINITY, s = 0.f;
 
   // scalar head [0, e0), before the vectors, and scalar tail [e0 + nvec*VEC, V), after
   // them: warp 0 of split 0, one element per lane (so that warp meets its ids in order)
   const int tail0 = e0 + nvec * VEC;
   const bool scalars = split == 0 && warp == 0;
-  if (scalars) scalar_part<T>(rp, 0, e0, K, lane, acc, w);
+  if (scalars) scalar_part<T>(rp, 0, e0, K, lane, m, s, w);
 
   // main stream: batches of 16-byte vectors, the next one's loads in flight
   const uint4* vp = reinterpret_cast<const uint4*>(rp + e0);
-  stream_chunk<T, NT, U>(vp, v_begin, v_end, (uint32_t)e0, K, tid, lane, acc, w, &sh.cta_thr,
+  stream_chunk<T, NT, U>(vp, v_begin, v_end, (uint32_t)e0, K, tid, lane, m, s, w, &sh.cta_thr,
                          sh.wtop);
-  if (scalars) scalar_part<T>(rp, tail0, V, K, lane, acc, w);
-  finish_piece<NT>(sh, w, acc, row, K, splits, split,
+  if (scalars) scalar_part<T>(rp, tail0, V, K, lane, m, s, w);
+  finish_piece<NT>(sh, w, m, s, row, K, splits, split,
                    partials + (size_t)row * splits * rec_bytes, rec_bytes, counters, pout, ids,
                    logp, lse, status);
 }
@@ -922,8 +774,6 @@ topk_merge_kernel(const unsigned char* __restrict__ recs, size_t ld_p, size_t ld
 
 }  // namespace
 
-static size_t wide_rec_bytes(int K) { return align_up(offsetof(WideRec, keys) + 8 * (size_t)K, 16); }
-
 TopkPlan topk_plan(int rows, int V, int K, lilicorr_dtype_t dt) {
   if (rows < 1) rows = 1;                    // sizes of an empty call
   const int vec = dt == LILICORR_BF16 ? 8 : 4;
@@ -962,20 +812,20 @@ size_t topk_ws_bytes(int rows, int V, int K, lilicorr_dtype_t dt) {
   return 256 + align_up((size_t)rows * 4, 256) + align_up((size_t)rows * p.pieces * p.rec_bytes, 256);
 }
 
-template <class Acc, typename T, class Out>
+template <typename T>
 lilicorr_status_t launch_plan(const TopkPlan& p, const T* x, int rows, int V, int K, int32_t* ids,
                               float* logp, float* lse, uint32_t* status, uint32_t* counters,
-                              unsigned char* part, const Out& pout, cudaStream_t st) {
+                              unsigned char* part, const PartialOut& pout, cudaStream_t st) {
   const dim3 grid(p.splits, rows);
   if (p.threads == TK_THREADS_MANY)
-    return launch_k(topk_lse_kernel<T, TK_THREADS_MANY, TK_UNROLL, Acc, Out>, grid, TK_THREADS_MANY, 0, st,
+    return launch_k(topk_lse_kernel<T, TK_THREADS_MANY, TK_UNROLL>, grid, TK_THREADS_MANY, 0, st,
                     x, V, K, p.splits, p.chunk_vecs, p.rec_bytes, ids, logp, lse, status, counters,
                     part, pout);
   if (p.unroll == TK_UNROLL_FEW)
-    return launch_k(topk_lse_kernel<T, TK_THREADS, TK_UNROLL_FEW, Acc, Out>, grid, TK_THREADS, 0, st, x, V,
+    return launch_k(topk_lse_kernel<T, TK_THREADS, TK_UNROLL_FEW>, grid, TK_THREADS, 0, st, x, V,
                     K, p.splits, p.chunk_vecs, p.rec_bytes, ids, logp, lse, status, counters, part,
                     pout);
-  return launch_k(topk_lse_kernel<T, TK_THREADS, TK_UNROLL, Acc, Out>, grid, TK_THREADS, 0, st, x, V, K,
+  return launch_k(topk_lse_kernel<T, TK_THREADS, TK_UNROLL>, grid, TK_THREADS, 0, st, x, V, K,
                   p.splits, p.chunk_vecs, p.rec_bytes, ids, logp, lse, status, counters, part,
                   pout);
 }
@@ -989,30 +839,10 @@ lilicorr_status_t launch_topk_lse(const void* logits, lilicorr_dtype_t dt, int r
   const TopkPlan p = topk_plan(rows, V, K, dt);
   unsigned char* part = static_cast<unsigned char*>(partials);
   if (dt == LILICORR_BF16)
-    return launch_plan<Lse>(p, static_cast<const uint16_t*>(logits), rows, V, K, ids, logp, lse,
-                            status, counters, part, pout, st);
-  return launch_plan<Lse>(p, static_cast<const float*>(logits), rows, V, K, ids, logp, lse, status,
-                          counters, part, pout, st);
-}
-
-size_t beam_rows_ws_bytes(int rows, int V, int K, lilicorr_dtype_t dt) {
-  const TopkPlan p = topk_plan(rows, V, K, dt);
-  return align_up((size_t)rows * 4, 256) + align_up((size_t)rows * p.pieces * wide_rec_bytes(K), 256);
-}
-
-lilicorr_status_t launch_beam_rows(const void* logits, lilicorr_dtype_t dt, int rows, int V, int K,
-                                   const float* scores, const uint8_t* done, void* records,
-                                   uint32_t* status, void* ws, cudaStream_t st) {
-  TopkPlan p = topk_plan(rows, V, K, dt);
-  p.rec_bytes = wide_rec_bytes(K);
-  uint32_t* counters = static_cast<uint32_t*>(ws);
-  unsigned char* part = static_cast<unsigned char*>(ws) + align_up((size_t)rows * 4, 256);
-  const BeamOut out{static_cast<unsigned char*>(records), scores, done};
-  if (dt == LILICORR_BF16)
-    return launch_plan<LseWide>(p, static_cast<const uint16_t*>(logits), rows, V, K, nullptr,
-                                nullptr, nullptr, status, counters, part, out, st);
-  return launch_plan<LseWide>(p, static_cast<const float*>(logits), rows, V, K, nullptr, nullptr,
-                              nullptr, status, counters, part, out, st);
+    return launch_plan(p, static_cast<const uint16_t*>(logits), rows, V, K, ids, logp, lse, status,
+                       counters, part, pout, st);
+  return launch_plan(p, static_cast<const float*>(logits), rows, V, K, ids, logp, lse, status,
+                     counters, part, pout, st);
 }
 
 lilicorr_status_t launch_topk_merge(const void* partials, size_t ld_p, size_t ld_row, int P,

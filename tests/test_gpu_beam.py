@@ -190,6 +190,44 @@ def test_beam_select_equal_logits_and_equal_beams():
     assert sc[0, 0] == sc[0, 1]
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["constant", "falling", "rising", "grid", "head_and_tail"])
+@pytest.mark.parametrize("W,V,n", [(8, 40001, 32), (3, 5003, 8), (12, 151936, 24)])
+def test_beam_select_rows_of_equal_and_of_ordered_logits(dtype, kind, W, V, n):
+    """Ties over the whole vocabulary, and rows whose best logits all lie next to one another."""
+    ll = _ll()
+    rng = np.random.default_rng(V + n)
+    at = np.arange(V)
+    if kind == "constant":
+        x = np.full((2, W, V), 1.5)
+    elif kind == "falling":
+        x = np.tile(-0.25 * (at // 3), (2, W, 1))
+    elif kind == "rising":
+        x = np.tile(0.25 * ((at - V) // 5), (2, W, 1))
+    elif kind == "grid":
+        x = np.round(rng.standard_normal((2, W, V)) * 4) / 4
+    else:
+        x = rng.standard_normal((2, W, V))
+        x[:, :, [0, 1, 2, V - 3, V - 2, V - 1]] += 20.0
+    x = x.astype(np.float32)
+    if dtype == "bf16":
+        x = workloads.round_to_bf16(x)
+    scores = -np.arange(2 * W, dtype=np.float32).reshape(2, W) / 1000
+    want = _want_select(x, scores, n, None, -1)
+    _check_select(_run_select(ll, x, scores, n, dtype), want, scores, None, -1)
+
+
+def test_beam_select_equal_beams_with_equal_rows():
+    """Eight beams alike in everything, constant rows: position alone orders all candidates."""
+    ll = _ll()
+    x = torch.zeros((1, 8, 151936), dtype=torch.bfloat16, device="cuda")
+    tok, par, sc, _ = ll.beam_select(x, torch.zeros((1, 8), device="cuda"), 32)
+    assert tok.cpu().tolist() == [list(range(32))] and par.cpu().tolist() == [[0] * 32]
+    x[0, :, 1000:1100] = 2.0
+    tok, par, sc, _ = ll.beam_select(x, torch.zeros((1, 8), device="cuda"), 32)
+    assert tok.cpu().tolist() == [list(range(1000, 1032))] and par.cpu().tolist() == [[0] * 32]
+
+
 @pytest.mark.parametrize("bad", [np.nan, np.inf, "row", "score_nan", "score_inf"])
 @pytest.mark.parametrize("V", [37, 20000])
 def test_beam_select_nonfinite(bad, V):
