@@ -327,7 +327,7 @@ lilicorr_status_t lilicorr_select_block_walk(const lilicorr_head* head, int B, c
  *   end_id               the token that ends a beam, or -1 (only where done is NULL)
  * A live beam w offers each of its tokens v at total = scores[w] + logp(v | w); a beam that is done
  * offers the one candidate (end_id, scores[w]), and nothing else about it is read. Totals are formed
- * and compared in 64 bits; equal totals order by lower beam, in a beam by the candidates' order. A
+ * and compared to 48 bits or more; equal totals order by lower beam, in a beam by the candidates' order. A
  * candidate of total -inf (a banned token) is never kept. Outputs, best first:
  *   tokens, parents [R, n] int32   token and beam of each kept candidate; -1 where there are fewer
  *   next_scores     [R, n] fp32    the total, rounded once; -inf where there are fewer

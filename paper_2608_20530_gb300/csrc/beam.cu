@@ -2,7 +2,7 @@
 // beams that continue them.
 //
 // Selection from logits takes two launches.
-//   (1) beam_stream_kernel reads every live row once, in chunks of 32 x 4 vectors of 16 bytes, one
+//   (1) beam_stream_kernel reads every live row once, in chunks of 32 x 8 vectors of 16 bytes, one
 //       warp a chunk, and leaves each chunk's largest logit and the row's sum of exponentials.
 //   (2) beam_choose_kernel, one CTA a request, forms the rows' normalisers, takes the n chunks whose
 //       largest totals (score + logit - normaliser) come first, reads those chunks again and ranks
@@ -22,17 +22,59 @@ namespace {
 
 constexpr unsigned FULL = 0xffffffffu;
 constexpr int BM_THREADS = 128;
-constexpr int BM_CAND = LILICORR_MAX_BEAMS * LILICORR_MAX_K;
 constexpr float LOG2E = 1.4426950408889634f;
-constexpr float LOG2E_LO = 1.92596299e-8f;     // log2(e) - LOG2E
+constexpr float LOG2E_REST = 1.33497e-8f;      // (log2(e) - LOG2E) ln 2
 
-// Order-preserving image of a double that is not NaN; 0 is never one (it marks "no candidate").
-__device__ __forceinline__ uint64_t ord64(double v) {
-  const uint64_t b = (uint64_t)__double_as_longlong(v + 0.0);      // -0 to +0
-  return (b >> 63) ? ~b : (b | (1ull << 63));
+// order-preserving 32-bit image of a float (-0 below +0)
+__device__ __forceinline__ uint32_t ord32(float v) {
+  const uint32_t b = __float_as_uint(v);
+  return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
 }
-__device__ __forceinline__ double unord64(uint64_t o) {
-  return __longlong_as_double((long long)((o >> 63) ? (o & ~(1ull << 63)) : ~o));
+__device__ __forceinline__ float unord32(uint32_t o) {
+  return __uint_as_float((o & 0x80000000u) ? (o & 0x7FFFFFFFu) : ~o);
+}
+// s + c and s2 + c2 to s + c, the rounding of s + s2 kept in c
+__device__ __forceinline__ void add_pair(float& s, float& c, float s2, float c2) {
+  const float t = s + s2, bb = t - s;
+  c = (c + c2) + ((s - (t - bb)) + (s2 - bb));
+  s = t;
+}
+// Key of a total s + c (|c| at most half a step of s): order-preserving, 0 for -inf, NaN and +inf. Two
+// fp32 numbers carry 48 bits; GB300 would take 16 clocks a warp for any one operation in FP64.
+__device__ __forceinline__ uint64_t pair_key(float s, float c) {
+  if (!(s > -INFINITY && s < INFINITY)) return 0ull;
+  return ((uint64_t)ord32(s + 0.f) << 32) | ord32(c + 0.f);          // -0 to +0
+}
+__device__ __forceinline__ float key_score(uint64_t key) { return unord32((uint32_t)(key >> 32)); }
+// Key of (hi + lo) + x.
+__device__ __forceinline__ uint64_t sum_key(float hi, float lo, float x) {
+  add_pair(hi, lo, x, 0.f);
+  const float s = hi + lo;
+  return pair_key(s, lo - (s - hi));
+}
+// log(s + c) + e log 2 of s > 0 as hi + lo, to about 1e-9. log m = 2 atanh((m - 1) / (m + 1)) for s
+// scaled to m in [0.7, 1.42): the quotient as a pair, the series' further terms (below 0.004) in fp32.
+__device__ __forceinline__ void log_pair(float s, float c, float e, float& hi, float& lo) {
+  // s = m 2^k (s is normal: a sum of exponentials whose largest lies in (1/2, 1])
+  const int bits = __float_as_int(s);
+  int k = ((bits >> 23) & 255) - 127;
+  float m = __int_as_float((bits & 0x7FFFFF) | 0x3F800000);
+  if (m > 1.41421356f) { m *= 0.5f; ++k; }
+  const float mc = c * __int_as_float((127 - k) << 23);
+  const float num = m - 1.f, den = m + 1.f;          // num exact; den off by at most 2^-24
+  const float dl = m - (den - 1.f);
+  const float z = __fdividef(num, den);
+  const float zl = __fdividef(fmaf(-z, den, num) + mc - z * (dl + mc), den);
+  const float q = z * z;
+  const float rest = z * q * (0.66666667f + q * (0.4f + q * (0.28571429f + q * (0.22222222f + q * 0.18181818f))));
+  const float n = e + (float)k, l = 0.69314718f, ll = -1.9046543e-9f;   // log 2 = l + ll + ...
+  hi = n * l;
+  lo = fmaf(n, l, -hi) + n * ll;
+  add_pair(hi, lo, 2.f * z, 2.f * zl);
+  add_pair(hi, lo, rest, 0.f);
+  const float t = hi + lo;
+  lo -= t - hi;
+  hi = t;
 }
 // a precedes b: larger total, then lower position
 template <typename P>
@@ -40,15 +82,11 @@ __device__ __forceinline__ bool precedes(uint64_t ka, P pa, uint64_t kb, P pb) {
   return ka > kb || (ka == kb && pa < pb);
 }
 
-// The first n of `count` candidates in order: place(rank, key, position) for each; returns how many
-// there are, up to n. near(i): candidate i's total in fp32, off by at most 2^-22 of |total| + `scale`,
-// -inf for none; key(i) its 64-bit key (0: none).
-//
-// First a bound: 64 groups of threads put forward their best candidate (by near, one is as valid as
-// another), and nothing below the n-th of those 64 can be among the first n. Only the few candidates
-// that reach it get a 64-bit total (GB300 adds two of those a clock and SM) and are ranked against one
+// The first n of many candidates in order. First a bound: 64 groups of threads put forward their best
+// candidate (best as far as fp32 tells, one is as valid as another), and nothing below the n-th of
+// those 64 can be among the first n. The few candidates that reach it are kept and ranked against one
 // another, four lanes a candidate. Where very many reach it (equal totals everywhere) the n are taken
-// one after the other instead.
+// one after the other instead. Keys are order-preserving, 0 for no candidate.
 constexpr int RF_GROUPS = 64;
 constexpr int RF_CAP = 1024;
 struct RankShared {
@@ -58,81 +96,66 @@ struct RankShared {
   int count;
 };
 
-template <int NT, class Near, class Key, class Pos, class Place>
-__device__ __forceinline__ int rank_first(RankShared& sh, int count, int n, float scale, Near near,
-                                          Key key, Pos pos, Place place) {
-  constexpr int LPG = NT / RF_GROUPS;          // lanes a group
+// The threads' best candidates (key 0: none) to sh.bound: all NT threads, LPG = NT / 64 lanes a group.
+template <int NT>
+__device__ __forceinline__ void rank_bound(RankShared& sh, int n, uint64_t key, uint64_t pos) {
+  constexpr int LPG = NT / RF_GROUPS;
   static_assert(LPG >= 2 && LPG <= 32 && (LPG & (LPG - 1)) == 0 && RF_GROUPS >= LILICORR_MAX_K, "");
   const int tid = threadIdx.x;
-  float floor = -INFINITY;
-  uint64_t bound = 1ull, bound_pos = ~0ull;
+#pragma unroll
+  for (int o = 1; o < LPG; o <<= 1) {
+    const uint64_t k = __shfl_xor_sync(FULL, key, o), p = __shfl_xor_sync(FULL, pos, o);
+    if (precedes(k, p, key, pos)) { key = k; pos = p; }
+  }
+  const int g = tid / LPG, in = tid % LPG;
+  if (in == 0) { sh.gkey[g] = key; sh.gpos[g] = pos; }
   if (tid == 0) { sh.count = 0; sh.bound = 1ull; sh.bound_pos = ~0ull; }
-  if (count > RF_GROUPS) {
-    float best = -INFINITY;
-    int at = -1;
-    for (int i = tid; i < count; i += NT) {
-      const float v = near(i);
-      if (v > best) { best = v; at = i; }
-    }
-#pragma unroll
-    for (int o = 1; o < LPG; o <<= 1) {
-      const float v = __shfl_xor_sync(FULL, best, o);
-      const int x = __shfl_xor_sync(FULL, at, o);
-      if (v > best || (v == best && x > at)) { best = v; at = x; }
-    }
-    const int g = tid / LPG, in = tid % LPG;
-    const uint64_t gk = at >= 0 ? key(at) : 0ull, gp = at >= 0 ? pos(at) : (uint64_t)g;
-    if (in == 0) { sh.gkey[g] = gk; sh.gpos[g] = gp; }
-    __syncthreads();
-    int rank = 0;
-#pragma unroll
-    for (int j = 0; j < RF_GROUPS / LPG; ++j) {
-      const int o = j * LPG + in;
-      rank += precedes(sh.gkey[o], sh.gpos[o], gk, gp) ? 1 : 0;
-    }
-#pragma unroll
-    for (int o = 1; o < LPG; o <<= 1) rank += __shfl_xor_sync(FULL, rank, o);
-    if (in == 0 && gk && rank == n - 1) { sh.bound = gk; sh.bound_pos = gp; }
-    __syncthreads();
-    bound = sh.bound;
-    bound_pos = sh.bound_pos;
-    if (bound != 1ull) {
-      const float b = (float)unord64(bound);
-      floor = b - 0x1p-20f * (fabsf(b) + scale);
-    }
-  } else {
-    __syncthreads();
-  }
-  for (int i = tid; i < count; i += NT) {
-    const float v = near(i);
-    if (!(v >= floor) || v == -INFINITY) continue;
-    const uint64_t k = key(i), p = pos(i);
-    if (!k || precedes(bound, bound_pos, k, p)) continue;
-    const int at = atomicAdd(&sh.count, 1);
-    if (at < RF_CAP) { sh.key[at] = k; sh.pos[at] = p; }
-  }
   __syncthreads();
-  const int m = sh.count;
-  if (m <= RF_CAP) {
-    const int in = tid & 3;
-    for (int i0 = 0; i0 < m; i0 += NT / 4) {
-      const int i = i0 + (tid >> 2);
-      const uint64_t k = i < m ? sh.key[i] : ~0ull, p = i < m ? sh.pos[i] : 0ull;
-      int rank = 0;
-#pragma unroll 4
-      for (int j = in; j < m; j += 4) rank += precedes(sh.key[j], sh.pos[j], k, p) ? 1 : 0;
-      rank += __shfl_xor_sync(FULL, rank, 1);
-      rank += __shfl_xor_sync(FULL, rank, 2);
-      if (in == 0 && i < m && rank < n) place(rank, k, p);
-    }
-    return min(m, n);
+  int rank = 0;
+#pragma unroll
+  for (int j = 0; j < RF_GROUPS / LPG; ++j) {
+    const int o = j * LPG + in;
+    rank += precedes(sh.gkey[o], sh.gpos[o], key, pos) ? 1 : 0;
   }
+#pragma unroll
+  for (int o = 1; o < LPG; o <<= 1) rank += __shfl_xor_sync(FULL, rank, o);
+  if (in == 0 && key && rank == n - 1) { sh.bound = key; sh.bound_pos = pos; }
+  __syncthreads();
+}
+__device__ __forceinline__ void rank_keep(RankShared& sh, uint64_t k, uint64_t p) {
+  if (!k || precedes(sh.bound, sh.bound_pos, k, p)) return;
+  const int at = atomicAdd(&sh.count, 1);
+  if (at < RF_CAP) { sh.key[at] = k; sh.pos[at] = p; }
+}
+// place(rank, key, position) for the first n of what was kept; how many there are, up to n, or -1
+// where more were kept than fit. After a barrier.
+template <int NT, class Place>
+__device__ __forceinline__ int rank_kept(RankShared& sh, int n, Place place) {
+  const int m = sh.count;
+  if (m > RF_CAP) return -1;
+  const int tid = threadIdx.x, in = tid & 3;
+  for (int i0 = 0; i0 < m; i0 += NT / 4) {
+    const int i = i0 + (tid >> 2);
+    const uint64_t k = i < m ? sh.key[i] : ~0ull, p = i < m ? sh.pos[i] : 0ull;
+    int rank = 0;
+#pragma unroll 4
+    for (int j = in; j < m; j += 4) rank += precedes(sh.key[j], sh.pos[j], k, p) ? 1 : 0;
+    rank += __shfl_xor_sync(FULL, rank, 1);
+    rank += __shfl_xor_sync(FULL, rank, 2);
+    if (in == 0 && i < m && rank < n) place(rank, k, p);
+  }
+  return min(m, n);
+}
+// The same from all `count` candidates, one after the other; at least n of them have a key.
+template <int NT, class Key, class Pos, class Place>
+__device__ __noinline__ void rank_rounds(RankShared& sh, int count, int n, Key key_of, Pos pos_of,
+                                         Place place) {
+  const int tid = threadIdx.x;
   uint64_t last = ~0ull, last_pos = 0ull;      // before every candidate
-  for (int t = 0; t < n; ++t) {                // m > RF_CAP >= n: there is one each time
+  for (int t = 0; t < n; ++t) {
     uint64_t bk = 0ull, bp = ~0ull;
     for (int i = tid; i < count; i += NT) {
-      if (near(i) == -INFINITY) continue;
-      const uint64_t k = key(i), p = pos(i);
+      const uint64_t k = key_of(i), p = pos_of(i);
       if (k && precedes(last, last_pos, k, p) && precedes(k, p, bk, bp)) { bk = k; bp = p; }
     }
 #pragma unroll
@@ -140,6 +163,7 @@ __device__ __forceinline__ int rank_first(RankShared& sh, int count, int n, floa
       const uint64_t k = __shfl_xor_sync(FULL, bk, o), p = __shfl_xor_sync(FULL, bp, o);
       if (precedes(k, p, bk, bp)) { bk = k; bp = p; }
     }
+    __syncthreads();
     if ((tid & 31) == 0) { sh.gkey[tid >> 5] = bk; sh.gpos[tid >> 5] = bp; }
     __syncthreads();
     for (int w = 0; w < NT / 32; ++w)
@@ -147,8 +171,33 @@ __device__ __forceinline__ int rank_first(RankShared& sh, int count, int n, floa
     if (tid == 0) place(t, bk, bp);
     last = bk;
     last_pos = bp;
+  }
+}
+// All of it for keys that lie in shared memory (written before a barrier).
+template <int NT, class Pos, class Place>
+__device__ __forceinline__ int rank_first(RankShared& sh, const uint64_t* keys, int count, int n,
+                                          Pos pos_of, Place place) {
+  const int tid = threadIdx.x;
+  if (count > RF_GROUPS) {
+    uint64_t best = 0ull, best_p = ~0ull;
+    for (int i = tid; i < count; i += NT) {
+      const uint64_t k = keys[i];
+      if (k < best) continue;
+      const uint64_t p = pos_of(i);
+      if (precedes(k, p, best, best_p)) { best = k; best_p = p; }
+    }
+    rank_bound<NT>(sh, n, best, best_p);
+  } else {
+    if (tid == 0) { sh.count = 0; sh.bound = 1ull; sh.bound_pos = ~0ull; }
     __syncthreads();
   }
+  const uint64_t least = sh.bound;
+  for (int i = tid; i < count; i += NT)
+    if (keys[i] >= least) rank_keep(sh, keys[i], pos_of(i));
+  __syncthreads();
+  const int m = rank_kept<NT>(sh, n, place);
+  if (m >= 0) return m;
+  rank_rounds<NT>(sh, count, n, [&](int i) { return keys[i]; }, pos_of, place);
   return n;
 }
 
@@ -158,11 +207,11 @@ struct BeamOut {
   uint8_t* next_done;
   int32_t end_id;
   int n;
-  __device__ void put(int r, int rank, uint64_t key, int w, int32_t token, bool over) const {
+  __device__ void put(int r, int rank, float score, int w, int32_t token, bool over) const {
     const size_t at = (size_t)r * n + rank;
     tokens[at] = token;
     parents[at] = w;
-    next_scores[at] = (float)unord64(key);
+    next_scores[at] = score;
     if (next_done) next_done[at] = over || (end_id >= 0 && token == end_id);
   }
   __device__ void none(int r, int rank) const {
@@ -174,55 +223,111 @@ struct BeamOut {
   }
 };
 
-// A total's key: 0 (and `bad`) for NaN and +inf, 0 for -inf.
-__device__ __forceinline__ uint64_t total_key(double total, bool& bad) {
-  if (!(total < INFINITY)) { bad = true; return 0ull; }
-  return total > -INFINITY ? ord64(total) : 0ull;
+// Candidate lists: one CTA a request, a warp a list at a time (lane = rank), each warp keeping the 32
+// first it has seen in order. Two runs of 32 in order merge in six steps: the larger of a[i] and
+// b[31 - i] are the 32 first, and a bitonic sequence. Lists that do not come in order are sorted first.
+constexpr int BM_WARPS = BM_THREADS / 32;
+
+struct Cand { uint64_t key; int pos; };
+__device__ __forceinline__ Cand cand_xor(const Cand& a, int o) {
+  Cand b;
+  b.key = __shfl_xor_sync(FULL, a.key, o);
+  b.pos = __shfl_xor_sync(FULL, a.pos, o);
+  return b;
+}
+// the earlier (or, with `later`, the later) of the two
+__device__ __forceinline__ Cand cand_pick(const Cand& a, const Cand& b, bool later) {
+  return precedes(a.key, a.pos, b.key, b.pos) != later ? a : b;
+}
+__device__ __forceinline__ void cand_bitonic(Cand& a, int lane) {      // a bitonic run to one in order
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) a = cand_pick(a, cand_xor(a, o), (lane & o) != 0);
+}
+__device__ __noinline__ Cand cand_sort(Cand a, int lane) {
+  for (int size = 2; size <= 32; size <<= 1)
+    for (int o = size >> 1; o > 0; o >>= 1)
+      a = cand_pick(a, cand_xor(a, o), ((lane & o) != 0) != ((lane & size) != 0));
+  return a;
+}
+__device__ __forceinline__ void cand_merge(Cand& a, const Cand& b, int lane) {
+  a = cand_pick(a, cand_xor(b, 31), false);
+  cand_bitonic(a, lane);
 }
 
-// Candidate lists: one CTA a request.
 __global__ void __launch_bounds__(BM_THREADS)
 beam_merge_kernel(const int32_t* __restrict__ ids, const float* __restrict__ logp, int W, int K,
                   const float* __restrict__ scores, const uint8_t* __restrict__ done, BeamOut out,
                   uint32_t* status) {
   pdl_wait();
-  __shared__ uint64_t s_key[BM_CAND];
-  __shared__ float s_near[BM_CAND];
-  __shared__ RankShared sh;
-  const int tid = threadIdx.x, r = blockIdx.x, M = W * K;
+  __shared__ uint64_t s_key[BM_WARPS - 1][32];
+  __shared__ int s_pos[BM_WARPS - 1][32];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = blockIdx.x;
   const size_t row0 = (size_t)r * W;
+  Cand top{0ull, 0x7FFFFFFF};
   bool bad = false;
-  for (int i = tid; i < M; i += BM_THREADS) {
-    const int w = i / K;
-    const float sc = scores[row0 + w], lp = logp[row0 * K + i];
-    double total = -INFINITY;
-    if (done && done[row0 + w]) {
-      if (i == w * K) total = (double)sc;
-    } else if (sc != -INFINITY) {
-      total = (double)sc + (double)lp;
+  constexpr int AHEAD = 4;                             // lists whose loads go out together
+  for (int w0 = warp; w0 < W; w0 += AHEAD * BM_WARPS) {
+    float sc[AHEAD], lp[AHEAD];
+    bool over[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const int w = w0 + u * BM_WARPS;
+      sc[u] = lp[u] = -INFINITY;
+      over[u] = false;
+      if (w >= W) continue;
+      sc[u] = scores[row0 + w];
+      if (done) over[u] = done[row0 + w] != 0;
+      if (lane < K) lp[u] = logp[(row0 + w) * K + lane];
     }
-    const uint64_t key = total_key(total, bad);
-    s_key[i] = key;
-    s_near[i] = key ? (float)total : -INFINITY;
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const int w = w0 + u * BM_WARPS;
+      if (w >= W) break;
+      // the exact sum as its rounding to fp32 and what that lost
+      float total = -INFINITY, lost = 0.f;
+      if (over[u]) {
+        if (lane == 0) total = sc[u];
+      } else if (sc[u] != -INFINITY && lane < K) {
+        total = sc[u];
+        add_pair(total, lost, lp[u], 0.f);
+      }
+      if (!(total < INFINITY)) bad = true;             // NaN, +inf
+      Cand c{pair_key(total, lost), w * K + lane};
+      const uint64_t after = __shfl_down_sync(FULL, c.key, 1);
+      if (!__all_sync(FULL, lane == 31 || c.key >= after)) c = cand_sort(c, lane);
+      if (w == warp) top = c;
+      else cand_merge(top, c, lane);
+    }
   }
   if (bad) set_status(status, LILICORR_ERR_NONFINITE);
-  // (a thread reads back what it wrote, but for its group's best)
-  __syncthreads();
-  const int m = rank_first<BM_THREADS>(
-      sh, M, out.n, 0.f, [&](int i) { return s_near[i]; }, [&](int i) { return s_key[i]; },
-      [&](int i) { return (uint64_t)i; },
-      [&](int rank, uint64_t key, uint64_t p) {
-        const int w = (int)p / K;
-        const bool over = done && done[row0 + w];
-        out.put(r, rank, key, w, over ? out.end_id : ids[row0 * K + p], over);
-      });
-  for (int i = m + tid; i < out.n; i += BM_THREADS) out.none(r, i);      // fewer candidates than n
+  // the warps' runs, two and two
+#pragma unroll
+  for (int half = BM_WARPS / 2; half > 0; half >>= 1) {
+    if (warp >= half && warp < 2 * half) {
+      s_key[warp - 1][lane] = top.key;
+      s_pos[warp - 1][lane] = top.pos;
+    }
+    __syncthreads();
+    if (warp < half && warp + half < W)
+      cand_merge(top, Cand{s_key[warp + half - 1][lane], s_pos[warp + half - 1][lane]}, lane);
+  }
+  if (warp == 0 && lane < out.n) {
+    if (top.key == 0ull) {
+      out.none(r, lane);                               // fewer candidates than n
+    } else {
+      const int w = top.pos / K;
+      const bool over = done && done[row0 + w];
+      out.put(r, lane, key_score(top.key), w, over ? out.end_id : ids[row0 * K + top.pos], over);
+    }
+  }
 }
 
 // ---------------------------------------------------------------------------- from logits
 constexpr int BS_THREADS = 256;                // of the streaming kernel
-constexpr int BS_U = 4;                        // 16-byte vectors per lane and chunk
-constexpr int BC_THREADS = 256;                // of the choosing kernel
+constexpr int BS_U = 8;                        // 16-byte vectors per lane and chunk
+constexpr int BS_STAGES = 3;                   // chunks of a warp in flight or in use
+constexpr int BS_CTAS = 2;                     // CTAs an SM
+constexpr int BC_THREADS = 512;                // of the choosing kernel
 
 // How rows are cut: chunk 0 of a row holds the ids before its first 16-byte boundary where rows need
 // not start on one (`odd`), the others runs of `size` ids; warp i of the streaming kernel takes the
@@ -252,20 +357,20 @@ BeamCut beam_cut(int rows, int V, lilicorr_dtype_t dt) {
   c.size = 32 * BS_U * c.vec;
   c.odd = V % c.vec != 0;
   c.chunks = ceil_div(V, c.size) + c.odd;
-  // one wave of 32 warps an SM
-  const long long total = (long long)rows * c.chunks, warps = 32ll * num_sms();
+  // one wave of CTAs
+  const long long total = (long long)rows * c.chunks;
+  const long long warps = (long long)BS_CTAS * (BS_THREADS / 32) * num_sms();
   c.per_warp = (int)((total + warps - 1) / warps);
   if (c.per_warp < 1) c.per_warp = 1;
   c.slots = (c.chunks + c.per_warp - 1) / c.per_warp + 1;
   return c;
 }
 
-// A row's sum of exponentials over some chunks: s in units of 2^e, e a whole number (-inf: nothing
-// but -inf was met, s 0, or NaN). A whole power of two as the reference makes every rescale exact.
-struct SumRec {
-  double s;
-  float e;
-  float pad;
+// A row's sum of exponentials over some chunks: (s + c) 2^e, c what the additions lost, e a whole
+// number (-inf: nothing but -inf was met, s 0, or NaN). A whole power of two as the reference makes
+// every rescale exact.
+struct __align__(16) SumRec {
+  float s, c, e, pad;
 };
 
 // 2^d of a whole number d <= 0 (0 below the normal range and for -inf)
@@ -277,37 +382,11 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ uint64_t pack2(float lo, float hi) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-  return r;
-}
-__device__ __forceinline__ void unpack2(uint64_t v, float& lo, float& hi) {
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t d;
-  asm("fma.rn.ftz.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-  return d;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("add.rn.ftz.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-// order-preserving 32-bit image of a float (-0 below +0)
-__device__ __forceinline__ uint32_t ord32(float v) {
-  const uint32_t b = __float_as_uint(v);
-  return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
-}
-__device__ __forceinline__ float unord32(uint32_t o) {
-  return __uint_as_float((o & 0x80000000u) ? (o & 0x7FFFFFFFu) : ~o);
-}
-
 // One vector of logits as words: bf16 pairs or floats.
 template <typename T> struct Elem;
 template <> struct Elem<uint16_t> {
   static constexpr int N = 8;
+  __device__ static float value(uint16_t x) { return bf16_to_f32(x); }
   static constexpr uint32_t NONE = 0xFF80FF80u;
   __device__ static void pair(const uint4& v, int i, float& a, float& b) {
     const uint32_t w = i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w;
@@ -319,6 +398,18 @@ template <> struct Elem<uint16_t> {
     asm("max.bf16x2 %0, %1, %2;" : "=r"(m) : "r"(v.x), "r"(v.y));
     asm("max.bf16x2 %0, %1, %2;" : "=r"(n) : "r"(v.z), "r"(v.w));
     asm("max.bf16x2 %0, %1, %2;" : "=r"(m) : "r"(m), "r"(n));
+    return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xFFFF0000u));
+  }
+  __device__ static float vmax(const uint4 (&v)[BS_U]) {
+    uint32_t m = NONE, n = NONE;
+#pragma unroll
+    for (int u = 0; u < BS_U; ++u) {
+      asm("max.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(v[u].x));
+      asm("max.bf16x2 %0, %0, %1;" : "+r"(n) : "r"(v[u].y));
+      asm("max.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(v[u].z));
+      asm("max.bf16x2 %0, %0, %1;" : "+r"(n) : "r"(v[u].w));
+    }
+    asm("max.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(n));
     return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xFFFF0000u));
   }
   __device__ static uint4 gather(const uint16_t* p, int live) {      // the first `live` of a vector
@@ -334,6 +425,7 @@ template <> struct Elem<uint16_t> {
 };
 template <> struct Elem<float> {
   static constexpr int N = 4;
+  __device__ static float value(float x) { return x; }
   static constexpr uint32_t NONE = 0xFF800000u;
   __device__ static void pair(const uint4& v, int i, float& a, float& b) {
     a = __uint_as_float(i == 0 ? v.x : v.z);
@@ -342,6 +434,12 @@ template <> struct Elem<float> {
   __device__ static float vmax(const uint4& v) {
     return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)),
                  fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
+  }
+  __device__ static float vmax(const uint4 (&v)[BS_U]) {
+    float m = vmax(v[0]);
+#pragma unroll
+    for (int u = 1; u < BS_U; ++u) m = fmaxf(m, vmax(v[u]));
+    return m;
   }
   __device__ static uint4 gather(const float* p, int live) {
     uint32_t w[4] = {NONE, NONE, NONE, NONE};
@@ -374,41 +472,92 @@ __device__ __forceinline__ void load_chunk(const T* __restrict__ row, int begin,
   }
 }
 
-// Bound by HBM: 16 bytes a lane and load, the next chunk's four in flight while this one is summed;
-// no shared memory, no barrier.
+// Bound by HBM. A warp's chunks lie one after the other; each lane copies its own 128 bytes of a chunk
+// into its own part of a ring in shared memory, two chunks ahead, and reads back only what it copied:
+// 128 KB a SM in flight, no registers for it and no barrier.
 template <typename T>
-__global__ void __launch_bounds__(BS_THREADS, 1024 / BS_THREADS)
-beam_stream_kernel(const T* __restrict__ logits, int rows, const float* __restrict__ scores,
-                   const uint8_t* __restrict__ done, BeamCut cut, float* __restrict__ maxima,
+__global__ void __launch_bounds__(BS_THREADS, BS_CTAS)
+beam_stream_kernel(const T* __restrict__ logits, unsigned rows, const float* __restrict__ scores,
+                   const uint8_t* __restrict__ done, const BeamCut cut, float* __restrict__ maxima,
                    SumRec* __restrict__ sums) {
   pdl_wait();
+  constexpr int N = Elem<T>::N;
+  constexpr unsigned STAGE = BS_U * 32;
+  extern __shared__ uint4 ring[];
   const int lane = threadIdx.x & 31;
-  const long long wid = (long long)blockIdx.x * (BS_THREADS / 32) + (threadIdx.x >> 5);
-  const long long total = (long long)rows * cut.chunks;
-  long long at = wid * cut.per_warp;
-  const long long stop = min(total, at + cut.per_warp);
-  while (at < stop) {
-    const int row = (int)(at / cut.chunks);
-    const int c0 = (int)(at - (long long)row * cut.chunks);
-    const int c1 = (int)min((long long)cut.chunks, c0 + (stop - at));
-    at += c1 - c0;
-    if (!(scores[row] > -INFINITY) || (done && done[row])) continue;
-    const T* rp = logits + (size_t)row * cut.V;
-    float s = 0.f, lost = 0.f, e = -INFINITY;         // e is the same in all lanes
-    uint4 cur[BS_U], nxt[BS_U];
-    int b, en;
-    cut.range(row, c0, b, en);
-    load_chunk<T>(rp, b, en, lane, cur);
-    for (int c = c0; c < c1; ++c) {
-      if (c + 1 < c1) {
-        cut.range(row, c + 1, b, en);
-        load_chunk<T>(rp, b, en, lane, nxt);
-      }
-      float m = Elem<T>::vmax(cur[0]);
+  uint4* mine = ring + (threadIdx.x >> 5) * (BS_STAGES * STAGE) + lane;
+  const unsigned wid = blockIdx.x * (BS_THREADS / 32) + (threadIdx.x >> 5);
+  const unsigned chunks = (unsigned)cut.chunks, total = rows * chunks;
+  const unsigned begin = wid * (unsigned)cut.per_warp, stop = min(total, begin + (unsigned)cut.per_warp);
+  if (begin >= total) return;
+
+  // A row as a run of chunks: its first full chunk's logits, and how many full ones follow (shorter
+  // ones, at the row's ends, are loaded when they are summed).
+  struct Row {
+    const T* full;
+    unsigned first, count;
+    bool live;
+  };
+  auto open = [&](unsigned row) {
+    Row x;
+    const int h = cut.head(row);
+    x.live = scores[row] > -INFINITY && !(done && done[row]);
+    x.full = logits + (size_t)row * cut.V + h;
+    x.first = (unsigned)cut.odd;
+    x.count = (unsigned)(cut.V - h) / (unsigned)cut.size;
+    return x;
+  };
+  unsigned row = begin / chunks, c = begin - row * chunks;
+  Row here = open(row);
+
+  // the copying side, ahead of the summing one
+  unsigned at = begin, crow = row, cc = c, cstage = 0;
+  Row ahead = here;
+  const T* src = ahead.full + (size_t)(cc < ahead.first ? 0u : cc - ahead.first) * cut.size + lane * N;
+  // (sure: the row is live, or that is not known yet and the copy does not wait for it)
+  auto copy = [&](bool sure) {
+    if (at < stop) {
+      if (cc - ahead.first < ahead.count && (sure || ahead.live)) {
+        const uint32_t dst = (uint32_t)__cvta_generic_to_shared(mine + cstage * STAGE);
 #pragma unroll
-      for (int u = 1; u < BS_U; ++u) m = fmaxf(m, Elem<T>::vmax(cur[u]));
-      m = unord32(__reduce_max_sync(FULL, ord32(m)));
-      if (lane == 0) maxima[(size_t)row * cut.chunks + c] = m;
+        for (int u = 0; u < BS_U; ++u)
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + u * 512),
+                       "l"(src + u * 32 * N)
+                       : "memory");
+      }
+      if (cc >= ahead.first) src += cut.size;
+      ++at;
+      if (++cc == chunks) {
+        cc = 0;
+        if (at < stop) {
+          ahead = open(++crow);
+          src = ahead.full + lane * N;
+        }
+      }
+    }
+    cstage = cstage + 1 == BS_STAGES ? 0 : cstage + 1;
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+#pragma unroll
+  for (int i = 0; i < BS_STAGES - 1; ++i) copy(true);
+
+  unsigned stage = 0;
+  float s = 0.f, lost = 0.f, e = -INFINITY;             // e is the same in all lanes
+  for (unsigned i = begin; i < stop; ++i) {
+    copy(false);
+    asm volatile("cp.async.wait_group %0;" ::"n"(BS_STAGES - 1) : "memory");
+    if (here.live) {
+      uint4 raw[BS_U];
+      if (c - here.first < here.count) {
+#pragma unroll
+        for (int u = 0; u < BS_U; ++u) raw[u] = mine[stage * STAGE + u * 32];
+      } else {
+        int b, en;
+        cut.range(row, (int)c, b, en);
+        load_chunk<T>(logits + (size_t)row * cut.V, b, en, lane, raw);
+      }
+      const float m = unord32(__reduce_max_sync(FULL, ord32(Elem<T>::vmax(raw))));
+      if (lane == 0) maxima[i] = m;
       const float ce = ceilf(m * LOG2E);
       if (ce > e) {
         const float f = e == -INFINITY ? 1.f : pow2_whole(e - ce);   // before: 0, or NaN
@@ -416,44 +565,95 @@ beam_stream_kernel(const T* __restrict__ logits, int rows, const float* __restri
         lost *= f;
         e = ce;
       }
-      // arguments x log2(e) - e with log2(e) in two parts; -inf adds 0, NaN stays
+      // terms 2^(x LOG2E - e); -inf adds 0, NaN stays
       const float ref = e == -INFINITY ? 0.f : e;
-      const uint64_t hi = pack2(LOG2E, LOG2E), lo = pack2(LOG2E_LO, LOG2E_LO), nm = pack2(-ref, -ref);
-      uint64_t a0 = pack2(0.f, 0.f), a1 = a0;
+      float p0 = 0.f, p1 = 0.f, p2 = 0.f, p3 = 0.f;
 #pragma unroll
       for (int u = 0; u < BS_U; ++u)
 #pragma unroll
-        for (int i = 0; i < Elem<T>::N / 2; ++i) {
+        for (int k = 0; k < N / 2; ++k) {
           float x0, x1;
-          Elem<T>::pair(cur[u], i, x0, x1);
-          const uint64_t x = pack2(x0, x1);
-          unpack2(fma2(x, lo, fma2(x, hi, nm)), x0, x1);
-          const uint64_t p = pack2(ex2(x0), ex2(x1));
-          if (i & 1) a1 = add2(a1, p); else a0 = add2(a0, p);
+          Elem<T>::pair(raw[u], k, x0, x1);
+          x0 = ex2(fmaf(x0, LOG2E, -ref));
+          x1 = ex2(fmaf(x1, LOG2E, -ref));
+          if (k & 1) { p2 += x0; p3 += x1; } else { p0 += x0; p1 += x1; }
         }
-      float p0, p1, p2, p3;
-      unpack2(a0, p0, p1);
-      unpack2(a1, p2, p3);
-      // what the running sum's additions lose is kept beside it
-      const float add = (p0 + p1) + (p2 + p3), t = s + add, bb = t - s;
-      lost += (s - (t - bb)) + (add - bb);
-      s = t;
-#pragma unroll
-      for (int u = 0; u < BS_U; ++u) cur[u] = nxt[u];
+      // LOG2E is log2(e) to 2^-26, so a term wants (1 + x LOG2E_REST) more; x of the terms that count is
+      // the chunk's largest or a few below it, and 1e-8 times those few is what this leaves
+      const float part = (p0 + p1) + (p2 + p3);
+      add_pair(s, lost, part, e == -INFINITY ? 0.f : part * (m * LOG2E_REST));
     }
-    double d = (double)s + (double)lost;
+    stage = stage + 1 == BS_STAGES ? 0 : stage + 1;
+    if (++c == chunks || i + 1 == stop) {               // the warp's last chunk of this row
+      if (here.live) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) d += __shfl_xor_sync(FULL, d, o);
-    if (lane == 0) {
-      const long long first = (long long)row * cut.chunks / cut.per_warp;
-      SumRec* rec = sums + (size_t)row * cut.slots + (wid - first);
-      rec->s = d;
-      rec->e = e;
+        for (int o = 16; o > 0; o >>= 1)
+          add_pair(s, lost, __shfl_xor_sync(FULL, s, o), __shfl_xor_sync(FULL, lost, o));
+        if (lane == 0)
+          *reinterpret_cast<float4*>(sums + (size_t)row * cut.slots +
+                                     (wid - row * chunks / (unsigned)cut.per_warp)) =
+              make_float4(s, lost, e, 0.f);
+      }
+      s = lost = 0.f;
+      e = -INFINITY;
+      c = 0;
+      if (i + 1 < stop) here = open(++row);
     }
   }
 }
 
-// One CTA a request: normalisers, the n chunks to look at, their elements, the n best.
+// More than n of a chunk's elements reach the bound (equal logits, or a row that falls steadily): its
+// first n, by a search over the bits of the n-th largest value; of those equal to it the lowest ids.
+// hot: this lane's elements (element j of vector u: bit u * N + j), at: the chunk's first.
+template <typename T>
+__device__ __noinline__ uint64_t chunk_first(const T* __restrict__ at, uint64_t hot, int n, int lane) {
+  constexpr int N = Elem<T>::N;
+  auto image = [&](int bit) {
+    return ord32(Elem<T>::value(at[((bit / N) * 32 + lane) * N + bit % N]) + 0.f);   // -0 to +0
+  };
+  uint32_t nth = 0;
+  for (int b = 31; b >= 0; --b) {
+    const uint32_t t = nth | (1u << b);
+    int cnt = 0;
+    for (uint64_t h = hot; h; h &= h - 1) cnt += image(__ffsll((long long)h) - 1) >= t ? 1 : 0;
+    if (__reduce_add_sync(FULL, cnt) >= n) nth = t;
+  }
+  uint64_t above = 0, equal = 0;
+  for (uint64_t h = hot; h; h &= h - 1) {
+    const int j = __ffsll((long long)h) - 1;
+    const uint32_t o = image(j);
+    if (o > nth) above |= 1ull << j;
+    if (o == nth) equal |= 1ull << j;
+  }
+  int room = n - __reduce_add_sync(FULL, __popcll(above));
+  for (int u = 0; u < BS_U; ++u) {
+    const uint64_t mask = (N == 8 ? 0xFFull : 0xFull) << (u * N);
+    const int mine = __popcll(equal & mask);
+    int before = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(FULL, before, o);
+      if (lane >= o) before += x;
+    }
+    const int all = __shfl_sync(FULL, before, 31);
+    int left = room - (before - mine);
+    for (uint64_t h = equal & mask; h; h &= h - 1, --left)
+      if (left <= 0) equal &= ~(1ull << (__ffsll((long long)h) - 1));
+    room -= all;
+  }
+  return above | equal;
+}
+
+constexpr int BC_MAX = 4, BC_REC = 4;          // maxima, records of a lane loaded together
+
+__device__ __forceinline__ void load_maxima(const float* __restrict__ p, int c0, int chunks,
+                                            float (&v)[BC_MAX]) {
+#pragma unroll
+  for (int u = 0; u < BC_MAX; ++u) v[u] = c0 + 32 * u < chunks ? p[c0 + 32 * u] : -INFINITY;
+}
+
+// One CTA a request: normalisers, the n chunks to look at, their elements, the n best. Bound by
+// latency: what the phases cost is loads one after the other, barriers and instructions first met.
 template <typename T>
 __global__ void __launch_bounds__(BC_THREADS)
 beam_choose_kernel(const T* __restrict__ logits, int W, const float* __restrict__ scores,
@@ -463,83 +663,141 @@ beam_choose_kernel(const T* __restrict__ logits, int W, const float* __restrict_
   constexpr int N = Elem<T>::N;
   constexpr int NW = BC_THREADS / 32;
   constexpr int CAND = LILICORR_MAX_K * LILICORR_MAX_K;
-  __shared__ double s_lse[LILICORR_MAX_BEAMS];
-  __shared__ float s_score[LILICORR_MAX_BEAMS];
+  __shared__ float2 s_base[LILICORR_MAX_BEAMS];         // score - normaliser, as a pair
   __shared__ uint8_t s_kind[LILICORR_MAX_BEAMS];        // 0 absent, 1 live, 2 done
-  __shared__ float s_base[LILICORR_MAX_BEAMS];          // score - lse, to fp32
+  // a lane's largest chunk maximum of a row, while chunks are chosen; the candidates after that
+  __shared__ union {
+    float lanes[LILICORR_MAX_BEAMS][32];
+    struct { uint64_t key[CAND], at[CAND]; } cand;
+  } s_u;
+  auto& s_lane = s_u.lanes;
+  auto& s_key = s_u.cand.key;
+  auto& s_at = s_u.cand.at;
   __shared__ RankShared sh;
   __shared__ uint64_t s_ckey[LILICORR_MAX_K], s_cpos[LILICORR_MAX_K];
-  __shared__ uint64_t s_key[CAND], s_at[CAND];
   __shared__ int s_cand;
-  __shared__ uint32_t s_scale;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = blockIdx.x;
   const size_t row0 = (size_t)r * W;
-  if (tid == 0) { s_cand = 0; s_scale = 0u; }
-  __syncthreads();
+  const float* mx = maxima + row0 * cut.chunks;
+  if (tid == 0) s_cand = 0;
 
+  // a warp a row: its normaliser from the records, and each lane's best chunk; of all its rows this
+  // thread's best
+  uint64_t best_key = 0ull, best_pos = ~0ull;
   for (int w = warp; w < W; w += NW) {
-    const float sc = scores[row0 + w];
     const size_t row = row0 + w;
-    int kind = !(sc > -INFINITY) ? 0 : (done && done[row]) ? 2 : 1;
-    bool bad = sc != sc || sc == INFINITY;
-    double lse = 0.0;
-    if (kind == 1) {
-      const long long first = (long long)row * cut.chunks / cut.per_warp;
-      const int count = (int)(((long long)(row + 1) * cut.chunks - 1) / cut.per_warp - first) + 1;
-      float e = -INFINITY;
-      double s = 0.0;
-      for (int i = lane; i < count; i += 32) {
-        const SumRec x = sums[row * cut.slots + i];
-        const float big = fmaxf(e, x.e);
-        s = (e == -INFINITY ? s : s * (double)pow2_whole(e - big)) +
-            (x.e == -INFINITY ? x.s : x.s * (double)pow2_whole(x.e - big));
-        e = big;
-      }
-      const float E = warp_max(e);
-      s = e == -INFINITY ? s : s * (double)pow2_whole(e - E);
+    // every load at once: what a row that is not live left there is not used
+    const float sc = scores[row];
+    const bool over = done && done[row];
+    const unsigned g0 = (unsigned)row * (unsigned)cut.chunks, first = g0 / (unsigned)cut.per_warp;
+    const int count = (int)((g0 + (unsigned)cut.chunks - 1) / (unsigned)cut.per_warp - first) + 1;
+    const float4* rec = reinterpret_cast<const float4*>(sums + row * cut.slots);
+    float4 x[BC_REC];
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(FULL, s, o);
-      lse = (double)E * 0.69314718055994530942 + log(s);
-      if (!isfinite(lse)) bad = true;
+    for (int u = 0; u < BC_REC; ++u)
+      x[u] = lane + 32 * u < count ? rec[lane + 32 * u] : make_float4(0.f, 0.f, -INFINITY, 0.f);
+    float best = -INFINITY, hi = sc, lo = 0.f;
+    int at = 0;
+    for (int c0 = lane; c0 < cut.chunks; c0 += 32 * BC_MAX) {
+      float v[BC_MAX];
+      load_maxima(mx + (size_t)w * cut.chunks, c0, cut.chunks, v);
+#pragma unroll
+      for (int u = 0; u < BC_MAX; ++u)
+        if (v[u] > best) { best = v[u]; at = c0 + 32 * u; }
+    }
+    int kind = !(sc > -INFINITY) ? 0 : over ? 2 : 1;
+    bool bad = sc != sc || sc == INFINITY;
+    if (kind == 1) {
+      float e = x[0].z, s = x[0].x, c = x[0].y;
+      auto add = [&](const float4& y) {
+        const float big = fmaxf(e, y.z);
+        const float f = e == -INFINITY ? 1.f : pow2_whole(e - big);
+        const float g = y.z == -INFINITY ? 1.f : pow2_whole(y.z - big);
+        s *= f;
+        c *= f;
+        add_pair(s, c, y.x * g, y.y * g);
+        e = big;
+      };
+#pragma unroll
+      for (int u = 1; u < BC_REC; ++u)
+        if (32 * u < count) add(x[u]);
+      for (int i = lane + 32 * BC_REC; i < count; i += 32) add(rec[i]);
+      const float E = warp_max(e), f = e == -INFINITY ? 1.f : pow2_whole(e - E);
+      s *= f;
+      c *= f;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1)
+        add_pair(s, c, __shfl_xor_sync(FULL, s, o), __shfl_xor_sync(FULL, c, o));
+      if (!(s > 0.f && s < INFINITY && E > -INFINITY && E < INFINITY)) bad = true;
+      float lh, ll;
+      log_pair(s, c, E, lh, ll);
+      add_pair(hi, lo, -lh, -ll);
+    } else {
+      best = kind == 2 && lane == 0 ? 0.f : -INFINITY;  // the one candidate of a beam that is done
+      at = 0;
     }
     if (bad) kind = 0;
+    if (kind == 0) best = -INFINITY;
+    s_lane[w][lane] = best;
     if (lane == 0) {
       if (bad) set_status(status, LILICORR_ERR_NONFINITE);
-      const float base = kind == 0 ? -INFINITY : (float)((double)sc - lse);
-      s_lse[w] = lse;
-      s_score[w] = sc;
-      s_base[w] = base;
+      s_base[w] = make_float2(hi, lo);
       s_kind[w] = (uint8_t)kind;
-      if (kind) atomicMax(&s_scale, __float_as_uint(fabsf(base)));
+    }
+    const uint64_t key = best == -INFINITY ? 0ull : sum_key(hi, lo, best);
+    const uint64_t pos = ((uint64_t)w << 32) | (uint32_t)at;
+    if (precedes(key, pos, best_key, best_pos)) { best_key = key; best_pos = pos; }
+  }
+
+  // the first n chunks, by their largest total; a done beam is one chunk of one candidate
+  rank_bound<BC_THREADS>(sh, out.n, best_key, best_pos);
+  const uint64_t bound = sh.bound;
+  for (int w = warp; w < W; w += NW) {
+    const float2 base = s_base[w];
+    const float v = s_lane[w][lane];
+    // by the logit first, with a margin for the rounding
+    const float need = key_score(bound);
+    const float thr = bound == 1ull ? -INFINITY
+                                    : (need - base.x) - 0x1p-20f * (fabsf(need) + fabsf(base.x));
+    if (v == -INFINITY || v < thr) continue;             // nor any other of the lane's
+    const uint64_t pos = (uint64_t)w << 32;
+    if (s_kind[w] == 2) {
+      rank_keep(sh, sum_key(base.x, base.y, 0.f), pos);
+      continue;
+    }
+    for (int c0 = lane; c0 < cut.chunks; c0 += 32 * BC_MAX) {
+      float x[BC_MAX];
+      load_maxima(mx + (size_t)w * cut.chunks, c0, cut.chunks, x);
+#pragma unroll
+      for (int u = 0; u < BC_MAX; ++u) {
+        if (x[u] >= thr && x[u] > -INFINITY)
+          rank_keep(sh, sum_key(base.x, base.y, x[u]), pos | (uint32_t)(c0 + 32 * u));
+      }
     }
   }
   __syncthreads();
-
-  // the first n chunks, by their largest total; a done beam is one chunk of one candidate
-  const int M = W * cut.chunks;
-  const float* mx = maxima + row0 * cut.chunks;
-  bool ignore = false;
-  const int taken = rank_first<BC_THREADS>(
-      sh, M, out.n, __uint_as_float(s_scale),
-      [&](int i) {
-        const int w = i / cut.chunks;
-        if (s_kind[w] == 2) return i == w * cut.chunks ? s_base[w] : -INFINITY;
-        return s_kind[w] ? s_base[w] + mx[i] : -INFINITY;
-      },
-      [&](int i) -> uint64_t {
-        const int w = i / cut.chunks;
-        if (s_kind[w] == 2) return total_key((double)s_score[w], ignore);
-        return total_key((double)s_score[w] + ((double)mx[i] - s_lse[w]), ignore);
-      },
-      [&](int i) { return (uint64_t)i; },
-      [&](int rank, uint64_t key, uint64_t p) {
-        s_ckey[rank] = key;
-        s_cpos[rank] = p;
-      });
+  auto take = [&](int rank, uint64_t key, uint64_t p) {
+    s_ckey[rank] = key;
+    s_cpos[rank] = p;
+  };
+  int taken = rank_kept<BC_THREADS>(sh, out.n, take);
+  if (taken < 0) {
+    rank_rounds<BC_THREADS>(
+        sh, W * cut.chunks, out.n,
+        [&](int i) -> uint64_t {
+          const int w = i / cut.chunks;
+          if (s_kind[w] == 0 || (s_kind[w] == 2 && i != w * cut.chunks)) return 0ull;
+          const float x = s_kind[w] == 2 ? 0.f : mx[i];
+          return x > -INFINITY ? sum_key(s_base[w].x, s_base[w].y, x) : 0ull;
+        },
+        [&](int i) { return ((uint64_t)(i / cut.chunks) << 32) | (uint32_t)(i % cut.chunks); }, take);
+    taken = out.n;
+  }
   __syncthreads();
-  const double least = taken == out.n ? unord64(s_ckey[taken - 1]) : -INFINITY;
+  const uint64_t least = taken == out.n ? s_ckey[taken - 1] : 1ull;
   for (int c = warp; c < taken; c += NW) {
-    const int i = (int)s_cpos[c], w = i / cut.chunks;
+    const uint64_t cpos = s_cpos[c];
+    const int w = (int)(cpos >> 32);
     const size_t row = row0 + w;
     if (s_kind[w] == 2) {
       if (lane == 0) {
@@ -550,87 +808,43 @@ beam_choose_kernel(const T* __restrict__ logits, int W, const float* __restrict_
       continue;
     }
     int b, en;
-    cut.range(row, i - w * cut.chunks, b, en);
+    cut.range(row, (int)(uint32_t)cpos, b, en);
     uint4 raw[BS_U];
-    load_chunk<T>(logits + row * cut.V, b, en, lane, raw);
-    const double sc = (double)s_score[w], lse = s_lse[w];
-    // an element whose total reaches `least`, by its logit with a margin for the rounding
-    const double x0 = least - sc + lse;
-    const float thr = x0 == -INFINITY ? -INFINITY : (float)(x0 - 1e-5 * (1.0 + fabs(x0)));
-    uint32_t hot = 0;                                   // element j of vector u: bit u * N + j
+    const T* rp = logits + row * cut.V;
+    load_chunk<T>(rp, b, en, lane, raw);
+    const float2 base = s_base[w];
+    // elements whose total may reach `least`: by the logit, with a margin for the rounding
+    const float need = key_score(least);
+    const float thr = taken < out.n ? -INFINITY
+                                    : (need - base.x) - 0x1p-20f * (fabsf(need) + fabsf(base.x));
+    uint64_t hot = 0;                                   // element j of vector u: bit u * N + j
 #pragma unroll
-    for (int u = 0; u < BS_U; ++u)
+    for (int u = 0; u < BS_U; ++u) {
+      if (!__any_sync(FULL, Elem<T>::vmax(raw[u]) >= thr)) continue;
 #pragma unroll
       for (int j = 0; j < N / 2; ++j) {
-        float a, d;
-        Elem<T>::pair(raw[u], j, a, d);
-        hot |= (a >= thr && a > -INFINITY ? 1u : 0u) << (u * N + 2 * j);
-        hot |= (d >= thr && d > -INFINITY ? 1u : 0u) << (u * N + 2 * j + 1);
+        float x0, x1;
+        Elem<T>::pair(raw[u], j, x0, x1);
+        hot |= (x0 >= thr && x0 > -INFINITY ? 1ull : 0ull) << (u * N + 2 * j);
+        hot |= (x1 >= thr && x1 > -INFINITY ? 1ull : 0ull) << (u * N + 2 * j + 1);
       }
-    auto value = [&](int bit) {
-      float v = 0.f;
-#pragma unroll
-      for (int u = 0; u < BS_U; ++u)
-#pragma unroll
-        for (int j = 0; j < N / 2; ++j) {
-          float a, d;
-          Elem<T>::pair(raw[u], j, a, d);
-          if (bit == u * N + 2 * j) v = a;
-          if (bit == u * N + 2 * j + 1) v = d;
-        }
-      return v + 0.f;                                   // -0 to +0
-    };
-    const int hits = __reduce_add_sync(FULL, __popc(hot));
-    if (hits > out.n) {
-      // more than n in one chunk (equal logits, or a row that falls steadily): its n first, by a
-      // search over the bits of the n-th largest value; of those equal to it the lowest ids
-      uint32_t nth = 0;
-      for (int bit = 31; bit >= 0; --bit) {
-        const uint32_t t = nth | (1u << bit);
-        int cnt = 0;
-        for (uint32_t h = hot; h; h &= h - 1) cnt += ord32(value(__ffs(h) - 1)) >= t ? 1 : 0;
-        if (__reduce_add_sync(FULL, cnt) >= out.n) nth = t;
-      }
-      uint32_t above = 0, equal = 0;
-      for (uint32_t h = hot; h; h &= h - 1) {
-        const int j = __ffs(h) - 1;
-        const uint32_t o = ord32(value(j));
-        if (o > nth) above |= 1u << j;
-        if (o == nth) equal |= 1u << j;
-      }
-      int room = out.n - __reduce_add_sync(FULL, __popc(above));
-      for (int u = 0; u < BS_U; ++u) {
-        const uint32_t mask = ((N == 8 ? 0xFFu : 0xFu) << (u * N));
-        const int mine = __popc(equal & mask);
-        int before = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const int x = __shfl_up_sync(FULL, before, o);
-          if (lane >= o) before += x;
-        }
-        const int all = __shfl_sync(FULL, before, 31);
-        int left = room - (before - mine);
-        for (uint32_t h = equal & mask; h; h &= h - 1, --left)
-          if (left <= 0) equal &= ~(1u << (__ffs(h) - 1));
-        room -= all;
-      }
-      hot = above | equal;
     }
-    for (uint32_t h = hot; h; h &= h - 1) {
-      const int j = __ffs(h) - 1;
+    if (__reduce_add_sync(FULL, __popcll(hot)) > out.n) hot = chunk_first<T>(rp + b, hot, out.n, lane);
+    for (uint64_t h = hot; h; h &= h - 1) {
+      const int j = __ffsll((long long)h) - 1, id = b + ((j / N) * 32 + lane) * N + j % N;
+      const uint64_t key = sum_key(base.x, base.y, Elem<T>::value(rp[id]));
+      if (key < least) continue;
       const int at = atomicAdd(&s_cand, 1);
-      bool no = false;
-      s_key[at] = total_key(sc + ((double)value(j) - lse), no);
-      s_at[at] = ((uint64_t)w << 32) | (uint32_t)(b + ((j / N) * 32 + lane) * N + j % N);
+      s_key[at] = key;
+      s_at[at] = ((uint64_t)w << 32) | (uint32_t)id;
     }
   }
   __syncthreads();
   const int found = rank_first<BC_THREADS>(
-      sh, s_cand, out.n, 0.f, [&](int i) { return (float)unord64(s_key[i]); },
-      [&](int i) { return s_key[i]; }, [&](int i) { return s_at[i]; },
+      sh, s_key, s_cand, out.n, [&](int i) { return s_at[i]; },
       [&](int rank, uint64_t key, uint64_t p) {
         const int w = (int)(p >> 32);
-        out.put(r, rank, key, w, (int32_t)(uint32_t)p, s_kind[w] == 2);
+        out.put(r, rank, key_score(key), w, (int32_t)(uint32_t)p, s_kind[w] == 2);
       });
   for (int i = found + tid; i < out.n; i += BC_THREADS) out.none(r, i);  // fewer candidates than n
 }
@@ -717,8 +931,11 @@ lilicorr_status_t run_select(const T* logits, lilicorr_dtype_t dt, int requests,
   SumRec* sums = reinterpret_cast<SumRec*>(
       w + 256 + align_up((size_t)rows * cut.chunks * sizeof(float), 256));
   const long long warps = ((long long)rows * cut.chunks + cut.per_warp - 1) / cut.per_warp;
-  LL_TRY(launch_k(beam_stream_kernel<T>, ceil_div(warps, BS_THREADS / 32), BS_THREADS, 0, st, logits,
-                  rows, scores, done, cut, maxima, sums));
+  static bool configured[64] = {false};
+  LL_TRY(allow_max_dynamic_smem(beam_stream_kernel<T>, configured));
+  LL_TRY(launch_k(beam_stream_kernel<T>, ceil_div(warps, BS_THREADS / 32), BS_THREADS,
+                  (size_t)BS_THREADS * BS_STAGES * BS_U * sizeof(uint4), st, logits, (unsigned)rows,
+                  scores, done, cut, maxima, sums));
   return launch_k(beam_choose_kernel<T>, requests, BC_THREADS, 0, st, logits, W, scores, done, cut,
                   maxima, sums, out, reinterpret_cast<uint32_t*>(w));
 }
@@ -737,7 +954,8 @@ extern "C" {
 size_t lilicorr_beam_select_workspace_bytes(int requests, int beams, int V, int n) {
   if (!beam_shape_ok(requests, beams, n) || V <= 0 || n > (long long)beams * V) return 0;
   const long long rows = (long long)requests * beams;
-  if (rows > 65535) return 0;
+  // (chunks of 4 KB: 2^31 of them are more than the device holds)
+  if (rows > 65535 || rows * (V / 1024 + 2ll) >= 0x7FFFFFFFll) return 0;
   const size_t a = select_ws_bytes((int)rows, V, LILICORR_F32);
   const size_t b = select_ws_bytes((int)rows, V, LILICORR_BF16);
   return a > b ? a : b;
