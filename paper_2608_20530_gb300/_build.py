@@ -17,7 +17,8 @@ LIB = os.path.join(LIBDIR, "liblilicorr.so")
 SOURCES = ["api.cu", "topk_lse.cu", "head_kernels.cu", "pair_walk.cu", "gemm_tc.cu",
            "attention_tc.cu", "attention_umma.cu", "net_fused.cu",
            "diagnostics.cu", "gemm_small.cu", "gemm_split.cu", "lm_head.cu",
-           "net_cluster.cu", "net_pair.cu", "beam.cu", "prefix_attention.cu"]
+           "net_cluster.cu", "net_pair.cu", "beam.cu", "prefix_attention.cu",
+           "prefix_attention_tc.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr",
          "-I", INCLUDE, "-I", CSRC]

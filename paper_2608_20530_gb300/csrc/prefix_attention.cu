@@ -412,21 +412,46 @@ pa_combine_kernel(const PaArgs a) {
   const size_t nt = row / a.Hq;
   const int t = (int)(nt % a.T), n = (int)(nt / a.T);
   if (a.seq_len[n] < 0) return;                   // no such sequence: its rows stay as they are
+  // pieces of the row: the segments of its item, then the slots
+  int segs = 0;
+  size_t seg0 = 0;
+  if (a.seg_ctas) {
+    const int g = n / a.W, hk = h / a.rep;
+    const int r = ((n - g * a.W) * a.T + t) * a.rep + (h - hk * a.rep);
+    const uint32_t hb = (uint32_t)a.Hkv * a.seg_blocks;
+    const uint32_t before = a.seg_start[g], tiles = a.seg_start[g + 1] - before;
+    if (tiles) {
+      const uint32_t per = pa_per_cta(a.seg_start[a.G] * hb, a.seg_ctas);
+      const uint32_t in = (uint32_t)hk * a.seg_blocks + r / PA_BLOCK;
+      const uint32_t first = before * hb + in * tiles;
+      const uint32_t c0 = first / per, c1 = (first + tiles - 1) / per;
+      segs = (int)(c1 - c0) + 1;
+      seg0 = ((size_t)c0 + (size_t)g * hb + in) * PA_BLOCK + r % PA_BLOCK;
+    }
+  }
+  const int pieces = segs + a.slots;
+  auto ml_of = [&](int s) {
+    return s < segs ? a.seg_ml[seg0 + (size_t)s * PA_BLOCK] : a.ml[(size_t)(s - segs) * rows + row];
+  };
+  auto po_of = [&](int s) {
+    return s < segs ? a.seg_po + (seg0 + (size_t)s * PA_BLOCK) * a.d
+                    : a.po + ((size_t)(s - segs) * rows + row) * a.d;
+  };
   float M = -INFINITY;
-  for (int s = lane; s < a.slots; s += 32) M = fmaxf(M, a.ml[s * rows + row].x);
+  for (int s = lane; s < pieces; s += 32) M = fmaxf(M, ml_of(s).x);
   M = warp_max(M);
   const float u = M == -INFINITY ? 0.f : M;
   float L = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int s0 = 0; s0 < a.slots; s0 += 32) {
-    const float2 ml = s0 + lane < a.slots ? a.ml[(s0 + lane) * rows + row] : make_float2(-INFINITY, 0.f);
+  for (int s0 = 0; s0 < pieces; s0 += 32) {
+    const float2 ml = s0 + lane < pieces ? ml_of(s0 + lane) : make_float2(-INFINITY, 0.f);
     const float f = ml.x == -INFINITY ? 0.f : pa_ex2(ml.x - u);
     L += f * ml.y;
-    for (int j = 0; j < min(32, a.slots - s0); ++j) {
+    for (int j = 0; j < min(32, pieces - s0); ++j) {
       const float w = __shfl_sync(0xffffffffu, f, j);
       const float mx = __shfl_sync(0xffffffffu, ml.x, j);
       if (mx == -INFINITY || lane * 4 >= a.d) continue;    // no keys: nothing was written
-      const float4 p = *reinterpret_cast<const float4*>(a.po + ((s0 + j) * rows + row) * a.d + lane * 4);
+      const float4 p = *reinterpret_cast<const float4*>(po_of(s0 + j) + lane * 4);
       o.x = fmaf(w, p.x, o.x);
       o.y = fmaf(w, p.y, o.y);
       o.z = fmaf(w, p.z, o.z);
@@ -499,8 +524,9 @@ lilicorr_status_t launch_pa_combine(const PaArgs& a, lilicorr_dtype_t dt, cudaSt
 namespace {
 
 struct PaPlan {
-  int psplits, ssplits;
-  size_t rows, ml_off, po_off, total;
+  int psplits, ssplits;        // psplits 0: the prefix's pieces are segments
+  int seg_ctas, seg_blocks;
+  size_t rows, ml_off, po_off, start_off, seg_ml_off, seg_po_off, total;
 };
 
 bool stride_ok(const int64_t (&s)[3], const int (&extent)[3], int per16) {
@@ -527,15 +553,27 @@ bool pa_plan(const lilicorr_prefix_attention_desc* d, PaPlan* p) {
     return (int)(n < 1 ? 1 : n > 128 ? 128 : n);
   };
   const long long prow = (long long)d->beams * d->tokens * rep;
+  const bool tc = d->dtype == LILICORR_BF16 && d->prefix_capacity;
+  const long long blocks = (prow + PA_BLOCK - 1) / PA_BLOCK;
+  // (tiles are counted in 32 bits)
+  if (tc && (double)d->groups * d->kv_heads * blocks * ((double)d->prefix_capacity / PA_TILE + 1) >=
+                2147483648.0)
+    return false;
+  p->seg_ctas = tc ? sms : 0;
+  p->seg_blocks = tc ? (int)blocks : 0;
   p->psplits = d->prefix_capacity
                    ? pieces((long long)d->groups * d->kv_heads * ((prow + 63) / 64), d->prefix_capacity)
                    : 0;
   p->ssplits = d->own_capacity ? pieces((long long)d->groups * d->beams * d->kv_heads, d->own_capacity) : 0;
   p->rows = (size_t)rows;
   const size_t slots = (size_t)p->psplits + p->ssplits;
+  const size_t segs = tc ? (size_t)sms + (size_t)d->groups * d->kv_heads * blocks : 0;
   p->ml_off = 256;
   p->po_off = p->ml_off + align_up(slots * p->rows * sizeof(float2), 256);
-  p->total = p->po_off + align_up(slots * p->rows * d->head_dim * sizeof(float), 256);
+  p->start_off = p->po_off + align_up(slots * p->rows * d->head_dim * sizeof(float), 256);
+  p->seg_ml_off = p->start_off + align_up(((size_t)d->groups + 1) * sizeof(uint32_t), 256);
+  p->seg_po_off = p->seg_ml_off + align_up(segs * PA_BLOCK * sizeof(float2), 256);
+  p->total = p->seg_po_off + align_up(segs * PA_BLOCK * d->head_dim * sizeof(float), 256);
   return true;
 }
 
@@ -591,7 +629,11 @@ lilicorr_status_t lilicorr_prefix_attention(const lilicorr_prefix_attention_desc
   a.Hq = desc->q_heads; a.Hkv = desc->kv_heads; a.rep = desc->q_heads / desc->kv_heads;
   a.d = desc->head_dim;
   a.scale_log2 = desc->scale * PA_LOG2E;
-  a.slots = p.psplits + p.ssplits;
+  a.seg_ctas = p.seg_ctas;
+  a.seg_blocks = p.seg_blocks;
+  a.seg_start = reinterpret_cast<uint32_t*>(w + p.start_off);
+  a.seg_ml = reinterpret_cast<float2*>(w + p.seg_ml_off);
+  a.seg_po = reinterpret_cast<float*>(w + p.seg_po_off);
   a.status = reinterpret_cast<uint32_t*>(w);
   a.ml = reinterpret_cast<float2*>(w + p.ml_off);
   a.po = reinterpret_cast<float*>(w + p.po_off);
@@ -609,9 +651,15 @@ lilicorr_status_t lilicorr_prefix_attention(const lilicorr_prefix_attention_desc
   pre.k = prefix_k; pre.v = prefix_v; pre.len = prefix_len;
   pre.capacity = desc->prefix_capacity; pre.splits = p.psplits; pre.slot0 = 0; pre.own = 0;
   own.k = k; own.v = v; own.len = seq_len;
-  own.capacity = desc->own_capacity; own.splits = p.ssplits; own.slot0 = p.psplits; own.own = 1;
+  own.capacity = desc->own_capacity; own.splits = p.ssplits; own.own = 1;
   const bool bf = desc->dtype == LILICORR_BF16;
-  if (has_p) LL_TRY(bf ? launch_pa_mma(a, pre, stream) : launch_pa_simt(a, pre, stream));
+  const bool tc = has_p && bf && pa_tc_takes(a, pre);
+  if (!tc) a.seg_ctas = 0;
+  else pre.splits = 0;
+  own.slot0 = pre.splits;
+  a.slots = pre.splits + own.splits;
+  if (tc) LL_TRY(launch_pa_tc(a, pre, stream));
+  else if (has_p) LL_TRY(bf ? launch_pa_mma(a, pre, stream) : launch_pa_simt(a, pre, stream));
   if (has_s) LL_TRY(bf ? launch_pa_mma(a, own, stream) : launch_pa_simt(a, own, stream));
   return launch_pa_combine(a, desc->dtype, stream);
 }

@@ -3,6 +3,7 @@
 
 #include "internal.cuh"
 
+
 namespace lilicorr {
 
 // One side of the keys: the prefix of each group (shared by its sequences), or each sequence's own.
@@ -26,12 +27,32 @@ struct PaArgs {
   const int32_t* seq_len;      // [N]
   int G, W, T, Hq, Hkv, rep, d;
   float scale_log2;            // scale * log2(e): scores in log2 units
-  int slots;                   // partial results per row
-  float2* ml;                  // [slots][rows] (maximum, sum of 2^(s - maximum)); maximum -inf: none
-  float* po;                   // [slots][rows][d] sums of 2^(s - maximum) V
+  // partial results of a piece of the keys: (maximum, sum of 2^(s - maximum)) and the sums of
+  // 2^(s - maximum) V, fp32; a maximum of -inf: no keys, and no sums were written
+  int slots;                   // pieces per row that are kept by row
+  float2* ml;                  // [slots][rows]
+  float* po;                   // [slots][rows][d]
+  // the prefix's pieces of the tensor-core kernel, kept by segment (PaSegments)
+  int seg_ctas;                // its CTAs (0: the prefix's pieces are among the slots)
+  int seg_blocks;              // blocks of PA_BLOCK rows per (group, key head)
+  float2* seg_ml;              // [segments][PA_BLOCK]
+  float* seg_po;               // [segments][PA_BLOCK][d]
+  uint32_t* seg_start;         // [G + 1] tiles before each group (of one key head and row block)
   uint32_t* status;
   __device__ __host__ size_t rows() const { return (size_t)G * W * T * Hq; }
 };
+
+// The tensor-core kernel's work is the list of all (group, key head, block of PA_BLOCK rows, tile of
+// PA_TILE keys), in that order, cut evenly among its CTAs: CTA b takes tiles [b * per, (b + 1) * per). A
+// segment is what one CTA has of one (group, key head, block) = item; its number is CTA + item, which
+// no other segment has, the list being walked in order.
+constexpr int PA_BLOCK = 256;
+constexpr int PA_TILE = 128;
+constexpr int PA_MIN_TILES = 2;          // of a CTA
+__host__ __device__ __forceinline__ uint32_t pa_per_cta(uint32_t tiles, int ctas) {
+  const uint32_t per = (tiles + ctas - 1) / ctas;
+  return per < PA_MIN_TILES ? PA_MIN_TILES : per;
+}
 
 constexpr float PA_LOG2E = 1.4426950408889634f;
 
@@ -61,6 +82,9 @@ __device__ __forceinline__ float pa_ex2(float x) {
   return y;
 }
 
+// the prefix on the 5th-generation tensor cores (prefix_attention_tc.cu)
+bool pa_tc_takes(const PaArgs& a, const PaKeys& k);
+lilicorr_status_t launch_pa_tc(const PaArgs& a, const PaKeys& k, cudaStream_t st);
 lilicorr_status_t launch_pa_mma(const PaArgs& a, const PaKeys& k, cudaStream_t st);
 lilicorr_status_t launch_pa_simt(const PaArgs& a, const PaKeys& k, cudaStream_t st);
 lilicorr_status_t launch_pa_combine(const PaArgs& a, lilicorr_dtype_t dt, cudaStream_t st);

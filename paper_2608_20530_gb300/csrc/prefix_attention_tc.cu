@@ -1,0 +1,525 @@
+// The shared prefix on the 5th-generation tensor cores (bf16): the rows of all sequences of a group
+// (PA_BLOCK at a time, two tiles of 128) against tiles of 128 of its keys.
+//
+// One CTA an SM. Warp 8 feeds K and V tiles by TMA into two rings. Warp 9 issues
+//   S = Q K^T   (M 128, N 128)   into tensor memory, and
+//   O += P V    (M 128, N d)     with P read from tensor memory, V as the MN-major operand.
+// Warps 0-3 and 4-7 are two streams: a thread a row reads its 128 scores, takes the running maximum,
+// writes P = 2^(s - m) as bf16 over them and keeps the row's sum. While one stream is at its
+// exponentials the tensor cores work for the other. With two row tiles the streams share each key
+// tile; with one they take the key tiles in turn and join at the end.
+//
+// O is not rescaled whenever a maximum grows: m is the maximum that a row's sums are taken against, and
+// it moves only when a score would pass it by 2^8, so that terms stay below 2^8 and sums exact to fp32.
+//
+// What bounds it: bytes of K and V for up to about 256 rows a group (each is read from HBM once and
+// from L2 by the further row blocks), beyond that the two products (512 clocks each of an SM's tensor
+// cores a 128 x 128 tile at d = 128) beside 16,384 exponentials (512 clocks at 32 a clock).
+#include "prefix_attention.cuh"
+#include "tc_ptx.cuh"
+
+namespace lilicorr {
+
+namespace {
+using namespace tc;
+
+constexpr int PT_THREADS = 320;
+constexpr uint32_t PT_CHUNK = 128 * 128;             // 128 rows of 128 bytes
+constexpr long long PT_WAIT = 4000000000ll;          // SM cycles, about 2 s
+constexpr uint32_t PT_TMEM = 512;
+
+template <int DP>
+struct PtCfg {
+  static constexpr int CH = DP / 64;                 // 64-column chunks of a row
+  static constexpr uint32_t TILE = CH * PT_CHUNK;    // bytes of a K, V or Q tile
+  static constexpr int NK = DP == 128 ? 3 : 5, NV = DP == 128 ? 2 : 5;
+  static constexpr size_t SMEM = 1024 + (size_t)(2 + NK + NV) * TILE;
+  // tensor-memory columns: scores, output, and probabilities. At d = 128 the probabilities lie over the
+  // scores they came from: the next scores of the stream are issued behind the product that reads
+  // them, and products of one shape run in the order of issue. At d = 64 the two products differ in
+  // shape, and there is room for the probabilities elsewhere.
+  static constexpr uint32_t S(int s) { return s * 128; }
+  static constexpr uint32_t O(int s) { return 256 + s * DP; }
+  static constexpr uint32_t P(int s) { return DP == 128 ? S(s) : 384 + s * 64; }
+};
+
+// A of the product from tensor memory
+__device__ __forceinline__ void mma_bf16_ta(uint32_t tmem_d, uint32_t tmem_a, uint64_t b, uint32_t idesc,
+                                            uint32_t accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(tmem_d),
+      "r"(tmem_a), "l"(b), "r"(idesc), "r"(accumulate));
+}
+// MN-major operand of 128-byte-swizzled rows: 64-column chunks PT_CHUNK bytes apart, 8-row groups 1024
+__device__ __forceinline__ uint64_t smem_desc_mn(const void* tile) {
+  return smem_desc(tile) & ~(0x3FFFull << 16) | ((uint64_t)(PT_CHUNK >> 4) << 16);
+}
+
+// Where a CTA is in the list of tiles.
+struct Cursor {
+  int g;                       // group
+  uint32_t item;               // key head * blocks + block
+  uint32_t tile;               // of the item
+  uint32_t left;               // tiles of this CTA from here on
+};
+__device__ __forceinline__ int pt_len(const PaKeys& k, int g) {
+  return min(max(k.len[g], 0), k.capacity);
+}
+__device__ __forceinline__ uint32_t pt_tiles(const PaKeys& k, int g) {
+  return (uint32_t)(pt_len(k, g) + PA_TILE - 1) / PA_TILE;
+}
+// The tiles of the segment that starts here; `next` moves behind them.
+__device__ __forceinline__ uint32_t pt_here(const PaKeys& k, const Cursor& c) {
+  return min(c.left, pt_tiles(k, c.g) - c.tile);
+}
+__device__ __forceinline__ void pt_next(const PaArgs& a, const PaKeys& k, Cursor& c, uint32_t here) {
+  c.left -= here;
+  c.tile = 0;
+  if (c.left == 0) return;
+  if (++c.item == (uint32_t)a.Hkv * a.seg_blocks) {
+    c.item = 0;
+    do ++c.g;
+    while (pt_tiles(k, c.g) == 0);
+  }
+}
+
+template <int DP>
+__global__ void __launch_bounds__(PT_THREADS, 1)
+pa_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+             int copies, const PaArgs a, const PaKeys kk, int rows) {
+  using Cfg = PtCfg<DP>;
+  constexpr int NK = Cfg::NK, NV = Cfg::NV;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>(
+      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  uint8_t* sQ = smem;
+  uint8_t* sK = smem + 2 * Cfg::TILE;
+  uint8_t* sV = sK + NK * Cfg::TILE;
+  uint32_t* s_sum = reinterpret_cast<uint32_t*>(sQ);             // before the first Q
+  float* s_o = reinterpret_cast<float*>(sQ);                     // after the last product with Q
+  float2* s_ml = reinterpret_cast<float2*>(s_o + 32 * 128);
+  __shared__ __align__(8) uint64_t k_full[NK], k_empty[NK], v_full[NV], v_empty[NV];
+  __shared__ __align__(8) uint64_t s_ready[2], p_ready[2], o_ready[2];
+  __shared__ uint32_t tmem_base;
+  __shared__ volatile int abort_flag;
+  __shared__ Cursor s_cur;
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    for (int i = 0; i < NK; ++i) { mbar_init(&k_full[i], 1); mbar_init(&k_empty[i], 1); }
+    for (int i = 0; i < NV; ++i) { mbar_init(&v_full[i], 1); mbar_init(&v_empty[i], 1); }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&s_ready[i], 1);
+      mbar_init(&p_ready[i], 4);
+      mbar_init(&o_ready[i], 1);
+    }
+    abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 9) tmem_alloc(&tmem_base, PT_TMEM);
+  pdl_wait();
+
+  // ---- this CTA's part of the list: tiles of each thread's run of groups, their scan
+  const uint32_t hb = (uint32_t)a.Hkv * a.seg_blocks;
+  const int run = (a.G + PT_THREADS - 1) / PT_THREADS;
+  const int ga = min(a.G, tid * run), gb = min(a.G, ga + run);
+  uint32_t mine = 0;
+  for (int g = ga; g < gb; ++g) mine += pt_tiles(kk, g);
+  s_sum[tid] = mine;
+  if (tid == 0) s_cur.left = 0;
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  uint32_t before = 0, total = 0;
+  const int used = (a.G + run - 1) / run;            // threads that have groups
+  for (int i = 0; i < used; ++i) {
+    if (i == tid) before = total;
+    total += s_sum[i];
+  }
+  const uint32_t all = total * hb, per = pa_per_cta(all, a.seg_ctas);
+  const uint32_t from = min(all, blockIdx.x * per), to = min(all, from + per);
+  uint32_t at = before;
+  for (int g = ga; g < gb; ++g) {
+    const uint32_t n = pt_tiles(kk, g);
+    if (blockIdx.x == 0) a.seg_start[g] = at;
+    if (from < to && from >= at * hb && from < (at + n) * hb) {
+      const uint32_t in = from - at * hb;
+      s_cur.g = g;
+      s_cur.item = in / n;
+      s_cur.tile = in % n;
+      s_cur.left = to - from;
+    }
+    at += n;
+  }
+  if (blockIdx.x == 0 && tid == 0) a.seg_start[a.G] = total;
+  __syncthreads();
+  Cursor cur = s_cur;
+  const uint32_t tmem = tmem_base;
+  auto wait = [&](uint64_t* bar, uint32_t parity) {
+    if (abort_flag) return false;
+    if (mbar_wait(bar, parity, PT_WAIT)) return true;
+    abort_flag = 1;
+    return false;
+  };
+
+  if (warp == 8) {
+    // ---- copies: K and V tiles of all segments, as the rings have room
+    if (lane == 0) {
+      uint32_t i = 0;
+      bool ok = true;
+      while (cur.left && ok) {
+        const uint32_t here = pt_here(kk, cur);
+        const int hk = (int)(cur.item / a.seg_blocks);
+        for (uint32_t t = 0; t < here; ++t, ++i) {
+          const int key = (int)(cur.tile + t) * PA_TILE;
+          const uint32_t ks = i % NK, vs = i % NV;
+          if (!wait(&k_empty[ks], ((i / NK) & 1u) ^ 1u)) { ok = false; break; }
+          mbar_expect_tx(&k_full[ks], Cfg::TILE);
+          for (int c = 0; c < copies; ++c)
+            tma_load_5d(sK + ks * Cfg::TILE + c * PT_CHUNK, &map_k, &k_full[ks], c * 64, key, 0, hk, cur.g);
+          if (!wait(&v_empty[vs], ((i / NV) & 1u) ^ 1u)) { ok = false; ++i; break; }
+          mbar_expect_tx(&v_full[vs], Cfg::TILE);
+          for (int c = 0; c < copies; ++c)
+            tma_load_5d(sV + vs * Cfg::TILE + c * PT_CHUNK, &map_v, &v_full[vs], c * 64, key, 0, hk, cur.g);
+        }
+        pt_next(a, kk, cur, here);
+      }
+      if (!ok) {
+        // given up: the copies under way land before the CTA's memory goes
+        for (uint32_t j = i > NK ? i - NK : 0; j < i; ++j) mbar_wait(&k_full[j % NK], (j / NK) & 1u, PT_WAIT);
+        for (uint32_t j = i > NV + 1 ? i - NV - 1 : 0; j + 1 < i; ++j)
+          mbar_wait(&v_full[j % NV], (j / NV) & 1u, PT_WAIT);
+      }
+    }
+    __syncwarp();
+  } else if (warp == 9) {
+    // ---- products
+    constexpr uint32_t idesc_s = instr_desc(128, 128);
+    constexpr uint32_t idesc_o = instr_desc(128, DP) | (1u << 16);       // V MN-major
+    uint32_t i0 = 0;                                 // tiles of earlier segments
+    uint32_t pn[2] = {0, 0};                         // probabilities taken so far, per stream
+    while (cur.left) {
+      const uint32_t here = pt_here(kk, cur);
+      const int block = (int)(cur.item % a.seg_blocks);
+      const bool two = rows - block * PA_BLOCK > 128;
+      const int end = pt_len(kk, cur.g) - (int)cur.tile * PA_TILE;       // keys from this segment on
+      named_bar(1, 288);                             // Q is there
+      if (lane == 0) {
+        tc_fence_after();
+        bool ok = true;
+        auto scores = [&](int s, uint32_t t) {       // S of stream s from key tile t
+          const uint32_t ks = (i0 + t) % NK;
+          const uint8_t* q = sQ + (two ? s : 0) * Cfg::TILE;
+#pragma unroll
+          for (int c = 0; c < Cfg::CH; ++c) {
+            const uint64_t qd = smem_desc(q + c * PT_CHUNK);
+            const uint64_t kd = smem_desc(sK + ks * Cfg::TILE + c * PT_CHUNK);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              mma_bf16(tmem + Cfg::S(s), qd + 2ull * k, kd + 2ull * k, idesc_s, (c | k) > 0);
+          }
+          mma_commit(&s_ready[s]);
+        };
+        auto k_wait = [&](uint32_t t) {
+          const uint32_t i = i0 + t;
+          if (!wait(&k_full[i % NK], (i / NK) & 1u)) ok = false;
+          tc_fence_after();
+        };
+        auto k_done = [&](uint32_t t) { mma_commit(&k_empty[(i0 + t) % NK]); };
+        // one step of stream s: O += P V of key tile t, then its next scores, of tile t + step
+        auto step = [&](int s, uint32_t t, uint32_t ahead, bool first_o, bool waits_v, bool frees_v,
+                        bool waits_k, bool frees_k) {
+          const uint32_t i = i0 + t;
+          if (!wait(&p_ready[s], pn[s] & 1u)) { ok = false; return; }
+          ++pn[s];
+          if (waits_v && !wait(&v_full[i % NV], (i / NV) & 1u)) { ok = false; return; }
+          tc_fence_after();
+          const uint8_t* v = sV + (i % NV) * Cfg::TILE;
+          const int keys = min(PA_TILE, end - (int)t * PA_TILE);
+          for (int k = 0; k * 16 < keys; ++k)
+            mma_bf16_ta(tmem + Cfg::O(s), tmem + Cfg::P(s) + k * 8, smem_desc_mn(v + k * 2048), idesc_o,
+                        !(first_o && k == 0));
+          if (frees_v) mma_commit(&v_empty[i % NV]);
+          if (ahead < here) {
+            if (waits_k) k_wait(ahead);
+            if (!ok) return;
+            scores(s, ahead);
+            if (frees_k) k_done(ahead);
+          } else {
+            mma_commit(&o_ready[s]);
+          }
+        };
+        if (two) {
+          k_wait(0);
+          if (ok) {
+            scores(0, 0);
+            scores(1, 0);
+            k_done(0);
+          }
+          for (uint32_t t = 0; t < here && ok; ++t) {
+            step(0, t, t + 1, t == 0, true, false, true, false);
+            if (ok) step(1, t, t + 1, t == 0, false, true, false, true);
+          }
+        } else {
+          for (uint32_t t = 0; t < 2 && t < here && ok; ++t) {
+            k_wait(t);
+            if (!ok) break;
+            scores((int)t, t);
+            k_done(t);
+          }
+          for (uint32_t t = 0; t < here && ok; ++t)
+            step((int)(t & 1u), t, t + 2, t < 2, true, true, true, true);
+        }
+      }
+      i0 += here;
+      __syncwarp();
+      named_bar(2, 288);                             // the segment is done with
+      pt_next(a, kk, cur, here);
+    }
+  } else if (warp < 8) {
+    // ---- the streams: a thread a row
+    const int s = warp >> 2, row = tid & 127;
+    const uint32_t lane_base = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+    uint32_t sn = 0, on = 0;                         // scores and outputs met so far
+    uint32_t i0 = 0;
+    while (cur.left) {
+      const uint32_t here = pt_here(kk, cur);
+      const int block = (int)(cur.item % a.seg_blocks), hk = (int)(cur.item / a.seg_blocks);
+      const bool two = rows - block * PA_BLOCK > 128;
+      const int end = pt_len(kk, cur.g) - (int)cur.tile * PA_TILE;
+      // Q of the block: 16-byte pieces in swizzled rows, zeros past the rows and the head's width
+      {
+        const int pieces = DP / 8, n = (two ? 256 : 128) * pieces;
+        const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.q);
+#pragma unroll 4
+        for (int x = tid; x < n; x += 256) {
+          const int r = x / pieces, p = x % pieces;
+          uint4 v = make_uint4(0, 0, 0, 0);
+          if (block * PA_BLOCK + r < rows && p * 8 < a.d) {
+            const PaRow w = pa_row(a, 0, cur.g, hk, block * PA_BLOCK + r);
+            v = *reinterpret_cast<const uint4*>(q + (int64_t)w.n * a.q_s[0] + (int64_t)w.t * a.q_s[1] +
+                                                (int64_t)w.h * a.q_s[2] + p * 8);
+          }
+          *reinterpret_cast<uint4*>(sQ + (r >> 7) * Cfg::TILE + (p >> 3) * PT_CHUNK + swz(r & 127, p & 7)) = v;
+        }
+        fence_async_shared();
+      }
+      named_bar(1, 288);
+      float m = -INFINITY, l = 0.f;
+      bool ok = true;
+      const uint32_t first = two ? 0 : (uint32_t)s, step = two ? 1 : 2;
+      for (uint32_t t = first; t < here; t += step) {
+        if (!wait(&s_ready[s], sn & 1u)) { ok = false; break; }
+        ++sn;
+        tc_fence_after();
+        // the maximum over both halves of the row's scores, of which the first stays in registers for
+        // the exponentials and the second is read again (all 128 at once spill)
+        const int keys = end - (int)t * PA_TILE;
+        uint32_t x[2][32];
+        auto load = [&](int half) {
+          tmem_ld32_nowait(lane_base + Cfg::S(s) + 64 * half, x[0]);
+          tmem_ld32_nowait(lane_base + Cfg::S(s) + 64 * half + 32, x[1]);
+          tmem_wait_ld();
+          if (keys < PA_TILE) {
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+              for (int e = 0; e < 32; ++e)
+                if (64 * half + 32 * c + e >= keys) x[c][e] = 0xFF800000u;       // -inf
+          }
+        };
+        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        auto maximum = [&]() {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) {
+            mx[e & 1] = fmaxf(mx[e & 1], __uint_as_float(x[0][e]));
+            mx[2 + (e & 1)] = fmaxf(mx[2 + (e & 1)], __uint_as_float(x[1][e]));
+          }
+        };
+        load(1);
+        maximum();
+        load(0);
+        maximum();
+        if (keys < PA_TILE) {
+          // V behind the last key: zeros, whatever the cache holds there (to the product's 16)
+          const uint32_t i = i0 + t;
+          if (!wait(&v_full[i % NV], (i / NV) & 1u)) { ok = false; break; }
+          uint8_t* v = sV + (i % NV) * Cfg::TILE;
+          const int up = (keys + 15) / 16 * 16;
+          for (int z = row; z < (up - keys) * (DP / 8); z += 128) {
+            const int r = keys + z / (DP / 8), p = z % (DP / 8);
+            *reinterpret_cast<uint4*>(v + (p >> 3) * PT_CHUNK + r * 128 + (p & 7) * 16) =
+                make_uint4(0, 0, 0, 0);
+          }
+          fence_async_shared();
+        }
+        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2;
+        if (t == first) {
+          m = top;
+        } else if (__any_sync(0xffffffffu, top > m + 8.f)) {
+          // the sums so far to the new maximum (their product is complete: the scores came behind it)
+          const float to = fmaxf(m, top), f = pa_ex2(m - to);
+          m = to;
+          l *= f;
+#pragma unroll
+          for (int c = 0; c < DP / 32; ++c) {
+            uint32_t o[32];
+            tmem_ld32(lane_base + Cfg::O(s) + 32 * c, o);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+            tmem_st32(lane_base + Cfg::O(s) + 32 * c, o);
+          }
+        }
+        const float base = m == -INFINITY ? 0.f : m;
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          if (half) load(1);
+          uint32_t p[32];
+#pragma unroll
+          for (int e = 0; e < 32; ++e) {
+            const int c = e >> 4, j = (e & 15) * 2;
+            const float p0 = pa_ex2(fmaf(__uint_as_float(x[c][j]), a.scale_log2, -base));
+            const float p1 = pa_ex2(fmaf(__uint_as_float(x[c][j + 1]), a.scale_log2, -base));
+            sum[(e & 1) * 2] += p0;
+            sum[(e & 1) * 2 + 1] += p1;
+            p[e] = pack_bf16x2(p0, p1);
+          }
+          tmem_st32(lane_base + Cfg::P(s) + 32 * half, p);
+        }
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&p_ready[s]);
+      }
+      const bool some = first < here;
+      if (ok && some) {
+        if (!wait(&o_ready[s], on & 1u)) ok = false;
+        ++on;
+        tc_fence_after();
+      }
+      const uint32_t item = (uint32_t)cur.g * hb + cur.item;
+      const size_t seg = ((size_t)blockIdx.x + item) * PA_BLOCK;
+      const int r = two ? s * 128 + row : row;
+      const bool live = block * PA_BLOCK + r < rows;
+      if (!two && here > 1) {
+        // the streams' halves of the keys: the second's sums pass through Q's space (the rings may hold
+        // tiles of the next segment already), the first adds them to its own
+        named_bar(3, 256);                           // both are done with their products
+        if (s == 1) s_ml[row] = make_float2(m, l);
+        float f0 = 1.f, f1 = 0.f;
+#pragma unroll
+        for (int c = 0; c < DP / 32; ++c) {
+          uint32_t o[32];
+          if (s == 1) {
+            tmem_ld32(lane_base + Cfg::O(1) + 32 * c, o);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) s_o[e * 128 + row] = __uint_as_float(o[e]);
+          }
+          named_bar(3, 256);
+          if (s == 0) {
+            if (c == 0) {
+              const float2 y = s_ml[row];
+              const float to = fmaxf(m, y.x), base = to == -INFINITY ? 0.f : to;
+              f0 = pa_ex2(m - base);
+              f1 = pa_ex2(y.x - base);
+              m = to;
+              l = l * f0 + y.y * f1;
+            }
+            tmem_ld32(lane_base + Cfg::O(0) + 32 * c, o);
+            if (ok && live) {
+              float* dst = a.seg_po + (seg + r) * a.d + 32 * c;
+#pragma unroll
+              for (int e = 0; e < 32; e += 4)
+                if (32 * c + e < a.d)
+                  *reinterpret_cast<float4*>(dst + e) =
+                      make_float4(__uint_as_float(o[e]) * f0 + s_o[e * 128 + row] * f1,
+                                  __uint_as_float(o[e + 1]) * f0 + s_o[(e + 1) * 128 + row] * f1,
+                                  __uint_as_float(o[e + 2]) * f0 + s_o[(e + 2) * 128 + row] * f1,
+                                  __uint_as_float(o[e + 3]) * f0 + s_o[(e + 3) * 128 + row] * f1);
+            }
+          }
+          named_bar(3, 256);
+        }
+      } else if (two || s == 0) {
+#pragma unroll
+        for (int c = 0; c < DP / 32; ++c) {
+          uint32_t o[32];
+          tmem_ld32(lane_base + Cfg::O(s) + 32 * c, o);
+          if (ok && live) {
+            float* dst = a.seg_po + (seg + r) * a.d + 32 * c;
+#pragma unroll
+            for (int e = 0; e < 32; e += 4)
+              if (32 * c + e < a.d)
+                *reinterpret_cast<float4*>(dst + e) =
+                    make_float4(__uint_as_float(o[e]), __uint_as_float(o[e + 1]),
+                                __uint_as_float(o[e + 2]), __uint_as_float(o[e + 3]));
+          }
+        }
+      }
+      if ((two || s == 0) && live) a.seg_ml[seg + r] = make_float2(m, l);
+      i0 += here;
+      tc_fence_before();
+      named_bar(2, 288);
+      tc_fence_after();
+      pt_next(a, kk, cur, here);
+    }
+  }
+  if (abort_flag && tid == 0) set_status(a.status, LILICORR_ERR_TIMEOUT);
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 9) {
+    tc_fence_after();
+    tmem_dealloc(tmem, PT_TMEM);
+  }
+}
+
+// K or V as (64 columns, position, 64-column block, head, group): one copy a tile where the width is a
+// multiple of 64; else blocks by the first coordinate, zeros past the width.
+bool pt_map(CUtensorMap* map, const void* base, const int64_t (&s)[3], const PaArgs& a, int capacity,
+            int* copies) {
+  const bool whole = a.d % 64 == 0;
+  const uint64_t dims[5] = {whole ? 64u : (uint64_t)a.d, (uint64_t)capacity,
+                            whole ? (uint64_t)a.d / 64 : 1u, (uint64_t)a.Hkv, (uint64_t)a.G};
+  // (a dimension of one has stride 0 here, which a map does not take)
+  auto bytes = [&](int64_t stride, int extent) {
+    return extent > 1 ? (uint64_t)stride * 2 : (uint64_t)16 * ((a.d + 7) / 8);
+  };
+  const uint64_t strides[5] = {2, bytes(s[1], capacity), whole ? 128u : bytes(0, 1), bytes(s[2], a.Hkv),
+                               bytes(s[0], a.G)};
+  for (int i = 1; i < 5; ++i)
+    if (strides[i] == 0) return false;               // an expanded dimension
+  const uint32_t box[5] = {64, PA_TILE, whole ? (uint32_t)a.d / 64 : 1u, 1, 1};
+  *copies = whole ? 1 : (a.d + 63) / 64;
+  return make_map_nd(map, base, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, dims, strides, box);
+}
+
+template <int DP>
+lilicorr_status_t launch_tc(const PaArgs& a, const PaKeys& k, cudaStream_t st) {
+  static bool configured[64] = {false};
+  LL_TRY(allow_max_dynamic_smem(pa_tc_kernel<DP>, configured));
+  CUtensorMap mk, mv;
+  int copies = 1;
+  if (!pt_map(&mk, k.k, k.k_s, a, k.capacity, &copies) || !pt_map(&mv, k.v, k.v_s, a, k.capacity, &copies))
+    return LILICORR_ERR_CUDA;
+  const int rows = a.W * a.T * a.rep;
+  return launch_k(pa_tc_kernel<DP>, a.seg_ctas, PT_THREADS, PtCfg<DP>::SMEM, st, mk, mv, copies, a, k,
+                  rows);
+}
+
+}  // namespace
+
+bool pa_tc_takes(const PaArgs& a, const PaKeys& k) {
+  CUtensorMap m;
+  int copies;
+  return encode_fn() != nullptr && pt_map(&m, k.k, k.k_s, a, k.capacity, &copies) &&
+         pt_map(&m, k.v, k.v_s, a, k.capacity, &copies);
+}
+
+lilicorr_status_t launch_pa_tc(const PaArgs& a, const PaKeys& k, cudaStream_t st) {
+  return a.d <= 64 ? launch_tc<64>(a, k, st) : launch_tc<128>(a, k, st);
+}
+
+}  // namespace lilicorr
