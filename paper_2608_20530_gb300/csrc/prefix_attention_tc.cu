@@ -4,10 +4,11 @@
 // One CTA an SM. Warp 8 feeds K and V tiles by TMA into two rings. Warp 9 issues
 //   S = Q K^T   (M 128, N 128)   into tensor memory, and
 //   O += P V    (M 128, N d)     with P read from tensor memory, V as the MN-major operand.
-// Warps 0-3 and 4-7 are two streams: a thread a row reads its 128 scores, takes the running maximum,
-// writes P = 2^(s - m) as bf16 over them and keeps the row's sum. While one stream is at its
-// exponentials the tensor cores work for the other. With two row tiles the streams share each key
-// tile; with one they take the key tiles in turn and join at the end.
+// Warps 0-3 and 4-7 are two streams, a thread a row: it reads the row's 128 scores (one wait: a load
+// from tensor memory takes 400 clocks beside running products), takes the running maximum, writes
+// P = 2^(s - m) as bf16 and keeps the row's sum. While one stream is at its exponentials the tensor
+// cores work for the other. With two row tiles the streams share each key tile; with one they take the
+// key tiles in turn and join at the end. Warps without a row do nothing but keep the count of arrivals.
 //
 // O is not rescaled whenever a maximum grows: m is the maximum that a row's sums are taken against, and
 // it moves only when a score would pass it by 2^8, so that terms stay below 2^8 and sums exact to fp32.
@@ -24,6 +25,7 @@ namespace {
 using namespace tc;
 
 constexpr int PT_THREADS = 320;
+constexpr int PT_SOFT = 256;                         // of them in the streams
 constexpr uint32_t PT_CHUNK = 128 * 128;             // 128 rows of 128 bytes
 constexpr long long PT_WAIT = 4000000000ll;          // SM cycles, about 2 s
 constexpr uint32_t PT_TMEM = 512;
@@ -34,13 +36,14 @@ struct PtCfg {
   static constexpr uint32_t TILE = CH * PT_CHUNK;    // bytes of a K, V or Q tile
   static constexpr int NK = DP == 128 ? 3 : 5, NV = DP == 128 ? 2 : 5;
   static constexpr size_t SMEM = 1024 + (size_t)(2 + NK + NV) * TILE;
-  // tensor-memory columns: scores, output, and probabilities. At d = 128 the probabilities lie over the
-  // scores they came from: the next scores of the stream are issued behind the product that reads
-  // them, and products of one shape run in the order of issue. At d = 64 the two products differ in
-  // shape, and there is room for the probabilities elsewhere.
-  static constexpr uint32_t S(int s) { return s * 128; }
-  static constexpr uint32_t O(int s) { return 256 + s * DP; }
-  static constexpr uint32_t P(int s) { return DP == 128 ? S(s) : 384 + s * 64; }
+  // tensor-memory columns: scores, output, and the probabilities of keys [16 k, 16 k + 16). At d = 128
+  // those lie over the scores, which their thread has read: the next scores of the stream are issued
+  // behind the product that reads them, and products of one shape run in the order of issue. At d = 64 the two products differ in shape, and there is room elsewhere.
+  __device__ static constexpr uint32_t S(int s) { return s * 128; }
+  __device__ static constexpr uint32_t O(int s) { return 256 + s * DP; }
+  __device__ static constexpr uint32_t P(int s, int k) {
+    return (DP == 128 ? S(s) : 384 + s * 64) + k * 8;
+  }
 };
 
 // A of the product from tensor memory
@@ -54,6 +57,33 @@ __device__ __forceinline__ void mma_bf16_ta(uint32_t tmem_d, uint32_t tmem_a, ui
 // MN-major operand of 128-byte-swizzled rows: 64-column chunks PT_CHUNK bytes apart, 8-row groups 1024
 __device__ __forceinline__ uint64_t smem_desc_mn(const void* tile) {
   return smem_desc(tile) & ~(0x3FFFull << 16) | ((uint64_t)(PT_CHUNK >> 4) << 16);
+}
+
+// one lane of a converged warp
+__device__ __forceinline__ bool elect_one() {
+  uint32_t r;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(r));
+  return r != 0;
+}
+// packed fp32 pairs: one instruction for both halves (a tensor-memory load leaves its columns in
+// neighbouring registers, so no moves pair them up)
+__device__ __forceinline__ uint64_t pair_of(uint32_t lo, uint32_t hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(lo), "r"(hi));
+  return r;
+}
+__device__ __forceinline__ void halves(uint64_t v, float& lo, float& hi) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.ftz.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t add_pairs(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.ftz.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
 }
 
 // Where a CTA is in the list of tiles.
@@ -157,10 +187,16 @@ pa_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
   Cursor cur = s_cur;
   const uint32_t tmem = tmem_base;
   auto wait = [&](uint64_t* bar, uint32_t parity) {
-    if (abort_flag) return false;
-    if (mbar_wait(bar, parity, PT_WAIT)) return true;
-    abort_flag = 1;
-    return false;
+    if (mbar_try_wait(bar, parity)) return true;
+    const long long t0 = clock64();
+    while (!mbar_try_wait(bar, parity)) {
+      if (abort_flag) return false;
+      if (clock64() - t0 > PT_WAIT) {
+        abort_flag = 1;
+        return false;
+      }
+    }
+    return true;
   };
 
   if (warp == 8) {
@@ -194,92 +230,91 @@ pa_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     }
     __syncwarp();
   } else if (warp == 9) {
-    // ---- products
+    // ---- products. The whole warp walks, one lane issues: a single thread's own loop, with its
+    // descriptors formed one by one, took 80 clocks a product and was what everything waited for.
     constexpr uint32_t idesc_s = instr_desc(128, 128);
     constexpr uint32_t idesc_o = instr_desc(128, DP) | (1u << 16);       // V MN-major
-    uint32_t i0 = 0;                                 // tiles of earlier segments
-    uint32_t pn[2] = {0, 0};                         // probabilities taken so far, per stream
+    const bool leader = elect_one();
+    const uint64_t q_desc = smem_desc(sQ), k_desc = smem_desc(sK), v_desc = smem_desc_mn(sV);
+    uint32_t ki = 0, kp = 0, vi = 0, vp = 0;         // the rings' next slots and their parities
+    uint32_t pp[2] = {0, 0};                         // parity of the streams' probabilities
     while (cur.left) {
       const uint32_t here = pt_here(kk, cur);
       const int block = (int)(cur.item % a.seg_blocks);
       const bool two = rows - block * PA_BLOCK > 128;
       const int end = pt_len(kk, cur.g) - (int)cur.tile * PA_TILE;       // keys from this segment on
-      named_bar(1, 288);                             // Q is there
-      if (lane == 0) {
-        tc_fence_after();
-        bool ok = true;
-        auto scores = [&](int s, uint32_t t) {       // S of stream s from key tile t
-          const uint32_t ks = (i0 + t) % NK;
-          const uint8_t* q = sQ + (two ? s : 0) * Cfg::TILE;
+      named_bar(1, PT_SOFT + 32);                    // Q is there
+      tc_fence_after();
+      bool ok = true;
+      // S of stream s from the K tile in the ring's next slot; last: the slot's last use
+      auto scores = [&](int s, bool first, bool last) {
+        if (first) {
+          if (!wait(&k_full[ki], kp)) { ok = false; return; }
+          tc_fence_after();
+        }
+        const uint64_t qd = q_desc + (two ? s : 0) * (Cfg::TILE >> 4), kd = k_desc + ki * (Cfg::TILE >> 4);
+        if (leader) {
 #pragma unroll
-          for (int c = 0; c < Cfg::CH; ++c) {
-            const uint64_t qd = smem_desc(q + c * PT_CHUNK);
-            const uint64_t kd = smem_desc(sK + ks * Cfg::TILE + c * PT_CHUNK);
+          for (int c = 0; c < Cfg::CH; ++c)
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-              mma_bf16(tmem + Cfg::S(s), qd + 2ull * k, kd + 2ull * k, idesc_s, (c | k) > 0);
-          }
+              mma_bf16(tmem + Cfg::S(s), qd + c * (PT_CHUNK >> 4) + 2 * k, kd + c * (PT_CHUNK >> 4) + 2 * k,
+                       idesc_s, (c | k) > 0);
           mma_commit(&s_ready[s]);
-        };
-        auto k_wait = [&](uint32_t t) {
-          const uint32_t i = i0 + t;
-          if (!wait(&k_full[i % NK], (i / NK) & 1u)) ok = false;
-          tc_fence_after();
-        };
-        auto k_done = [&](uint32_t t) { mma_commit(&k_empty[(i0 + t) % NK]); };
-        // one step of stream s: O += P V of key tile t, then its next scores, of tile t + step
-        auto step = [&](int s, uint32_t t, uint32_t ahead, bool first_o, bool waits_v, bool frees_v,
-                        bool waits_k, bool frees_k) {
-          const uint32_t i = i0 + t;
-          if (!wait(&p_ready[s], pn[s] & 1u)) { ok = false; return; }
-          ++pn[s];
-          if (waits_v && !wait(&v_full[i % NV], (i / NV) & 1u)) { ok = false; return; }
-          tc_fence_after();
-          const uint8_t* v = sV + (i % NV) * Cfg::TILE;
-          const int keys = min(PA_TILE, end - (int)t * PA_TILE);
-          for (int k = 0; k * 16 < keys; ++k)
-            mma_bf16_ta(tmem + Cfg::O(s), tmem + Cfg::P(s) + k * 8, smem_desc_mn(v + k * 2048), idesc_o,
-                        !(first_o && k == 0));
-          if (frees_v) mma_commit(&v_empty[i % NV]);
-          if (ahead < here) {
-            if (waits_k) k_wait(ahead);
-            if (!ok) return;
-            scores(s, ahead);
-            if (frees_k) k_done(ahead);
+          if (last) mma_commit(&k_empty[ki]);
+        }
+        __syncwarp();
+        if (last && ++ki == NK) { ki = 0; kp ^= 1u; }
+      };
+      // O += P V of stream s and the key tile `keys` long in the V ring's next slot
+      auto sums = [&](int s, int keys, bool fresh, bool first, bool last, bool done) {
+        if (!wait(&p_ready[s], pp[s])) { ok = false; return; }
+        pp[s] ^= 1u;
+        if (first && !wait(&v_full[vi], vp)) { ok = false; return; }
+        tc_fence_after();
+        const uint64_t vd = v_desc + vi * (Cfg::TILE >> 4);
+        if (leader) {
+          if (keys >= PA_TILE) {
+#pragma unroll
+            for (int k = 0; k < PA_TILE / 16; ++k)
+              mma_bf16_ta(tmem + Cfg::O(s), tmem + Cfg::P(s, k), vd + k * 128, idesc_o, !fresh || k > 0);
           } else {
-            mma_commit(&o_ready[s]);
+#pragma unroll 1
+            for (int k = 0; k * 16 < keys; ++k)
+              mma_bf16_ta(tmem + Cfg::O(s), tmem + Cfg::P(s, k), vd + k * 128, idesc_o, !fresh || k > 0);
           }
-        };
-        if (two) {
-          k_wait(0);
-          if (ok) {
-            scores(0, 0);
-            scores(1, 0);
-            k_done(0);
-          }
-          for (uint32_t t = 0; t < here && ok; ++t) {
-            step(0, t, t + 1, t == 0, true, false, true, false);
-            if (ok) step(1, t, t + 1, t == 0, false, true, false, true);
-          }
-        } else {
-          for (uint32_t t = 0; t < 2 && t < here && ok; ++t) {
-            k_wait(t);
-            if (!ok) break;
-            scores((int)t, t);
-            k_done(t);
-          }
-          for (uint32_t t = 0; t < here && ok; ++t)
-            step((int)(t & 1u), t, t + 2, t < 2, true, true, true, true);
+          if (last) mma_commit(&v_empty[vi]);
+          if (done) mma_commit(&o_ready[s]);
+        }
+        __syncwarp();
+        if (last && ++vi == NV) { vi = 0; vp ^= 1u; }
+      };
+      if (two) {
+        scores(0, true, false);
+        if (ok) scores(1, false, true);
+        for (uint32_t t = 0; t < here && ok; ++t) {
+          const int keys = end - (int)t * PA_TILE;
+          const bool more = t + 1 < here;
+          sums(0, keys, t == 0, true, false, !more);
+          if (ok && more) scores(0, true, false);
+          if (ok) sums(1, keys, t == 0, false, true, !more);
+          if (ok && more) scores(1, false, true);
+        }
+      } else {
+        scores(0, true, true);
+        if (ok && here > 1) scores(1, true, true);
+        for (uint32_t t = 0; t < here && ok; ++t) {
+          const int s = (int)(t & 1u);
+          sums(s, end - (int)t * PA_TILE, t < 2, true, true, t + 2 >= here);
+          if (ok && t + 2 < here) scores(s, true, true);
         }
       }
-      i0 += here;
-      __syncwarp();
-      named_bar(2, 288);                             // the segment is done with
+      named_bar(2, PT_SOFT + 32);                    // the segment is done with
       pt_next(a, kk, cur, here);
     }
-  } else if (warp < 8) {
+  } else {
     // ---- the streams: a thread a row
-    const int s = warp >> 2, row = tid & 127;
+    const int s = warp >> 2, row = (warp & 3) * 32 + lane;
     const uint32_t lane_base = tmem + ((uint32_t)((warp & 3) * 32) << 16);
     uint32_t sn = 0, on = 0;                         // scores and outputs met so far
     uint32_t i0 = 0;
@@ -292,8 +327,8 @@ pa_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       {
         const int pieces = DP / 8, n = (two ? 256 : 128) * pieces;
         const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.q);
-#pragma unroll 4
-        for (int x = tid; x < n; x += 256) {
+#pragma unroll 2
+        for (int x = tid; x < n; x += PT_SOFT) {
           const int r = x / pieces, p = x % pieces;
           uint4 v = make_uint4(0, 0, 0, 0);
           if (block * PA_BLOCK + r < rows && p * 8 < a.d) {
@@ -305,22 +340,31 @@ pa_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         }
         fence_async_shared();
       }
-      named_bar(1, 288);
+      named_bar(1, PT_SOFT + 32);
+      const int r = two ? s * 128 + row : row;       // of the block
+      const int tile_rows = min(128, rows - block * PA_BLOCK - (two ? s * 128 : 0));
+      const int warps = (tile_rows + 31) / 32;       // of the stream's that have rows
+      const bool idle = (warp & 3) >= warps;
       float m = -INFINITY, l = 0.f;
       bool ok = true;
       const uint32_t first = two ? 0 : (uint32_t)s, step = two ? 1 : 2;
       for (uint32_t t = first; t < here; t += step) {
         if (!wait(&s_ready[s], sn & 1u)) { ok = false; break; }
         ++sn;
+        if (idle) {                                  // (what P holds for its rows reaches no other row)
+          if (lane == 0) mbar_arrive(&p_ready[s]);
+          continue;
+        }
         tc_fence_after();
-        // the maximum over both halves of the row's scores, of which the first stays in registers for
-        // the exponentials and the second is read again (all 128 at once spill)
         const int keys = end - (int)t * PA_TILE;
+        // 64 scores at a time: the first half stays for the exponentials, the second is read again (128
+        // of them spill beside the rest)
         uint32_t x[2][32];
         auto load = [&](int half) {
           tmem_ld32_nowait(lane_base + Cfg::S(s) + 64 * half, x[0]);
           tmem_ld32_nowait(lane_base + Cfg::S(s) + 64 * half + 32, x[1]);
-          tmem_wait_ld();
+        };
+        auto mask = [&](int half) {
           if (keys < PA_TILE) {
 #pragma unroll
             for (int c = 0; c < 2; ++c)
@@ -332,14 +376,20 @@ pa_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
         auto maximum = [&]() {
 #pragma unroll
-          for (int e = 0; e < 32; ++e) {
-            mx[e & 1] = fmaxf(mx[e & 1], __uint_as_float(x[0][e]));
-            mx[2 + (e & 1)] = fmaxf(mx[2 + (e & 1)], __uint_as_float(x[1][e]));
-          }
+          for (int e = 0; e < 32; e += 4)              // three at a time
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              mx[c] = fmaxf(fmaxf(mx[c], __uint_as_float(x[c][e])), __uint_as_float(x[c][e + 1]));
+              mx[2 + c] = fmaxf(fmaxf(mx[2 + c], __uint_as_float(x[c][e + 2])), __uint_as_float(x[c][e + 3]));
+            }
         };
         load(1);
+        tmem_wait_ld();
+        mask(1);
         maximum();
         load(0);
+        tmem_wait_ld();
+        mask(0);
         maximum();
         if (keys < PA_TILE) {
           // V behind the last key: zeros, whatever the cache holds there (to the product's 16)
@@ -347,9 +397,9 @@ pa_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
           if (!wait(&v_full[i % NV], (i / NV) & 1u)) { ok = false; break; }
           uint8_t* v = sV + (i % NV) * Cfg::TILE;
           const int up = (keys + 15) / 16 * 16;
-          for (int z = row; z < (up - keys) * (DP / 8); z += 128) {
-            const int r = keys + z / (DP / 8), p = z % (DP / 8);
-            *reinterpret_cast<uint4*>(v + (p >> 3) * PT_CHUNK + r * 128 + (p & 7) * 16) =
+          for (int z = row; z < (up - keys) * (DP / 8); z += warps * 32) {
+            const int vr = keys + z / (DP / 8), p = z % (DP / 8);
+            *reinterpret_cast<uint4*>(v + (p >> 3) * PT_CHUNK + vr * 128 + (p & 7) * 16) =
                 make_uint4(0, 0, 0, 0);
           }
           fence_async_shared();
@@ -363,88 +413,93 @@ pa_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
           m = to;
           l *= f;
 #pragma unroll
-          for (int c = 0; c < DP / 32; ++c) {
-            uint32_t o[32];
-            tmem_ld32(lane_base + Cfg::O(s) + 32 * c, o);
+          for (int c = 0; c < DP / 16; ++c) {
+            uint32_t o[16];
+            tmem_ld16(lane_base + Cfg::O(s) + 16 * c, o);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-            tmem_st32(lane_base + Cfg::O(s) + 32 * c, o);
+            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+            tmem_st16(lane_base + Cfg::O(s) + 16 * c, o);
           }
         }
         const float base = m == -INFINITY ? 0.f : m;
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        uint64_t sum0 = 0ull, sum1 = 0ull;
+        const uint64_t sc2 = pair_of(__float_as_uint(a.scale_log2), __float_as_uint(a.scale_log2));
+        const uint64_t nb2 = pair_of(__float_as_uint(-base), __float_as_uint(-base));
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          if (half) load(1);
-          uint32_t p[32];
+        for (int c = 0; c < 4; ++c) {
+          if (c == 2) {
+            load(1);
+            tmem_wait_ld();
+            mask(1);
+          }
+          uint32_t p[16];
 #pragma unroll
-          for (int e = 0; e < 32; ++e) {
-            const int c = e >> 4, j = (e & 15) * 2;
-            const float p0 = pa_ex2(fmaf(__uint_as_float(x[c][j]), a.scale_log2, -base));
-            const float p1 = pa_ex2(fmaf(__uint_as_float(x[c][j + 1]), a.scale_log2, -base));
-            sum[(e & 1) * 2] += p0;
-            sum[(e & 1) * 2 + 1] += p1;
+          for (int e = 0; e < 16; ++e) {
+            float p0, p1;
+            halves(fma_pair(pair_of(x[c & 1][2 * e], x[c & 1][2 * e + 1]), sc2, nb2), p0, p1);
+            p0 = pa_ex2(p0);
+            p1 = pa_ex2(p1);
+            const uint64_t pp = pair_of(__float_as_uint(p0), __float_as_uint(p1));
+            if (e & 1) sum1 = add_pairs(sum1, pp);
+            else sum0 = add_pairs(sum0, pp);
             p[e] = pack_bf16x2(p0, p1);
           }
-          tmem_st32(lane_base + Cfg::P(s) + 32 * half, p);
+          tmem_st16(lane_base + Cfg::P(s, 2 * c), p);
         }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        float l0, l1;
+        halves(add_pairs(sum0, sum1), l0, l1);
+        l += l0 + l1;
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&p_ready[s]);
       }
-      const bool some = first < here;
-      if (ok && some) {
+      if (ok && first < here) {
         if (!wait(&o_ready[s], on & 1u)) ok = false;
         ++on;
         tc_fence_after();
       }
       const uint32_t item = (uint32_t)cur.g * hb + cur.item;
       const size_t seg = ((size_t)blockIdx.x + item) * PA_BLOCK;
-      const int r = two ? s * 128 + row : row;
       const bool live = block * PA_BLOCK + r < rows;
       if (!two && here > 1) {
-        // the streams' halves of the keys: the second's sums pass through Q's space (the rings may hold
+        // the streams' parts of the keys: the second's sums pass through Q's space (the rings may hold
         // tiles of the next segment already), the first adds them to its own
-        named_bar(3, 256);                           // both are done with their products
+        named_bar(3, PT_SOFT);                         // every product with Q is done
         if (s == 1) s_ml[row] = make_float2(m, l);
         float f0 = 1.f, f1 = 0.f;
-#pragma unroll
+#pragma unroll 1
         for (int c = 0; c < DP / 32; ++c) {
           uint32_t o[32];
-          if (s == 1) {
-            tmem_ld32(lane_base + Cfg::O(1) + 32 * c, o);
+          if (!idle) tmem_ld32(lane_base + Cfg::O(s) + 32 * c, o);
+          if (s == 1 && !idle) {
 #pragma unroll
             for (int e = 0; e < 32; ++e) s_o[e * 128 + row] = __uint_as_float(o[e]);
           }
-          named_bar(3, 256);
-          if (s == 0) {
-            if (c == 0) {
-              const float2 y = s_ml[row];
-              const float to = fmaxf(m, y.x), base = to == -INFINITY ? 0.f : to;
-              f0 = pa_ex2(m - base);
-              f1 = pa_ex2(y.x - base);
-              m = to;
-              l = l * f0 + y.y * f1;
-            }
-            tmem_ld32(lane_base + Cfg::O(0) + 32 * c, o);
-            if (ok && live) {
-              float* dst = a.seg_po + (seg + r) * a.d + 32 * c;
-#pragma unroll
-              for (int e = 0; e < 32; e += 4)
-                if (32 * c + e < a.d)
-                  *reinterpret_cast<float4*>(dst + e) =
-                      make_float4(__uint_as_float(o[e]) * f0 + s_o[e * 128 + row] * f1,
-                                  __uint_as_float(o[e + 1]) * f0 + s_o[(e + 1) * 128 + row] * f1,
-                                  __uint_as_float(o[e + 2]) * f0 + s_o[(e + 2) * 128 + row] * f1,
-                                  __uint_as_float(o[e + 3]) * f0 + s_o[(e + 3) * 128 + row] * f1);
-            }
+          named_bar(3, PT_SOFT);
+          if (s == 0 && c == 0) {
+            const float2 y = s_ml[row];
+            const float to = fmaxf(m, y.x), base = to == -INFINITY ? 0.f : to;
+            f0 = pa_ex2(m - base);
+            f1 = pa_ex2(y.x - base);
+            m = to;
+            l = l * f0 + y.y * f1;
           }
-          named_bar(3, 256);
-        }
-      } else if (two || s == 0) {
+          if (s == 0 && ok && live) {
+            float* dst = a.seg_po + (seg + r) * a.d + 32 * c;
 #pragma unroll
+            for (int e = 0; e < 32; e += 4)
+              if (32 * c + e < a.d)
+                *reinterpret_cast<float4*>(dst + e) =
+                    make_float4(__uint_as_float(o[e]) * f0 + s_o[e * 128 + row] * f1,
+                                __uint_as_float(o[e + 1]) * f0 + s_o[(e + 1) * 128 + row] * f1,
+                                __uint_as_float(o[e + 2]) * f0 + s_o[(e + 2) * 128 + row] * f1,
+                                __uint_as_float(o[e + 3]) * f0 + s_o[(e + 3) * 128 + row] * f1);
+          }
+          named_bar(3, PT_SOFT);
+        }
+      } else if ((two || s == 0) && !idle) {
+#pragma unroll 1
         for (int c = 0; c < DP / 32; ++c) {
           uint32_t o[32];
           tmem_ld32(lane_base + Cfg::O(s) + 32 * c, o);
@@ -462,7 +517,7 @@ pa_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       if ((two || s == 0) && live) a.seg_ml[seg + r] = make_float2(m, l);
       i0 += here;
       tc_fence_before();
-      named_bar(2, 288);
+      named_bar(2, PT_SOFT + 32);
       tc_fence_after();
       pt_next(a, kk, cur, here);
     }
