@@ -18,7 +18,7 @@ namespace {
 
 constexpr int PM_THREADS = 128;
 constexpr int PM_KT = 64;                // keys per stage
-constexpr int PM_STAGES = 3;
+constexpr int PM_STAGES = 2;
 
 __device__ __forceinline__ uint32_t sm_addr(const void* p) {
   return static_cast<uint32_t>(__cvta_generic_to_shared(p));
@@ -67,12 +67,103 @@ __device__ __forceinline__ void stage_rows(unsigned char* dst, const unsigned ch
   }
 }
 
+// One row's result, by one warp, four columns a lane: the prefix's segments and the slots joined with
+// (m, l, o) that the warp has already (m -inf: nothing), to out and lse.
+template <typename T>
+__device__ __forceinline__ void join_row(const PaArgs& a, const PaRow& w, float m, float l, float4 o,
+                                         int lane) {
+  const size_t rows = a.rows(), row = pa_index(a, w);
+  int segs = 0;
+  size_t seg0 = 0;
+  if (a.seg_ctas) {
+    const int g = w.n / a.W, hk = w.h / a.rep;
+    const int r = ((w.n - g * a.W) * a.T + w.t) * a.rep + (w.h - hk * a.rep);
+    const uint32_t hb = (uint32_t)a.Hkv * a.seg_blocks;
+    const uint32_t before = a.seg_start[g], tiles = a.seg_start[g + 1] - before;
+    if (tiles) {
+      const uint32_t per = pa_per_cta(a.seg_start[a.G] * hb, a.seg_ctas);
+      const uint32_t in = (uint32_t)hk * a.seg_blocks + r / PA_BLOCK;
+      const uint32_t first = before * hb + in * tiles;
+      const uint32_t c0 = first / per, c1 = (first + tiles - 1) / per;
+      segs = (int)(c1 - c0) + 1;
+      seg0 = ((size_t)c0 + (size_t)g * hb + in) * PA_BLOCK + r % PA_BLOCK;
+    }
+  }
+  const int pieces = segs + a.slots;
+  auto ml_of = [&](int s) {
+    return s < segs ? a.seg_ml[seg0 + (size_t)s * PA_BLOCK] : a.ml[(size_t)(s - segs) * rows + row];
+  };
+  auto po_of = [&](int s) {
+    return s < segs ? a.seg_po + (seg0 + (size_t)s * PA_BLOCK) * a.d
+                    : a.po + ((size_t)(s - segs) * rows + row) * a.d;
+  };
+  for (int s0 = 0; s0 < pieces; s0 += 32) {
+    const float2 ml = s0 + lane < pieces ? ml_of(s0 + lane) : make_float2(-INFINITY, 0.f);
+    const float M = fmaxf(m, warp_max(ml.x)), u = M == -INFINITY ? 0.f : M;
+    const float keep = pa_ex2(m - u);
+    const float f = ml.x == -INFINITY ? 0.f : pa_ex2(ml.x - u);
+    m = M;
+    l = l * keep + warp_sum(f * ml.y);
+    o.x *= keep; o.y *= keep; o.z *= keep; o.w *= keep;
+    const unsigned there = __ballot_sync(0xffffffffu, ml.x != -INFINITY);    // others wrote no sums
+    const int n = min(32, pieces - s0);
+    constexpr int U = 4;                             // sums on their way together
+    for (int j0 = 0; j0 < n; j0 += U) {
+      float4 p[U];
+#pragma unroll
+      for (int u2 = 0; u2 < U; ++u2) {
+        p[u2] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (j0 + u2 < n && (there >> (j0 + u2) & 1u) && lane * 4 < a.d)
+          p[u2] = *reinterpret_cast<const float4*>(po_of(s0 + j0 + u2) + lane * 4);
+      }
+#pragma unroll
+      for (int u2 = 0; u2 < U; ++u2) {
+        const float w2 = __shfl_sync(0xffffffffu, f, (j0 + u2) & 31);
+        if (j0 + u2 >= n) continue;
+        o.x = fmaf(w2, p[u2].x, o.x);
+        o.y = fmaf(w2, p[u2].y, o.y);
+        o.z = fmaf(w2, p[u2].z, o.z);
+        o.w = fmaf(w2, p[u2].w, o.w);
+      }
+    }
+  }
+  const float inv = l > 0.f ? 1.0f / l : (m == -INFINITY ? 0.f : l);       // (NaN stays)
+  T* out = static_cast<T*>(a.out) + (int64_t)w.n * a.o_s[0] + (int64_t)w.t * a.o_s[1] + (int64_t)w.h * a.o_s[2];
+  if (lane * 4 < a.d) {
+    o.x *= inv; o.y *= inv; o.z *= inv; o.w *= inv;
+    if constexpr (sizeof(T) == 4)
+      *reinterpret_cast<float4*>(out + lane * 4) = o;
+    else
+      *reinterpret_cast<uint2*>(out + lane * 4) = make_uint2(bf16_pack2(o.x, o.y), bf16_pack2(o.z, o.w));
+  }
+  if (lane == 0) a.lse[row] = m == -INFINITY ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+}
+
+// Join the rows' pieces where no kernel of the own keys does: one warp a row.
+template <typename T>
+__global__ void __launch_bounds__(128)
+pa_combine_kernel(const PaArgs a) {
+  pdl_wait();
+  const size_t row = (size_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+  if (row >= a.rows()) return;
+  PaRow w;
+  w.h = (int)(row % a.Hq);
+  const size_t nt = row / a.Hq;
+  w.t = (int)(nt % a.T);
+  w.n = (int)(nt / a.T);
+  if (a.seq_len[w.n] < 0) return;                   // no such sequence: its rows stay as they are
+  join_row<T>(a, w, -INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f), threadIdx.x & 31);
+}
+
 // bf16: four warps, RB of the four over 16 query rows each, the other 4 / RB over the keys of a stage
 // (warp-level products; the pieces of the keys meet in shared memory at the end).
-template <int DP, int RB>
-__global__ void __launch_bounds__(PM_THREADS)
+// JOIN: the own keys in one piece; the kernel joins it with the prefix's pieces and writes the result. The
+// prefix's kernel runs before it and waited for everything before itself, so the inputs may be read, and
+// the own keys' part done, while that kernel still runs.
+template <int DP, int RB, bool JOIN>
+__global__ void __launch_bounds__(PM_THREADS, 3)
 pa_mma_kernel(const PaArgs a, const PaKeys kk, int rows, int blocks) {
-  pdl_wait();
+  if (!JOIN || !kk.behind) pdl_wait();
   constexpr int LD = (DP + 8) * 2;                  // bytes of a staged row
   constexpr int PH = 4 / RB, KW = PM_KT / PH;       // key phases, keys per warp and stage
   constexpr int KS = DP / 16, NB = KW / 8, OB = DP / 8;
@@ -91,7 +182,11 @@ pa_mma_kernel(const PaArgs a, const PaKeys kk, int rows, int blocks) {
   pa_piece(held, kk.splits, split, k0, k1);
   const int r0 = block * 16 * RB;
   const int slot = kk.slot0 + split;
-  if (k0 >= k1) {
+  if (JOIN && kk.len[b] < 0) {                     // no such sequence
+    if (kk.behind) pdl_wait();                     // (no grid ends before the one that it is behind)
+    return;
+  }
+  if (!JOIN && k0 >= k1) {
     for (int r = r0 + tid; r < min(rows, r0 + 16 * RB); r += PM_THREADS)
       a.ml[(size_t)slot * a.rows() + pa_index(a, pa_row(a, kk.own, b, hk, r))] =
           make_float2(-INFINITY, 0.f);
@@ -241,9 +336,10 @@ pa_mma_kernel(const PaArgs a, const PaKeys kk, int rows, int blocks) {
       }
     }
     __syncthreads();
-    if (ph > 0) return;
+    if (!JOIN && ph > 0) return;
 #pragma unroll
     for (int p = 0; p < PH - 1; ++p) {
+      if (ph > 0) break;
       const int row = (p * RB + rb) * 16 + g;
       const float pm0 = xm[2 * row], pl0 = xm[2 * row + 1];
       const float pm1 = xm[2 * (row + 8)], pl1 = xm[2 * (row + 8) + 1];
@@ -264,6 +360,35 @@ pa_mma_kernel(const PaArgs a, const PaKeys kk, int rows, int blocks) {
         o[i][3] = o[i][3] * c1 + q1.y * e1;
       }
     }
+  }
+  if constexpr (JOIN) {
+    // the rows as they are to shared memory, then a warp a row
+    if constexpr (PH == 1) copy_wait<0>();
+    __syncthreads();
+    float* xr = reinterpret_cast<float*>(sm);
+    constexpr int XL = DP + 4;
+    float* xm = xr + (size_t)RB * 16 * XL;
+    if (ph == 0) {
+      const int row = rb * 16 + g;
+      if (c == 0) {
+        xm[2 * row] = m0; xm[2 * row + 1] = l0;
+        xm[2 * (row + 8)] = m1; xm[2 * (row + 8) + 1] = l1;
+      }
+#pragma unroll
+      for (int i = 0; i < OB; ++i) {
+        *reinterpret_cast<float2*>(xr + (size_t)row * XL + i * 8 + 2 * c) = make_float2(o[i][0], o[i][1]);
+        *reinterpret_cast<float2*>(xr + (size_t)(row + 8) * XL + i * 8 + 2 * c) =
+            make_float2(o[i][2], o[i][3]);
+      }
+    }
+    if (kk.behind) pdl_wait();
+    __syncthreads();
+    for (int r = warp; r < min(16 * RB, rows - r0); r += 4) {
+      const float4 own = lane < DP / 4 ? *reinterpret_cast<const float4*>(xr + (size_t)r * XL + lane * 4)
+                                       : make_float4(0.f, 0.f, 0.f, 0.f);
+      join_row<__nv_bfloat16>(a, pa_row(a, kk.own, b, hk, r0 + r), xm[2 * r], xm[2 * r + 1], own, lane);
+    }
+    return;
   }
   const int ra = r0 + rb * 16 + g;
 #pragma unroll
@@ -399,90 +524,27 @@ pa_simt_kernel(const PaArgs a, const PaKeys kk, int rows, int blocks) {
   }
 }
 
-// Join a row's pieces: one warp a row, four columns a lane.
-template <typename T>
-__global__ void __launch_bounds__(128)
-pa_combine_kernel(const PaArgs a) {
-  pdl_wait();
-  const int lane = threadIdx.x & 31;
-  const size_t rows = a.rows();
-  const size_t row = (size_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-  if (row >= rows) return;
-  const int h = (int)(row % a.Hq);
-  const size_t nt = row / a.Hq;
-  const int t = (int)(nt % a.T), n = (int)(nt / a.T);
-  if (a.seq_len[n] < 0) return;                   // no such sequence: its rows stay as they are
-  // pieces of the row: the segments of its item, then the slots
-  int segs = 0;
-  size_t seg0 = 0;
-  if (a.seg_ctas) {
-    const int g = n / a.W, hk = h / a.rep;
-    const int r = ((n - g * a.W) * a.T + t) * a.rep + (h - hk * a.rep);
-    const uint32_t hb = (uint32_t)a.Hkv * a.seg_blocks;
-    const uint32_t before = a.seg_start[g], tiles = a.seg_start[g + 1] - before;
-    if (tiles) {
-      const uint32_t per = pa_per_cta(a.seg_start[a.G] * hb, a.seg_ctas);
-      const uint32_t in = (uint32_t)hk * a.seg_blocks + r / PA_BLOCK;
-      const uint32_t first = before * hb + in * tiles;
-      const uint32_t c0 = first / per, c1 = (first + tiles - 1) / per;
-      segs = (int)(c1 - c0) + 1;
-      seg0 = ((size_t)c0 + (size_t)g * hb + in) * PA_BLOCK + r % PA_BLOCK;
-    }
-  }
-  const int pieces = segs + a.slots;
-  auto ml_of = [&](int s) {
-    return s < segs ? a.seg_ml[seg0 + (size_t)s * PA_BLOCK] : a.ml[(size_t)(s - segs) * rows + row];
-  };
-  auto po_of = [&](int s) {
-    return s < segs ? a.seg_po + (seg0 + (size_t)s * PA_BLOCK) * a.d
-                    : a.po + ((size_t)(s - segs) * rows + row) * a.d;
-  };
-  float M = -INFINITY;
-  for (int s = lane; s < pieces; s += 32) M = fmaxf(M, ml_of(s).x);
-  M = warp_max(M);
-  const float u = M == -INFINITY ? 0.f : M;
-  float L = 0.f;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int s0 = 0; s0 < pieces; s0 += 32) {
-    const float2 ml = s0 + lane < pieces ? ml_of(s0 + lane) : make_float2(-INFINITY, 0.f);
-    const float f = ml.x == -INFINITY ? 0.f : pa_ex2(ml.x - u);
-    L += f * ml.y;
-    for (int j = 0; j < min(32, pieces - s0); ++j) {
-      const float w = __shfl_sync(0xffffffffu, f, j);
-      const float mx = __shfl_sync(0xffffffffu, ml.x, j);
-      if (mx == -INFINITY || lane * 4 >= a.d) continue;    // no keys: nothing was written
-      const float4 p = *reinterpret_cast<const float4*>(po_of(s0 + j) + lane * 4);
-      o.x = fmaf(w, p.x, o.x);
-      o.y = fmaf(w, p.y, o.y);
-      o.z = fmaf(w, p.z, o.z);
-      o.w = fmaf(w, p.w, o.w);
-    }
-  }
-  L = warp_sum(L);
-  const float inv = L > 0.f ? 1.0f / L : (M == -INFINITY ? 0.f : L);
-  T* out = static_cast<T*>(a.out) + (int64_t)n * a.o_s[0] + (int64_t)t * a.o_s[1] + (int64_t)h * a.o_s[2];
-  if (lane * 4 < a.d) {
-    o.x *= inv; o.y *= inv; o.z *= inv; o.w *= inv;
-    if constexpr (sizeof(T) == 4)
-      *reinterpret_cast<float4*>(out + lane * 4) = o;
-    else
-      *reinterpret_cast<uint2*>(out + lane * 4) = make_uint2(bf16_pack2(o.x, o.y), bf16_pack2(o.z, o.w));
-  }
-  if (lane == 0) a.lse[row] = M == -INFINITY ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
-}
-
 int key_sets(const PaArgs& a, const PaKeys& k) { return k.own ? a.G * a.W : a.G; }
 int key_rows(const PaArgs& a, const PaKeys& k) { return (k.own ? 1 : a.W) * a.T * a.rep; }
 
-template <int DP, int RB>
+template <int DP, int RB, bool JOIN>
 lilicorr_status_t launch_mma(const PaArgs& a, const PaKeys& k, cudaStream_t st) {
   static bool configured[64] = {false};
-  LL_TRY(allow_max_dynamic_smem(pa_mma_kernel<DP, RB>, configured));
+  auto* kernel = pa_mma_kernel<DP, RB, JOIN>;
+  LL_TRY(allow_max_dynamic_smem(kernel, configured));
   const int rows = key_rows(a, k), blocks = ceil_div(rows, 16 * RB);
   const size_t smem = (size_t)PM_STAGES * 2 * PM_KT * (DP + 8) * 2;
   const size_t grid = (size_t)key_sets(a, k) * a.Hkv * blocks * k.splits;
   if (grid > 0x7FFFFFFFull) return LILICORR_ERR_SHAPE;
-  return launch_k(pa_mma_kernel<DP, RB>, (unsigned)grid, PM_THREADS, smem, st, a, k, rows, blocks);
+  return launch_k(kernel, (unsigned)grid, PM_THREADS, smem, st, a, k, rows, blocks);
+}
+
+template <int DP, bool JOIN>
+lilicorr_status_t launch_mma_rows(const PaArgs& a, const PaKeys& k, cudaStream_t st) {
+  const int rows = key_rows(a, k);
+  if (rows <= 16) return launch_mma<DP, 1, JOIN>(a, k, st);
+  if (rows <= 32) return launch_mma<DP, 2, JOIN>(a, k, st);
+  return launch_mma<DP, 4, JOIN>(a, k, st);
 }
 
 template <int DP>
@@ -499,15 +561,8 @@ lilicorr_status_t launch_simt(const PaArgs& a, const PaKeys& k, cudaStream_t st)
 }  // namespace
 
 lilicorr_status_t launch_pa_mma(const PaArgs& a, const PaKeys& k, cudaStream_t st) {
-  const int rows = key_rows(a, k);
-  if (a.d <= 64) {
-    if (rows <= 16) return launch_mma<64, 1>(a, k, st);
-    if (rows <= 32) return launch_mma<64, 2>(a, k, st);
-    return launch_mma<64, 4>(a, k, st);
-  }
-  if (rows <= 16) return launch_mma<128, 1>(a, k, st);
-  if (rows <= 32) return launch_mma<128, 2>(a, k, st);
-  return launch_mma<128, 4>(a, k, st);
+  if (k.join) return a.d <= 64 ? launch_mma_rows<64, true>(a, k, st) : launch_mma_rows<128, true>(a, k, st);
+  return a.d <= 64 ? launch_mma_rows<64, false>(a, k, st) : launch_mma_rows<128, false>(a, k, st);
 }
 
 lilicorr_status_t launch_pa_simt(const PaArgs& a, const PaKeys& k, cudaStream_t st) {
@@ -553,7 +608,7 @@ bool pa_plan(const lilicorr_prefix_attention_desc* d, PaPlan* p) {
     return (int)(n < 1 ? 1 : n > 128 ? 128 : n);
   };
   const long long prow = (long long)d->beams * d->tokens * rep;
-  const bool tc = d->dtype == LILICORR_BF16 && d->prefix_capacity;
+  const bool tc_type = d->dtype == LILICORR_BF16, tc = tc_type && d->prefix_capacity;
   const long long blocks = (prow + PA_BLOCK - 1) / PA_BLOCK;
   // (tiles are counted in 32 bits)
   if (tc && (double)d->groups * d->kv_heads * blocks * ((double)d->prefix_capacity / PA_TILE + 1) >=
@@ -564,7 +619,10 @@ bool pa_plan(const lilicorr_prefix_attention_desc* d, PaPlan* p) {
   p->psplits = d->prefix_capacity
                    ? pieces((long long)d->groups * d->kv_heads * ((prow + 63) / 64), d->prefix_capacity)
                    : 0;
-  p->ssplits = d->own_capacity ? pieces((long long)d->groups * d->beams * d->kv_heads, d->own_capacity) : 0;
+  // own keys: in one piece while that is a wave of CTAs or the keys are few
+  const long long own = (long long)d->groups * d->beams * d->kv_heads * ((d->tokens * (long long)rep + 63) / 64);
+  p->ssplits = !d->own_capacity ? 0
+               : tc_type && (own >= sms || d->own_capacity <= 512) ? 1 : pieces(own, d->own_capacity);
   p->rows = (size_t)rows;
   const size_t slots = (size_t)p->psplits + p->ssplits;
   const size_t segs = tc ? (size_t)sms + (size_t)d->groups * d->kv_heads * blocks : 0;
@@ -658,10 +716,14 @@ lilicorr_status_t lilicorr_prefix_attention(const lilicorr_prefix_attention_desc
   else pre.splits = 0;
   own.slot0 = pre.splits;
   a.slots = pre.splits + own.splits;
+  // the own keys in one piece: their kernel joins it with the prefix's and writes the result
+  own.join = bf && own.splits == 1;
+  own.behind = has_p;
+  if (own.join) a.slots = pre.splits;
   if (tc) LL_TRY(launch_pa_tc(a, pre, stream));
   else if (has_p) LL_TRY(bf ? launch_pa_mma(a, pre, stream) : launch_pa_simt(a, pre, stream));
   if (has_s) LL_TRY(bf ? launch_pa_mma(a, own, stream) : launch_pa_simt(a, own, stream));
-  return launch_pa_combine(a, desc->dtype, stream);
+  return own.join ? LILICORR_OK : launch_pa_combine(a, desc->dtype, stream);
 }
 
 }  // extern "C"

@@ -16,6 +16,8 @@ struct PaKeys {
   int splits;                  // pieces that each key range is cut into
   int slot0;                   // first partial slot
   int own;                     // 0: prefix, 1: the sequences' own keys (causal over the T tokens)
+  int join;                    // the kernel of these keys also joins all pieces and writes the result
+  int behind;                  // it runs behind the prefix's kernel of the same call
 };
 
 struct PaArgs {

@@ -127,8 +127,7 @@ pa_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
   uint8_t* sK = smem + 2 * Cfg::TILE;
   uint8_t* sV = sK + NK * Cfg::TILE;
   uint32_t* s_sum = reinterpret_cast<uint32_t*>(sQ);             // before the first Q
-  float* s_o = reinterpret_cast<float*>(sQ);                     // after the last product with Q
-  float2* s_ml = reinterpret_cast<float2*>(s_o + 32 * 128);
+  __shared__ float2 s_ml[128];
   __shared__ __align__(8) uint64_t k_full[NK], k_empty[NK], v_full[NV], v_empty[NV];
   __shared__ __align__(8) uint64_t s_ready[2], p_ready[2], o_ready[2];
   __shared__ uint32_t tmem_base;
@@ -323,21 +322,28 @@ pa_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       const int block = (int)(cur.item % a.seg_blocks), hk = (int)(cur.item / a.seg_blocks);
       const bool two = rows - block * PA_BLOCK > 128;
       const int end = pt_len(kk, cur.g) - (int)cur.tile * PA_TILE;
-      // Q of the block: 16-byte pieces in swizzled rows, zeros past the rows and the head's width
+      // Q of the block: 16-byte pieces in swizzled rows, zeros past the rows and the head's width. A lane
+      // finds the place of one row, the warp copies its 32 (or 16) rows one or two at a time.
       {
-        const int pieces = DP / 8, n = (two ? 256 : 128) * pieces;
-        const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.q);
-#pragma unroll 2
-        for (int x = tid; x < n; x += PT_SOFT) {
-          const int r = x / pieces, p = x % pieces;
-          uint4 v = make_uint4(0, 0, 0, 0);
-          if (block * PA_BLOCK + r < rows && p * 8 < a.d) {
-            const PaRow w = pa_row(a, 0, cur.g, hk, block * PA_BLOCK + r);
-            v = *reinterpret_cast<const uint4*>(q + (int64_t)w.n * a.q_s[0] + (int64_t)w.t * a.q_s[1] +
-                                                (int64_t)w.h * a.q_s[2] + p * 8);
-          }
-          *reinterpret_cast<uint4*>(sQ + (r >> 7) * Cfg::TILE + (p >> 3) * PT_CHUNK + swz(r & 127, p & 7)) = v;
+        constexpr int PIECES = DP / 8, AT_ONCE = 32 / PIECES;
+        const int per_warp = two ? 32 : 16, r0 = warp * per_warp;
+        int64_t off = -1;
+        if (lane < per_warp && block * PA_BLOCK + r0 + lane < rows) {
+          const PaRow w = pa_row(a, 0, cur.g, hk, block * PA_BLOCK + r0 + lane);
+          off = (int64_t)w.n * a.q_s[0] + (int64_t)w.t * a.q_s[1] + (int64_t)w.h * a.q_s[2];
         }
+        const int p = lane % PIECES;
+        for (int x = 0; x < per_warp; x += AT_ONCE) {
+          const int r = r0 + x + lane / PIECES;
+          const int64_t at = __shfl_sync(0xffffffffu, off, x + lane / PIECES);
+          const bool there = at >= 0 && p * 8 < a.d;
+          const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q) + (there ? at + p * 8 : 0);
+          const uint32_t dst = smem_u32(sQ + (r >> 7) * Cfg::TILE + (p >> 3) * PT_CHUNK + swz(r & 127, p & 7));
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src),
+                       "r"(there ? 16 : 0)
+                       : "memory");
+        }
+        asm volatile("cp.async.commit_group;\n cp.async.wait_group 0;" ::: "memory");
         fence_async_shared();
       }
       named_bar(1, PT_SOFT + 32);
@@ -462,19 +468,27 @@ pa_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       const uint32_t item = (uint32_t)cur.g * hb + cur.item;
       const size_t seg = ((size_t)blockIdx.x + item) * PA_BLOCK;
       const bool live = block * PA_BLOCK + r < rows;
-      if (!two && here > 1) {
-        // the streams' parts of the keys: the second's sums pass through Q's space (the rings may hold
-        // tiles of the next segment already), the first adds them to its own
-        named_bar(3, PT_SOFT);                         // every product with Q is done
-        if (s == 1) s_ml[row] = make_float2(m, l);
-        float f0 = 1.f, f1 = 0.f;
+      // the rows' sums to memory, 32 columns at a time by way of the warp's 4 KB of Q's space (every
+      // product with Q is done): a lane has a row there, and 128 bytes of a row leave together
+      named_bar(3, PT_SOFT);
+      const bool join = !two && here > 1;            // the streams have parts of the keys
+      if (join && s == 1) s_ml[row] = make_float2(m, l);
+      float f0 = 1.f, f1 = 0.f;
+      uint8_t* box = sQ + warp * 4096;
+      const uint8_t* other = sQ + ((warp & 3) + 4) * 4096;
+      auto piece = [&](int rr, int p) { return rr * 128 + ((p ^ (rr & 7)) << 4); };
 #pragma unroll 1
-        for (int c = 0; c < DP / 32; ++c) {
-          uint32_t o[32];
-          if (!idle) tmem_ld32(lane_base + Cfg::O(s) + 32 * c, o);
-          if (s == 1 && !idle) {
+      for (int c = 0; c < DP / 32; ++c) {
+        if (32 * c >= a.d) break;
+        uint32_t o[32];
+        const bool has = !idle && (two || s == 0 || join);
+        if (has) tmem_ld32(lane_base + Cfg::O(s) + 32 * c, o);
+        if (join) {
+          if (s == 1 && has) {
 #pragma unroll
-            for (int e = 0; e < 32; ++e) s_o[e * 128 + row] = __uint_as_float(o[e]);
+            for (int p = 0; p < 8; ++p)
+              *reinterpret_cast<uint4*>(box + piece(lane, p)) =
+                  make_uint4(o[4 * p], o[4 * p + 1], o[4 * p + 2], o[4 * p + 3]);
           }
           named_bar(3, PT_SOFT);
           if (s == 0 && c == 0) {
@@ -485,34 +499,35 @@ pa_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
             m = to;
             l = l * f0 + y.y * f1;
           }
-          if (s == 0 && ok && live) {
-            float* dst = a.seg_po + (seg + r) * a.d + 32 * c;
+          if (s == 0 && has) {
 #pragma unroll
-            for (int e = 0; e < 32; e += 4)
-              if (32 * c + e < a.d)
-                *reinterpret_cast<float4*>(dst + e) =
-                    make_float4(__uint_as_float(o[e]) * f0 + s_o[e * 128 + row] * f1,
-                                __uint_as_float(o[e + 1]) * f0 + s_o[(e + 1) * 128 + row] * f1,
-                                __uint_as_float(o[e + 2]) * f0 + s_o[(e + 2) * 128 + row] * f1,
-                                __uint_as_float(o[e + 3]) * f0 + s_o[(e + 3) * 128 + row] * f1);
-          }
-          named_bar(3, PT_SOFT);
-        }
-      } else if ((two || s == 0) && !idle) {
-#pragma unroll 1
-        for (int c = 0; c < DP / 32; ++c) {
-          uint32_t o[32];
-          tmem_ld32(lane_base + Cfg::O(s) + 32 * c, o);
-          if (ok && live) {
-            float* dst = a.seg_po + (seg + r) * a.d + 32 * c;
-#pragma unroll
-            for (int e = 0; e < 32; e += 4)
-              if (32 * c + e < a.d)
-                *reinterpret_cast<float4*>(dst + e) =
-                    make_float4(__uint_as_float(o[e]), __uint_as_float(o[e + 1]),
-                                __uint_as_float(o[e + 2]), __uint_as_float(o[e + 3]));
+            for (int p = 0; p < 8; ++p) {
+              const float4 y = *reinterpret_cast<const float4*>(other + piece(lane, p));
+              o[4 * p] = __float_as_uint(__uint_as_float(o[4 * p]) * f0 + y.x * f1);
+              o[4 * p + 1] = __float_as_uint(__uint_as_float(o[4 * p + 1]) * f0 + y.y * f1);
+              o[4 * p + 2] = __float_as_uint(__uint_as_float(o[4 * p + 2]) * f0 + y.z * f1);
+              o[4 * p + 3] = __float_as_uint(__uint_as_float(o[4 * p + 3]) * f0 + y.w * f1);
+            }
           }
         }
+        if (has && (two || s == 0)) {
+          __syncwarp();
+#pragma unroll
+          for (int p = 0; p < 8; ++p)
+            *reinterpret_cast<uint4*>(box + piece(lane, p)) =
+                make_uint4(o[4 * p], o[4 * p + 1], o[4 * p + 2], o[4 * p + 3]);
+          __syncwarp();
+          const int col = 32 * c + 4 * (lane & 7);
+          float* dst = a.seg_po + (seg + (r - lane)) * a.d + col;
+#pragma unroll
+          for (int x = 0; x < 32; x += 4) {
+            const int rr = x + (lane >> 3);
+            if (ok && col < a.d && block * PA_BLOCK + (r - lane) + rr < rows)
+              *reinterpret_cast<float4*>(dst + (size_t)rr * a.d) =
+                  *reinterpret_cast<const float4*>(box + piece(rr, lane & 7));
+          }
+        }
+        if (join) named_bar(3, PT_SOFT);             // the second stream's space is free again
       }
       if ((two || s == 0) && live) a.seg_ml[seg + r] = make_float2(m, l);
       i0 += here;
