@@ -864,8 +864,13 @@ struct Reorder {
 
 // One (array, request) per grid row. A thread owns one vector-wide column of all W beams: it loads
 // every beam that moves from its parent, then stores, so the move is in place without a second
-// buffer and without a barrier: nobody else reads or writes its column.
-template <typename V, int WMAX>
+// buffer and without a barrier: nobody else reads or writes its column. Bound by HBM: loads and stores
+// past the caches (nothing is read twice but a parent of several beams, by one thread) and many CTAs,
+// so that the run that a CTA takes of each beam is a few KB at a time: 32 x 8 beams of 4 x 512 x 2 KB,
+// 0.9 GB moved, 6.5 TB/s; 19 CTAs a pair instead of 76 6.1, cached accesses 5.6.
+// DENSE: the positions of a head follow one another, and the grid has the heads: no divisions, which
+// cost a third of the time (238 us).
+template <typename V, int WMAX, bool DENSE>
 __global__ void __launch_bounds__(BR_THREADS)
 beam_reorder_kernel(const __grid_constant__ Reorder a) {
   pdl_wait();
@@ -875,43 +880,56 @@ beam_reorder_kernel(const __grid_constant__ Reorder a) {
     const int p = a.parents[(size_t)r * a.W + tid];
     s_parent[tid] = (p < 0 || p >= a.W) ? tid : p;
   }
-  __syncthreads();
   int len = a.positions;
   if (a.lengths) len = min(max(a.lengths[r], 0), a.positions);
-  const uint32_t per_pos = (uint32_t)a.heads * a.pieces, total = (uint32_t)len * per_pos;
-  unsigned char* base = a.state[blockIdx.z] + (int64_t)r * a.s_req;
+  __syncthreads();
+  const uint32_t per_pos = DENSE ? a.pieces : (uint32_t)a.heads * a.pieces;
+  const uint32_t total = (uint32_t)len * per_pos;
+  const int st = DENSE ? blockIdx.z / a.heads : blockIdx.z;
+  unsigned char* base = a.state[st] + (int64_t)r * a.s_req;
+  if (DENSE) base += (int64_t)(blockIdx.z - st * a.heads) * a.s_head;
   for (uint32_t u = blockIdx.x * BR_THREADS + tid; u < total; u += gridDim.x * BR_THREADS) {
-    const uint32_t pos = u / per_pos, in = u - pos * per_pos, h = in / a.pieces, c = in - h * a.pieces;
-    unsigned char* col = base + (int64_t)pos * a.s_pos + (int64_t)h * a.s_head + (int64_t)c * sizeof(V);
+    unsigned char* col = base + (int64_t)u * sizeof(V);
+    if (!DENSE) {
+      const uint32_t pos = u / per_pos, in = u - pos * per_pos, h = in / a.pieces, c = in - h * a.pieces;
+      col = base + (int64_t)pos * a.s_pos + (int64_t)h * a.s_head + (int64_t)c * sizeof(V);
+    }
     V v[WMAX];
 #pragma unroll
     for (int w = 0; w < WMAX; ++w)
       if (w < a.W && s_parent[w] != w)
-        v[w] = *reinterpret_cast<const V*>(col + (int64_t)s_parent[w] * a.s_beam);
+        v[w] = __ldcs(reinterpret_cast<const V*>(col + (int64_t)s_parent[w] * a.s_beam));
 #pragma unroll
     for (int w = 0; w < WMAX; ++w)
-      if (w < a.W && s_parent[w] != w) *reinterpret_cast<V*>(col + (int64_t)w * a.s_beam) = v[w];
+      if (w < a.W && s_parent[w] != w) __stcs(reinterpret_cast<V*>(col + (int64_t)w * a.s_beam), v[w]);
   }
+}
+
+template <typename V, bool DENSE>
+lilicorr_status_t launch_reorder_form(const Reorder& a, int count, int requests, cudaStream_t st) {
+  const long long most = (long long)a.positions * a.pieces * (DENSE ? 1 : a.heads);
+  const long long z = (long long)count * (DENSE ? a.heads : 1), pairs = z * requests;
+  long long x = (most + BR_THREADS - 1) / BR_THREADS;
+  const long long want = (64ll * num_sms() + pairs - 1) / pairs;     // the rest by the loop
+  if (x > want) x = want;
+  if (x < 1) x = 1;
+  const dim3 grid((unsigned)x, (unsigned)requests, (unsigned)z);
+  if (a.W <= 4) return launch_k(beam_reorder_kernel<V, 4, DENSE>, grid, BR_THREADS, 0, st, a);
+  if (a.W <= 8) return launch_k(beam_reorder_kernel<V, 8, DENSE>, grid, BR_THREADS, 0, st, a);
+  if (a.W <= 16) return launch_k(beam_reorder_kernel<V, 16, DENSE>, grid, BR_THREADS, 0, st, a);
+  if constexpr (sizeof(V) <= 8)
+    if (a.W <= 32) return launch_k(beam_reorder_kernel<V, 32, DENSE>, grid, BR_THREADS, 0, st, a);
+  if constexpr (sizeof(V) <= 4)
+    return launch_k(beam_reorder_kernel<V, 64, DENSE>, grid, BR_THREADS, 0, st, a);
+  return LILICORR_ERR_SHAPE;
 }
 
 template <typename V>
 lilicorr_status_t launch_reorder(const Reorder& a, int count, int requests, cudaStream_t st) {
-  // CTAs for about four waves over all (array, request) pairs; the rest by the loop
-  const long long most = (long long)a.positions * a.heads * a.pieces;
-  const long long pairs = (long long)count * requests;
-  long long x = (most + BR_THREADS - 1) / BR_THREADS;
-  const long long want = (16ll * num_sms() + pairs - 1) / pairs;
-  if (x > want) x = want;
-  if (x < 1) x = 1;
-  const dim3 grid((unsigned)x, (unsigned)requests, (unsigned)count);
-  if (a.W <= 4) return launch_k(beam_reorder_kernel<V, 4>, grid, BR_THREADS, 0, st, a);
-  if (a.W <= 8) return launch_k(beam_reorder_kernel<V, 8>, grid, BR_THREADS, 0, st, a);
-  if (a.W <= 16) return launch_k(beam_reorder_kernel<V, 16>, grid, BR_THREADS, 0, st, a);
-  if constexpr (sizeof(V) <= 8)
-    if (a.W <= 32) return launch_k(beam_reorder_kernel<V, 32>, grid, BR_THREADS, 0, st, a);
-  if constexpr (sizeof(V) <= 4)
-    return launch_k(beam_reorder_kernel<V, 64>, grid, BR_THREADS, 0, st, a);
-  return LILICORR_ERR_SHAPE;
+  if ((a.positions == 1 || a.s_pos == (int64_t)a.pieces * (int64_t)sizeof(V)) &&
+      (long long)count * a.heads <= 65535)
+    return launch_reorder_form<V, true>(a, count, requests, st);
+  return launch_reorder_form<V, false>(a, count, requests, st);
 }
 
 size_t select_ws_bytes(int rows, int V, lilicorr_dtype_t dt) {

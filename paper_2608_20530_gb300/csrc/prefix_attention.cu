@@ -16,9 +16,7 @@ namespace lilicorr {
 
 namespace {
 
-constexpr int PM_THREADS = 128;
-constexpr int PM_KT = 64;                // keys per stage
-constexpr int PM_STAGES = 2;
+constexpr int PM_STAGES = 3;
 
 __device__ __forceinline__ uint32_t sm_addr(const void* p) {
   return static_cast<uint32_t>(__cvta_generic_to_shared(p));
@@ -66,77 +64,116 @@ __device__ __forceinline__ void stage_rows(unsigned char* dst, const unsigned ch
     copy16(dst + j * ld + p * 16, live ? src + (int64_t)(key0 + j) * s_pos + p * 16 : src, live);
   }
 }
+// the same, keys from `front` on up to `held` from a second place
+template <int KT, int PIECES, int NT>
+__device__ __forceinline__ void stage_rows(unsigned char* dst, const unsigned char* src, int64_t s_pos,
+                                           int ld, int key0, int front, int pieces, int tid,
+                                           const unsigned char* src2, int64_t s_pos2, int held) {
+#pragma unroll 4
+  for (int i = tid; i < KT * PIECES; i += NT) {
+    const int key = key0 + i / PIECES, p = i % PIECES;
+    const bool live = key < held && p < pieces;
+    const unsigned char* at = key < front ? src + (int64_t)key * s_pos : src2 + (int64_t)key * s_pos2;
+    copy16(dst + i / PIECES * ld + p * 16, live ? at + p * 16 : src, live);
+  }
+}
 
-// One row's result, by one warp, four columns a lane: the prefix's segments and the slots joined with
-// (m, l, o) that the warp has already (m -inf: nothing), to out and lse.
-template <typename T>
-__device__ __forceinline__ void join_row(const PaArgs& a, const PaRow& w, float m, float l, float4 o,
-                                         int lane) {
-  const size_t rows = a.rows(), row = pa_index(a, w);
-  int segs = 0;
-  size_t seg0 = 0;
-  if (a.seg_ctas) {
-    const int g = w.n / a.W, hk = w.h / a.rep;
-    const int r = ((w.n - g * a.W) * a.T + w.t) * a.rep + (w.h - hk * a.rep);
-    const uint32_t hb = (uint32_t)a.Hkv * a.seg_blocks;
-    const uint32_t before = a.seg_start[g], tiles = a.seg_start[g + 1] - before;
-    if (tiles) {
-      const uint32_t per = pa_per_cta(a.seg_start[a.G] * hb, a.seg_ctas);
-      const uint32_t in = (uint32_t)hk * a.seg_blocks + r / PA_BLOCK;
-      const uint32_t first = before * hb + in * tiles;
-      const uint32_t c0 = first / per, c1 = (first + tiles - 1) / per;
-      segs = (int)(c1 - c0) + 1;
-      seg0 = ((size_t)c0 + (size_t)g * hb + in) * PA_BLOCK + r % PA_BLOCK;
+// R rows' results, by one warp, four columns a lane: the prefix's segments and the slots joined with
+// (m, l, o) that the warp has already (m -inf: nothing), to out and lse. Several rows at a time, so that
+// their loads are under way together; `count` of them are there.
+template <typename T, int R>
+__device__ __forceinline__ void join_rows(const PaArgs& a, const PaRow (&w)[R], int count, float (&m)[R],
+                                          float (&l)[R], float4 (&o)[R], int lane) {
+  const size_t rows = a.rows();
+  size_t row[R], seg0[R];
+  int segs[R], most = 0;
+  const uint32_t hb = (uint32_t)a.Hkv * a.seg_blocks;
+  const uint32_t per = a.seg_ctas ? pa_per_cta(a.seg_start[a.G] * hb, a.seg_ctas) : 1u;
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    row[i] = pa_index(a, w[i]);
+    segs[i] = 0;
+    seg0[i] = 0;
+    if (i >= count) continue;
+    if (a.seg_ctas) {
+      const int g = w[i].n / a.W, hk = w[i].h / a.rep;
+      const int r = ((w[i].n - g * a.W) * a.T + w[i].t) * a.rep + (w[i].h - hk * a.rep);
+      const uint32_t before = a.seg_start[g], tiles = a.seg_start[g + 1] - before;
+      if (tiles) {
+        const uint32_t in = (uint32_t)hk * a.seg_blocks + r / PA_BLOCK;
+        const uint32_t first = before * hb + in * tiles;
+        const uint32_t c0 = first / per, c1 = (first + tiles - 1) / per;
+        segs[i] = (int)(c1 - c0) + 1;
+        seg0[i] = ((size_t)c0 + (size_t)g * hb + in) * PA_BLOCK + r % PA_BLOCK;
+      }
     }
+    most = max(most, segs[i] + a.slots);
   }
-  const int pieces = segs + a.slots;
-  auto ml_of = [&](int s) {
-    return s < segs ? a.seg_ml[seg0 + (size_t)s * PA_BLOCK] : a.ml[(size_t)(s - segs) * rows + row];
-  };
-  auto po_of = [&](int s) {
-    return s < segs ? a.seg_po + (seg0 + (size_t)s * PA_BLOCK) * a.d
-                    : a.po + ((size_t)(s - segs) * rows + row) * a.d;
-  };
-  for (int s0 = 0; s0 < pieces; s0 += 32) {
-    const float2 ml = s0 + lane < pieces ? ml_of(s0 + lane) : make_float2(-INFINITY, 0.f);
-    const float M = fmaxf(m, warp_max(ml.x)), u = M == -INFINITY ? 0.f : M;
-    const float keep = pa_ex2(m - u);
-    const float f = ml.x == -INFINITY ? 0.f : pa_ex2(ml.x - u);
-    m = M;
-    l = l * keep + warp_sum(f * ml.y);
-    o.x *= keep; o.y *= keep; o.z *= keep; o.w *= keep;
-    const unsigned there = __ballot_sync(0xffffffffu, ml.x != -INFINITY);    // others wrote no sums
-    const int n = min(32, pieces - s0);
-    constexpr int U = 4;                             // sums on their way together
+  constexpr int U = R >= 4 ? 2 : 4;                  // pieces of a row on their way together
+  for (int s0 = 0; s0 < most; s0 += 32) {
+    float f[R];
+    unsigned there[R];
+    float2 ml[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const int s = s0 + lane;
+      ml[i] = make_float2(-INFINITY, 0.f);
+      if (i < count && s < segs[i] + a.slots)
+        ml[i] = s < segs[i] ? a.seg_ml[seg0[i] + (size_t)s * PA_BLOCK]
+                            : a.ml[(size_t)(s - segs[i]) * rows + row[i]];
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const float M = fmaxf(m[i], warp_max(ml[i].x)), u = M == -INFINITY ? 0.f : M;
+      const float keep = pa_ex2(m[i] - u);
+      f[i] = ml[i].x == -INFINITY ? 0.f : pa_ex2(ml[i].x - u);
+      m[i] = M;
+      l[i] = l[i] * keep + warp_sum(f[i] * ml[i].y);
+      o[i].x *= keep; o[i].y *= keep; o[i].z *= keep; o[i].w *= keep;
+      there[i] = __ballot_sync(0xffffffffu, ml[i].x != -INFINITY);       // others wrote no sums
+    }
+    const int n = min(32, most - s0);
     for (int j0 = 0; j0 < n; j0 += U) {
-      float4 p[U];
+      float4 p[R][U];
 #pragma unroll
-      for (int u2 = 0; u2 < U; ++u2) {
-        p[u2] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (j0 + u2 < n && (there >> (j0 + u2) & 1u) && lane * 4 < a.d)
-          p[u2] = *reinterpret_cast<const float4*>(po_of(s0 + j0 + u2) + lane * 4);
-      }
+      for (int i = 0; i < R; ++i)
 #pragma unroll
-      for (int u2 = 0; u2 < U; ++u2) {
-        const float w2 = __shfl_sync(0xffffffffu, f, (j0 + u2) & 31);
-        if (j0 + u2 >= n) continue;
-        o.x = fmaf(w2, p[u2].x, o.x);
-        o.y = fmaf(w2, p[u2].y, o.y);
-        o.z = fmaf(w2, p[u2].z, o.z);
-        o.w = fmaf(w2, p[u2].w, o.w);
-      }
+        for (int v = 0; v < U; ++v) {
+          const int s = s0 + j0 + v;
+          p[i][v] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (j0 + v < n && (there[i] >> (j0 + v) & 1u) && lane * 4 < a.d)
+            p[i][v] = *reinterpret_cast<const float4*>(
+                (s < segs[i] ? a.seg_po + (seg0[i] + (size_t)s * PA_BLOCK) * a.d
+                             : a.po + ((size_t)(s - segs[i]) * rows + row[i]) * a.d) + lane * 4);
+        }
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int v = 0; v < U; ++v) {
+          const float x = __shfl_sync(0xffffffffu, f[i], (j0 + v) & 31);     // (0 with p: nothing there)
+          o[i].x = fmaf(x, p[i][v].x, o[i].x);
+          o[i].y = fmaf(x, p[i][v].y, o[i].y);
+          o[i].z = fmaf(x, p[i][v].z, o[i].z);
+          o[i].w = fmaf(x, p[i][v].w, o[i].w);
+        }
     }
   }
-  const float inv = l > 0.f ? 1.0f / l : (m == -INFINITY ? 0.f : l);       // (NaN stays)
-  T* out = static_cast<T*>(a.out) + (int64_t)w.n * a.o_s[0] + (int64_t)w.t * a.o_s[1] + (int64_t)w.h * a.o_s[2];
-  if (lane * 4 < a.d) {
-    o.x *= inv; o.y *= inv; o.z *= inv; o.w *= inv;
-    if constexpr (sizeof(T) == 4)
-      *reinterpret_cast<float4*>(out + lane * 4) = o;
-    else
-      *reinterpret_cast<uint2*>(out + lane * 4) = make_uint2(bf16_pack2(o.x, o.y), bf16_pack2(o.z, o.w));
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    if (i >= count) continue;
+    const float inv = l[i] > 0.f ? 1.0f / l[i] : (m[i] == -INFINITY ? 0.f : l[i]);       // (NaN stays)
+    T* out = static_cast<T*>(a.out) + (int64_t)w[i].n * a.o_s[0] + (int64_t)w[i].t * a.o_s[1] +
+             (int64_t)w[i].h * a.o_s[2];
+    if (lane * 4 < a.d) {
+      const float4 y = make_float4(o[i].x * inv, o[i].y * inv, o[i].z * inv, o[i].w * inv);
+      if constexpr (sizeof(T) == 4)
+        *reinterpret_cast<float4*>(out + lane * 4) = y;
+      else
+        *reinterpret_cast<uint2*>(out + lane * 4) = make_uint2(bf16_pack2(y.x, y.y), bf16_pack2(y.z, y.w));
+    }
+    if (lane == 0)
+      a.lse[row[i]] = m[i] == -INFINITY ? -INFINITY : (m[i] + log2f(l[i])) * 0.6931471805599453f;
   }
-  if (lane == 0) a.lse[row] = m == -INFINITY ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
 }
 
 // Join the rows' pieces where no kernel of the own keys does: one warp a row.
@@ -146,29 +183,37 @@ pa_combine_kernel(const PaArgs a) {
   pdl_wait();
   const size_t row = (size_t)blockIdx.x * 4 + (threadIdx.x >> 5);
   if (row >= a.rows()) return;
-  PaRow w;
-  w.h = (int)(row % a.Hq);
+  PaRow w[1];
+  w[0].h = (int)(row % a.Hq);
   const size_t nt = row / a.Hq;
-  w.t = (int)(nt % a.T);
-  w.n = (int)(nt / a.T);
-  if (a.seq_len[w.n] < 0) return;                   // no such sequence: its rows stay as they are
-  join_row<T>(a, w, -INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f), threadIdx.x & 31);
+  w[0].t = (int)(nt % a.T);
+  w[0].n = (int)(nt / a.T);
+  if (a.seq_len[w[0].n] < 0) return;                // no such sequence: its rows stay as they are
+  float m[1] = {-INFINITY}, l[1] = {0.f};
+  float4 o[1] = {make_float4(0.f, 0.f, 0.f, 0.f)};
+  join_rows<T, 1>(a, w, 1, m, l, o, threadIdx.x & 31);
 }
 
-// bf16: four warps, RB of the four over 16 query rows each, the other 4 / RB over the keys of a stage
+// bf16: RB of the CTA's warps over 16 query rows each, the others over the keys of a stage, KW keys a warp
 // (warp-level products; the pieces of the keys meet in shared memory at the end).
-// JOIN: the own keys in one piece; the kernel joins it with the prefix's pieces and writes the result. The
-// prefix's kernel runs before it and waited for everything before itself, so the inputs may be read, and
-// the own keys' part done, while that kernel still runs.
+// JOIN: the own keys in one piece, and the kernel writes the result: there is no prefix, or (`front`) its
+// keys come before the own ones in the kernel's own walk, and there is no other launch.
+template <int DP, int RB>
+struct PmCfg {
+  static constexpr int WARPS = 4, PH = WARPS / RB, KW = 64 / PH;
+  static constexpr int THREADS = 32 * WARPS, KT = PH * KW;
+  static constexpr int LD = (DP + 8) * 2;            // bytes of a staged row
+  static constexpr int STAGE = 2 * KT * LD;
+  static constexpr size_t SMEM = (size_t)PM_STAGES * STAGE;
+};
 template <int DP, int RB, bool JOIN>
-__global__ void __launch_bounds__(PM_THREADS, 3)
+__global__ void __launch_bounds__(32 * PmCfg<DP, RB>::WARPS, 12 / PmCfg<DP, RB>::WARPS)
 pa_mma_kernel(const PaArgs a, const PaKeys kk, int rows, int blocks) {
-  if (!JOIN || !kk.behind) pdl_wait();
-  constexpr int LD = (DP + 8) * 2;                  // bytes of a staged row
-  constexpr int PH = 4 / RB, KW = PM_KT / PH;       // key phases, keys per warp and stage
-  constexpr int KS = DP / 16, NB = KW / 8, OB = DP / 8;
+  pdl_wait();
+  using Cfg = PmCfg<DP, RB>;
+  constexpr int LD = Cfg::LD, PH = Cfg::PH, KW = Cfg::KW, KT = Cfg::KT, NT = Cfg::THREADS;
+  constexpr int KS = DP / 16, NB = KW / 8, OB = DP / 8, STAGE = Cfg::STAGE;
   extern __shared__ __align__(16) unsigned char sm[];
-  constexpr int STAGE = 2 * PM_KT * LD;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int rb = warp % RB, ph = warp / RB;
 
@@ -177,17 +222,16 @@ pa_mma_kernel(const PaArgs a, const PaKeys kk, int rows, int blocks) {
   const int hk = x % a.Hkv; x /= a.Hkv;
   const int b = x % (kk.own ? a.G * a.W : a.G);
   const int split = x / (kk.own ? a.G * a.W : a.G);
-  const int held = min(max(kk.len[b], 0), kk.capacity);
+  const int own = kk.len[b];
+  const int front = JOIN && kk.front ? min(max(kk.front_len[b / a.W], 0), kk.front_capacity) : 0;
+  const int held = front + min(max(own, 0), kk.capacity);
   int k0, k1;
   pa_piece(held, kk.splits, split, k0, k1);
   const int r0 = block * 16 * RB;
   const int slot = kk.slot0 + split;
-  if (JOIN && kk.len[b] < 0) {                     // no such sequence
-    if (kk.behind) pdl_wait();                     // (no grid ends before the one that it is behind)
-    return;
-  }
+  if (JOIN && own < 0) return;                     // no such sequence
   if (!JOIN && k0 >= k1) {
-    for (int r = r0 + tid; r < min(rows, r0 + 16 * RB); r += PM_THREADS)
+    for (int r = r0 + tid; r < min(rows, r0 + 16 * RB); r += NT)
       a.ml[(size_t)slot * a.rows() + pa_index(a, pa_row(a, kk.own, b, hk, r))] =
           make_float2(-INFINITY, 0.f);
     return;
@@ -196,19 +240,35 @@ pa_mma_kernel(const PaArgs a, const PaKeys kk, int rows, int blocks) {
                             2 * ((int64_t)b * kk.k_s[0] + (int64_t)hk * kk.k_s[2]);
   const unsigned char* vp = static_cast<const unsigned char*>(kk.v) +
                             2 * ((int64_t)b * kk.v_s[0] + (int64_t)hk * kk.v_s[2]);
-  const int pieces = a.d / 8, tiles = (k1 - k0 + PM_KT - 1) / PM_KT;
+  const unsigned char *fk = kp, *fv = vp;
+  if (front) {
+    fk = static_cast<const unsigned char*>(kk.front_k) +
+         2 * ((int64_t)(b / a.W) * kk.front_k_s[0] + (int64_t)hk * kk.front_k_s[2]);
+    fv = static_cast<const unsigned char*>(kk.front_v) +
+         2 * ((int64_t)(b / a.W) * kk.front_v_s[0] + (int64_t)hk * kk.front_v_s[2]);
+    kp -= 2 * (int64_t)front * kk.k_s[1];          // rows are counted from the front's first
+    vp -= 2 * (int64_t)front * kk.v_s[1];
+  }
+  const int pieces = a.d / 8, tiles = (k1 - k0 + KT - 1) / KT;
   auto stage = [&](int t) {
     unsigned char* s = sm + (t % PM_STAGES) * STAGE;
     if (t < tiles) {
-      stage_rows<PM_KT, DP / 8, PM_THREADS>(s, kp, kk.k_s[1] * 2, LD, k0 + t * PM_KT, k1, pieces, tid);
-      stage_rows<PM_KT, DP / 8, PM_THREADS>(s + PM_KT * LD, vp, kk.v_s[1] * 2, LD, k0 + t * PM_KT, k1,
-                                            pieces, tid);
+      const int key = k0 + t * KT;
+      if (front) {
+        stage_rows<KT, DP / 8, NT>(s, fk, kk.front_k_s[1] * 2, LD, key, min(k1, front), pieces, tid, kp,
+                                   kk.k_s[1] * 2, k1);
+        stage_rows<KT, DP / 8, NT>(s + KT * LD, fv, kk.front_v_s[1] * 2, LD, key, min(k1, front), pieces,
+                                   tid, vp, kk.v_s[1] * 2, k1);
+      } else {
+        stage_rows<KT, DP / 8, NT>(s, kp, kk.k_s[1] * 2, LD, key, k1, pieces, tid);
+        stage_rows<KT, DP / 8, NT>(s + KT * LD, vp, kk.v_s[1] * 2, LD, key, k1, pieces, tid);
+      }
     }
     copy_commit();
   };
   // the queries pass through the last stage's space
   unsigned char* sq = sm + (PM_STAGES - 1) * STAGE;
-  for (int i = tid; i < 16 * RB * (DP / 8); i += PM_THREADS) {
+  for (int i = tid; i < 16 * RB * (DP / 8); i += NT) {
     const int r = r0 + i / (DP / 8), p = i % (DP / 8);
     const bool live = r < rows && p < pieces;
     const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q);
@@ -233,8 +293,8 @@ pa_mma_kernel(const PaArgs a, const PaKeys kk, int rows, int blocks) {
   int lim0 = k1, lim1 = k1;
   if (kk.own) {
     const int t0 = (r0 + rb * 16 + g) / a.rep, t1 = (r0 + rb * 16 + g + 8) / a.rep;
-    lim0 = min(k1, held - (a.T - 1 - t0));
-    lim1 = min(k1, held - (a.T - 1 - t1));
+    lim0 = min(k1, max(front, held - (a.T - 1 - t0)));
+    lim1 = min(k1, max(front, held - (a.T - 1 - t1)));
   }
   float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
   float o[OB][4];
@@ -246,8 +306,8 @@ pa_mma_kernel(const PaArgs a, const PaKeys kk, int rows, int blocks) {
     __syncthreads();                               // tile t landed; tile t - 1's space is free
     stage(t + PM_STAGES - 1);
     const unsigned char* sk = sm + (t % PM_STAGES) * STAGE + ph * KW * LD;
-    const unsigned char* sv = sk + PM_KT * LD;
-    const int key0 = k0 + t * PM_KT + ph * KW;
+    const unsigned char* sv = sk + KT * LD;
+    const int key0 = k0 + t * KT + ph * KW;
     float s[NB][4];
 #pragma unroll
     for (int i = 0; i < NB; ++i) s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f;
@@ -381,12 +441,23 @@ pa_mma_kernel(const PaArgs a, const PaKeys kk, int rows, int blocks) {
             make_float2(o[i][2], o[i][3]);
       }
     }
-    if (kk.behind) pdl_wait();
     __syncthreads();
-    for (int r = warp; r < min(16 * RB, rows - r0); r += 4) {
-      const float4 own = lane < DP / 4 ? *reinterpret_cast<const float4*>(xr + (size_t)r * XL + lane * 4)
-                                       : make_float4(0.f, 0.f, 0.f, 0.f);
-      join_row<__nv_bfloat16>(a, pa_row(a, kk.own, b, hk, r0 + r), xm[2 * r], xm[2 * r + 1], own, lane);
+    constexpr int R = 4;
+    const int here = min(16 * RB, rows - r0);
+    for (int r = warp * R; r < here; r += R * Cfg::WARPS) {
+      PaRow w[R];
+      float jm[R], jl[R];
+      float4 jo[R];
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        const int y = min(r + i, here - 1);
+        w[i] = pa_row(a, kk.own, b, hk, r0 + y);
+        jm[i] = xm[2 * y];
+        jl[i] = xm[2 * y + 1];
+        jo[i] = lane < DP / 4 ? *reinterpret_cast<const float4*>(xr + (size_t)y * XL + lane * 4)
+                              : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+      join_rows<__nv_bfloat16, R>(a, w, min(R, here - r), jm, jl, jo, lane);
     }
     return;
   }
@@ -533,10 +604,10 @@ lilicorr_status_t launch_mma(const PaArgs& a, const PaKeys& k, cudaStream_t st) 
   auto* kernel = pa_mma_kernel<DP, RB, JOIN>;
   LL_TRY(allow_max_dynamic_smem(kernel, configured));
   const int rows = key_rows(a, k), blocks = ceil_div(rows, 16 * RB);
-  const size_t smem = (size_t)PM_STAGES * 2 * PM_KT * (DP + 8) * 2;
   const size_t grid = (size_t)key_sets(a, k) * a.Hkv * blocks * k.splits;
   if (grid > 0x7FFFFFFFull) return LILICORR_ERR_SHAPE;
-  return launch_k(kernel, (unsigned)grid, PM_THREADS, smem, st, a, k, rows, blocks);
+  return launch_k(kernel, (unsigned)grid, PmCfg<DP, RB>::THREADS, PmCfg<DP, RB>::SMEM, st, a, k, rows,
+                  blocks);
 }
 
 template <int DP, bool JOIN>
@@ -583,6 +654,12 @@ struct PaPlan {
   int seg_ctas, seg_blocks;
   size_t rows, ml_off, po_off, start_off, seg_ml_off, seg_po_off, total;
 };
+
+// A short prefix that few sequences share is read again by each of them, in the walk over their own keys.
+bool front_takes(const PaArgs& a, const PaKeys& pre) {
+  const long long ctas = (long long)a.G * a.W * a.Hkv * ceil_div((long long)a.T * a.rep, 64);
+  return pre.capacity <= 512 && ctas <= 2ll * num_sms();
+}
 
 bool stride_ok(const int64_t (&s)[3], const int (&extent)[3], int per16) {
   for (int i = 0; i < 3; ++i)
@@ -716,10 +793,19 @@ lilicorr_status_t lilicorr_prefix_attention(const lilicorr_prefix_attention_desc
   else pre.splits = 0;
   own.slot0 = pre.splits;
   a.slots = pre.splits + own.splits;
-  // the own keys in one piece: their kernel joins it with the prefix's and writes the result
-  own.join = bf && own.splits == 1;
-  own.behind = has_p;
-  if (own.join) a.slots = pre.splits;
+  // no prefix, or one that the own keys' kernel walks through first: one launch
+  own.join = bf && own.splits == 1 && (!has_p || front_takes(a, pre));
+  if (own.join) a.slots = 0;
+  if (own.join && has_p) {
+    own.front = 1;
+    own.front_k = pre.k;
+    own.front_v = pre.v;
+    for (int i = 0; i < 3; ++i) { own.front_k_s[i] = pre.k_s[i]; own.front_v_s[i] = pre.v_s[i]; }
+    own.front_len = pre.len;
+    own.front_capacity = pre.capacity;
+    a.seg_ctas = 0;
+    return launch_pa_mma(a, own, stream);
+  }
   if (tc) LL_TRY(launch_pa_tc(a, pre, stream));
   else if (has_p) LL_TRY(bf ? launch_pa_mma(a, pre, stream) : launch_pa_simt(a, pre, stream));
   if (has_s) LL_TRY(bf ? launch_pa_mma(a, own, stream) : launch_pa_simt(a, own, stream));

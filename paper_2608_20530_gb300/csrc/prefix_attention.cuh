@@ -16,8 +16,13 @@ struct PaKeys {
   int splits;                  // pieces that each key range is cut into
   int slot0;                   // first partial slot
   int own;                     // 0: prefix, 1: the sequences' own keys (causal over the T tokens)
-  int join;                    // the kernel of these keys also joins all pieces and writes the result
-  int behind;                  // it runs behind the prefix's kernel of the same call
+  int join;                    // the kernel of these keys writes the result
+  int front;                   // the prefix's keys come first in its own walk
+  const void* front_k;
+  const void* front_v;
+  int64_t front_k_s[3], front_v_s[3];
+  const int32_t* front_len;    // [groups]
+  int front_capacity;
 };
 
 struct PaArgs {
