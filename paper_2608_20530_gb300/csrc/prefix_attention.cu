@@ -86,13 +86,14 @@ __device__ __forceinline__ void join_rows(const PaArgs& a, const PaRow (&w)[R], 
                                           float (&l)[R], float4 (&o)[R], int lane) {
   const size_t rows = a.rows();
   size_t row[R], seg0[R];
-  int segs[R], most = 0;
+  int segs[R], step[R], most = 0;
   const uint32_t hb = (uint32_t)a.Hkv * a.seg_blocks;
   const uint32_t per = a.seg_ctas ? pa_per_cta(a.seg_start[a.G] * hb, a.seg_ctas) : 1u;
 #pragma unroll
   for (int i = 0; i < R; ++i) {
     row[i] = pa_index(a, w[i]);
     segs[i] = 0;
+    step[i] = PA_BLOCK;
     seg0[i] = 0;
     if (i >= count) continue;
     if (a.seg_ctas) {
@@ -103,7 +104,10 @@ __device__ __forceinline__ void join_rows(const PaArgs& a, const PaRow (&w)[R], 
         const uint32_t in = (uint32_t)hk * a.seg_blocks + r / PA_BLOCK;
         const uint32_t first = before * hb + in * tiles;
         const uint32_t c0 = first / per, c1 = (first + tiles - 1) / per;
-        segs[i] = (int)(c1 - c0) + 1;
+        // in halves of a block: one a segment where the block has two row tiles, else two pieces a segment
+        const bool two = a.seg_rows - r / PA_BLOCK * PA_BLOCK > 128;
+        step[i] = two ? PA_BLOCK : PA_BLOCK / 2;
+        segs[i] = ((int)(c1 - c0) + 1) * (two ? 1 : 2);
         seg0[i] = ((size_t)c0 + (size_t)g * hb + in) * PA_BLOCK + r % PA_BLOCK;
       }
     }
@@ -119,7 +123,7 @@ __device__ __forceinline__ void join_rows(const PaArgs& a, const PaRow (&w)[R], 
       const int s = s0 + lane;
       ml[i] = make_float2(-INFINITY, 0.f);
       if (i < count && s < segs[i] + a.slots)
-        ml[i] = s < segs[i] ? a.seg_ml[seg0[i] + (size_t)s * PA_BLOCK]
+        ml[i] = s < segs[i] ? a.seg_ml[seg0[i] + (size_t)s * step[i]]
                             : a.ml[(size_t)(s - segs[i]) * rows + row[i]];
     }
 #pragma unroll
@@ -143,7 +147,7 @@ __device__ __forceinline__ void join_rows(const PaArgs& a, const PaRow (&w)[R], 
           p[i][v] = make_float4(0.f, 0.f, 0.f, 0.f);
           if (j0 + v < n && (there[i] >> (j0 + v) & 1u) && lane * 4 < a.d)
             p[i][v] = *reinterpret_cast<const float4*>(
-                (s < segs[i] ? a.seg_po + (seg0[i] + (size_t)s * PA_BLOCK) * a.d
+                (s < segs[i] ? a.seg_po + (seg0[i] + (size_t)s * step[i]) * a.d
                              : a.po + ((size_t)(s - segs[i]) * rows + row[i]) * a.d) + lane * 4);
         }
 #pragma unroll
@@ -766,6 +770,7 @@ lilicorr_status_t lilicorr_prefix_attention(const lilicorr_prefix_attention_desc
   a.scale_log2 = desc->scale * PA_LOG2E;
   a.seg_ctas = p.seg_ctas;
   a.seg_blocks = p.seg_blocks;
+  a.seg_rows = a.W * a.T * a.rep;
   a.seg_start = reinterpret_cast<uint32_t*>(w + p.start_off);
   a.seg_ml = reinterpret_cast<float2*>(w + p.seg_ml_off);
   a.seg_po = reinterpret_cast<float*>(w + p.seg_po_off);

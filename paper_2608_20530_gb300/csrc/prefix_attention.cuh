@@ -42,6 +42,7 @@ struct PaArgs {
   // the prefix's pieces of the tensor-core kernel, kept by segment (PaSegments)
   int seg_ctas;                // its CTAs (0: the prefix's pieces are among the slots)
   int seg_blocks;              // blocks of PA_BLOCK rows per (group, key head)
+  int seg_rows;                // rows per (group, key head)
   float2* seg_ml;              // [segments][PA_BLOCK]
   float* seg_po;               // [segments][PA_BLOCK][d]
   uint32_t* seg_start;         // [G + 1] tiles before each group (of one key head and row block)
@@ -52,7 +53,8 @@ struct PaArgs {
 // The tensor-core kernel's work is the list of all (group, key head, block of PA_BLOCK rows, tile of
 // PA_TILE keys), in that order, cut evenly among its CTAs: CTA b takes tiles [b * per, (b + 1) * per). A
 // segment is what one CTA has of one (group, key head, block) = item; its number is CTA + item, which
-// no other segment has, the list being walked in order.
+// no other segment has, the list being walked in order. A block of 128 rows or fewer leaves two pieces a
+// segment, the second in the places of the rows from 128 on.
 constexpr int PA_BLOCK = 256;
 constexpr int PA_TILE = 128;
 constexpr int PA_MIN_TILES = 2;          // of a CTA

@@ -1,14 +1,14 @@
 // The shared prefix on the 5th-generation tensor cores (bf16): the rows of all sequences of a group
 // (PA_BLOCK at a time, two tiles of 128) against tiles of 128 of its keys.
 //
-// One CTA an SM. Warp 8 feeds K and V tiles by TMA into two rings. Warp 9 issues
+// One CTA an SM. Warps 8 and 10 feed K and V tiles by TMA into two rings. Warp 9 issues
 //   S = Q K^T   (M 128, N 128)   into tensor memory, and
 //   O += P V    (M 128, N d)     with P read from tensor memory, V as the MN-major operand.
 // Warps 0-3 and 4-7 are two streams, a thread a row: it reads the row's 128 scores (one wait: a load
 // from tensor memory takes 400 clocks beside running products), takes the running maximum, writes
 // P = 2^(s - m) as bf16 and keeps the row's sum. While one stream is at its exponentials the tensor
 // cores work for the other. With two row tiles the streams share each key tile; with one they take the
-// key tiles in turn and join at the end. Warps without a row do nothing but keep the count of arrivals.
+// key tiles in turn, and each leaves its own sums. Warps without a row do nothing but keep the count of arrivals.
 //
 // O is not rescaled whenever a maximum grows: m is the maximum that a row's sums are taken against, and
 // it moves only when a score would pass it by 2^8, so that terms stay below 2^8 and sums exact to fp32.
@@ -24,18 +24,23 @@ namespace lilicorr {
 namespace {
 using namespace tc;
 
-constexpr int PT_THREADS = 320;
+constexpr int PT_THREADS = 352;
 constexpr int PT_SOFT = 256;                         // of them in the streams
 constexpr uint32_t PT_CHUNK = 128 * 128;             // 128 rows of 128 bytes
 constexpr long long PT_WAIT = 4000000000ll;          // SM cycles, about 2 s
 constexpr uint32_t PT_TMEM = 512;
 
-template <int DP>
+// ONE: no group has more than 128 rows: one row tile, and the second's space goes to the rings, which
+// then hold three tiles of K and of V (d = 128) where two row tiles leave room for three and two. The
+// bytes under way are what bounds few rows: 32 rows a group, 41 K keys a head, 48 -> 36 us.
+template <int DP, bool ONE>
 struct PtCfg {
   static constexpr int CH = DP / 64;                 // 64-column chunks of a row
   static constexpr uint32_t TILE = CH * PT_CHUNK;    // bytes of a K, V or Q tile
-  static constexpr int NK = DP == 128 ? 3 : 5, NV = DP == 128 ? 2 : 5;
-  static constexpr size_t SMEM = 1024 + (size_t)(2 + NK + NV) * TILE;
+  static constexpr int NQ = ONE ? 1 : 2;
+  static constexpr int NK = DP == 128 ? 3 : 6, NV = DP == 128 ? (ONE ? 3 : 2) : 6;
+  static constexpr size_t QBYTES = NQ * TILE < 32768 ? 32768 : NQ * TILE;      // (and the rows' way out)
+  static constexpr size_t SMEM = 1024 + QBYTES + (size_t)(NK + NV) * TILE;
   // tensor-memory columns: scores, output, and the probabilities of keys [16 k, 16 k + 16). At d = 128
   // those lie over the scores, which their thread has read: the next scores of the stream are issued
   // behind the product that reads them, and products of one shape run in the order of issue. At d = 64 the two products differ in shape, and there is room elsewhere.
@@ -114,20 +119,19 @@ __device__ __forceinline__ void pt_next(const PaArgs& a, const PaKeys& k, Cursor
   }
 }
 
-template <int DP>
+template <int DP, bool ONE>
 __global__ void __launch_bounds__(PT_THREADS, 1)
 pa_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
              int copies, const PaArgs a, const PaKeys kk, int rows) {
-  using Cfg = PtCfg<DP>;
+  using Cfg = PtCfg<DP, ONE>;
   constexpr int NK = Cfg::NK, NV = Cfg::NV;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   uint8_t* sQ = smem;
-  uint8_t* sK = smem + 2 * Cfg::TILE;
+  uint8_t* sK = smem + Cfg::QBYTES;
   uint8_t* sV = sK + NK * Cfg::TILE;
   uint32_t* s_sum = reinterpret_cast<uint32_t*>(sQ);             // before the first Q
-  __shared__ float2 s_ml[128];
   __shared__ __align__(8) uint64_t k_full[NK], k_empty[NK], v_full[NV], v_empty[NV];
   __shared__ __align__(8) uint64_t s_ready[2], p_ready[2], o_ready[2];
   __shared__ uint32_t tmem_base;
@@ -198,34 +202,37 @@ pa_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     return true;
   };
 
-  if (warp == 8) {
-    // ---- copies: K and V tiles of all segments, as the rings have room
+  if (warp == 8 || warp == 10) {
+    // ---- copies, K by one warp and V by the other: a K tile's place is free as soon as its scores are
+    // there, long before V's, and waits for no V tile. The first queries go first: behind 24 MB of
+    // tiles that all SMs ask for at once they came 7 us later.
+    if (cur.left) named_bar(4, PT_SOFT + 64);
     if (lane == 0) {
-      uint32_t i = 0;
+      const bool is_k = warp == 8;
+      const CUtensorMap* map = is_k ? &map_k : &map_v;
+      uint64_t* full = is_k ? k_full : v_full;
+      uint64_t* empty = is_k ? k_empty : v_empty;
+      uint8_t* ring = is_k ? sK : sV;
+      const uint32_t slots = is_k ? NK : NV;
+      uint32_t slot = 0, parity = 1, issued = 0;
       bool ok = true;
       while (cur.left && ok) {
         const uint32_t here = pt_here(kk, cur);
         const int hk = (int)(cur.item / a.seg_blocks);
-        for (uint32_t t = 0; t < here; ++t, ++i) {
-          const int key = (int)(cur.tile + t) * PA_TILE;
-          const uint32_t ks = i % NK, vs = i % NV;
-          if (!wait(&k_empty[ks], ((i / NK) & 1u) ^ 1u)) { ok = false; break; }
-          mbar_expect_tx(&k_full[ks], Cfg::TILE);
+        for (uint32_t t = 0; t < here; ++t) {
+          if (!wait(&empty[slot], parity)) { ok = false; break; }
+          mbar_expect_tx(&full[slot], Cfg::TILE);
           for (int c = 0; c < copies; ++c)
-            tma_load_5d(sK + ks * Cfg::TILE + c * PT_CHUNK, &map_k, &k_full[ks], c * 64, key, 0, hk, cur.g);
-          if (!wait(&v_empty[vs], ((i / NV) & 1u) ^ 1u)) { ok = false; ++i; break; }
-          mbar_expect_tx(&v_full[vs], Cfg::TILE);
-          for (int c = 0; c < copies; ++c)
-            tma_load_5d(sV + vs * Cfg::TILE + c * PT_CHUNK, &map_v, &v_full[vs], c * 64, key, 0, hk, cur.g);
+            tma_load_5d(ring + slot * Cfg::TILE + c * PT_CHUNK, map, &full[slot], c * 64,
+                        (int)(cur.tile + t) * PA_TILE, 0, hk, cur.g);
+          ++issued;
+          if (++slot == slots) { slot = 0; parity ^= 1u; }
         }
         pt_next(a, kk, cur, here);
       }
-      if (!ok) {
-        // given up: the copies under way land before the CTA's memory goes
-        for (uint32_t j = i > NK ? i - NK : 0; j < i; ++j) mbar_wait(&k_full[j % NK], (j / NK) & 1u, PT_WAIT);
-        for (uint32_t j = i > NV + 1 ? i - NV - 1 : 0; j + 1 < i; ++j)
-          mbar_wait(&v_full[j % NV], (j / NV) & 1u, PT_WAIT);
-      }
+      if (!ok)                                       // given up: the copies under way land before the
+        for (uint32_t x = issued > slots ? issued - slots : 0; x < issued; ++x)      // CTA's memory goes
+          mbar_wait(&full[x % slots], (x / slots) & 1u, PT_WAIT);
     }
     __syncwarp();
   } else if (warp == 9) {
@@ -240,7 +247,7 @@ pa_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     while (cur.left) {
       const uint32_t here = pt_here(kk, cur);
       const int block = (int)(cur.item % a.seg_blocks);
-      const bool two = rows - block * PA_BLOCK > 128;
+      const bool two = !ONE && rows - block * PA_BLOCK > 128;
       const int end = pt_len(kk, cur.g) - (int)cur.tile * PA_TILE;       // keys from this segment on
       named_bar(1, PT_SOFT + 32);                    // Q is there
       tc_fence_after();
@@ -311,7 +318,7 @@ pa_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       named_bar(2, PT_SOFT + 32);                    // the segment is done with
       pt_next(a, kk, cur, here);
     }
-  } else {
+  } else if (warp < 8) {
     // ---- the streams: a thread a row
     const int s = warp >> 2, row = (warp & 3) * 32 + lane;
     const uint32_t lane_base = tmem + ((uint32_t)((warp & 3) * 32) << 16);
@@ -320,7 +327,7 @@ pa_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     while (cur.left) {
       const uint32_t here = pt_here(kk, cur);
       const int block = (int)(cur.item % a.seg_blocks), hk = (int)(cur.item / a.seg_blocks);
-      const bool two = rows - block * PA_BLOCK > 128;
+      const bool two = !ONE && rows - block * PA_BLOCK > 128;
       const int end = pt_len(kk, cur.g) - (int)cur.tile * PA_TILE;
       // Q of the block: 16-byte pieces in swizzled rows, zeros past the rows and the head's width. A lane
       // finds the place of one row, the warp copies its 32 (or 16) rows one or two at a time.
@@ -343,11 +350,11 @@ pa_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                        "r"(there ? 16 : 0)
                        : "memory");
         }
+        if (i0 == 0) named_bar(4, PT_SOFT + 64);       // the first segment's: the tiles may follow
         asm volatile("cp.async.commit_group;\n cp.async.wait_group 0;" ::: "memory");
         fence_async_shared();
       }
       named_bar(1, PT_SOFT + 32);
-      const int r = two ? s * 128 + row : row;       // of the block
       const int tile_rows = min(128, rows - block * PA_BLOCK - (two ? s * 128 : 0));
       const int warps = (tile_rows + 31) / 32;       // of the stream's that have rows
       const bool idle = (warp & 3) >= warps;
@@ -467,50 +474,18 @@ pa_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       }
       const uint32_t item = (uint32_t)cur.g * hb + cur.item;
       const size_t seg = ((size_t)blockIdx.x + item) * PA_BLOCK;
-      const bool live = block * PA_BLOCK + r < rows;
       // the rows' sums to memory, 32 columns at a time by way of the warp's 4 KB of Q's space (every
-      // product with Q is done): a lane has a row there, and 128 bytes of a row leave together
+      // product with Q is done): a lane has a row there, and 128 bytes of a row leave together. With one
+      // row tile the second stream's part of the keys takes the place of the second tile's rows.
       named_bar(3, PT_SOFT);
-      const bool join = !two && here > 1;            // the streams have parts of the keys
-      if (join && s == 1) s_ml[row] = make_float2(m, l);
-      float f0 = 1.f, f1 = 0.f;
+      const int place = s * 128 + (warp & 3) * 32;   // the warp's first row of the segment
       uint8_t* box = sQ + warp * 4096;
-      const uint8_t* other = sQ + ((warp & 3) + 4) * 4096;
       auto piece = [&](int rr, int p) { return rr * 128 + ((p ^ (rr & 7)) << 4); };
+      if (!idle && first < here) {
 #pragma unroll 1
-      for (int c = 0; c < DP / 32; ++c) {
-        if (32 * c >= a.d) break;
-        uint32_t o[32];
-        const bool has = !idle && (two || s == 0 || join);
-        if (has) tmem_ld32(lane_base + Cfg::O(s) + 32 * c, o);
-        if (join) {
-          if (s == 1 && has) {
-#pragma unroll
-            for (int p = 0; p < 8; ++p)
-              *reinterpret_cast<uint4*>(box + piece(lane, p)) =
-                  make_uint4(o[4 * p], o[4 * p + 1], o[4 * p + 2], o[4 * p + 3]);
-          }
-          named_bar(3, PT_SOFT);
-          if (s == 0 && c == 0) {
-            const float2 y = s_ml[row];
-            const float to = fmaxf(m, y.x), base = to == -INFINITY ? 0.f : to;
-            f0 = pa_ex2(m - base);
-            f1 = pa_ex2(y.x - base);
-            m = to;
-            l = l * f0 + y.y * f1;
-          }
-          if (s == 0 && has) {
-#pragma unroll
-            for (int p = 0; p < 8; ++p) {
-              const float4 y = *reinterpret_cast<const float4*>(other + piece(lane, p));
-              o[4 * p] = __float_as_uint(__uint_as_float(o[4 * p]) * f0 + y.x * f1);
-              o[4 * p + 1] = __float_as_uint(__uint_as_float(o[4 * p + 1]) * f0 + y.y * f1);
-              o[4 * p + 2] = __float_as_uint(__uint_as_float(o[4 * p + 2]) * f0 + y.z * f1);
-              o[4 * p + 3] = __float_as_uint(__uint_as_float(o[4 * p + 3]) * f0 + y.w * f1);
-            }
-          }
-        }
-        if (has && (two || s == 0)) {
+        for (int c = 0; 32 * c < a.d; ++c) {
+          uint32_t o[32];
+          tmem_ld32(lane_base + Cfg::O(s) + 32 * c, o);
           __syncwarp();
 #pragma unroll
           for (int p = 0; p < 8; ++p)
@@ -518,18 +493,17 @@ pa_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                 make_uint4(o[4 * p], o[4 * p + 1], o[4 * p + 2], o[4 * p + 3]);
           __syncwarp();
           const int col = 32 * c + 4 * (lane & 7);
-          float* dst = a.seg_po + (seg + (r - lane)) * a.d + col;
+          float* dst = a.seg_po + (seg + place) * a.d + col;
 #pragma unroll
           for (int x = 0; x < 32; x += 4) {
             const int rr = x + (lane >> 3);
-            if (ok && col < a.d && block * PA_BLOCK + (r - lane) + rr < rows)
+            if (ok && col < a.d && (warp & 3) * 32 + rr < tile_rows)
               *reinterpret_cast<float4*>(dst + (size_t)rr * a.d) =
                   *reinterpret_cast<const float4*>(box + piece(rr, lane & 7));
           }
         }
-        if (join) named_bar(3, PT_SOFT);             // the second stream's space is free again
       }
-      if ((two || s == 0) && live) a.seg_ml[seg + r] = make_float2(m, l);
+      if (row < tile_rows) a.seg_ml[seg + place + lane] = make_float2(m, l);
       i0 += here;
       tc_fence_before();
       named_bar(2, PT_SOFT + 32);
@@ -566,17 +540,17 @@ bool pt_map(CUtensorMap* map, const void* base, const int64_t (&s)[3], const PaA
   return make_map_nd(map, base, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, dims, strides, box);
 }
 
-template <int DP>
+template <int DP, bool ONE>
 lilicorr_status_t launch_tc(const PaArgs& a, const PaKeys& k, cudaStream_t st) {
   static bool configured[64] = {false};
-  LL_TRY(allow_max_dynamic_smem(pa_tc_kernel<DP>, configured));
+  auto* kernel = pa_tc_kernel<DP, ONE>;
+  LL_TRY(allow_max_dynamic_smem(kernel, configured));
   CUtensorMap mk, mv;
   int copies = 1;
   if (!pt_map(&mk, k.k, k.k_s, a, k.capacity, &copies) || !pt_map(&mv, k.v, k.v_s, a, k.capacity, &copies))
     return LILICORR_ERR_CUDA;
   const int rows = a.W * a.T * a.rep;
-  return launch_k(pa_tc_kernel<DP>, a.seg_ctas, PT_THREADS, PtCfg<DP>::SMEM, st, mk, mv, copies, a, k,
-                  rows);
+  return launch_k(kernel, a.seg_ctas, PT_THREADS, PtCfg<DP, ONE>::SMEM, st, mk, mv, copies, a, k, rows);
 }
 
 }  // namespace
@@ -589,7 +563,9 @@ bool pa_tc_takes(const PaArgs& a, const PaKeys& k) {
 }
 
 lilicorr_status_t launch_pa_tc(const PaArgs& a, const PaKeys& k, cudaStream_t st) {
-  return a.d <= 64 ? launch_tc<64>(a, k, st) : launch_tc<128>(a, k, st);
+  if (a.W * a.T * a.rep <= 128)
+    return a.d <= 64 ? launch_tc<64, true>(a, k, st) : launch_tc<128, true>(a, k, st);
+  return a.d <= 64 ? launch_tc<64, false>(a, k, st) : launch_tc<128, false>(a, k, st);
 }
 
 }  // namespace lilicorr
