@@ -198,6 +198,263 @@ pa_combine_kernel(const PaArgs a) {
   join_rows<T, 1>(a, w, 1, m, l, o, threadIdx.x & 31);
 }
 
+// What one CTA of the warp-level kernels has: a piece of the keys of one (group or sequence, key head) and
+// a block of the rows that meet them.
+struct PaPlace {
+  int block, hk, b, slot;
+  int own;                     // the sequence's own length as given
+  int front, held, k0, k1;     // keys of the prefix in front, all keys, this piece
+};
+template <bool JOIN>
+__device__ __forceinline__ PaPlace pa_place(const PaArgs& a, const PaKeys& kk, int blocks) {
+  PaPlace p;
+  int x = blockIdx.x;
+  p.block = x % blocks; x /= blocks;
+  p.hk = x % a.Hkv; x /= a.Hkv;
+  const int sets = kk.own ? a.G * a.W : a.G;
+  p.b = x % sets;
+  const int split = x / sets;
+  p.own = kk.len[p.b];
+  p.front = JOIN && kk.front ? min(max(kk.front_len[p.b / a.W], 0), kk.front_capacity) : 0;
+  p.held = p.front + min(max(p.own, 0), kk.capacity);
+  pa_piece(p.held, kk.splits, split, p.k0, p.k1);
+  p.slot = kk.slot0 + split;
+  return p;
+}
+// Where the keys of a place lie: its own from key `front` on, before that the prefix's.
+struct PaSource {
+  const unsigned char *k, *v, *fk, *fv;
+  int64_t k_s, v_s, fk_s, fv_s;                      // bytes from key to key
+};
+__device__ __forceinline__ PaSource pa_source(const PaArgs& a, const PaKeys& kk, const PaPlace& p, int es) {
+  PaSource s;
+  s.k_s = kk.k_s[1] * es;
+  s.v_s = kk.v_s[1] * es;
+  s.k = static_cast<const unsigned char*>(kk.k) +
+        es * ((int64_t)p.b * kk.k_s[0] + (int64_t)p.hk * kk.k_s[2]) - p.front * s.k_s;
+  s.v = static_cast<const unsigned char*>(kk.v) +
+        es * ((int64_t)p.b * kk.v_s[0] + (int64_t)p.hk * kk.v_s[2]) - p.front * s.v_s;
+  s.fk = s.k;
+  s.fv = s.v;
+  s.fk_s = s.fv_s = 0;
+  if (p.front) {
+    s.fk_s = kk.front_k_s[1] * es;
+    s.fv_s = kk.front_v_s[1] * es;
+    s.fk = static_cast<const unsigned char*>(kk.front_k) +
+           es * ((int64_t)(p.b / a.W) * kk.front_k_s[0] + (int64_t)p.hk * kk.front_k_s[2]);
+    s.fv = static_cast<const unsigned char*>(kk.front_v) +
+           es * ((int64_t)(p.b / a.W) * kk.front_v_s[0] + (int64_t)p.hk * kk.front_v_s[2]);
+  }
+  return s;
+}
+// Stage keys [key, key + KT) of K at dst and of V behind it.
+template <int KT, int PIECES, int NT>
+__device__ __forceinline__ void stage_tile(unsigned char* dst, const PaSource& s, const PaPlace& p, int ld,
+                                           int key, int pieces, int tid) {
+  if (p.front) {
+    stage_rows<KT, PIECES, NT>(dst, s.fk, s.fk_s, ld, key, min(p.k1, p.front), pieces, tid, s.k, s.k_s, p.k1);
+    stage_rows<KT, PIECES, NT>(dst + KT * ld, s.fv, s.fv_s, ld, key, min(p.k1, p.front), pieces, tid, s.v,
+                               s.v_s, p.k1);
+  } else {
+    stage_rows<KT, PIECES, NT>(dst, s.k, s.k_s, ld, key, p.k1, pieces, tid);
+    stage_rows<KT, PIECES, NT>(dst + KT * ld, s.v, s.v_s, ld, key, p.k1, pieces, tid);
+  }
+}
+// Rows [r0, r0 + n) of a place have no key: said in their slot.
+template <int NT>
+__device__ __forceinline__ void no_keys(const PaArgs& a, const PaKeys& kk, const PaPlace& p, int r0, int n,
+                                        int rows, int tid) {
+  for (int r = r0 + tid; r < min(rows, r0 + n); r += NT)
+    a.ml[(size_t)p.slot * a.rows() + pa_index(a, pa_row(a, kk.own, p.b, p.hk, r))] =
+        make_float2(-INFINITY, 0.f);
+}
+// Queries [r0, r0 + n) to shared memory, zeros behind the rows and the head's width.
+template <int N, int PIECES, int NT>
+__device__ __forceinline__ void stage_queries(unsigned char* dst, const PaArgs& a, const PaKeys& kk,
+                                              const PaPlace& p, int ld, int r0, int rows, int pieces,
+                                              int tid) {
+  for (int i = tid; i < N * PIECES; i += NT) {
+    const int r = r0 + i / PIECES, c = i % PIECES;
+    const bool live = r < rows && c < pieces;
+    const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q);
+    if (live) {
+      const PaRow w = pa_row(a, kk.own, p.b, p.hk, r);
+      src += (int64_t)w.n * a.q_s[0] + (int64_t)w.t * a.q_s[1] + (int64_t)w.h * a.q_s[2] + c * 8;
+    }
+    copy16(dst + i / PIECES * ld + c * 16, src, live);
+  }
+}
+
+// bf16, up to 8 rows a (group or sequence, key head): the products turned round, keys and columns of V as
+// the 16-row operand and the queries as the 8-wide one, S^T = K Q^T and O^T = V^T P^T, which halves the
+// instructions and the registers of 16-row tiles that are half empty. Four warps, 16 keys of a stage
+// each. Short caches are waits more than work: both stages are asked for before anything is waited for,
+// and three CTAs share an SM. The caller's `behind`: the launch before is of the same call and has waited
+// for everything before it, so that the inputs may be read at once; it is waited for at the end.
+constexpr int PF_THREADS = 128, PF_KT = 64, PF_STAGES = 2;
+template <int DP>
+struct PfCfg {
+  static constexpr int LD = (DP + 8) * 2, STAGE = 2 * PF_KT * LD;
+  static constexpr size_t SMEM = (size_t)PF_STAGES * STAGE + 8 * LD;
+};
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+template <int DP, bool JOIN>
+__global__ void __launch_bounds__(PF_THREADS, 3)
+pa_few_kernel(const PaArgs a, const PaKeys kk, int rows) {
+  if (!kk.behind) pdl_wait();
+  using Cfg = PfCfg<DP>;
+  constexpr int LD = Cfg::LD, KS = DP / 16, NT = PF_THREADS;
+  extern __shared__ __align__(16) unsigned char sm[];
+  unsigned char* sq = sm + PF_STAGES * Cfg::STAGE;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const PaPlace p = pa_place<JOIN>(a, kk, 1);
+  if (JOIN && p.own < 0) return;                     // no such sequence
+  if (!JOIN && p.k0 >= p.k1) {
+    if (kk.behind) pdl_wait();
+    no_keys<NT>(a, kk, p, 0, rows, rows, tid);
+    return;
+  }
+  const PaSource src = pa_source(a, kk, p, 2);
+  const int pieces = a.d / 8, tiles = (p.k1 - p.k0 + PF_KT - 1) / PF_KT;
+  auto stage = [&](int t) {
+    if (t < tiles)
+      stage_tile<PF_KT, DP / 8, NT>(sm + (t % PF_STAGES) * Cfg::STAGE, src, p, LD, p.k0 + t * PF_KT, pieces,
+                                    tid);
+    copy_commit();
+  };
+  stage_queries<8, DP / 8, NT>(sq, a, kk, p, LD, 0, rows, pieces, tid);
+  copy_commit();
+#pragma unroll
+  for (int t = 0; t < PF_STAGES; ++t) stage(t);
+  copy_wait<PF_STAGES>();
+  __syncthreads();
+  uint32_t qb[KS][2];
+#pragma unroll
+  for (int ks = 0; ks < KS; ks += 2) {
+    uint32_t x[4];
+    ldsm4(sm_addr(sq + (lane & 7) * LD + (ks * 16 + (lane >> 3) * 8) * 2), x);
+    qb[ks][0] = x[0];
+    qb[ks][1] = x[1];
+    qb[ks + 1][0] = x[2];
+    qb[ks + 1][1] = x[3];
+  }
+  // this thread's two rows, 2 c and 2 c + 1, and how many keys each may see
+  const int g = lane >> 2, c = lane & 3;
+  int lim[2];
+#pragma unroll
+  for (int e = 0; e < 2; ++e)
+    lim[e] = kk.own ? min(p.k1, max(p.front, p.held - (a.T - 1 - (2 * c + e) / a.rep))) : p.k1;
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+  float o[KS][4];
+#pragma unroll
+  for (int i = 0; i < KS; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+
+  for (int t = 0; t < tiles; ++t) {
+    copy_wait<PF_STAGES - 1>();
+    __syncthreads();                                 // tile t landed
+    const unsigned char* sk = sm + (t % PF_STAGES) * Cfg::STAGE + warp * 16 * LD;
+    const unsigned char* sv = sk + PF_KT * LD;
+    const int key = p.k0 + t * PF_KT + warp * 16 + g;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      uint32_t ka[4];
+      ldsm4(sm_addr(sk + (lane & 15) * LD + (ks * 16 + (lane >> 4) * 8) * 2), ka);
+      mma_16x8x16(s, ka, qb[ks][0], qb[ks][1]);
+    }
+    uint32_t pb[2];
+    float f[2], pr[4];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const float s0 = key < lim[e] ? s[e] * a.scale_log2 : -INFINITY;
+      const float s1 = key + 8 < lim[e] ? s[2 + e] * a.scale_log2 : -INFINITY;
+      float top = fmaxf(s0, s1);
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+      const float n = fmaxf(m[e], top);
+      // a row that has seen no key yet keeps maximum -inf; its terms are taken against 0
+      const float u = n == -INFINITY ? 0.f : n;
+      f[e] = pa_ex2(m[e] - u);
+      m[e] = n;
+      pr[e] = pa_ex2(s0 - u);
+      pr[2 + e] = pa_ex2(s1 - u);
+      l[e] = l[e] * f[e] + (pr[e] + pr[2 + e]);      // this thread's keys
+    }
+    pb[0] = transpose8(bf16_pack2(pr[0], pr[1]));
+    pb[1] = transpose8(bf16_pack2(pr[2], pr[3]));
+#pragma unroll
+    for (int i = 0; i < KS; ++i) {
+      o[i][0] *= f[0]; o[i][1] *= f[1];
+      o[i][2] *= f[0]; o[i][3] *= f[1];
+      uint32_t va[4];
+      ldsm4_t(sm_addr(sv + ((lane & 7) + ((lane >> 4) << 3)) * LD + (i * 16 + ((lane >> 3) & 1) * 8) * 2), va);
+      mma_16x8x16(o[i], va, pb[0], pb[1]);
+    }
+    __syncthreads();                                 // the tile's space is free
+    stage(t + PF_STAGES);
+  }
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    l[e] += __shfl_xor_sync(0xffffffffu, l[e], 4);
+    l[e] += __shfl_xor_sync(0xffffffffu, l[e], 8);
+    l[e] += __shfl_xor_sync(0xffffffffu, l[e], 16);
+  }
+  // the warps' parts of the keys, a warp a row
+  copy_wait<0>();
+  __syncthreads();
+  constexpr int XL = DP + 4;
+  float* xo = reinterpret_cast<float*>(sm);          // [warp][row][XL]
+  float2* xm = reinterpret_cast<float2*>(xo + 4 * 8 * XL);
+  if (g == 0) {
+    xm[warp * 8 + 2 * c] = make_float2(m[0], l[0]);
+    xm[warp * 8 + 2 * c + 1] = make_float2(m[1], l[1]);
+  }
+#pragma unroll
+  for (int i = 0; i < KS; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      xo[(warp * 8 + 2 * c + (e & 1)) * XL + i * 16 + g + (e >> 1) * 8] = o[i][e];
+  __syncthreads();
+  if (kk.behind) pdl_wait();
+  for (int r = warp; r < rows; r += 4) {
+    float M = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) M = fmaxf(M, xm[w * 8 + r].x);
+    const float u = M == -INFINITY ? 0.f : M;
+    float L = 0.f;
+    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float2 ml = xm[w * 8 + r];
+      const float x = pa_ex2(ml.x - u);
+      L += x * ml.y;
+      if (lane < DP / 4) {
+        const float4 z = *reinterpret_cast<const float4*>(xo + (w * 8 + r) * XL + lane * 4);
+        y.x = fmaf(x, z.x, y.x);
+        y.y = fmaf(x, z.y, y.y);
+        y.z = fmaf(x, z.z, y.z);
+        y.w = fmaf(x, z.w, y.w);
+      }
+    }
+    const PaRow w = pa_row(a, kk.own, p.b, p.hk, r);
+    if constexpr (JOIN) {
+      PaRow jw[1] = {w};
+      float jm[1] = {M}, jl[1] = {L};
+      float4 jo[1] = {y};
+      join_rows<__nv_bfloat16, 1>(a, jw, 1, jm, jl, jo, lane);
+    } else {
+      const size_t at = (size_t)p.slot * a.rows() + pa_index(a, w);
+      if (lane == 0) a.ml[at] = make_float2(M, L);
+      if (lane * 4 < a.d) *reinterpret_cast<float4*>(a.po + at * a.d + lane * 4) = y;
+    }
+  }
+}
+
 // bf16: RB of the CTA's warps over 16 query rows each, the others over the keys of a stage, KW keys a warp
 // (warp-level products; the pieces of the keys meet in shared memory at the end).
 // JOIN: the own keys in one piece, and the kernel writes the result: there is no prefix, or (`front`) its
@@ -213,7 +470,7 @@ struct PmCfg {
 template <int DP, int RB, bool JOIN>
 __global__ void __launch_bounds__(32 * PmCfg<DP, RB>::WARPS, 12 / PmCfg<DP, RB>::WARPS)
 pa_mma_kernel(const PaArgs a, const PaKeys kk, int rows, int blocks) {
-  pdl_wait();
+  if (!kk.behind) pdl_wait();
   using Cfg = PmCfg<DP, RB>;
   constexpr int LD = Cfg::LD, PH = Cfg::PH, KW = Cfg::KW, KT = Cfg::KT, NT = Cfg::THREADS;
   constexpr int KS = DP / 16, NB = KW / 8, OB = DP / 8, STAGE = Cfg::STAGE;
@@ -221,67 +478,25 @@ pa_mma_kernel(const PaArgs a, const PaKeys kk, int rows, int blocks) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int rb = warp % RB, ph = warp / RB;
 
-  int x = blockIdx.x;
-  const int block = x % blocks; x /= blocks;
-  const int hk = x % a.Hkv; x /= a.Hkv;
-  const int b = x % (kk.own ? a.G * a.W : a.G);
-  const int split = x / (kk.own ? a.G * a.W : a.G);
-  const int own = kk.len[b];
-  const int front = JOIN && kk.front ? min(max(kk.front_len[b / a.W], 0), kk.front_capacity) : 0;
-  const int held = front + min(max(own, 0), kk.capacity);
-  int k0, k1;
-  pa_piece(held, kk.splits, split, k0, k1);
-  const int r0 = block * 16 * RB;
-  const int slot = kk.slot0 + split;
-  if (JOIN && own < 0) return;                     // no such sequence
+  const PaPlace p = pa_place<JOIN>(a, kk, blocks);
+  const int hk = p.hk, b = p.b, front = p.front, held = p.held, k0 = p.k0, k1 = p.k1, slot = p.slot;
+  const int r0 = p.block * 16 * RB;
+  if (JOIN && p.own < 0) return;                   // no such sequence
   if (!JOIN && k0 >= k1) {
-    for (int r = r0 + tid; r < min(rows, r0 + 16 * RB); r += NT)
-      a.ml[(size_t)slot * a.rows() + pa_index(a, pa_row(a, kk.own, b, hk, r))] =
-          make_float2(-INFINITY, 0.f);
+    if (kk.behind) pdl_wait();
+    no_keys<NT>(a, kk, p, r0, 16 * RB, rows, tid);
     return;
   }
-  const unsigned char* kp = static_cast<const unsigned char*>(kk.k) +
-                            2 * ((int64_t)b * kk.k_s[0] + (int64_t)hk * kk.k_s[2]);
-  const unsigned char* vp = static_cast<const unsigned char*>(kk.v) +
-                            2 * ((int64_t)b * kk.v_s[0] + (int64_t)hk * kk.v_s[2]);
-  const unsigned char *fk = kp, *fv = vp;
-  if (front) {
-    fk = static_cast<const unsigned char*>(kk.front_k) +
-         2 * ((int64_t)(b / a.W) * kk.front_k_s[0] + (int64_t)hk * kk.front_k_s[2]);
-    fv = static_cast<const unsigned char*>(kk.front_v) +
-         2 * ((int64_t)(b / a.W) * kk.front_v_s[0] + (int64_t)hk * kk.front_v_s[2]);
-    kp -= 2 * (int64_t)front * kk.k_s[1];          // rows are counted from the front's first
-    vp -= 2 * (int64_t)front * kk.v_s[1];
-  }
+  const PaSource src = pa_source(a, kk, p, 2);
   const int pieces = a.d / 8, tiles = (k1 - k0 + KT - 1) / KT;
   auto stage = [&](int t) {
-    unsigned char* s = sm + (t % PM_STAGES) * STAGE;
-    if (t < tiles) {
-      const int key = k0 + t * KT;
-      if (front) {
-        stage_rows<KT, DP / 8, NT>(s, fk, kk.front_k_s[1] * 2, LD, key, min(k1, front), pieces, tid, kp,
-                                   kk.k_s[1] * 2, k1);
-        stage_rows<KT, DP / 8, NT>(s + KT * LD, fv, kk.front_v_s[1] * 2, LD, key, min(k1, front), pieces,
-                                   tid, vp, kk.v_s[1] * 2, k1);
-      } else {
-        stage_rows<KT, DP / 8, NT>(s, kp, kk.k_s[1] * 2, LD, key, k1, pieces, tid);
-        stage_rows<KT, DP / 8, NT>(s + KT * LD, vp, kk.v_s[1] * 2, LD, key, k1, pieces, tid);
-      }
-    }
+    if (t < tiles)
+      stage_tile<KT, DP / 8, NT>(sm + (t % PM_STAGES) * STAGE, src, p, LD, k0 + t * KT, pieces, tid);
     copy_commit();
   };
   // the queries pass through the last stage's space
   unsigned char* sq = sm + (PM_STAGES - 1) * STAGE;
-  for (int i = tid; i < 16 * RB * (DP / 8); i += NT) {
-    const int r = r0 + i / (DP / 8), p = i % (DP / 8);
-    const bool live = r < rows && p < pieces;
-    const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q);
-    if (live) {
-      const PaRow w = pa_row(a, kk.own, b, hk, r);
-      src += (int64_t)w.n * a.q_s[0] + (int64_t)w.t * a.q_s[1] + (int64_t)w.h * a.q_s[2] + p * 8;
-    }
-    copy16(sq + (i / (DP / 8)) * LD + p * 16, src, live);
-  }
+  stage_queries<16 * RB, DP / 8, NT>(sq, a, kk, p, LD, r0, rows, pieces, tid);
   copy_commit();
 #pragma unroll
   for (int t = 0; t < PM_STAGES - 1; ++t) stage(t);
@@ -400,7 +615,10 @@ pa_mma_kernel(const PaArgs a, const PaKeys kk, int rows, int blocks) {
       }
     }
     __syncthreads();
-    if (!JOIN && ph > 0) return;
+    if (!JOIN && ph > 0) {
+      if (kk.behind) pdl_wait();
+      return;
+    }
 #pragma unroll
     for (int p = 0; p < PH - 1; ++p) {
       if (ph > 0) break;
@@ -465,6 +683,7 @@ pa_mma_kernel(const PaArgs a, const PaKeys kk, int rows, int blocks) {
     }
     return;
   }
+  if (kk.behind) pdl_wait();
   const int ra = r0 + rb * 16 + g;
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
@@ -617,6 +836,14 @@ lilicorr_status_t launch_mma(const PaArgs& a, const PaKeys& k, cudaStream_t st) 
 template <int DP, bool JOIN>
 lilicorr_status_t launch_mma_rows(const PaArgs& a, const PaKeys& k, cudaStream_t st) {
   const int rows = key_rows(a, k);
+  if (rows <= 8) {
+    static bool configured[64] = {false};
+    auto* kernel = pa_few_kernel<DP, JOIN>;
+    LL_TRY(allow_max_dynamic_smem(kernel, configured));
+    const size_t grid = (size_t)key_sets(a, k) * a.Hkv * k.splits;
+    if (grid > 0x7FFFFFFFull) return LILICORR_ERR_SHAPE;
+    return launch_k(kernel, (unsigned)grid, PF_THREADS, PfCfg<DP>::SMEM, st, a, k, rows);
+  }
   if (rows <= 16) return launch_mma<DP, 1, JOIN>(a, k, st);
   if (rows <= 32) return launch_mma<DP, 2, JOIN>(a, k, st);
   return launch_mma<DP, 4, JOIN>(a, k, st);
@@ -811,6 +1038,7 @@ lilicorr_status_t lilicorr_prefix_attention(const lilicorr_prefix_attention_desc
     a.seg_ctas = 0;
     return launch_pa_mma(a, own, stream);
   }
+  own.behind = bf && has_p;
   if (tc) LL_TRY(launch_pa_tc(a, pre, stream));
   else if (has_p) LL_TRY(bf ? launch_pa_mma(a, pre, stream) : launch_pa_simt(a, pre, stream));
   if (has_s) LL_TRY(bf ? launch_pa_mma(a, own, stream) : launch_pa_simt(a, own, stream));

@@ -17,6 +17,7 @@ struct PaKeys {
   int slot0;                   // first partial slot
   int own;                     // 0: prefix, 1: the sequences' own keys (causal over the T tokens)
   int join;                    // the kernel of these keys writes the result
+  int behind;                  // the launch before it is the prefix's of the same call
   int front;                   // the prefix's keys come first in its own walk
   const void* front_k;
   const void* front_v;
