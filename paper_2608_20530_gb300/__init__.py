@@ -527,17 +527,26 @@ def select_block(head: Head, logits: torch.Tensor, hidden: torch.Tensor, target:
 
 
 # --------------------------------------------------------------------------- beams
-def _beam_args(dev: int, scores: torch.Tensor, done: Optional[torch.Tensor], R: int, W: int, n: int):
-    _here(scores, "scores", dev, torch.float32, (R, W), True)
+def _refuse(t: torch.Tensor, name: str, dev: int, dtype: Optional[torch.dtype], shape) -> None:
+    """The reason why ``t`` was refused: what _here says, or that it is not contiguous."""
+    _here(t, name, dev, dtype, shape)
+    raise ValueError(f"{name} must be contiguous")
+
+
+def _beam_outputs(scores: torch.Tensor, done: Optional[torch.Tensor], dev: int, shape, R: int, n: int):
+    """Checks of the beams' scores and done flags (the same for both calls), and the outputs."""
+    if (scores.get_device() != dev or scores.dtype is not torch.float32 or scores.shape != shape or
+            not scores.is_contiguous()):
+        _refuse(scores, "scores", dev, torch.float32, shape)
     if done is not None:
         if done.dtype is not torch.bool and done.dtype is not torch.uint8:
             raise ValueError("done must be bool or uint8")
-        _here(done, "done", dev, None, (R, W), True)
-    shape, on = (R, max(n, 0)), scores.device
-    return (torch.empty(shape, dtype=torch.int32, device=on),
-            torch.empty(shape, dtype=torch.int32, device=on),
-            torch.empty(shape, dtype=torch.float32, device=on),
-            torch.empty(shape, dtype=torch.bool, device=on))
+        if done.get_device() != dev or done.shape != shape or not done.is_contiguous():
+            _refuse(done, "done", dev, None, shape)
+    size, on = (R, n if n > 0 else 0), scores.device
+    empty = torch.empty
+    return (empty(size, dtype=torch.int32, device=on), empty(size, dtype=torch.int32, device=on),
+            empty(size, dtype=torch.float32, device=on), empty(size, dtype=torch.bool, device=on))
 
 
 def beam_select_workspace_bytes(requests: int, beams: int, V: int, n: int) -> int:
@@ -552,19 +561,22 @@ def beam_select(logits: torch.Tensor, scores: torch.Tensor, n: int,
     [R, W, V] (fp32 or bf16) and running scores [R, W] fp32 -> (tokens [R, n] int32, parents [R, n]
     int32, scores [R, n] fp32, done [R, n] bool), best first. A score of -inf is an absent beam;
     beams that are ``done`` [R, W] keep their score and offer ``end_id`` (see lilicorr.h)."""
-    if logits.dim() != 3:
+    shape = logits.shape
+    if len(shape) != 3:
         raise ValueError("logits must be [requests, beams, V]")
     dev = torch.cuda.current_device()
-    _here(logits, "logits", dev, dense=True)
-    R, W, V = logits.shape
-    n = int(n)
-    tokens, parents, best, over = out = _beam_args(dev, scores, done, R, W, n)
+    if logits.get_device() != dev or not logits.is_contiguous():
+        _refuse(logits, "logits", dev, None, None)
+    R, W, V = shape
+    tokens, parents, best, over = out = _beam_outputs(scores, done, dev, shape[:2], R, n)
     if ws is None:
         ws = Workspace(beam_select_workspace_bytes(R, W, V, n), logits.device)
-    _check(lib().lilicorr_beam_select(logits.data_ptr(), _dtype_code(logits), R, W, V, n,
-                                      scores.data_ptr(), _ptr(done), end_id, tokens.data_ptr(),
-                                      parents.data_ptr(), best.data_ptr(), over.data_ptr(), ws.ptr,
-                                      ws.nbytes, _stream()), "beam_select")
+    status = lib().lilicorr_beam_select(
+        logits.data_ptr(), _dtype_code(logits), R, W, V, n, scores.data_ptr(),
+        None if done is None else done.data_ptr(), end_id, tokens.data_ptr(), parents.data_ptr(),
+        best.data_ptr(), over.data_ptr(), ws.buf.data_ptr(), ws.nbytes, _stream())
+    if status:
+        _check(status, "beam_select")
     return out
 
 
@@ -573,20 +585,25 @@ def beam_merge(ids: torch.Tensor, logp: torch.Tensor, scores: torch.Tensor, n: i
                status: Optional[torch.Tensor] = None):
     """beam_select from candidate lists ids [R, W, K] int32, logp [R, W, K] fp32 (of topk_lse,
     lm_head_topk or topk_lse_merge): the exact beam search step where K >= min(n, V)."""
-    if ids.dim() != 3:
+    shape = ids.shape
+    if len(shape) != 3:
         raise ValueError("ids must be [requests, beams, K]")
     dev = torch.cuda.current_device()
-    R, W, K = shape = ids.shape
-    n = int(n)
-    _here(ids, "ids", dev, torch.int32, None, True)
-    _here(logp, "logp", dev, torch.float32, shape, True)
+    R, W, K = shape
+    if ids.get_device() != dev or ids.dtype is not torch.int32 or not ids.is_contiguous():
+        _refuse(ids, "ids", dev, torch.int32, None)
+    if (logp.get_device() != dev or logp.dtype is not torch.float32 or logp.shape != shape or
+            not logp.is_contiguous()):
+        _refuse(logp, "logp", dev, torch.float32, shape)
     if status is not None:
         _here(status, "status", dev)
-    tokens, parents, best, over = out = _beam_args(dev, scores, done, R, W, n)
-    _check(lib().lilicorr_beam_merge(ids.data_ptr(), logp.data_ptr(), R, W, K, n, scores.data_ptr(),
-                                     _ptr(done), end_id, tokens.data_ptr(), parents.data_ptr(),
-                                     best.data_ptr(), over.data_ptr(), _ptr(status), _stream()),
-           "beam_merge")
+    tokens, parents, best, over = out = _beam_outputs(scores, done, dev, shape[:2], R, n)
+    code = lib().lilicorr_beam_merge(
+        ids.data_ptr(), logp.data_ptr(), R, W, K, n, scores.data_ptr(),
+        None if done is None else done.data_ptr(), end_id, tokens.data_ptr(), parents.data_ptr(),
+        best.data_ptr(), over.data_ptr(), None if status is None else status.data_ptr(), _stream())
+    if code:
+        _check(code, "beam_merge")
     return out
 
 
@@ -618,46 +635,41 @@ def beam_reorder(states, parents: torch.Tensor, lengths: Optional[torch.Tensor] 
         raise ValueError("parents must be [requests, beams]")
     R, W = parents.shape
     dev = torch.cuda.current_device()
-    _here(parents, "parents", dev, torch.int32, None, True)
-    if lengths is not None:
-        _here(lengths, "lengths", dev, torch.int32, (R,), True)
+    if parents.get_device() != dev or parents.dtype is not torch.int32 or not parents.is_contiguous():
+        _refuse(parents, "parents", dev, torch.int32, None)
+    if lengths is not None and (lengths.get_device() != dev or lengths.dtype is not torch.int32 or
+                                lengths.shape != (R,) or not lengths.is_contiguous()):
+        _refuse(lengths, "lengths", dev, torch.int32, (R,))
     # arrays of one layout go together
     groups: Dict[tuple, list] = {}
-    layouts: Dict[tuple, tuple] = {}
     for i, t in enumerate(tensors):
-        _here(t, f"states[{i}]", dev)
-        key = (t.shape, t.stride(), t.dtype)
-        layout = layouts.get(key)
-        if layout is None:
-            layout = layouts[key] = _state_layout(t, R, W, f"states[{i}]")
-        groups.setdefault(layout, []).append(t.data_ptr())
-    for (positions, heads, row, *strides), ptrs in groups.items():
-        _check(lib().lilicorr_beam_reorder((_P * len(ptrs))(*ptrs), len(ptrs), R, W, positions, heads,
-                                           row, *strides, parents.data_ptr(), _ptr(lengths),
-                                           _stream()), "beam_reorder")
+        if t.get_device() != dev:
+            _here(t, f"states[{i}]", dev)
+        groups.setdefault((t.shape, t.stride(), t.dtype), []).append(t)
+    for same in groups.values():
+        i = next(i for i, t in enumerate(tensors) if t is same[0])
+        positions, heads, row, *strides = _state_layout(same[0], R, W, f"states[{i}]")
+        code = lib().lilicorr_beam_reorder(
+            (_P * len(same))(*[t.data_ptr() for t in same]), len(same), R, W, positions, heads, row,
+            *strides, parents.data_ptr(), None if lengths is None else lengths.data_ptr(), _stream())
+        if code:
+            _check(code, "beam_reorder")
     return states
 
 
 # --------------------------------------------------------------------------- shared prefixes
 _PA_DESC = struct.Struct("9if18q")          # the layout of lilicorr_prefix_attention_desc
-_NO_STRIDES = (0,) * 18
-
-
-def _attention_desc(q: torch.Tensor, prefix_k: torch.Tensor, k: torch.Tensor, scale: float,
-                    strides=_NO_STRIDES) -> bytes:
+def prefix_attention_workspace_bytes(q: torch.Tensor, prefix_k: torch.Tensor, k: torch.Tensor) -> int:
+    """Bytes of the workspace that prefix_attention needs for tensors of these shapes."""
     if q.dim() != 4 or prefix_k.dim() != 4 or k.dim() != 4:
         raise ValueError("q is [N, T, q_heads, d], caches are [groups or N, capacity, kv_heads, d]")
     N, T, Hq, d = q.shape
     G, P, Hkv, _ = prefix_k.shape
-    if N % max(G, 1) or (G == 0 and N):
+    if N % G if G else N:
         raise ValueError(f"{N} sequences do not divide into {G} groups")
-    return _PA_DESC.pack(G, N // G if G else 1, T, Hq, Hkv, d, P, k.shape[1], _dtype_code(q), scale,
-                         *strides)
-
-
-def prefix_attention_workspace_bytes(q: torch.Tensor, prefix_k: torch.Tensor, k: torch.Tensor) -> int:
-    """Bytes of the workspace that prefix_attention needs for tensors of these shapes."""
-    return int(lib().lilicorr_prefix_attention_workspace_bytes(_attention_desc(q, prefix_k, k, 1.0)))
+    return int(lib().lilicorr_prefix_attention_workspace_bytes(
+        _PA_DESC.pack(G, N // G if G else 1, T, Hq, Hkv, d, P, k.shape[1], _dtype_code(q), 1.0,
+                      *(0,) * 18)))
 
 
 def prefix_attention(q: torch.Tensor, prefix_k: torch.Tensor, prefix_v: torch.Tensor, k: torch.Tensor,
@@ -670,37 +682,44 @@ def prefix_attention(q: torch.Tensor, prefix_k: torch.Tensor, prefix_v: torch.Te
     T newest included (causal among them) -> (out like q, lse [N, T, q_heads] fp32). fp32 or bf16, any
     strides that keep 16-byte rows. seq_len < 0: no such sequence, its rows of ``out`` and ``lse``
     stay as they are. scale defaults to 1 / sqrt(d)."""
-    if q.dim() != 4 or prefix_k.dim() != 4 or k.dim() != 4:
+    qs, ps, ks = q.shape, prefix_k.shape, k.shape
+    if len(qs) != 4 or len(ps) != 4 or len(ks) != 4:
         raise ValueError("q is [N, T, q_heads, d], caches are [groups or N, capacity, kv_heads, d]")
     dev, dt = torch.cuda.current_device(), q.dtype
-    N, T, Hq, d = qs = q.shape
-    G, P, Hkv, _ = ps = prefix_k.shape
-    ks = k.shape
-    if ks[0] != N or ks[2] != Hkv or ks[3] != d or ps[3] != d:
+    N, T, Hq, d = qs
+    G, P, Hkv, _ = ps
+    if ks[0] != N or ks[2] != Hkv or ks[3] != d or ps[3] != d or (N % G if G else N):
         raise ValueError(f"caches {tuple(ps)} and {tuple(ks)} do not go with q {tuple(qs)}")
     if out is None:
         out = torch.empty(qs, dtype=dt, device=q.device)
     if lse is None:
         lse = torch.empty((N, T, Hq), dtype=torch.float32, device=q.device)
     strides: list = []
-    for t, name, shape in ((q, "q", qs), (out, "out", qs), (prefix_k, "prefix_k", ps),
-                           (prefix_v, "prefix_v", ps), (k, "k", ks), (v, "v", ks)):
-        _here(t, name, dev, dt, shape)
-        a, b, c, one = t.stride()
-        if one != 1 and d > 1 and t.numel():
+    for t, shape in ((q, qs), (out, qs), (prefix_k, ps), (prefix_v, ps), (k, ks), (v, ks)):
+        st = t.stride()
+        if t.get_device() != dev or t.dtype is not dt or t.shape != shape or (
+                st[3] != 1 and d > 1 and t.numel()):
+            name = next(n for n, x in (("q", q), ("out", out), ("prefix_k", prefix_k),
+                                       ("prefix_v", prefix_v), ("k", k), ("v", v)) if x is t)
+            _here(t, name, dev, dt, shape)
             raise ValueError(f"{name}: the last dimension must be dense")
-        strides += (a, b, c)
-    _here(lse, "lse", dev, torch.float32, (N, T, Hq), True)
-    _here(prefix_len, "prefix_len", dev, torch.int32, (G,), True)
-    _here(seq_len, "seq_len", dev, torch.int32, (N,), True)
-    desc = _attention_desc(q, prefix_k, k, scale if scale is not None else max(d, 1) ** -0.5, strides)
+        strides += st[:3]
+    if lse.get_device() != dev or lse.dtype is not torch.float32 or lse.shape != (N, T, Hq) or \
+            not lse.is_contiguous():
+        _refuse(lse, "lse", dev, torch.float32, (N, T, Hq))
+    for t, n in ((prefix_len, G), (seq_len, N)):
+        if t.get_device() != dev or t.dtype is not torch.int32 or t.shape != (n,) or not t.is_contiguous():
+            _refuse(t, "prefix_len" if t is prefix_len else "seq_len", dev, torch.int32, (n,))
+    desc = _PA_DESC.pack(G, N // G if G else 1, T, Hq, Hkv, d, P, ks[1], _dtype_code(q),
+                         max(d, 1) ** -0.5 if scale is None else scale, *strides)
     if ws is None:
         ws = Workspace(int(lib().lilicorr_prefix_attention_workspace_bytes(desc)), q.device)
-    _check(lib().lilicorr_prefix_attention(desc, q.data_ptr(), prefix_k.data_ptr(),
-                                           prefix_v.data_ptr(), prefix_len.data_ptr(), k.data_ptr(),
-                                           v.data_ptr(), seq_len.data_ptr(), out.data_ptr(),
-                                           lse.data_ptr(), ws.ptr, ws.nbytes, _stream()),
-           "prefix_attention")
+    status = lib().lilicorr_prefix_attention(
+        desc, q.data_ptr(), prefix_k.data_ptr(), prefix_v.data_ptr(), prefix_len.data_ptr(),
+        k.data_ptr(), v.data_ptr(), seq_len.data_ptr(), out.data_ptr(), lse.data_ptr(),
+        ws.buf.data_ptr(), ws.nbytes, _stream())
+    if status:
+        _check(status, "prefix_attention")
     return out, lse
 
 

@@ -1020,14 +1020,9 @@ lilicorr_status_t lilicorr_prefix_attention(const lilicorr_prefix_attention_desc
   own.k = k; own.v = v; own.len = seq_len;
   own.capacity = desc->own_capacity; own.splits = p.ssplits; own.own = 1;
   const bool bf = desc->dtype == LILICORR_BF16;
-  const bool tc = has_p && bf && pa_tc_takes(a, pre);
-  if (!tc) a.seg_ctas = 0;
-  else pre.splits = 0;
-  own.slot0 = pre.splits;
-  a.slots = pre.splits + own.splits;
   // no prefix, or one that the own keys' kernel walks through first: one launch
   own.join = bf && own.splits == 1 && (!has_p || front_takes(a, pre));
-  if (own.join) a.slots = 0;
+  a.slots = 0;
   if (own.join && has_p) {
     own.front = 1;
     own.front_k = pre.k;
@@ -1038,8 +1033,14 @@ lilicorr_status_t lilicorr_prefix_attention(const lilicorr_prefix_attention_desc
     a.seg_ctas = 0;
     return launch_pa_mma(a, own, stream);
   }
+  PaMaps maps;
+  const bool tc = has_p && bf && pa_tc_maps(a, pre, &maps);
+  if (!tc) a.seg_ctas = 0;
+  else pre.splits = 0;
+  own.slot0 = pre.splits;
+  a.slots = own.join ? 0 : pre.splits + own.splits;
   own.behind = bf && has_p;
-  if (tc) LL_TRY(launch_pa_tc(a, pre, stream));
+  if (tc) LL_TRY(launch_pa_tc(a, pre, maps, stream));
   else if (has_p) LL_TRY(bf ? launch_pa_mma(a, pre, stream) : launch_pa_simt(a, pre, stream));
   if (has_s) LL_TRY(bf ? launch_pa_mma(a, own, stream) : launch_pa_simt(a, own, stream));
   return own.join ? LILICORR_OK : launch_pa_combine(a, desc->dtype, stream);

@@ -1,5 +1,6 @@
 // Attention of sequences that share their request's prefix: what its kernels have in common.
 #pragma once
+#include <cuda.h>
 
 #include "internal.cuh"
 
@@ -92,9 +93,14 @@ __device__ __forceinline__ float pa_ex2(float x) {
   return y;
 }
 
-// the prefix on the 5th-generation tensor cores (prefix_attention_tc.cu)
-bool pa_tc_takes(const PaArgs& a, const PaKeys& k);
-lilicorr_status_t launch_pa_tc(const PaArgs& a, const PaKeys& k, cudaStream_t st);
+// the prefix on the 5th-generation tensor cores (prefix_attention_tc.cu): false where the driver makes no
+// tensor maps of these keys (an expanded dimension)
+struct PaMaps {
+  CUtensorMap k, v;
+  int copies;                  // of a tile
+};
+bool pa_tc_maps(const PaArgs& a, const PaKeys& k, PaMaps* maps);
+lilicorr_status_t launch_pa_tc(const PaArgs& a, const PaKeys& k, const PaMaps& maps, cudaStream_t st);
 lilicorr_status_t launch_pa_mma(const PaArgs& a, const PaKeys& k, cudaStream_t st);
 lilicorr_status_t launch_pa_simt(const PaArgs& a, const PaKeys& k, cudaStream_t st);
 lilicorr_status_t launch_pa_combine(const PaArgs& a, lilicorr_dtype_t dt, cudaStream_t st);

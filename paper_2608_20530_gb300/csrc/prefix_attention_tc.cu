@@ -541,31 +541,25 @@ bool pt_map(CUtensorMap* map, const void* base, const int64_t (&s)[3], const PaA
 }
 
 template <int DP, bool ONE>
-lilicorr_status_t launch_tc(const PaArgs& a, const PaKeys& k, cudaStream_t st) {
+lilicorr_status_t launch_tc(const PaArgs& a, const PaKeys& k, const PaMaps& m, cudaStream_t st) {
   static bool configured[64] = {false};
   auto* kernel = pa_tc_kernel<DP, ONE>;
   LL_TRY(allow_max_dynamic_smem(kernel, configured));
-  CUtensorMap mk, mv;
-  int copies = 1;
-  if (!pt_map(&mk, k.k, k.k_s, a, k.capacity, &copies) || !pt_map(&mv, k.v, k.v_s, a, k.capacity, &copies))
-    return LILICORR_ERR_CUDA;
-  const int rows = a.W * a.T * a.rep;
-  return launch_k(kernel, a.seg_ctas, PT_THREADS, PtCfg<DP, ONE>::SMEM, st, mk, mv, copies, a, k, rows);
+  return launch_k(kernel, a.seg_ctas, PT_THREADS, PtCfg<DP, ONE>::SMEM, st, m.k, m.v, m.copies, a, k,
+                  a.seg_rows);
 }
 
 }  // namespace
 
-bool pa_tc_takes(const PaArgs& a, const PaKeys& k) {
-  CUtensorMap m;
-  int copies;
-  return encode_fn() != nullptr && pt_map(&m, k.k, k.k_s, a, k.capacity, &copies) &&
-         pt_map(&m, k.v, k.v_s, a, k.capacity, &copies);
+bool pa_tc_maps(const PaArgs& a, const PaKeys& k, PaMaps* m) {
+  return encode_fn() != nullptr && pt_map(&m->k, k.k, k.k_s, a, k.capacity, &m->copies) &&
+         pt_map(&m->v, k.v, k.v_s, a, k.capacity, &m->copies);
 }
 
-lilicorr_status_t launch_pa_tc(const PaArgs& a, const PaKeys& k, cudaStream_t st) {
-  if (a.W * a.T * a.rep <= 128)
-    return a.d <= 64 ? launch_tc<64, true>(a, k, st) : launch_tc<128, true>(a, k, st);
-  return a.d <= 64 ? launch_tc<64, false>(a, k, st) : launch_tc<128, false>(a, k, st);
+lilicorr_status_t launch_pa_tc(const PaArgs& a, const PaKeys& k, const PaMaps& m, cudaStream_t st) {
+  if (a.seg_rows <= 128)
+    return a.d <= 64 ? launch_tc<64, true>(a, k, m, st) : launch_tc<128, true>(a, k, m, st);
+  return a.d <= 64 ? launch_tc<64, false>(a, k, m, st) : launch_tc<128, false>(a, k, m, st);
 }
 
 }  // namespace lilicorr
