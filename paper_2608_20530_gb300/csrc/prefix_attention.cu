@@ -709,49 +709,35 @@ constexpr int PS_STAGES = 2;
 template <int DP>
 __global__ void __launch_bounds__(PS_THREADS)
 pa_simt_kernel(const PaArgs a, const PaKeys kk, int rows, int blocks) {
-  pdl_wait();
+  if (!kk.behind) pdl_wait();
   constexpr int LD = (DP + 4) * 4;
   constexpr int STAGE = 2 * PS_KT * LD;
   extern __shared__ __align__(16) unsigned char sm[];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  int x = blockIdx.x;
-  const int block = x % blocks; x /= blocks;
-  const int hk = x % a.Hkv; x /= a.Hkv;
-  const int b = x % (kk.own ? a.G * a.W : a.G);
-  const int split = x / (kk.own ? a.G * a.W : a.G);
-  const int held = min(max(kk.len[b], 0), kk.capacity);
-  int k0, k1;
-  pa_piece(held, kk.splits, split, k0, k1);
-  const int r0 = block * PS_ROWS;
-  const int slot = kk.slot0 + split;
+  const PaPlace p = pa_place<false>(a, kk, blocks);
+  const int hk = p.hk, b = p.b, held = p.held, k0 = p.k0, k1 = p.k1, slot = p.slot;
+  const int r0 = p.block * PS_ROWS;
   if (k0 >= k1) {
-    for (int r = r0 + tid; r < min(rows, r0 + PS_ROWS); r += PS_THREADS)
-      a.ml[(size_t)slot * a.rows() + pa_index(a, pa_row(a, kk.own, b, hk, r))] =
-          make_float2(-INFINITY, 0.f);
+    if (kk.behind) pdl_wait();
+    no_keys<PS_THREADS>(a, kk, p, r0, PS_ROWS, rows, tid);
     return;
   }
-  const unsigned char* kp = static_cast<const unsigned char*>(kk.k) +
-                            4 * ((int64_t)b * kk.k_s[0] + (int64_t)hk * kk.k_s[2]);
-  const unsigned char* vp = static_cast<const unsigned char*>(kk.v) +
-                            4 * ((int64_t)b * kk.v_s[0] + (int64_t)hk * kk.v_s[2]);
+  const PaSource from = pa_source(a, kk, p, 4);
   const int pieces = a.d / 4, tiles = (k1 - k0 + PS_KT - 1) / PS_KT;
   float* sq = reinterpret_cast<float*>(sm + PS_STAGES * STAGE);          // [16][DP]
   auto stage = [&](int t) {
-    unsigned char* s = sm + (t % PS_STAGES) * STAGE;
-    if (t < tiles) {
-      stage_rows<PS_KT, DP / 4, PS_THREADS>(s, kp, kk.k_s[1] * 4, LD, k0 + t * PS_KT, k1, pieces, tid);
-      stage_rows<PS_KT, DP / 4, PS_THREADS>(s + PS_KT * LD, vp, kk.v_s[1] * 4, LD, k0 + t * PS_KT, k1,
+    if (t < tiles)
+      stage_tile<PS_KT, DP / 4, PS_THREADS>(sm + (t % PS_STAGES) * STAGE, from, p, LD, k0 + t * PS_KT,
                                             pieces, tid);
-    }
     copy_commit();
   };
   for (int i = tid; i < PS_ROWS * (DP / 4); i += PS_THREADS) {
-    const int r = r0 + i / (DP / 4), p = i % (DP / 4);
-    const bool live = r < rows && p < pieces;
+    const int r = r0 + i / (DP / 4), c = i % (DP / 4);
+    const bool live = r < rows && c < pieces;
     const float* src = static_cast<const float*>(a.q);
     if (live) {
       const PaRow w = pa_row(a, kk.own, b, hk, r);
-      src += (int64_t)w.n * a.q_s[0] + (int64_t)w.t * a.q_s[1] + (int64_t)w.h * a.q_s[2] + p * 4;
+      src += (int64_t)w.n * a.q_s[0] + (int64_t)w.t * a.q_s[1] + (int64_t)w.h * a.q_s[2] + c * 4;
     }
     copy16(sq + i * 4, src, live);
   }
@@ -777,11 +763,11 @@ pa_simt_kernel(const PaArgs a, const PaKeys kk, int rows, int blocks) {
     const int key = k0 + t * PS_KT + lane;
     float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
-    for (int p = 0; p < DP / 4; ++p) {
-      const float4 kv = *reinterpret_cast<const float4*>(sk + lane * LD + p * 16);
+    for (int c = 0; c < DP / 4; ++c) {
+      const float4 kv = *reinterpret_cast<const float4*>(sk + lane * LD + c * 16);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        s[i] = dot4(*reinterpret_cast<const float4*>(sq + (warp * 4 + i) * DP + p * 4), kv, s[i]);
+        s[i] = dot4(*reinterpret_cast<const float4*>(sq + (warp * 4 + i) * DP + c * 4), kv, s[i]);
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -799,14 +785,15 @@ pa_simt_kernel(const PaArgs a, const PaKeys kk, int rows, int blocks) {
       const float4 v = *reinterpret_cast<const float4*>(sv + j * LD + (lane % (DP / 4)) * 16);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float p = __shfl_sync(0xffffffffu, s[i], j);
-        o[i].x = fmaf(p, v.x, o[i].x);
-        o[i].y = fmaf(p, v.y, o[i].y);
-        o[i].z = fmaf(p, v.z, o[i].z);
-        o[i].w = fmaf(p, v.w, o[i].w);
+        const float x = __shfl_sync(0xffffffffu, s[i], j);
+        o[i].x = fmaf(x, v.x, o[i].x);
+        o[i].y = fmaf(x, v.y, o[i].y);
+        o[i].z = fmaf(x, v.z, o[i].z);
+        o[i].w = fmaf(x, v.w, o[i].w);
       }
     }
   }
+  if (kk.behind) pdl_wait();
   if (rw >= rows) return;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -908,15 +895,20 @@ bool pa_plan(const lilicorr_prefix_attention_desc* d, PaPlan* p) {
   if (rows >= 2147483648.0 || (double)d->groups * d->beams * d->kv_heads >= 2147483648.0) return false;
   const int sms = num_sms();
   const int rep = d->q_heads / d->kv_heads;
-  // pieces of a key range: about four CTAs an SM over all ranges, none below 256 keys
-  auto pieces = [&](long long ranges, int cap) {
-    const long long want = ranges > 0 ? (4ll * sms + ranges - 1) / ranges : 1;
-    const long long most = (cap + 255) / 256;
+  // pieces of a key range, of which a kernel takes `blocks` of rows: a wave of CTAs (three an SM) over all
+  // ranges, none below 256 keys, or 64 in fp32, where a stage of 32 keys takes the CUDA cores as long as
+  // a bf16 tile of 128 (15 sequences of 96-wide heads behind 1,777 keys: 256 keys at least 49 us)
+  const bool f32 = d->dtype == LILICORR_F32;
+  const int least = f32 ? 64 : 256, per_block = f32 ? 16 : 64;
+  auto pieces = [&](long long ranges, long long rows, int cap) {
+    ranges *= (rows + per_block - 1) / per_block;
+    const long long want = ranges > 0 ? (3ll * sms + ranges - 1) / ranges : 1;
+    const long long most = (cap + least - 1) / least;
     long long n = want < most ? want : most;
     return (int)(n < 1 ? 1 : n > 128 ? 128 : n);
   };
   const long long prow = (long long)d->beams * d->tokens * rep;
-  const bool tc_type = d->dtype == LILICORR_BF16, tc = tc_type && d->prefix_capacity;
+  const bool tc = !f32 && d->prefix_capacity;
   const long long blocks = (prow + PA_BLOCK - 1) / PA_BLOCK;
   // (tiles are counted in 32 bits)
   if (tc && (double)d->groups * d->kv_heads * blocks * ((double)d->prefix_capacity / PA_TILE + 1) >=
@@ -924,13 +916,12 @@ bool pa_plan(const lilicorr_prefix_attention_desc* d, PaPlan* p) {
     return false;
   p->seg_ctas = tc ? sms : 0;
   p->seg_blocks = tc ? (int)blocks : 0;
-  p->psplits = d->prefix_capacity
-                   ? pieces((long long)d->groups * d->kv_heads * ((prow + 63) / 64), d->prefix_capacity)
-                   : 0;
-  // own keys: in one piece while that is a wave of CTAs or the keys are few
-  const long long own = (long long)d->groups * d->beams * d->kv_heads * ((d->tokens * (long long)rep + 63) / 64);
+  p->psplits = d->prefix_capacity ? pieces((long long)d->groups * d->kv_heads, prow, d->prefix_capacity) : 0;
+  // own keys: bf16 in one piece while that is a wave of CTAs or the keys are few
+  const long long own = (long long)d->groups * d->beams * d->kv_heads, orow = (long long)d->tokens * rep;
   p->ssplits = !d->own_capacity ? 0
-               : tc_type && (own >= sms || d->own_capacity <= 512) ? 1 : pieces(own, d->own_capacity);
+               : !f32 && (own * ((orow + 63) / 64) >= sms || d->own_capacity <= 512)
+                   ? 1 : pieces(own, orow, d->own_capacity);
   p->rows = (size_t)rows;
   const size_t slots = (size_t)p->psplits + p->ssplits;
   const size_t segs = tc ? (size_t)sms + (size_t)d->groups * d->kv_heads * blocks : 0;
@@ -1039,7 +1030,7 @@ lilicorr_status_t lilicorr_prefix_attention(const lilicorr_prefix_attention_desc
   else pre.splits = 0;
   own.slot0 = pre.splits;
   a.slots = own.join ? 0 : pre.splits + own.splits;
-  own.behind = bf && has_p;
+  own.behind = has_p;
   if (tc) LL_TRY(launch_pa_tc(a, pre, maps, stream));
   else if (has_p) LL_TRY(bf ? launch_pa_mma(a, pre, stream) : launch_pa_simt(a, pre, stream));
   if (has_s) LL_TRY(bf ? launch_pa_mma(a, own, stream) : launch_pa_simt(a, own, stream));
