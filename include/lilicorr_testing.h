@@ -69,6 +69,15 @@ lilicorr_status_t lilicorr_test_lm_head_timeout(const void* hidden, const void* 
                                                 long long wait_cycles, int second_only,
                                                 cudaStream_t stream);
 
+/* lilicorr_prefix_attention with the K (which = 1) or V (2) copies of its tensor-core kernel withheld
+ * and a limit as above: the workspace's status word receives LILICORR_ERR_TIMEOUT, the outputs unspecified
+ * values. LILICORR_ERR_SHAPE where that kernel does not take the call (F32, no prefix, or a short one). */
+lilicorr_status_t lilicorr_test_prefix_attention_timeout(
+    const lilicorr_prefix_attention_desc* desc, const void* q, const void* prefix_k,
+    const void* prefix_v, const int32_t* prefix_len, const void* k, const void* v,
+    const int32_t* seq_len, void* out, float* lse, void* ws, size_t ws_bytes, long long wait_cycles,
+    int which, cudaStream_t stream);
+
 /* Switch for the fused scoring-network kernels (bf16 heads with D = 256, 8 heads,
  * FFN 2D, L*K <= 128): mode 1 (the default) takes the cluster kernel (four CTAs per
  * sequence) while every sequence's cluster fits on the GPU and the one-CTA kernel for

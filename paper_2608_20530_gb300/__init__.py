@@ -98,6 +98,7 @@ _SIGS = {
                               [ctypes.c_int64] * 4 + [_P, _P, _P]),
     "lilicorr_prefix_attention_workspace_bytes": (_S, [_P]),
     "lilicorr_prefix_attention": (_I, [_P] * 11 + [_S, _P]),
+    "lilicorr_test_prefix_attention_timeout": (_I, [_P] * 11 + [_S, ctypes.c_longlong, _I, _P]),
     "lilicorr_test_linear": (_I, [_P, _I, _I, _P, _I, _I, _P, _I, _I, _I, _I, _I, _P, _P, _I, _I,
                                   _P, _P]),
     "lilicorr_test_linear_timeout": (_I, [_P, _P, _P, _I, _I, _I, ctypes.c_longlong, _P, _P]),
@@ -782,6 +783,23 @@ def test_lm_head_timeout(hidden: torch.Tensor, w_vocab: torch.Tensor, K: int, ws
                                                ws.ptr, ws.nbytes, int(wait_cycles),
                                                int(second_only), _stream()),
            "test_lm_head_timeout")
+
+
+def test_prefix_attention_timeout(q: torch.Tensor, prefix_k: torch.Tensor, prefix_v: torch.Tensor,
+                                  k: torch.Tensor, v: torch.Tensor, prefix_len: torch.Tensor,
+                                  seq_len: torch.Tensor, ws: Workspace, wait_cycles: int,
+                                  which: int) -> None:
+    """Test hook: prefix_attention of dense tensors with the K (``which`` 1) or V (2) copies of its
+    tensor-core kernel withheld, so that its bounded waits run out and ``ws`` holds the timeout status."""
+    N, T, Hq, d = q.shape
+    G, P, Hkv, _ = prefix_k.shape
+    out, lse = torch.empty_like(q), torch.empty((N, T, Hq), dtype=torch.float32, device=q.device)
+    strides = [s for t in (q, out, prefix_k, prefix_v, k, v) for s in t.stride()[:3]]
+    desc = _PA_DESC.pack(G, N // G, T, Hq, Hkv, d, P, k.shape[1], _dtype_code(q), d ** -0.5, *strides)
+    _check(lib().lilicorr_test_prefix_attention_timeout(
+        desc, q.data_ptr(), prefix_k.data_ptr(), prefix_v.data_ptr(), prefix_len.data_ptr(),
+        k.data_ptr(), v.data_ptr(), seq_len.data_ptr(), out.data_ptr(), lse.data_ptr(), ws.ptr, ws.nbytes,
+        int(wait_cycles), int(which), _stream()), "test_prefix_attention_timeout")
 
 
 def test_attention_path(mode: int) -> int:

@@ -12,6 +12,8 @@
 // unrounded ones.
 #include "prefix_attention.cuh"
 
+#include "lilicorr_testing.h"
+
 namespace lilicorr {
 
 namespace {
@@ -934,23 +936,12 @@ bool pa_plan(const lilicorr_prefix_attention_desc* d, PaPlan* p) {
   return true;
 }
 
-}  // namespace
-}  // namespace lilicorr
-
-using namespace lilicorr;
-
-extern "C" {
-
-size_t lilicorr_prefix_attention_workspace_bytes(const lilicorr_prefix_attention_desc* desc) {
-  PaPlan p;
-  return pa_plan(desc, &p) ? p.total : 0;
-}
-
-lilicorr_status_t lilicorr_prefix_attention(const lilicorr_prefix_attention_desc* desc, const void* q,
-                                            const void* prefix_k, const void* prefix_v,
-                                            const int32_t* prefix_len, const void* k, const void* v,
-                                            const int32_t* seq_len, void* out, float* lse, void* ws,
-                                            size_t ws_bytes, cudaStream_t stream) {
+lilicorr_status_t run_prefix_attention(const lilicorr_prefix_attention_desc* desc, const void* q,
+                                       const void* prefix_k, const void* prefix_v,
+                                       const int32_t* prefix_len, const void* k, const void* v,
+                                       const int32_t* seq_len, void* out, float* lse, void* ws,
+                                       size_t ws_bytes, cudaStream_t stream, long long wait_limit,
+                                       int starve) {
   if (!desc) return LILICORR_ERR_ARG;
   if (desc->dtype != LILICORR_F32 && desc->dtype != LILICORR_BF16) return LILICORR_ERR_DTYPE;
   PaPlan p;
@@ -993,6 +984,8 @@ lilicorr_status_t lilicorr_prefix_attention(const lilicorr_prefix_attention_desc
   a.seg_ml = reinterpret_cast<float2*>(w + p.seg_ml_off);
   a.seg_po = reinterpret_cast<float*>(w + p.seg_po_off);
   a.status = reinterpret_cast<uint32_t*>(w);
+  a.wait_limit = wait_limit;
+  a.test_starve = starve;
   a.ml = reinterpret_cast<float2*>(w + p.ml_off);
   a.po = reinterpret_cast<float*>(w + p.po_off);
   PaKeys pre, own;
@@ -1014,6 +1007,7 @@ lilicorr_status_t lilicorr_prefix_attention(const lilicorr_prefix_attention_desc
   // no prefix, or one that the own keys' kernel walks through first: one launch
   own.join = bf && own.splits == 1 && (!has_p || front_takes(a, pre));
   a.slots = 0;
+  if (starve && (!has_p || own.join || !bf)) return LILICORR_ERR_SHAPE;
   if (own.join && has_p) {
     own.front = 1;
     own.front_k = pre.k;
@@ -1026,6 +1020,7 @@ lilicorr_status_t lilicorr_prefix_attention(const lilicorr_prefix_attention_desc
   }
   PaMaps maps;
   const bool tc = has_p && bf && pa_tc_maps(a, pre, &maps);
+  if (starve && !tc) return LILICORR_ERR_SHAPE;
   if (!tc) a.seg_ctas = 0;
   else pre.splits = 0;
   own.slot0 = pre.splits;
@@ -1035,6 +1030,37 @@ lilicorr_status_t lilicorr_prefix_attention(const lilicorr_prefix_attention_desc
   else if (has_p) LL_TRY(bf ? launch_pa_mma(a, pre, stream) : launch_pa_simt(a, pre, stream));
   if (has_s) LL_TRY(bf ? launch_pa_mma(a, own, stream) : launch_pa_simt(a, own, stream));
   return own.join ? LILICORR_OK : launch_pa_combine(a, desc->dtype, stream);
+}
+
+}  // namespace
+}  // namespace lilicorr
+
+using namespace lilicorr;
+
+extern "C" {
+
+size_t lilicorr_prefix_attention_workspace_bytes(const lilicorr_prefix_attention_desc* desc) {
+  PaPlan p;
+  return pa_plan(desc, &p) ? p.total : 0;
+}
+
+lilicorr_status_t lilicorr_prefix_attention(const lilicorr_prefix_attention_desc* desc, const void* q,
+                                            const void* prefix_k, const void* prefix_v,
+                                            const int32_t* prefix_len, const void* k, const void* v,
+                                            const int32_t* seq_len, void* out, float* lse, void* ws,
+                                            size_t ws_bytes, cudaStream_t stream) {
+  return run_prefix_attention(desc, q, prefix_k, prefix_v, prefix_len, k, v, seq_len, out, lse, ws,
+                              ws_bytes, stream, PA_WAIT, 0);
+}
+
+lilicorr_status_t lilicorr_test_prefix_attention_timeout(
+    const lilicorr_prefix_attention_desc* desc, const void* q, const void* prefix_k,
+    const void* prefix_v, const int32_t* prefix_len, const void* k, const void* v,
+    const int32_t* seq_len, void* out, float* lse, void* ws, size_t ws_bytes, long long wait_cycles,
+    int which, cudaStream_t stream) {
+  if (wait_cycles < 100000 || wait_cycles > PA_WAIT || which < 1 || which > 2) return LILICORR_ERR_ARG;
+  return run_prefix_attention(desc, q, prefix_k, prefix_v, prefix_len, k, v, seq_len, out, lse, ws,
+                              ws_bytes, stream, wait_cycles, which);
 }
 
 }  // extern "C"

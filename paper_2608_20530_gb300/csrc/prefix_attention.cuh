@@ -49,6 +49,8 @@ struct PaArgs {
   float* seg_po;               // [segments][PA_BLOCK][d]
   uint32_t* seg_start;         // [G + 1] tiles before each group (of one key head and row block)
   uint32_t* status;
+  long long wait_limit;        // SM cycles per bounded wait of the tensor-core kernel
+  int test_starve;             // test hook only: it issues no copies of K (1) or V (2)
   __device__ __host__ size_t rows() const { return (size_t)G * W * T * Hq; }
 };
 
@@ -64,6 +66,8 @@ __host__ __device__ __forceinline__ uint32_t pa_per_cta(uint32_t tiles, int ctas
   const uint32_t per = (tiles + ctas - 1) / ctas;
   return per < PA_MIN_TILES ? PA_MIN_TILES : per;
 }
+
+constexpr long long PA_WAIT = 4000000000ll;          // about 2 s
 
 constexpr float PA_LOG2E = 1.4426950408889634f;
 

@@ -27,7 +27,6 @@ using namespace tc;
 constexpr int PT_THREADS = 352;
 constexpr int PT_SOFT = 256;                         // of them in the streams
 constexpr uint32_t PT_CHUNK = 128 * 128;             // 128 rows of 128 bytes
-constexpr long long PT_WAIT = 4000000000ll;          // SM cycles, about 2 s
 constexpr uint32_t PT_TMEM = 512;
 
 // ONE: no group has more than 128 rows: one row tile, and the second's space goes to the rings, which
@@ -91,6 +90,20 @@ __device__ __forceinline__ uint64_t add_pairs(uint64_t a, uint64_t b) {
   return d;
 }
 
+// A wait that did not end at once: false after `limit` SM cycles, or when another warp gave up.
+__device__ __noinline__ bool wait_long(uint64_t* bar, uint32_t parity, long long limit,
+                                       volatile int* abort_flag) {
+  const long long t0 = clock64();
+  while (!mbar_try_wait(bar, parity)) {
+    if (*abort_flag) return false;
+    if (clock64() - t0 > limit) {
+      *abort_flag = 1;
+      return false;
+    }
+  }
+  return true;
+}
+
 // Where a CTA is in the list of tiles.
 struct Cursor {
   int g;                       // group
@@ -133,7 +146,7 @@ pa_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
   uint8_t* sV = sK + NK * Cfg::TILE;
   uint32_t* s_sum = reinterpret_cast<uint32_t*>(sQ);             // before the first Q
   __shared__ __align__(8) uint64_t k_full[NK], k_empty[NK], v_full[NV], v_empty[NV];
-  __shared__ __align__(8) uint64_t s_ready[2], p_ready[2], o_ready[2];
+  __shared__ __align__(8) uint64_t s_ready[2], p_ready[2], o_ready[2], drain;
   __shared__ uint32_t tmem_base;
   __shared__ volatile int abort_flag;
   __shared__ Cursor s_cur;
@@ -147,6 +160,7 @@ pa_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       mbar_init(&p_ready[i], 4);
       mbar_init(&o_ready[i], 1);
     }
+    mbar_init(&drain, 1);
     abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -190,16 +204,12 @@ pa_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
   Cursor cur = s_cur;
   const uint32_t tmem = tmem_base;
   auto wait = [&](uint64_t* bar, uint32_t parity) {
-    if (mbar_try_wait(bar, parity)) return true;
-    const long long t0 = clock64();
-    while (!mbar_try_wait(bar, parity)) {
-      if (abort_flag) return false;
-      if (clock64() - t0 > PT_WAIT) {
-        abort_flag = 1;
-        return false;
-      }
-    }
-    return true;
+    return mbar_try_wait(bar, parity) || wait_long(bar, parity, a.wait_limit, &abort_flag);
+  };
+  // the same for a whole warp: all lanes go on, or none
+  auto wait_all = [&](uint64_t* bar, uint32_t parity) {
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+    return __all_sync(0xffffffffu, wait_long(bar, parity, a.wait_limit, &abort_flag)) != 0;
   };
 
   if (warp == 8 || warp == 10) {
@@ -216,7 +226,8 @@ pa_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       const uint32_t slots = is_k ? NK : NV;
       uint32_t slot = 0, parity = 1, issued = 0;
       bool ok = true;
-      while (cur.left && ok) {
+      const bool starve = a.test_starve == (is_k ? 1 : 2);
+      while (cur.left && ok && !starve) {
         const uint32_t here = pt_here(kk, cur);
         const int hk = (int)(cur.item / a.seg_blocks);
         for (uint32_t t = 0; t < here; ++t) {
@@ -232,7 +243,7 @@ pa_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       }
       if (!ok)                                       // given up: the copies under way land before the
         for (uint32_t x = issued > slots ? issued - slots : 0; x < issued; ++x)      // CTA's memory goes
-          mbar_wait(&full[x % slots], (x / slots) & 1u, PT_WAIT);
+          mbar_wait(&full[x % slots], (x / slots) & 1u, a.wait_limit);
     }
     __syncwarp();
   } else if (warp == 9) {
@@ -255,7 +266,7 @@ pa_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       // S of stream s from the K tile in the ring's next slot; last: the slot's last use
       auto scores = [&](int s, bool first, bool last) {
         if (first) {
-          if (!wait(&k_full[ki], kp)) { ok = false; return; }
+          if (!wait_all(&k_full[ki], kp)) { ok = false; return; }
           tc_fence_after();
         }
         const uint64_t qd = q_desc + (two ? s : 0) * (Cfg::TILE >> 4), kd = k_desc + ki * (Cfg::TILE >> 4);
@@ -274,9 +285,9 @@ pa_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       };
       // O += P V of stream s and the key tile `keys` long in the V ring's next slot
       auto sums = [&](int s, int keys, bool fresh, bool first, bool last, bool done) {
-        if (!wait(&p_ready[s], pp[s])) { ok = false; return; }
+        if (!wait_all(&p_ready[s], pp[s])) { ok = false; return; }
         pp[s] ^= 1u;
-        if (first && !wait(&v_full[vi], vp)) { ok = false; return; }
+        if (first && !wait_all(&v_full[vi], vp)) { ok = false; return; }
         tc_fence_after();
         const uint64_t vd = v_desc + vi * (Cfg::TILE >> 4);
         if (leader) {
@@ -317,6 +328,11 @@ pa_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       }
       named_bar(2, PT_SOFT + 32);                    // the segment is done with
       pt_next(a, kk, cur, here);
+    }
+    if (abort_flag) {                                // products under way, before their memory goes
+      if (leader) mma_commit(&drain);
+      mbar_wait(&drain, 0, a.wait_limit);
+      __syncwarp();
     }
   } else if (warp < 8) {
     // ---- the streams: a thread a row
@@ -362,7 +378,7 @@ pa_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       bool ok = true;
       const uint32_t first = two ? 0 : (uint32_t)s, step = two ? 1 : 2;
       for (uint32_t t = first; t < here; t += step) {
-        if (!wait(&s_ready[s], sn & 1u)) { ok = false; break; }
+        if (!wait_all(&s_ready[s], sn & 1u)) { ok = false; break; }
         ++sn;
         if (idle) {                                  // (what P holds for its rows reaches no other row)
           if (lane == 0) mbar_arrive(&p_ready[s]);
@@ -407,7 +423,7 @@ pa_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         if (keys < PA_TILE) {
           // V behind the last key: zeros, whatever the cache holds there (to the product's 16)
           const uint32_t i = i0 + t;
-          if (!wait(&v_full[i % NV], (i / NV) & 1u)) { ok = false; break; }
+          if (!wait_all(&v_full[i % NV], (i / NV) & 1u)) { ok = false; break; }
           uint8_t* v = sV + (i % NV) * Cfg::TILE;
           const int up = (keys + 15) / 16 * 16;
           for (int z = row; z < (up - keys) * (DP / 8); z += warps * 32) {
@@ -468,7 +484,7 @@ pa_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         if (lane == 0) mbar_arrive(&p_ready[s]);
       }
       if (ok && first < here) {
-        if (!wait(&o_ready[s], on & 1u)) ok = false;
+        if (!wait_all(&o_ready[s], on & 1u)) ok = false;
         ++on;
         tc_fence_after();
       }

@@ -168,6 +168,20 @@ def test_beam_select_done_absent_and_banned(dtype, R, W, V, n, banned):
     assert ws.status() == 0
 
 
+def test_beam_select_one_workspace_for_calls_of_many_shapes():
+    """Calls of different shapes, sharing one workspace in turn, each find it usable."""
+    ll = _ll()
+    shapes = [(1, 4, 151936, 8, "bf16"), (40, 3, 900, 5, "f32"), (6, 8, 40001, 16, "f32"),
+              (2, 2, 5000, 4, "bf16"), (300, 2, 64, 4, "bf16")]
+    ws = ll.Workspace(max(ll.beam_select_workspace_bytes(*s[:4]) for s in shapes))
+    for turn in range(2):
+        for i, (R, W, V, n, dtype) in enumerate(shapes):
+            x, scores, _ = _select_inputs(R, W, V, dtype, 100 * turn + i)
+            want = _want_select(x, scores, n, None, -1)
+            _check_select(_run_select(ll, x, scores, n, dtype, ws=ws), want, scores, None, -1)
+    assert ws.status() == 0
+
+
 def test_beam_select_no_beam_at_all():
     ll = _ll()
     x = np.full((2, 3, 100), np.nan, np.float32)

@@ -102,6 +102,8 @@ SHAPES = [
     (3, 5, 2, 8, 4, 96, 177, 33), (1, 1, 16, 8, 1, 128, 300, 40), (2, 4, 16, 4, 2, 64, 129, 17),
     (1, 33, 1, 8, 2, 80, 1000, 7), (2, 7, 5, 6, 2, 32, 511, 70), (1, 130, 1, 4, 2, 128, 700, 65),
     (1, 9, 3, 10, 1, 48, 1500, 129), (5, 1, 1, 16, 2, 128, 2100, 300), (1, 64, 4, 8, 2, 128, 260, 9),
+    (2, 3, 1, 32, 4, 128, 1500, 600), (3, 2, 4, 8, 1, 64, 513, 530), (2, 60, 2, 16, 4, 96, 777, 40),
+    (1, 2, 1, 4, 1, 128, 5000, 1100), (4, 8, 1, 8, 8, 128, 512, 64), (1, 40, 3, 8, 2, 128, 512, 7),
     (1, 300, 1, 2, 2, 64, 640, 5), (1, 129, 1, 1, 1, 128, 4000, 1), (2, 40, 8, 8, 8, 128, 130, 130),
 ]
 
@@ -243,6 +245,20 @@ def test_two_streams_at_once():
     torch.cuda.synchronize()
     for o, x in zip(outs, xs):
         _check(o, x, "bf16")
+
+
+@pytest.mark.parametrize("which", [1, 2])
+@pytest.mark.parametrize("W", [3, 70])
+def test_bounded_waits_run_out(which, W):
+    """The tensor-core kernel without its K or its V copies: it records the timeout, and the context and
+    the workspace are as good as before."""
+    ll = _ll()
+    x = _inputs(2, W, 1, 8, 2, 64, 700, 8, "bf16", 3, [700, 530], [4] * (2 * W))
+    ws = ll.Workspace(ll.prefix_attention_workspace_bytes(x[0], x[1], x[3]))
+    ll.test_prefix_attention_timeout(*x, ws, 2_000_000, which)
+    assert ws.status() == 6
+    _check(ll.prefix_attention(*x, ws=ws), x, "bf16")
+    assert ws.status() == 0
 
 
 def test_python_refusals():
