@@ -339,7 +339,7 @@ lilicorr_status_t lilicorr_select_block_walk(const lilicorr_head* head, int B, c
 
 /* From logits [R, W, V] (F32 or BF16), one pass over the rows of live beams:
  * logp(v | w) = logits[w, v] - log sum_u exp(logits[w, u]), in a beam equal logits by lower id.
- * n <= W * V, R * W <= 65535. ws: zero-filled once, at least
+ * n <= W * V, R * W <= 65535, logits and ws 16-byte aligned. ws: zero-filled once, at least
  * lilicorr_beam_select_workspace_bytes(R, W, V, n) bytes (0: unsupported shape); its first word is
  * the device status. */
 size_t lilicorr_beam_select_workspace_bytes(int requests, int beams, int V, int n);
@@ -364,7 +364,8 @@ lilicorr_status_t lilicorr_beam_merge(const int32_t* ids, const float* logp, int
  * request r and position p < lengths[r],
  *   state[r, w, p, h, :] = (state before the call)[r, parents[r, w], p, h, :].
  * An array is [requests, beams, positions, heads] rows of row_bytes contiguous bytes, the strides in
- * bytes and the same for all arrays (which must not overlap one another, nor an array itself).
+ * bytes and the same for all arrays, in any order but nested: each is at least what the smaller ones
+ * span. Arrays that share a byte, or an array that overlaps itself, are refused.
  *   parents [R, W] int32 device; a value outside [0, W) leaves that beam as it is
  *   lengths [R] int32 device, at most `positions` of them are moved; NULL: all positions
  * No alignment is asked for; rows and strides that are multiples of 16 bytes are fastest. positions *
@@ -391,8 +392,9 @@ lilicorr_status_t lilicorr_beam_reorder(void* const* host_states, int n_states, 
  *   head_dim]; k, v [N, own_capacity, kv_heads, head_dim], all of dtype, each with its strides in
  *   elements (the last dimension is dense), 16-byte aligned, strides multiples of 16 bytes and not
  *   negative; lse [N, T, q_heads] fp32; prefix_len [groups], seq_len [N] int32 on the device
- * head_dim a multiple of 8 up to 128, q_heads a multiple of kv_heads, capacities from 0 (then the
- * pointers of that side may be NULL) to 2^30. F32 runs in fp32 throughout; BF16 takes bf16 products
+ * head_dim a multiple of 8 up to 128, q_heads a multiple of kv_heads, 0 < scale < inf, capacities from
+ * 0 (then the pointers of that side may be NULL) to 2^30. Caches may overlap themselves (a stride of 0:
+ * one prefix for all groups), out may not, nor may out and lse overlap an input. F32 runs in fp32 throughout; BF16 takes bf16 products
  * with fp32 accumulation, softmax and sums in fp32. ws: zero-filled once, at least
  * lilicorr_prefix_attention_workspace_bytes(desc) bytes (0: unsupported); its first word is the
  * device status. */

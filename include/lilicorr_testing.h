@@ -78,6 +78,11 @@ lilicorr_status_t lilicorr_test_prefix_attention_timeout(
     const int32_t* seq_len, void* out, float* lse, void* ws, size_t ws_bytes, long long wait_cycles,
     int which, cudaStream_t stream);
 
+/* Whether lilicorr_beam_reorder refuses these arrays (their addresses are not read): strides and extents
+ * are those of [requests, beams, positions, heads] rows of row_bytes. */
+int lilicorr_test_states_overlap(void* const* host_states, int n_states, const int64_t* strides,
+                                 const int64_t* extents, size_t row_bytes);
+
 /* Switch for the fused scoring-network kernels (bf16 heads with D = 256, 8 heads,
  * FFN 2D, L*K <= 128): mode 1 (the default) takes the cluster kernel (four CTAs per
  * sequence) while every sequence's cluster fits on the GPU and the one-CTA kernel for

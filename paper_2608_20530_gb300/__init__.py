@@ -534,6 +534,12 @@ def _refuse(t: torch.Tensor, name: str, dev: int, dtype: Optional[torch.dtype], 
     raise ValueError(f"{name} must be contiguous")
 
 
+def _fits(*values: int) -> None:
+    """The library takes 32-bit sizes and ids; nothing is cut to them."""
+    if max(values) > 0x7FFFFFFF or min(values) < -0x80000000:
+        raise ValueError("sizes, n and ids must fit 32 bits")
+
+
 def _beam_outputs(scores: torch.Tensor, done: Optional[torch.Tensor], dev: int, shape, R: int, n: int):
     """Checks of the beams' scores and done flags (the same for both calls), and the outputs."""
     if (scores.get_device() != dev or scores.dtype is not torch.float32 or scores.shape != shape or
@@ -544,7 +550,7 @@ def _beam_outputs(scores: torch.Tensor, done: Optional[torch.Tensor], dev: int, 
             raise ValueError("done must be bool or uint8")
         if done.get_device() != dev or done.shape != shape or not done.is_contiguous():
             _refuse(done, "done", dev, None, shape)
-    size, on = (R, n if n > 0 else 0), scores.device
+    size, on = (R, n if 0 < n <= MAX_K else 0), scores.device    # another n is refused by the call
     empty = torch.empty
     return (empty(size, dtype=torch.int32, device=on), empty(size, dtype=torch.int32, device=on),
             empty(size, dtype=torch.float32, device=on), empty(size, dtype=torch.bool, device=on))
@@ -569,9 +575,12 @@ def beam_select(logits: torch.Tensor, scores: torch.Tensor, n: int,
     if logits.get_device() != dev or not logits.is_contiguous():
         _refuse(logits, "logits", dev, None, None)
     R, W, V = shape
+    _fits(R, W, V, n, end_id)
     tokens, parents, best, over = out = _beam_outputs(scores, done, dev, shape[:2], R, n)
     if ws is None:
         ws = Workspace(beam_select_workspace_bytes(R, W, V, n), logits.device)
+    elif ws.buf.get_device() != dev:
+        _here(ws.buf, "ws", dev)
     status = lib().lilicorr_beam_select(
         logits.data_ptr(), _dtype_code(logits), R, W, V, n, scores.data_ptr(),
         None if done is None else done.data_ptr(), end_id, tokens.data_ptr(), parents.data_ptr(),
@@ -591,6 +600,7 @@ def beam_merge(ids: torch.Tensor, logp: torch.Tensor, scores: torch.Tensor, n: i
         raise ValueError("ids must be [requests, beams, K]")
     dev = torch.cuda.current_device()
     R, W, K = shape
+    _fits(R, W, K, n, end_id)
     if ids.get_device() != dev or ids.dtype is not torch.int32 or not ids.is_contiguous():
         _refuse(ids, "ids", dev, torch.int32, None)
     if (logp.get_device() != dev or logp.dtype is not torch.float32 or logp.shape != shape or
@@ -630,7 +640,8 @@ def beam_reorder(states, parents: torch.Tensor, lengths: Optional[torch.Tensor] 
     [R, W, positions, ...] of ``states`` (one or a sequence, e.g. the layers' key and value caches)
     state[r, w, :lengths[r]] = state[r, parents[r, w], :lengths[r]] as it was before the call.
     parents [R, W] int32 (outside [0, W): the beam stays), lengths [R] int32 (None: all). Tensors may
-    be strided views ([R, W, positions, heads, d] of any layout with dense d). Returns ``states``."""
+    be strided views ([R, W, positions, heads, d] of any layout with dense d) that share no memory with
+    one another or with themselves. Returns ``states``."""
     tensors = [states] if isinstance(states, torch.Tensor) else list(states)
     if parents.dim() != 2:
         raise ValueError("parents must be [requests, beams]")
@@ -641,15 +652,20 @@ def beam_reorder(states, parents: torch.Tensor, lengths: Optional[torch.Tensor] 
     if lengths is not None and (lengths.get_device() != dev or lengths.dtype is not torch.int32 or
                                 lengths.shape != (R,) or not lengths.is_contiguous()):
         _refuse(lengths, "lengths", dev, torch.int32, (R,))
-    # arrays of one layout go together
+    # arrays of one layout go together; the call looks for overlaps among them
     groups: Dict[tuple, list] = {}
     for i, t in enumerate(tensors):
         if t.get_device() != dev:
             _here(t, f"states[{i}]", dev)
         groups.setdefault((t.shape, t.stride(), t.dtype), []).append(t)
+    if len(groups) > 1:
+        starts = [t.data_ptr() for t in tensors if t.numel()]
+        if len(set(starts)) < len(starts):
+            raise ValueError("states must not overlap")
     for same in groups.values():
         i = next(i for i, t in enumerate(tensors) if t is same[0])
         positions, heads, row, *strides = _state_layout(same[0], R, W, f"states[{i}]")
+        _fits(R, W, positions, heads)
         code = lib().lilicorr_beam_reorder(
             (_P * len(same))(*[t.data_ptr() for t in same]), len(same), R, W, positions, heads, row,
             *strides, parents.data_ptr(), None if lengths is None else lengths.data_ptr(), _stream())
@@ -715,6 +731,8 @@ def prefix_attention(q: torch.Tensor, prefix_k: torch.Tensor, prefix_v: torch.Te
                          max(d, 1) ** -0.5 if scale is None else scale, *strides)
     if ws is None:
         ws = Workspace(int(lib().lilicorr_prefix_attention_workspace_bytes(desc)), q.device)
+    elif ws.buf.get_device() != dev:
+        _here(ws.buf, "ws", dev)
     status = lib().lilicorr_prefix_attention(
         desc, q.data_ptr(), prefix_k.data_ptr(), prefix_v.data_ptr(), prefix_len.data_ptr(),
         k.data_ptr(), v.data_ptr(), seq_len.data_ptr(), out.data_ptr(), lse.data_ptr(),

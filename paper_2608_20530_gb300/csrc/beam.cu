@@ -959,6 +959,18 @@ lilicorr_status_t run_select(const T* logits, lilicorr_dtype_t dt, int requests,
                   maxima, sums, out, reinterpret_cast<uint32_t*>(w));
 }
 
+// A column of the beams is moved by one thread: rows that share bytes would race.
+bool states_overlap(void* const* states, int n, const int64_t* strides, const int64_t* extents,
+                    int64_t row_bytes) {
+  const StrideNest nest(strides, extents, 4, row_bytes);
+  if (!nest.nests()) return true;
+  for (int i = 1; i < n; ++i)
+    for (int j = 0; j < i; ++j)
+      if (nest.meets((__int128)reinterpret_cast<intptr_t>(states[i]) - reinterpret_cast<intptr_t>(states[j])))
+        return true;
+  return false;
+}
+
 bool beam_shape_ok(int requests, int beams, int n) {
   return requests >= 0 && beams >= 1 && beams <= LILICORR_MAX_BEAMS && n >= 1 && n <= LILICORR_MAX_K;
 }
@@ -1030,6 +1042,8 @@ lilicorr_status_t lilicorr_beam_reorder(void* const* host_states, int n_states, 
   if (!host_states || !parents) return LILICORR_ERR_ARG;
   if (row_bytes > (1ull << 31) || (double)positions * heads * (double)row_bytes >= 16.0 * 2147483648.0)
     return LILICORR_ERR_SHAPE;
+  for (int i = 0; i < n_states; ++i)
+    if (!host_states[i]) return LILICORR_ERR_ARG;
   // heads that follow one another are one longer row
   if (heads > 1 && stride_head == (int64_t)row_bytes) {
     row_bytes *= heads;
@@ -1040,13 +1054,13 @@ lilicorr_status_t lilicorr_beam_reorder(void* const* host_states, int n_states, 
                   (beams > 1 ? (uint64_t)stride_beam : 0) |
                   (positions > 1 ? (uint64_t)stride_position : 0) |
                   (heads > 1 ? (uint64_t)stride_head : 0);
-  for (int i = 0; i < n_states; ++i) {
-    if (!host_states[i]) return LILICORR_ERR_ARG;
-    bits |= reinterpret_cast<uintptr_t>(host_states[i]);
-  }
+  for (int i = 0; i < n_states; ++i) bits |= reinterpret_cast<uintptr_t>(host_states[i]);
   int vec = beams <= 16 ? 16 : beams <= 32 ? 8 : 4;
   while (bits & (uint64_t)(vec - 1)) vec >>= 1;
   if ((double)positions * heads * (double)(row_bytes / vec) >= 2147483648.0) return LILICORR_ERR_SHAPE;
+  const int64_t strides[4] = {stride_request, stride_beam, stride_position, stride_head};
+  const int64_t extents[4] = {requests, beams, positions, heads};
+  if (states_overlap(host_states, n_states, strides, extents, (int64_t)row_bytes)) return LILICORR_ERR_ARG;
   Reorder a;
   a.W = beams;
   a.positions = positions;
@@ -1071,6 +1085,11 @@ lilicorr_status_t lilicorr_beam_reorder(void* const* host_states, int n_states, 
     }
   }
   return LILICORR_OK;
+}
+
+int lilicorr_test_states_overlap(void* const* host_states, int n_states, const int64_t* strides,
+                                 const int64_t* extents, size_t row_bytes) {
+  return states_overlap(host_states, n_states, strides, extents, (int64_t)row_bytes);
 }
 
 }  // extern "C"

@@ -125,6 +125,41 @@ lilicorr_status_t allow_max_dynamic_smem(F* func, bool (&done)[64]) {
   return LILICORR_OK;
 }
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+// Rows of `row` contiguous units at sums of i_d * stride_d, 0 <= i_d < extent_d, of up to four
+// dimensions, larger strides first. The layouts of dense arrays and of their slices, in any order of
+// dimensions, nest: each stride is at least what the smaller ones span, so no two rows overlap.
+struct StrideNest {
+  int n = 0;
+  __int128 stride[4], extent[4], rest[5];            // rest[d]: units that dimensions d.. and a row span
+  StrideNest(const int64_t* strides, const int64_t* extents, int dims, int64_t row) {
+    for (int d = 0; d < dims; ++d) {
+      if (extents[d] <= 1) continue;
+      const __int128 s = strides[d] < 0 ? -(__int128)strides[d] : (__int128)strides[d];
+      int at = n++;
+      for (; at > 0 && stride[at - 1] < s; --at) { stride[at] = stride[at - 1]; extent[at] = extent[at - 1]; }
+      stride[at] = s;
+      extent[at] = extents[d];
+    }
+    rest[n] = row;
+    for (int d = n - 1; d >= 0; --d) rest[d] = (extent[d] - 1) * stride[d] + rest[d + 1];
+  }
+  bool nests() const {
+    for (int d = 0; d < n; ++d)
+      if (stride[d] < rest[d + 1]) return false;
+    return true;
+  }
+  // Does a second array of this (nested) layout, `delta` units away, share a unit with the first? In each
+  // dimension only two differences of the index leave what the smaller strides can make up.
+  bool meets(__int128 delta, int d = 0) const {
+    if (delta < 0) delta = -delta;                   // differences come in both signs
+    if (delta >= rest[d]) return false;
+    if (d == n) return true;
+    const __int128 k = delta / stride[d];
+    return (k < extent[d] && meets(delta - k * stride[d], d + 1)) ||
+           (k + 1 < extent[d] && meets(delta - (k + 1) * stride[d], d + 1));
+  }
+};
 inline int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
 
 int num_sms();   // of the current device, cached per device

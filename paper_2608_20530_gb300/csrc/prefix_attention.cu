@@ -964,6 +964,8 @@ lilicorr_status_t run_prefix_attention(const lilicorr_prefix_attention_desc* des
                  !stride_ok(desc->prefix_v_stride, pre_e, per16))) ||
       (has_s && (!stride_ok(desc->k_stride, own_e, per16) || !stride_ok(desc->v_stride, own_e, per16))))
     return LILICORR_ERR_ARG;
+  const int64_t out_e[3] = {N, desc->tokens, desc->q_heads};
+  if (!StrideNest(desc->out_stride, out_e, 3, desc->head_dim).nests()) return LILICORR_ERR_ARG;
   if (ws_bytes < p.total) return LILICORR_ERR_WORKSPACE;
 
   unsigned char* w = static_cast<unsigned char*>(ws);

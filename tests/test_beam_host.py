@@ -61,3 +61,55 @@ def test_beam_reorder_refusals(lib):
         assert f(**none) == 0, none
     assert f(states=None) == 1 and f(parents=None) == 1
     assert f(states=(ctypes.c_void_p * 1)(None)) == 1
+
+
+def test_beam_reorder_refuses_arrays_that_overlap(lib):
+    """No byte may belong to two rows: the stride nest and its pairs against the sets of bytes."""
+    import itertools
+    import random
+    rng = random.Random(7)
+
+    def cells(at, extents, strides, row):
+        return [at + sum(i * s for i, s in zip(idx, strides)) + b
+                for idx in itertools.product(*map(range, extents)) for b in range(row)]
+
+    def refused(at, extents, strides, row):
+        return lib.lilicorr_test_states_overlap((ctypes.c_void_p * len(at))(*at), len(at),
+                                                (ctypes.c_int64 * 4)(*strides),
+                                                (ctypes.c_int64 * 4)(*extents), ctypes.c_size_t(row))
+
+    seen = [0, 0]
+    for _ in range(400):
+        row = rng.choice((1, 2, 4))
+        extents = [rng.randint(1, 4) for _ in range(4)]
+        order = list(range(4))
+        rng.shuffle(order)
+        strides, span = [0] * 4, row
+        for d in order:                                        # a slice of a dense array, or nearly
+            strides[d] = (span + rng.choice((0, 0, 1, 3))) * rng.choice((1, 1, 1, -1))
+            span += (extents[d] - 1) * abs(strides[d])
+        one = cells(0, extents, strides, row)
+        assert len(set(one)) == len(one)
+        delta = rng.randint(-span - 2, span + 2)
+        both = one + cells(delta, extents, strides, row)
+        want = int(len(set(both)) < len(both))
+        assert refused([5000, 5000 + delta], extents, strides, row) == want, (extents, strides, delta)
+        assert refused([5000], extents, strides, row) == 0
+        seen[want] += 1
+    assert min(seen) > 50
+    assert refused([4096], (2, 2, 1, 1), (0, 64, 0, 0), 64) == 1    # one array for all requests
+    assert refused([4096], (1, 2, 3, 1), (0, 0, 64, 0), 64) == 1    # beams that share their rows
+    assert refused([4096], (1, 1, 3, 1), (0, 0, 48, 0), 64) == 1
+    assert refused([4096, 8192, 4096], (1, 2, 3, 1), (0, 192, 64, 0), 64) == 1
+
+
+def test_beam_reorder_call_refuses_them(lib):
+    p = ctypes.c_void_p(4096)
+
+    def f(at, strides):
+        return lib.lilicorr_beam_reorder((ctypes.c_void_p * len(at))(*at), len(at), 2, 2, 3, 1, 16,
+                                         *strides, p, None, None)
+    assert f([4096, 4096], (96, 48, 16, 0)) == 1
+    assert f([4096], (0, 48, 16, 0)) == 1
+    assert f([4096], (96, 0, 16, 0)) == 1
+    assert f([4096], (96, 32, 16, 0)) == 1

@@ -478,3 +478,34 @@ def test_beam_calls_in_a_graph_and_on_another_stream():
         torch.cuda.synchronize()
         _check_select(out, _want_select(x, scores, n, None, -1), scores, None, -1)
         assert torch.equal(cache.cpu(), _moved(c0, out[1].cpu(), None))
+
+
+def test_beam_sizes_are_not_cut_to_32_bits():
+    ll = _ll()
+    x, sc = torch.zeros((1, 2, 50), device="cuda"), torch.zeros((1, 2), device="cuda")
+    ids = torch.zeros((1, 2, 4), dtype=torch.int32, device="cuda")
+    for bad in (dict(n=4, end_id=(1 << 32) + 5), dict(n=(1 << 32) + 4), dict(n=4, end_id=-(1 << 40))):
+        with pytest.raises(ValueError):
+            ll.beam_select(x, sc, **bad)
+        with pytest.raises(ValueError):
+            ll.beam_merge(ids, ids.float(), sc, **bad)
+    with pytest.raises(ll.LilicorrError):
+        ll.beam_select(x, sc, 1 << 30)
+
+
+def test_beam_reorder_refuses_states_that_share_memory():
+    ll = _ll()
+    parents = torch.tensor([[1, 0]], dtype=torch.int32, device="cuda")
+    s = torch.arange(48, dtype=torch.float32, device="cuda").reshape(1, 2, 6, 4)
+    keep = s.clone()
+    with pytest.raises(ll.LilicorrError):
+        ll.beam_reorder([s, s], parents)
+    with pytest.raises(ll.LilicorrError):                      # halves of the positions, one in common
+        ll.beam_reorder([s[:, :, :4], s[:, :, 2:]], parents)
+    with pytest.raises(ll.LilicorrError):
+        ll.beam_reorder(s[:, :1].expand(1, 2, 6, 4), parents)
+    with pytest.raises(ValueError):
+        ll.beam_reorder([s, s.view(torch.int32)], parents)
+    assert torch.equal(s, keep)
+    ll.beam_reorder([s[:, :, :2], s[:, :, 4:], s[:, :, 2:4]], parents)
+    assert torch.equal(s, keep.flip(1))

@@ -69,6 +69,16 @@ def test_arguments_are_refused(ll):
     assert need > 256 and _call(ll, x, ws_bytes=need - 1) == 7
 
 
+def test_out_that_overlaps_itself_is_refused(ll):
+    """Every row of ``out`` is written by somebody; caches may be shared, and are read."""
+    for s in ((0, 512, 64), (512, 512, 0), (512, 512, 56), (448, 512, 64)):
+        assert _call(ll, _desc(ll, out_stride=s), ws_bytes=16) == 1, s
+    for s in ((512, 512, 64), (64, 512, 6 * 64), (1024, 8, 64), (520, 0, 64)):
+        assert _call(ll, _desc(ll, out_stride=s), ws_bytes=16) == 7, s
+    assert _call(ll, _desc(ll, prefix_k_stride=(0, 128, 64), prefix_v_stride=(0, 128, 64)),
+                 ws_bytes=16) == 7
+
+
 def test_strides_of_single_entries_do_not_count(ll):
     """A dimension of one has no stride: the refusal that comes next is the workspace's."""
     x = _desc(ll, q_stride=(512, 3, 64), out_stride=(512, -5, 64))
