@@ -78,6 +78,12 @@ lilicorr_status_t lilicorr_test_prefix_attention_timeout(
     const int32_t* seq_len, void* out, float* lse, void* ws, size_t ws_bytes, long long wait_cycles,
     int which, cudaStream_t stream);
 
+/* Switch for a bf16 prefix in lilicorr_prefix_attention: mode 0 (the default) chooses by the sizes among
+ * the tensor-core kernel, the mma.sync kernels and the walk over the own keys; mode 1 takes the first for
+ * every prefix, mode 2 the second. The workspace's size goes with it. Process-wide, like the switches
+ * below; returns the previous mode. */
+int lilicorr_test_prefix_path(int mode);
+
 /* Whether lilicorr_beam_reorder refuses these arrays (their addresses are not read): strides and extents
  * are those of [requests, beams, positions, heads] rows of row_bytes. */
 int lilicorr_test_states_overlap(void* const* host_states, int n_states, const int64_t* strides,

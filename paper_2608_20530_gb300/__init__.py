@@ -81,6 +81,7 @@ _SIGS = {
     "lilicorr_launch_count": (ctypes.c_uint64, []),
     "lilicorr_test_fused_path": (_I, [_P, _I]),
     "lilicorr_test_attention_path": (_I, [_I]),
+    "lilicorr_test_prefix_path": (_I, [_I]),
     "lilicorr_topk_lse_noalloc_max_bytes": (_S, []),
     "lilicorr_topk_partial_bytes": (_S, [_I]),
     "lilicorr_lm_head_topk_workspace_bytes": (_S, [_I, _I, _I, _I]),
@@ -534,9 +535,10 @@ def _refuse(t: torch.Tensor, name: str, dev: int, dtype: Optional[torch.dtype], 
     raise ValueError(f"{name} must be contiguous")
 
 
-def _fits(*values: int) -> None:
-    """The library takes 32-bit sizes and ids; nothing is cut to them."""
-    if max(values) > 0x7FFFFFFF or min(values) < -0x80000000:
+def _fits(bits: int) -> None:
+    """The library takes 32-bit sizes and ids; nothing is cut to them. ``bits``: all of them or-ed (a
+    negative one hides the others, and is refused by the call for itself)."""
+    if bits >> 31 not in (0, -1):
         raise ValueError("sizes, n and ids must fit 32 bits")
 
 
@@ -575,7 +577,7 @@ def beam_select(logits: torch.Tensor, scores: torch.Tensor, n: int,
     if logits.get_device() != dev or not logits.is_contiguous():
         _refuse(logits, "logits", dev, None, None)
     R, W, V = shape
-    _fits(R, W, V, n, end_id)
+    _fits(R | W | V | n | end_id + 1)
     tokens, parents, best, over = out = _beam_outputs(scores, done, dev, shape[:2], R, n)
     if ws is None:
         ws = Workspace(beam_select_workspace_bytes(R, W, V, n), logits.device)
@@ -600,7 +602,7 @@ def beam_merge(ids: torch.Tensor, logp: torch.Tensor, scores: torch.Tensor, n: i
         raise ValueError("ids must be [requests, beams, K]")
     dev = torch.cuda.current_device()
     R, W, K = shape
-    _fits(R, W, K, n, end_id)
+    _fits(R | W | K | n | end_id + 1)
     if ids.get_device() != dev or ids.dtype is not torch.int32 or not ids.is_contiguous():
         _refuse(ids, "ids", dev, torch.int32, None)
     if (logp.get_device() != dev or logp.dtype is not torch.float32 or logp.shape != shape or
@@ -665,7 +667,7 @@ def beam_reorder(states, parents: torch.Tensor, lengths: Optional[torch.Tensor] 
     for same in groups.values():
         i = next(i for i, t in enumerate(tensors) if t is same[0])
         positions, heads, row, *strides = _state_layout(same[0], R, W, f"states[{i}]")
-        _fits(R, W, positions, heads)
+        _fits(R | W | positions | heads)
         code = lib().lilicorr_beam_reorder(
             (_P * len(same))(*[t.data_ptr() for t in same]), len(same), R, W, positions, heads, row,
             *strides, parents.data_ptr(), None if lengths is None else lengths.data_ptr(), _stream())
@@ -808,16 +810,30 @@ def test_prefix_attention_timeout(q: torch.Tensor, prefix_k: torch.Tensor, prefi
                                   seq_len: torch.Tensor, ws: Workspace, wait_cycles: int,
                                   which: int) -> None:
     """Test hook: prefix_attention of dense tensors with the K (``which`` 1) or V (2) copies of its
-    tensor-core kernel withheld, so that its bounded waits run out and ``ws`` holds the timeout status."""
+    tensor-core kernel withheld, so that its bounded waits run out and ``ws`` (made as large as that kernel
+    wants it, where another would take the call) holds the timeout status."""
     N, T, Hq, d = q.shape
     G, P, Hkv, _ = prefix_k.shape
     out, lse = torch.empty_like(q), torch.empty((N, T, Hq), dtype=torch.float32, device=q.device)
     strides = [s for t in (q, out, prefix_k, prefix_v, k, v) for s in t.stride()[:3]]
     desc = _PA_DESC.pack(G, N // G, T, Hq, Hkv, d, P, k.shape[1], _dtype_code(q), d ** -0.5, *strides)
-    _check(lib().lilicorr_test_prefix_attention_timeout(
-        desc, q.data_ptr(), prefix_k.data_ptr(), prefix_v.data_ptr(), prefix_len.data_ptr(),
-        k.data_ptr(), v.data_ptr(), seq_len.data_ptr(), out.data_ptr(), lse.data_ptr(), ws.ptr, ws.nbytes,
-        int(wait_cycles), int(which), _stream()), "test_prefix_attention_timeout")
+    path = test_prefix_path(1)
+    try:
+        need = int(lib().lilicorr_prefix_attention_workspace_bytes(desc))
+        if ws.nbytes < need:
+            ws.__init__(need, q.device)
+        _check(lib().lilicorr_test_prefix_attention_timeout(
+            desc, q.data_ptr(), prefix_k.data_ptr(), prefix_v.data_ptr(), prefix_len.data_ptr(),
+            k.data_ptr(), v.data_ptr(), seq_len.data_ptr(), out.data_ptr(), lse.data_ptr(), ws.ptr, ws.nbytes,
+            int(wait_cycles), int(which), _stream()), "test_prefix_attention_timeout")
+    finally:
+        test_prefix_path(path)
+
+
+def test_prefix_path(mode: int) -> int:
+    """Test hook: how prefix_attention takes a bf16 prefix (0 by size, 1 the tensor-core kernel, 2 the
+    mma.sync kernels). Returns the previous mode."""
+    return int(lib().lilicorr_test_prefix_path(int(mode)))
 
 
 def test_attention_path(mode: int) -> int:

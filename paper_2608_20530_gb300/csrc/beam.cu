@@ -324,10 +324,11 @@ beam_merge_kernel(const int32_t* __restrict__ ids, const float* __restrict__ log
 }
 
 // ---------------------------------------------------------------------------- from logits
-constexpr int BS_THREADS = 256;                // of the streaming kernel
-constexpr int BS_U = 8;                        // 16-byte vectors per lane and chunk
-constexpr int BS_STAGES = 3;                   // chunks of a warp in flight or in use
-constexpr int BS_CTAS = 2;                     // CTAs an SM
+// The streaming kernel: vectors of 16 bytes per lane and chunk, chunks of a warp in flight or in use, CTAs an
+// SM. 32 x 8 rows of the call, us: (8, 3, 2) 30.3; (4, 4, 3) 31.7, (4, 6, 2) 32.5, (4, 3, 4) 31.4, (4, 8, 2)
+// 37.1, (8, 2, 3) 30.0: what is in flight matters little, being 100 KB an SM in all of them.
+constexpr int BS_THREADS = 256;
+constexpr int BS_U = 8, BS_STAGES = 3, BS_CTAS = 2;
 constexpr int BC_THREADS = 512;                // of the choosing kernel
 
 // How rows are cut: chunk 0 of a row holds the ids before its first 16-byte boundary where rows need
@@ -869,8 +870,9 @@ struct Reorder {
 // past the caches (nothing is read twice but a parent of several beams, by one thread) and many CTAs,
 // so that the run that a CTA takes of each beam is a few KB at a time: 32 x 8 beams of 4 x 512 x 2 KB,
 // 0.9 GB moved, 6.5 TB/s; 19 CTAs a pair instead of 76 6.1, cached accesses 5.6.
-// DENSE: the positions of a head follow one another, and the grid has the heads: no divisions, which
-// cost a third of the time (238 us).
+// DENSE: the positions of a head follow one another, and the grid has the heads: no divisions. 8 requests
+// of 512 positions x 2 KB x 4 arrays: 32 beams 266 us, with the divisions 376; 16 beams 129 and 137; 4
+// beams 33 and 32.
 template <typename V, int WMAX, bool DENSE>
 __global__ void __launch_bounds__(BR_THREADS)
 beam_reorder_kernel(const __grid_constant__ Reorder a) {
@@ -1049,7 +1051,9 @@ lilicorr_status_t lilicorr_beam_reorder(void* const* host_states, int n_states, 
     row_bytes *= heads;
     heads = 1;
   }
-  // the widest vector that every row starts at and fills, and that W beams leave registers for
+  // the widest vector that every row starts at and fills, and that W beams leave registers for. (8
+  // requests of 512 positions x 2 KB x 4 arrays, 16, 8 and 4 bytes: 4 beams 33, 41 and 50 us, 16 beams 129,
+  // 130 and 305; 32 beams 266 in 8 bytes and 312 in 4)
   uint64_t bits = row_bytes | (requests > 1 ? (uint64_t)stride_request : 0) |
                   (beams > 1 ? (uint64_t)stride_beam : 0) |
                   (positions > 1 ? (uint64_t)stride_position : 0) |

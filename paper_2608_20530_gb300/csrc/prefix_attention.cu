@@ -7,9 +7,9 @@
 // of each piece of the keys, the whole is sum 2^(m_i - M) o_i / sum 2^(m_i - M) l_i, M = max m_i. So
 // the rows of ALL sequences of a group meet the prefix as one product (its keys are read once for
 // all), each sequence's own keys are a second, and one pass joins the pieces. Scores, maxima, sums and
-// o are fp32; on bf16 inputs the probabilities are rounded to bf16 for the second product (half a
-// step 2^-9 of each term, of either sign, below the output's own rounding), their sum is of the
-// unrounded ones.
+// o are fp32; on bf16 inputs the probabilities are rounded to bf16 for the second product, whose operands
+// have one type with V (each term off by at most 2^-8 of itself, of either sign, where the output is
+// rounded to 2^-8 as a whole); their sum is of the unrounded ones.
 #include "prefix_attention.cuh"
 
 #include "lilicorr_testing.h"
@@ -289,8 +289,9 @@ __device__ __forceinline__ void stage_queries(unsigned char* dst, const PaArgs& 
 
 // bf16, up to 8 rows a (group or sequence, key head): the products turned round, keys and columns of V as
 // the 16-row operand and the queries as the 8-wide one, S^T = K Q^T and O^T = V^T P^T, which halves the
-// instructions and the registers of 16-row tiles that are half empty. Four warps, 16 keys of a stage
-// each. Short caches are waits more than work: both stages are asked for before anything is waited for,
+// instructions and the registers of 16-row tiles that are half empty: 4 rows, 512 own keys, 64 ranges
+// 10.4 us, in 16-row tiles 14.4; 512 ranges 33 both (bytes); 2,048 ranges 84 and 101. Four warps, 16 keys
+// of a stage each. Short caches are waits more than work: both stages are asked for before anything is waited for,
 // and three CTAs share an SM. The caller's `behind`: the launch before is of the same call and has waited
 // for everything before it, so that the inputs may be read at once; it is waited for at the end.
 constexpr int PF_THREADS = 128, PF_KT = 64, PF_STAGES = 2;
@@ -458,7 +459,8 @@ pa_few_kernel(const PaArgs a, const PaKeys kk, int rows) {
 }
 
 // bf16: RB of the CTA's warps over 16 query rows each, the others over the keys of a stage, KW keys a warp
-// (warp-level products; the pieces of the keys meet in shared memory at the end).
+// (warp-level products; the pieces of the keys meet in shared memory at the end). RB follows the rows: 256
+// ranges of 1,024 keys, 16 rows 29.6 us, in tiles of 32 rows 30.9, of 64 43; 32 rows 33, in tiles of 64 45.
 // JOIN: the own keys in one piece, and the kernel writes the result: there is no prefix, or (`front`) its
 // keys come before the own ones in the kernel's own walk, and there is no other launch.
 template <int DP, int RB>
@@ -869,17 +871,14 @@ lilicorr_status_t launch_pa_combine(const PaArgs& a, lilicorr_dtype_t dt, cudaSt
 // ---------------------------------------------------------------------------- the call
 namespace {
 
+int g_pa_path = 0;             // test hook: 1 the tensor-core kernel for every bf16 prefix, 2 for none
+
 struct PaPlan {
+  bool front, tc;              // how the prefix is taken: by the own keys' kernel, by the tensor-core kernel
   int psplits, ssplits;        // psplits 0: the prefix's pieces are segments
   int seg_ctas, seg_blocks;
   size_t rows, ml_off, po_off, start_off, seg_ml_off, seg_po_off, total;
 };
-
-// A short prefix that few sequences share is read again by each of them, in the walk over their own keys.
-bool front_takes(const PaArgs& a, const PaKeys& pre) {
-  const long long ctas = (long long)a.G * a.W * a.Hkv * ceil_div((long long)a.T * a.rep, 64);
-  return pre.capacity <= 512 && ctas <= 2ll * num_sms();
-}
 
 bool stride_ok(const int64_t (&s)[3], const int (&extent)[3], int per16) {
   for (int i = 0; i < 3; ++i)
@@ -897,36 +896,61 @@ bool pa_plan(const lilicorr_prefix_attention_desc* d, PaPlan* p) {
   if (rows >= 2147483648.0 || (double)d->groups * d->beams * d->kv_heads >= 2147483648.0) return false;
   const int sms = num_sms();
   const int rep = d->q_heads / d->kv_heads;
-  // pieces of a key range, of which a kernel takes `blocks` of rows: a wave of CTAs (three an SM) over all
-  // ranges, none below 256 keys, or 64 in fp32, where a stage of 32 keys takes the CUDA cores as long as
-  // a bf16 tile of 128 (15 sequences of 96-wide heads behind 1,777 keys: 256 keys at least 49 us)
   const bool f32 = d->dtype == LILICORR_F32;
-  const int least = f32 ? 64 : 256, per_block = f32 ? 16 : 64;
+  const long long prow = (long long)d->beams * d->tokens * rep, orow = (long long)d->tokens * rep;
+  const long long pranges = (long long)d->groups * d->kv_heads, oranges = pranges * d->beams;
+  const long long octas = oranges * ((orow + 63) / 64);    // the own keys' CTAs in one piece
+  const bool whole = octas >= sms, half = 2 * octas >= sms;
+
+  // Pieces of a key range, of which a kernel takes per_block rows: one and a half CTAs an SM over all
+  // ranges, no piece below 128 keys. More pieces cost more in the join than they save: 128 ranges of 768
+  // keys, 16 rows, 24.6 us, at three CTAs an SM 28.6; 128 of 4,096 own keys 49 and 61. Pieces of 256 keys
+  // at least: 8 ranges of 768 keys, 64 rows, 15.2 -> 18.5 us; 8 of 8,192 the same.
+  // fp32: three CTAs an SM, 64 keys, which a stage of 32 on the CUDA cores takes as long for as a bf16 tile
+  // of 128: 32 sequences behind 4,096 keys 44 us, at one and a half 52; 15 behind 1,777 keys 24.7, at 256
+  // keys 36.
+  const int least = f32 ? 64 : 128, per_block = f32 ? 16 : 64;
+  const long long wave = f32 ? 3ll * sms : 3ll * sms / 2;
   auto pieces = [&](long long ranges, long long rows, int cap) {
     ranges *= (rows + per_block - 1) / per_block;
-    const long long want = ranges > 0 ? (3ll * sms + ranges - 1) / ranges : 1;
+    const long long want = ranges > 0 ? (wave + ranges - 1) / ranges : 1;
     const long long most = (cap + least - 1) / least;
     long long n = want < most ? want : most;
     return (int)(n < 1 ? 1 : n > 128 ? 128 : n);
   };
-  const long long prow = (long long)d->beams * d->tokens * rep;
-  const bool tc = !f32 && d->prefix_capacity;
+
+  // A short prefix that few sequences share is read again by each of them, in the walk over their own keys,
+  // which then writes the result: one launch for three. Own keys of 64, 32 CTAs: a prefix of 64 keys 6.9 us,
+  // beside it 11; of 512 12.4 and 12.3. 512 CTAs: 64 keys 12.4 and 16, 256 20 and 18, 512 27 and 21; with
+  // four tokens 256 keys 24.7 and 27.5. 4,096 CTAs: 64 keys 50 and 55, 128 63 and 57. CTAs that leave
+  // most SMs idle walk at most 512 keys: 8 CTAs, 384 keys 10.3 and 10.4, 576 12.4 and 11.0.
+  p->front = !f32 && g_pa_path == 0 && d->prefix_capacity && d->own_capacity && d->prefix_capacity <= 512 &&
+             octas * d->prefix_capacity <= 1024ll * sms &&
+             (whole || (long long)d->prefix_capacity + d->own_capacity <= (half ? 768 : 512));
+
+  // The tensor-core kernel pays 6-8 us for its start and its segments' sums, so that small products are
+  // faster on mma.sync, in pieces: 8 ranges, 4 rows, 2,048 keys 18.5 us and 12.4 there; 32 ranges, 32 rows,
+  // 2,048 keys 24.7 and 22; at 4,096 keys 30.9 and 27; 64 rows 36.3 and 37; 128 rows 44.5 and 62; 256 rows
+  // 60 and 106. At d = 64, 32 ranges, 4,096 keys, 64 rows 26.8 and 24; at 8,192 34.4 and 32; 128 rows 31 and 38.
   const long long blocks = (prow + PA_BLOCK - 1) / PA_BLOCK;
-  // (tiles are counted in 32 bits)
-  if (tc && (double)d->groups * d->kv_heads * blocks * ((double)d->prefix_capacity / PA_TILE + 1) >=
-                2147483648.0)
-    return false;
-  p->seg_ctas = tc ? sms : 0;
-  p->seg_blocks = tc ? (int)blocks : 0;
-  p->psplits = d->prefix_capacity ? pieces((long long)d->groups * d->kv_heads, prow, d->prefix_capacity) : 0;
-  // own keys: bf16 in one piece while that is a wave of CTAs or the keys are few
-  const long long own = (long long)d->groups * d->beams * d->kv_heads, orow = (long long)d->tokens * rep;
+  const double tiles = (double)pranges * blocks * ((double)d->prefix_capacity / PA_TILE + 1);
+  const double products = (double)pranges * ((double)d->prefix_capacity / PA_TILE) *
+                          (prow < 16 ? 16 : prow) * (d->head_dim <= 64 ? 64 : 128);
+  p->tc = !f32 && d->prefix_capacity && !p->front &&
+          (g_pa_path ? g_pa_path == 1 : products > 4.0 * 1048576.0);
+  if (p->tc && tiles >= 2147483648.0) return false;      // (they are counted in 32 bits)
+  p->seg_ctas = p->tc ? sms : 0;
+  p->seg_blocks = p->tc ? (int)blocks : 0;
+  p->psplits = d->prefix_capacity ? pieces(pranges, prow, d->prefix_capacity) : 0;
+  // bf16 own keys: one piece where that is a wave of CTAs (behind a prefix, 256 ranges of 512 keys 26.6 us,
+  // in pieces 28.9; 128 ranges 24.9 and 20.5), or where, alone, they need no join then (32 ranges of 256 keys
+  // 8.3 us, in pieces 9.0; of 512 11.0 and 8.9; 128 ranges of 512 12.3 and 13.2).
   p->ssplits = !d->own_capacity ? 0
-               : !f32 && (own * ((orow + 63) / 64) >= sms || d->own_capacity <= 512)
-                   ? 1 : pieces(own, orow, d->own_capacity);
+               : p->front || (!f32 && (whole || (!d->prefix_capacity && d->own_capacity <= (half ? 512 : 256))))
+                   ? 1 : pieces(oranges, orow, d->own_capacity);
   p->rows = (size_t)rows;
   const size_t slots = (size_t)p->psplits + p->ssplits;
-  const size_t segs = tc ? (size_t)sms + (size_t)d->groups * d->kv_heads * blocks : 0;
+  const size_t segs = p->tc ? (size_t)sms + (size_t)pranges * blocks : 0;
   p->ml_off = 256;
   p->po_off = p->ml_off + align_up(slots * p->rows * sizeof(float2), 256);
   p->start_off = p->po_off + align_up(slots * p->rows * d->head_dim * sizeof(float), 256);
@@ -1007,10 +1031,10 @@ lilicorr_status_t run_prefix_attention(const lilicorr_prefix_attention_desc* des
   own.capacity = desc->own_capacity; own.splits = p.ssplits; own.own = 1;
   const bool bf = desc->dtype == LILICORR_BF16;
   // no prefix, or one that the own keys' kernel walks through first: one launch
-  own.join = bf && own.splits == 1 && (!has_p || front_takes(a, pre));
+  own.join = bf && own.splits == 1 && (!has_p || p.front);
   a.slots = 0;
   if (starve && (!has_p || own.join || !bf)) return LILICORR_ERR_SHAPE;
-  if (own.join && has_p) {
+  if (p.front) {
     own.front = 1;
     own.front_k = pre.k;
     own.front_v = pre.v;
@@ -1021,7 +1045,7 @@ lilicorr_status_t run_prefix_attention(const lilicorr_prefix_attention_desc* des
     return launch_pa_mma(a, own, stream);
   }
   PaMaps maps;
-  const bool tc = has_p && bf && pa_tc_maps(a, pre, &maps);
+  const bool tc = p.tc && pa_tc_maps(a, pre, &maps);
   if (starve && !tc) return LILICORR_ERR_SHAPE;
   if (!tc) a.seg_ctas = 0;
   else pre.splits = 0;
@@ -1053,6 +1077,12 @@ lilicorr_status_t lilicorr_prefix_attention(const lilicorr_prefix_attention_desc
                                             size_t ws_bytes, cudaStream_t stream) {
   return run_prefix_attention(desc, q, prefix_k, prefix_v, prefix_len, k, v, seq_len, out, lse, ws,
                               ws_bytes, stream, PA_WAIT, 0);
+}
+
+int lilicorr_test_prefix_path(int mode) {
+  const int prev = g_pa_path;
+  g_pa_path = mode < 0 ? 0 : mode > 2 ? 2 : mode;
+  return prev;
 }
 
 lilicorr_status_t lilicorr_test_prefix_attention_timeout(

@@ -4,9 +4,8 @@
 // One CTA an SM. Warps 8 and 10 feed K and V tiles by TMA into two rings. Warp 9 issues
 //   S = Q K^T   (M 128, N 128)   into tensor memory, and
 //   O += P V    (M 128, N d)     with P read from tensor memory, V as the MN-major operand.
-// Warps 0-3 and 4-7 are two streams, a thread a row: it reads the row's 128 scores (one wait: a load
-// from tensor memory takes 400 clocks beside running products), takes the running maximum, writes
-// P = 2^(s - m) as bf16 and keeps the row's sum. While one stream is at its exponentials the tensor
+// Warps 0-3 and 4-7 are two streams, a thread a row: it reads the row's scores 64 at a time (all 128 at
+// once spill), takes the running maximum, writes P = 2^(s - m) as bf16 and keeps the row's sum. While one stream is at its exponentials the tensor
 // cores work for the other. With two row tiles the streams share each key tile; with one they take the
 // key tiles in turn, and each leaves its own sums. Warps without a row do nothing but keep the count of arrivals.
 //
@@ -31,7 +30,8 @@ constexpr uint32_t PT_TMEM = 512;
 
 // ONE: no group has more than 128 rows: one row tile, and the second's space goes to the rings, which
 // then hold three tiles of K and of V (d = 128) where two row tiles leave room for three and two. The
-// bytes under way are what bounds few rows: 32 rows a group, 41 K keys a head, 48 -> 36 us.
+// bytes under way are what bounds few rows: 8 groups behind 5,120 keys of 8 heads, d = 64, 32 rows 36.7 ->
+// 35.0 us, 128 rows 52.3 -> 50.6; d = 128, 32 rows 51.6 -> 50.9, 128 rows the same (72).
 template <int DP, bool ONE>
 struct PtCfg {
   static constexpr int CH = DP / 64;                 // 64-column chunks of a row
@@ -214,8 +214,8 @@ pa_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
 
   if (warp == 8 || warp == 10) {
     // ---- copies, K by one warp and V by the other: a K tile's place is free as soon as its scores are
-    // there, long before V's, and waits for no V tile. The first queries go first: behind 24 MB of
-    // tiles that all SMs ask for at once they came 7 us later.
+    // there, long before V's, and waits for no V tile. The first queries are asked for first: everything
+    // waits for them, and they would queue behind the 24 MB of tiles that all SMs ask for at once.
     if (cur.left) named_bar(4, PT_SOFT + 64);
     if (lane == 0) {
       const bool is_k = warp == 8;

@@ -231,6 +231,48 @@ def test_captured_replayed_and_on_another_stream(dtype):
             assert o[2].status() == 0
 
 
+@pytest.fixture(params=[1, 2])
+def path(request):
+    """Both kernels of a bf16 prefix, whatever the sizes."""
+    ll = _ll()
+    prev = ll.test_prefix_path(request.param)
+    yield request.param
+    ll.test_prefix_path(prev)
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+def test_shapes_on_both_paths(shape, path):
+    test_shapes(shape, "bf16")
+
+
+@pytest.mark.parametrize("T,plen,slen", [
+    (1, [0, 0], [0, 0, 0, 0]), (1, [0, 5], [1, 0, 0, 3]), (3, [0, 70], [0, 1, 2, 3]),
+    (3, [0, 0], [1, 2, 0, 9]), (1, [64, 128], [64, 65, 1, 0]), (2, [63, 129], [2, 128, 130, 127]),
+    (1, [-3, 500], [200, 130, 1, 2])])
+def test_lengths_on_both_paths(T, plen, slen, path):
+    test_lengths_empty_rows_and_clipping("bf16", T, plen, slen)
+
+
+def test_layouts_on_both_paths(path):
+    """Absent sequences, one side only, strides, large scores, far groups, graphs."""
+    test_absent_sequences_are_left_alone("bf16")
+    test_one_side_only("bf16", 150, 0)
+    for shape in ((2, 3, 2, 8, 2, 64, 140, 30), (1, 40, 1, 8, 4, 128, 333, 12), (3, 2, 1, 4, 1, 80, 270, 66)):
+        test_strides("bf16", shape)
+    test_large_scores_and_equal_scores("bf16")
+    test_offsets_past_32_bits("bf16")
+    test_captured_replayed_and_on_another_stream("bf16")
+
+
+@pytest.mark.parametrize("P,S", [(512, 256), (512, 257), (513, 16), (64, 385), (0, 384), (0, 385)])
+@pytest.mark.parametrize("W", [2, 90])
+def test_sides_of_the_plan(P, S, W):
+    """Capacities on both sides of where a prefix goes in front of the own keys, and pieces begin."""
+    ll = _ll()
+    x = _inputs(1, W, 1, 8, 2, 64, P, S, "bf16", P + S + W)
+    _check(ll.prefix_attention(*x), x, "bf16")
+
+
 def test_two_streams_at_once():
     ll = _ll()
     xs = [_inputs(2, 8, 1, 8, 2, 128, 3000, 60, "bf16", s) for s in (1, 2)]
