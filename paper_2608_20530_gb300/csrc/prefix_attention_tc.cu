@@ -9,8 +9,8 @@
 // cores work for the other. With two row tiles the streams share each key tile; with one they take the
 // key tiles in turn, and each leaves its own sums. Warps without a row do nothing but keep the count of arrivals.
 //
-// O is not rescaled whenever a maximum grows: m is the maximum that a row's sums are taken against, and
-// it moves only when a score would pass it by 2^8, so that terms stay below 2^8 and sums exact to fp32.
+// O is not rescaled whenever a maximum grows: m, a whole number, is what a row's sums are taken against, and
+// it moves only when a score would pass it by 8, so that terms stay below 2^8 and sums exact to fp32.
 //
 // What bounds it: bytes of K and V for up to about 256 rows a group (each is read from HBM once and
 // from L2 by the further row blocks), beyond that the two products (512 clocks each of an SM's tensor
@@ -88,6 +88,19 @@ __device__ __forceinline__ uint64_t add_pairs(uint64_t a, uint64_t b) {
   uint64_t d;
   asm("add.rn.ftz.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
+}
+
+// Nothing that uses these registers moves above this point (a load from tensor memory fills them until
+// its wait).
+__device__ __forceinline__ void pin(uint32_t (&r)[32]) {
+#pragma unroll
+  for (int i = 0; i < 32; i += 8)
+    asm volatile("" : "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]),
+                      "+r"(r[i + 5]), "+r"(r[i + 6]), "+r"(r[i + 7]));
+}
+// 2^d of a whole number d <= 0 (0 below the normal range, and for -inf)
+__device__ __forceinline__ float pow2_down(float d) {
+  return d < -126.f ? 0.f : __int_as_float((127 + (int)d) << 23);
 }
 
 // A wait that did not end at once: false after `limit` SM cycles, or when another warp gave up.
@@ -386,40 +399,20 @@ pa_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         }
         tc_fence_after();
         const int keys = end - (int)t * PA_TILE;
-        // 64 scores at a time: the first half stays for the exponentials, the second is read again (128
-        // of them spill beside the rest)
+        // 64 scores at a time, a step of the running maximum each: the second half's are read while the
+        // first's exponentials run (all 128 at once spill beside the rest)
         uint32_t x[2][32];
-        auto load = [&](int half) {
-          tmem_ld32_nowait(lane_base + Cfg::S(s) + 64 * half, x[0]);
-          tmem_ld32_nowait(lane_base + Cfg::S(s) + 64 * half + 32, x[1]);
+        auto load = [&](int quarter) {
+          tmem_ld32_nowait(lane_base + Cfg::S(s) + 32 * quarter, x[quarter & 1]);
         };
-        auto mask = [&](int half) {
-          if (keys < PA_TILE) {
-#pragma unroll
-            for (int c = 0; c < 2; ++c)
-#pragma unroll
-              for (int e = 0; e < 32; ++e)
-                if (64 * half + 32 * c + e >= keys) x[c][e] = 0xFF800000u;       // -inf
-          }
+        auto landed = [&]() {
+          tmem_wait_ld();
+          pin(x[0]);
+          pin(x[1]);
         };
-        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-        auto maximum = [&]() {
-#pragma unroll
-          for (int e = 0; e < 32; e += 4)              // three at a time
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-              mx[c] = fmaxf(fmaxf(mx[c], __uint_as_float(x[c][e])), __uint_as_float(x[c][e + 1]));
-              mx[2 + c] = fmaxf(fmaxf(mx[2 + c], __uint_as_float(x[c][e + 2])), __uint_as_float(x[c][e + 3]));
-            }
-        };
-        load(1);
-        tmem_wait_ld();
-        mask(1);
-        maximum();
         load(0);
-        tmem_wait_ld();
-        mask(0);
-        maximum();
+        load(1);
+        landed();
         if (keys < PA_TILE) {
           // V behind the last key: zeros, whatever the cache holds there (to the product's 16)
           const uint32_t i = i0 + t;
@@ -432,52 +425,83 @@ pa_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                 make_uint4(0, 0, 0, 0);
           }
           fence_async_shared();
+          __syncwarp();
         }
-        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2;
-        if (t == first) {
-          m = top;
-        } else if (__any_sync(0xffffffffu, top > m + 8.f)) {
-          // the sums so far to the new maximum (their product is complete: the scores came behind it)
-          const float to = fmaxf(m, top), f = pa_ex2(m - to);
-          m = to;
-          l *= f;
 #pragma unroll
-          for (int c = 0; c < DP / 16; ++c) {
-            uint32_t o[16];
-            tmem_ld16(lane_base + Cfg::O(s) + 16 * c, o);
+        for (int half = 0; half < 2; ++half) {
+          if (keys < PA_TILE) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-            tmem_st16(lane_base + Cfg::O(s) + 16 * c, o);
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+              for (int e = 0; e < 32; ++e)
+                if (64 * half + 32 * c + e >= keys) x[c][e] = 0xFF800000u;         // -inf
           }
+          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int e = 0; e < 32; e += 4)              // three at a time
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              mx[c] = fmaxf(fmaxf(mx[c], __uint_as_float(x[c][e])), __uint_as_float(x[c][e + 1]));
+              mx[2 + c] = fmaxf(fmaxf(mx[2 + c], __uint_as_float(x[c][e + 2])), __uint_as_float(x[c][e + 3]));
+            }
+          const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2;
+          if (half == 0 && t == first) {
+            m = ceilf(top);
+          } else if (__any_sync(0xffffffffu, top > m + 8.f)) {
+            // the sums so far, and the first half's probabilities, to the new maximum: by a whole power
+            // of two, which rounds nothing (their product is complete: the scores came behind it)
+            const float to = fmaxf(m, ceilf(top)), f = pow2_down(m - to);
+            m = to;
+            l *= f;
+            if (t != first) {
+#pragma unroll 1
+              for (int c = 0; c < DP / 16; ++c) {
+                uint32_t o[16];
+                tmem_ld16(lane_base + Cfg::O(s) + 16 * c, o);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                tmem_st16(lane_base + Cfg::O(s) + 16 * c, o);
+              }
+            }
+            if (half == 1) {
+              tmem_wait_st();
+#pragma unroll 1
+              for (int c = 0; c < 2; ++c) {
+                uint32_t p[16];
+                tmem_ld16(lane_base + Cfg::P(s, 2 * c), p);
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                  p[e] = pack_bf16x2(__uint_as_float(p[e] << 16) * f, __uint_as_float(p[e] & 0xFFFF0000u) * f);
+                tmem_st16(lane_base + Cfg::P(s, 2 * c), p);
+              }
+            }
+          }
+          const float base = m == -INFINITY ? 0.f : m;
+          uint64_t sum0 = 0ull, sum1 = 0ull;
+          const uint64_t sc2 = pair_of(__float_as_uint(a.scale_log2), __float_as_uint(a.scale_log2));
+          const uint64_t nb2 = pair_of(__float_as_uint(-base), __float_as_uint(-base));
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            uint32_t p[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              float p0, p1;
+              halves(fma_pair(pair_of(x[c][2 * e], x[c][2 * e + 1]), sc2, nb2), p0, p1);
+              p0 = pa_ex2(p0);
+              p1 = pa_ex2(p1);
+              const uint64_t pp = pair_of(__float_as_uint(p0), __float_as_uint(p1));
+              if (e & 1) sum1 = add_pairs(sum1, pp);
+              else sum0 = add_pairs(sum0, pp);
+              p[e] = pack_bf16x2(p0, p1);
+            }
+            if (half == 0) load(2 + c);
+            tmem_st16(lane_base + Cfg::P(s, 4 * half + 2 * c), p);
+          }
+          float l0, l1;
+          halves(add_pairs(sum0, sum1), l0, l1);
+          l += l0 + l1;
+          if (half == 0) landed();
         }
-        const float base = m == -INFINITY ? 0.f : m;
-        uint64_t sum0 = 0ull, sum1 = 0ull;
-        const uint64_t sc2 = pair_of(__float_as_uint(a.scale_log2), __float_as_uint(a.scale_log2));
-        const uint64_t nb2 = pair_of(__float_as_uint(-base), __float_as_uint(-base));
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          if (c == 2) {
-            load(1);
-            tmem_wait_ld();
-            mask(1);
-          }
-          uint32_t p[16];
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            float p0, p1;
-            halves(fma_pair(pair_of(x[c & 1][2 * e], x[c & 1][2 * e + 1]), sc2, nb2), p0, p1);
-            p0 = pa_ex2(p0);
-            p1 = pa_ex2(p1);
-            const uint64_t pp = pair_of(__float_as_uint(p0), __float_as_uint(p1));
-            if (e & 1) sum1 = add_pairs(sum1, pp);
-            else sum0 = add_pairs(sum0, pp);
-            p[e] = pack_bf16x2(p0, p1);
-          }
-          tmem_st16(lane_base + Cfg::P(s, 2 * c), p);
-        }
-        float l0, l1;
-        halves(add_pairs(sum0, sum1), l0, l1);
-        l += l0 + l1;
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
