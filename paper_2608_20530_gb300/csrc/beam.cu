@@ -390,6 +390,19 @@ template <> struct Elem<uint16_t> {
   static constexpr int N = 8;
   __device__ static float value(uint16_t x) { return bf16_to_f32(x); }
   static constexpr uint32_t NONE = 0xFF80FF80u;
+  static constexpr int BITS = 16;
+  // the value whose ord32 begins with these 16 bits, and how many of a lane's share reach it
+  __device__ static float image(uint32_t code) { return unord32((code >> 31) ? code : code | 0xFFFFu); }
+  __device__ static int at_least(const uint4 (&v)[BS_U], uint32_t code) {
+    const __nv_bfloat162 t = __float2bfloat162_rn(image(code));          // (exact)
+    auto reach = [&](uint32_t w) {
+      return __popc(__hge2_mask(*reinterpret_cast<const __nv_bfloat162*>(&w), t));
+    };
+    int n = 0;
+#pragma unroll
+    for (int u = 0; u < BS_U; ++u) n += (reach(v[u].x) + reach(v[u].y)) + (reach(v[u].z) + reach(v[u].w));
+    return n >> 4;
+  }
   __device__ static void pair(const uint4& v, int i, float& a, float& b) {
     const uint32_t w = i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w;
     a = __uint_as_float(w << 16);
@@ -429,6 +442,17 @@ template <> struct Elem<float> {
   static constexpr int N = 4;
   __device__ static float value(float x) { return x; }
   static constexpr uint32_t NONE = 0xFF800000u;
+  static constexpr int BITS = 32;
+  __device__ static float image(uint32_t code) { return unord32(code); }
+  __device__ static int at_least(const uint4 (&v)[BS_U], uint32_t code) {
+    const float t = image(code);
+    int n = 0;
+#pragma unroll
+    for (int u = 0; u < BS_U; ++u)
+      n += ((__uint_as_float(v[u].x) >= t) + (__uint_as_float(v[u].y) >= t)) +
+           ((__uint_as_float(v[u].z) >= t) + (__uint_as_float(v[u].w) >= t));
+    return n;
+  }
   __device__ static void pair(const uint4& v, int i, float& a, float& b) {
     a = __uint_as_float(i == 0 ? v.x : v.z);
     b = __uint_as_float(i == 0 ? v.y : v.w);
@@ -583,7 +607,8 @@ beam_stream_kernel(const T* __restrict__ logits, unsigned rows, const float* __r
       // LOG2E is log2(e) to 2^-26, so a term wants (1 + x LOG2E_REST) more; x of the terms that count is
       // the chunk's largest or a few below it, and 1e-8 times those few is what this leaves
       const float part = (p0 + p1) + (p2 + p3);
-      add_pair(s, lost, part, e == -INFINITY ? 0.f : part * (m * LOG2E_REST));
+      // (a chunk of -inf alone, behind others or before them, adds 0)
+      add_pair(s, lost, part, m == -INFINITY ? 0.f : part * (m * LOG2E_REST));
     }
     stage = stage + 1 == BS_STAGES ? 0 : stage + 1;
     if (++c == chunks || i + 1 == stop) {               // the warp's last chunk of this row
@@ -604,29 +629,31 @@ beam_stream_kernel(const T* __restrict__ logits, unsigned rows, const float* __r
   }
 }
 
-// More than n of a chunk's elements reach the bound (equal logits, or a row that falls steadily): its
-// first n, by a search over the bits of the n-th largest value; of those equal to it the lowest ids.
-// hot: this lane's elements (element j of vector u: bit u * N + j), at: the chunk's first.
+// More than n of a chunk's elements reach the bound (few chunks for n, equal logits, a row that falls
+// steadily): its first n, by a search over the bits of the n-th largest value, in registers; of those
+// equal to it the lowest ids. hot: this lane's elements (element j of vector u: bit u * N + j). What lies
+// below the bound does not change a count that is compared with n.
 template <typename T>
-__device__ __noinline__ uint64_t chunk_first(const T* __restrict__ at, uint64_t hot, int n, int lane) {
+__device__ __forceinline__ uint64_t chunk_first(const uint4 (&raw)[BS_U], uint64_t hot, int n, int lane) {
   constexpr int N = Elem<T>::N;
-  auto image = [&](int bit) {
-    return ord32(Elem<T>::value(at[((bit / N) * 32 + lane) * N + bit % N]) + 0.f);   // -0 to +0
-  };
   uint32_t nth = 0;
-  for (int b = 31; b >= 0; --b) {
+  for (int b = 31; b >= 32 - Elem<T>::BITS; --b) {
     const uint32_t t = nth | (1u << b);
-    int cnt = 0;
-    for (uint64_t h = hot; h; h &= h - 1) cnt += image(__ffsll((long long)h) - 1) >= t ? 1 : 0;
-    if (__reduce_add_sync(FULL, cnt) >= n) nth = t;
+    if (__reduce_add_sync(FULL, Elem<T>::at_least(raw, t)) >= n) nth = t;
   }
+  const float v = Elem<T>::image(nth);
   uint64_t above = 0, equal = 0;
-  for (uint64_t h = hot; h; h &= h - 1) {
-    const int j = __ffsll((long long)h) - 1;
-    const uint32_t o = image(j);
-    if (o > nth) above |= 1ull << j;
-    if (o == nth) equal |= 1ull << j;
-  }
+#pragma unroll
+  for (int u = 0; u < BS_U; ++u)
+#pragma unroll
+    for (int j = 0; j < N / 2; ++j) {
+      float x0, x1;
+      Elem<T>::pair(raw[u], j, x0, x1);
+      above |= (x0 > v ? 1ull : 0ull) << (u * N + 2 * j) | (x1 > v ? 1ull : 0ull) << (u * N + 2 * j + 1);
+      equal |= (x0 == v ? 1ull : 0ull) << (u * N + 2 * j) | (x1 == v ? 1ull : 0ull) << (u * N + 2 * j + 1);
+    }
+  above &= hot;
+  equal &= hot;
   int room = n - __reduce_add_sync(FULL, __popcll(above));
   for (int u = 0; u < BS_U; ++u) {
     const uint64_t mask = (N == 8 ? 0xFFull : 0xFull) << (u * N);
@@ -831,7 +858,7 @@ beam_choose_kernel(const T* __restrict__ logits, int W, const float* __restrict_
         hot |= (x1 >= thr && x1 > -INFINITY ? 1ull : 0ull) << (u * N + 2 * j + 1);
       }
     }
-    if (__reduce_add_sync(FULL, __popcll(hot)) > out.n) hot = chunk_first<T>(rp + b, hot, out.n, lane);
+    if (__reduce_add_sync(FULL, __popcll(hot)) > out.n) hot = chunk_first<T>(raw, hot, out.n, lane);
     for (uint64_t h = hot; h; h &= h - 1) {
       const int j = __ffsll((long long)h) - 1, id = b + ((j / N) * 32 + lane) * N + j % N;
       const uint64_t key = sum_key(base.x, base.y, Elem<T>::value(rp[id]));

@@ -340,6 +340,38 @@ def test_beam_merge_of_topk_lists_is_beam_select():
     _check(ll.beam_merge(ids, logp, torch.from_numpy(scores).cuda(), 8), want[:4], 2.0 ** -19)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V,ban", [(6148, None), (8198, None), (4102, (0, 2100)), (9000, (2000, 7000)),
+                                   (8192, (4096, 8192)), (5001, (0, 4990))])
+def test_beam_select_runs_of_banned_tokens(V, ban, dtype):
+    """Whole pieces of a row without a finite logit (a run of banned tokens, or none left of the row), where
+    a warp walks several pieces: they add nothing to the row's sum, and the row stays."""
+    ll = _ll()
+    R, W, n = 80, 8, 6
+    x, scores, _ = _select_inputs(R, W, V, dtype, V)
+    if ban:
+        x[:, :, ban[0]:ban[1]] = NINF
+    ws = ll.Workspace(ll.beam_select_workspace_bytes(R, W, V, n))
+    got = _run_select(ll, x, scores, n, dtype, ws=ws)
+    _check_select(got, _want_select(x, scores, n, None, -1), scores, None, -1)
+    assert ws.status() == 0
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("R,W,V,n", [(3, 16, 1697, 32), (5, 4, 900, 32), (2, 2, 40, 31), (4, 13, 2375, 26),
+                                     (1, 1, 2048, 32)])
+def test_beam_select_few_pieces(R, W, V, n, dtype):
+    """Fewer pieces of the rows than continuations, or not many more: most of a piece reaches the bound.
+    Logits of few values too, so that ids decide."""
+    ll = _ll()
+    for grid in (None, 4, 1, -1):
+        x, scores, _ = _select_inputs(R, W, V, dtype, R + V)
+        if grid is not None:                                    # -1: all equal, negative
+            x = np.full_like(x, -3.0) if grid < 0 else (np.round(x * grid / 4) / grid).astype(np.float32) + 0.0
+        want = _want_select(x, scores, n, None, -1)
+        _check_select(_run_select(ll, x, scores, n, dtype), want, scores, None, -1)
+
+
 def test_beam_python_refusals():
     ll = _ll()
     x, sc = torch.zeros((2, 3, 50), device="cuda"), torch.zeros((2, 3), device="cuda")
