@@ -694,12 +694,14 @@ beam_choose_kernel(const T* __restrict__ logits, int W, const float* __restrict_
   constexpr int CAND = LILICORR_MAX_K * LILICORR_MAX_K;
   __shared__ float2 s_base[LILICORR_MAX_BEAMS];         // score - normaliser, as a pair
   __shared__ uint8_t s_kind[LILICORR_MAX_BEAMS];        // 0 absent, 1 live, 2 done
-  // a lane's largest chunk maximum of a row, while chunks are chosen; the candidates after that
+  // a lane's largest chunk maximum of a row and where it is, while chunks are chosen; the candidates
+  // after that
   __shared__ union {
-    float lanes[LILICORR_MAX_BEAMS][32];
+    struct { float top[LILICORR_MAX_BEAMS][32]; int at[LILICORR_MAX_BEAMS][32]; } lanes;
     struct { uint64_t key[CAND], at[CAND]; } cand;
   } s_u;
-  auto& s_lane = s_u.lanes;
+  auto& s_lane = s_u.lanes.top;
+  auto& s_lane_at = s_u.lanes.at;
   auto& s_key = s_u.cand.key;
   auto& s_at = s_u.cand.at;
   __shared__ RankShared sh;
@@ -768,6 +770,7 @@ beam_choose_kernel(const T* __restrict__ logits, int W, const float* __restrict_
     if (bad) kind = 0;
     if (kind == 0) best = -INFINITY;
     s_lane[w][lane] = best;
+    s_lane_at[w][lane] = at;
     if (lane == 0) {
       if (bad) set_status(status, LILICORR_ERR_NONFINITE);
       s_base[w] = make_float2(hi, lo);
@@ -780,6 +783,23 @@ beam_choose_kernel(const T* __restrict__ logits, int W, const float* __restrict_
 
   // the first n chunks, by their largest total; a done beam is one chunk of one candidate
   rank_bound<BC_THREADS>(sh, out.n, best_key, best_pos);
+  // Few groups have a row of their own where beams are few, and many chunks reach the n-th of them where
+  // beams differ: the n-th of all lanes' best instead
+  for (int w = warp; w < W; w += NW) {
+    const float v = s_lane[w][lane];
+    if (v == -INFINITY) continue;
+    const float2 base = s_base[w];
+    rank_keep(sh, sum_key(base.x, base.y, v), ((uint64_t)w << 32) | (uint32_t)s_lane_at[w][lane]);
+  }
+  __syncthreads();
+  uint64_t nth = 0ull, nth_pos = 0ull;
+  rank_kept<BC_THREADS>(sh, out.n, [&](int rank, uint64_t key, uint64_t p) {
+    if (rank == out.n - 1) { nth = key; nth_pos = p; }
+  });
+  __syncthreads();
+  if (nth) { sh.bound = nth; sh.bound_pos = nth_pos; }
+  if (tid == 0) sh.count = 0;
+  __syncthreads();
   const uint64_t bound = sh.bound;
   for (int w = warp; w < W; w += NW) {
     const float2 base = s_base[w];
