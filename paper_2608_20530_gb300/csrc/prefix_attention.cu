@@ -931,13 +931,17 @@ bool pa_plan(const lilicorr_prefix_attention_desc* d, PaPlan* p) {
   // The tensor-core kernel pays 6-8 us for its start and its segments' sums, so that small products are
   // faster on mma.sync, in pieces: 8 ranges, 4 rows, 2,048 keys 18.5 us and 12.4 there; 32 ranges, 32 rows,
   // 2,048 keys 24.7 and 22; at 4,096 keys 30.9 and 27; 64 rows 36.3 and 37; 128 rows 44.5 and 62; 256 rows
-  // 60 and 106. At d = 64, 32 ranges, 4,096 keys, 64 rows 26.8 and 24; at 8,192 34.4 and 32; 128 rows 31 and 38.
+  // 60 and 106. At d = 64, 32 ranges, 4,096 keys, 64 rows 26.8 and 24; at 8,192 34.4 and 32; 128 rows 31 and
+  // 38. Each range costs it 4 us or more besides: 2,048 ranges of 256 keys, 4 rows 106 us and 70; 256 of 256,
+  // 64 rows 62 and 56; 512 of 2,048, 16 rows 119 and 114; 512 of 1,024, 64 rows 142 and 157; 256 of 256, 256
+  // rows 181 and 197. And at d = 64 up to 16 rows never fill it: 512 ranges of 2,048 keys 91 and 68.
   const long long blocks = (prow + PA_BLOCK - 1) / PA_BLOCK;
   const double tiles = (double)pranges * blocks * ((double)d->prefix_capacity / PA_TILE + 1);
-  const double products = (double)pranges * ((double)d->prefix_capacity / PA_TILE) *
-                          (prow < 16 ? 16 : prow) * (d->head_dim <= 64 ? 64 : 128);
+  const double item = (double)d->prefix_capacity / PA_TILE * (prow < 16 ? 16 : prow) *
+                      (d->head_dim <= 64 ? 64 : 128);
   p->tc = !f32 && d->prefix_capacity && !p->front &&
-          (g_pa_path ? g_pa_path == 1 : products > 4.0 * 1048576.0);
+          (g_pa_path ? g_pa_path == 1
+                     : pranges * item > 4.0 * 1048576.0 && item > 32768.0 && (prow > 16 || d->head_dim > 64));
   if (p->tc && tiles >= 2147483648.0) return false;      // (they are counted in 32 bits)
   p->seg_ctas = p->tc ? sms : 0;
   p->seg_blocks = p->tc ? (int)blocks : 0;
