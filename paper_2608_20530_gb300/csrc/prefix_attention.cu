@@ -19,6 +19,7 @@ namespace lilicorr {
 namespace {
 
 constexpr int PM_STAGES = 3;
+constexpr float LN2 = 0.69314718f, LN2_REST = -1.9046543e-9f;      // ln 2 = LN2 + LN2_REST
 
 __device__ __forceinline__ uint32_t sm_addr(const void* p) {
   return static_cast<uint32_t>(__cvta_generic_to_shared(p));
@@ -178,7 +179,8 @@ __device__ __forceinline__ void join_rows(const PaArgs& a, const PaRow (&w)[R], 
         *reinterpret_cast<uint2*>(out + lane * 4) = make_uint2(bf16_pack2(y.x, y.y), bf16_pack2(y.z, y.w));
     }
     if (lane == 0)
-      a.lse[row[i]] = m[i] == -INFINITY ? -INFINITY : (m[i] + log2f(l[i])) * 0.6931471805599453f;
+      a.lse[row[i]] = m[i] == -INFINITY ? -INFINITY
+                                        : fmaf(m[i], LN2, fmaf(m[i], LN2_REST, logf(l[i])));
   }
 }
 
@@ -765,22 +767,29 @@ pa_simt_kernel(const PaArgs a, const PaKeys kk, int rows, int blocks) {
     const unsigned char* sk = sm + (t % PS_STAGES) * STAGE;
     const unsigned char* sv = sk + PS_KT * LD;
     const int key = k0 + t * PS_KT + lane;
-    float s[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-    for (int c = 0; c < DP / 4; ++c) {
+    float s[4] = {0.f, 0.f, 0.f, 0.f}, odd[4] = {0.f, 0.f, 0.f, 0.f};      // two shorter chains of roundings
+#pragma unroll 4
+    for (int c = 0; c < DP / 4; c += 2) {
       const float4 kv = *reinterpret_cast<const float4*>(sk + lane * LD + c * 16);
+      const float4 kw = *reinterpret_cast<const float4*>(sk + lane * LD + c * 16 + 16);
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        s[i] = dot4(*reinterpret_cast<const float4*>(sq + (warp * 4 + i) * DP + c * 4), kv, s[i]);
+      for (int i = 0; i < 4; ++i) {
+        const float* q = sq + (warp * 4 + i) * DP + c * 4;
+        s[i] = dot4(*reinterpret_cast<const float4*>(q), kv, s[i]);
+        odd[i] = dot4(*reinterpret_cast<const float4*>(q + 4), kw, odd[i]);
+      }
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      s[i] = key < lim[i] ? s[i] * a.scale_log2 : -INFINITY;
-      const float n = fmaxf(m[i], warp_max(s[i]));
+      s[i] += odd[i];
+      // (the exponent's argument rounds once, and the scale's own rounding is made good: scores of 20 would
+      // leave 1e-6 of a term otherwise)
+      const bool seen = key < lim[i];
+      const float n = fmaxf(m[i], warp_max(seen ? s[i] * a.scale_log2 : -INFINITY));
       const float u = n == -INFINITY ? 0.f : n;
       const float f = pa_ex2(m[i] - u);
       m[i] = n;
-      s[i] = pa_ex2(s[i] - u);
+      s[i] = seen ? pa_ex2(fmaf(s[i], a.scale_log2, fmaf(s[i], a.scale_rest, -u))) : 0.f;
       l[i] = l[i] * f + s[i];                     // this lane's share of the sum
       o[i].x *= f; o[i].y *= f; o[i].z *= f; o[i].w *= f;
     }
@@ -1006,7 +1015,9 @@ lilicorr_status_t run_prefix_attention(const lilicorr_prefix_attention_desc* des
   a.G = desc->groups; a.W = desc->beams; a.T = desc->tokens;
   a.Hq = desc->q_heads; a.Hkv = desc->kv_heads; a.rep = desc->q_heads / desc->kv_heads;
   a.d = desc->head_dim;
-  a.scale_log2 = desc->scale * PA_LOG2E;
+  const double scale = (double)desc->scale * 1.4426950408889634;       // log2(e)
+  a.scale_log2 = (float)scale;
+  a.scale_rest = (float)(scale - a.scale_log2);
   a.seg_ctas = p.seg_ctas;
   a.seg_blocks = p.seg_blocks;
   a.seg_rows = a.W * a.T * a.rep;

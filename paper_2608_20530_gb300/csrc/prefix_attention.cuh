@@ -36,6 +36,7 @@ struct PaArgs {
   const int32_t* seq_len;      // [N]
   int G, W, T, Hq, Hkv, rep, d;
   float scale_log2;            // scale * log2(e): scores in log2 units
+  float scale_rest;            // what its rounding left
   // partial results of a piece of the keys: (maximum, sum of 2^(s - maximum)) and the sums of
   // 2^(s - maximum) V, fp32; a maximum of -inf: no keys, and no sums were written
   int slots;                   // pieces per row that are kept by row
@@ -70,8 +71,6 @@ __host__ __device__ __forceinline__ uint32_t pa_per_cta(uint32_t tiles, int ctas
 }
 
 constexpr long long PA_WAIT = 4000000000ll;          // about 2 s
-
-constexpr float PA_LOG2E = 1.4426950408889634f;
 
 // Rows that share a key range: (sequence of the group, token, query head of the key head), in that
 // order. Row r of (group or sequence b, key head h) as (sequence, token, query head).
