@@ -11,8 +11,8 @@
 //       element that goes before everything in a chunk not taken (a larger total, or an equal one at
 //       a lower beam or id, chunks being runs of ids).
 // So the pass over the vocabulary carries no candidates, only a maximum that the sum needs anyway.
-// Totals are 64-bit sums and the normalisers good to about 1e-8: beams whose totals differ by less
-// than an fp32 rounding of either normaliser are still told apart.
+// Totals are sums of 48 bits, the normalisers good to about 1e-8; two normalisers of a request that agree to
+// 2^-22 are taken as one, so that beams of one content tie.
 #include <math.h>
 
 #include "internal.cuh"
@@ -693,6 +693,7 @@ beam_choose_kernel(const T* __restrict__ logits, int W, const float* __restrict_
   constexpr int NW = BC_THREADS / 32;
   constexpr int CAND = LILICORR_MAX_K * LILICORR_MAX_K;
   __shared__ float2 s_base[LILICORR_MAX_BEAMS];         // score - normaliser, as a pair
+  __shared__ float2 s_norm[LILICORR_MAX_BEAMS];         // the normaliser, as a pair (+inf: none)
   __shared__ uint8_t s_kind[LILICORR_MAX_BEAMS];        // 0 absent, 1 live, 2 done
   // a lane's largest chunk maximum of a row and where it is, while chunks are chosen; the candidates
   // after that
@@ -712,9 +713,7 @@ beam_choose_kernel(const T* __restrict__ logits, int W, const float* __restrict_
   const float* mx = maxima + row0 * cut.chunks;
   if (tid == 0) s_cand = 0;
 
-  // a warp a row: its normaliser from the records, and each lane's best chunk; of all its rows this
-  // thread's best
-  uint64_t best_key = 0ull, best_pos = ~0ull;
+  // a warp a row: its normaliser from the records, and each lane's best chunk
   for (int w = warp; w < W; w += NW) {
     const size_t row = row0 + w;
     // every load at once: what a row that is not live left there is not used
@@ -727,8 +726,9 @@ beam_choose_kernel(const T* __restrict__ logits, int W, const float* __restrict_
 #pragma unroll
     for (int u = 0; u < BC_REC; ++u)
       x[u] = lane + 32 * u < count ? rec[lane + 32 * u] : make_float4(0.f, 0.f, -INFINITY, 0.f);
-    float best = -INFINITY, hi = sc, lo = 0.f;
+    float best = -INFINITY;
     int at = 0;
+    float2 norm = make_float2(INFINITY, 0.f);
     for (int c0 = lane; c0 < cut.chunks; c0 += 32 * BC_MAX) {
       float v[BC_MAX];
       load_maxima(mx + (size_t)w * cut.chunks, c0, cut.chunks, v);
@@ -760,9 +760,7 @@ beam_choose_kernel(const T* __restrict__ logits, int W, const float* __restrict_
       for (int o = 16; o > 0; o >>= 1)
         add_pair(s, c, __shfl_xor_sync(FULL, s, o), __shfl_xor_sync(FULL, c, o));
       if (!(s > 0.f && s < INFINITY && E > -INFINITY && E < INFINITY)) bad = true;
-      float lh, ll;
-      log_pair(s, c, E, lh, ll);
-      add_pair(hi, lo, -lh, -ll);
+      log_pair(s, c, E, norm.x, norm.y);
     } else {
       best = kind == 2 && lane == 0 ? 0.f : -INFINITY;  // the one candidate of a beam that is done
       at = 0;
@@ -773,11 +771,38 @@ beam_choose_kernel(const T* __restrict__ logits, int W, const float* __restrict_
     s_lane_at[w][lane] = at;
     if (lane == 0) {
       if (bad) set_status(status, LILICORR_ERR_NONFINITE);
-      s_base[w] = make_float2(hi, lo);
+      s_norm[w] = kind == 1 ? norm : make_float2(INFINITY, 0.f);
+      s_base[w] = make_float2(sc, 0.f);
       s_kind[w] = (uint8_t)kind;
     }
+  }
+  __syncthreads();
+
+  // Rows of one content, which differ in alignment or in where warps met them, have normalisers that differ by
+  // roundings (1e-8 mostly, 2^-23 where all logits are equal and so round alike); so that such beams tie,
+  // one that is within 2^-22 of a lower beam's takes that one's.
+  // Then each row's base, and of all its rows this thread's best.
+  uint64_t best_key = 0ull, best_pos = ~0ull;
+  for (int w = warp; w < W; w += NW) {
+    const float best = s_lane[w][lane];
+    float hi = s_base[w].x, lo = 0.f;
+    if (s_kind[w] == 1) {
+      float2 norm = s_norm[w];
+      for (int w0 = 0; w0 < w; w0 += 32) {
+        const int v = w0 + lane;
+        const float2 x = v < w ? s_norm[v] : make_float2(INFINITY, 0.f);
+        const unsigned same = __ballot_sync(FULL, fabsf((x.x - norm.x) + (x.y - norm.y)) <= 0x1p-22f);
+        if (same) {
+          norm = s_norm[w0 + __ffs(same) - 1];
+          break;
+        }
+      }
+      add_pair(hi, lo, -norm.x, -norm.y);
+    }
+    __syncwarp();
+    if (lane == 0) s_base[w] = make_float2(hi, lo);
     const uint64_t key = best == -INFINITY ? 0ull : sum_key(hi, lo, best);
-    const uint64_t pos = ((uint64_t)w << 32) | (uint32_t)at;
+    const uint64_t pos = ((uint64_t)w << 32) | (uint32_t)s_lane_at[w][lane];
     if (precedes(key, pos, best_key, best_pos)) { best_key = key; best_pos = pos; }
   }
 

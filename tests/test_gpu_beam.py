@@ -341,6 +341,28 @@ def test_beam_merge_of_topk_lists_is_beam_select():
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("R,W,V,n", [(1, 8, 151935, 12), (30, 5, 4771, 12), (90, 16, 2049, 32), (7, 64, 1001, 20),
+                                     (200, 3, 40, 7)])
+def test_beam_select_beams_of_one_content(R, W, V, n, dtype):
+    """Beams with the same logits and the same score, at every alignment: equal totals go to the lower
+    beam, whatever the order in which the rows were summed."""
+    ll = _ll()
+    x, _, _ = _select_inputs(R, 1, V, dtype, V + W)
+    x[:, 0, :] = np.round(x[:, 0, :] * 8) / 8                    # (equal logits too)
+    x[:, 0, V // 2] = 30.0                                       # two that are ahead of all others
+    x[:, 0, V // 3] = 29.5
+    ids = np.argsort(-x[:, 0], axis=1, kind="stable")
+    x = np.repeat(x, W, axis=1)
+    scores = np.zeros((R, W), np.float32)
+    tok, par, sc, _ = (t.cpu().numpy() for t in _run_select(ll, x, scores, n, dtype))
+    for r in range(R):
+        first = sorted((-x[r, w, v], w, v) for w in range(W) for v in ids[r, :n])[:n]
+        assert par[r].tolist() == [c[1] for c in first]
+        assert tok[r].tolist() == [c[2] for c in first]
+        assert all(sc[r, j] == sc[r, j - 1] for j in range(1, n) if first[j][0] == first[j - 1][0])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("V,ban", [(6148, None), (8198, None), (4102, (0, 2100)), (9000, (2000, 7000)),
                                    (8192, (4096, 8192)), (5001, (0, 4990))])
 def test_beam_select_runs_of_banned_tokens(V, ban, dtype):
