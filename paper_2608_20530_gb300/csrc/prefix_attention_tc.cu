@@ -5,9 +5,10 @@
 //   S = Q K^T   (M 128, N 128)   into tensor memory, and
 //   O += P V    (M 128, N d)     with P read from tensor memory, V as the MN-major operand.
 // Warps 0-3 and 4-7 are two streams, a thread a row: it reads the row's scores 64 at a time (all 128 at
-// once spill), takes the running maximum, writes P = 2^(s - m) as bf16 and keeps the row's sum. While one stream is at its exponentials the tensor
-// cores work for the other. With two row tiles the streams share each key tile; with one they take the
-// key tiles in turn, and each leaves its own sums. Warps without a row do nothing but keep the count of arrivals.
+// once spill), takes the running maximum, writes P = 2^(s - m) as bf16 and keeps the row's sum. While one
+// stream is at its exponentials the tensor cores work for the other. With two row tiles the streams share
+// each key tile; with one they take the key tiles in turn, and each leaves its own sums. Warps without a row
+// do nothing but keep the count of arrivals.
 //
 // O is not rescaled whenever a maximum grows: m, a whole number, is what a row's sums are taken against, and
 // it moves only when a score would pass it by 8, so that terms stay below 2^8 and sums exact to fp32.
@@ -42,7 +43,8 @@ struct PtCfg {
   static constexpr size_t SMEM = 1024 + QBYTES + (size_t)(NK + NV) * TILE;
   // tensor-memory columns: scores, output, and the probabilities of keys [16 k, 16 k + 16). At d = 128
   // those lie over the scores, which their thread has read: the next scores of the stream are issued
-  // behind the product that reads them, and products of one shape run in the order of issue. At d = 64 the two products differ in shape, and there is room elsewhere.
+  // behind the product that reads them, and products of one shape run in the order of issue. At d = 64 the
+  // two products differ in shape, and there is room elsewhere.
   __device__ static constexpr uint32_t S(int s) { return s * 128; }
   __device__ static constexpr uint32_t O(int s) { return 256 + s * DP; }
   __device__ static constexpr uint32_t P(int s, int k) {

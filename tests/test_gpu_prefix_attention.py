@@ -264,6 +264,15 @@ def test_layouts_on_both_paths(path):
     test_captured_replayed_and_on_another_stream("bf16")
 
 
+def test_many_groups_on_both_paths(path):
+    """More groups than a CTA has threads, some without a prefix: the list of tiles is cut inside and between
+    them."""
+    ll = _ll()
+    G = 800
+    x = _inputs(G, 1, 1, 2, 1, 64, 200, 3, "bf16", 11, [(37 * g) % 201 if g % 5 else 0 for g in range(G)])
+    _check(ll.prefix_attention(*x), x, "bf16")
+
+
 @pytest.mark.parametrize("P,S", [(512, 256), (512, 257), (513, 16), (64, 385), (0, 384), (0, 385)])
 @pytest.mark.parametrize("W", [2, 90])
 def test_sides_of_the_plan(P, S, W):
