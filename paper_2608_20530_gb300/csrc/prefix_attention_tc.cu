@@ -455,6 +455,7 @@ pa_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
             const float to = fmaxf(m, ceilf(top)), f = pow2_down(m - to);
             m = to;
             l *= f;
+            if (half == 1) tmem_wait_st();             // the first half's stores, of O too where it moved
             if (t != first) {
 #pragma unroll 1
               for (int c = 0; c < DP / 16; ++c) {
@@ -466,7 +467,6 @@ pa_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
               }
             }
             if (half == 1) {
-              tmem_wait_st();
 #pragma unroll 1
               for (int c = 0; c < 2; ++c) {
                 uint32_t p[16];
