@@ -378,6 +378,18 @@ lilicorr_status_t lilicorr_beam_reorder(void* const* host_states, int n_states, 
                                         const int32_t* parents, const int32_t* lengths,
                                         cudaStream_t stream);
 
+/* The same for arrays of several layouts (keys and values of different widths, say) in one call: all
+ * of it is refused, or all of it is enqueued. */
+typedef struct {
+  void* const* host_states;
+  int n_states, positions, heads;
+  size_t row_bytes;
+  int64_t stride_request, stride_beam, stride_position, stride_head;
+} lilicorr_beam_states;
+lilicorr_status_t lilicorr_beam_reorder_layouts(const lilicorr_beam_states* host_layouts, int n_layouts,
+                                               int requests, int beams, const int32_t* parents,
+                                               const int32_t* lengths, cudaStream_t stream);
+
 /* Attention of sequences that share a prefix. Not from the paper: the pass in which the target
  * verifies several drafted blocks of a request (the greedy walk's and the best path's, say), or in
  * which the beams of a request take their next step. N = groups * beams sequences, sequence n of

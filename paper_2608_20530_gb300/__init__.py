@@ -52,6 +52,13 @@ class PrefixAttentionDesc(ctypes.Structure):
                  "v_stride")]
 
 
+class BeamStates(ctypes.Structure):
+    _fields_ = [("host_states", ctypes.POINTER(ctypes.c_void_p)), ("n_states", ctypes.c_int),
+                ("positions", ctypes.c_int), ("heads", ctypes.c_int), ("row_bytes", ctypes.c_size_t)] + \
+               [(n, ctypes.c_int64) for n in
+                ("stride_request", "stride_beam", "stride_position", "stride_head")]
+
+
 _LIB: Optional[ctypes.CDLL] = None
 _P = ctypes.c_void_p
 _I = ctypes.c_int
@@ -97,6 +104,7 @@ _SIGS = {
                                  _P]),
     "lilicorr_beam_reorder": (_I, [ctypes.POINTER(_P), _I, _I, _I, _I, _I, _S] +
                               [ctypes.c_int64] * 4 + [_P, _P, _P]),
+    "lilicorr_beam_reorder_layouts": (_I, [_P, _I, _I, _I, _P, _P, _P]),
     "lilicorr_prefix_attention_workspace_bytes": (_S, [_P]),
     "lilicorr_prefix_attention": (_I, [_P] * 11 + [_S, _P]),
     "lilicorr_test_prefix_attention_timeout": (_I, [_P] * 11 + [_S, ctypes.c_longlong, _I, _P]),
@@ -643,7 +651,7 @@ def beam_reorder(states, parents: torch.Tensor, lengths: Optional[torch.Tensor] 
     state[r, w, :lengths[r]] = state[r, parents[r, w], :lengths[r]] as it was before the call.
     parents [R, W] int32 (outside [0, W): the beam stays), lengths [R] int32 (None: all). Tensors may
     be strided views ([R, W, positions, heads, d] of any layout with dense d) that share no memory with
-    one another or with themselves. Returns ``states``."""
+    one another or with themselves. Nothing is moved by a call that is refused. Returns ``states``."""
     tensors = [states] if isinstance(states, torch.Tensor) else list(states)
     if parents.dim() != 2:
         raise ValueError("parents must be [requests, beams]")
@@ -654,7 +662,7 @@ def beam_reorder(states, parents: torch.Tensor, lengths: Optional[torch.Tensor] 
     if lengths is not None and (lengths.get_device() != dev or lengths.dtype is not torch.int32 or
                                 lengths.shape != (R,) or not lengths.is_contiguous()):
         _refuse(lengths, "lengths", dev, torch.int32, (R,))
-    # arrays of one layout go together; the call looks for overlaps among them
+    # arrays of one layout go together
     groups: Dict[tuple, list] = {}
     for i, t in enumerate(tensors):
         if t.get_device() != dev:
@@ -664,15 +672,26 @@ def beam_reorder(states, parents: torch.Tensor, lengths: Optional[torch.Tensor] 
         starts = [t.data_ptr() for t in tensors if t.numel()]
         if len(set(starts)) < len(starts):
             raise ValueError("states must not overlap")
+    layouts = []                                   # all of them are looked at before anything moves
     for same in groups.values():
         i = next(i for i, t in enumerate(tensors) if t is same[0])
-        positions, heads, row, *strides = _state_layout(same[0], R, W, f"states[{i}]")
+        positions, heads, *_ = layout = _state_layout(same[0], R, W, f"states[{i}]")
         _fits(R | W | positions | heads)
-        code = lib().lilicorr_beam_reorder(
-            (_P * len(same))(*[t.data_ptr() for t in same]), len(same), R, W, positions, heads, row,
-            *strides, parents.data_ptr(), None if lengths is None else lengths.data_ptr(), _stream())
-        if code:
-            _check(code, "beam_reorder")
+        layouts.append(((_P * len(same))(*[t.data_ptr() for t in same]), len(same), layout))
+    if not layouts:
+        return states
+    lens = None if lengths is None else lengths.data_ptr()
+    if len(layouts) == 1:
+        (at, count, (positions, heads, row, *strides)), = layouts
+        code = lib().lilicorr_beam_reorder(at, count, R, W, positions, heads, row, *strides,
+                                           parents.data_ptr(), lens, _stream())
+    else:
+        code = lib().lilicorr_beam_reorder_layouts(
+            (BeamStates * len(layouts))(*[BeamStates(ctypes.cast(at, ctypes.POINTER(_P)), count, *layout)
+                                          for at, count, layout in layouts]),
+            len(layouts), R, W, parents.data_ptr(), lens, _stream())
+    if code:
+        _check(code, "beam_reorder")
     return states
 
 

@@ -1080,6 +1080,50 @@ bool states_overlap(void* const* states, int n, const int64_t* strides, const in
   return false;
 }
 
+// The checks of one layout but for overlaps, and how its arrays are moved: all of `a` but the arrays, parents
+// and lengths, and the bytes a thread takes at a time (0: there is nothing to move).
+lilicorr_status_t reorder_layout(const lilicorr_beam_states& s, int requests, int beams,
+                                 const int32_t* parents, Reorder* a, int* bytes) {
+  *bytes = 0;
+  if (s.n_states < 0 || s.positions < 0 || s.heads < 0) return LILICORR_ERR_SHAPE;
+  if (s.n_states == 0 || requests == 0 || s.positions == 0 || s.heads == 0 || s.row_bytes == 0)
+    return LILICORR_OK;
+  if (!s.host_states || !parents) return LILICORR_ERR_ARG;
+  if (s.row_bytes > (1ull << 31) ||
+      (double)s.positions * s.heads * (double)s.row_bytes >= 16.0 * 2147483648.0)
+    return LILICORR_ERR_SHAPE;
+  for (int i = 0; i < s.n_states; ++i)
+    if (!s.host_states[i]) return LILICORR_ERR_ARG;
+  // heads that follow one another are one longer row
+  size_t row_bytes = s.row_bytes;
+  int heads = s.heads;
+  if (heads > 1 && s.stride_head == (int64_t)row_bytes) {
+    row_bytes *= heads;
+    heads = 1;
+  }
+  // the widest vector that every row starts at and fills, and that W beams leave registers for. (8
+  // requests of 512 positions x 2 KB x 4 arrays, 16, 8 and 4 bytes: 4 beams 33, 41 and 50 us, 16 beams 129,
+  // 130 and 305; 32 beams 266 in 8 bytes and 312 in 4)
+  uint64_t bits = row_bytes | (requests > 1 ? (uint64_t)s.stride_request : 0) |
+                  (beams > 1 ? (uint64_t)s.stride_beam : 0) |
+                  (s.positions > 1 ? (uint64_t)s.stride_position : 0) |
+                  (heads > 1 ? (uint64_t)s.stride_head : 0);
+  for (int i = 0; i < s.n_states; ++i) bits |= reinterpret_cast<uintptr_t>(s.host_states[i]);
+  int vec = beams <= 16 ? 16 : beams <= 32 ? 8 : 4;
+  while (bits & (uint64_t)(vec - 1)) vec >>= 1;
+  if ((double)s.positions * heads * (double)(row_bytes / vec) >= 2147483648.0) return LILICORR_ERR_SHAPE;
+  a->W = beams;
+  a->positions = s.positions;
+  a->heads = heads;
+  a->pieces = (uint32_t)(row_bytes / vec);
+  a->s_req = s.stride_request;
+  a->s_beam = s.stride_beam;
+  a->s_pos = s.stride_position;
+  a->s_head = s.stride_head;
+  *bytes = vec;
+  return LILICORR_OK;
+}
+
 bool beam_shape_ok(int requests, int beams, int n) {
   return requests >= 0 && beams >= 1 && beams <= LILICORR_MAX_BEAMS && n >= 1 && n <= LILICORR_MAX_K;
 }
@@ -1137,65 +1181,55 @@ lilicorr_status_t lilicorr_beam_merge(const int32_t* ids, const float* logp, int
                   done, out, status);
 }
 
+lilicorr_status_t lilicorr_beam_reorder_layouts(const lilicorr_beam_states* host_layouts, int n_layouts,
+                                               int requests, int beams, const int32_t* parents,
+                                               const int32_t* lengths, cudaStream_t stream) {
+  if (n_layouts < 0 || requests < 0 || requests > 65535 || beams < 1 || beams > LILICORR_MAX_BEAMS)
+    return LILICORR_ERR_SHAPE;
+  if (n_layouts > 0 && !host_layouts) return LILICORR_ERR_ARG;
+  // every layout is looked at before the first array is moved
+  Reorder a;
+  int vec;
+  for (int i = 0; i < n_layouts; ++i) {
+    const lilicorr_beam_states& s = host_layouts[i];
+    LL_TRY(reorder_layout(s, requests, beams, parents, &a, &vec));
+    if (vec == 0) continue;
+    const int64_t strides[4] = {a.s_req, a.s_beam, a.s_pos, a.s_head};
+    const int64_t extents[4] = {requests, beams, a.positions, a.heads};
+    if (states_overlap(s.host_states, s.n_states, strides, extents, (int64_t)a.pieces * vec))
+      return LILICORR_ERR_ARG;
+  }
+  a.parents = parents;
+  a.lengths = lengths;
+  for (int i = 0; i < n_layouts; ++i) {
+    const lilicorr_beam_states& s = host_layouts[i];
+    LL_TRY(reorder_layout(s, requests, beams, parents, &a, &vec));
+    if (vec == 0) continue;
+    for (int i0 = 0; i0 < s.n_states; i0 += BR_STATES) {
+      const int count = s.n_states - i0 < BR_STATES ? s.n_states - i0 : BR_STATES;
+      for (int j = 0; j < BR_STATES; ++j)
+        a.state[j] = j < count ? static_cast<unsigned char*>(s.host_states[i0 + j]) : nullptr;
+      switch (vec) {
+        case 16: LL_TRY(launch_reorder<uint4>(a, count, requests, stream)); break;
+        case 8: LL_TRY(launch_reorder<uint2>(a, count, requests, stream)); break;
+        case 4: LL_TRY(launch_reorder<uint32_t>(a, count, requests, stream)); break;
+        case 2: LL_TRY(launch_reorder<uint16_t>(a, count, requests, stream)); break;
+        default: LL_TRY(launch_reorder<uint8_t>(a, count, requests, stream)); break;
+      }
+    }
+  }
+  return LILICORR_OK;
+}
+
 lilicorr_status_t lilicorr_beam_reorder(void* const* host_states, int n_states, int requests,
                                         int beams, int positions, int heads, size_t row_bytes,
                                         int64_t stride_request, int64_t stride_beam,
                                         int64_t stride_position, int64_t stride_head,
                                         const int32_t* parents, const int32_t* lengths,
                                         cudaStream_t stream) {
-  if (n_states < 0 || requests < 0 || requests > 65535 || positions < 0 || heads < 0 || beams < 1 ||
-      beams > LILICORR_MAX_BEAMS)
-    return LILICORR_ERR_SHAPE;
-  if (n_states == 0 || requests == 0 || positions == 0 || heads == 0 || row_bytes == 0)
-    return LILICORR_OK;
-  if (!host_states || !parents) return LILICORR_ERR_ARG;
-  if (row_bytes > (1ull << 31) || (double)positions * heads * (double)row_bytes >= 16.0 * 2147483648.0)
-    return LILICORR_ERR_SHAPE;
-  for (int i = 0; i < n_states; ++i)
-    if (!host_states[i]) return LILICORR_ERR_ARG;
-  // heads that follow one another are one longer row
-  if (heads > 1 && stride_head == (int64_t)row_bytes) {
-    row_bytes *= heads;
-    heads = 1;
-  }
-  // the widest vector that every row starts at and fills, and that W beams leave registers for. (8
-  // requests of 512 positions x 2 KB x 4 arrays, 16, 8 and 4 bytes: 4 beams 33, 41 and 50 us, 16 beams 129,
-  // 130 and 305; 32 beams 266 in 8 bytes and 312 in 4)
-  uint64_t bits = row_bytes | (requests > 1 ? (uint64_t)stride_request : 0) |
-                  (beams > 1 ? (uint64_t)stride_beam : 0) |
-                  (positions > 1 ? (uint64_t)stride_position : 0) |
-                  (heads > 1 ? (uint64_t)stride_head : 0);
-  for (int i = 0; i < n_states; ++i) bits |= reinterpret_cast<uintptr_t>(host_states[i]);
-  int vec = beams <= 16 ? 16 : beams <= 32 ? 8 : 4;
-  while (bits & (uint64_t)(vec - 1)) vec >>= 1;
-  if ((double)positions * heads * (double)(row_bytes / vec) >= 2147483648.0) return LILICORR_ERR_SHAPE;
-  const int64_t strides[4] = {stride_request, stride_beam, stride_position, stride_head};
-  const int64_t extents[4] = {requests, beams, positions, heads};
-  if (states_overlap(host_states, n_states, strides, extents, (int64_t)row_bytes)) return LILICORR_ERR_ARG;
-  Reorder a;
-  a.W = beams;
-  a.positions = positions;
-  a.heads = heads;
-  a.pieces = (uint32_t)(row_bytes / vec);
-  a.s_req = stride_request;
-  a.s_beam = stride_beam;
-  a.s_pos = stride_position;
-  a.s_head = stride_head;
-  a.parents = parents;
-  a.lengths = lengths;
-  for (int i0 = 0; i0 < n_states; i0 += BR_STATES) {
-    const int count = n_states - i0 < BR_STATES ? n_states - i0 : BR_STATES;
-    for (int i = 0; i < BR_STATES; ++i)
-      a.state[i] = i < count ? static_cast<unsigned char*>(host_states[i0 + i]) : nullptr;
-    switch (vec) {
-      case 16: LL_TRY(launch_reorder<uint4>(a, count, requests, stream)); break;
-      case 8: LL_TRY(launch_reorder<uint2>(a, count, requests, stream)); break;
-      case 4: LL_TRY(launch_reorder<uint32_t>(a, count, requests, stream)); break;
-      case 2: LL_TRY(launch_reorder<uint16_t>(a, count, requests, stream)); break;
-      default: LL_TRY(launch_reorder<uint8_t>(a, count, requests, stream)); break;
-    }
-  }
-  return LILICORR_OK;
+  const lilicorr_beam_states one = {host_states, n_states, positions, heads, row_bytes, stride_request,
+                                    stride_beam, stride_position, stride_head};
+  return lilicorr_beam_reorder_layouts(&one, 1, requests, beams, parents, lengths, stream);
 }
 
 int lilicorr_test_states_overlap(void* const* host_states, int n_states, const int64_t* strides,
