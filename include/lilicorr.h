@@ -379,7 +379,8 @@ lilicorr_status_t lilicorr_beam_reorder(void* const* host_states, int n_states, 
                                         cudaStream_t stream);
 
 /* The same for arrays of several layouts (keys and values of different widths, say) in one call: all
- * of it is refused, or all of it is enqueued. */
+ * of it is refused, or all of it is enqueued. Arrays that share a byte are refused across layouts too, and so
+ * are layouts that interleave without a stride in common where 2^20 steps do not tell them apart. */
 typedef struct {
   void* const* host_states;
   int n_states, positions, heads;

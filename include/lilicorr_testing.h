@@ -89,6 +89,10 @@ int lilicorr_test_prefix_path(int mode);
 int lilicorr_test_states_overlap(void* const* host_states, int n_states, const int64_t* strides,
                                  const int64_t* extents, size_t row_bytes);
 
+/* The same of lilicorr_beam_reorder_layouts. */
+int lilicorr_test_layouts_overlap(const lilicorr_beam_states* host_layouts, int n_layouts, int requests,
+                                  int beams);
+
 /* Switch for the fused scoring-network kernels (bf16 heads with D = 256, 8 heads,
  * FFN 2D, L*K <= 128): mode 1 (the default) takes the cluster kernel (four CTAs per
  * sequence) while every sequence's cluster fits on the GPU and the one-CTA kernel for

@@ -1068,18 +1068,6 @@ lilicorr_status_t run_select(const T* logits, lilicorr_dtype_t dt, int requests,
                   maxima, sums, out, reinterpret_cast<uint32_t*>(w));
 }
 
-// A column of the beams is moved by one thread: rows that share bytes would race.
-bool states_overlap(void* const* states, int n, const int64_t* strides, const int64_t* extents,
-                    int64_t row_bytes) {
-  const StrideNest nest(strides, extents, 4, row_bytes);
-  if (!nest.nests()) return true;
-  for (int i = 1; i < n; ++i)
-    for (int j = 0; j < i; ++j)
-      if (nest.meets((__int128)reinterpret_cast<intptr_t>(states[i]) - reinterpret_cast<intptr_t>(states[j])))
-        return true;
-  return false;
-}
-
 // The checks of one layout but for overlaps, and how its arrays are moved: all of `a` but the arrays, parents
 // and lengths, and the bytes a thread takes at a time (0: there is nothing to move).
 lilicorr_status_t reorder_layout(const lilicorr_beam_states& s, int requests, int beams,
@@ -1122,6 +1110,107 @@ lilicorr_status_t reorder_layout(const lilicorr_beam_states& s, int requests, in
   a->s_head = s.stride_head;
   *bytes = vec;
   return LILICORR_OK;
+}
+
+// Rows that share bytes would race: a column of the beams is moved by one thread.
+bool states_overlap(void* const* states, int n, const int64_t* strides, const int64_t* extents,
+                    int64_t row_bytes) {
+  const StrideNest nest(strides, extents, 4, row_bytes);
+  if (!nest.nests()) return true;
+  for (int i = 1; i < n; ++i)
+    for (int j = 0; j < i; ++j)
+      if (nest.meets((__int128)reinterpret_cast<intptr_t>(states[i]) - reinterpret_cast<intptr_t>(states[j])))
+        return true;
+  return false;
+}
+
+// Do two arrays of different layouts share a byte? The distance of two of their rows is the bases' and a
+// whole multiple of each stride that occurs, the multiple an index of the one, the other, or a difference of
+// both; from the largest stride down, only multiples that the smaller ones can make up for are followed.
+// Layouts cut from one buffer share their strides, and few multiples are left. `steps` bounds the search
+// where layouts have nothing in common; past it the answer is yes.
+struct RowDistance {
+  struct Term { __int128 stride; int64_t lo, hi; };
+  int n = 0;
+  Term term[8];
+  __int128 lo[9], hi[9];                   // what the terms from here on can add
+  int64_t row_a, row_b;                    // bytes of a row
+  __int128 shift = 0;                      // of the bases, from rows at negative strides
+  void add(int64_t stride, int64_t extent, bool second) {
+    if (extent <= 1) return;
+    __int128 s = stride;
+    if (s < 0) {                           // counted from its lowest row
+      shift += (second ? s : -s) * (extent - 1);
+      s = -s;
+    }
+    int i = 0;
+    while (i < n && term[i].stride > s) ++i;
+    if (i == n || term[i].stride != s) {
+      for (int j = n; j > i; --j) term[j] = term[j - 1];
+      term[i] = {s, 0, 0};
+      ++n;
+    }
+    if (second) term[i].hi += extent - 1;
+    else term[i].lo -= extent - 1;
+  }
+  void close(int64_t a, int64_t b) {
+    row_a = a;
+    row_b = b;
+    lo[n] = hi[n] = 0;
+    for (int i = n - 1; i >= 0; --i) {
+      lo[i] = lo[i + 1] + term[i].lo * term[i].stride;
+      hi[i] = hi[i + 1] + term[i].hi * term[i].stride;
+    }
+  }
+  // second row - first row = d so far
+  bool meets(__int128 d, long long* steps, int i = 0) const {
+    if (d + lo[i] >= row_a || d + hi[i] <= -row_b) return false;
+    if (i == n || --*steps <= 0) return true;
+    const __int128 s = term[i].stride;
+    // -row_b < d + c s + hi[i + 1] and d + c s + lo[i + 1] < row_a (s > 0: no layout has equal rows)
+    const __int128 from = -row_b - d - hi[i + 1], to = row_a - d - lo[i + 1];
+    const __int128 least = from >= 0 ? from / s + 1 : 1 - (-from + s - 1) / s;
+    const __int128 most = to > 0 ? (to - 1) / s : -((s - to) / s);
+    const __int128 c0 = least > term[i].lo ? least : term[i].lo, c1 = most < term[i].hi ? most : term[i].hi;
+    for (__int128 c = c0; c <= c1; ++c)
+      if (meets(d + c * s, steps, i + 1)) return true;
+    return false;
+  }
+};
+
+// All arrays of a call, of layouts that passed reorder_layout.
+constexpr long long OVERLAP_STEPS = 1 << 20;         // some 10 ms of the host
+bool layouts_overlap(const lilicorr_beam_states* layouts, int n, int requests, int beams) {
+  long long steps = OVERLAP_STEPS;
+  auto empty = [](const lilicorr_beam_states& s) {
+    return s.n_states == 0 || s.positions == 0 || s.heads == 0 || s.row_bytes == 0;
+  };
+  for (int i = 0; i < n; ++i) {
+    const lilicorr_beam_states& b = layouts[i];
+    if (empty(b)) continue;
+    const int64_t strides[4] = {b.stride_request, b.stride_beam, b.stride_position, b.stride_head};
+    const int64_t extents[4] = {requests, beams, b.positions, b.heads};
+    if (states_overlap(b.host_states, b.n_states, strides, extents, (int64_t)b.row_bytes)) return true;
+    for (int j = 0; j < i; ++j) {
+      const lilicorr_beam_states& a = layouts[j];
+      if (empty(a)) continue;
+      RowDistance dist;
+      const int64_t strides_a[4] = {a.stride_request, a.stride_beam, a.stride_position, a.stride_head};
+      const int64_t extents_a[4] = {requests, beams, a.positions, a.heads};
+      for (int d = 0; d < 4; ++d) {
+        dist.add(strides_a[d], extents_a[d], false);
+        dist.add(strides[d], extents[d], true);
+      }
+      dist.close((int64_t)a.row_bytes, (int64_t)b.row_bytes);
+      for (int x = 0; x < a.n_states; ++x)
+        for (int y = 0; y < b.n_states; ++y) {
+          const __int128 d = (__int128)reinterpret_cast<intptr_t>(b.host_states[y]) -
+                             reinterpret_cast<intptr_t>(a.host_states[x]);
+          if (dist.meets(d + dist.shift, &steps)) return true;
+        }
+    }
+  }
+  return false;
 }
 
 bool beam_shape_ok(int requests, int beams, int n) {
@@ -1190,15 +1279,9 @@ lilicorr_status_t lilicorr_beam_reorder_layouts(const lilicorr_beam_states* host
   // every layout is looked at before the first array is moved
   Reorder a;
   int vec;
-  for (int i = 0; i < n_layouts; ++i) {
-    const lilicorr_beam_states& s = host_layouts[i];
-    LL_TRY(reorder_layout(s, requests, beams, parents, &a, &vec));
-    if (vec == 0) continue;
-    const int64_t strides[4] = {a.s_req, a.s_beam, a.s_pos, a.s_head};
-    const int64_t extents[4] = {requests, beams, a.positions, a.heads};
-    if (states_overlap(s.host_states, s.n_states, strides, extents, (int64_t)a.pieces * vec))
-      return LILICORR_ERR_ARG;
-  }
+  for (int i = 0; i < n_layouts; ++i)
+    LL_TRY(reorder_layout(host_layouts[i], requests, beams, parents, &a, &vec));
+  if (requests > 0 && layouts_overlap(host_layouts, n_layouts, requests, beams)) return LILICORR_ERR_ARG;
   a.parents = parents;
   a.lengths = lengths;
   for (int i = 0; i < n_layouts; ++i) {
@@ -1235,6 +1318,11 @@ lilicorr_status_t lilicorr_beam_reorder(void* const* host_states, int n_states, 
 int lilicorr_test_states_overlap(void* const* host_states, int n_states, const int64_t* strides,
                                  const int64_t* extents, size_t row_bytes) {
   return states_overlap(host_states, n_states, strides, extents, (int64_t)row_bytes);
+}
+
+int lilicorr_test_layouts_overlap(const lilicorr_beam_states* host_layouts, int n_layouts, int requests,
+                                  int beams) {
+  return layouts_overlap(host_layouts, n_layouts, requests, beams);
 }
 
 }  // extern "C"

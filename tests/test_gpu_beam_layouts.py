@@ -44,3 +44,18 @@ def test_a_refused_state_leaves_the_others(bad, at):
     assert all(torch.equal(s, k) for s, k in zip(states, keep))
     ll.beam_reorder(states, p.cuda())
     assert all(torch.equal(s.cpu(), _moved(k.cpu(), p, None)) for s, k in zip(states, keep))
+
+
+def test_layouts_that_share_memory_are_refused():
+    """Views of one cache: of overlapping positions, refused and not moved; side by side, moved."""
+    ll = _ll()
+    p = torch.tensor(PARENTS, dtype=torch.int32)
+    x = torch.arange(2 * 4 * 100 * 24, dtype=torch.float32, device="cuda").view(2, 4, 100, 24)
+    keep = x.clone()
+    for bad in ([x[:, :, :64], x[:, :, 32:]], [x[:, :, :, :16], x[:, :, 10:, 15:]],
+                [x[:, :, 3:], x.view(torch.int32)[:, :, :50]]):
+        with pytest.raises(ll.LilicorrError):
+            ll.beam_reorder(bad, p.cuda())
+        assert torch.equal(x, keep)
+    ll.beam_reorder([x[:, :, :64, :16], x[:, :, 64:, :16], x[:, :, :, 16:]], p.cuda())
+    assert torch.equal(x.cpu(), _moved(keep.cpu(), p, None))
