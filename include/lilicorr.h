@@ -327,7 +327,7 @@ lilicorr_status_t lilicorr_select_block_walk(const lilicorr_head* head, int B, c
  *   end_id               the token that ends a beam, or -1 (only where done is NULL)
  * A live beam w offers each of its tokens v at total = scores[w] + logp(v | w); a beam that is done
  * offers the one candidate (end_id, scores[w]), and nothing else about it is read. Totals are formed
- * and compared to 48 bits or more; equal totals order by lower beam, in a beam by the candidates' order. A
+ * and compared to 48 bits; equal totals order by lower beam, in a beam by the candidates' order. A
  * candidate of total -inf (a banned token) is never kept. Outputs, best first:
  *   tokens, parents [R, n] int32   token and beam of each kept candidate; -1 where there are fewer
  *   next_scores     [R, n] fp32    the total, rounded once; -inf where there are fewer
@@ -338,8 +338,10 @@ lilicorr_status_t lilicorr_select_block_walk(const lilicorr_head* head, int B, c
 #define LILICORR_MAX_BEAMS 64
 
 /* From logits [R, W, V] (F32 or BF16), one pass over the rows of live beams:
- * logp(v | w) = logits[w, v] - log sum_u exp(logits[w, u]), in a beam equal logits by lower id. Two
- * normalisers of a request that agree to 2^-22 are taken as one: beams of one content tie.
+ * logp(v | w) = logits[w, v] - log sum_u exp(logits[w, u]), in a beam equal logits by lower id. Finite
+ * logits of any size are taken (a row whose logits are all the type's lowest value is a uniform one). logp
+ * is good to 2^-20 and never above 0. Two normalisers of a request that agree to 2^-22 are taken as one: beams
+ * of one content tie.
  * n <= W * V, R * W <= 65535, logits and ws 16-byte aligned. ws: zero-filled once, at least
  * lilicorr_beam_select_workspace_bytes(R, W, V, n) bytes (0: unsupported shape); its first word is
  * the device status. */

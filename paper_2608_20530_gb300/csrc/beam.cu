@@ -4,15 +4,19 @@
 // Selection from logits takes two launches. (In one, the CTA that finishes a request choosing for it, the
 // choosing ran beside warps that still stream and behind their fences: 32 x 8 rows 30 -> 34 us.)
 //   (1) beam_stream_kernel reads every live row once, in chunks of 32 x 8 vectors of 16 bytes, one
-//       warp a chunk, and leaves each chunk's largest logit and the row's sum of exponentials.
+//       warp a chunk, and leaves each chunk's largest logit m and the sum of exp(x - m).
 //   (2) beam_choose_kernel, one CTA a request, forms the rows' normalisers, takes the n chunks whose
-//       largest totals (score + logit - normaliser) come first, reads those chunks again and ranks
-//       their elements. No other chunk can hold one of the n best: each of the n chunks taken has an
-//       element that goes before everything in a chunk not taken (a larger total, or an equal one at
-//       a lower beam or id, chunks being runs of ids).
+//       largest totals come first, reads those chunks again and ranks their elements. No other chunk
+//       can hold one of the n best: each of the n chunks taken has an element that goes before
+//       everything in a chunk not taken (a larger total, or an equal one at a lower beam or id, chunks
+//       being runs of ids).
 // So the pass over the vocabulary carries no candidates, only a maximum that the sum needs anyway.
-// Totals are sums of 48 bits, the normalisers good to about 1e-8; two normalisers of a request that agree to
-// 2^-22 are taken as one, so that beams of one content tie.
+// A total is (score - log S) + (x - M), M the row's largest logit and S the sum of exp(x - M): whatever the
+// logits' size, x - M keeps what tells them apart. S is at least 1 (the largest logit's own term is 1 exactly),
+// so that no total lies above its score. Totals are sums of 48 bits of inputs that are not: ex2.approx is good
+// to 2^-22 and its argument of up to 17 log2 units, before a term that counts, to 2^-20, so that log S is good to
+// 2^-20 at worst, and to some 1e-8 where many unlike terms share the sum. Two normalisers of a request that
+// agree to 2^-22, their M the same, are taken as one, so that beams of one content tie.
 #include <math.h>
 
 #include "internal.cuh"
@@ -24,7 +28,6 @@ namespace {
 constexpr unsigned FULL = 0xffffffffu;
 constexpr int BM_THREADS = 128;
 constexpr float LOG2E = 1.4426950408889634f;
-constexpr float LOG2E_REST = 1.33497e-8f;      // (log2(e) - LOG2E) ln 2
 
 // order-preserving 32-bit image of a float (-0 below +0)
 __device__ __forceinline__ uint32_t ord32(float v) {
@@ -47,16 +50,26 @@ __device__ __forceinline__ uint64_t pair_key(float s, float c) {
   return ((uint64_t)ord32(s + 0.f) << 32) | ord32(c + 0.f);          // -0 to +0
 }
 __device__ __forceinline__ float key_score(uint64_t key) { return unord32((uint32_t)(key >> 32)); }
-// Key of (hi + lo) + x.
-__device__ __forceinline__ uint64_t sum_key(float hi, float lo, float x) {
-  add_pair(hi, lo, x, 0.f);
+// A row's totals: (hi + lo) + (x - top) for its logits x <= top.
+struct Base {
+  float hi, lo, top;
+};
+__device__ __forceinline__ uint64_t sum_key(const Base& b, float x) {
+  float d = x, rest = 0.f, hi = b.hi, lo = b.lo;
+  add_pair(d, rest, -b.top, 0.f);
+  add_pair(hi, lo, d, rest);
   const float s = hi + lo;
   return pair_key(s, lo - (s - hi));
 }
-// log(s + c) + e log 2 of s > 0 as hi + lo, to about 1e-9. log m = 2 atanh((m - 1) / (m + 1)) for s
+// No logit below this reaches a total of `need`: by fp32, with a margin for its roundings.
+__device__ __forceinline__ float logit_floor(const Base& b, float need) {
+  const float d = (need - b.hi) - 0x1p-20f * (fabsf(need) + fabsf(b.hi));
+  return (b.top + d) - 0x1p-22f * fabsf(b.top);
+}
+// log(s + c) of s >= 1 as hi + lo, to about 1e-9. log m = 2 atanh((m - 1) / (m + 1)) for s
 // scaled to m in [0.7, 1.42): the quotient as a pair, the series' further terms (below 0.004) in fp32.
-__device__ __forceinline__ void log_pair(float s, float c, float e, float& hi, float& lo) {
-  // s = m 2^k (s is normal: a sum of exponentials whose largest lies in (1/2, 1])
+__device__ __forceinline__ void log_pair(float s, float c, float& hi, float& lo) {
+  // s = m 2^k
   const int bits = __float_as_int(s);
   int k = ((bits >> 23) & 255) - 127;
   float m = __int_as_float((bits & 0x7FFFFF) | 0x3F800000);
@@ -68,7 +81,7 @@ __device__ __forceinline__ void log_pair(float s, float c, float e, float& hi, f
   const float zl = __fdividef(fmaf(-z, den, num) + mc - z * (dl + mc), den);
   const float q = z * z;
   const float rest = z * q * (0.66666667f + q * (0.4f + q * (0.28571429f + q * (0.22222222f + q * 0.18181818f))));
-  const float n = e + (float)k, l = 0.69314718f, ll = -1.9046543e-9f;   // log 2 = l + ll + ...
+  const float n = (float)k, l = 0.69314718f, ll = -1.9046543e-9f;   // log 2 = l + ll + ...
   hi = n * l;
   lo = fmaf(n, l, -hi) + n * ll;
   add_pair(hi, lo, 2.f * z, 2.f * zl);
@@ -333,10 +346,10 @@ constexpr int BC_THREADS = 512;                // of the choosing kernel
 
 // How rows are cut: chunk 0 of a row holds the ids before its first 16-byte boundary where rows need
 // not start on one (`odd`), the others runs of `size` ids; warp i of the streaming kernel takes the
-// chunks [i * per_warp, (i + 1) * per_warp) of all rows, and leaves a record for each row among them.
+// chunks [i * per_warp, (i + 1) * per_warp) of all rows.
 struct BeamCut {
   int V, vec, size, odd, chunks;               // chunks per row
-  int per_warp, slots;                         // records per row
+  int per_warp;
   __host__ __device__ int head(size_t row) const {
     if (!odd) return 0;
     const int h = (int)((vec - (row * (size_t)V) % vec) % vec);
@@ -364,21 +377,9 @@ BeamCut beam_cut(int rows, int V, lilicorr_dtype_t dt) {
   const long long warps = (long long)BS_CTAS * (BS_THREADS / 32) * num_sms();
   c.per_warp = (int)((total + warps - 1) / warps);
   if (c.per_warp < 1) c.per_warp = 1;
-  c.slots = (c.chunks + c.per_warp - 1) / c.per_warp + 1;
   return c;
 }
 
-// A row's sum of exponentials over some chunks: (s + c) 2^e, c what the additions lost, e a whole
-// number (-inf: nothing but -inf was met, s 0, or NaN). A whole power of two as the reference makes
-// every rescale exact.
-struct __align__(16) SumRec {
-  float s, c, e, pad;
-};
-
-// 2^d of a whole number d <= 0 (0 below the normal range and for -inf)
-__device__ __forceinline__ float pow2_whole(float d) {
-  return d < -126.f ? 0.f : __int_as_float((127 + (int)d) << 23);
-}
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -505,7 +506,7 @@ template <typename T>
 __global__ void __launch_bounds__(BS_THREADS, BS_CTAS)
 beam_stream_kernel(const T* __restrict__ logits, unsigned rows, const float* __restrict__ scores,
                    const uint8_t* __restrict__ done, const BeamCut cut, float* __restrict__ maxima,
-                   SumRec* __restrict__ sums) {
+                   float* __restrict__ sums) {
   pdl_wait();
   constexpr int N = Elem<T>::N;
   constexpr unsigned STAGE = BS_U * 32;
@@ -568,7 +569,6 @@ beam_stream_kernel(const T* __restrict__ logits, unsigned rows, const float* __r
   for (int i = 0; i < BS_STAGES - 1; ++i) copy(true);
 
   unsigned stage = 0;
-  float s = 0.f, lost = 0.f, e = -INFINITY;             // e is the same in all lanes
   for (unsigned i = begin; i < stop; ++i) {
     copy(false);
     asm volatile("cp.async.wait_group %0;" ::"n"(BS_STAGES - 1) : "memory");
@@ -583,16 +583,9 @@ beam_stream_kernel(const T* __restrict__ logits, unsigned rows, const float* __r
         load_chunk<T>(logits + (size_t)row * cut.V, b, en, lane, raw);
       }
       const float m = unord32(__reduce_max_sync(FULL, ord32(Elem<T>::vmax(raw))));
-      if (lane == 0) maxima[i] = m;
-      const float ce = ceilf(m * LOG2E);
-      if (ce > e) {
-        const float f = e == -INFINITY ? 1.f : pow2_whole(e - ce);   // before: 0, or NaN
-        s *= f;
-        lost *= f;
-        e = ce;
-      }
-      // terms 2^(x LOG2E - e); -inf adds 0, NaN stays
-      const float ref = e == -INFINITY ? 0.f : e;
+      // terms exp(x - m): -inf adds 0 (in a chunk of nothing else too), NaN stays. The difference first, which
+      // is exact for what counts, whatever the size of m.
+      const float ref = m == -INFINITY ? 0.f : m;
       float p0 = 0.f, p1 = 0.f, p2 = 0.f, p3 = 0.f;
 #pragma unroll
       for (int u = 0; u < BS_U; ++u)
@@ -600,29 +593,18 @@ beam_stream_kernel(const T* __restrict__ logits, unsigned rows, const float* __r
         for (int k = 0; k < N / 2; ++k) {
           float x0, x1;
           Elem<T>::pair(raw[u], k, x0, x1);
-          x0 = ex2(fmaf(x0, LOG2E, -ref));
-          x1 = ex2(fmaf(x1, LOG2E, -ref));
+          x0 = ex2((x0 - ref) * LOG2E);
+          x1 = ex2((x1 - ref) * LOG2E);
           if (k & 1) { p2 += x0; p3 += x1; } else { p0 += x0; p1 += x1; }
         }
-      // LOG2E is log2(e) to 2^-26, so a term wants (1 + x LOG2E_REST) more; x of the terms that count is
-      // the chunk's largest or a few below it, and 1e-8 times those few is what this leaves
-      const float part = (p0 + p1) + (p2 + p3);
-      // (a chunk of -inf alone, behind others or before them, adds 0)
-      add_pair(s, lost, part, m == -INFINITY ? 0.f : part * (m * LOG2E_REST));
+      const float sum = warp_sum((p0 + p1) + (p2 + p3));
+      if (lane == 0) {
+        maxima[i] = m;
+        sums[i] = sum;
+      }
     }
     stage = stage + 1 == BS_STAGES ? 0 : stage + 1;
-    if (++c == chunks || i + 1 == stop) {               // the warp's last chunk of this row
-      if (here.live) {
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1)
-          add_pair(s, lost, __shfl_xor_sync(FULL, s, o), __shfl_xor_sync(FULL, lost, o));
-        if (lane == 0)
-          *reinterpret_cast<float4*>(sums + (size_t)row * cut.slots +
-                                     (wid - row * chunks / (unsigned)cut.per_warp)) =
-              make_float4(s, lost, e, 0.f);
-      }
-      s = lost = 0.f;
-      e = -INFINITY;
+    if (++c == chunks) {
       c = 0;
       if (i + 1 < stop) here = open(++row);
     }
@@ -673,7 +655,7 @@ __device__ __forceinline__ uint64_t chunk_first(const uint4 (&raw)[BS_U], uint64
   return above | equal;
 }
 
-constexpr int BC_MAX = 4, BC_REC = 4;          // maxima, records of a lane loaded together
+constexpr int BC_MAX = 4;                      // maxima of a lane loaded together
 
 __device__ __forceinline__ void load_maxima(const float* __restrict__ p, int c0, int chunks,
                                             float (&v)[BC_MAX]) {
@@ -687,13 +669,13 @@ template <typename T>
 __global__ void __launch_bounds__(BC_THREADS)
 beam_choose_kernel(const T* __restrict__ logits, int W, const float* __restrict__ scores,
                    const uint8_t* __restrict__ done, BeamCut cut, const float* __restrict__ maxima,
-                   const SumRec* __restrict__ sums, BeamOut out, uint32_t* status) {
+                   const float* __restrict__ sums, BeamOut out, uint32_t* status) {
   pdl_wait();
   constexpr int N = Elem<T>::N;
   constexpr int NW = BC_THREADS / 32;
   constexpr int CAND = LILICORR_MAX_K * LILICORR_MAX_K;
-  __shared__ float2 s_base[LILICORR_MAX_BEAMS];         // score - normaliser, as a pair
-  __shared__ float2 s_norm[LILICORR_MAX_BEAMS];         // the normaliser, as a pair (+inf: none)
+  __shared__ Base s_base[LILICORR_MAX_BEAMS];           // (score - log S, as a pair; M)
+  __shared__ float2 s_norm[LILICORR_MAX_BEAMS];         // log S, as a pair (+inf: none)
   __shared__ uint8_t s_kind[LILICORR_MAX_BEAMS];        // 0 absent, 1 live, 2 done
   // a lane's largest chunk maximum of a row and where it is, while chunks are chosen; the candidates
   // after that
@@ -713,54 +695,44 @@ beam_choose_kernel(const T* __restrict__ logits, int W, const float* __restrict_
   const float* mx = maxima + row0 * cut.chunks;
   if (tid == 0) s_cand = 0;
 
-  // a warp a row: its normaliser from the records, and each lane's best chunk
+  // a warp a row: its normaliser from the chunks' sums, and each lane's best chunk
   for (int w = warp; w < W; w += NW) {
     const size_t row = row0 + w;
     // every load at once: what a row that is not live left there is not used
     const float sc = scores[row];
     const bool over = done && done[row];
-    const unsigned g0 = (unsigned)row * (unsigned)cut.chunks, first = g0 / (unsigned)cut.per_warp;
-    const int count = (int)((g0 + (unsigned)cut.chunks - 1) / (unsigned)cut.per_warp - first) + 1;
-    const float4* rec = reinterpret_cast<const float4*>(sums + row * cut.slots);
-    float4 x[BC_REC];
+    const float* rm = mx + (size_t)w * cut.chunks;
+    const float* rs = sums + row * cut.chunks;
+    float v[BC_MAX], part[BC_MAX];
+    load_maxima(rm, lane, cut.chunks, v);
 #pragma unroll
-    for (int u = 0; u < BC_REC; ++u)
-      x[u] = lane + 32 * u < count ? rec[lane + 32 * u] : make_float4(0.f, 0.f, -INFINITY, 0.f);
+    for (int u = 0; u < BC_MAX; ++u) part[u] = lane + 32 * u < cut.chunks ? rs[lane + 32 * u] : 0.f;
     float best = -INFINITY;
     int at = 0;
-    float2 norm = make_float2(INFINITY, 0.f);
-    for (int c0 = lane; c0 < cut.chunks; c0 += 32 * BC_MAX) {
-      float v[BC_MAX];
-      load_maxima(mx + (size_t)w * cut.chunks, c0, cut.chunks, v);
 #pragma unroll
-      for (int u = 0; u < BC_MAX; ++u)
-        if (v[u] > best) { best = v[u]; at = c0 + 32 * u; }
-    }
+    for (int u = 0; u < BC_MAX; ++u)
+      if (v[u] > best) { best = v[u]; at = lane + 32 * u; }
+    for (int c = lane + 32 * BC_MAX; c < cut.chunks; c += 32)
+      if (rm[c] > best) { best = rm[c]; at = c; }
+    float2 norm = make_float2(INFINITY, 0.f);
+    float top = 0.f;
     int kind = !(sc > -INFINITY) ? 0 : over ? 2 : 1;
     bool bad = sc != sc || sc == INFINITY;
     if (kind == 1) {
-      float e = x[0].z, s = x[0].x, c = x[0].y;
-      auto add = [&](const float4& y) {
-        const float big = fmaxf(e, y.z);
-        const float f = e == -INFINITY ? 1.f : pow2_whole(e - big);
-        const float g = y.z == -INFINITY ? 1.f : pow2_whole(y.z - big);
-        s *= f;
-        c *= f;
-        add_pair(s, c, y.x * g, y.y * g);
-        e = big;
-      };
+      // S in an order of its own: whatever warps met the chunks, the same bits
+      top = warp_max(best);
+      float s = 0.f, c = 0.f;
 #pragma unroll
-      for (int u = 1; u < BC_REC; ++u)
-        if (32 * u < count) add(x[u]);
-      for (int i = lane + 32 * BC_REC; i < count; i += 32) add(rec[i]);
-      const float E = warp_max(e), f = e == -INFINITY ? 1.f : pow2_whole(e - E);
-      s *= f;
-      c *= f;
+      for (int u = 0; u < BC_MAX; ++u) add_pair(s, c, part[u] * ex2((v[u] - top) * LOG2E), 0.f);
+      for (int i = lane + 32 * BC_MAX; i < cut.chunks; i += 32)
+        add_pair(s, c, rs[i] * ex2((rm[i] - top) * LOG2E), 0.f);
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1)
         add_pair(s, c, __shfl_xor_sync(FULL, s, o), __shfl_xor_sync(FULL, c, o));
-      if (!(s > 0.f && s < INFINITY && E > -INFINITY && E < INFINITY)) bad = true;
-      log_pair(s, c, E, norm.x, norm.y);
+      // (no finite logit: NaN, as from one)
+      if (!(s >= 1.f && s < INFINITY)) bad = true;
+      log_pair(s, c, norm.x, norm.y);
+      if (norm.x < 0.f) norm = make_float2(0.f, 0.f);     // (a rounding of the sum's second half)
     } else {
       best = kind == 2 && lane == 0 ? 0.f : -INFINITY;  // the one candidate of a beam that is done
       at = 0;
@@ -772,7 +744,7 @@ beam_choose_kernel(const T* __restrict__ logits, int W, const float* __restrict_
     if (lane == 0) {
       if (bad) set_status(status, LILICORR_ERR_NONFINITE);
       s_norm[w] = kind == 1 ? norm : make_float2(INFINITY, 0.f);
-      s_base[w] = make_float2(sc, 0.f);
+      s_base[w] = Base{sc, 0.f, top};
       s_kind[w] = (uint8_t)kind;
     }
   }
@@ -785,23 +757,26 @@ beam_choose_kernel(const T* __restrict__ logits, int W, const float* __restrict_
   uint64_t best_key = 0ull, best_pos = ~0ull;
   for (int w = warp; w < W; w += NW) {
     const float best = s_lane[w][lane];
-    float hi = s_base[w].x, lo = 0.f;
+    Base base = s_base[w];
     if (s_kind[w] == 1) {
       float2 norm = s_norm[w];
       for (int w0 = 0; w0 < w; w0 += 32) {
         const int v = w0 + lane;
         const float2 x = v < w ? s_norm[v] : make_float2(INFINITY, 0.f);
-        const unsigned same = __ballot_sync(FULL, fabsf((x.x - norm.x) + (x.y - norm.y)) <= 0x1p-22f);
+        const unsigned same = __ballot_sync(
+            FULL, v < w && s_base[v].top == base.top && fabsf((x.x - norm.x) + (x.y - norm.y)) <= 0x1p-22f);
         if (same) {
           norm = s_norm[w0 + __ffs(same) - 1];
           break;
         }
       }
-      add_pair(hi, lo, -norm.x, -norm.y);
+      add_pair(base.hi, base.lo, -norm.x, -norm.y);
     }
-    __syncwarp();
-    if (lane == 0) s_base[w] = make_float2(hi, lo);
-    const uint64_t key = best == -INFINITY ? 0ull : sum_key(hi, lo, best);
+    if (lane == 0) {                                     // (others read its top meanwhile, which stays)
+      s_base[w].hi = base.hi;
+      s_base[w].lo = base.lo;
+    }
+    const uint64_t key = best == -INFINITY ? 0ull : sum_key(base, best);
     const uint64_t pos = ((uint64_t)w << 32) | (uint32_t)s_lane_at[w][lane];
     if (precedes(key, pos, best_key, best_pos)) { best_key = key; best_pos = pos; }
   }
@@ -813,8 +788,7 @@ beam_choose_kernel(const T* __restrict__ logits, int W, const float* __restrict_
   for (int w = warp; w < W; w += NW) {
     const float v = s_lane[w][lane];
     if (v == -INFINITY) continue;
-    const float2 base = s_base[w];
-    rank_keep(sh, sum_key(base.x, base.y, v), ((uint64_t)w << 32) | (uint32_t)s_lane_at[w][lane]);
+    rank_keep(sh, sum_key(s_base[w], v), ((uint64_t)w << 32) | (uint32_t)s_lane_at[w][lane]);
   }
   __syncthreads();
   uint64_t nth = 0ull, nth_pos = 0ull;
@@ -827,16 +801,13 @@ beam_choose_kernel(const T* __restrict__ logits, int W, const float* __restrict_
   __syncthreads();
   const uint64_t bound = sh.bound;
   for (int w = warp; w < W; w += NW) {
-    const float2 base = s_base[w];
+    const Base base = s_base[w];
     const float v = s_lane[w][lane];
-    // by the logit first, with a margin for the rounding
-    const float need = key_score(bound);
-    const float thr = bound == 1ull ? -INFINITY
-                                    : (need - base.x) - 0x1p-20f * (fabsf(need) + fabsf(base.x));
+    const float thr = bound == 1ull ? -INFINITY : logit_floor(base, key_score(bound));
     if (v == -INFINITY || v < thr) continue;             // nor any other of the lane's
     const uint64_t pos = (uint64_t)w << 32;
     if (s_kind[w] == 2) {
-      rank_keep(sh, sum_key(base.x, base.y, 0.f), pos);
+      rank_keep(sh, sum_key(base, 0.f), pos);
       continue;
     }
     for (int c0 = lane; c0 < cut.chunks; c0 += 32 * BC_MAX) {
@@ -845,7 +816,7 @@ beam_choose_kernel(const T* __restrict__ logits, int W, const float* __restrict_
 #pragma unroll
       for (int u = 0; u < BC_MAX; ++u) {
         if (x[u] >= thr && x[u] > -INFINITY)
-          rank_keep(sh, sum_key(base.x, base.y, x[u]), pos | (uint32_t)(c0 + 32 * u));
+          rank_keep(sh, sum_key(base, x[u]), pos | (uint32_t)(c0 + 32 * u));
       }
     }
   }
@@ -862,7 +833,7 @@ beam_choose_kernel(const T* __restrict__ logits, int W, const float* __restrict_
           const int w = i / cut.chunks;
           if (s_kind[w] == 0 || (s_kind[w] == 2 && i != w * cut.chunks)) return 0ull;
           const float x = s_kind[w] == 2 ? 0.f : mx[i];
-          return x > -INFINITY ? sum_key(s_base[w].x, s_base[w].y, x) : 0ull;
+          return x > -INFINITY ? sum_key(s_base[w], x) : 0ull;
         },
         [&](int i) { return ((uint64_t)(i / cut.chunks) << 32) | (uint32_t)(i % cut.chunks); }, take);
     taken = out.n;
@@ -900,8 +871,7 @@ beam_choose_kernel(const T* __restrict__ logits, int W, const float* __restrict_
       const int c = warp + i * NW;
       const float top = Elem<T>::vmax(raw[i]);
       if (top == -INFINITY) continue;
-      const float2 base = s_base[(int)(s_cpos[c] >> 32)];
-      const uint64_t key = sum_key(base.x, base.y, top), pos = (uint64_t)(c * 32 + lane);
+      const uint64_t key = sum_key(s_base[(int)(s_cpos[c] >> 32)], top), pos = (uint64_t)(c * 32 + lane);
       if (precedes(key, pos, best_key, best_pos)) { best_key = key; best_pos = pos; }
     }
     rank_bound<BC_THREADS>(sh, out.n, best_key, best_pos);
@@ -921,11 +891,9 @@ beam_choose_kernel(const T* __restrict__ logits, int W, const float* __restrict_
       continue;
     }
     const T* rp = logits + (row0 + w) * cut.V;
-    const float2 base = s_base[w];
-    // elements whose total may reach `least`: by the logit, with a margin for the rounding
-    const float need = key_score(least);
-    const float thr = least == 1ull ? -INFINITY
-                                    : (need - base.x) - 0x1p-20f * (fabsf(need) + fabsf(base.x));
+    const Base base = s_base[w];
+    // elements whose total may reach `least`
+    const float thr = least == 1ull ? -INFINITY : logit_floor(base, key_score(least));
     uint64_t hot = 0;                                   // element j of vector u: bit u * N + j
 #pragma unroll
     for (int u = 0; u < BS_U; ++u) {
@@ -941,7 +909,7 @@ beam_choose_kernel(const T* __restrict__ logits, int W, const float* __restrict_
     if (__reduce_add_sync(FULL, __popcll(hot)) > out.n) hot = chunk_first<T>(raw[i], hot, out.n, lane);
     for (uint64_t h = hot; h; h &= h - 1) {
       const int j = __ffsll((long long)h) - 1, id = from[i] + ((j / N) * 32 + lane) * N + j % N;
-      const uint64_t key = sum_key(base.x, base.y, Elem<T>::value(rp[id]));
+      const uint64_t key = sum_key(base, Elem<T>::value(rp[id]));
       if (key < least) continue;
       const int at = atomicAdd(&s_cand, 1);
       s_key[at] = key;
@@ -1045,7 +1013,7 @@ lilicorr_status_t launch_reorder(const Reorder& a, int count, int requests, cuda
 size_t select_ws_bytes(int rows, int V, lilicorr_dtype_t dt) {
   const BeamCut c = beam_cut(rows, V, dt);
   return 256 + align_up((size_t)rows * c.chunks * sizeof(float), 256) +
-         align_up((size_t)rows * c.slots * sizeof(SumRec), 256);
+         align_up((size_t)rows * c.chunks * sizeof(float), 256);
 }
 
 template <typename T>
@@ -1056,7 +1024,7 @@ lilicorr_status_t run_select(const T* logits, lilicorr_dtype_t dt, int requests,
   const BeamCut cut = beam_cut(rows, V, dt);
   unsigned char* w = static_cast<unsigned char*>(ws);
   float* maxima = reinterpret_cast<float*>(w + 256);
-  SumRec* sums = reinterpret_cast<SumRec*>(
+  float* sums = reinterpret_cast<float*>(
       w + 256 + align_up((size_t)rows * cut.chunks * sizeof(float), 256));
   const long long warps = ((long long)rows * cut.chunks + cut.per_warp - 1) / cut.per_warp;
   static bool configured[64] = {false};

@@ -1,0 +1,128 @@
+"""The normaliser of beam_select: rows of logits of any size, rows that one token dominates.
+
+logp = (x - M) - log S, S the sum of exp(x - M) over the row, M its largest logit. Each term of S is off by at most
+2^-22 of itself (ex2.approx), the constant log2(e) by 2^-26 of the argument, and the argument's rounding by
+half a step: 2^-20 up to 32 log2 units. Terms weigh e^-t at t nats, and at most 2^18 of them lie there, so what
+an error of the argument does to log S is largest near t = 11: 0.7 (2^-22 + 2^-21.5 + 2^-23) < 2^-20.6. The
+sums in fp32 (chains of 16 or fewer, then halves) add 2^-22.5: below 2^-20 in all. S is not below 1."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import workloads
+from test_gpu_beam import NINF, _ll, _plain, _run_select
+
+pytestmark = pytest.mark.gpu
+
+TOL = 2.0 ** -20
+
+
+def _want(x, scores, n, done=None, end_id=-1):
+    """As the definition, each row taken from its largest logit: differences in 64 bits lose nothing that
+    counts, whatever the logits' size."""
+    R, W, V = x.shape
+    K = min(n, V)
+    ids, total = np.zeros((R, W, K), np.int64), np.full((R, W, K), NINF)
+    for r in range(R):
+        for w in range(W):
+            if not scores[r, w] > NINF or (done is not None and done[r, w]):
+                continue
+            row = x[r, w].astype(np.float64)
+            ids[r, w] = np.lexsort((np.arange(V), -row))[:K]
+            row = row - row.max()
+            total[r, w] = np.float64(scores[r, w]) + (row[ids[r, w]] - math.log1p(np.sort(np.exp(row))[:-1].sum()))
+    total[total < -float(np.finfo(np.float32).max)] = NINF         # no total that fp32 holds
+    return _plain(ids, total, scores, n, done, end_id)
+
+
+def _check(got, want):
+    """Picks, and totals to the stated bound."""
+    tok, par, sc, over = (t.cpu().numpy() for t in got)
+    assert np.array_equal(tok, want[0]) and np.array_equal(par, want[1]) and np.array_equal(over, want[3])
+    fin = np.isfinite(want[2])
+    assert np.array_equal(np.isfinite(sc), fin)
+    err = np.abs(sc[fin] - want[2][fin]) - (TOL + 2.0 ** -24 * np.abs(want[2][fin]))
+    assert np.all(err <= 0), err.max()
+
+
+LOW = {"f32": float(np.finfo(np.float32).min), "bf16": float(torch.finfo(torch.bfloat16).min)}
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["lowest", "lowest_but_few", "highest", "highest_and_lowest", "1e9", "-1e9", "1e6",
+                                  "-3e4", "mixed"])
+@pytest.mark.parametrize("V", [37, 5001, 40000])
+def test_rows_of_finite_logits_of_any_size(kind, V, dtype):
+    """Masks of the type's lowest value over all of a row or most of it, logits near both ends of fp32's range, and
+    rows far from 0, next to an ordinary beam."""
+    ll = _ll()
+    rng = np.random.default_rng(V)
+    R, W, n = 3, 3, 4
+    x = np.round(rng.standard_normal((R, W, V)) * 64) / 64
+    x[:, :, V // 3] += 9.0                                     # ahead of its row
+    few = rng.permutation(V)[:5]
+    y = x[:, 1].copy()
+    low = LOW[dtype]
+    if kind == "lowest":
+        y[:] = low
+    elif kind == "lowest_but_few":
+        y[:] = low
+        y[:, few] = x[:, 1][:, few]
+    elif kind == "highest":
+        y[:, few[:3]] = [-low, -low, -low / 2]
+    elif kind == "highest_and_lowest":
+        y[:] = low
+        y[:, few[:2]] = -low
+    elif kind == "mixed":
+        y[:] = np.where(rng.uniform(size=y.shape) < 0.5, low, -1e9)
+        y[:, few] = [30.0, 29.0, 28.5, 2e4, 2e4]
+    else:
+        y += float(kind)
+    x[:, 1] = y
+    x = x.astype(np.float32)
+    if dtype == "bf16":
+        x = workloads.round_to_bf16(x)
+    assert np.isfinite(x).all()
+    scores = np.array([[-1.0, -0.5, -1.25]] * R, np.float32)
+    want = _want(x, scores, n)
+    t = want[2]                                                # (totals of two beams are apart, or the test says nothing)
+    assert all(want[1][r, j] == want[1][r, j + 1] or t[r, j] - t[r, j + 1] > 4 * TOL
+               for r in range(R) for j in range(n - 1))
+    ws = ll.Workspace(ll.beam_select_workspace_bytes(R, W, V, n))
+    _check(_run_select(ll, x, scores, n, dtype, ws=ws), want)
+    assert ws.status() == 0
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [2, 1000, 1003, 60000])
+def test_a_row_that_one_token_dominates(V, dtype):
+    """No total lies above its score, and each is the definition's to the stated bound."""
+    ll = _ll()
+    rng = np.random.default_rng(V)
+    R, W = 8, 60
+    x = rng.standard_normal((R, W, V)).astype(np.float32)
+    peak = np.linspace(3.0, 90.0, R * W).reshape(R, W) + rng.uniform(0, 0.2, (R, W))
+    at = rng.integers(0, V, (R, W))
+    for r in range(R):
+        for w in range(W):
+            x[r, w, at[r, w]] = peak[r, w]
+    if dtype == "bf16":
+        x = workloads.round_to_bf16(x)
+    scores = np.zeros((R, W), np.float32)
+    # a request a row, so that each one's own best is seen
+    flat = x.reshape(R * W, 1, V)
+    got = _run_select(ll, flat, scores.reshape(R * W, 1), 1, dtype)
+    tok, _, sc, _ = (t.cpu().numpy() for t in got)
+    assert np.all(sc <= 0.0), sc.max()
+    row = flat[:, 0].astype(np.float64)
+    m = row.max(1)
+    rest = np.exp(row - m[:, None])
+    exact = -np.log1p(np.sort(rest, axis=1)[:, :-1].sum(1))
+    assert np.array_equal(tok[:, 0], row.argmax(1))
+    assert np.all(np.abs(sc[:, 0] - exact) <= TOL + 2.0 ** -24 * np.abs(exact))
+    # and against scores of a few nats: never above them
+    sc7 = -rng.uniform(0, 7, (R * W, 1)).astype(np.float32)
+    out = _run_select(ll, flat, sc7, 1, dtype)[2].cpu().numpy()
+    assert np.all(out <= sc7)
