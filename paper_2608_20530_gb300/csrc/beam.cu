@@ -15,8 +15,11 @@
 // logits' size, x - M keeps what tells them apart. S is at least 1 (the largest logit's own term is 1 exactly),
 // so that no total lies above its score. Totals are sums of 48 bits of inputs that are not: ex2.approx is good
 // to 2^-22 and its argument of up to 17 log2 units, before a term that counts, to 2^-20, so that log S is good to
-// 2^-20 at worst, and to some 1e-8 where many unlike terms share the sum. Two normalisers of a request that
-// agree to 2^-22, their M the same, are taken as one, so that beams of one content tie.
+// 2^-20 at worst, and to some 1e-8 where many unlike terms share the sum.
+// Beams of one content tie: the sums have one order, and rows that are cut alike (V a multiple of a vector) the
+// same bits. Where rows start off their 16-byte boundaries their chunks differ, and with them the roundings;
+// there the pass also adds up the logits' bits as whole numbers, which no order changes, and rows of a request
+// with the same M, the same such sum and normalisers within 2^-19 (twice the above) take the lower beam's.
 #include <math.h>
 
 #include "internal.cuh"
@@ -392,6 +395,8 @@ template <> struct Elem<uint16_t> {
   __device__ static float value(uint16_t x) { return bf16_to_f32(x); }
   static constexpr uint32_t NONE = 0xFF80FF80u;
   static constexpr int BITS = 16;
+  __device__ static uint32_t mark(uint32_t w, uint32_t sum) { return __dp2a_lo(w, 0x0101u, sum); }   // + both halves
+  static constexpr uint32_t MARK_NONE = 0xFF80u;           // of one element that is not there
   // the value whose ord32 begins with these 16 bits, and how many of a lane's share reach it
   __device__ static float image(uint32_t code) { return unord32((code >> 31) ? code : code | 0xFFFFu); }
   __device__ static int at_least(const uint4 (&v)[BS_U], uint32_t code) {
@@ -444,6 +449,8 @@ template <> struct Elem<float> {
   __device__ static float value(float x) { return x; }
   static constexpr uint32_t NONE = 0xFF800000u;
   static constexpr int BITS = 32;
+  __device__ static uint32_t mark(uint32_t w, uint32_t sum) { return sum + w; }
+  static constexpr uint32_t MARK_NONE = NONE;
   __device__ static float image(uint32_t code) { return unord32(code); }
   __device__ static int at_least(const uint4 (&v)[BS_U], uint32_t code) {
     const float t = image(code);
@@ -502,11 +509,12 @@ __device__ __forceinline__ void load_chunk(const T* __restrict__ row, int begin,
 // Bound by HBM. A warp's chunks lie one after the other; each lane copies its own 128 bytes of a chunk
 // into its own part of a ring in shared memory, two chunks ahead, and reads back only what it copied:
 // 128 KB a SM in flight, no registers for it and no barrier.
-template <typename T>
+// ODD: as in the cut; the chunks' sums of bits go to `marks`.
+template <typename T, bool ODD>
 __global__ void __launch_bounds__(BS_THREADS, BS_CTAS)
 beam_stream_kernel(const T* __restrict__ logits, unsigned rows, const float* __restrict__ scores,
                    const uint8_t* __restrict__ done, const BeamCut cut, float* __restrict__ maxima,
-                   float* __restrict__ sums) {
+                   float* __restrict__ sums, uint32_t* __restrict__ marks) {
   pdl_wait();
   constexpr int N = Elem<T>::N;
   constexpr unsigned STAGE = BS_U * 32;
@@ -574,6 +582,7 @@ beam_stream_kernel(const T* __restrict__ logits, unsigned rows, const float* __r
     asm volatile("cp.async.wait_group %0;" ::"n"(BS_STAGES - 1) : "memory");
     if (here.live) {
       uint4 raw[BS_U];
+      int missing = 0;                                  // elements that a short chunk lacks
       if (c - here.first < here.count) {
 #pragma unroll
         for (int u = 0; u < BS_U; ++u) raw[u] = mine[stage * STAGE + u * 32];
@@ -581,6 +590,7 @@ beam_stream_kernel(const T* __restrict__ logits, unsigned rows, const float* __r
         int b, en;
         cut.range(row, (int)c, b, en);
         load_chunk<T>(logits + (size_t)row * cut.V, b, en, lane, raw);
+        missing = 32 * BS_U * N - (en - b);
       }
       const float m = unord32(__reduce_max_sync(FULL, ord32(Elem<T>::vmax(raw))));
       // terms exp(x - m): -inf adds 0 (in a chunk of nothing else too), NaN stays. The difference first, which
@@ -601,6 +611,14 @@ beam_stream_kernel(const T* __restrict__ logits, unsigned rows, const float* __r
       if (lane == 0) {
         maxima[i] = m;
         sums[i] = sum;
+      }
+      if constexpr (ODD) {
+        uint32_t mark = 0;
+#pragma unroll
+        for (int u = 0; u < BS_U; ++u)
+          mark = Elem<T>::mark(raw[u].w, Elem<T>::mark(raw[u].z, Elem<T>::mark(raw[u].y, Elem<T>::mark(raw[u].x, mark))));
+        mark = __reduce_add_sync(FULL, mark) - (uint32_t)missing * Elem<T>::MARK_NONE;
+        if (lane == 0) marks[i] = mark;
       }
     }
     stage = stage + 1 == BS_STAGES ? 0 : stage + 1;
@@ -669,13 +687,15 @@ template <typename T>
 __global__ void __launch_bounds__(BC_THREADS)
 beam_choose_kernel(const T* __restrict__ logits, int W, const float* __restrict__ scores,
                    const uint8_t* __restrict__ done, BeamCut cut, const float* __restrict__ maxima,
-                   const float* __restrict__ sums, BeamOut out, uint32_t* status) {
+                   const float* __restrict__ sums, const uint32_t* __restrict__ marks, BeamOut out,
+                   uint32_t* status) {
   pdl_wait();
   constexpr int N = Elem<T>::N;
   constexpr int NW = BC_THREADS / 32;
   constexpr int CAND = LILICORR_MAX_K * LILICORR_MAX_K;
   __shared__ Base s_base[LILICORR_MAX_BEAMS];           // (score - log S, as a pair; M)
   __shared__ float2 s_norm[LILICORR_MAX_BEAMS];         // log S, as a pair (+inf: none)
+  __shared__ uint32_t s_mark[LILICORR_MAX_BEAMS];       // the rows' sums of bits (odd cuts)
   __shared__ uint8_t s_kind[LILICORR_MAX_BEAMS];        // 0 absent, 1 live, 2 done
   // a lane's largest chunk maximum of a row and where it is, while chunks are chosen; the candidates
   // after that
@@ -707,6 +727,12 @@ beam_choose_kernel(const T* __restrict__ logits, int W, const float* __restrict_
     load_maxima(rm, lane, cut.chunks, v);
 #pragma unroll
     for (int u = 0; u < BC_MAX; ++u) part[u] = lane + 32 * u < cut.chunks ? rs[lane + 32 * u] : 0.f;
+    uint32_t mark = 0;
+    if (cut.odd) {
+#pragma unroll
+      for (int u = 0; u < BC_MAX; ++u)
+        if (lane + 32 * u < cut.chunks) mark += marks[row * cut.chunks + lane + 32 * u];
+    }
     float best = -INFINITY;
     int at = 0;
 #pragma unroll
@@ -731,6 +757,11 @@ beam_choose_kernel(const T* __restrict__ logits, int W, const float* __restrict_
         add_pair(s, c, __shfl_xor_sync(FULL, s, o), __shfl_xor_sync(FULL, c, o));
       // (no finite logit: NaN, as from one)
       if (!(s >= 1.f && s < INFINITY)) bad = true;
+      if (cut.odd) {
+        for (int i = lane + 32 * BC_MAX; i < cut.chunks; i += 32) mark += marks[row * cut.chunks + i];
+        mark = __reduce_add_sync(FULL, mark);
+        if (lane == 0) s_mark[w] = mark;
+      }
       log_pair(s, c, norm.x, norm.y);
       if (norm.x < 0.f) norm = make_float2(0.f, 0.f);     // (a rounding of the sum's second half)
     } else {
@@ -750,21 +781,20 @@ beam_choose_kernel(const T* __restrict__ logits, int W, const float* __restrict_
   }
   __syncthreads();
 
-  // Rows of one content, which differ in alignment or in where warps met them, have normalisers that differ by
-  // roundings (1e-8 mostly, 2^-23 where all logits are equal and so round alike); so that such beams tie,
-  // one that is within 2^-22 of a lower beam's takes that one's.
-  // Then each row's base, and of all its rows this thread's best.
+  // Rows of one content take one normaliser (see above). Then each row's base, and of all its rows this
+  // thread's best.
   uint64_t best_key = 0ull, best_pos = ~0ull;
   for (int w = warp; w < W; w += NW) {
     const float best = s_lane[w][lane];
     Base base = s_base[w];
     if (s_kind[w] == 1) {
       float2 norm = s_norm[w];
-      for (int w0 = 0; w0 < w; w0 += 32) {
+      for (int w0 = 0; cut.odd && w0 < w; w0 += 32) {
         const int v = w0 + lane;
-        const float2 x = v < w ? s_norm[v] : make_float2(INFINITY, 0.f);
+        const float2 x = v < w ? s_norm[v] : make_float2(INFINITY, 0.f);       // (+inf: not live)
         const unsigned same = __ballot_sync(
-            FULL, v < w && s_base[v].top == base.top && fabsf((x.x - norm.x) + (x.y - norm.y)) <= 0x1p-22f);
+            FULL, fabsf((x.x - norm.x) + (x.y - norm.y)) <= 0x1p-19f && s_base[v].top == base.top &&
+                      s_mark[v] == s_mark[w]);
         if (same) {
           norm = s_norm[w0 + __ffs(same) - 1];
           break;
@@ -1012,8 +1042,20 @@ lilicorr_status_t launch_reorder(const Reorder& a, int count, int requests, cuda
 
 size_t select_ws_bytes(int rows, int V, lilicorr_dtype_t dt) {
   const BeamCut c = beam_cut(rows, V, dt);
-  return 256 + align_up((size_t)rows * c.chunks * sizeof(float), 256) +
-         align_up((size_t)rows * c.chunks * sizeof(float), 256);
+  return 256 + (c.odd ? 3 : 2) * align_up((size_t)rows * c.chunks * sizeof(float), 256);
+}
+
+template <typename T, bool ODD>
+lilicorr_status_t launch_stream(const T* logits, int rows, const float* scores, const uint8_t* done,
+                                const BeamCut& cut, float* maxima, float* sums, uint32_t* marks,
+                                cudaStream_t st) {
+  const long long warps = ((long long)rows * cut.chunks + cut.per_warp - 1) / cut.per_warp;
+  static bool configured[64] = {false};
+  auto* kernel = beam_stream_kernel<T, ODD>;
+  LL_TRY(allow_max_dynamic_smem(kernel, configured));
+  return launch_k(kernel, ceil_div(warps, BS_THREADS / 32), BS_THREADS,
+                  (size_t)BS_THREADS * BS_STAGES * BS_U * sizeof(uint4), st, logits, (unsigned)rows,
+                  scores, done, cut, maxima, sums, marks);
 }
 
 template <typename T>
@@ -1023,17 +1065,14 @@ lilicorr_status_t run_select(const T* logits, lilicorr_dtype_t dt, int requests,
   const int rows = requests * W;
   const BeamCut cut = beam_cut(rows, V, dt);
   unsigned char* w = static_cast<unsigned char*>(ws);
+  const size_t each = align_up((size_t)rows * cut.chunks * sizeof(float), 256);
   float* maxima = reinterpret_cast<float*>(w + 256);
-  float* sums = reinterpret_cast<float*>(
-      w + 256 + align_up((size_t)rows * cut.chunks * sizeof(float), 256));
-  const long long warps = ((long long)rows * cut.chunks + cut.per_warp - 1) / cut.per_warp;
-  static bool configured[64] = {false};
-  LL_TRY(allow_max_dynamic_smem(beam_stream_kernel<T>, configured));
-  LL_TRY(launch_k(beam_stream_kernel<T>, ceil_div(warps, BS_THREADS / 32), BS_THREADS,
-                  (size_t)BS_THREADS * BS_STAGES * BS_U * sizeof(uint4), st, logits, (unsigned)rows,
-                  scores, done, cut, maxima, sums));
+  float* sums = reinterpret_cast<float*>(w + 256 + each);
+  uint32_t* marks = cut.odd ? reinterpret_cast<uint32_t*>(w + 256 + 2 * each) : nullptr;
+  if (cut.odd) LL_TRY((launch_stream<T, true>(logits, rows, scores, done, cut, maxima, sums, marks, st)));
+  else LL_TRY((launch_stream<T, false>(logits, rows, scores, done, cut, maxima, sums, marks, st)));
   return launch_k(beam_choose_kernel<T>, requests, BC_THREADS, 0, st, logits, W, scores, done, cut,
-                  maxima, sums, out, reinterpret_cast<uint32_t*>(w));
+                  maxima, sums, marks, out, reinterpret_cast<uint32_t*>(w));
 }
 
 // The checks of one layout but for overlaps, and how its arrays are moved: all of `a` but the arrays, parents

@@ -126,3 +126,48 @@ def test_a_row_that_one_token_dominates(V, dtype):
     sc7 = -rng.uniform(0, 7, (R * W, 1)).astype(np.float32)
     out = _run_select(ll, flat, sc7, 1, dtype)[2].cpu().numpy()
     assert np.all(out <= sc7)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [4096, 4097, 3 * 4096 + 5])
+def test_unlike_beams_keep_their_totals_apart(V, dtype):
+    """Rows of zeros, each with one logit a little lower, by 2^-10 more in every beam: log S falls by 2^-10 / V a
+    beam, 2.4e-7 at most, which fp32's totals do not show. Terms of 1 are exact; with the one other, halves of
+    half steps of sums of up to 2,048, below 2^-13 in all, are 1/8 of a gap. The likeliest beam's zeros come first."""
+    ll = _ll()
+    W, n = 8, 24
+    x = np.zeros((2, W, V), np.float32)
+    order = [list(range(W)), [3, 6, 1, 7, 0, 5, 2, 4]]         # how much lower each beam's logit is
+    for r in range(2):
+        for w in range(W):
+            x[r, w, 17 * w + 3] = -(2.0 ** -10) * order[r][w]
+    assert np.array_equal(workloads.round_to_bf16(x), x)
+    scores = np.full((2, W), -2.0, np.float32)
+    want = _want(x, scores, n)
+    assert want[1].tolist() == [[W - 1] * n, [3] * n]
+    _check(_run_select(ll, x, scores, n, dtype), want)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("R,W,V", [(3, 16, 2049), (2, 9, 40001), (5, 8, 8192), (1, 64, 1003)])
+@pytest.mark.parametrize("kind", ["level", "far"])
+def test_beams_of_one_content_tie_with_banned_tokens(kind, R, W, V, dtype):
+    """The same logits at every alignment, of one value behind a peak (all roundings alike) or of many, some
+    banned, some beams absent: the lower beam goes first throughout."""
+    ll = _ll()
+    rng = np.random.default_rng(V)
+    row = np.full((R, 1, V), -9.7) if kind == "level" else rng.standard_normal((R, 1, V)) * 3 - 1e4
+    row[:, 0, V // 3] = row.max() + 10.4
+    row[:, 0, V // 2:V // 2 + V // 8] = NINF
+    x = np.repeat(row.astype(np.float32), W, axis=1)
+    if dtype == "bf16":
+        x = workloads.round_to_bf16(x)
+    scores = np.full((R, W), -0.75, np.float32)
+    scores[:, 1] = NINF
+    n = min(32, W - 1)
+    tok, par, sc, _ = (t.cpu().numpy() for t in _run_select(ll, x, scores, n, dtype))
+    for r in range(R):
+        ids = np.argsort(-x[r, 0], kind="stable")[:n]              # (bf16 near -1e4: most logits are equal)
+        first = sorted((-x[r, w, v], w, v) for w in range(W) if w != 1 for v in ids)[:n]
+        assert par[r].tolist() == [c[1] for c in first] and tok[r].tolist() == [c[2] for c in first]
+        assert all(sc[r, j] == sc[r, j - 1] for j in range(1, n) if first[j][0] == first[j - 1][0])
