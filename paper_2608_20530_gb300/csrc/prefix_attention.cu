@@ -782,14 +782,14 @@ pa_simt_kernel(const PaArgs a, const PaKeys kk, int rows, int blocks) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       s[i] += odd[i];
-      // (the exponent's argument rounds once, and the scale's own rounding is made good: scores of 20 would
-      // leave 1e-6 of a term otherwise)
+      // (the product with the scale is exact beside u, and what the scale's own rounding left is added to that
+      // small difference, where it counts: scores of 20 would leave 1e-6 of a term otherwise)
       const bool seen = key < lim[i];
       const float n = fmaxf(m[i], warp_max(seen ? s[i] * a.scale_log2 : -INFINITY));
       const float u = n == -INFINITY ? 0.f : n;
       const float f = pa_ex2(m[i] - u);
       m[i] = n;
-      s[i] = seen ? pa_ex2(fmaf(s[i], a.scale_log2, fmaf(s[i], a.scale_rest, -u))) : 0.f;
+      s[i] = seen ? pa_ex2(fmaf(s[i], a.scale_rest, fmaf(s[i], a.scale_log2, -u))) : 0.f;
       l[i] = l[i] * f + s[i];                     // this lane's share of the sum
       o[i].x *= f; o[i].y *= f; o[i].z *= f; o[i].w *= f;
     }
