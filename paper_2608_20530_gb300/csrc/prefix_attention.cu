@@ -81,125 +81,96 @@ __device__ __forceinline__ void stage_rows(unsigned char* dst, const unsigned ch
   }
 }
 
-// R rows' results, by one warp, four columns a lane: the prefix's segments and the slots joined with
-// (m, l, o) that the warp has already (m -inf: nothing), to out and lse. Several rows at a time, so that
-// their loads are under way together; `count` of them are there.
-template <typename T, int R>
-__device__ __forceinline__ void join_rows(const PaArgs& a, const PaRow (&w)[R], int count, float (&m)[R],
-                                          float (&l)[R], float4 (&o)[R], int lane) {
-  const size_t rows = a.rows();
-  size_t row[R], seg0[R];
-  int segs[R], step[R], most = 0;
-  const uint32_t hb = (uint32_t)a.Hkv * a.seg_blocks;
-  const uint32_t per = a.seg_ctas ? pa_per_cta(a.seg_start[a.G] * hb, a.seg_ctas) : 1u;
-#pragma unroll
-  for (int i = 0; i < R; ++i) {
-    row[i] = pa_index(a, w[i]);
-    segs[i] = 0;
-    step[i] = PA_BLOCK;
-    seg0[i] = 0;
-    if (i >= count) continue;
-    if (a.seg_ctas) {
-      const int g = w[i].n / a.W, hk = w[i].h / a.rep;
-      const int r = ((w[i].n - g * a.W) * a.T + w[i].t) * a.rep + (w[i].h - hk * a.rep);
-      const uint32_t before = a.seg_start[g], tiles = a.seg_start[g + 1] - before;
-      if (tiles) {
-        const uint32_t in = (uint32_t)hk * a.seg_blocks + r / PA_BLOCK;
-        const uint32_t first = before * hb + in * tiles;
-        const uint32_t c0 = first / per, c1 = (first + tiles - 1) / per;
-        // in halves of a block: one a segment where the block has two row tiles, else two pieces a segment
-        const bool two = a.seg_rows - r / PA_BLOCK * PA_BLOCK > 128;
-        step[i] = two ? PA_BLOCK : PA_BLOCK / 2;
-        segs[i] = ((int)(c1 - c0) + 1) * (two ? 1 : 2);
-        seg0[i] = ((size_t)c0 + (size_t)g * hb + in) * PA_BLOCK + r % PA_BLOCK;
-      }
-    }
-    most = max(most, segs[i] + a.slots);
+// A row's result from its maximum, its sum and its sums of V, four columns a lane, to out and lse.
+template <typename T>
+__device__ __forceinline__ void write_row(const PaArgs& a, const PaRow& w, float m, float l, const float4& o,
+                                          int lane) {
+  const float inv = l > 0.f ? 1.0f / l : (m == -INFINITY ? 0.f : l);       // (NaN stays)
+  T* out = static_cast<T*>(a.out) + (int64_t)w.n * a.o_s[0] + (int64_t)w.t * a.o_s[1] +
+           (int64_t)w.h * a.o_s[2];
+  if (lane * 4 < a.d) {
+    const float4 y = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+    if constexpr (sizeof(T) == 4)
+      *reinterpret_cast<float4*>(out + lane * 4) = y;
+    else
+      *reinterpret_cast<uint2*>(out + lane * 4) = make_uint2(bf16_pack2(y.x, y.y), bf16_pack2(y.z, y.w));
   }
-  constexpr int U = R >= 4 ? 2 : 4;                  // pieces of a row on their way together
-  for (int s0 = 0; s0 < most; s0 += 32) {
-    float f[R];
-    unsigned there[R];
-    float2 ml[R];
-#pragma unroll
-    for (int i = 0; i < R; ++i) {
-      const int s = s0 + lane;
-      ml[i] = make_float2(-INFINITY, 0.f);
-      if (i < count && s < segs[i] + a.slots)
-        ml[i] = s < segs[i] ? a.seg_ml[seg0[i] + (size_t)s * step[i]]
-                            : a.ml[(size_t)(s - segs[i]) * rows + row[i]];
-    }
-#pragma unroll
-    for (int i = 0; i < R; ++i) {
-      const float M = fmaxf(m[i], warp_max(ml[i].x)), u = M == -INFINITY ? 0.f : M;
-      const float keep = pa_ex2(m[i] - u);
-      f[i] = ml[i].x == -INFINITY ? 0.f : pa_ex2(ml[i].x - u);
-      m[i] = M;
-      l[i] = l[i] * keep + warp_sum(f[i] * ml[i].y);
-      o[i].x *= keep; o[i].y *= keep; o[i].z *= keep; o[i].w *= keep;
-      there[i] = __ballot_sync(0xffffffffu, ml[i].x != -INFINITY);       // others wrote no sums
-    }
-    const int n = min(32, most - s0);
-    for (int j0 = 0; j0 < n; j0 += U) {
-      float4 p[R][U];
-#pragma unroll
-      for (int i = 0; i < R; ++i)
-#pragma unroll
-        for (int v = 0; v < U; ++v) {
-          const int s = s0 + j0 + v;
-          p[i][v] = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (j0 + v < n && (there[i] >> (j0 + v) & 1u) && lane * 4 < a.d)
-            p[i][v] = *reinterpret_cast<const float4*>(
-                (s < segs[i] ? a.seg_po + (seg0[i] + (size_t)s * step[i]) * a.d
-                             : a.po + ((size_t)(s - segs[i]) * rows + row[i]) * a.d) + lane * 4);
-        }
-#pragma unroll
-      for (int i = 0; i < R; ++i)
-#pragma unroll
-        for (int v = 0; v < U; ++v) {
-          const float x = __shfl_sync(0xffffffffu, f[i], (j0 + v) & 31);     // (0 with p: nothing there)
-          o[i].x = fmaf(x, p[i][v].x, o[i].x);
-          o[i].y = fmaf(x, p[i][v].y, o[i].y);
-          o[i].z = fmaf(x, p[i][v].z, o[i].z);
-          o[i].w = fmaf(x, p[i][v].w, o[i].w);
-        }
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < R; ++i) {
-    if (i >= count) continue;
-    const float inv = l[i] > 0.f ? 1.0f / l[i] : (m[i] == -INFINITY ? 0.f : l[i]);       // (NaN stays)
-    T* out = static_cast<T*>(a.out) + (int64_t)w[i].n * a.o_s[0] + (int64_t)w[i].t * a.o_s[1] +
-             (int64_t)w[i].h * a.o_s[2];
-    if (lane * 4 < a.d) {
-      const float4 y = make_float4(o[i].x * inv, o[i].y * inv, o[i].z * inv, o[i].w * inv);
-      if constexpr (sizeof(T) == 4)
-        *reinterpret_cast<float4*>(out + lane * 4) = y;
-      else
-        *reinterpret_cast<uint2*>(out + lane * 4) = make_uint2(bf16_pack2(y.x, y.y), bf16_pack2(y.z, y.w));
-    }
-    if (lane == 0)
-      a.lse[row[i]] = m[i] == -INFINITY ? -INFINITY
-                                        : fmaf(m[i], LN2, fmaf(m[i], LN2_REST, logf(l[i])));
-  }
+  if (lane == 0)
+    a.lse[pa_index(a, w)] = m == -INFINITY ? -INFINITY : fmaf(m, LN2, fmaf(m, LN2_REST, logf(l)));
 }
 
-// Join the rows' pieces where no kernel of the own keys does: one warp a row.
+// Join the rows' pieces, the prefix's segments and the slots, where no kernel of the own keys writes the result:
+// one warp a row, the sums of four pieces on their way together.
 template <typename T>
-__global__ void __launch_bounds__(128)
+__global__ void __launch_bounds__(128, 8)
 pa_combine_kernel(const PaArgs a) {
   pdl_wait();
-  const size_t row = (size_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-  if (row >= a.rows()) return;
-  PaRow w[1];
-  w[0].h = (int)(row % a.Hq);
+  const size_t rows = a.rows(), row = (size_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  if (row >= rows) return;
+  PaRow w;
+  w.h = (int)(row % a.Hq);
   const size_t nt = row / a.Hq;
-  w[0].t = (int)(nt % a.T);
-  w[0].n = (int)(nt / a.T);
-  if (a.seq_len[w[0].n] < 0) return;                // no such sequence: its rows stay as they are
-  float m[1] = {-INFINITY}, l[1] = {0.f};
-  float4 o[1] = {make_float4(0.f, 0.f, 0.f, 0.f)};
-  join_rows<T, 1>(a, w, 1, m, l, o, threadIdx.x & 31);
+  w.t = (int)(nt % a.T);
+  w.n = (int)(nt / a.T);
+  if (a.seq_len[w.n] < 0) return;                   // no such sequence: its rows stay as they are
+  int segs = 0, step = PA_BLOCK;
+  size_t seg0 = 0;
+  if (a.seg_ctas) {
+    const uint32_t hb = (uint32_t)a.Hkv * a.seg_blocks;
+    const uint32_t per = pa_per_cta(a.seg_start[a.G] * hb, a.seg_ctas);
+    const int g = w.n / a.W, hk = w.h / a.rep;
+    const int r = ((w.n - g * a.W) * a.T + w.t) * a.rep + (w.h - hk * a.rep);
+    const uint32_t before = a.seg_start[g], tiles = a.seg_start[g + 1] - before;
+    if (tiles) {
+      const uint32_t in = (uint32_t)hk * a.seg_blocks + r / PA_BLOCK;
+      const uint32_t first = before * hb + in * tiles;
+      const uint32_t c0 = first / per, c1 = (first + tiles - 1) / per;
+      // in halves of a block: one a segment where the block has two row tiles, else two pieces a segment
+      const bool two = a.seg_rows - r / PA_BLOCK * PA_BLOCK > 128;
+      step = two ? PA_BLOCK : PA_BLOCK / 2;
+      segs = ((int)(c1 - c0) + 1) * (two ? 1 : 2);
+      seg0 = ((size_t)c0 + (size_t)g * hb + in) * PA_BLOCK + r % PA_BLOCK;
+    }
+  }
+  const int all = segs + a.slots;
+  float m = -INFINITY, l = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  constexpr int U = 4;
+  for (int s0 = 0; s0 < all; s0 += 32) {
+    const int mine = s0 + lane;
+    float2 ml = make_float2(-INFINITY, 0.f);
+    if (mine < all)
+      ml = mine < segs ? a.seg_ml[seg0 + (size_t)mine * step] : a.ml[(size_t)(mine - segs) * rows + row];
+    const float M = fmaxf(m, warp_max(ml.x)), u = M == -INFINITY ? 0.f : M;
+    const float keep = pa_ex2(m - u), f = ml.x == -INFINITY ? 0.f : pa_ex2(ml.x - u);
+    m = M;
+    l = l * keep + warp_sum(f * ml.y);
+    o.x *= keep; o.y *= keep; o.z *= keep; o.w *= keep;
+    const unsigned there = __ballot_sync(0xffffffffu, ml.x != -INFINITY);       // others wrote no sums
+    const int n = min(32, all - s0);
+    for (int j0 = 0; j0 < n; j0 += U) {
+      float4 p[U];
+#pragma unroll
+      for (int v = 0; v < U; ++v) {
+        const int s = s0 + j0 + v;
+        p[v] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (j0 + v < n && (there >> (j0 + v) & 1u) && lane * 4 < a.d)
+          p[v] = *reinterpret_cast<const float4*>(
+              (s < segs ? a.seg_po + (seg0 + (size_t)s * step) * a.d
+                        : a.po + ((size_t)(s - segs) * rows + row) * a.d) + lane * 4);
+      }
+#pragma unroll
+      for (int v = 0; v < U; ++v) {
+        const float x = __shfl_sync(0xffffffffu, f, (j0 + v) & 31);     // (0 with p: nothing there)
+        o.x = fmaf(x, p[v].x, o.x);
+        o.y = fmaf(x, p[v].y, o.y);
+        o.z = fmaf(x, p[v].z, o.z);
+        o.w = fmaf(x, p[v].w, o.w);
+      }
+    }
+  }
+  write_row<T>(a, w, m, l, o, lane);
 }
 
 // What one CTA of the warp-level kernels has: a piece of the keys of one (group or sequence, key head) and
@@ -310,7 +281,7 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
 template <int DP, bool JOIN>
 __global__ void __launch_bounds__(PF_THREADS, 3)
 pa_few_kernel(const PaArgs a, const PaKeys kk, int rows) {
-  if (!kk.behind) pdl_wait();
+  if (JOIN || !kk.behind) pdl_wait();
   using Cfg = PfCfg<DP>;
   constexpr int LD = Cfg::LD, KS = DP / 16, NT = PF_THREADS;
   extern __shared__ __align__(16) unsigned char sm[];
@@ -425,7 +396,8 @@ pa_few_kernel(const PaArgs a, const PaKeys kk, int rows) {
     for (int e = 0; e < 4; ++e)
       xo[(warp * 8 + 2 * c + (e & 1)) * XL + i * 16 + g + (e >> 1) * 8] = o[i][e];
   __syncthreads();
-  if (kk.behind) pdl_wait();
+  if (!JOIN && kk.behind) pdl_wait();
+#pragma unroll 1
   for (int r = warp; r < rows; r += 4) {
     float M = -INFINITY;
 #pragma unroll
@@ -448,10 +420,7 @@ pa_few_kernel(const PaArgs a, const PaKeys kk, int rows) {
     }
     const PaRow w = pa_row(a, kk.own, p.b, p.hk, r);
     if constexpr (JOIN) {
-      PaRow jw[1] = {w};
-      float jm[1] = {M}, jl[1] = {L};
-      float4 jo[1] = {y};
-      join_rows<__nv_bfloat16, 1>(a, jw, 1, jm, jl, jo, lane);
+      write_row<__nv_bfloat16>(a, w, M, L, y, lane);
     } else {
       const size_t at = (size_t)p.slot * a.rows() + pa_index(a, w);
       if (lane == 0) a.ml[at] = make_float2(M, L);
@@ -476,7 +445,7 @@ struct PmCfg {
 template <int DP, int RB, bool JOIN>
 __global__ void __launch_bounds__(32 * PmCfg<DP, RB>::WARPS, 12 / PmCfg<DP, RB>::WARPS)
 pa_mma_kernel(const PaArgs a, const PaKeys kk, int rows, int blocks) {
-  if (!kk.behind) pdl_wait();
+  if (JOIN || !kk.behind) pdl_wait();
   using Cfg = PmCfg<DP, RB>;
   constexpr int LD = Cfg::LD, PH = Cfg::PH, KW = Cfg::KW, KT = Cfg::KT, NT = Cfg::THREADS;
   constexpr int KS = DP / 16, NB = KW / 8, OB = DP / 8, STAGE = Cfg::STAGE;
@@ -670,23 +639,15 @@ pa_mma_kernel(const PaArgs a, const PaKeys kk, int rows, int blocks) {
       }
     }
     __syncthreads();
-    constexpr int R = 4;
     const int here = min(16 * RB, rows - r0);
-    for (int r = warp * R; r < here; r += R * Cfg::WARPS) {
-      PaRow w[R];
-      float jm[R], jl[R];
-      float4 jo[R];
+    constexpr int R = 4;                             // rows of a warp at a time: their divisions side by side
+    for (int r = warp * R; r < here; r += R * Cfg::WARPS)
 #pragma unroll
-      for (int i = 0; i < R; ++i) {
-        const int y = min(r + i, here - 1);
-        w[i] = pa_row(a, kk.own, b, hk, r0 + y);
-        jm[i] = xm[2 * y];
-        jl[i] = xm[2 * y + 1];
-        jo[i] = lane < DP / 4 ? *reinterpret_cast<const float4*>(xr + (size_t)y * XL + lane * 4)
-                              : make_float4(0.f, 0.f, 0.f, 0.f);
-      }
-      join_rows<__nv_bfloat16, R>(a, w, min(R, here - r), jm, jl, jo, lane);
-    }
+      for (int y = r; y < r + R; ++y)
+        if (y < here)
+          write_row<__nv_bfloat16>(a, pa_row(a, kk.own, b, hk, r0 + y), xm[2 * y], xm[2 * y + 1],
+                                   lane < DP / 4 ? *reinterpret_cast<const float4*>(xr + (size_t)y * XL + lane * 4)
+                                                 : make_float4(0.f, 0.f, 0.f, 0.f), lane);
     return;
   }
   if (kk.behind) pdl_wait();
@@ -1056,7 +1017,6 @@ lilicorr_status_t run_prefix_attention(const lilicorr_prefix_attention_desc* des
     for (int i = 0; i < 3; ++i) { own.front_k_s[i] = pre.k_s[i]; own.front_v_s[i] = pre.v_s[i]; }
     own.front_len = pre.len;
     own.front_capacity = pre.capacity;
-    a.seg_ctas = 0;
     return launch_pa_mma(a, own, stream);
   }
   PaMaps maps;
