@@ -190,10 +190,11 @@ __device__ __noinline__ void rank_rounds(RankShared& sh, int count, int n, Key k
     last_pos = bp;
   }
 }
-// All of it for keys that lie in shared memory (written before a barrier).
-template <int NT, class Pos, class Place>
-__device__ __forceinline__ int rank_first(RankShared& sh, const uint64_t* keys, int count, int n,
+// All of it for keys that lie in shared memory (written before a barrier), no more than fit.
+template <int NT, int CAP, class Pos, class Place>
+__device__ __forceinline__ int rank_first(RankShared& sh, const uint64_t (&keys)[CAP], int count, int n,
                                           Pos pos_of, Place place) {
+  static_assert(CAP <= RF_CAP, "");
   const int tid = threadIdx.x;
   if (count > RF_GROUPS) {
     uint64_t best = 0ull, best_p = ~0ull;
@@ -212,10 +213,7 @@ __device__ __forceinline__ int rank_first(RankShared& sh, const uint64_t* keys, 
   for (int i = tid; i < count; i += NT)
     if (keys[i] >= least) rank_keep(sh, keys[i], pos_of(i));
   __syncthreads();
-  const int m = rank_kept<NT>(sh, n, place);
-  if (m >= 0) return m;
-  rank_rounds<NT>(sh, count, n, [&](int i) { return keys[i]; }, pos_of, place);
-  return n;
+  return rank_kept<NT>(sh, n, place);
 }
 
 struct BeamOut {
