@@ -868,10 +868,14 @@ beam_choose_kernel(const T* __restrict__ logits, int W, const float* __restrict_
   }
   __syncthreads();
   uint64_t least = taken == out.n ? s_ckey[taken - 1] : 1ull;
-  // The chunks' elements, and a bound from the groups' best of them: where chunks are few for n, or beams
-  // differ, much of the first chunks lies above the last one's maximum (44 requests of 15 rows of 16,000,
-  // n 30: 47 -> 23 us; 32 x 8 rows of 151,936, n 32: 35 -> 30). Elsewhere there is little to drop, and
-  // the step costs what it takes (1 x 4 rows of 151,936, n 8: 12.4 us without it, 14.4 with it).
+  // The chunks' elements, and a bound from the groups' best of them where a row has no more chunks than n: with
+  // one beam ahead of the others the n chunks are then all of its own and more, and most of them lies above
+  // the last one's maximum. Without and with the step, one beam far ahead / beams near one another, us: 44 x 15
+  // rows of 16,000 bf16 (8 chunks), n 4 13.3 14.4 / 13.0 14.2, n 8 19.8 15.1 / 13.5 14.7, n 32 39 30 / 19.7 18.5;
+  // fp32 (16 chunks), n 12 17.2 18.4 / 16.8 17.9, n 16 21.6 18.8 / 17.2 18.3, n 32 39 24 / 23 24; 16 x 2 rows of
+  // 50,000 (25 chunks), n 16 10.1 11.1 / 9.9 11.0, n 24 14.4 12.8 / 11.4 12.7, n 32 35 13.5 / 12.9 13.4; 32 x 8 rows of
+  // 151,936 (75 chunks), n 8 23.4 25.0 / 23.1 24.4, n 32 30.4 33.1 / 29.7 32.1. 64 x 16 rows of 2,000 (1 chunk),
+  // n 1 15.9 16.8 / 14.0 15.0, n 4 16.4 17.6 / 16.1 15.1, n 16 25 19 / 24 19.
   constexpr int MINE = (LILICORR_MAX_K + NW - 1) / NW;
   uint4 raw[MINE][BS_U];
   int from[MINE];                                       // a chunk's first id, or -1
@@ -892,7 +896,7 @@ beam_choose_kernel(const T* __restrict__ logits, int W, const float* __restrict_
     cut.range(row0 + w, (int)(uint32_t)cpos, from[i], en);
     load_chunk<T>(logits + (row0 + w) * cut.V, from[i], en, lane, raw[i]);
   }
-  if (out.n > 8 || W * cut.chunks < 16 * out.n) {
+  if (out.n > 1 && cut.chunks <= out.n) {
 #pragma unroll
     for (int i = 0; i < MINE; ++i) {
       if (from[i] < 0) continue;
