@@ -18,7 +18,7 @@
 // 2^-20 at worst, and to some 1e-8 where many unlike terms share the sum.
 // Beams of one content tie: the sums have one order, and rows that are cut alike (V a multiple of a vector) the
 // same bits. Where rows start off their 16-byte boundaries their chunks differ, and with them the roundings;
-// there the pass also adds up the logits' bits as whole numbers, which no order changes, and rows of a request
+// there the pass also adds up the logits' bits (-0 as +0) as whole numbers, which no order changes, and rows of a request
 // with the same M, the same such sum and normalisers within 2^-19 (twice the above) take the lower beam's.
 #include <math.h>
 
@@ -393,7 +393,11 @@ template <> struct Elem<uint16_t> {
   __device__ static float value(uint16_t x) { return bf16_to_f32(x); }
   static constexpr uint32_t NONE = 0xFF80FF80u;
   static constexpr int BITS = 16;
-  __device__ static uint32_t mark(uint32_t w, uint32_t sum) { return __dp2a_lo(w, 0x0101u, sum); }   // + both halves
+  // the sum of bits with those of both halves, -0 as +0
+  __device__ static uint32_t mark(uint32_t w, uint32_t sum) {
+    const __nv_bfloat162 x = __hadd2(*reinterpret_cast<const __nv_bfloat162*>(&w), __float2bfloat162_rn(0.f));
+    return __dp2a_lo(*reinterpret_cast<const uint32_t*>(&x), 0x0101u, sum);
+  }
   static constexpr uint32_t MARK_NONE = 0xFF80u;           // of one element that is not there
   // the value whose ord32 begins with these 16 bits, and how many of a lane's share reach it
   __device__ static float image(uint32_t code) { return unord32((code >> 31) ? code : code | 0xFFFFu); }
@@ -447,7 +451,9 @@ template <> struct Elem<float> {
   __device__ static float value(float x) { return x; }
   static constexpr uint32_t NONE = 0xFF800000u;
   static constexpr int BITS = 32;
-  __device__ static uint32_t mark(uint32_t w, uint32_t sum) { return sum + w; }
+  __device__ static uint32_t mark(uint32_t w, uint32_t sum) {
+    return sum + __float_as_uint(__uint_as_float(w) + 0.f);
+  }
   static constexpr uint32_t MARK_NONE = NONE;
   __device__ static float image(uint32_t code) { return unord32(code); }
   __device__ static int at_least(const uint4 (&v)[BS_U], uint32_t code) {

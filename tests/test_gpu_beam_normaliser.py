@@ -171,3 +171,20 @@ def test_beams_of_one_content_tie_with_banned_tokens(kind, R, W, V, dtype):
         first = sorted((-x[r, w, v], w, v) for w in range(W) if w != 1 for v in ids)[:n]
         assert par[r].tolist() == [c[1] for c in first] and tok[r].tolist() == [c[2] for c in first]
         assert all(sc[r, j] == sc[r, j - 1] for j in range(1, n) if first[j][0] == first[j - 1][0])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [5, 1003, 4097, 4096, 12345])
+def test_zeros_of_either_sign_are_the_same_logit(V, dtype):
+    """Beams alike but for the signs of their zeros tie, at every alignment."""
+    ll = _ll()
+    rng = np.random.default_rng(V)
+    R, W, n = 3, 9, 12
+    row = np.round(rng.standard_normal((R, 1, V)) * 2) / 4
+    row[:, :, V // 2] = 3.0
+    x = np.repeat(row, W, axis=1)
+    x = np.where((x == 0) & (rng.uniform(size=x.shape) < 0.5), -0.0, x + 0.0).astype(np.float32)
+    assert np.signbit(x[x == 0]).any() and not np.signbit(x[x == 0]).all()
+    scores = np.zeros((R, W), np.float32)
+    want = _want(x, scores, n)
+    _check(_run_select(ll, x, scores, n, dtype), want)
