@@ -403,7 +403,8 @@ lilicorr_status_t lilicorr_beam_reorder_layouts(const lilicorr_beam_states* host
  * 1 - t), key head h / (q_heads / kv_heads); lse[n, t, h] = log sum_j exp(scale q . key_j). A row
  * that sees no key gets out 0 and lse -inf. Lengths are clipped to [0, capacity], but seq_len[n] < 0
  * says that there is no sequence n: its rows of out and lse are left as they were. What a cache holds
- * behind its length is not looked at (NaN included); what it holds before it has to be finite.
+ * behind its length is not looked at (NaN included); what it holds before it has to be finite. A query
+ * with a NaN gives its own row NaN, in out and in lse, and no other.
  *   q, out [N, T, q_heads, head_dim]; prefix_k, prefix_v [groups, prefix_capacity, kv_heads,
  *   head_dim]; k, v [N, own_capacity, kv_heads, head_dim], all of dtype, each with its strides in
  *   elements (the last dimension is dense), 16-byte aligned, strides multiples of 16 bytes and not

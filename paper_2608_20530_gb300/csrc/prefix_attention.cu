@@ -81,11 +81,12 @@ __device__ __forceinline__ void stage_rows(unsigned char* dst, const unsigned ch
   }
 }
 
-// A row's result from its maximum, its sum and its sums of V, four columns a lane, to out and lse.
+// A row's result from its maximum, its sum and its sums of V, four columns a lane, to out and lse. A row that
+// saw no key has the sum 0 (any other's is positive, or NaN, which stays; maxima pass over NaN).
 template <typename T>
 __device__ __forceinline__ void write_row(const PaArgs& a, const PaRow& w, float m, float l, const float4& o,
                                           int lane) {
-  const float inv = l > 0.f ? 1.0f / l : (m == -INFINITY ? 0.f : l);       // (NaN stays)
+  const float inv = l == 0.f ? 0.f : 1.0f / l;
   T* out = static_cast<T*>(a.out) + (int64_t)w.n * a.o_s[0] + (int64_t)w.t * a.o_s[1] +
            (int64_t)w.h * a.o_s[2];
   if (lane * 4 < a.d) {
@@ -96,7 +97,7 @@ __device__ __forceinline__ void write_row(const PaArgs& a, const PaRow& w, float
       *reinterpret_cast<uint2*>(out + lane * 4) = make_uint2(bf16_pack2(y.x, y.y), bf16_pack2(y.z, y.w));
   }
   if (lane == 0)
-    a.lse[pa_index(a, w)] = m == -INFINITY ? -INFINITY : fmaf(m, LN2, fmaf(m, LN2_REST, logf(l)));
+    a.lse[pa_index(a, w)] = l == 0.f ? -INFINITY : fmaf(m, LN2, fmaf(m, LN2_REST, logf(l)));
 }
 
 // Join the rows' pieces, the prefix's segments and the slots, where no kernel of the own keys writes the result:
@@ -143,11 +144,11 @@ pa_combine_kernel(const PaArgs a) {
     if (mine < all)
       ml = mine < segs ? a.seg_ml[seg0 + (size_t)mine * step] : a.ml[(size_t)(mine - segs) * rows + row];
     const float M = fmaxf(m, warp_max(ml.x)), u = M == -INFINITY ? 0.f : M;
-    const float keep = pa_ex2(m - u), f = ml.x == -INFINITY ? 0.f : pa_ex2(ml.x - u);
+    const float keep = pa_ex2(m - u), f = pa_ex2(ml.x - u);
     m = M;
     l = l * keep + warp_sum(f * ml.y);
     o.x *= keep; o.y *= keep; o.z *= keep; o.w *= keep;
-    const unsigned there = __ballot_sync(0xffffffffu, ml.x != -INFINITY);       // others wrote no sums
+    const unsigned there = __ballot_sync(0xffffffffu, ml.y != 0.f);             // others wrote no sums
     const int n = min(32, all - s0);
     for (int j0 = 0; j0 < n; j0 += U) {
       float4 p[U];

@@ -38,7 +38,7 @@ struct PaArgs {
   float scale_log2;            // scale * log2(e): scores in log2 units
   float scale_rest;            // what its rounding left
   // partial results of a piece of the keys: (maximum, sum of 2^(s - maximum)) and the sums of
-  // 2^(s - maximum) V, fp32; a maximum of -inf: no keys, and no sums were written
+  // 2^(s - maximum) V, fp32; a sum of 0: no keys, and no sums of V were written
   int slots;                   // pieces per row that are kept by row
   float2* ml;                  // [slots][rows]
   float* po;                   // [slots][rows][d]
