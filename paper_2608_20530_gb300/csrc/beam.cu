@@ -503,10 +503,10 @@ __device__ __forceinline__ void load_chunk(const T* __restrict__ row, int begin,
   }
 #pragma unroll
   for (int u = 0; u < BS_U; ++u) {
-    const int at = begin + (u * 32 + lane) * N;
+    const unsigned at = (unsigned)begin + (u * 32 + lane) * N;     // (may pass 2^31 - 1, as V may come near it)
     raw[u] = make_uint4(NI, NI, NI, NI);
-    if (at + N <= end) raw[u] = __ldcs(reinterpret_cast<const uint4*>(row + at));
-    else if (at < end) raw[u] = Elem<T>::gather(row + at, end - at);
+    if (at + N <= (unsigned)end) raw[u] = __ldcs(reinterpret_cast<const uint4*>(row + at));
+    else if (at < (unsigned)end) raw[u] = Elem<T>::gather(row + at, end - (int)at);
   }
 }
 

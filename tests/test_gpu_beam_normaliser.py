@@ -188,3 +188,21 @@ def test_zeros_of_either_sign_are_the_same_logit(V, dtype):
     scores = np.zeros((R, W), np.float32)
     want = _want(x, scores, n)
     _check(_run_select(ll, x, scores, n, dtype), want)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V", [(1 << 31) - 1, (1 << 31) - 8])
+def test_a_vocabulary_that_ends_at_31_bits(V, dtype):
+    """Ids up to the largest int32: the row's last piece ends there, inside a vector or at one's end."""
+    ll = _ll()
+    x = torch.full((1, 1, V), -1.0, dtype=dtype, device="cuda")
+    at = {V - 1: 30.0, 0: 29.0, V - 2050: 28.0, 1500000001: 27.0, V - 2: 26.5}
+    for v, y in at.items():
+        x[0, 0, v] = y
+    ws = ll.Workspace(ll.beam_select_workspace_bytes(1, 1, V, 5))
+    tok, par, sc, _ = ll.beam_select(x, torch.zeros((1, 1), device="cuda"), 5, ws=ws)
+    lse = math.log(sum(math.exp(y) for y in at.values()) + (V - 5) * math.exp(-1.0))
+    assert tok.cpu().tolist() == [list(at)] and par.cpu().tolist() == [[0] * 5] and ws.status() == 0
+    for got, y in zip(sc.cpu().tolist()[0], at.values()):
+        assert abs(got - (y - lse)) <= TOL + 2.0 ** -24 * abs(y - lse)
+    del x
