@@ -409,7 +409,7 @@ lilicorr_status_t lilicorr_beam_reorder_layouts(const lilicorr_beam_states* host
  *   head_dim]; k, v [N, own_capacity, kv_heads, head_dim], all of dtype, each with its strides in
  *   elements (the last dimension is dense), 16-byte aligned, strides multiples of 16 bytes and not
  *   negative; lse [N, T, q_heads] fp32; prefix_len [groups], seq_len [N] int32 on the device
- * head_dim a multiple of 8 up to 128, q_heads a multiple of kv_heads, 0 < scale < inf, capacities from
+ * head_dim a multiple of 8 up to 128, q_heads a multiple of kv_heads, 0 < scale < 2^127, capacities from
  * 0 (then the pointers of that side may be NULL) to 2^30. Caches may overlap themselves (a stride of 0:
  * one prefix for all groups), out may not, nor may out and lse overlap an input. F32 runs in fp32
  * throughout; BF16 takes bf16 products with fp32 accumulation, softmax and sums in fp32. ws: zero-filled

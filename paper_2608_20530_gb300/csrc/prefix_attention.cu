@@ -945,7 +945,7 @@ lilicorr_status_t run_prefix_attention(const lilicorr_prefix_attention_desc* des
   if (desc->dtype != LILICORR_F32 && desc->dtype != LILICORR_BF16) return LILICORR_ERR_DTYPE;
   PaPlan p;
   if (!pa_plan(desc, &p)) return LILICORR_ERR_SHAPE;
-  if (!(desc->scale > 0.f) || !(desc->scale < INFINITY)) return LILICORR_ERR_ARG;
+  if (!(desc->scale > 0.f) || !(desc->scale < 0x1p127f)) return LILICORR_ERR_ARG;      // (times log2(e): finite)
   if (desc->groups == 0) return LILICORR_OK;
   const bool has_p = desc->prefix_capacity > 0, has_s = desc->own_capacity > 0;
   if (!q || !out || !lse || !ws || !seq_len) return LILICORR_ERR_ARG;
