@@ -332,7 +332,8 @@ lilicorr_status_t lilicorr_select_block_walk(const lilicorr_head* head, int B, c
  *   tokens, parents [R, n] int32   token and beam of each kept candidate; -1 where there are fewer
  *   next_scores     [R, n] fp32    the total, rounded once; -inf where there are fewer
  *   next_done       [R, n] bytes   1 where the parent was done or the token is end_id (may be NULL)
- * so outputs are inputs of the next step, -inf and -1 included. Outputs must not overlap inputs. A
+ * so outputs are inputs of the next step, -inf and -1 included (of up to LILICORR_MAX_K beams: a search of more
+ * cannot keep them all, though a step may read up to LILICORR_MAX_BEAMS). Outputs must not overlap inputs. A
  * NaN or +inf score or log-probability, and a live beam whose normaliser is not finite (NaN or +inf
  * logits, or only -inf), set LILICORR_ERR_NONFINITE; such a candidate, or beam, is not kept. */
 #define LILICORR_MAX_BEAMS 64

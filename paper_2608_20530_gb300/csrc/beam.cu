@@ -2,7 +2,7 @@
 // beams that continue them.
 //
 // Selection from logits takes two launches. (In one, the CTA that finishes a request choosing for it, the
-// choosing ran beside warps that still stream and behind their fences: 32 x 8 rows 30 -> 34 us.)
+// choosing ran beside warps that still stream and behind their fences: 34 us for 32 x 8 rows, when two took 30.)
 //   (1) beam_stream_kernel reads every live row once, in chunks of 32 x 8 vectors of 16 bytes, one
 //       warp a chunk, and leaves each chunk's largest logit m and the sum of exp(x - m).
 //   (2) beam_choose_kernel, one CTA a request, forms the rows' normalisers, takes the n chunks whose
@@ -339,8 +339,10 @@ beam_merge_kernel(const int32_t* __restrict__ ids, const float* __restrict__ log
 
 // ---------------------------------------------------------------------------- from logits
 // The streaming kernel: vectors of 16 bytes per lane and chunk, chunks of a warp in flight or in use, CTAs an
-// SM. 32 x 8 rows of the call, us: (8, 3, 2) 30.3; (4, 4, 3) 31.7, (4, 6, 2) 32.5, (4, 3, 4) 31.4, (4, 8, 2)
-// 37.1, (8, 2, 3) 30.0: what is in flight matters little, being 100 KB an SM in all of them.
+// SM. The call on 32 x 8 bf16 rows of 151,936 and on 24 x 5 fp32 rows of 128,257, device us: (8, 3, 2) 23.8 and
+// 20.6; (8, 2, 3) 23.9 and 19.8; (4, 4, 3) 26.9 and 23.1, (4, 6, 2) 27.9 and 24.7, (4, 4, 2) 29.3 and 24.6. What is
+// in flight (96 KB an SM in the second and the last, 128 to 160 in the others) matters less than what each chunk
+// costs besides its elements.
 constexpr int BS_THREADS = 256;
 constexpr int BS_U = 8, BS_STAGES = 3, BS_CTAS = 2;
 constexpr int BC_THREADS = 512;                // of the choosing kernel

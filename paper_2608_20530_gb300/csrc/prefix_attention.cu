@@ -906,6 +906,7 @@ bool pa_plan(const lilicorr_prefix_attention_desc* d, PaPlan* p) {
   // 38. Each range costs it 4 us or more besides: 2,048 ranges of 256 keys, 4 rows 106 us and 70; 256 of 256,
   // 64 rows 62 and 56; 512 of 2,048, 16 rows 119 and 114; 512 of 1,024, 64 rows 142 and 157; 256 of 256, 256
   // rows 181 and 197. And at d = 64 up to 16 rows never fill it: 512 ranges of 2,048 keys 91 and 68.
+  // (Heads of 72 to 120 are computed as 128 wide by either, and counted so.)
   const long long blocks = (prow + PA_BLOCK - 1) / PA_BLOCK;
   const double tiles = (double)pranges * blocks * ((double)d->prefix_capacity / PA_TILE + 1);
   const double item = (double)d->prefix_capacity / PA_TILE * (prow < 16 ? 16 : prow) *

@@ -451,7 +451,8 @@ pa_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
             m = ceilf(top);
           } else if (__any_sync(0xffffffffu, top > m + 8.f)) {
             // the sums so far, and the first half's probabilities, to the new maximum: by a whole power
-            // of two, which rounds nothing (their product is complete: the scores came behind it)
+            // of two, which rounds nothing that 2^-118 of the row's largest term would show (their product is
+            // complete: the scores came behind it)
             const float to = fmaxf(m, ceilf(top)), f = pow2_down(m - to);
             m = to;
             l *= f;
