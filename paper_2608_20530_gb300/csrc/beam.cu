@@ -18,8 +18,9 @@
 // 2^-20 at worst, and to some 1e-8 where many unlike terms share the sum.
 // Beams of one content tie: the sums have one order, and rows that are cut alike (V a multiple of a vector) the
 // same bits. Where rows start off their 16-byte boundaries their chunks differ, and with them the roundings;
-// there the pass also adds up the logits' bits (-0 as +0) as whole numbers, which no order changes, and rows of a request
-// with the same M, the same such sum and normalisers within 2^-19 (twice the above) take the lower beam's.
+// there the pass also adds up the logits' bits (-0 as +0) as whole numbers, which no order changes, and rows of
+// a request with the same M, the same such sum and normalisers within 2^-19 (twice the above) take the lower
+// beam's.
 #include <math.h>
 
 #include "internal.cuh"
@@ -621,8 +622,10 @@ beam_stream_kernel(const T* __restrict__ logits, unsigned rows, const float* __r
       if constexpr (ODD) {
         uint32_t mark = 0;
 #pragma unroll
-        for (int u = 0; u < BS_U; ++u)
-          mark = Elem<T>::mark(raw[u].w, Elem<T>::mark(raw[u].z, Elem<T>::mark(raw[u].y, Elem<T>::mark(raw[u].x, mark))));
+        for (int u = 0; u < BS_U; ++u) {
+          mark = Elem<T>::mark(raw[u].y, Elem<T>::mark(raw[u].x, mark));
+          mark = Elem<T>::mark(raw[u].w, Elem<T>::mark(raw[u].z, mark));
+        }
         mark = __reduce_add_sync(FULL, mark) - (uint32_t)missing * Elem<T>::MARK_NONE;
         if (lane == 0) marks[i] = mark;
       }
