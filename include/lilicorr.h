@@ -341,8 +341,8 @@ lilicorr_status_t lilicorr_select_block_walk(const lilicorr_head* head, int B, c
 /* From logits [R, W, V] (F32 or BF16), one pass over the rows of live beams:
  * logp(v | w) = logits[w, v] - log sum_u exp(logits[w, u]), in a beam equal logits by lower id. Finite
  * logits of any size are taken (a row whose logits are all the type's lowest value is a uniform one). logp
- * is good to 2^-20 and never above 0. Rows of the same logits have the same normaliser: such beams of a request
- * tie where their scores do.
+ * is good to 2^-20 (2^-19 where V is above 151,936) and never above 0. Rows of the same logits have the same
+ * normaliser: such beams of a request tie where their scores do.
  * n <= W * V, R * W <= 65535, logits and ws 16-byte aligned. ws: zero-filled once, at least
  * lilicorr_beam_select_workspace_bytes(R, W, V, n) bytes (0: unsupported shape); its first word is
  * the device status. */

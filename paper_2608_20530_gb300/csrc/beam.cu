@@ -14,12 +14,13 @@
 // A total is (score - log S) + (x - M), M the row's largest logit and S the sum of exp(x - M): whatever the
 // logits' size, x - M keeps what tells them apart. S is at least 1 (the largest logit's own term is 1 exactly),
 // so that no total lies above its score. Totals are sums of 48 bits of inputs that are not: ex2.approx is good
-// to 2^-22 and its argument of up to 17 log2 units, before a term that counts, to 2^-20, so that log S is good to
-// 2^-20 at worst, and to some 1e-8 where many unlike terms share the sum.
+// to 2^-22 and its argument to half a step, 2^-20 from 16 log2 units on, so that log S is good to 2^-20 at worst for V
+// up to 151,936 (terms 11 nats below M, half of S together), to 2^-19 at any V, and to some 1e-8 where many
+// unlike terms share the sum.
 // Beams of one content tie: the sums have one order, and rows that are cut alike (V a multiple of a vector) the
 // same bits. Where rows start off their 16-byte boundaries their chunks differ, and with them the roundings;
 // there the pass also adds up the logits' bits (-0 as +0) as whole numbers, which no order changes, and rows of
-// a request with the same M, the same such sum and normalisers within 2^-19 (twice the above) take the lower
+// a request with the same M, the same such sum and normalisers within 2^-18 (twice the above) take the lower
 // beam's.
 #include <math.h>
 
@@ -802,7 +803,7 @@ beam_choose_kernel(const T* __restrict__ logits, int W, const float* __restrict_
         const int v = w0 + lane;
         const float2 x = v < w ? s_norm[v] : make_float2(INFINITY, 0.f);       // (+inf: not live)
         const unsigned same = __ballot_sync(
-            FULL, fabsf((x.x - norm.x) + (x.y - norm.y)) <= 0x1p-19f && s_base[v].top == base.top &&
+            FULL, fabsf((x.x - norm.x) + (x.y - norm.y)) <= 0x1p-18f && s_base[v].top == base.top &&
                       s_mark[v] == s_mark[w]);
         if (same) {
           norm = s_norm[w0 + __ffs(same) - 1];

@@ -1,10 +1,11 @@
 """The normaliser of beam_select: rows of logits of any size, rows that one token dominates.
 
 logp = (x - M) - log S, S the sum of exp(x - M) over the row, M its largest logit. Each term of S is off by at most
-2^-22 of itself (ex2.approx), the constant log2(e) by 2^-26 of the argument, and the argument's rounding by
-half a step: 2^-20 up to 32 log2 units. Terms weigh e^-t at t nats, and at most 2^18 of them lie there, so what
-an error of the argument does to log S is largest near t = 11: 0.7 (2^-22 + 2^-21.5 + 2^-23) < 2^-20.6. The
-sums in fp32 (chains of 16 or fewer, then halves) add 2^-22.5: below 2^-20 in all. S is not below 1."""
+2^-22 of itself (ex2.approx, 2.4e-7), by 1.3e-8 a nat below M (the constant log2(e)), and by half a step of its
+argument in log2 units: 1.7e-7 up to 8 of them, 3.3e-7 up to 16, 6.6e-7 up to 32. The terms at t nats count
+e^-t each, V of them at most V e^-t / (1 + V e^-t) of S: with V = 60,000 the worst lies at t = 6 to 9, 6.5e-7 of S
+(near t = 11.1, where the argument passes 16, 5.0e-7; with V = 151,936 there 7.3e-7). The sums in fp32 (chains of
+16 or fewer, then halves) add 1.7e-7: below 2^-20 = 9.5e-7 in all. S is not below 1."""
 import math
 
 import numpy as np
@@ -206,3 +207,17 @@ def test_a_vocabulary_that_ends_at_31_bits(V, dtype):
     for got, y in zip(sc.cpu().tolist()[0], at.values()):
         assert abs(got - (y - lse)) <= TOL + 2.0 ** -24 * abs(y - lse)
     del x
+
+
+@pytest.mark.parametrize("V", [151936, 128257])
+def test_a_level_background_behind_a_peak(V):
+    """All terms but one round alike, the case the bound on log S is made of: 96 distances of the peak."""
+    ll = _ll()
+    t = np.float32(2.0) + np.arange(96, dtype=np.float32) * np.float32(0.15625)          # up to 16.8 nats
+    x = torch.zeros((96, 1, V), device="cuda")
+    x[:, 0, V // 2] = torch.from_numpy(t).cuda()
+    tok, _, sc, _ = ll.beam_select(x, torch.zeros((96, 1), device="cuda"), 2)
+    exact = -np.log1p((V - 1) * np.exp(-t.astype(np.float64)))
+    assert tok.cpu().tolist() == [[V // 2, 0]] * 96
+    err = np.abs(sc.cpu().numpy()[:, 0] - exact)
+    assert np.all(err <= TOL + 2.0 ** -24 * np.abs(exact)), err.max()
