@@ -432,6 +432,97 @@ lilicorr_status_t lilicorr_prefix_attention(const lilicorr_prefix_attention_desc
                                             const int32_t* seq_len, void* out, float* lse, void* ws,
                                             size_t ws_bytes, cudaStream_t stream);
 
+/* A decoding cache held in 4 bits. Not from the paper: the target's and the drafter's keys and values of
+ * long contexts, in 9/32 of the bytes of bf16. A record holds one key and one value of one (sequence,
+ * position, kv head), lilicorr_cache_record_bytes(head_dim) = head_dim + 16 bytes of
+ *   head_dim / 2 bytes  the key's elements, two a byte, the one of even index in the low half: sign, two
+ *                       bits of exponent, one of fraction (0, 0.5, 1, 1.5, 2, 3, 4, 6)
+ *   8 bytes             its scales, one for 16 elements that follow one another: four bits of exponent, three
+ *                       of fraction, no sign (bias 7, up to 448, 127 is NaN); unused ones are 0
+ *   the same for the value.
+ * Element i is code_i * scale_(i / 16) * unit, which bf16 holds exactly. k_unit and v_unit are powers of two
+ * from 2^-60 to 2^60, the same in every call on a cache: 1, unless the values lie far from 1 (a group's
+ * scale is a multiple of 2^-9, and a value is cut at 2688 units).
+ * A cache is [sequences, capacity, kv_heads] records, 16-byte aligned, the strides in bytes, multiples of 16
+ * and not negative. Where it is written no two of its records may overlap. head_dim is a multiple of 16 up
+ * to 128, capacity at most 2^30. Sequence n holds the positions below seq_len[n] (int32, on the device),
+ * clipped to [0, capacity]; below 0 there is no such sequence. What lies behind is not looked at.
+ * weights [sequences, kv_heads, capacity] fp32, where there are any, hold what attention each key has
+ * gathered: appended at 0, added to by lilicorr_cache_attention, read and moved by lilicorr_cache_evict. */
+typedef struct {
+  int sequences, capacity, kv_heads, head_dim;
+  int64_t stride[3];                                 /* bytes: sequence, position, head */
+  float k_unit, v_unit;
+} lilicorr_cache_desc;
+
+/* Bytes of a record (0: head_dim is not supported). */
+size_t lilicorr_cache_record_bytes(int head_dim);
+
+/* The keys and values k, v [sequences, tokens, kv_heads, head_dim] (F32 or BF16, strides in elements of
+ * (sequence, token, head), the last dimension dense, 16-byte aligned) of each sequence's `tokens` newest
+ * tokens, rounded into the cache: token t becomes position seq_len[n] - tokens + t, and is left out where
+ * that is outside [0, capacity). A group of 16 elements x has the scale nearest to max |x| / (6 unit), at
+ * least 2^-9 and at most 448, and the codes nearest to x / (scale unit), at most 6 (ties to the even
+ * code; infinities are cut). A group with a NaN becomes NaN. The weights of the new positions become 0
+ * (NULL: there are none). */
+lilicorr_status_t lilicorr_cache_append(const lilicorr_cache_desc* desc, void* cache,
+                                        lilicorr_dtype_t dtype, int tokens, const void* k,
+                                        const int64_t host_k_stride[3], const void* v,
+                                        const int64_t host_v_stride[3], const int32_t* seq_len,
+                                        float* weights, cudaStream_t stream);
+
+/* The way back: the values that the cache holds for each sequence's `tokens` newest tokens, in k and v
+ * of dtype; 0 where there is no such position (seq_len[n] - tokens + t as above) or sequence. k and v
+ * may not overlap themselves, one another or the cache. */
+lilicorr_status_t lilicorr_cache_read(const lilicorr_cache_desc* desc, const void* cache,
+                                      lilicorr_dtype_t dtype, int tokens, void* k,
+                                      const int64_t host_k_stride[3], void* v,
+                                      const int64_t host_v_stride[3], const int32_t* seq_len,
+                                      cudaStream_t stream);
+
+/* Attention of each sequence's `tokens` newest tokens, which are in the cache, over its positions:
+ *   out[n, t, h] = sum_j softmax_j(scale q[n, t, h] . key_j) value_j,  j < seq_len[n] - (tokens - 1 - t),
+ * kv head h / (q_heads / kv_heads); lse[n, t, h] = log sum_j exp(scale q . key_j). A row that sees no key
+ * gets out 0 and lse -inf; where seq_len[n] < 0 the rows of out and lse are left as they were. A query
+ * with a NaN gives its own row NaN, and no other. What the cache holds for the positions has to be finite.
+ * weights (may be NULL) [n, kv head, j] += sum of softmax_j over the tokens and the kv head's query heads
+ * (rows whose lse is not finite add nothing).
+ *   q, out [sequences, tokens, q_heads, head_dim] of dtype, strides in elements, 16-byte aligned; lse
+ *   [sequences, tokens, q_heads] fp32
+ * q_heads a multiple of kv_heads, 0 < scale * k_unit < 2^100. The cache may overlap itself; out may not, nor
+ * may out, lse and weights overlap anything else. Products are exact for F32 queries to 2^-33 and for
+ * BF16 ones; softmax and sums are fp32. ws: zero-filled once, at least
+ * lilicorr_cache_attention_workspace_bytes(desc) bytes (0: unsupported); its first word is the device status. */
+typedef struct {
+  lilicorr_cache_desc cache;
+  int tokens, q_heads;
+  lilicorr_dtype_t dtype;
+  float scale;
+  int64_t q_stride[3], out_stride[3];                /* elements: sequence, token, head */
+} lilicorr_cache_attention_desc;
+size_t lilicorr_cache_attention_workspace_bytes(const lilicorr_cache_attention_desc* desc);
+lilicorr_status_t lilicorr_cache_attention(const lilicorr_cache_attention_desc* desc, const void* q,
+                                           const void* cache, const int32_t* seq_len, void* out,
+                                           float* lse, float* weights, void* ws, size_t ws_bytes,
+                                           cudaStream_t stream);
+
+/* Sequences of more than `budget` positions are cut to so many: of each kv head the `first` first and the
+ * `recent` newest positions stay, and of the others the budget - first - recent of largest weight (equal
+ * ones by lower position; -0 equals +0, NaN counts as less than anything). Records and weights of what
+ * stays move, in the order of their positions, to positions 0, 1, ..., in place or, with `into` (of the
+ * same sequences, kv_heads and head_dim, capacity at least budget, units of `desc`), to another cache and
+ * its weights, to which shorter sequences are copied whole. Positions behind keep what they held.
+ *   kept [sequences, kv_heads, budget] int32: the positions that stayed, in order, then -1
+ *   new_len [sequences] int32: min(seq_len, budget) (a negative seq_len as it is); not seq_len itself,
+ *   which other layers may still need
+ * 1 <= budget, first + recent <= budget. The spans of memory of the two caches, and of their weights,
+ * must not overlap. */
+lilicorr_status_t lilicorr_cache_evict(const lilicorr_cache_desc* desc, void* cache, float* weights,
+                                       const int32_t* seq_len, int budget, int recent, int first,
+                                       const lilicorr_cache_desc* into, void* into_cache,
+                                       float* into_weights, int32_t* kept, int32_t* new_len,
+                                       cudaStream_t stream);
+
 /* Device view of a select_block workspace after the call, for inspection:
  * pointers into ws of the intermediates of the last call (ids [B,L,K] int32,
  * logp [B,L,K] fp32, lse [B,L] fp32, anchor [B,K] fp32, pair [B,L-1,K,K] fp32,

@@ -8,7 +8,8 @@ library is missing, every call raises.
 Names follow the C ABI: ``topk_lse``, ``embed_in_out``, ``pair_scores``,
 ``greedy_walk``, ``select_block``, plus ``Head`` (an uploaded scoring head) and
 ``Workspace`` (caller-owned scratch); for several continuations of a request (beams, drafted
-blocks) ``beam_select``, ``beam_merge``, ``beam_reorder`` and ``prefix_attention``.
+blocks) ``beam_select``, ``beam_merge``, ``beam_reorder`` and ``prefix_attention``; for a decoding
+cache held in 4 bits ``cache_append``, ``cache_read``, ``cache_attention`` and ``cache_evict``.
 """
 from __future__ import annotations
 
@@ -59,6 +60,17 @@ class BeamStates(ctypes.Structure):
                 ("stride_request", "stride_beam", "stride_position", "stride_head")]
 
 
+class CacheDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("sequences", "capacity", "kv_heads", "head_dim")] + \
+               [("stride", ctypes.c_int64 * 3), ("k_unit", ctypes.c_float), ("v_unit", ctypes.c_float)]
+
+
+class CacheAttentionDesc(ctypes.Structure):
+    _fields_ = [("cache", CacheDesc), ("tokens", ctypes.c_int), ("q_heads", ctypes.c_int),
+                ("dtype", ctypes.c_int), ("scale", ctypes.c_float),
+                ("q_stride", ctypes.c_int64 * 3), ("out_stride", ctypes.c_int64 * 3)]
+
+
 _LIB: Optional[ctypes.CDLL] = None
 _P = ctypes.c_void_p
 _I = ctypes.c_int
@@ -107,6 +119,12 @@ _SIGS = {
     "lilicorr_beam_reorder_layouts": (_I, [_P, _I, _I, _I, _P, _P, _P]),
     "lilicorr_prefix_attention_workspace_bytes": (_S, [_P]),
     "lilicorr_prefix_attention": (_I, [_P] * 11 + [_S, _P]),
+    "lilicorr_cache_record_bytes": (_S, [_I]),
+    "lilicorr_cache_append": (_I, [_P, _P, _I, _I, _P, _P, _P, _P, _P, _P, _P]),
+    "lilicorr_cache_read": (_I, [_P, _P, _I, _I, _P, _P, _P, _P, _P, _P]),
+    "lilicorr_cache_attention_workspace_bytes": (_S, [_P]),
+    "lilicorr_cache_attention": (_I, [_P] * 8 + [_S, _P]),
+    "lilicorr_cache_evict": (_I, [_P] * 4 + [_I] * 3 + [_P] * 6),
     "lilicorr_test_prefix_attention_timeout": (_I, [_P] * 11 + [_S, ctypes.c_longlong, _I, _P]),
     "lilicorr_test_linear": (_I, [_P, _I, _I, _P, _I, _I, _P, _I, _I, _I, _I, _I, _P, _P, _I, _I,
                                   _P, _P]),
@@ -761,6 +779,190 @@ def prefix_attention(q: torch.Tensor, prefix_k: torch.Tensor, prefix_v: torch.Te
     if status:
         _check(status, "prefix_attention")
     return out, lse
+
+
+# --------------------------------------------------------------------------- a cache held in 4 bits
+_CACHE_DESC = struct.Struct("@4i3q2f")               # the layout of lilicorr_cache_desc
+_CA_DESC = struct.Struct("@4i3q2f3if6q")             # of lilicorr_cache_attention_desc
+_STRIDES = struct.Struct("@3q")
+
+
+def cache_record_bytes(head_dim: int) -> int:
+    """Bytes of one (sequence, position, kv head)'s key and value (0: head_dim is not supported, which
+    is a multiple of 16 up to 128). A cache is a uint8 tensor [sequences, capacity, kv_heads, bytes]."""
+    return int(lib().lilicorr_cache_record_bytes(int(head_dim)))
+
+
+def _cache(cache: torch.Tensor, dev: int, name: str = "cache"):
+    """(sequences, capacity, kv_heads, head_dim, the strides) of a cache tensor."""
+    shape, st = cache.shape, cache.stride()
+    if len(shape) != 4 or cache.dtype is not torch.uint8:
+        raise ValueError(f"{name} must be uint8 [sequences, capacity, kv_heads, record bytes]")
+    if cache.get_device() != dev:
+        _here(cache, name, dev)
+    if st[3] != 1 and cache.numel():
+        raise ValueError(f"{name}: records must be dense")
+    N, S, H, R = shape
+    if not 32 <= R <= 144 or R % 16:
+        raise ValueError(f"{name}: records of {R} bytes (see cache_record_bytes)")
+    return (N, S, H, R - 16, *st[:3])
+
+
+def _cache_weights(weights: torch.Tensor, x, dev: int, name: str = "weights") -> int:
+    shape = (x[0], x[2], x[1])
+    if (weights.get_device() != dev or weights.dtype is not torch.float32 or weights.shape != shape or
+            not weights.is_contiguous()):
+        _refuse(weights, name, dev, torch.float32, shape)
+    return weights.data_ptr()
+
+
+def _seq_len(seq_len: torch.Tensor, N: int, dev: int) -> int:
+    if (seq_len.get_device() != dev or seq_len.dtype is not torch.int32 or seq_len.shape != (N,) or
+            not seq_len.is_contiguous()):
+        _refuse(seq_len, "seq_len", dev, torch.int32, (N,))
+    return seq_len.data_ptr()
+
+
+def _rows(t: torch.Tensor, name: str, dev: int, dtype: torch.dtype, shape) -> bytes:
+    st = t.stride()
+    if t.get_device() != dev or t.dtype is not dtype or t.shape != shape or (
+            st[3] != 1 and t.numel() and shape[3] > 1):
+        _here(t, name, dev, dtype, shape)
+        raise ValueError(f"{name}: the last dimension must be dense")
+    return _STRIDES.pack(*st[:3])
+
+
+def cache_append(cache: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seq_len: torch.Tensor,
+                 weights: Optional[torch.Tensor] = None, k_unit: float = 1.0,
+                 v_unit: float = 1.0) -> torch.Tensor:
+    """The keys and values k, v [N, T, kv_heads, d] (fp32 or bf16, any strides that keep 16-byte rows) of
+    each sequence's T newest tokens rounded into the cache [N, S, kv_heads, d + 16] (uint8): token t becomes
+    position seq_len[n] - T + t, seq_len [N] int32 being the lengths with the new tokens; positions
+    outside the cache are left out. The weights [N, kv_heads, S] fp32 of new positions become 0. Units
+    are powers of two (see lilicorr.h). Returns ``cache``."""
+    dev, dt = torch.cuda.current_device(), k.dtype
+    x = _cache(cache, dev)
+    if k.dim() != 4:
+        raise ValueError("k and v are [sequences, tokens, kv_heads, head_dim]")
+    T = k.shape[1]
+    shape = (x[0], T, x[2], x[3])
+    ks, vs = _rows(k, "k", dev, dt, shape), _rows(v, "v", dev, dt, shape)
+    _fits(x[0] | x[1] | x[2] | T)
+    w = None if weights is None else _cache_weights(weights, x, dev)
+    status = lib().lilicorr_cache_append(_CACHE_DESC.pack(*x, k_unit, v_unit), cache.data_ptr(),
+                                         _dtype_code(k), T, k.data_ptr(), ks, v.data_ptr(), vs,
+                                         _seq_len(seq_len, x[0], dev), w, _stream())
+    if status:
+        _check(status, "cache_append")
+    return cache
+
+
+def cache_read(cache: torch.Tensor, seq_len: torch.Tensor, tokens: int,
+               dtype: torch.dtype = torch.bfloat16, k_unit: float = 1.0, v_unit: float = 1.0):
+    """The values that the cache holds for each sequence's newest ``tokens`` positions: (k, v)
+    [N, tokens, kv_heads, d] of dtype (fp32 or bf16, exact in both), as prefix_attention takes them;
+    0 where there is no such position or sequence."""
+    dev = torch.cuda.current_device()
+    x = _cache(cache, dev)
+    _fits(x[0] | x[1] | x[2] | tokens)
+    if tokens < 0:
+        raise ValueError("tokens must not be negative")
+    shape = (x[0], tokens, x[2], x[3])
+    k = torch.empty(shape, dtype=dtype, device=cache.device)
+    v = torch.empty(shape, dtype=dtype, device=cache.device)
+    s = _STRIDES.pack(*k.stride()[:3])
+    status = lib().lilicorr_cache_read(_CACHE_DESC.pack(*x, k_unit, v_unit), cache.data_ptr(),
+                                       _dtype_code(k), tokens, k.data_ptr(), s, v.data_ptr(), s,
+                                       _seq_len(seq_len, x[0], dev), _stream())
+    if status:
+        _check(status, "cache_read")
+    return k, v
+
+
+def cache_attention_workspace_bytes(q: torch.Tensor, cache: torch.Tensor) -> int:
+    """Bytes of the workspace that cache_attention needs for tensors of these shapes."""
+    if q.dim() != 4 or cache.dim() != 4:
+        raise ValueError("q is [N, T, q_heads, d], the cache [N, capacity, kv_heads, record bytes]")
+    N, S, H, R = cache.shape
+    _fits(N | S | H | q.shape[1] | q.shape[2])
+    return int(lib().lilicorr_cache_attention_workspace_bytes(
+        _CA_DESC.pack(N, S, H, R - 16, 0, 0, 0, 1.0, 1.0, q.shape[1], q.shape[2], _dtype_code(q), 1.0,
+                      *(0,) * 6)))
+
+
+def cache_attention(q: torch.Tensor, cache: torch.Tensor, seq_len: torch.Tensor,
+                    scale: Optional[float] = None, weights: Optional[torch.Tensor] = None,
+                    k_unit: float = 1.0, v_unit: float = 1.0, ws: Optional[Workspace] = None,
+                    out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None):
+    """Attention over a cache held in 4 bits: q [N, T, q_heads, d] (fp32 or bf16; the T newest tokens of
+    each sequence, which cache_append has put into the cache) over cache [N, S, kv_heads, d + 16], of which
+    seq_len [N] int32 positions are held, causal among the T -> (out like q, lse [N, T, q_heads] fp32).
+    seq_len < 0: no such sequence, its rows of ``out`` and ``lse`` stay as they are. weights [N,
+    kv_heads, S] fp32 gain what attention each position gets, summed over tokens and query heads. scale
+    defaults to 1 / sqrt(d)."""
+    dev, dt = torch.cuda.current_device(), q.dtype
+    x = _cache(cache, dev)
+    if q.dim() != 4:
+        raise ValueError("q is [sequences, tokens, q_heads, head_dim]")
+    N, d = x[0], x[3]
+    _, T, Hq, _ = q.shape
+    shape = (N, T, Hq, d)
+    _fits(N | x[1] | x[2] | T | Hq)
+    qs = _rows(q, "q", dev, dt, shape)
+    if out is None:
+        out = torch.empty(shape, dtype=dt, device=q.device)
+    os_ = _rows(out, "out", dev, dt, shape)
+    if lse is None:
+        lse = torch.empty((N, T, Hq), dtype=torch.float32, device=q.device)
+    elif lse.get_device() != dev or lse.dtype is not torch.float32 or lse.shape != (N, T, Hq) or \
+            not lse.is_contiguous():
+        _refuse(lse, "lse", dev, torch.float32, (N, T, Hq))
+    w = None if weights is None else _cache_weights(weights, x, dev)
+    desc = _CA_DESC.pack(*x, k_unit, v_unit, T, Hq, _dtype_code(q), d ** -0.5 if scale is None else scale,
+                         *_STRIDES.unpack(qs), *_STRIDES.unpack(os_))
+    if ws is None:
+        ws = Workspace(int(lib().lilicorr_cache_attention_workspace_bytes(desc)), q.device)
+    elif ws.buf.get_device() != dev:
+        _here(ws.buf, "ws", dev)
+    status = lib().lilicorr_cache_attention(desc, q.data_ptr(), cache.data_ptr(),
+                                            _seq_len(seq_len, N, dev), out.data_ptr(), lse.data_ptr(), w,
+                                            ws.buf.data_ptr(), ws.nbytes, _stream())
+    if status:
+        _check(status, "cache_attention")
+    return out, lse
+
+
+def cache_evict(cache: torch.Tensor, weights: torch.Tensor, seq_len: torch.Tensor, budget: int,
+                recent: int = 0, first: int = 0, into: Optional[torch.Tensor] = None,
+                into_weights: Optional[torch.Tensor] = None):
+    """Cut sequences of more than ``budget`` positions to so many: per kv head the ``first`` first and
+    the ``recent`` newest stay, and of the others those of the largest weights [N, kv_heads, S] fp32 (ties
+    to the lower position). What stays moves to the front, in order, weights with it: in place, or to
+    another cache ``into`` [N, S2, kv_heads, d + 16] with ``into_weights`` [N, kv_heads, S2], to which
+    shorter sequences are copied whole. Returns (kept [N, kv_heads, budget] int32, the positions that
+    stayed, then -1; new_len [N] int32). seq_len is left as it is: other layers need it."""
+    dev = torch.cuda.current_device()
+    x = _cache(cache, dev)
+    _fits(x[0] | x[1] | x[2] | budget | recent | first)
+    w = _cache_weights(weights, x, dev)
+    to = to_p = to_w = None
+    if into is not None:
+        y = _cache(into, dev, "into")
+        if into_weights is None:
+            raise ValueError("into needs into_weights")
+        to, to_p = _CACHE_DESC.pack(*y, 1.0, 1.0), into.data_ptr()
+        _fits(y[0] | y[1] | y[2])
+        to_w = _cache_weights(into_weights, y, dev, "into_weights")
+    elif into_weights is not None:
+        raise ValueError("into_weights needs into")
+    kept = torch.empty((x[0], x[2], max(budget, 0)), dtype=torch.int32, device=cache.device)
+    new_len = torch.empty((x[0],), dtype=torch.int32, device=cache.device)
+    status = lib().lilicorr_cache_evict(_CACHE_DESC.pack(*x, 1.0, 1.0), cache.data_ptr(), w,
+                                        _seq_len(seq_len, x[0], dev), budget, recent, first, to, to_p, to_w,
+                                        kept.data_ptr(), new_len.data_ptr(), _stream())
+    if status:
+        _check(status, "cache_evict")
+    return kept, new_len
 
 
 def test_linear(A: torch.Tensor, W: torch.Tensor, out_dtype=torch.float32, bias=None,
