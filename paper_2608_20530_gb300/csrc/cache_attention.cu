@@ -1,8 +1,26 @@
 // Attention over a cache held in 4 bits.
+//
+// A record's elements are products of 2 and 4 significant bits: exact in fp16. So both products run on fp16
+// matrix instructions with fp32 sums, without a rounding of keys or values: queries are brought to fp16 by a
+// power of two of their row (bf16: exact to 2^-38 of the row's largest; fp32: as three fp16 numbers that add
+// up to it), the probabilities are rounded to fp16 (for fp32 queries, kept as three numbers again).
+//
+// Products are turned round: keys (of the second product, elements) are the 16 rows of a matrix instruction,
+// query rows its 8 columns, so the few rows of a decoding step fill it, and what is read from the cache is
+// expanded once, in the registers that the instruction reads, whatever the number of rows.
+#include <float.h>
+
 #include "cache.cuh"
 
 namespace lilicorr {
 namespace {
+
+constexpr int CA_WARPS = 8;                  // of a CTA, each with its own 16 keys of a tile
+constexpr int CA_THREADS = 32 * CA_WARPS;
+constexpr int CA_KEYS = 16 * CA_WARPS;       // keys of a tile
+// Probabilities are 2^(s - m + CA_UP) with the row's reference m, which follows its maximum when that is
+// more than CA_SLACK above: at most 2^14, and fp16 numbers of full precision down to 2^-20 of 2^m.
+constexpr float CA_UP = 6.f, CA_SLACK = 8.f;
 
 struct CaArgs {
   CacheView c;
@@ -14,83 +32,858 @@ struct CaArgs {
   const int32_t* seq_len;
   float* weights;              // [N, H, S] or null
   int T, Hq, rep;
-  float scale;
+  int blocks;                  // row blocks of a (sequence, kv head)
+  int whole;                   // a CTA an item (else the list of all tiles is cut evenly)
+  float scale;                 // scale * k_unit * log2(e): scores in log2 units
+  float scale_rest;            // what its rounding left
+  float rest_ratio;            // scale_rest / scale
+  uint32_t* start;             // [N + 1] tiles before each sequence
+  float2* ml;                  // [2 * CTAs][rows of a block]: reference and sum of an item's part
+  float* po;                   // [2 * CTAs][rows of a block][DP]: its sum of p V
+  float2* rows;                // [N, T, Hq] reference and sum of whole rows, for the weights
 };
 
-__device__ __forceinline__ float ca_element(const unsigned char* half, int d, int i) {
-  const uint32_t c = (half[i / 2] >> (i % 2 * 4)) & 15u, s = half[d / 2 + i / 16];
-  const uint32_t e = (c >> 1) & 3u, f = c & 1u;
-  float x = e == 0 ? 0.5f * f : (1.f + 0.5f * f) * (float)(1 << (e - 1));
-  if (c & 8u) x = -x;
-  const uint32_t se = s >> 3, sf = s & 7u;
-  const float y = s == 127 ? NAN : se == 0 ? sf * 0x1p-9f : (8.f + sf) * exp2f((float)se - 10.f);
-  return x * y;
+// The work is the list of all (sequence, kv head, row block, tile of CA_KEYS keys), in that order; CTA b
+// takes tiles [b * per, (b + 1) * per). An item is one (sequence, kv head, block). A CTA leaves at most two
+// parts of items that other CTAs have parts of: of its first item (place 2 b) and its last (2 b + 1).
+constexpr uint32_t CA_MIN_TILES = 2;
+__device__ __forceinline__ uint32_t ca_per_cta(uint32_t tiles, uint32_t ctas) {
+  return max(CA_MIN_TILES, (tiles + ctas - 1) / ctas);
+}
+// tiles of a row block of a sequence: one even where there is no key, none where there is no sequence
+__device__ __forceinline__ int ca_tiles(int raw, int S) {
+  return raw < 0 ? 0 : max(1, (min(raw, S) + CA_KEYS - 1) / CA_KEYS);
 }
 
-// A warp a row: four elements of each key a lane, one key after the other. Then, where weights are asked
-// for, the scores once more.
-template <typename E>
-__global__ void __launch_bounds__(32) ca_simple_kernel(const CaArgs a) {
-  pdl_wait();
-  const int lane = threadIdx.x, d = a.c.d;
-  const int hq = blockIdx.x % a.Hq, nt = blockIdx.x / a.Hq, t = nt % a.T, n = nt / a.T, h = hq / a.rep;
-  const int raw = a.seq_len[n];
-  if (raw < 0) return;
-  const int seen = max(0, cache_len(raw, a.c.S) - (a.T - 1 - t));
-  const E* q = static_cast<const E*>(a.q) + n * a.q_s[0] + t * a.q_s[1] + hq * a.q_s[2];
-  float x[4], o[4] = {0.f, 0.f, 0.f, 0.f}, m = -INFINITY, l = 0.f;
-  for (int i = 0; i < 4; ++i) x[i] = lane * 4 + i < d ? ld_elem(q, lane * 4 + i) : 0.f;
-  auto score = [&](int j) {
-    const unsigned char* rec = a.c.at(n, j, h);
-    float s = 0.f;
-    for (int i = 0; i < 4; ++i)
-      if (lane * 4 + i < d) s = fmaf(x[i], ca_element(rec, d, lane * 4 + i), s);
-    return warp_sum(s) * (a.scale * a.c.k_unit);
-  };
-  for (int j = 0; j < seen; ++j) {
-    const float s = score(j), top = s > m ? s : m, f = expf(m - top), p = expf(s - top);
-    const unsigned char* rec = a.c.at(n, j, h) + cache_half_bytes(d);
-    l = l * f + p;
-    m = top;
-    for (int i = 0; i < 4; ++i)
-      if (lane * 4 + i < d) o[i] = o[i] * f + p * ca_element(rec, d, lane * 4 + i);
+// A place in the list.
+struct CaCursor {
+  int n, h, rb, tile, tiles, len;
+  __device__ __forceinline__ void sequence(const CaArgs& a, int at) {
+    n = at;
+    const int raw = a.seq_len[at];
+    len = cache_len(raw, a.c.S);
+    tiles = ca_tiles(raw, a.c.S);
   }
-  E* out = static_cast<E*>(a.out) + n * a.o_s[0] + t * a.o_s[1] + hq * a.o_s[2];
-  for (int i = 0; i < 4; ++i)
-    if (lane * 4 + i < d) st_elem(out, lane * 4 + i, seen ? o[i] / l * a.c.v_unit : 0.f);
-  const float lse = seen ? m + logf(l) : -INFINITY;
-  if (lane == 0) a.lse[(size_t)nt * a.Hq + hq] = lse;
-}
+  // the next tile; there has to be one
+  __device__ __forceinline__ void next(const CaArgs& a, int blocks) {
+    if (++tile < tiles) return;
+    tile = 0;
+    if (++rb < blocks) return;
+    rb = 0;
+    if (++h < a.c.H) return;
+    h = 0;
+    do sequence(a, n + 1); while (tiles == 0);
+  }
+};
 
-__global__ void __launch_bounds__(256) ca_simple_weights_kernel(const CaArgs a, int bf16) {
-  pdl_wait();
-  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= (size_t)a.c.N * a.c.H * a.c.S) return;
-  const int j = i % a.c.S, h = i / a.c.S % a.c.H, n = i / a.c.S / a.c.H, d = a.c.d;
-  const int raw = a.seq_len[n], L = cache_len(raw, a.c.S);
-  if (raw < 0 || j >= L) return;
-  const unsigned char* rec = a.c.at(n, j, h);
-  float sum = 0.f;
-  for (int t = max(0, a.T - L + j); t < a.T; ++t)
-    for (int r = 0; r < a.rep; ++r) {
-      const int64_t at = n * a.q_s[0] + t * a.q_s[1] + (h * a.rep + r) * a.q_s[2];
-      float s = 0.f;
-      for (int e = 0; e < d; ++e)
-        s = fmaf(bf16 ? ld_elem(static_cast<const __nv_bfloat16*>(a.q), at + e)
-                      : ld_elem(static_cast<const float*>(a.q), at + e), ca_element(rec, d, e), s);
-      const float lse = a.lse[((size_t)n * a.T + t) * a.Hq + h * a.rep + r];
-      if (fabsf(lse) < INFINITY) sum += expf(s * (a.scale * a.c.k_unit) - lse);
+// This CTA's part of the list: `count` tiles from `at` on. `keep`: the first CTA writes a.start.
+__device__ __forceinline__ uint32_t ca_range(const CaArgs& a, int blocks, bool keep, CaCursor* at,
+                                             uint32_t* first, uint32_t* total) {
+  __shared__ uint32_t sums[CA_WARPS];
+  __shared__ uint32_t place[2];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int N = a.c.N, chunk = (N + CA_THREADS - 1) / CA_THREADS;
+  const int n0 = min(N, tid * chunk), n1 = min(N, n0 + chunk);
+  const uint32_t per_tile = (uint32_t)a.c.H * blocks;
+  uint32_t mine = 0;
+  for (int n = n0; n < n1; ++n) mine += ca_tiles(a.seq_len[n], a.c.S) * per_tile;
+  uint32_t incl = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t x = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += x;
+  }
+  if (lane == 31) sums[warp] = incl;
+  __syncthreads();
+  uint32_t before = incl - mine;
+  *total = 0;
+#pragma unroll
+  for (int w = 0; w < CA_WARPS; ++w) {
+    if (w < warp) before += sums[w];
+    *total += sums[w];
+  }
+  const uint32_t per = ca_per_cta(*total, gridDim.x);
+  *first = blockIdx.x * per;
+  if (keep && blockIdx.x == 0) {
+    uint32_t b = before;
+    for (int n = n0; n < n1; ++n) {
+      a.start[n] = b;
+      b += ca_tiles(a.seq_len[n], a.c.S) * per_tile;
     }
-  a.weights[i] += sum;
+    if (tid == 0) a.start[N] = *total;
+  }
+  if (*first >= *total) return 0;
+  if (before <= *first && *first < before + mine) {  // one thread
+    uint32_t b = before;
+    for (int n = n0; n < n1; ++n) {
+      const uint32_t t = ca_tiles(a.seq_len[n], a.c.S) * per_tile;
+      if (*first < b + t) {
+        place[0] = n;
+        place[1] = *first - b;
+        break;
+      }
+      b += t;
+    }
+  }
+  __syncthreads();
+  at->sequence(a, place[0]);
+  const uint32_t item = place[1] / at->tiles;
+  at->tile = place[1] - item * at->tiles;
+  at->h = item / blocks;
+  at->rb = item - at->h * blocks;
+  return min(per, *total - *first);
 }
 
-lilicorr_status_t ca_shape(const lilicorr_cache_attention_desc* d) {
+// ------------------------------------------------------------------------------- small pieces
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+// 16 bytes to shared memory, zeros where !there
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0)
+               : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {   // an 8 x 8 matrix of 16-bit elements
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t half2_of(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ void half2_sub(uint32_t h, float& lo, float& hi) {   // what rounding to h left
+  float a, b;
+  asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %2;\n cvt.f32.f16 %0, l;\n cvt.f32.f16 %1, h;\n}"
+      : "=f"(a), "=f"(b) : "r"(h));
+  lo -= a;
+  hi -= b;
+}
+__device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+// the two codes of byte B of w
+template <int B>
+__device__ __forceinline__ uint32_t codes(uint32_t w) {
+  uint32_t r;
+  asm("{\n .reg .b8 x;\n .reg .b32 t;\n shr.u32 t, %1, %2;\n cvt.u8.u32 x, t;\n cvt.rn.f16x2.e2m1x2 %0, x;\n}"
+      : "=r"(r) : "r"(w), "n"(8 * B));
+  return r;
+}
+__device__ __forceinline__ uint32_t scales(uint32_t two) {     // of two bytes
+  uint32_t r;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)two));
+  return r;
+}
+
+// The key of row r, r < 8, of a matrix instruction; row r + 8 is the key behind it. In this order neither the
+// reads of keys (8 or 16 bytes a lane, four lanes a record) nor those of values (4 or 8 bytes a lane, eight
+// lanes a record, of every second key of the order) meet in a bank, for records of 80 and 144 bytes.
+__device__ __forceinline__ int key_of(int r) {
+  const int j = r >> 1, hi = j >> 1;
+  return 2 * (j & 1) + 8 * hi + 4 * ((r & 1) ^ hi);
+}
+
+template <typename F, int... I>
+__device__ __forceinline__ void steps(F& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+
+template <int DP>
+struct CaCfg {
+  static constexpr int KS = DP / 16;         // matrix steps of a score; tiles of 16 elements of the output
+  static constexpr int KB = DP / 8;          // key bytes a lane: elements [c * DP / 4, (c + 1) * DP / 4)
+  static constexpr int CH = (16 * (DP + 16) / 16 + 31) / 32;   // 16-byte pieces a lane of 16 records
+  static constexpr int XL = DP + 4;
+};
+
+// A lane's 16-byte pieces of 16 records (of their first `bytes` bytes).
+template <int DP>
+struct CaLane {
+  uint32_t off[CaCfg<DP>::CH];               // of its pieces of 16 records, in 16 bytes
+  int pieces, per;                           // 16-byte pieces: of 16 records, of one
+  __device__ __forceinline__ CaLane(const CaArgs& a, int bytes, int lane) {
+    per = bytes / 16;
+    pieces = 16 * per;
+#pragma unroll
+    for (int u = 0; u < CaCfg<DP>::CH; ++u) {
+      const int i = lane + 32 * u, key = i / per;
+      off[u] = (uint32_t)(key * (a.c.s[1] >> 4)) + (i - key * per);
+    }
+  }
+  // the 16 records from key k on, of `len` keys
+  __device__ __forceinline__ void copy(const CaArgs& a, int n, int h, int k, int len, uint32_t dst,
+                                       int lane) const {
+    const unsigned char* base = a.c.at(n, k, h);
+    if (k + 16 <= len) {
+#pragma unroll
+      for (int u = 0; u < CaCfg<DP>::CH; ++u)
+        if (lane + 32 * u < pieces) copy16(dst + (lane + 32 * u) * 16, base + (size_t)off[u] * 16, true);
+    } else {
+#pragma unroll
+      for (int u = 0; u < CaCfg<DP>::CH; ++u)
+        if (lane + 32 * u < pieces) {
+          const bool there = k + (lane + 32 * u) / per < len;
+          copy16(dst + (lane + 32 * u) * 16, there ? base + (size_t)off[u] * 16 : a.q, there);
+        }
+    }
+  }
+};
+
+// A lane's part of the keys of a matrix instruction: rows g and g + 8, all steps.
+template <int DP>
+struct CaKeyPart {
+  uint32_t w[2][DP / 32 < 1 ? 1 : DP / 32];  // codes, 8 a word
+  uint32_t s[2];                             // scales as fp16: DP 128 of two groups, else of one, twice
+  __device__ __forceinline__ void load(const unsigned char* rec, int R, int d, int c, uint32_t mask) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const unsigned char* p = rec + e * R + c * CaCfg<DP>::KB;
+      if constexpr (DP == 128) {
+        const uint4 x = *reinterpret_cast<const uint4*>(p);
+        w[e][0] = x.x; w[e][1] = x.y; w[e][2] = x.z; w[e][3] = x.w;
+        s[e] = scales(*reinterpret_cast<const uint16_t*>(rec + e * R + d / 2 + 2 * c) & mask);
+      } else {
+        if constexpr (DP == 64) {
+          const uint2 x = *reinterpret_cast<const uint2*>(p);
+          w[e][0] = x.x; w[e][1] = x.y;
+        } else {
+          w[e][0] = *reinterpret_cast<const uint32_t*>(p);
+        }
+        const uint32_t b = rec[e * R + d / 2 + (DP == 64 ? c : c >> 1)] & mask;
+        s[e] = scales(b | b << 8);
+      }
+    }
+  }
+  // the operand of step ks: a[0], a[2] of row g, a[1], a[3] of row g + 8
+  template <int ks>
+  __device__ __forceinline__ void operand(uint32_t (&a)[4]) const {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      uint32_t f = s[e];
+      if constexpr (DP == 128) f = __byte_perm(f, f, ks < 4 ? 0x1010 : 0x3232);
+      a[e] = mul2(codes<ks % 2 * 2>(w[e][ks / 2]), f);
+      a[e + 2] = mul2(codes<ks % 2 * 2 + 1>(w[e][ks / 2]), f);
+    }
+  }
+};
+// bytes of a lane's key scales that exist
+template <int DP>
+__device__ __forceinline__ uint32_t key_scale_mask(int d, int c) {
+  const int G = d / 16;
+  if (DP == 128) return (2 * c < G ? 0xFFu : 0u) | (2 * c + 1 < G ? 0xFF00u : 0u);
+  return (DP == 64 ? c : c >> 1) < G ? 0xFFu : 0u;
+}
+
+__device__ __forceinline__ void load16b(const float* p, float* x) {
+  const float4 v = *reinterpret_cast<const float4*>(p);
+  x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+}
+__device__ __forceinline__ void load16b(const __nv_bfloat16* p, float* x) {
+  const uint4 v = *reinterpret_cast<const uint4*>(p);
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(w[i] << 16);
+    x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+  }
+}
+// Queries as the second operand: of column g (row `row` of the item, or none) elements c * DP / 4 ..,
+// brought to fp16 by 2^(the result) of their row, in PIECES numbers that add up to them.
+template <int DP, int PIECES, typename E>
+__device__ __forceinline__ int load_query(const E* q, int d, int c, uint32_t (*b)[CaCfg<DP>::KS][2]) {
+  float x[DP / 4];
+  float top = 0.f;
+#pragma unroll
+  for (int i = 0; i < DP / 4; i += 16 / (int)sizeof(E)) {
+    const int at = c * (DP / 4) + i;
+    if (q && at < d) {
+      load16b(q + at, x + i);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 16 / (int)sizeof(E); ++j) x[i + j] = 0.f;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < DP / 4; ++i) top = fmaxf(top, fabsf(x[i]));
+  top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+  top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+  // 2^13 <= top * 2^up < 2^14; an infinity or a row of zeros stays as it is
+  const int up = top > 0.f && top < INFINITY ? 13 - ilogbf(top) : 0;
+#pragma unroll
+  for (int i = 0; i < DP / 4; i += 2) {
+    float lo = ldexpf(x[i], up), hi = ldexpf(x[i + 1], up);
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+      const uint32_t h = half2_of(lo, hi);
+      b[p][i / 4][i / 2 % 2] = h;
+      half2_sub(h, lo, hi);
+    }
+  }
+  return up;
+}
+
+// ------------------------------------------------------------------------------- the kernel
+template <int DP, int NT, int PIECES>
+struct CaSmem {
+  static constexpr bool QS = NT * PIECES > 1;            // queries in shared memory
+  static constexpr int STAGES = NT * PIECES > 1 ? 3 : 4;
+  static constexpr int STAGE = 16 * (DP + 16);           // bytes of a warp's 16 records
+  static constexpr int XO = CA_WARPS * 8 * CaCfg<DP>::XL * 4;
+  static constexpr int XM = CA_WARPS * 8 * 8;
+  static constexpr int Q = QS ? NT * PIECES * CaCfg<DP>::KS * 256 : 0;
+  static constexpr int AT_XO = CA_WARPS * STAGES * STAGE + 64;   // (lanes past a narrow record's end read on)
+  static constexpr int AT_XM = AT_XO + XO;
+  static constexpr int AT_Q = AT_XM + XM;
+  static constexpr int TOTAL = AT_Q + Q;
+};
+
+template <typename E>
+__device__ __forceinline__ void store4(E* p, const float4& v) {
+  if constexpr (sizeof(E) == 4) *reinterpret_cast<float4*>(p) = v;
+  else *reinterpret_cast<uint2*>(p) = make_uint2(bf16_pack2(v.x, v.y), bf16_pack2(v.z, v.w));
+}
+// a row's result from its reference, sum and the lane's four sums of p V
+template <typename E>
+__device__ __forceinline__ void ca_write(const CaArgs& a, int n, int t, int hq, float m, float l, float4 o,
+                                         int lane) {
+  E* out = static_cast<E*>(a.out) + n * a.o_s[0] + t * a.o_s[1] + hq * a.o_s[2];
+  const float f = l == 0.f ? 0.f : a.c.v_unit / l;
+  if (lane * 4 < a.c.d) store4(out + lane * 4, make_float4(o.x * f, o.y * f, o.z * f, o.w * f));
+  // the scores were taken in units that their factor's rounding moved
+  if (lane == 0) {
+    const size_t row = ((size_t)n * a.T + t) * a.Hq + hq;
+    a.lse[row] = l == 0.f ? -INFINITY
+                          : fmaf(fmaf(m, a.rest_ratio, m), 0.69314718f, fmaf(-CA_UP, 0.69314718f, logf(l)));
+    if (a.weights) a.rows[row] = make_float2(m, l);
+  }
+}
+
+template <int DP, int NT, int PIECES, typename E>
+__global__ void __launch_bounds__(CA_THREADS, NT * PIECES > 3 || NT > 2 ? 1 : 2)
+cache_attention_kernel(const CaArgs a) {
+  pdl_wait();
+  using Cfg = CaCfg<DP>;
+  using Sm = CaSmem<DP, NT, PIECES>;
+  constexpr int KS = Cfg::KS, ST = Sm::STAGES, ROWS = 8 * NT;
+  extern __shared__ __align__(16) unsigned char sm[];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
+  const int d = a.c.d, R = cache_record_bytes(d), half = cache_half_bytes(d), rows = a.T * a.rep;
+
+  CaCursor at;
+  uint32_t first = 0, total = 0, count;
+  if (a.whole) {
+    const int item = blockIdx.x, per_n = a.c.H * a.blocks;
+    at.sequence(a, item / per_n);
+    at.h = item % per_n / a.blocks;
+    at.rb = item % a.blocks;
+    at.tile = 0;
+    count = at.tiles;
+  } else {
+    count = ca_range(a, a.blocks, true, &at, &first, &total);
+  }
+  if (count == 0) return;
+
+  const CaLane<DP> mine(a, R, lane);
+  unsigned char* stage = sm + warp * ST * Sm::STAGE;
+  CaCursor ahead = at;                               // of the copies
+  uint32_t copied = 0;
+  auto copy_next = [&] {
+    if (copied < count) {
+      mine.copy(a, ahead.n, ahead.h, ahead.tile * CA_KEYS + warp * 16, ahead.len,
+                smem_u32(stage + copied % ST * Sm::STAGE), lane);
+      if (++copied < count) ahead.next(a, a.blocks);
+    }
+    copy_commit();
+  };
+#pragma unroll
+  for (int i = 0; i < ST - 1; ++i) copy_next();
+
+  // where this lane's keys and values lie in a warp's 16 records
+  const int key = key_of(g), va = key_of(2 * c), vb = key_of(2 * c + 1);
+  const uint32_t kmask = key_scale_mask<DP>(d, c);
+  const int vg = DP == 128 ? g : DP == 64 ? g >> 1 : g >> 2;   // the scale group of its values
+  const bool vthere = vg < d / 16;
+  const int vbyte = vthere ? g * (DP / 16) : 0;
+
+  uint32_t qr[Sm::QS ? 1 : PIECES][KS][2];
+  uint2* qs = reinterpret_cast<uint2*>(sm + Sm::AT_Q);         // [NT][PIECES][KS][lane]
+  float m[NT][2], l[NT][2], f[NT][2], fr[NT][2];               // f: a row's factor; fr: what it lacks
+  int lim[NT][2];
+  float o[KS][NT][4];
+  uint32_t done = 0;
+  bool fresh = true;
+  while (done < count) {
+    if (fresh) {                                     // an item begins
+      fresh = false;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const int r = at.rb * ROWS + nt * 8 + g, t = r / a.rep;
+        const E* q = r < rows ? static_cast<const E*>(a.q) + at.n * a.q_s[0] + t * a.q_s[1] +
+                                    (at.h * a.rep + (r - t * a.rep)) * a.q_s[2]
+                              : nullptr;
+        uint32_t qb[PIECES][KS][2];
+        const int up = load_query<DP, PIECES, E>(q, d, c, qb);
+        if constexpr (Sm::QS) {
+          if (warp == 0)
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p)
+#pragma unroll
+              for (int i = 0; i < KS; ++i)
+                qs[((nt * PIECES + p) * KS + i) * 32 + lane] = make_uint2(qb[p][i][0], qb[p][i][1]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < KS; ++i) { qr[0][i][0] = qb[0][i][0]; qr[0][i][1] = qb[0][i][1]; }
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {                // this lane's columns
+          const int col = 2 * c + e, rr = at.rb * ROWS + nt * 8 + col;
+          const int u = __shfl_sync(0xffffffffu, up, col * 4);
+          f[nt][e] = ldexpf(a.scale, -u);
+          fr[nt][e] = ldexpf(a.scale_rest, -u);
+          lim[nt][e] = rr < rows ? max(0, at.len - (a.T - 1 - rr / a.rep)) : 0;
+          m[nt][e] = -FLT_MAX;
+          l[nt][e] = 0.f;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < KS; ++i)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[i][nt][e] = 0.f;
+      if constexpr (Sm::QS) __syncthreads();
+    }
+    copy_wait<ST - 2>();
+    __syncwarp();
+    const unsigned char* rec = stage + done % ST * Sm::STAGE;
+    const int k0 = at.tile * CA_KEYS + warp * 16;
+
+    // ---- scores
+    float s[NT][4];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
+    {
+      CaKeyPart<DP> kp;
+      kp.load(rec + key * R, R, d, c, kmask);
+      auto step = [&](auto ks) {
+        constexpr int i = decltype(ks)::value;
+        uint32_t ka[4];
+        kp.template operand<i>(ka);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int p = PIECES - 1; p >= 0; --p) {    // the smallest parts first
+            if constexpr (Sm::QS) {
+              const uint2 b = qs[((nt * PIECES + p) * KS + i) * 32 + lane];
+              mma(s[nt], ka, b.x, b.y);
+            } else {
+              mma(s[nt], ka, qr[p][i][0], qr[p][i][1]);
+            }
+          }
+      };
+      steps(step, std::make_integer_sequence<int, KS>{});
+    }
+    if (k0 + 16 > at.len - (a.T - 1)) {              // some row may not see all of these keys
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (k0 + key + (e >> 1) >= lim[nt][e & 1]) s[nt][e] = -INFINITY;
+    }
+    // ---- probabilities: the reference moves when some row of the warp's has left it behind
+    bool up = false;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) up |= fmaf(s[nt][e], f[nt][e & 1], -m[nt][e & 1]) > CA_SLACK;
+    if (__any_sync(0xffffffffu, up)) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float top = fmaxf(s[nt][e], s[nt][e + 2]) * f[nt][e];
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+          const float to = fmaxf(m[nt][e], top), x = ex2(m[nt][e] - to);
+          m[nt][e] = to;
+          l[nt][e] *= x;
+#pragma unroll
+          for (int i = 0; i < KS; ++i) {
+            o[i][nt][e] *= x;
+            o[i][nt][e + 2] *= x;
+          }
+        }
+    }
+    uint32_t pb[NT][PIECES][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      float p[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float x = CA_UP - m[nt][e & 1];
+        // (a key that is not seen: no infinity times what the factor lacks, which has either sign)
+        if (PIECES > 1) x = fmaf(fmaxf(s[nt][e], -FLT_MAX), fr[nt][e & 1], x);
+        p[e] = ex2(fmaf(s[nt][e], f[nt][e & 1], x));
+      }
+      l[nt][0] += p[0] + p[2];
+      l[nt][1] += p[1] + p[3];
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) {
+        const uint32_t x = half2_of(p[0], p[1]), y = half2_of(p[2], p[3]);
+        pb[nt][i][0] = transpose8(x);
+        pb[nt][i][1] = transpose8(y);
+        if (PIECES > 1) {
+          half2_sub(x, p[0], p[1]);
+          half2_sub(y, p[2], p[3]);
+        }
+      }
+    }
+    // ---- sums of p V: two keys a register, so the codes of two records go together, byte by byte
+    {
+      const unsigned char* v = rec + half;
+      uint32_t fs[2], w[4][DP / 128 < 1 ? 1 : 2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const unsigned char *pa = v + (va + e) * R, *pb2 = v + (vb + e) * R;
+        if constexpr (DP == 128) {
+          const uint2 x = *reinterpret_cast<const uint2*>(pa + vbyte), y = *reinterpret_cast<const uint2*>(pb2 + vbyte);
+          w[2 * e][0] = x.x; w[2 * e][1] = x.y;
+          w[2 * e + 1][0] = y.x; w[2 * e + 1][1] = y.y;
+        } else if constexpr (DP == 64) {
+          w[2 * e][0] = *reinterpret_cast<const uint32_t*>(pa + vbyte);
+          w[2 * e + 1][0] = *reinterpret_cast<const uint32_t*>(pb2 + vbyte);
+        } else {
+          w[2 * e][0] = *reinterpret_cast<const uint16_t*>(pa + vbyte);
+          w[2 * e + 1][0] = *reinterpret_cast<const uint16_t*>(pb2 + vbyte);
+        }
+        uint32_t b = pa[d / 2 + vg] | (uint32_t)pb2[d / 2 + vg] << 8;
+        if (!vthere) b = 0;
+        fs[e] = scales(b);
+      }
+      auto step = [&](auto is) {
+        constexpr int i = decltype(is)::value, word = i / 4, byte = i % 4;
+        uint32_t oa[4];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t x = w[2 * e][word], y = w[2 * e + 1][word];
+          const uint32_t even = (x & 0x0F0F0F0Fu) | ((y << 4) & 0xF0F0F0F0u);
+          const uint32_t odd = ((x >> 4) & 0x0F0F0F0Fu) | (y & 0xF0F0F0F0u);
+          oa[2 * e] = mul2(codes<byte>(even), fs[e]);
+          oa[2 * e + 1] = mul2(codes<byte>(odd), fs[e]);
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int p = PIECES - 1; p >= 0; --p) mma(o[i][nt], oa, pb[nt][p][0], pb[nt][p][1]);
+      };
+      steps(step, std::make_integer_sequence<int, KS>{});
+    }
+    __syncwarp();                                    // the records' place is free
+    copy_next();
+    ++done;
+    const bool last = at.tile + 1 == at.tiles;
+    if (!last && done < count) {
+      ++at.tile;
+      continue;
+    }
+
+    // ---- the warps' parts of an item come together, 8 rows at a time, a warp a row
+    const uint32_t item_start = first + done - 1 - at.tile;    // its first tile in the list (mod 2^32)
+    const bool complete = a.whole || (last && item_start >= first);
+    float* xo = reinterpret_cast<float*>(sm + Sm::AT_XO);      // [warp][row][XL]
+    float2* xm = reinterpret_cast<float2*>(sm + Sm::AT_XM);
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float x = l[nt][e];
+        x += __shfl_xor_sync(0xffffffffu, x, 4);
+        x += __shfl_xor_sync(0xffffffffu, x, 8);
+        x += __shfl_xor_sync(0xffffffffu, x, 16);
+        if (g == 0) xm[warp * 8 + 2 * c + e] = make_float2(m[nt][e], x);
+        float* y = xo + (warp * 8 + 2 * c + e) * Cfg::XL + g * (DP / 8);
+#pragma unroll
+        for (int i = 0; i < KS; i += 2)
+          *reinterpret_cast<float4*>(y + 2 * i) =
+              make_float4(o[i][nt][e], o[i][nt][e + 2], o[i + 1][nt][e], o[i + 1][nt][e + 2]);
+      }
+      __syncthreads();
+      const int r = at.rb * ROWS + nt * 8 + warp;
+      if (r < rows) {
+        float M = -FLT_MAX, L = 0.f;
+#pragma unroll
+        for (int w = 0; w < CA_WARPS; ++w) M = fmaxf(M, xm[w * 8 + warp].x);
+        float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < CA_WARPS; ++w) {
+          const float2 z = xm[w * 8 + warp];
+          const float x = ex2(z.x - M);
+          L = fmaf(x, z.y, L);
+          if (lane < DP / 4) {
+            const float4 v = *reinterpret_cast<const float4*>(xo + (w * 8 + warp) * Cfg::XL + lane * 4);
+            y.x = fmaf(x, v.x, y.x);
+            y.y = fmaf(x, v.y, y.y);
+            y.z = fmaf(x, v.z, y.z);
+            y.w = fmaf(x, v.w, y.w);
+          }
+        }
+        if (complete) {
+          const int t = r / a.rep;
+          ca_write<E>(a, at.n, t, at.h * a.rep + (r - t * a.rep), M, L, y, lane);
+        } else {
+          const size_t place = ((size_t)2 * blockIdx.x + (item_start > first)) * ROWS + nt * 8 + warp;
+          if (lane == 0) a.ml[place] = make_float2(M, L);
+          if (lane < DP / 4) *reinterpret_cast<float4*>(a.po + place * DP + lane * 4) = y;
+        }
+      }
+    }
+    if (done < count) {
+      at.next(a, a.blocks);
+      fresh = true;
+      if constexpr (Sm::QS) __syncthreads();
+    }
+  }
+  copy_wait<0>();
+}
+
+// The items that several CTAs have parts of: CTA j here looks at the border between CTAs j and j + 1 of the
+// list, and joins the parts of the item there, if that is the item's first border. A warp a row.
+template <int DP, int NT, typename E>
+__global__ void __launch_bounds__(128) cache_attention_join_kernel(const CaArgs a) {
+  pdl_wait();
+  constexpr int ROWS = 8 * NT;
+  __shared__ int found;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, N = a.c.N;
+  const uint32_t total = a.start[N], ctas = gridDim.x + 1, per = ca_per_cta(total, ctas);
+  const uint32_t x = (blockIdx.x + 1) * per;
+  if (x >= total) return;
+  for (int n = tid; n < N; n += 128)
+    if (a.start[n] <= x && x < a.start[n + 1]) found = n;
+  __syncthreads();
+  const int n = found;
+  const uint32_t s0 = a.start[n], tiles = (a.start[n + 1] - s0) / (uint32_t)(a.c.H * a.blocks);
+  const uint32_t item = (x - s0) / tiles, s = s0 + item * tiles, e = s + tiles;
+  const uint32_t b0 = s / per, b1 = (e - 1) / per;
+  if (x == s || b0 != blockIdx.x) return;
+  const int h = item / a.blocks, rb = item - h * a.blocks, rows = a.T * a.rep;
+  for (int i = warp; i < ROWS; i += 4) {
+    const int r = rb * ROWS + i;
+    if (r >= rows) break;
+    auto place = [&](uint32_t b) { return ((size_t)2 * b + (b * per < s)) * ROWS + i; };
+    float M = -FLT_MAX, L = 0.f;
+    for (uint32_t b = b0 + lane; b <= b1; b += 32) M = fmaxf(M, a.ml[place(b)].x);
+    M = warp_max(M);
+    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (uint32_t b = b0; b <= b1; ++b) {
+      const size_t p = place(b);
+      const float2 z = a.ml[p];
+      const float f = ex2(z.x - M);
+      L = fmaf(f, z.y, L);
+      if (lane < DP / 4) {
+        const float4 v = *reinterpret_cast<const float4*>(a.po + p * DP + lane * 4);
+        y.x = fmaf(f, v.x, y.x);
+        y.y = fmaf(f, v.y, y.y);
+        y.z = fmaf(f, v.z, y.z);
+        y.w = fmaf(f, v.w, y.w);
+      }
+    }
+    const int t = r / a.rep;
+    ca_write<E>(a, n, t, h * a.rep + (r - t * a.rep), M, L, y, lane);
+  }
+}
+
+// What each key gets: the scores once more, against their rows' references and sums, a warp 16 keys; rows go
+// through shared memory 8 NT at a time, and each key's weight is read and written by one lane.
+template <int DP, int NT, int PIECES, typename E>
+__global__ void __launch_bounds__(CA_THREADS, 2) cache_attention_weights_kernel(const CaArgs a) {
+  pdl_wait();
+  constexpr int KS = CaCfg<DP>::KS, ST = 4, ROWS = 8 * NT, STAGE = 16 * (DP / 2 + 16);
+  extern __shared__ __align__(16) unsigned char sm[];
+  uint2* qs = reinterpret_cast<uint2*>(sm + CA_WARPS * ST * STAGE);      // [NT][PIECES][KS][lane]
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
+  const int d = a.c.d, R = (cache_half_bytes(d) + 15) / 16 * 16, rows = a.T * a.rep;
+  CaCursor at;
+  uint32_t first, total;
+  uint32_t count = ca_range(a, 1, false, &at, &first, &total);
+  const CaLane<DP> mine(a, R, lane);
+  unsigned char* stage = sm + warp * ST * STAGE;
+  const int key = key_of(g);
+  const uint32_t kmask = key_scale_mask<DP>(d, c);
+  while (count > 0) {
+    const int tile0 = at.tile, tile1 = min((uint32_t)at.tiles, tile0 + count);
+    for (int r0 = 0; r0 < rows; r0 += ROWS) {
+      __syncthreads();
+      float f[NT][2], fr[NT][2], ref[NT][2], inv[NT][2];
+      int lim[NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const int r = r0 + nt * 8 + g, t = r / a.rep, hq = at.h * a.rep + (r - t * a.rep);
+        float2 ml = make_float2(0.f, 0.f);
+        if (r < rows) ml = a.rows[((size_t)at.n * a.T + t) * a.Hq + hq];
+        // rows without keys, or without a finite sum, add nothing
+        const bool there = ml.y > 0.f && ml.y < INFINITY && fabsf(ml.x) < INFINITY;
+        uint32_t qb[PIECES][KS][2];
+        const int up = load_query<DP, PIECES, E>(
+            there ? static_cast<const E*>(a.q) + at.n * a.q_s[0] + t * a.q_s[1] + hq * a.q_s[2] : nullptr, d, c,
+            qb);
+        if (warp == nt % CA_WARPS)
+#pragma unroll
+          for (int p = 0; p < PIECES; ++p)
+#pragma unroll
+            for (int i = 0; i < KS; ++i)
+              qs[((nt * PIECES + p) * KS + i) * 32 + lane] = make_uint2(qb[p][i][0], qb[p][i][1]);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int col = 2 * c + e, rr = r0 + nt * 8 + col;
+          const int u = __shfl_sync(0xffffffffu, up, col * 4);
+          const float m = __shfl_sync(0xffffffffu, ml.x, col * 4);
+          const bool ok = __shfl_sync(0xffffffffu, there, col * 4);
+          const float l = __shfl_sync(0xffffffffu, ml.y, col * 4);
+          f[nt][e] = ldexpf(a.scale, -u);
+          fr[nt][e] = ldexpf(a.scale_rest, -u);
+          ref[nt][e] = CA_UP - m;
+          inv[nt][e] = 1.f / l;
+          lim[nt][e] = ok ? max(0, at.len - (a.T - 1 - rr / a.rep)) : 0;
+        }
+      }
+      int ahead = tile0;
+      auto copy_next = [&] {
+        if (ahead < tile1)
+          mine.copy(a, at.n, at.h, ahead * CA_KEYS + warp * 16, at.len, smem_u32(stage + ahead % ST * STAGE), lane);
+        ++ahead;
+        copy_commit();
+      };
+#pragma unroll
+      for (int i = 0; i < ST - 1; ++i) copy_next();
+      __syncthreads();
+      for (int tile = tile0; tile < tile1; ++tile) {
+        copy_wait<ST - 2>();
+        __syncwarp();
+        const int k0 = tile * CA_KEYS + warp * 16;
+        float s[NT][4];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
+        CaKeyPart<DP> kp;
+        kp.load(stage + tile % ST * STAGE + key * R, R, d, c, kmask);
+        auto step = [&](auto ks) {
+          constexpr int i = decltype(ks)::value;
+          uint32_t ka[4];
+          kp.template operand<i>(ka);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int p = PIECES - 1; p >= 0; --p) {
+              const uint2 b = qs[((nt * PIECES + p) * KS + i) * 32 + lane];
+              mma(s[nt], ka, b.x, b.y);
+            }
+        };
+        steps(step, std::make_integer_sequence<int, KS>{});
+        float sum[2] = {0.f, 0.f};
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float x = ref[nt][e & 1];
+            if (PIECES > 1) x = fmaf(s[nt][e], fr[nt][e & 1], x);
+            const float p = ex2(fmaf(s[nt][e], f[nt][e & 1], x));
+            if (k0 + key + (e >> 1) < lim[nt][e & 1]) sum[e >> 1] = fmaf(p, inv[nt][e & 1], sum[e >> 1]);
+          }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          sum[e] += __shfl_xor_sync(0xffffffffu, sum[e], 1);
+          sum[e] += __shfl_xor_sync(0xffffffffu, sum[e], 2);
+        }
+        if (c < 2 && k0 + key + c < at.len)
+          a.weights[((size_t)at.n * a.c.H + at.h) * a.c.S + k0 + key + c] += c ? sum[1] : sum[0];
+        __syncwarp();
+        copy_next();
+      }
+      copy_wait<0>();
+    }
+    count -= tile1 - tile0;
+    if (count > 0) {
+      at.tile = tile1 - 1;
+      at.next(a, 1);
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------- the call
+struct CaPlan {
+  int dp, nt, pieces, blocks, ctas;
+  bool whole;
+  size_t items, start_off, ml_off, po_off, rows_off, total;
+};
+
+lilicorr_status_t ca_plan(const lilicorr_cache_attention_desc* d, CaPlan* p) {
   if (!d) return LILICORR_ERR_ARG;
   LL_TRY(cache_shape(&d->cache));
   if (d->dtype != LILICORR_F32 && d->dtype != LILICORR_BF16) return LILICORR_ERR_DTYPE;
-  if (d->tokens < 1 || d->q_heads < 1 || d->q_heads % d->cache.kv_heads) return LILICORR_ERR_SHAPE;
-  if ((double)d->cache.sequences * d->tokens * d->q_heads >= 2147483648.0) return LILICORR_ERR_SHAPE;
+  const lilicorr_cache_desc& c = d->cache;
+  if (d->tokens < 1 || d->q_heads < 1 || d->q_heads % c.kv_heads) return LILICORR_ERR_SHAPE;
+  const double all = (double)c.sequences * d->tokens * d->q_heads;
+  if (all >= 2147483648.0) return LILICORR_ERR_SHAPE;
+  const int rows = d->tokens * (d->q_heads / c.kv_heads);
+  p->dp = c.head_dim <= 32 ? 32 : c.head_dim <= 64 ? 64 : 128;
+  p->pieces = d->dtype == LILICORR_BF16 ? 1 : 3;
+  p->nt = rows <= 8 ? 1 : rows <= 16 || p->pieces > 1 ? 2 : 4;
+  p->blocks = (rows + 8 * p->nt - 1) / (8 * p->nt);
+  const int tiles = c.capacity <= CA_KEYS ? 1 : (c.capacity + CA_KEYS - 1) / CA_KEYS;
+  p->items = (size_t)c.sequences * c.kv_heads * p->blocks;
+  if ((double)p->items * tiles >= 2147483648.0) return LILICORR_ERR_SHAPE;
+  p->ctas = num_sms() * (p->nt * p->pieces > 3 || p->nt > 2 ? 1 : 2);
+  p->whole = tiles <= 4;
+  const size_t parts = p->whole ? 0 : (size_t)2 * p->ctas * 8 * p->nt;
+  p->start_off = 256;
+  p->ml_off = p->start_off + align_up(((size_t)c.sequences + 1) * 4, 256);
+  p->po_off = p->ml_off + align_up(parts * sizeof(float2), 256);
+  p->rows_off = p->po_off + parts * p->dp * sizeof(float);
+  p->total = p->rows_off + align_up((size_t)all * sizeof(float2), 256);
   return LILICORR_OK;
+}
+
+template <int DP, int NT, int PIECES, typename E>
+lilicorr_status_t ca_launch(const CaArgs& a, const CaPlan& p, cudaStream_t st) {
+  static bool configured[64] = {false}, configured_w[64] = {false};
+  auto* kernel = cache_attention_kernel<DP, NT, PIECES, E>;
+  LL_TRY(allow_max_dynamic_smem(kernel, configured));
+  LL_TRY(launch_k(kernel, p.whole ? (unsigned)p.items : (unsigned)p.ctas, CA_THREADS, CaSmem<DP, NT, PIECES>::TOTAL,
+                  st, a));
+  if (!p.whole)
+    LL_TRY(launch_k(cache_attention_join_kernel<DP, NT, E>, (unsigned)p.ctas - 1, 128, 0, st, a));
+  if (!a.weights) return LILICORR_OK;
+  constexpr int WT = PIECES > 1 ? 1 : NT;
+  auto* weights = cache_attention_weights_kernel<DP, WT, PIECES, E>;
+  LL_TRY(allow_max_dynamic_smem(weights, configured_w));
+  const size_t smem = CA_WARPS * 4 * 16 * (DP / 2 + 16) + WT * PIECES * (DP / 16) * 256;
+  return launch_k(weights, (unsigned)(2 * num_sms()), CA_THREADS, smem, st, a);
+}
+
+template <int DP>
+lilicorr_status_t ca_launch_rows(const CaArgs& a, const CaPlan& p, cudaStream_t st) {
+  if (p.pieces > 1)
+    return p.nt == 1 ? ca_launch<DP, 1, 3, float>(a, p, st) : ca_launch<DP, 2, 3, float>(a, p, st);
+  return p.nt == 1   ? ca_launch<DP, 1, 1, __nv_bfloat16>(a, p, st)
+         : p.nt == 2 ? ca_launch<DP, 2, 1, __nv_bfloat16>(a, p, st)
+                     : ca_launch<DP, 4, 1, __nv_bfloat16>(a, p, st);
 }
 
 }  // namespace
@@ -101,16 +894,18 @@ using namespace lilicorr;
 extern "C" {
 
 size_t lilicorr_cache_attention_workspace_bytes(const lilicorr_cache_attention_desc* desc) {
-  return ca_shape(desc) == LILICORR_OK ? 256 : 0;
+  CaPlan p;
+  return ca_plan(desc, &p) == LILICORR_OK ? p.total : 0;
 }
 
 lilicorr_status_t lilicorr_cache_attention(const lilicorr_cache_attention_desc* desc, const void* q,
                                            const void* cache, const int32_t* seq_len, void* out,
                                            float* lse, float* weights, void* ws, size_t ws_bytes,
                                            cudaStream_t stream) {
-  LL_TRY(ca_shape(desc));
-  const float scale = desc->scale;
-  if (!(scale > 0.f) || !((double)scale * desc->cache.k_unit < 0x1p100)) return LILICORR_ERR_ARG;
+  CaPlan p;
+  LL_TRY(ca_plan(desc, &p));
+  const double scale = (double)desc->scale * desc->cache.k_unit;
+  if (!(scale > 0.0) || !(scale < 0x1p100)) return LILICORR_ERR_ARG;
   CaArgs a;
   memset(&a, 0, sizeof(a));
   LL_TRY(cache_view(&desc->cache, cache, false, &a.c));
@@ -122,7 +917,8 @@ lilicorr_status_t lilicorr_cache_attention(const lilicorr_cache_attention_desc* 
   if (!cache_rows_ok(desc->q_stride, e, per16, a.c.d, false) ||
       !cache_rows_ok(desc->out_stride, e, per16, a.c.d, true))
     return LILICORR_ERR_ARG;
-  if (ws_bytes < 256) return LILICORR_ERR_WORKSPACE;
+  if (ws_bytes < p.total) return LILICORR_ERR_WORKSPACE;
+  unsigned char* w = static_cast<unsigned char*>(ws);
   a.q = q;
   a.out = out;
   for (int i = 0; i < 3; ++i) {
@@ -135,15 +931,19 @@ lilicorr_status_t lilicorr_cache_attention(const lilicorr_cache_attention_desc* 
   a.T = desc->tokens;
   a.Hq = desc->q_heads;
   a.rep = desc->q_heads / a.c.H;
-  a.scale = scale;
-  const bool bf = desc->dtype == LILICORR_BF16;
-  const unsigned grid = (unsigned)(e[0] * e[1] * e[2]);
-  if (bf) LL_TRY(launch_k(ca_simple_kernel<__nv_bfloat16>, grid, 32, 0, stream, a));
-  else LL_TRY(launch_k(ca_simple_kernel<float>, grid, 32, 0, stream, a));
-  const size_t keys = (size_t)a.c.N * a.c.H * a.c.S;
-  if (!weights || !keys) return LILICORR_OK;
-  if ((keys + 255) / 256 > 0x7FFFFFFFull) return LILICORR_ERR_SHAPE;
-  return launch_k(ca_simple_weights_kernel, (unsigned)((keys + 255) / 256), 256, 0, stream, a, (int)bf);
+  a.blocks = p.blocks;
+  a.whole = p.whole;
+  const double log2e = 1.4426950408889634 * scale;
+  a.scale = (float)log2e;
+  a.scale_rest = (float)(log2e - a.scale);
+  a.rest_ratio = (float)((log2e - a.scale) / log2e);
+  a.start = reinterpret_cast<uint32_t*>(w + p.start_off);
+  a.ml = reinterpret_cast<float2*>(w + p.ml_off);
+  a.po = reinterpret_cast<float*>(w + p.po_off);
+  a.rows = reinterpret_cast<float2*>(w + p.rows_off);
+  return p.dp == 32   ? ca_launch_rows<32>(a, p, stream)
+         : p.dp == 64 ? ca_launch_rows<64>(a, p, stream)
+                      : ca_launch_rows<128>(a, p, stream);
 }
 
 }  // extern "C"
