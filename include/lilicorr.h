@@ -444,7 +444,7 @@ lilicorr_status_t lilicorr_prefix_attention(const lilicorr_prefix_attention_desc
  * from 2^-60 to 2^60, the same in every call on a cache: 1, unless the values lie far from 1 (a group's
  * scale is a multiple of 2^-9, and a value is cut at 2688 units).
  * A cache is [sequences, capacity, kv_heads] records, 16-byte aligned, the strides in bytes, multiples of 16
- * and not negative. Where it is written no two of its records may overlap. head_dim is a multiple of 16 up
+ * and not negative (of positions below 2^28). Where it is written no two of its records may overlap. head_dim is a multiple of 16 up
  * to 128, capacity at most 2^30. Sequence n holds the positions below seq_len[n] (int32, on the device),
  * clipped to [0, capacity]; below 0 there is no such sequence. What lies behind is not looked at.
  * weights [sequences, kv_heads, capacity] fp32, where there are any, hold what attention each key has

@@ -32,6 +32,7 @@ lilicorr_status_t cache_view(const lilicorr_cache_desc* d, const void* cache, bo
   if (d->sequences && d->capacity && (!cache || !aligned16(cache))) return LILICORR_ERR_ARG;
   const int64_t e[3] = {d->sequences, d->capacity, d->kv_heads};
   if (!cache_rows_ok(d->stride, e, 16, cache_record_bytes(d->head_dim), written)) return LILICORR_ERR_ARG;
+  if (e[1] > 1 && d->stride[1] >= (1 << 28)) return LILICORR_ERR_ARG;        // 16 positions in 32 bits
   v->p = static_cast<unsigned char*>(const_cast<void*>(cache));
   for (int i = 0; i < 3; ++i) v->s[i] = e[i] > 1 ? d->stride[i] : 0;
   v->N = d->sequences;

@@ -15,12 +15,12 @@
 namespace lilicorr {
 namespace {
 
-constexpr int CA_WARPS = 8;                  // of a CTA, each with its own 16 keys of a tile
+constexpr int CA_WARPS = 8;                  // of a CTA, each with its own keys of a tile
 constexpr int CA_THREADS = 32 * CA_WARPS;
-constexpr int CA_KEYS = 16 * CA_WARPS;       // keys of a tile
-// Probabilities are 2^(s - m + CA_UP) with the row's reference m, which follows its maximum when that is
-// more than CA_SLACK above: at most 2^14, and fp16 numbers of full precision down to 2^-20 of 2^m.
-constexpr float CA_UP = 6.f, CA_SLACK = 8.f;
+// Probabilities are 2^(s - m + CA_UP) with the row's reference m. Only where a score is more than CA_SLACK above
+// it does it move, to CA_ROOM above the largest so far, so that few steps have sums to rescale: at most 2^14,
+// and fp16 numbers of full precision down to 2^-16 of the largest.
+constexpr float CA_UP = 6.f, CA_SLACK = 8.f, CA_ROOM = 4.f;
 
 struct CaArgs {
   CacheView c;
@@ -33,6 +33,7 @@ struct CaArgs {
   float* weights;              // [N, H, S] or null
   int T, Hq, rep;
   int blocks;                  // row blocks of a (sequence, kv head)
+  int team;                    // CTAs that take the same tiles, of as many kv heads; divides H
   int whole;                   // a CTA an item (else the list of all tiles is cut evenly)
   float scale;                 // scale * k_unit * log2(e): scores in log2 units
   float scale_rest;            // what its rounding left
@@ -43,50 +44,55 @@ struct CaArgs {
   float2* rows;                // [N, T, Hq] reference and sum of whole rows, for the weights
 };
 
-// The work is the list of all (sequence, kv head, row block, tile of CA_KEYS keys), in that order; CTA b
-// takes tiles [b * per, (b + 1) * per). An item is one (sequence, kv head, block). A CTA leaves at most two
-// parts of items that other CTAs have parts of: of its first item (place 2 b) and its last (2 b + 1).
-constexpr uint32_t CA_MIN_TILES = 2;
-__device__ __forceinline__ uint32_t ca_per_cta(uint32_t tiles, uint32_t ctas) {
-  return max(CA_MIN_TILES, (tiles + ctas - 1) / ctas);
+// The work is the list of all (sequence, team of kv heads, row block, tile of KEYS keys), in that order, cut
+// evenly over the teams of CTAs: team g takes tiles [g * per, (g + 1) * per), each of its CTAs for its own head.
+// So the heads of a position, which may lie side by side in 64 bytes that memory reads at once, are read
+// at about the same time. An item is one (sequence, kv head, row block). A CTA leaves at most two parts of items
+// that other CTAs have parts of: of its first item (place 2 b) and of its last (2 b + 1).
+constexpr uint32_t CA_MIN_TILES = 1;
+__device__ __forceinline__ uint32_t ca_per_team(uint32_t tiles, uint32_t teams) {
+  return max(CA_MIN_TILES, (tiles + teams - 1) / teams);
 }
 // tiles of a row block of a sequence: one even where there is no key, none where there is no sequence
+template <int KEYS>
 __device__ __forceinline__ int ca_tiles(int raw, int S) {
-  return raw < 0 ? 0 : max(1, (min(raw, S) + CA_KEYS - 1) / CA_KEYS);
+  return raw < 0 ? 0 : max(1, (min(raw, S) + KEYS - 1) / KEYS);
 }
 
 // A place in the list.
+template <int KEYS>
 struct CaCursor {
   int n, h, rb, tile, tiles, len;
   __device__ __forceinline__ void sequence(const CaArgs& a, int at) {
     n = at;
     const int raw = a.seq_len[at];
     len = cache_len(raw, a.c.S);
-    tiles = ca_tiles(raw, a.c.S);
+    tiles = ca_tiles<KEYS>(raw, a.c.S);
   }
-  // the next tile; there has to be one
+  // the next item; there has to be one
   __device__ __forceinline__ void next(const CaArgs& a, int blocks) {
-    if (++tile < tiles) return;
     tile = 0;
     if (++rb < blocks) return;
     rb = 0;
-    if (++h < a.c.H) return;
-    h = 0;
+    h += a.team;
+    if (h < a.c.H) return;
+    h -= a.c.H;
     do sequence(a, n + 1); while (tiles == 0);
   }
 };
 
 // This CTA's part of the list: `count` tiles from `at` on. `keep`: the first CTA writes a.start.
-__device__ __forceinline__ uint32_t ca_range(const CaArgs& a, int blocks, bool keep, CaCursor* at,
+template <int KEYS>
+__device__ __forceinline__ uint32_t ca_range(const CaArgs& a, int blocks, bool keep, CaCursor<KEYS>* at,
                                              uint32_t* first, uint32_t* total) {
   __shared__ uint32_t sums[CA_WARPS];
   __shared__ uint32_t place[2];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int N = a.c.N, chunk = (N + CA_THREADS - 1) / CA_THREADS;
   const int n0 = min(N, tid * chunk), n1 = min(N, n0 + chunk);
-  const uint32_t per_tile = (uint32_t)a.c.H * blocks;
+  const uint32_t per_tile = (uint32_t)(a.c.H / a.team) * blocks;
   uint32_t mine = 0;
-  for (int n = n0; n < n1; ++n) mine += ca_tiles(a.seq_len[n], a.c.S) * per_tile;
+  for (int n = n0; n < n1; ++n) mine += ca_tiles<KEYS>(a.seq_len[n], a.c.S) * per_tile;
   uint32_t incl = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -102,13 +108,13 @@ __device__ __forceinline__ uint32_t ca_range(const CaArgs& a, int blocks, bool k
     if (w < warp) before += sums[w];
     *total += sums[w];
   }
-  const uint32_t per = ca_per_cta(*total, gridDim.x);
-  *first = blockIdx.x * per;
+  const uint32_t per = ca_per_team(*total, gridDim.x / a.team), g = blockIdx.x / a.team;
+  *first = g * per;
   if (keep && blockIdx.x == 0) {
     uint32_t b = before;
     for (int n = n0; n < n1; ++n) {
       a.start[n] = b;
-      b += ca_tiles(a.seq_len[n], a.c.S) * per_tile;
+      b += ca_tiles<KEYS>(a.seq_len[n], a.c.S) * per_tile;
     }
     if (tid == 0) a.start[N] = *total;
   }
@@ -116,7 +122,7 @@ __device__ __forceinline__ uint32_t ca_range(const CaArgs& a, int blocks, bool k
   if (before <= *first && *first < before + mine) {  // one thread
     uint32_t b = before;
     for (int n = n0; n < n1; ++n) {
-      const uint32_t t = ca_tiles(a.seq_len[n], a.c.S) * per_tile;
+      const uint32_t t = ca_tiles<KEYS>(a.seq_len[n], a.c.S) * per_tile;
       if (*first < b + t) {
         place[0] = n;
         place[1] = *first - b;
@@ -131,6 +137,7 @@ __device__ __forceinline__ uint32_t ca_range(const CaArgs& a, int blocks, bool k
   at->tile = place[1] - item * at->tiles;
   at->h = item / blocks;
   at->rb = item - at->h * blocks;
+  at->h = at->h * a.team + (blockIdx.x - g * a.team);
   return min(per, *total - *first);
 }
 
@@ -138,7 +145,7 @@ __device__ __forceinline__ uint32_t ca_range(const CaArgs& a, int blocks, bool k
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 // 16 bytes to shared memory, zeros where !there
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0)
+  asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0)
                : "memory");
 }
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
@@ -176,13 +183,11 @@ __device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b) {
   asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
-// the two codes of byte B of w
-template <int B>
-__device__ __forceinline__ uint32_t codes(uint32_t w) {
-  uint32_t r;
-  asm("{\n .reg .b8 x;\n .reg .b32 t;\n shr.u32 t, %1, %2;\n cvt.u8.u32 x, t;\n cvt.rn.f16x2.e2m1x2 %0, x;\n}"
-      : "=r"(r) : "r"(w), "n"(8 * B));
-  return r;
+// the two codes of each byte of w
+__device__ __forceinline__ void codes(uint32_t w, uint32_t (&r)[4]) {
+  asm("{\n .reg .b8 a, b, c, d;\n mov.b32 {a, b, c, d}, %4;\n cvt.rn.f16x2.e2m1x2 %0, a;\n"
+      " cvt.rn.f16x2.e2m1x2 %1, b;\n cvt.rn.f16x2.e2m1x2 %2, c;\n cvt.rn.f16x2.e2m1x2 %3, d;\n}"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(w));
 }
 __device__ __forceinline__ uint32_t scales(uint32_t two) {     // of two bytes
   uint32_t r;
@@ -214,7 +219,7 @@ struct CaCfg {
 // A lane's 16-byte pieces of 16 records (of their first `bytes` bytes).
 template <int DP>
 struct CaLane {
-  uint32_t off[CaCfg<DP>::CH];               // of its pieces of 16 records, in 16 bytes
+  uint32_t off[CaCfg<DP>::CH];               // in the cache
   int pieces, per;                           // 16-byte pieces: of 16 records, of one
   __device__ __forceinline__ CaLane(const CaArgs& a, int bytes, int lane) {
     per = bytes / 16;
@@ -222,23 +227,22 @@ struct CaLane {
 #pragma unroll
     for (int u = 0; u < CaCfg<DP>::CH; ++u) {
       const int i = lane + 32 * u, key = i / per;
-      off[u] = (uint32_t)(key * (a.c.s[1] >> 4)) + (i - key * per);
+      off[u] = (uint32_t)key * (uint32_t)a.c.s[1] + (i - key * per) * 16;
     }
   }
-  // the 16 records from key k on, of `len` keys
-  __device__ __forceinline__ void copy(const CaArgs& a, int n, int h, int k, int len, uint32_t dst,
+  // the 16 records at src, of which `there` are held (any number)
+  __device__ __forceinline__ void copy(const CaArgs& a, const unsigned char* src, int there, uint32_t dst,
                                        int lane) const {
-    const unsigned char* base = a.c.at(n, k, h);
-    if (k + 16 <= len) {
+    if (there >= 16) {
 #pragma unroll
       for (int u = 0; u < CaCfg<DP>::CH; ++u)
-        if (lane + 32 * u < pieces) copy16(dst + (lane + 32 * u) * 16, base + (size_t)off[u] * 16, true);
+        if (lane + 32 * u < pieces) copy16(dst + (lane + 32 * u) * 16, src + off[u], true);
     } else {
 #pragma unroll
       for (int u = 0; u < CaCfg<DP>::CH; ++u)
         if (lane + 32 * u < pieces) {
-          const bool there = k + (lane + 32 * u) / per < len;
-          copy16(dst + (lane + 32 * u) * 16, there ? base + (size_t)off[u] * 16 : a.q, there);
+          const bool held = (lane + 32 * u) / per < there;
+          copy16(dst + (lane + 32 * u) * 16, held ? static_cast<const void*>(src + off[u]) : a.q, held);
         }
     }
   }
@@ -269,15 +273,18 @@ struct CaKeyPart {
       }
     }
   }
-  // the operand of step ks: a[0], a[2] of row g, a[1], a[3] of row g + 8
-  template <int ks>
-  __device__ __forceinline__ void operand(uint32_t (&a)[4]) const {
+  // the operands of steps 2 i and 2 i + 1: a[0], a[2] of row g, a[1], a[3] of row g + 8
+  template <int i>
+  __device__ __forceinline__ void operands(uint32_t (&a)[2][4]) const {
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      uint32_t f = s[e];
-      if constexpr (DP == 128) f = __byte_perm(f, f, ks < 4 ? 0x1010 : 0x3232);
-      a[e] = mul2(codes<ks % 2 * 2>(w[e][ks / 2]), f);
-      a[e + 2] = mul2(codes<ks % 2 * 2 + 1>(w[e][ks / 2]), f);
+      uint32_t f = s[e], r[4];
+      if constexpr (DP == 128) f = __byte_perm(f, f, i < 2 ? 0x1010 : 0x3232);
+      codes(w[e][i], r);
+      a[0][e] = mul2(r[0], f);
+      a[0][e + 2] = mul2(r[1], f);
+      a[1][e] = mul2(r[2], f);
+      a[1][e + 2] = mul2(r[3], f);
     }
   }
 };
@@ -341,8 +348,10 @@ __device__ __forceinline__ int load_query(const E* q, int d, int c, uint32_t (*b
 template <int DP, int NT, int PIECES>
 struct CaSmem {
   static constexpr bool QS = NT * PIECES > 1;            // queries in shared memory
-  static constexpr int STAGES = NT * PIECES > 1 ? 3 : 4;
-  static constexpr int STAGE = 16 * (DP + 16);           // bytes of a warp's 16 records
+  static constexpr int SUB = NT == 2 || PIECES > 1 ? 1 : 2;   // 16 keys each, of a warp's step
+  static constexpr int KEYS = 16 * SUB * CA_WARPS;       // of a tile
+  static constexpr int STAGES = SUB > 1 ? 2 : 3;
+  static constexpr int STAGE = 16 * SUB * (DP + 16);     // bytes of a warp's records
   static constexpr int XO = CA_WARPS * 8 * CaCfg<DP>::XL * 4;
   static constexpr int XM = CA_WARPS * 8 * 8;
   static constexpr int Q = QS ? NT * PIECES * CaCfg<DP>::KS * 256 : 0;
@@ -379,41 +388,58 @@ cache_attention_kernel(const CaArgs a) {
   pdl_wait();
   using Cfg = CaCfg<DP>;
   using Sm = CaSmem<DP, NT, PIECES>;
-  constexpr int KS = Cfg::KS, ST = Sm::STAGES, ROWS = 8 * NT;
+  constexpr int KS = Cfg::KS, ST = Sm::STAGES, SUB = Sm::SUB, KEYS = Sm::KEYS, ROWS = 8 * NT;
   extern __shared__ __align__(16) unsigned char sm[];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
   const int d = a.c.d, R = cache_record_bytes(d), half = cache_half_bytes(d), rows = a.T * a.rep;
 
-  CaCursor at;
+  CaCursor<KEYS> at;
   uint32_t first = 0, total = 0, count;
   if (a.whole) {
-    const int item = blockIdx.x, per_n = a.c.H * a.blocks;
-    at.sequence(a, item / per_n);
-    at.h = item % per_n / a.blocks;
+    const int item = blockIdx.x / a.c.H;
+    at.sequence(a, item / a.blocks);
+    at.h = blockIdx.x - item * a.c.H;
     at.rb = item % a.blocks;
     at.tile = 0;
     count = at.tiles;
   } else {
-    count = ca_range(a, a.blocks, true, &at, &first, &total);
+    count = ca_range<KEYS>(a, a.blocks, true, &at, &first, &total);
   }
   if (count == 0) return;
 
   const CaLane<DP> mine(a, R, lane);
   unsigned char* stage = sm + warp * ST * Sm::STAGE;
-  CaCursor ahead = at;                               // of the copies
+  CaCursor<KEYS> ahead = at;                         // of the copies
+  const unsigned char* src;
+  int held;                                          // keys from src on
   uint32_t copied = 0;
-  auto copy_next = [&] {
+  auto seek = [&] {
+    const int k = ahead.tile * KEYS + warp * (16 * SUB);
+    src = a.c.at(ahead.n, k, ahead.h);
+    held = ahead.len - k;
+  };
+  seek();
+  auto copy_next = [&](int place) {
     if (copied < count) {
-      mine.copy(a, ahead.n, ahead.h, ahead.tile * CA_KEYS + warp * 16, ahead.len,
-                smem_u32(stage + copied % ST * Sm::STAGE), lane);
-      if (++copied < count) ahead.next(a, a.blocks);
+      const uint32_t dst = smem_u32(stage + place * Sm::STAGE);
+#pragma unroll
+      for (int i = 0; i < SUB; ++i) mine.copy(a, src + i * 16 * a.c.s[1], held - 16 * i, dst + i * 16 * R, lane);
+      if (++copied < count) {
+        if (++ahead.tile < ahead.tiles) {
+          src += KEYS * a.c.s[1];
+          held -= KEYS;
+        } else {
+          ahead.next(a, a.blocks);
+          seek();
+        }
+      }
     }
     copy_commit();
   };
 #pragma unroll
-  for (int i = 0; i < ST - 1; ++i) copy_next();
+  for (int i = 0; i < ST; ++i) copy_next(i);
 
-  // where this lane's keys and values lie in a warp's 16 records
+  // where this lane's keys and values lie in 16 records
   const int key = key_of(g), va = key_of(2 * c), vb = key_of(2 * c + 1);
   const uint32_t kmask = key_scale_mask<DP>(d, c);
   const int vg = DP == 128 ? g : DP == 64 ? g >> 1 : g >> 2;   // the scale group of its values
@@ -423,9 +449,9 @@ cache_attention_kernel(const CaArgs a) {
   uint32_t qr[Sm::QS ? 1 : PIECES][KS][2];
   uint2* qs = reinterpret_cast<uint2*>(sm + Sm::AT_Q);         // [NT][PIECES][KS][lane]
   float m[NT][2], l[NT][2], f[NT][2], fr[NT][2];               // f: a row's factor; fr: what it lacks
-  int lim[NT][2];
   float o[KS][NT][4];
   uint32_t done = 0;
+  int place = 0;
   bool fresh = true;
   while (done < count) {
     if (fresh) {                                     // an item begins
@@ -451,11 +477,9 @@ cache_attention_kernel(const CaArgs a) {
         }
 #pragma unroll
         for (int e = 0; e < 2; ++e) {                // this lane's columns
-          const int col = 2 * c + e, rr = at.rb * ROWS + nt * 8 + col;
-          const int u = __shfl_sync(0xffffffffu, up, col * 4);
+          const int u = __shfl_sync(0xffffffffu, up, (2 * c + e) * 4);
           f[nt][e] = ldexpf(a.scale, -u);
           fr[nt][e] = ldexpf(a.scale_rest, -u);
-          lim[nt][e] = rr < rows ? max(0, at.len - (a.T - 1 - rr / a.rep)) : 0;
           m[nt][e] = -FLT_MAX;
           l[nt][e] = 0.f;
         }
@@ -468,59 +492,75 @@ cache_attention_kernel(const CaArgs a) {
           for (int e = 0; e < 4; ++e) o[i][nt][e] = 0.f;
       if constexpr (Sm::QS) __syncthreads();
     }
-    copy_wait<ST - 2>();
+    copy_wait<ST - 1>();
     __syncwarp();
-    const unsigned char* rec = stage + done % ST * Sm::STAGE;
-    const int k0 = at.tile * CA_KEYS + warp * 16;
+    const unsigned char* rec = stage + place * Sm::STAGE;
 
     // ---- scores
-    float s[NT][4];
+    float s[SUB][NT][4];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
-    {
+    for (int u = 0; u < SUB; ++u) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) s[u][nt][0] = s[u][nt][1] = s[u][nt][2] = s[u][nt][3] = 0.f;
       CaKeyPart<DP> kp;
-      kp.load(rec + key * R, R, d, c, kmask);
-      auto step = [&](auto ks) {
-        constexpr int i = decltype(ks)::value;
-        uint32_t ka[4];
-        kp.template operand<i>(ka);
+      kp.load(rec + (16 * u + key) * R, R, d, c, kmask);
+      auto step = [&](auto is) {
+        constexpr int i = decltype(is)::value;
+        uint32_t ka[2][4];
+        kp.template operands<i>(ka);
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
-          for (int p = PIECES - 1; p >= 0; --p) {    // the smallest parts first
-            if constexpr (Sm::QS) {
-              const uint2 b = qs[((nt * PIECES + p) * KS + i) * 32 + lane];
-              mma(s[nt], ka, b.x, b.y);
-            } else {
-              mma(s[nt], ka, qr[p][i][0], qr[p][i][1]);
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int p = PIECES - 1; p >= 0; --p) {  // the smallest parts first
+              if constexpr (Sm::QS) {
+                const uint2 b = qs[((nt * PIECES + p) * KS + 2 * i + j) * 32 + lane];
+                mma(s[u][nt], ka[j], b.x, b.y);
+              } else {
+                mma(s[u][nt], ka[j], qr[p][2 * i + j][0], qr[p][2 * i + j][1]);
+              }
             }
-          }
       };
-      steps(step, std::make_integer_sequence<int, KS>{});
+      steps(step, std::make_integer_sequence<int, KS / 2>{});
     }
-    if (k0 + 16 > at.len - (a.T - 1)) {              // some row may not see all of these keys
+    const int k0 = at.tile * KEYS + warp * (16 * SUB);
+    if (k0 + 16 * SUB > at.len - (a.T - 1)) {        // some row may not see all of these keys
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (k0 + key + (e >> 1) >= lim[nt][e & 1]) s[nt][e] = -INFINITY;
+        for (int e = 0; e < 2; ++e) {
+          const int r = at.rb * ROWS + nt * 8 + 2 * c + e;
+          const int seen = at.len - (a.T - 1 - r / a.rep) - k0 - key;
+#pragma unroll
+          for (int u = 0; u < SUB; ++u) {
+            if (16 * u >= seen) s[u][nt][e] = -INFINITY;
+            if (16 * u + 1 >= seen) s[u][nt][e + 2] = -INFINITY;
+          }
+        }
     }
     // ---- probabilities: the reference moves when some row of the warp's has left it behind
+    float top[NT][2];
     bool up = false;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) up |= fmaf(s[nt][e], f[nt][e & 1], -m[nt][e & 1]) > CA_SLACK;
+      for (int e = 0; e < 2; ++e) {
+        top[nt][e] = fmaxf(s[0][nt][e], s[0][nt][e + 2]);
+#pragma unroll
+        for (int u = 1; u < SUB; ++u) top[nt][e] = fmaxf(top[nt][e], fmaxf(s[u][nt][e], s[u][nt][e + 2]));
+        up |= fmaf(top[nt][e], f[nt][e], -m[nt][e]) > CA_SLACK;
+      }
     if (__any_sync(0xffffffffu, up)) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          float top = fmaxf(s[nt][e], s[nt][e + 2]) * f[nt][e];
-          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
-          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
-          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-          const float to = fmaxf(m[nt][e], top), x = ex2(m[nt][e] - to);
+          float t = top[nt][e];
+          t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 4));
+          t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 8));
+          t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 16));
+          const float to = fmaxf(m[nt][e], fmaf(t, f[nt][e], CA_ROOM)), x = ex2(m[nt][e] - to);
           m[nt][e] = to;
           l[nt][e] *= x;
 #pragma unroll
@@ -530,33 +570,34 @@ cache_attention_kernel(const CaArgs a) {
           }
         }
     }
-    uint32_t pb[NT][PIECES][2];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      float p[4];
+    for (int u = 0; u < SUB; ++u) {
+      uint32_t pb[NT][PIECES][2];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float x = CA_UP - m[nt][e & 1];
-        // (a key that is not seen: no infinity times what the factor lacks, which has either sign)
-        if (PIECES > 1) x = fmaf(fmaxf(s[nt][e], -FLT_MAX), fr[nt][e & 1], x);
-        p[e] = ex2(fmaf(s[nt][e], f[nt][e & 1], x));
-      }
-      l[nt][0] += p[0] + p[2];
-      l[nt][1] += p[1] + p[3];
+      for (int nt = 0; nt < NT; ++nt) {
+        float p[4];
 #pragma unroll
-      for (int i = 0; i < PIECES; ++i) {
-        const uint32_t x = half2_of(p[0], p[1]), y = half2_of(p[2], p[3]);
-        pb[nt][i][0] = transpose8(x);
-        pb[nt][i][1] = transpose8(y);
-        if (PIECES > 1) {
-          half2_sub(x, p[0], p[1]);
-          half2_sub(y, p[2], p[3]);
+        for (int e = 0; e < 4; ++e) {
+          float x = CA_UP - m[nt][e & 1];
+          // (a key that is not seen: no infinity times what the factor lacks, which has either sign)
+          if (PIECES > 1) x = fmaf(fmaxf(s[u][nt][e], -FLT_MAX), fr[nt][e & 1], x);
+          p[e] = ex2(fmaf(s[u][nt][e], f[nt][e & 1], x));
+        }
+        l[nt][0] += p[0] + p[2];
+        l[nt][1] += p[1] + p[3];
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+          const uint32_t x = half2_of(p[0], p[1]), y = half2_of(p[2], p[3]);
+          pb[nt][i][0] = transpose8(x);
+          pb[nt][i][1] = transpose8(y);
+          if (PIECES > 1) {
+            half2_sub(x, p[0], p[1]);
+            half2_sub(y, p[2], p[3]);
+          }
         }
       }
-    }
-    // ---- sums of p V: two keys a register, so the codes of two records go together, byte by byte
-    {
-      const unsigned char* v = rec + half;
+      // ---- sums of p V: two keys a register, so the codes of two records go together, byte by byte
+      const unsigned char* v = rec + 16 * u * R + half;
       uint32_t fs[2], w[4][DP / 128 < 1 ? 1 : 2];
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
@@ -577,25 +618,33 @@ cache_attention_kernel(const CaArgs a) {
         fs[e] = scales(b);
       }
       auto step = [&](auto is) {
-        constexpr int i = decltype(is)::value, word = i / 4, byte = i % 4;
-        uint32_t oa[4];
+        constexpr int i = decltype(is)::value;       // four tiles of 16 elements (DP 32: two)
+        constexpr int tiles = KS < 4 ? KS : 4;
+        uint32_t oa[4][4];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const uint32_t x = w[2 * e][word], y = w[2 * e + 1][word];
-          const uint32_t even = (x & 0x0F0F0F0Fu) | ((y << 4) & 0xF0F0F0F0u);
-          const uint32_t odd = ((x >> 4) & 0x0F0F0F0Fu) | (y & 0xF0F0F0F0u);
-          oa[2 * e] = mul2(codes<byte>(even), fs[e]);
-          oa[2 * e + 1] = mul2(codes<byte>(odd), fs[e]);
+          const uint32_t x = w[2 * e][i], y = w[2 * e + 1][i];
+          uint32_t even[4], odd[4];
+          codes((x & 0x0F0F0F0Fu) | ((y << 4) & 0xF0F0F0F0u), even);
+          codes(((x >> 4) & 0x0F0F0F0Fu) | (y & 0xF0F0F0F0u), odd);
+#pragma unroll
+          for (int j = 0; j < tiles; ++j) {
+            oa[j][2 * e] = mul2(even[j], fs[e]);
+            oa[j][2 * e + 1] = mul2(odd[j], fs[e]);
+          }
         }
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int j = 0; j < tiles; ++j)
 #pragma unroll
-          for (int p = PIECES - 1; p >= 0; --p) mma(o[i][nt], oa, pb[nt][p][0], pb[nt][p][1]);
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int p = PIECES - 1; p >= 0; --p) mma(o[4 * i + j][nt], oa[j], pb[nt][p][0], pb[nt][p][1]);
       };
-      steps(step, std::make_integer_sequence<int, KS>{});
+      steps(step, std::make_integer_sequence<int, DP == 128 ? 2 : 1>{});
     }
     __syncwarp();                                    // the records' place is free
-    copy_next();
+    copy_next(place);
+    place = place + 1 == ST ? 0 : place + 1;
     ++done;
     const bool last = at.tile + 1 == at.tiles;
     if (!last && done < count) {
@@ -648,9 +697,9 @@ cache_attention_kernel(const CaArgs a) {
           const int t = r / a.rep;
           ca_write<E>(a, at.n, t, at.h * a.rep + (r - t * a.rep), M, L, y, lane);
         } else {
-          const size_t place = ((size_t)2 * blockIdx.x + (item_start > first)) * ROWS + nt * 8 + warp;
-          if (lane == 0) a.ml[place] = make_float2(M, L);
-          if (lane < DP / 4) *reinterpret_cast<float4*>(a.po + place * DP + lane * 4) = y;
+          const size_t part = ((size_t)2 * blockIdx.x + (item_start > first)) * ROWS + nt * 8 + warp;
+          if (lane == 0) a.ml[part] = make_float2(M, L);
+          if (lane < DP / 4) *reinterpret_cast<float4*>(a.po + part * DP + lane * 4) = y;
         }
       }
     }
@@ -663,30 +712,31 @@ cache_attention_kernel(const CaArgs a) {
   copy_wait<0>();
 }
 
-// The items that several CTAs have parts of: CTA j here looks at the border between CTAs j and j + 1 of the
-// list, and joins the parts of the item there, if that is the item's first border. A warp a row.
+// The items that several CTAs have parts of: CTA j of a head here looks at the border between teams j and j + 1
+// of the list, and joins the parts of the item there, if that is the item's first border. A warp a row.
 template <int DP, int NT, typename E>
 __global__ void __launch_bounds__(128) cache_attention_join_kernel(const CaArgs a) {
   pdl_wait();
   constexpr int ROWS = 8 * NT;
   __shared__ int found;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, N = a.c.N;
-  const uint32_t total = a.start[N], ctas = gridDim.x + 1, per = ca_per_cta(total, ctas);
-  const uint32_t x = (blockIdx.x + 1) * per;
+  const uint32_t team = a.team, border = blockIdx.x / team, head = blockIdx.x - border * team;
+  const uint32_t total = a.start[N], per = ca_per_team(total, gridDim.x / team + 1);
+  const uint32_t x = (border + 1) * per;
   if (x >= total) return;
   for (int n = tid; n < N; n += 128)
     if (a.start[n] <= x && x < a.start[n + 1]) found = n;
   __syncthreads();
   const int n = found;
-  const uint32_t s0 = a.start[n], tiles = (a.start[n + 1] - s0) / (uint32_t)(a.c.H * a.blocks);
+  const uint32_t s0 = a.start[n], tiles = (a.start[n + 1] - s0) / (a.c.H / team * a.blocks);
   const uint32_t item = (x - s0) / tiles, s = s0 + item * tiles, e = s + tiles;
   const uint32_t b0 = s / per, b1 = (e - 1) / per;
-  if (x == s || b0 != blockIdx.x) return;
-  const int h = item / a.blocks, rb = item - h * a.blocks, rows = a.T * a.rep;
+  if (x == s || b0 != border) return;
+  const int ht = item / a.blocks, rb = item - ht * a.blocks, h = ht * team + head, rows = a.T * a.rep;
   for (int i = warp; i < ROWS; i += 4) {
     const int r = rb * ROWS + i;
     if (r >= rows) break;
-    auto place = [&](uint32_t b) { return ((size_t)2 * b + (b * per < s)) * ROWS + i; };
+    auto place = [&](uint32_t b) { return (2 * ((size_t)b * team + head) + (b * per < s)) * ROWS + i; };
     float M = -FLT_MAX, L = 0.f;
     for (uint32_t b = b0 + lane; b <= b1; b += 32) M = fmaxf(M, a.ml[place(b)].x);
     M = warp_max(M);
@@ -715,14 +765,14 @@ __global__ void __launch_bounds__(128) cache_attention_join_kernel(const CaArgs 
 template <int DP, int NT, int PIECES, typename E>
 __global__ void __launch_bounds__(CA_THREADS, 2) cache_attention_weights_kernel(const CaArgs a) {
   pdl_wait();
-  constexpr int KS = CaCfg<DP>::KS, ST = 4, ROWS = 8 * NT, STAGE = 16 * (DP / 2 + 16);
+  constexpr int KS = CaCfg<DP>::KS, ST = 4, ROWS = 8 * NT, STAGE = 16 * (DP / 2 + 16), KEYS = 16 * CA_WARPS;
   extern __shared__ __align__(16) unsigned char sm[];
   uint2* qs = reinterpret_cast<uint2*>(sm + CA_WARPS * ST * STAGE);      // [NT][PIECES][KS][lane]
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
   const int d = a.c.d, R = (cache_half_bytes(d) + 15) / 16 * 16, rows = a.T * a.rep;
-  CaCursor at;
+  CaCursor<KEYS> at;
   uint32_t first, total;
-  uint32_t count = ca_range(a, 1, false, &at, &first, &total);
+  uint32_t count = ca_range<KEYS>(a, 1, false, &at, &first, &total);
   const CaLane<DP> mine(a, R, lane);
   unsigned char* stage = sm + warp * ST * STAGE;
   const int key = key_of(g);
@@ -767,7 +817,8 @@ __global__ void __launch_bounds__(CA_THREADS, 2) cache_attention_weights_kernel(
       int ahead = tile0;
       auto copy_next = [&] {
         if (ahead < tile1)
-          mine.copy(a, at.n, at.h, ahead * CA_KEYS + warp * 16, at.len, smem_u32(stage + ahead % ST * STAGE), lane);
+          mine.copy(a, a.c.at(at.n, ahead * KEYS + warp * 16, at.h), at.len - (ahead * KEYS + warp * 16),
+                    smem_u32(stage + ahead % ST * STAGE), lane);
         ++ahead;
         copy_commit();
       };
@@ -777,7 +828,7 @@ __global__ void __launch_bounds__(CA_THREADS, 2) cache_attention_weights_kernel(
       for (int tile = tile0; tile < tile1; ++tile) {
         copy_wait<ST - 2>();
         __syncwarp();
-        const int k0 = tile * CA_KEYS + warp * 16;
+        const int k0 = tile * KEYS + warp * 16;
         float s[NT][4];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
@@ -785,17 +836,19 @@ __global__ void __launch_bounds__(CA_THREADS, 2) cache_attention_weights_kernel(
         kp.load(stage + tile % ST * STAGE + key * R, R, d, c, kmask);
         auto step = [&](auto ks) {
           constexpr int i = decltype(ks)::value;
-          uint32_t ka[4];
-          kp.template operand<i>(ka);
+          uint32_t ka[2][4];
+          kp.template operands<i>(ka);
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
+          for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int p = PIECES - 1; p >= 0; --p) {
-              const uint2 b = qs[((nt * PIECES + p) * KS + i) * 32 + lane];
-              mma(s[nt], ka, b.x, b.y);
-            }
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int p = PIECES - 1; p >= 0; --p) {
+                const uint2 b = qs[((nt * PIECES + p) * KS + 2 * i + j) * 32 + lane];
+                mma(s[nt], ka[j], b.x, b.y);
+              }
         };
-        steps(step, std::make_integer_sequence<int, KS>{});
+        steps(step, std::make_integer_sequence<int, KS / 2>{});
         float sum[2] = {0.f, 0.f};
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -820,7 +873,6 @@ __global__ void __launch_bounds__(CA_THREADS, 2) cache_attention_weights_kernel(
     }
     count -= tile1 - tile0;
     if (count > 0) {
-      at.tile = tile1 - 1;
       at.next(a, 1);
     }
   }
@@ -828,7 +880,7 @@ __global__ void __launch_bounds__(CA_THREADS, 2) cache_attention_weights_kernel(
 
 // ------------------------------------------------------------------------------- the call
 struct CaPlan {
-  int dp, nt, pieces, blocks, ctas;
+  int dp, nt, pieces, blocks, ctas, team;
   bool whole;
   size_t items, start_off, ml_off, po_off, rows_off, total;
 };
@@ -846,11 +898,14 @@ lilicorr_status_t ca_plan(const lilicorr_cache_attention_desc* d, CaPlan* p) {
   p->pieces = d->dtype == LILICORR_BF16 ? 1 : 3;
   p->nt = rows <= 8 ? 1 : rows <= 16 || p->pieces > 1 ? 2 : 4;
   p->blocks = (rows + 8 * p->nt - 1) / (8 * p->nt);
-  const int tiles = c.capacity <= CA_KEYS ? 1 : (c.capacity + CA_KEYS - 1) / CA_KEYS;
   p->items = (size_t)c.sequences * c.kv_heads * p->blocks;
-  if ((double)p->items * tiles >= 2147483648.0) return LILICORR_ERR_SHAPE;
-  p->ctas = num_sms() * (p->nt * p->pieces > 3 || p->nt > 2 ? 1 : 2);
-  p->whole = tiles <= 4;
+  if ((double)p->items * (c.capacity / 128 + 1) >= 2147483648.0) return LILICORR_ERR_SHAPE;
+  // the widest team of at most 16: all heads of a position where there are so few
+  p->team = 1;
+  for (int i = 2; i <= 16; ++i)
+    if (c.kv_heads % i == 0) p->team = i;
+  p->ctas = num_sms() * (p->nt * p->pieces > 3 || p->nt > 2 ? 1 : 2) / p->team * p->team;
+  p->whole = c.capacity <= 512;
   const size_t parts = p->whole ? 0 : (size_t)2 * p->ctas * 8 * p->nt;
   p->start_off = 256;
   p->ml_off = p->start_off + align_up(((size_t)c.sequences + 1) * 4, 256);
@@ -868,13 +923,13 @@ lilicorr_status_t ca_launch(const CaArgs& a, const CaPlan& p, cudaStream_t st) {
   LL_TRY(launch_k(kernel, p.whole ? (unsigned)p.items : (unsigned)p.ctas, CA_THREADS, CaSmem<DP, NT, PIECES>::TOTAL,
                   st, a));
   if (!p.whole)
-    LL_TRY(launch_k(cache_attention_join_kernel<DP, NT, E>, (unsigned)p.ctas - 1, 128, 0, st, a));
+    LL_TRY(launch_k(cache_attention_join_kernel<DP, NT, E>, (unsigned)(p.ctas - p.team), 128, 0, st, a));
   if (!a.weights) return LILICORR_OK;
   constexpr int WT = PIECES > 1 ? 1 : NT;
   auto* weights = cache_attention_weights_kernel<DP, WT, PIECES, E>;
   LL_TRY(allow_max_dynamic_smem(weights, configured_w));
   const size_t smem = CA_WARPS * 4 * 16 * (DP / 2 + 16) + WT * PIECES * (DP / 16) * 256;
-  return launch_k(weights, (unsigned)(2 * num_sms()), CA_THREADS, smem, st, a);
+  return launch_k(weights, (unsigned)(2 * num_sms() / p.team * p.team), CA_THREADS, smem, st, a);
 }
 
 template <int DP>
@@ -932,6 +987,7 @@ lilicorr_status_t lilicorr_cache_attention(const lilicorr_cache_attention_desc* 
   a.Hq = desc->q_heads;
   a.rep = desc->q_heads / a.c.H;
   a.blocks = p.blocks;
+  a.team = p.team;
   a.whole = p.whole;
   const double log2e = 1.4426950408889634 * scale;
   a.scale = (float)log2e;
