@@ -33,11 +33,15 @@ lilicorr_status_t ca_plan(const lilicorr_cache_attention_desc* d, CaPlan* p) {
   p->ctas = num_sms() * (p->nt * p->pieces > 3 || p->nt > 2 ? 1 : 2) / p->team * p->team;
   p->whole = c.capacity <= 512;
   const size_t parts = p->whole ? 0 : (size_t)2 * p->ctas * 8 * p->nt;
-  p->start_off = 256;
-  p->ml_off = p->start_off + align_up(((size_t)c.sequences + 1) * 4, 256);
+  p->pad = rows <= 16 ? (rows + 1) / 2 * 2 : 0;
+  const size_t keys = (size_t)c.sequences * c.kv_heads * c.capacity;
+  p->left_off = 256;
+  p->ml_off = p->left_off + align_up(p->whole ? 0 : (size_t)2 * p->ctas * 4, 256);
   p->po_off = p->ml_off + align_up(parts * sizeof(float2), 256);
   p->rows_off = p->po_off + parts * p->dp * sizeof(float);
-  p->total = p->rows_off + align_up((size_t)all * sizeof(float2), 256);
+  p->factors_off = p->rows_off + align_up((size_t)all * sizeof(float2), 256);
+  p->scores_off = p->factors_off + align_up((size_t)all * sizeof(float), 256);
+  p->total = p->scores_off + align_up(keys * p->pad * sizeof(float), 256);
   return LILICORR_OK;
 }
 
@@ -93,10 +97,13 @@ lilicorr_status_t lilicorr_cache_attention(const lilicorr_cache_attention_desc* 
   a.scale = (float)log2e;
   a.scale_rest = (float)(log2e - a.scale);
   a.rest_ratio = (float)((log2e - a.scale) / log2e);
-  a.start = reinterpret_cast<uint32_t*>(w + p.start_off);
+  a.left = reinterpret_cast<uint32_t*>(w + p.left_off);
   a.ml = reinterpret_cast<float2*>(w + p.ml_off);
   a.po = reinterpret_cast<float*>(w + p.po_off);
   a.rows = reinterpret_cast<float2*>(w + p.rows_off);
+  a.factors = reinterpret_cast<float*>(w + p.factors_off);
+  a.scores = weights && p.pad ? reinterpret_cast<float*>(w + p.scores_off) : nullptr;
+  a.pad = p.pad;
   if (a.c.d == 128) return ca_launch_rows<128, 128>(a, p, stream);
   if (a.c.d == 64) return ca_launch_rows<64, 64>(a, p, stream);
   return p.dp == 32   ? ca_launch_rows<32, 0>(a, p, stream)

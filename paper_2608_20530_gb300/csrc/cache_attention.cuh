@@ -20,16 +20,20 @@ struct CaArgs {
   float scale;                 // scale * k_unit * log2(e): scores in log2 units
   float scale_rest;            // what its rounding left
   float rest_ratio;            // scale_rest / scale
-  uint32_t* start;             // [N + 1] tiles before each sequence
+  uint32_t* left;              // [2 * CTAs] parts that an item's CTAs have left; 0 between calls
   float2* ml;                  // [2 * CTAs][rows of a block]: reference and sum of an item's part
   float* po;                   // [2 * CTAs][rows of a block][DP]: its sum of p V
   float2* rows;                // [N, T, Hq] reference and sum of whole rows, for the weights
+  float* factors;              // [N, T, Hq] what takes a row's products to scores in log2 units
+  float* scores;               // [N, H, S, pad] the products themselves, or null: computed again
+  int pad;                     // rows, even
 };
 
 struct CaPlan {
   int dp, nt, pieces, blocks, ctas, team;
   bool whole;
-  size_t items, start_off, ml_off, po_off, rows_off, total;
+  int pad;                     // rows whose products are kept (0: none)
+  size_t items, left_off, ml_off, po_off, rows_off, factors_off, scores_off, total;
 };
 
 // The launches of a call, for widths up to DP (cache_attention_any.cu), or for DP itself.

@@ -27,7 +27,8 @@ constexpr float CA_UP = 6.f, CA_SLACK = 8.f, CA_ROOM = 4.f;
 // evenly over the teams of CTAs: team g takes tiles [g * per, (g + 1) * per), each of its CTAs for its own head.
 // So the heads of a position, which may lie side by side in 64 bytes that memory reads at once, are read
 // at about the same time. An item is one (sequence, kv head, row block). A CTA leaves at most two parts of items
-// that other CTAs have parts of: of its first item (place 2 b) and of its last (2 b + 1).
+// that other CTAs have parts of: of its first item (place 2 b) and of its last (2 b + 1). Of the CTAs that have parts
+// of an item, the last to leave its own joins them, in the order of the list.
 constexpr uint32_t CA_MIN_TILES = 1;
 __device__ __forceinline__ uint32_t ca_per_team(uint32_t tiles, uint32_t teams) {
   return max(CA_MIN_TILES, (tiles + teams - 1) / teams);
@@ -42,12 +43,12 @@ __device__ __forceinline__ int ca_tiles(int raw, int S) {
 template <int KEYS>
 struct CaCursor {
   int n, h, rb, tile, tiles, len;
-  __device__ __forceinline__ void sequence(const CaArgs& a, int at) {
+  __device__ __forceinline__ void set(const CaArgs& a, int at, int raw) {
     n = at;
-    const int raw = a.seq_len[at];
     len = cache_len(raw, a.c.S);
     tiles = ca_tiles<KEYS>(raw, a.c.S);
   }
+  __device__ __forceinline__ void sequence(const CaArgs& a, int at) { set(a, at, a.seq_len[at]); }
   // the next item; there has to be one
   __device__ __forceinline__ void next(const CaArgs& a, int blocks) {
     tile = 0;
@@ -60,18 +61,21 @@ struct CaCursor {
   }
 };
 
-// This CTA's part of the list: `count` tiles from `at` on. `keep`: the first CTA writes a.start.
+// This CTA's part of the list: as many tiles as it returns, from `at` on, which is place `first` of the list.
 template <int KEYS>
-__device__ __forceinline__ uint32_t ca_range(const CaArgs& a, int blocks, bool keep, CaCursor<KEYS>* at,
-                                             uint32_t* first, uint32_t* total) {
+__device__ __forceinline__ uint32_t ca_range(const CaArgs& a, int blocks, CaCursor<KEYS>* at, uint32_t* first,
+                                             uint32_t* per) {
   __shared__ uint32_t sums[CA_WARPS];
   __shared__ uint32_t place[2];
+  __shared__ int length;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int N = a.c.N, chunk = (N + CA_THREADS - 1) / CA_THREADS;
   const int n0 = min(N, tid * chunk), n1 = min(N, n0 + chunk);
   const uint32_t per_tile = (uint32_t)(a.c.H / a.team) * blocks;
-  uint32_t mine = 0;
-  for (int n = n0; n < n1; ++n) mine += ca_tiles<KEYS>(a.seq_len[n], a.c.S) * per_tile;
+  int raw = -1;                                      // of n0, the only one in most calls
+  if (n0 < n1) raw = a.seq_len[n0];
+  uint32_t mine = ca_tiles<KEYS>(raw, a.c.S) * per_tile;
+  for (int n = n0 + 1; n < n1; ++n) mine += ca_tiles<KEYS>(a.seq_len[n], a.c.S) * per_tile;
   uint32_t incl = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -80,44 +84,37 @@ __device__ __forceinline__ uint32_t ca_range(const CaArgs& a, int blocks, bool k
   }
   if (lane == 31) sums[warp] = incl;
   __syncthreads();
-  uint32_t before = incl - mine;
-  *total = 0;
+  uint32_t before = incl - mine, total = 0;
 #pragma unroll
   for (int w = 0; w < CA_WARPS; ++w) {
     if (w < warp) before += sums[w];
-    *total += sums[w];
+    total += sums[w];
   }
-  const uint32_t per = ca_per_team(*total, gridDim.x / a.team), g = blockIdx.x / a.team;
-  *first = g * per;
-  if (keep && blockIdx.x == 0) {
-    uint32_t b = before;
-    for (int n = n0; n < n1; ++n) {
-      a.start[n] = b;
-      b += ca_tiles<KEYS>(a.seq_len[n], a.c.S) * per_tile;
-    }
-    if (tid == 0) a.start[N] = *total;
-  }
-  if (*first >= *total) return 0;
+  const uint32_t g = blockIdx.x / a.team;
+  *per = ca_per_team(total, gridDim.x / a.team);
+  *first = g * *per;
+  if (*first >= total) return 0;
   if (before <= *first && *first < before + mine) {  // one thread
     uint32_t b = before;
-    for (int n = n0; n < n1; ++n) {
-      const uint32_t t = ca_tiles<KEYS>(a.seq_len[n], a.c.S) * per_tile;
-      if (*first < b + t) {
-        place[0] = n;
-        place[1] = *first - b;
-        break;
-      }
+    int n = n0;
+    while (true) {
+      const uint32_t t = ca_tiles<KEYS>(raw, a.c.S) * per_tile;
+      if (*first < b + t) break;
       b += t;
+      raw = a.seq_len[++n];
     }
+    place[0] = n;
+    place[1] = *first - b;
+    length = raw;
   }
   __syncthreads();
-  at->sequence(a, place[0]);
+  at->set(a, place[0], length);
   const uint32_t item = place[1] / at->tiles;
   at->tile = place[1] - item * at->tiles;
   at->h = item / blocks;
   at->rb = item - at->h * blocks;
   at->h = at->h * a.team + (blockIdx.x - g * a.team);
-  return min(per, *total - *first);
+  return min(*per, total - *first);
 }
 
 // ------------------------------------------------------------------------------- small pieces
@@ -373,11 +370,12 @@ cache_attention_kernel(const CaArgs a) {
   using Sm = CaSmem<DP, NT, PIECES>;
   constexpr int KS = Cfg::KS, ST = Sm::STAGES, SUB = Sm::SUB, KEYS = Sm::KEYS, ROWS = 8 * NT;
   extern __shared__ __align__(16) unsigned char sm[];
+  __shared__ bool joins;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
   const int d = DIM ? DIM : a.c.d, R = cache_record_bytes(d), half = cache_half_bytes(d), rows = a.T * a.rep;
 
   CaCursor<KEYS> at;
-  uint32_t first = 0, total = 0, count;
+  uint32_t first = 0, per = 0, count;
   if (a.whole) {
     const int item = blockIdx.x / a.c.H;
     at.sequence(a, item / a.blocks);
@@ -386,7 +384,7 @@ cache_attention_kernel(const CaArgs a) {
     at.tile = 0;
     count = at.tiles;
   } else {
-    count = ca_range<KEYS>(a, a.blocks, true, &at, &first, &total);
+    count = ca_range<KEYS>(a, a.blocks, &at, &first, &per);
   }
   if (count == 0) return;
 
@@ -464,6 +462,9 @@ cache_attention_kernel(const CaArgs a) {
           fr[nt][e] = a.scale_rest * pow2(-u);
           m[nt][e] = -FLT_MAX;
           l[nt][e] = 0.f;
+          const int r = at.rb * ROWS + nt * 8 + 2 * c + e, t = r / a.rep;
+          if (a.scores && warp == 0 && g == 0 && r < rows)
+            a.factors[((size_t)at.n * a.T + t) * a.Hq + at.h * a.rep + (r - t * a.rep)] = f[nt][e];
         }
       }
 #pragma unroll
@@ -524,6 +525,20 @@ cache_attention_kernel(const CaArgs a) {
             if (16 * u + 1 >= seen) s[u][nt][e + 2] = -INFINITY;
           }
         }
+    }
+    if (a.scores) {                                  // for what each key gets
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+        if (nt * 8 + 2 * c < a.pad)
+#pragma unroll
+          for (int u = 0; u < SUB; ++u)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const int k = k0 + 16 * u + key + e;
+              if (k < at.len)
+                *reinterpret_cast<float2*>(a.scores + (((size_t)at.n * a.c.H + at.h) * a.c.S + k) * a.pad +
+                                           nt * 8 + 2 * c) = make_float2(s[u][nt][2 * e], s[u][nt][2 * e + 1]);
+            }
     }
     // ---- probabilities: the reference moves when some row of the warp's has left it behind
     float top[NT][2];
@@ -684,6 +699,46 @@ cache_attention_kernel(const CaArgs a) {
         }
       }
     }
+    if (!complete) {
+      // the item's places in the list, and the teams that have parts of it
+      const uint32_t s0 = first + done - tile1, team0 = s0 / per, team1 = (s0 + at.tiles - 1) / per;
+      const int head = blockIdx.x % a.team;
+      auto part = [&](uint32_t t) { return 2 * ((size_t)t * a.team + head) + (t * per < s0); };
+      __threadfence();
+      __syncthreads();
+      if (tid == 0) {
+        uint32_t* left = a.left + part(team0);
+        const uint32_t before = atomicAdd(left, 1u);
+        joins = before == team1 - team0;
+        if (joins) *left = 0;                        // as it was, for the next call
+      }
+      __syncthreads();
+      if (joins) {
+        __threadfence();
+        for (int i = warp; i < ROWS && at.rb * ROWS + i < rows; i += CA_WARPS) {
+          float M = -FLT_MAX, L = 0.f;
+          for (uint32_t t = team0 + lane; t <= team1; t += 32) M = fmaxf(M, __ldcg(&a.ml[part(t) * ROWS + i].x));
+          M = warp_max(M);
+          float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+          for (uint32_t t = team0; t <= team1; ++t) {
+            const size_t p = part(t) * ROWS + i;
+            const float2 z = __ldcg(&a.ml[p]);
+            const float x = ex2(z.x - M);
+            L = fmaf(x, z.y, L);
+            if (lane < DP / 4) {
+              const float4 v = __ldcg(reinterpret_cast<const float4*>(a.po + p * DP + lane * 4));
+              y.x = fmaf(x, v.x, y.x);
+              y.y = fmaf(x, v.y, y.y);
+              y.z = fmaf(x, v.z, y.z);
+              y.w = fmaf(x, v.w, y.w);
+            }
+          }
+          const int r = at.rb * ROWS + i, t = r / a.rep;
+          ca_write<E>(a, at.n, t, at.h * a.rep + (r - t * a.rep), M, L, y, lane);
+        }
+      }
+    }
     if (done == count) break;
     at.next(a, a.blocks);
     if constexpr (Sm::QS) __syncthreads();
@@ -691,58 +746,57 @@ cache_attention_kernel(const CaArgs a) {
   copy_wait<0>();
 }
 
-// The items that several CTAs have parts of: CTA j of a head here looks at the border between teams j and j + 1
-// of the list, and joins the parts of the item there, if that is the item's first border. A warp a row.
-template <int DP, int NT, typename E>
-__global__ void __launch_bounds__(128) cache_attention_join_kernel(const CaArgs a) {
+// What each key gets, from the scores that the kernel left, against their rows' references and sums; a thread a
+// key, and a block KEYS keys of one kv head.
+constexpr int CS_KEYS = 512;
+template <int PIECES>
+__global__ void __launch_bounds__(256) cache_attention_spread_kernel(const CaArgs a, int pieces) {
   pdl_wait();
-  constexpr int ROWS = 8 * NT;
-  __shared__ int found;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, N = a.c.N;
-  const uint32_t team = a.team, border = blockIdx.x / team, head = blockIdx.x - border * team;
-  const uint32_t total = a.start[N], per = ca_per_team(total, gridDim.x / team + 1);
-  const uint32_t x = (border + 1) * per;
-  if (x >= total) return;
-  for (int n = tid; n < N; n += 128)
-    if (a.start[n] <= x && x < a.start[n + 1]) found = n;
+  __shared__ float4 row[16];                         // reference, 1 / sum, factor, what it lacks
+  const int nh = blockIdx.x / pieces, k0 = (blockIdx.x - nh * pieces) * CS_KEYS;
+  const int n = nh / a.c.H, h = nh - n * a.c.H, rows = a.T * a.rep, len = cache_len(a.seq_len[n], a.c.S);
+  if (k0 >= len) return;
+  if (threadIdx.x < a.pad) {
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (threadIdx.x < rows) {
+      const int t = threadIdx.x / a.rep;
+      const size_t at = ((size_t)n * a.T + t) * a.Hq + h * a.rep + (threadIdx.x - t * a.rep);
+      const float2 ml = a.rows[at];
+      const float f = a.factors[at];
+      // rows without keys, or without a finite sum, add nothing
+      if (ml.y > 0.f && ml.y < INFINITY && fabsf(ml.x) < INFINITY)
+        x = make_float4(CA_UP - ml.x, 1.f / ml.y, f, f * a.rest_ratio);
+    }
+    row[threadIdx.x] = x;
+  }
   __syncthreads();
-  const int n = found;
-  const uint32_t s0 = a.start[n], tiles = (a.start[n + 1] - s0) / (a.c.H / team * a.blocks);
-  const uint32_t item = (x - s0) / tiles, s = s0 + item * tiles, e = s + tiles;
-  const uint32_t b0 = s / per, b1 = (e - 1) / per;
-  if (x == s || b0 != border) return;
-  const int ht = item / a.blocks, rb = item - ht * a.blocks, h = ht * team + head, rows = a.T * a.rep;
-  for (int i = warp; i < ROWS; i += 4) {
-    const int r = rb * ROWS + i;
-    if (r >= rows) break;
-    auto place = [&](uint32_t b) { return (2 * ((size_t)b * team + head) + (b * per < s)) * ROWS + i; };
-    float M = -FLT_MAX, L = 0.f;
-    for (uint32_t b = b0 + lane; b <= b1; b += 32) M = fmaxf(M, a.ml[place(b)].x);
-    M = warp_max(M);
-    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (uint32_t b = b0; b <= b1; ++b) {
-      const size_t p = place(b);
-      const float2 z = a.ml[p];
-      const float f = ex2(z.x - M);
-      L = fmaf(f, z.y, L);
-      if (lane < DP / 4) {
-        const float4 v = *reinterpret_cast<const float4*>(a.po + p * DP + lane * 4);
-        y.x = fmaf(f, v.x, y.x);
-        y.y = fmaf(f, v.y, y.y);
-        y.z = fmaf(f, v.z, y.z);
-        y.w = fmaf(f, v.w, y.w);
+  const size_t base = ((size_t)n * a.c.H + h) * a.c.S;
+#pragma unroll
+  for (int i = 0; i < CS_KEYS / 256; ++i) {
+    const int k = k0 + i * 256 + threadIdx.x;
+    if (k >= len) break;
+    float sum = 0.f;
+    for (int r = 0; r < a.pad; r += 2) {
+      const float2 s = __ldcs(reinterpret_cast<const float2*>(a.scores + (base + k) * a.pad + r));
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float4 x = row[r + e];
+        const float v = e ? s.y : s.x;
+        if (x.y > 0.f && v > -INFINITY) {            // (a row that may not see the key has -infinity there)
+          float t = x.x;
+          if (PIECES > 1) t = fmaf(v, x.w, t);
+          sum = fmaf(ex2(fmaf(v, x.z, t)), x.y, sum);
+        }
       }
     }
-    const int t = r / a.rep;
-    ca_write<E>(a, n, t, h * a.rep + (r - t * a.rep), M, L, y, lane);
+    a.weights[base + k] += sum;
   }
 }
 
-// What each key gets: the scores once more, against their rows' references and sums, a warp 16 keys; rows go
+// The same where rows are too many to keep their scores: computed once more, a warp 16 keys; rows go
 // through shared memory 8 NT at a time, and each key's weight is read and written by one lane.
 template <int DP, int DIM, int NT, int PIECES, typename E>
-__global__ void __launch_bounds__(CA_THREADS, 2) cache_attention_weights_kernel(const CaArgs a) {
+__global__ void __launch_bounds__(CA_THREADS, NT > 2 ? 1 : 2) cache_attention_weights_kernel(const CaArgs a) {
   pdl_wait();
   constexpr int KS = CaCfg<DP>::KS, ST = 4, ROWS = 8 * NT, STAGE = 16 * (DP / 2 + 16), KEYS = 16 * CA_WARPS;
   extern __shared__ __align__(16) unsigned char sm[];
@@ -750,8 +804,8 @@ __global__ void __launch_bounds__(CA_THREADS, 2) cache_attention_weights_kernel(
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
   const int d = DIM ? DIM : a.c.d, R = (cache_half_bytes(d) + 15) / 16 * 16, rows = a.T * a.rep;
   CaCursor<KEYS> at;
-  uint32_t first, total;
-  uint32_t count = ca_range<KEYS>(a, 1, false, &at, &first, &total);
+  uint32_t first, per;
+  uint32_t count = ca_range<KEYS>(a, 1, &at, &first, &per);
   const CaLane<DP> mine(a, R, lane);
   unsigned char* stage = sm + warp * ST * STAGE;
   const int key = key_of(g);
@@ -864,9 +918,11 @@ lilicorr_status_t ca_launch(const CaArgs& a, const CaPlan& p, cudaStream_t st) {
   LL_TRY(allow_max_dynamic_smem(kernel, configured));
   LL_TRY(launch_k(kernel, p.whole ? (unsigned)p.items : (unsigned)p.ctas, CA_THREADS, CaSmem<DP, NT, PIECES>::TOTAL,
                   st, a));
-  if (!p.whole)
-    LL_TRY(launch_k(cache_attention_join_kernel<DP, NT, E>, (unsigned)(p.ctas - p.team), 128, 0, st, a));
   if (!a.weights) return LILICORR_OK;
+  if (a.scores) {
+    const int pieces = (a.c.S + CS_KEYS - 1) / CS_KEYS;
+    return launch_k(cache_attention_spread_kernel<PIECES>, (unsigned)(a.c.N * a.c.H * pieces), 256, 0, st, a, pieces);
+  }
   constexpr int WT = PIECES > 1 ? 1 : NT;
   auto* weights = cache_attention_weights_kernel<DP, DIM, WT, PIECES, E>;
   LL_TRY(allow_max_dynamic_smem(weights, configured_w));
