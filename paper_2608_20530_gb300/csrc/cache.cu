@@ -271,115 +271,317 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
   return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
 }
 
-constexpr int EV_THREADS = 1024;
+// A cluster of CTAs has one (sequence, kv head). Which positions stay is found by each of them for itself where
+// there are few (a barrier of the cluster costs as much as a pass), else each looks at a stretch of them. The
+// records that stay are moved by all of them together.
+constexpr int EV_THREADS = 512, EV_WARPS = EV_THREADS / 32;
+constexpr int EV_BINS = 2048;  // 11 bits a round
+constexpr int EV_COPIES = 4;   // of the counts: weights are alike in their upper bits, and lanes would queue
+constexpr int EV_KEYS = 8192;  // of a stretch, kept in shared memory; longer ones are read again each time
+constexpr int EV_RANKED = 384; // so many on the border are compared with one another
+constexpr int EV_VECS = 8;     // 16-byte pieces that a thread moves at a time
 
-// Exclusive sums of two flags over the block; `sums`: 64 words.
-__device__ __forceinline__ void scan2(bool a, bool b, int* sums, int& ra, int& rb, int& ta, int& tb) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const uint32_t ba = __ballot_sync(0xffffffffu, a), bb = __ballot_sync(0xffffffffu, b);
-  const uint32_t below = (1u << lane) - 1u;
-  __syncthreads();
-  if (lane == 0) {
-    sums[warp] = __popc(ba);
-    sums[32 + warp] = __popc(bb);
-  }
-  __syncthreads();
-  ra = __popc(ba & below);
-  rb = __popc(bb & below);
-  ta = tb = 0;
-  for (int i = 0; i < EV_THREADS / 32; ++i) {
-    const int x = sums[i], y = sums[32 + i];
-    if (i < warp) { ra += x; rb += y; }
-    ta += x;
-    tb += y;
-  }
+struct EvictSmem {
+  union {
+    int hist[EV_BINS * EV_COPIES];
+    int kept[EV_KEYS];                       // the list, where every CTA has all of it; else positions in hand
+  };
+  int sum[3][EV_BINS];                       // of rounds in turn; the first CTA's are the cluster's
+  int total;                                 // of this CTA's stretch, read by the others
+  int warp[EV_WARPS];
+  int found[3];
+  int place[EV_WARPS][EV_WARPS];
+  int cands;
+  uint64_t border;
+  uint64_t cand[EV_RANKED];
+  uint32_t keys[EV_KEYS];
+};
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ uint32_t cluster_size() {
+  uint32_t r;
+  asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t peer(const int* p, uint32_t rank) {   // the same variable of another CTA
+  uint32_t to;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+  return to;
+}
+__device__ __forceinline__ int peer_int(const int* p, uint32_t rank) {
+  int v;
+  asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(peer(p, rank)) : "memory");
+  return v;
+}
+__device__ __forceinline__ int4 peer_int4(const int* p, uint32_t rank) {
+  int4 v;
+  asm volatile("ld.shared::cluster.v4.s32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(peer(p, rank)) : "memory");
+  return v;
+}
+__device__ __forceinline__ void peer_add(int* p, uint32_t rank, int v) {
+  asm volatile("red.relaxed.cluster.shared::cluster.add.s32 [%0], %1;" ::"r"(peer(p, rank)), "r"(v) : "memory");
 }
 
-// The positions that stay, a CTA a (sequence, head): the weight of the last one that does, digit by digit
-// from the top, then all positions in order.
-__global__ void __launch_bounds__(EV_THREADS) cache_choose_kernel(const EvictArgs a) {
+// Sum over the block, to all threads.
+__device__ __forceinline__ int block_sum(int v, int* warp) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) warp[threadIdx.x >> 5] = v;
+  __syncthreads();
+  int t = 0;
+#pragma unroll
+  for (int w = 0; w < EV_WARPS; ++w) t += warp[w];
+  return t;
+}
+
+__global__ void __launch_bounds__(EV_THREADS, 2) cache_evict_kernel(const EvictArgs a) {
   pdl_wait();
-  __shared__ int hist[256], sums[64], found[2];
-  const int n = blockIdx.x / a.from.H, tid = threadIdx.x;
-  const int raw = a.seq_len[n], L = cache_len(raw, a.from.S);
-  const float* w = a.w + (size_t)blockIdx.x * a.from.S;
-  int32_t* kept = a.kept + (size_t)blockIdx.x * a.budget;
-  if (blockIdx.x % a.from.H == 0 && tid == 0) a.new_len[n] = raw < 0 ? raw : min(L, a.budget);
-  if (L <= a.budget) {
-    for (int i = tid; i < a.budget; i += EV_THREADS) kept[i] = i < L ? i : -1;
-    return;
-  }
-  const int lo = a.first, hi = L - a.recent;
-  int left = a.budget - a.first - a.recent;          // to be found among [lo, hi)
-  uint32_t top = 0;                                  // the digits known so far
-  const bool some = left > 0;
-  if (some)
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      for (int i = tid; i < 256; i += EV_THREADS) hist[i] = 0;
-      __syncthreads();
-      for (int i = lo + tid; i < hi; i += EV_THREADS) {
-        const uint32_t k = weight_key(w[i]);
-        if (shift == 24 || k >> (shift + 8) == top >> (shift + 8)) atomicAdd(&hist[(k >> shift) & 255], 1);
+  extern __shared__ __align__(16) unsigned char sm[];
+  EvictSmem& x = *reinterpret_cast<EvictSmem*>(sm);
+  const uint32_t C = cluster_size(), rank = cluster_rank();
+  const int item = blockIdx.x / C, n = item / a.from.H, h = item - n * a.from.H;
+  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+  const int raw = a.seq_len[n], L = cache_len(raw, a.from.S), stay = min(L, a.budget);
+  const float* w = a.w + (size_t)item * a.from.S;
+  float* to_w = a.to_w + (size_t)item * a.to.S;
+  int32_t* kept = a.kept + (size_t)item * a.budget;
+  if (h == 0 && rank == 0 && tid == 0) a.new_len[n] = raw < 0 ? raw : stay;
+  for (int j = stay + rank * EV_THREADS + tid; j < a.budget; j += C * EV_THREADS) kept[j] = -1;
+  const bool all = L <= a.budget;
+  if (all)
+    for (int j = rank * EV_THREADS + tid; j < L; j += C * EV_THREADS) kept[j] = j;
+  if (stay == 0 || (all && a.in_place)) return;      // (all CTAs of the cluster)
+  const bool whole = L <= EV_KEYS;                   // each CTA has all positions, and the whole list
+  if (!all) {
+    const bool split = !whole && C > 1;
+    const int chunk = split ? (int)(((int64_t)L + C - 1) / C + EV_THREADS - 1) / EV_THREADS * EV_THREADS : L;
+    const int p0 = split ? min((int64_t)L, (int64_t)rank * chunk) : 0, p1 = min((int64_t)L, (int64_t)p0 + chunk);
+    const int lo = a.first, hi = L - a.recent, c0 = max(p0, lo), c1 = min(p1, hi);
+    const bool cached = chunk <= EV_KEYS;
+    if (cached)
+      for (int i = p0 + tid; i < p1; i += EV_THREADS) x.keys[i - p0] = weight_key(w[i]);
+    auto key = [&](int i) { return cached ? x.keys[i - p0] : weight_key(w[i]); };
+    // Larger weights first, then lower positions: the order of weight << 32 | ~position.
+    auto order = [&](int i) { return (uint64_t)key(i) << 32 | (uint32_t)~i; };
+    int left = a.budget - a.first - a.recent;        // to be found among [lo, hi)
+    uint64_t border = ~0ull;                         // of them, the last in this order that stays
+    if (left > 0) {
+      for (int i = tid; i < EV_BINS * EV_COPIES / 4; i += EV_THREADS)
+        reinterpret_cast<int4*>(x.hist)[i] = make_int4(0, 0, 0, 0);
+      if (tid == 0) x.cands = 0;
+      if (split) {
+        for (int i = tid; i < 3 * EV_BINS / 4; i += EV_THREADS)
+          reinterpret_cast<int4*>(&x.sum[0][0])[i] = make_int4(0, 0, 0, 0);
+        cluster_sync();
       }
       __syncthreads();
-      if (tid == 0) {
-        int b = 255, need = left;
-        while (b > 0 && hist[b] < need) need -= hist[b--];
-        found[0] = b;
-        found[1] = need;
+      // eleven bits a round from the top, those of positions only where weights are equal
+      border = 0;
+#pragma unroll 1
+      for (int round = 0; round < 6; ++round) {
+        const int shift = 64 - 11 * (round + 1) > 0 ? 64 - 11 * (round + 1) : 0;
+        const uint64_t known = round == 0 ? 0ull : ~0ull << (64 - 11 * round);
+        const uint32_t digits = shift ? 2047 : (1 << (64 - 55)) - 1;
+        for (int i = c0 + tid; i < c1; i += EV_THREADS) {
+          const uint64_t k = order(i);
+          if (((k ^ border) & known) == 0)
+            atomicAdd(&x.hist[((uint32_t)(k >> shift) & digits) * EV_COPIES + (lane & (EV_COPIES - 1))], 1);
+        }
+        __syncthreads();
+        // each thread EV_BINS / EV_THREADS = 4 bins, the largest digits first
+        const int b0 = EV_BINS - 4 - 4 * tid;
+        int part[4];
+        int* sum = x.sum[round % 3];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int4 v = reinterpret_cast<const int4*>(x.hist)[b0 + i];
+          part[i] = v.x + v.y + v.z + v.w;
+          if (part[i]) {
+            reinterpret_cast<int4*>(x.hist)[b0 + i] = make_int4(0, 0, 0, 0);
+            if (split) peer_add(&sum[b0 + i], 0, part[i]);
+          }
+        }
+        if (split) {
+          cluster_sync();
+          const int4 t = peer_int4(&sum[b0], 0);
+          part[0] = t.x; part[1] = t.y; part[2] = t.z; part[3] = t.w;
+          // last read before this barrier, next written after the one to come
+          reinterpret_cast<int4*>(x.sum[(round + 2) % 3])[tid] = make_int4(0, 0, 0, 0);
+        }
+        const int mine = part[0] + part[1] + part[2] + part[3];
+        int before = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int y = __shfl_up_sync(0xffffffffu, before, o);
+          if (lane >= o) before += y;
+        }
+        if (lane == 31) x.warp[wid] = before;
+        __syncthreads();
+        before -= mine;
+#pragma unroll
+        for (int v = 0; v < EV_WARPS; ++v)
+          if (v < wid) before += x.warp[v];
+#pragma unroll
+        for (int i = 3; i >= 0; --i) {
+          if (before < left && left <= before + part[i]) {     // one bin of one thread
+            x.found[0] = b0 + i;
+            x.found[1] = left - before;
+            x.found[2] = part[i];
+          }
+          before += part[i];
+        }
+        __syncthreads();
+        border |= (uint64_t)x.found[0] << shift;
+        left = x.found[1];
+        const int cands = x.found[2];
+        if (left == cands) break;                    // all that begin so stay
+        if (whole && cands <= EV_RANKED) {
+          const uint64_t same = ~0ull << shift;
+          for (int i = c0 + tid; i < c1; i += EV_THREADS) {
+            const uint64_t k = order(i);
+            if (((k ^ border) & same) == 0) x.cand[atomicAdd(&x.cands, 1)] = k;
+          }
+          __syncthreads();
+          if (tid < cands) {
+            const uint64_t k = x.cand[tid];
+            int larger = 0;
+#pragma unroll 8
+            for (int i = 0; i < cands; ++i) larger += x.cand[i] > k;
+            if (larger == left - 1) x.border = k;
+          }
+          __syncthreads();
+          border = x.border;
+          break;
+        }
       }
-      __syncthreads();
-      top |= (uint32_t)found[0] << shift;
-      left = found[1];
     }
-  // of the weights equal to `top`, `left` stay
-  int at = 0, equal = 0;
-  for (int i0 = 0; i0 < L; i0 += EV_THREADS) {
-    const int i = i0 + tid;
-    const bool there = i < L, fixed = i < lo || i >= hi;
-    const uint32_t k = there && !fixed ? weight_key(w[i]) : 0;
-    const bool same = there && !fixed && some && k == top;
-    int r_same, r_keep, t_same, t_keep;
-    scan2(same, false, sums, r_same, r_keep, t_same, t_keep);
-    const bool keep = there && (fixed || (some && (k > top || (same && equal + r_same < left))));
-    equal += t_same;
-    scan2(keep, false, sums, r_keep, r_same, t_keep, t_same);
-    if (keep) kept[at + r_keep] = i;
-    at += t_keep;
+    __syncthreads();
+    // ---- each one's place, in order of position
+    auto stays = [&](int i) { return i < lo || i >= hi || order(i) >= border; };
+    int places = 0;                          // before this stretch
+    if (split) {
+      int m = 0;
+      for (int i = p0 + tid; i < p1; i += EV_THREADS) m += stays(i);
+      m = block_sum(m, x.warp);
+      if (tid == 0) x.total = m;
+      cluster_sync();
+      for (uint32_t r = 0; r < rank; ++r) places += peer_int(&x.total, r);
+    }
+    int32_t* list = whole ? x.kept : kept;
+#pragma unroll 1
+    for (int i0 = p0; i0 < p1; i0 += EV_THREADS * EV_WARPS) {
+      // sixteen positions a thread, EV_THREADS apart: counts of each 32 neighbours, then their sums
+      uint32_t ma[EV_WARPS];
+#pragma unroll
+      for (int u = 0; u < EV_WARPS; ++u) {
+        ma[u] = 0;
+        if (i0 + u * EV_THREADS < p1) {
+          const int i = i0 + u * EV_THREADS + tid;
+          ma[u] = __ballot_sync(0xffffffffu, i < p1 && stays(i));
+        }
+        if (lane == 0) x.place[u][wid] = __popc(ma[u]);
+      }
+      __syncthreads();
+      if (wid == 0) {                        // exclusive sums in order of (u, warp), eight entries a lane
+        int* p = &x.place[0][0] + lane * 8;
+        int v[8], t = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          v[i] = t;
+          t += p[i];
+        }
+        int sum = t;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int y = __shfl_up_sync(0xffffffffu, sum, o);
+          if (lane >= o) sum += y;
+        }
+        if (lane == 31) x.found[0] = sum;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i] = sum - t + v[i];
+      }
+      __syncthreads();
+      const uint32_t below = (1u << lane) - 1u;
+#pragma unroll
+      for (int u = 0; u < EV_WARPS; ++u)
+        if (ma[u] >> lane & 1) list[places + x.place[u][wid] + __popc(ma[u] & below)] = i0 + u * EV_THREADS + tid;
+      places += x.found[0];
+      __syncthreads();
+    }
+    if (whole) {
+      for (int j = rank * EV_THREADS + tid; j < stay; j += C * EV_THREADS) kept[j] = x.kept[j];
+    } else {
+      cluster_sync();                        // the list is whole
+    }
   }
-}
 
-constexpr int EV_STAGE = 128;  // records that move at a time
-
-// The records and weights that stay, moved to the front, a CTA a (sequence, head). In place a record moves to
-// its own or a lower position, past all that later ones come from, so records go in order, EV_STAGE at a
-// time, all of them read before any of them is written.
-__global__ void __launch_bounds__(256) cache_move_kernel(const EvictArgs a) {
-  pdl_wait();
-  __shared__ __align__(16) unsigned char stage[EV_STAGE * cache_record_bytes(128)];
-  __shared__ float sw[EV_STAGE];
-  const int n = blockIdx.x / a.from.H, h = blockIdx.x % a.from.H, tid = threadIdx.x;
-  const int L = cache_len(a.seq_len[n], a.from.S), keep = min(L, a.budget);
-  if (a.in_place && L <= a.budget) return;
-  const int32_t* kept = a.kept + (size_t)blockIdx.x * a.budget;
-  const float* w = a.w + (size_t)blockIdx.x * a.from.S;
-  float* to_w = a.to_w + (size_t)blockIdx.x * a.to.S;
+  // ---- records and weights that stay, in order, EV_VECS pieces a thread at a time. In place a record moves to
+  // its own or a lower position, past all that later ones come from: what is in hand is read by all CTAs before
+  // any of it is written.
   const int vecs = cache_record_bytes(a.from.d) / 16;
-  for (int j0 = 0; j0 < keep; j0 += EV_STAGE) {
-    const int m = min(EV_STAGE, keep - j0);
-    for (int i = tid; i < m * vecs; i += 256) {
-      const int j = i / vecs, v = i - j * vecs;
-      reinterpret_cast<uint4*>(stage)[i] = reinterpret_cast<const uint4*>(a.from.at(n, kept[j0 + j], h))[v];
+  const int mine = EV_THREADS * EV_VECS / vecs;      // records of a CTA at a time: 455 of 144 bytes
+  const int step = EV_THREADS / vecs, rest = EV_THREADS - step * vecs;
+  const int jt = tid / vecs, pt = tid - jt * vecs;
+  const unsigned char* from = a.from.at(n, 0, h);
+  unsigned char* to = a.to.at(n, 0, h);
+  const uint32_t from_s = (uint32_t)a.from.s[1], to_s = (uint32_t)a.to.s[1];
+#pragma unroll 1
+  for (int64_t r0 = 0; r0 < stay; r0 += (int64_t)C * mine) {
+    const int64_t j0 = r0 + (int64_t)rank * mine;
+    const int m = (int)max((int64_t)0, min((int64_t)mine, stay - j0));
+    const int* list = whole && !all ? x.kept + j0 : x.kept;
+    if (all || !whole) {
+      __syncthreads();
+      for (int j = tid; j < m; j += EV_THREADS) x.kept[j] = all ? (int)j0 + j : __ldcg(&kept[j0 + j]);
+      __syncthreads();
     }
-    if (tid < m) sw[tid] = w[kept[j0 + tid]];
-    __syncthreads();
-    for (int i = tid; i < m * vecs; i += 256) {
-      const int j = i / vecs, v = i - j * vecs;
-      reinterpret_cast<uint4*>(a.to.at(n, j0 + j, h))[v] = reinterpret_cast<const uint4*>(stage)[i];
+    uint4 v[EV_VECS];
+    float wv[4];                             // (narrow records: up to 2,048 of them)
+    int j = jt, part = pt;
+#pragma unroll
+    for (int u = 0; u < EV_VECS; ++u) {
+      if (j < m) v[u] = __ldcs(reinterpret_cast<const uint4*>(from + (uint64_t)(uint32_t)list[j] * from_s) + part);
+      j += step;
+      part += rest;
+      if (part >= vecs) {
+        part -= vecs;
+        ++j;
+      }
     }
-    if (tid < m) to_w[j0 + tid] = sw[tid];
-    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (tid + u * EV_THREADS < m) wv[u] = w[list[tid + u * EV_THREADS]];
+    if (a.in_place) {
+      if (C > 1) cluster_sync();
+      else __syncthreads();
+    }
+    unsigned char* dst = to + (uint64_t)(uint32_t)j0 * to_s;
+    j = jt;
+    part = pt;
+#pragma unroll
+    for (int u = 0; u < EV_VECS; ++u) {
+      if (j < m) reinterpret_cast<uint4*>(dst + (uint64_t)(uint32_t)j * to_s)[part] = v[u];
+      j += step;
+      part += rest;
+      if (part >= vecs) {
+        part -= vecs;
+        ++j;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (tid + u * EV_THREADS < m) to_w[j0 + tid + u * EV_THREADS] = wv[u];
   }
+  if (C > 1 && !whole) cluster_sync();       // nobody leaves while its counts may be read
 }
 
 // [first byte, last byte] of a cache's records, as offsets from 0
@@ -432,9 +634,15 @@ lilicorr_status_t run_evict(const lilicorr_cache_desc* desc, void* cache, float*
   a.in_place = into == nullptr;
   a.kept = kept;
   a.new_len = new_len;
-  const unsigned grid = (unsigned)(desc->sequences * desc->kv_heads);
-  LL_TRY(launch_k(cache_choose_kernel, grid, EV_THREADS, 0, st, a));
-  return launch_k(cache_move_kernel, grid, 256, 0, st, a);
+  // as many CTAs an item as keep two an SM busy, up to eight
+  const int64_t items = (int64_t)desc->sequences * desc->kv_heads;
+  int cluster = 8;
+  while (cluster > 1 && items * cluster > 2 * num_sms()) cluster /= 2;
+  if (items * cluster > 0x7FFFFFFFll) return LILICORR_ERR_SHAPE;
+  static bool configured[64] = {false};
+  LL_TRY(allow_max_dynamic_smem(cache_evict_kernel, configured));
+  return launch_cluster_k(cache_evict_kernel, (unsigned)(items * cluster), EV_THREADS, sizeof(EvictSmem), cluster,
+                          st, a);
 }
 
 }  // namespace
