@@ -61,56 +61,43 @@ struct CaCursor {
   }
 };
 
-// This CTA's part of the list: as many tiles as it returns, from `at` on, which is place `first` of the list.
+// This CTA's part of the list: as many tiles as it returns, from `at` on, which is place `first` of the list. Each
+// warp finds it for itself.
 template <int KEYS>
 __device__ __forceinline__ uint32_t ca_range(const CaArgs& a, int blocks, CaCursor<KEYS>* at, uint32_t* first,
                                              uint32_t* per) {
-  __shared__ uint32_t sums[CA_WARPS];
-  __shared__ uint32_t place[2];
-  __shared__ int length;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int N = a.c.N, chunk = (N + CA_THREADS - 1) / CA_THREADS;
-  const int n0 = min(N, tid * chunk), n1 = min(N, n0 + chunk);
+  const int lane = threadIdx.x & 31, N = a.c.N, chunk = (N + 31) / 32;
+  const int n0 = min(N, lane * chunk), n1 = min(N, n0 + chunk);
   const uint32_t per_tile = (uint32_t)(a.c.H / a.team) * blocks;
-  int raw = -1;                                      // of n0, the only one in most calls
+  int raw = -1;                                      // of n0, the only one up to 32 sequences
   if (n0 < n1) raw = a.seq_len[n0];
-  uint32_t mine = ca_tiles<KEYS>(raw, a.c.S) * per_tile;
-  for (int n = n0 + 1; n < n1; ++n) mine += ca_tiles<KEYS>(a.seq_len[n], a.c.S) * per_tile;
-  uint32_t incl = mine;
+  uint32_t mine = ca_tiles<KEYS>(raw, a.c.S);
+#pragma unroll 4
+  for (int n = n0 + 1; n < n1; ++n) mine += ca_tiles<KEYS>(a.seq_len[n], a.c.S);
+  mine *= per_tile;
+  uint32_t upto = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const uint32_t x = __shfl_up_sync(0xffffffffu, incl, o);
-    if (lane >= o) incl += x;
+    const uint32_t x = __shfl_up_sync(0xffffffffu, upto, o);
+    if (lane >= o) upto += x;
   }
-  if (lane == 31) sums[warp] = incl;
-  __syncthreads();
-  uint32_t before = incl - mine, total = 0;
-#pragma unroll
-  for (int w = 0; w < CA_WARPS; ++w) {
-    if (w < warp) before += sums[w];
-    total += sums[w];
-  }
-  const uint32_t g = blockIdx.x / a.team;
+  const uint32_t total = __shfl_sync(0xffffffffu, upto, 31), g = blockIdx.x / a.team;
   *per = ca_per_team(total, gridDim.x / a.team);
   *first = g * *per;
   if (*first >= total) return 0;
-  if (before <= *first && *first < before + mine) {  // one thread
-    uint32_t b = before;
-    int n = n0;
+  const int owner = __ffs(__ballot_sync(0xffffffffu, *first < upto)) - 1;
+  uint32_t b = upto - mine;
+  int n = n0;
+  if (lane == owner && chunk > 1)
     while (true) {
       const uint32_t t = ca_tiles<KEYS>(raw, a.c.S) * per_tile;
       if (*first < b + t) break;
       b += t;
       raw = a.seq_len[++n];
     }
-    place[0] = n;
-    place[1] = *first - b;
-    length = raw;
-  }
-  __syncthreads();
-  at->set(a, place[0], length);
-  const uint32_t item = place[1] / at->tiles;
-  at->tile = place[1] - item * at->tiles;
+  at->set(a, __shfl_sync(0xffffffffu, n, owner), __shfl_sync(0xffffffffu, raw, owner));
+  const uint32_t place = *first - __shfl_sync(0xffffffffu, b, owner), item = place / at->tiles;
+  at->tile = place - item * at->tiles;
   at->h = item / blocks;
   at->rb = item - at->h * blocks;
   at->h = at->h * a.team + (blockIdx.x - g * a.team);
@@ -704,40 +691,49 @@ cache_attention_kernel(const CaArgs a) {
       const uint32_t s0 = first + done - tile1, team0 = s0 / per, team1 = (s0 + at.tiles - 1) / per;
       const int head = blockIdx.x % a.team;
       auto part = [&](uint32_t t) { return 2 * ((size_t)t * a.team + head) + (t * per < s0); };
-      __threadfence();
       __syncthreads();
       if (tid == 0) {
+        __threadfence();
         uint32_t* left = a.left + part(team0);
-        const uint32_t before = atomicAdd(left, 1u);
-        joins = before == team1 - team0;
+        joins = atomicAdd(left, 1u) == team1 - team0;
         if (joins) *left = 0;                        // as it was, for the next call
+        __threadfence();
       }
       __syncthreads();
-      if (joins) {
-        __threadfence();
+      if (joins)
         for (int i = warp; i < ROWS && at.rb * ROWS + i < rows; i += CA_WARPS) {
           float M = -FLT_MAX, L = 0.f;
-          for (uint32_t t = team0 + lane; t <= team1; t += 32) M = fmaxf(M, __ldcg(&a.ml[part(t) * ROWS + i].x));
-          M = warp_max(M);
           float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-          for (uint32_t t = team0; t <= team1; ++t) {
-            const size_t p = part(t) * ROWS + i;
-            const float2 z = __ldcg(&a.ml[p]);
-            const float x = ex2(z.x - M);
-            L = fmaf(x, z.y, L);
-            if (lane < DP / 4) {
-              const float4 v = __ldcg(reinterpret_cast<const float4*>(a.po + p * DP + lane * 4));
-              y.x = fmaf(x, v.x, y.x);
-              y.y = fmaf(x, v.y, y.y);
-              y.z = fmaf(x, v.z, y.z);
-              y.w = fmaf(x, v.w, y.w);
+          for (uint32_t t0 = team0; t0 <= team1; t0 += 4) {        // four parts at a time
+            float2 z[4];
+            float4 v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              z[j] = make_float2(-FLT_MAX, 0.f);
+              v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+              if (t0 + j <= team1) {
+                const size_t p = part(t0 + j) * ROWS + i;
+                z[j] = __ldcg(&a.ml[p]);
+                if (lane < DP / 4) v[j] = __ldcg(reinterpret_cast<const float4*>(a.po + p * DP + lane * 4));
+              }
+            }
+            const float to = fmaxf(fmaxf(fmaxf(z[0].x, z[1].x), fmaxf(z[2].x, z[3].x)), M), x0 = ex2(M - to);
+            M = to;
+            L *= x0;
+            y.x *= x0; y.y *= x0; y.z *= x0; y.w *= x0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float x = ex2(z[j].x - to);
+              L = fmaf(x, z[j].y, L);
+              y.x = fmaf(x, v[j].x, y.x);
+              y.y = fmaf(x, v[j].y, y.y);
+              y.z = fmaf(x, v[j].z, y.z);
+              y.w = fmaf(x, v[j].w, y.w);
             }
           }
           const int r = at.rb * ROWS + i, t = r / a.rep;
           ca_write<E>(a, at.n, t, at.h * a.rep + (r - t * a.rep), M, L, y, lane);
         }
-      }
     }
     if (done == count) break;
     at.next(a, a.blocks);
@@ -913,16 +909,17 @@ __global__ void __launch_bounds__(CA_THREADS, NT > 2 ? 1 : 2) cache_attention_we
 
 template <int DP, int DIM, int NT, int PIECES, typename E>
 lilicorr_status_t ca_launch(const CaArgs& a, const CaPlan& p, cudaStream_t st) {
-  static bool configured[64] = {false}, configured_w[64] = {false};
+  static bool configured[64] = {false};
   auto* kernel = cache_attention_kernel<DP, DIM, NT, PIECES, E>;
   LL_TRY(allow_max_dynamic_smem(kernel, configured));
-  LL_TRY(launch_k(kernel, p.whole ? (unsigned)p.items : (unsigned)p.ctas, CA_THREADS, CaSmem<DP, NT, PIECES>::TOTAL,
-                  st, a));
+  LL_TRY(launch_k(kernel, p.whole ? (unsigned)p.items : (unsigned)p.ctas, CA_THREADS, CaSmem<DP, NT, PIECES>::TOTAL, st,
+                  a));
   if (!a.weights) return LILICORR_OK;
   if (a.scores) {
     const int pieces = (a.c.S + CS_KEYS - 1) / CS_KEYS;
     return launch_k(cache_attention_spread_kernel<PIECES>, (unsigned)(a.c.N * a.c.H * pieces), 256, 0, st, a, pieces);
   }
+  static bool configured_w[64] = {false};
   constexpr int WT = PIECES > 1 ? 1 : NT;
   auto* weights = cache_attention_weights_kernel<DP, DIM, WT, PIECES, E>;
   LL_TRY(allow_max_dynamic_smem(weights, configured_w));
