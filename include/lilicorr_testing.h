@@ -111,6 +111,19 @@ int lilicorr_test_fused_path(const lilicorr_head* head, int mode);
  * Process-wide, like the switch above. Returns the previous mode. */
 int lilicorr_test_attention_path(int mode);
 
+/* How lilicorr_cache_attention takes bf16 queries (0 by their number, 1 the tensor-core kernel, 2 mma.sync),
+ * the size of its workspace included. Returns the previous mode. */
+int lilicorr_test_cache_attention_path(int mode);
+
+/* lilicorr_cache_attention without weights on its tensor-core kernel, which expands no keys (`which` 1) or
+ * values (2) for its products, and a limit as above: the workspace's status word receives LILICORR_ERR_TIMEOUT, the
+ * outputs unspecified values. LILICORR_ERR_SHAPE where another kernel takes the call. */
+lilicorr_status_t lilicorr_test_cache_attention_timeout(const lilicorr_cache_attention_desc* desc, const void* q,
+                                                        const void* cache, const int32_t* seq_len, void* out,
+                                                        float* lse, void* ws, size_t ws_bytes,
+                                                        long long wait_cycles, int which,
+                                                        cudaStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

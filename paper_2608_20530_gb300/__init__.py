@@ -124,6 +124,8 @@ _SIGS = {
     "lilicorr_cache_read": (_I, [_P, _P, _I, _I, _P, _P, _P, _P, _P, _P]),
     "lilicorr_cache_attention_workspace_bytes": (_S, [_P]),
     "lilicorr_cache_attention": (_I, [_P] * 8 + [_S, _P]),
+    "lilicorr_test_cache_attention_path": (_I, [_I]),
+    "lilicorr_test_cache_attention_timeout": (_I, [_P] * 7 + [_S, ctypes.c_longlong, _I, _P]),
     "lilicorr_cache_evict": (_I, [_P] * 4 + [_I] * 3 + [_P] * 6),
     "lilicorr_test_prefix_attention_timeout": (_I, [_P] * 11 + [_S, ctypes.c_longlong, _I, _P]),
     "lilicorr_test_linear": (_I, [_P, _I, _I, _P, _I, _I, _P, _I, _I, _I, _I, _I, _P, _P, _I, _I,
@@ -1055,6 +1057,26 @@ def test_prefix_path(mode: int) -> int:
     """Test hook: how prefix_attention takes a bf16 prefix (0 by size, 1 the tensor-core kernel, 2 the
     mma.sync kernels). Returns the previous mode."""
     return int(lib().lilicorr_test_prefix_path(int(mode)))
+
+
+def test_cache_attention_path(mode: int) -> int:
+    """Test hook: how cache_attention takes bf16 queries (0 by their number, 1 the tensor-core kernel, 2 the
+    mma.sync kernels). Returns the previous mode."""
+    return int(lib().lilicorr_test_cache_attention_path(int(mode)))
+
+
+def test_cache_attention_timeout(q: torch.Tensor, cache: torch.Tensor, seq_len: torch.Tensor, ws: Workspace,
+                                 wait_cycles: int, which: int) -> None:
+    """Test hook: cache_attention of a dense q on its tensor-core kernel without its keys (``which`` 1) or
+    values (2), so that its bounded waits run out and ``ws`` holds the timeout status."""
+    N, S, H, R = cache.shape
+    _, T, Hq, d = q.shape
+    out, lse = torch.empty_like(q), torch.empty((N, T, Hq), dtype=torch.float32, device=q.device)
+    desc = _CA_DESC.pack(N, S, H, d, *cache.stride()[:3], 1.0, 1.0, T, Hq, _dtype_code(q), d ** -0.5,
+                         *q.stride()[:3], *out.stride()[:3])
+    _check(lib().lilicorr_test_cache_attention_timeout(
+        desc, q.data_ptr(), cache.data_ptr(), seq_len.data_ptr(), out.data_ptr(), lse.data_ptr(), ws.ptr, ws.nbytes,
+        int(wait_cycles), int(which), _stream()), "test_cache_attention_timeout")
 
 
 def test_attention_path(mode: int) -> int:

@@ -11,6 +11,9 @@ template lilicorr_status_t ca_launch_rows<128, 128>(const CaArgs&, const CaPlan&
 
 namespace {
 
+int g_ca_path = 0;             // test hook: 1 the tensor-core kernel for all bf16 queries, 2 for none
+
+
 lilicorr_status_t ca_plan(const lilicorr_cache_attention_desc* d, CaPlan* p) {
   if (!d) return LILICORR_ERR_ARG;
   LL_TRY(cache_shape(&d->cache));
@@ -22,17 +25,21 @@ lilicorr_status_t ca_plan(const lilicorr_cache_attention_desc* d, CaPlan* p) {
   const int rows = d->tokens * (d->q_heads / c.kv_heads);
   p->dp = c.head_dim <= 32 ? 32 : c.head_dim <= 64 ? 64 : 128;
   p->pieces = d->dtype == LILICORR_BF16 ? 1 : 3;
-  p->nt = rows <= 8 ? 1 : rows <= 16 || p->pieces > 1 ? 2 : 4;
-  p->blocks = (rows + 8 * p->nt - 1) / (8 * p->nt);
+  p->whole = c.capacity <= 512 && rows <= 16;
+  p->tc = p->pieces == 1 && (g_ca_path ? g_ca_path == 1 : rows > 8 && !p->whole);
+  if (p->tc) p->whole = false;
+  if (p->tc && p->dp < 64) p->dp = 64;
+  p->nt = rows <= 8 ? 1 : 2;
+  const int per_block = p->tc ? 128 : 8 * p->nt;
+  p->blocks = (rows + per_block - 1) / per_block;
   p->items = (size_t)c.sequences * c.kv_heads * p->blocks;
   if ((double)p->items * (c.capacity / 128 + 1) >= 2147483648.0) return LILICORR_ERR_SHAPE;
   // the widest team of at most 16: all heads of a position where there are so few
   p->team = 1;
   for (int i = 2; i <= 16; ++i)
     if (c.kv_heads % i == 0) p->team = i;
-  p->ctas = num_sms() * (p->nt * p->pieces > 3 || p->nt > 2 ? 1 : 2) / p->team * p->team;
-  p->whole = c.capacity <= 512;
-  const size_t parts = p->whole ? 0 : (size_t)2 * p->ctas * 8 * p->nt;
+  p->ctas = num_sms() * (p->tc || p->nt * p->pieces > 3 ? 1 : 2) / p->team * p->team;
+  const size_t parts = p->whole ? 0 : (size_t)2 * p->ctas * per_block;
   p->pad = rows <= 16 ? (rows + 1) / 2 * 2 : 0;
   const size_t keys = (size_t)c.sequences * c.kv_heads * c.capacity;
   p->left_off = 256;
@@ -45,22 +52,11 @@ lilicorr_status_t ca_plan(const lilicorr_cache_attention_desc* d, CaPlan* p) {
   return LILICORR_OK;
 }
 
-}  // namespace
-}  // namespace lilicorr
 
-using namespace lilicorr;
-
-extern "C" {
-
-size_t lilicorr_cache_attention_workspace_bytes(const lilicorr_cache_attention_desc* desc) {
-  CaPlan p;
-  return ca_plan(desc, &p) == LILICORR_OK ? p.total : 0;
-}
-
-lilicorr_status_t lilicorr_cache_attention(const lilicorr_cache_attention_desc* desc, const void* q,
-                                           const void* cache, const int32_t* seq_len, void* out,
-                                           float* lse, float* weights, void* ws, size_t ws_bytes,
-                                           cudaStream_t stream) {
+lilicorr_status_t run_cache_attention(const lilicorr_cache_attention_desc* desc, const void* q,
+                                      const void* cache, const int32_t* seq_len, void* out, float* lse,
+                                      float* weights, void* ws, size_t ws_bytes, cudaStream_t stream,
+                                      long long wait_limit, int starve) {
   CaPlan p;
   LL_TRY(ca_plan(desc, &p));
   const double scale = (double)desc->scale * desc->cache.k_unit;
@@ -77,6 +73,7 @@ lilicorr_status_t lilicorr_cache_attention(const lilicorr_cache_attention_desc* 
       !cache_rows_ok(desc->out_stride, e, per16, a.c.d, true))
     return LILICORR_ERR_ARG;
   if (ws_bytes < p.total) return LILICORR_ERR_WORKSPACE;
+  if (starve && !p.tc) return LILICORR_ERR_SHAPE;
   unsigned char* w = static_cast<unsigned char*>(ws);
   a.q = q;
   a.out = out;
@@ -100,6 +97,9 @@ lilicorr_status_t lilicorr_cache_attention(const lilicorr_cache_attention_desc* 
   a.left = reinterpret_cast<uint32_t*>(w + p.left_off);
   a.ml = reinterpret_cast<float2*>(w + p.ml_off);
   a.po = reinterpret_cast<float*>(w + p.po_off);
+  a.status = reinterpret_cast<uint32_t*>(w);
+  a.wait_limit = wait_limit;
+  a.test_starve = starve;
   a.rows = reinterpret_cast<float2*>(w + p.rows_off);
   a.factors = reinterpret_cast<float*>(w + p.factors_off);
   a.scores = weights && p.pad ? reinterpret_cast<float*>(w + p.scores_off) : nullptr;
@@ -109,6 +109,42 @@ lilicorr_status_t lilicorr_cache_attention(const lilicorr_cache_attention_desc* 
   return p.dp == 32   ? ca_launch_rows<32, 0>(a, p, stream)
          : p.dp == 64 ? ca_launch_rows<64, 0>(a, p, stream)
                       : ca_launch_rows<128, 0>(a, p, stream);
+}
+
+
+}  // namespace
+}  // namespace lilicorr
+
+using namespace lilicorr;
+
+extern "C" {
+
+size_t lilicorr_cache_attention_workspace_bytes(const lilicorr_cache_attention_desc* desc) {
+  CaPlan p;
+  return ca_plan(desc, &p) == LILICORR_OK ? p.total : 0;
+}
+
+lilicorr_status_t lilicorr_cache_attention(const lilicorr_cache_attention_desc* desc, const void* q,
+                                           const void* cache, const int32_t* seq_len, void* out,
+                                           float* lse, float* weights, void* ws, size_t ws_bytes,
+                                           cudaStream_t stream) {
+  return run_cache_attention(desc, q, cache, seq_len, out, lse, weights, ws, ws_bytes, stream, CA_WAIT, 0);
+}
+
+int lilicorr_test_cache_attention_path(int mode) {
+  const int prev = g_ca_path;
+  g_ca_path = mode < 0 ? 0 : mode > 2 ? 2 : mode;
+  return prev;
+}
+
+lilicorr_status_t lilicorr_test_cache_attention_timeout(const lilicorr_cache_attention_desc* desc, const void* q,
+                                                        const void* cache, const int32_t* seq_len, void* out,
+                                                        float* lse, void* ws, size_t ws_bytes,
+                                                        long long wait_cycles, int which,
+                                                        cudaStream_t stream) {
+  if (wait_cycles < 100000 || wait_cycles > CA_WAIT || which < 1 || which > 2) return LILICORR_ERR_ARG;
+  return run_cache_attention(desc, q, cache, seq_len, out, lse, nullptr, ws, ws_bytes, stream, wait_cycles,
+                             which);
 }
 
 }  // extern "C"

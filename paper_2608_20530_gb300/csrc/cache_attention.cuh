@@ -27,11 +27,14 @@ struct CaArgs {
   float* factors;              // [N, T, Hq] what takes a row's products to scores in log2 units
   float* scores;               // [N, H, S, pad] the products themselves, or null: computed again
   int pad;                     // rows, even
+  uint32_t* status;
+  long long wait_limit;        // SM cycles per bounded wait of the tensor-core kernel
+  int test_starve;             // test hook only: it expands no keys (1) or values (2)
 };
 
 struct CaPlan {
   int dp, nt, pieces, blocks, ctas, team;
-  bool whole;
+  bool tc, whole;
   int pad;                     // rows whose products are kept (0: none)
   size_t items, left_off, ml_off, po_off, rows_off, factors_off, scores_off, total;
 };
@@ -39,5 +42,10 @@ struct CaPlan {
 // The launches of a call, for widths up to DP (cache_attention_any.cu), or for DP itself.
 template <int DP, int DIM>
 lilicorr_status_t ca_launch_rows(const CaArgs& a, const CaPlan& p, cudaStream_t st);
+
+// bf16 queries on the 5th-generation tensor cores (cache_attention_tc.cu)
+lilicorr_status_t launch_ca_tc(const CaArgs& a, const CaPlan& p, cudaStream_t st);
+
+constexpr long long CA_WAIT = 4000000000ll;          // about 2 s
 
 }  // namespace lilicorr

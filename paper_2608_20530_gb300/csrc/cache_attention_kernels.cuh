@@ -273,6 +273,11 @@ __device__ __forceinline__ void load16b(const __nv_bfloat16* p, float* x) {
     x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
   }
 }
+// The power of two that takes a row's largest element to [2^13, 2^14); an infinity or a row of zeros stays as it is,
+// and numbers that no power of two in fp32 brings so far (below 2^-113) go as far as it does.
+__device__ __forceinline__ int query_shift(float top) {
+  return top > 0.f && top < INFINITY ? min(140 - (int)(__float_as_uint(top) >> 23), 126) : 0;
+}
 // Queries as the second operand: of column g (row `row` of the item, or none) elements c * DP / 4 ..,
 // brought to fp16 by 2^(the result) of their row, in PIECES numbers that add up to them.
 template <int DP, int PIECES, typename E>
@@ -293,9 +298,7 @@ __device__ __forceinline__ int load_query(const E* q, int d, int c, uint32_t (*b
   for (int i = 0; i < DP / 4; ++i) top = fmaxf(top, fabsf(x[i]));
   top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
   top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-  // 2^13 <= top * 2^up < 2^14; an infinity or a row of zeros stays as it is, and numbers that no power of two
-  // in fp32 brings so far (below 2^-113) go as far as it does
-  const int up = top > 0.f && top < INFINITY ? min(140 - (int)(__float_as_uint(top) >> 23), 126) : 0;
+  const int up = query_shift(top);
   const float by = pow2(up);
 #pragma unroll
   for (int i = 0; i < DP / 4; i += 2) {
@@ -332,20 +335,22 @@ __device__ __forceinline__ void store4(E* p, const float4& v) {
   if constexpr (sizeof(E) == 4) *reinterpret_cast<float4*>(p) = v;
   else *reinterpret_cast<uint2*>(p) = make_uint2(bf16_pack2(v.x, v.y), bf16_pack2(v.z, v.w));
 }
-// a row's result from its reference, sum and the lane's four sums of p V
+// a row's normaliser from its reference and sum
+__device__ __forceinline__ void ca_write_row(const CaArgs& a, int n, int t, int hq, float m, float l) {
+  // the scores were taken in units that their factor's rounding moved
+  const size_t row = ((size_t)n * a.T + t) * a.Hq + hq;
+  a.lse[row] = l == 0.f ? -INFINITY
+                        : fmaf(fmaf(m, a.rest_ratio, m), 0.69314718f, fmaf(-CA_UP, 0.69314718f, logf(l)));
+  if (a.weights) a.rows[row] = make_float2(m, l);
+}
+// a row's result from these and the lane's four sums of p V
 template <typename E>
 __device__ __forceinline__ void ca_write(const CaArgs& a, int n, int t, int hq, float m, float l, float4 o,
                                          int lane) {
   E* out = static_cast<E*>(a.out) + n * a.o_s[0] + t * a.o_s[1] + hq * a.o_s[2];
   const float f = l == 0.f ? 0.f : a.c.v_unit / l;
   if (lane * 4 < a.c.d) store4(out + lane * 4, make_float4(o.x * f, o.y * f, o.z * f, o.w * f));
-  // the scores were taken in units that their factor's rounding moved
-  if (lane == 0) {
-    const size_t row = ((size_t)n * a.T + t) * a.Hq + hq;
-    a.lse[row] = l == 0.f ? -INFINITY
-                          : fmaf(fmaf(m, a.rest_ratio, m), 0.69314718f, fmaf(-CA_UP, 0.69314718f, logf(l)));
-    if (a.weights) a.rows[row] = make_float2(m, l);
-  }
+  if (lane == 0) ca_write_row(a, n, t, hq, m, l);
 }
 
 // DIM: head_dim where it is DP, which makes all places in a record constants, else 0.
@@ -907,13 +912,9 @@ __global__ void __launch_bounds__(CA_THREADS, NT > 2 ? 1 : 2) cache_attention_we
   }
 }
 
+// What each key gets, behind the rows' results.
 template <int DP, int DIM, int NT, int PIECES, typename E>
-lilicorr_status_t ca_launch(const CaArgs& a, const CaPlan& p, cudaStream_t st) {
-  static bool configured[64] = {false};
-  auto* kernel = cache_attention_kernel<DP, DIM, NT, PIECES, E>;
-  LL_TRY(allow_max_dynamic_smem(kernel, configured));
-  LL_TRY(launch_k(kernel, p.whole ? (unsigned)p.items : (unsigned)p.ctas, CA_THREADS, CaSmem<DP, NT, PIECES>::TOTAL, st,
-                  a));
+lilicorr_status_t ca_launch_weights(const CaArgs& a, const CaPlan& p, cudaStream_t st) {
   if (!a.weights) return LILICORR_OK;
   if (a.scores) {
     const int pieces = (a.c.S + CS_KEYS - 1) / CS_KEYS;
@@ -927,15 +928,28 @@ lilicorr_status_t ca_launch(const CaArgs& a, const CaPlan& p, cudaStream_t st) {
   return launch_k(weights, (unsigned)(2 * num_sms() / p.team * p.team), CA_THREADS, smem, st, a);
 }
 
+template <int DP, int DIM, int NT, int PIECES, typename E>
+lilicorr_status_t ca_launch(const CaArgs& a, const CaPlan& p, cudaStream_t st) {
+  static bool configured[64] = {false};
+  auto* kernel = cache_attention_kernel<DP, DIM, NT, PIECES, E>;
+  LL_TRY(allow_max_dynamic_smem(kernel, configured));
+  LL_TRY(launch_k(kernel, p.whole ? (unsigned)p.items : (unsigned)p.ctas, CA_THREADS, CaSmem<DP, NT, PIECES>::TOTAL, st,
+                  a));
+  return ca_launch_weights<DP, DIM, NT, PIECES, E>(a, p, st);
+}
+
 }  // namespace
 
 template <int DP, int DIM>
 lilicorr_status_t ca_launch_rows(const CaArgs& a, const CaPlan& p, cudaStream_t st) {
   if (p.pieces > 1)
     return p.nt == 1 ? ca_launch<DP, DIM, 1, 3, float>(a, p, st) : ca_launch<DP, DIM, 2, 3, float>(a, p, st);
-  return p.nt == 1   ? ca_launch<DP, DIM, 1, 1, __nv_bfloat16>(a, p, st)
-         : p.nt == 2 ? ca_launch<DP, DIM, 2, 1, __nv_bfloat16>(a, p, st)
-                     : ca_launch<DP, DIM, 4, 1, __nv_bfloat16>(a, p, st);
+  if (p.tc) {
+    LL_TRY(launch_ca_tc(a, p, st));
+    return ca_launch_weights<DP, DIM, 4, 1, __nv_bfloat16>(a, p, st);
+  }
+  return p.nt == 1 ? ca_launch<DP, DIM, 1, 1, __nv_bfloat16>(a, p, st)
+                   : ca_launch<DP, DIM, 2, 1, __nv_bfloat16>(a, p, st);
 }
 
 }  // namespace lilicorr

@@ -232,13 +232,67 @@ def test_attention(shape, dtype):
     assert torch.equal(w1, w2) and ws.status() == 0
 
 
+@pytest.fixture
+def tensor_cores():
+    """bf16 queries on the kernel that takes many rows, however few there are."""
+    ll = _ll()
+    was = ll.test_cache_attention_path(1)
+    yield ll
+    ll.test_cache_attention_path(was)
+
+
+@pytest.mark.parametrize("shape", ATTENTION + [
+    (1, 16, 32, 2, 128, 2000), (2, 33, 8, 1, 64, 1300), (3, 8, 32, 8, 96, 5000), (1, 130, 4, 2, 32, 260),
+    (40, 4, 16, 4, 128, 700), (2, 20, 16, 1, 80, 390), (1, 64, 8, 4, 128, 9000)])
+def test_attention_on_tensor_cores(tensor_cores, shape):
+    ll, seed = tensor_cores, sum(shape)
+    q, c, lens, w = _case(ll, *shape, "bf16", seed, heads_first=seed % 2 == 0)
+    ws = ll.Workspace(ll.cache_attention_workspace_bytes(q, c))
+    first = ll.cache_attention(q, c, lens, ws=ws)
+    assert ws.status() == 0
+    _check(first, q, c, lens)
+    w1 = w.clone()
+    again = ll.cache_attention(q, c, lens, weights=w1, ws=ws)
+    _check(again, q, c, lens, w0=w, w=w1)
+    assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1]) and ws.status() == 0
+
+
+def test_far_scores_on_tensor_cores(tensor_cores):
+    """References that move at every step, queries of any size, and a row of NaN."""
+    test_units_scale_and_far_scores("bf16")
+    for T in (1, 3):
+        test_nan_query_spoils_its_own_row("bf16", T)
+
+
+@pytest.mark.parametrize("which", [1, 2])
+def test_bounded_waits_run_out(tensor_cores, which):
+    """Products whose keys or values never come: the waits end, the status says so, the context lives."""
+    ll = tensor_cores
+    q, c, lens, _ = _case(ll, 2, 16, 8, 2, 128, 700, "bf16", 3)
+    ws = ll.Workspace(ll.cache_attention_workspace_bytes(q, c))
+    ll.test_cache_attention_timeout(q, c, lens, ws, 2_000_000, which)
+    assert ws.status() == 6
+    ws = ll.Workspace(ll.cache_attention_workspace_bytes(q, c))
+    _check(ll.cache_attention(q, c, lens, ws=ws), q, c, lens)
+    assert ws.status() == 0
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("T,lens", [(1, [0, 1, 2]), (3, [0, 1, 2, 3, 4]), (5, [4, 70, 64, 65, 63]),
                                     (1, [500, 130, 129, 128, 127]), (2, [-3, 5, -1, 0, 130]),
                                     (16, [8, 16, 17, 15, 130])])
-def test_lengths(dtype, T, lens):
+@pytest.mark.parametrize("path", [0, 1])
+def test_lengths(dtype, T, lens, path):
     """Empty rows, absent sequences, lengths past the capacity; nothing behind a length is looked at."""
     ll = _ll()
+    was = ll.test_cache_attention_path(path)
+    try:
+        _lengths(ll, dtype, T, lens)
+    finally:
+        ll.test_cache_attention_path(was)
+
+
+def _lengths(ll, dtype, T, lens):
     q, c, lens, w = _case(ll, len(lens), T, 8, 2, 64, 130, dtype, T, lens, fill=0xFF)
     out, lse = torch.full_like(q, 7.0), torch.full(q.shape[:3], 7.0, device="cuda")
     w1 = w.clone()
