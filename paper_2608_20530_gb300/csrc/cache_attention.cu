@@ -25,11 +25,10 @@ lilicorr_status_t ca_plan(const lilicorr_cache_attention_desc* d, CaPlan* p) {
   const int rows = d->tokens * (d->q_heads / c.kv_heads);
   p->dp = c.head_dim <= 32 ? 32 : c.head_dim <= 64 ? 64 : 128;
   p->pieces = d->dtype == LILICORR_BF16 ? 1 : 3;
-  p->whole = c.capacity <= 512 && rows <= 16;
-  p->tc = p->pieces == 1 && (g_ca_path ? g_ca_path == 1 : rows > 8 && !p->whole);
-  if (p->tc) p->whole = false;
+  p->tc = p->pieces == 1 && (g_ca_path ? g_ca_path == 1 : rows > 32);
+  p->whole = !p->tc && c.capacity <= 512;
   if (p->tc && p->dp < 64) p->dp = 64;
-  p->nt = rows <= 8 ? 1 : 2;
+  p->nt = rows <= 8 ? 1 : rows <= 16 || p->pieces > 1 ? 2 : 4;
   const int per_block = p->tc ? 128 : 8 * p->nt;
   p->blocks = (rows + per_block - 1) / per_block;
   p->items = (size_t)c.sequences * c.kv_heads * p->blocks;
@@ -38,7 +37,7 @@ lilicorr_status_t ca_plan(const lilicorr_cache_attention_desc* d, CaPlan* p) {
   p->team = 1;
   for (int i = 2; i <= 16; ++i)
     if (c.kv_heads % i == 0) p->team = i;
-  p->ctas = num_sms() * (p->tc || p->nt * p->pieces > 3 ? 1 : 2) / p->team * p->team;
+  p->ctas = num_sms() * (p->tc || p->nt * p->pieces > 3 || p->nt > 2 ? 1 : 2) / p->team * p->team;
   const size_t parts = p->whole ? 0 : (size_t)2 * p->ctas * per_block;
   p->pad = rows <= 16 ? (rows + 1) / 2 * 2 : 0;
   const size_t keys = (size_t)c.sequences * c.kv_heads * c.capacity;

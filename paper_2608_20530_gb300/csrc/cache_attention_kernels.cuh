@@ -278,6 +278,11 @@ __device__ __forceinline__ void load16b(const __nv_bfloat16* p, float* x) {
 __device__ __forceinline__ int query_shift(float top) {
   return top > 0.f && top < INFINITY ? min(140 - (int)(__float_as_uint(top) >> 23), 126) : 0;
 }
+// What takes the products of a row shifted by `up` to scores in log2 units; never 0, which would make NaN of the
+// -infinity that stands for a key that is not seen.
+__device__ __forceinline__ float row_factor(const CaArgs& a, int up) {
+  return fmaxf(a.scale * pow2(-up), 0x1p-149f);
+}
 // Queries as the second operand: of column g (row `row` of the item, or none) elements c * DP / 4 ..,
 // brought to fp16 by 2^(the result) of their row, in PIECES numbers that add up to them.
 template <int DP, int PIECES, typename E>
@@ -450,7 +455,7 @@ cache_attention_kernel(const CaArgs a) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) {                // this lane's columns
           const int u = __shfl_sync(0xffffffffu, up, (2 * c + e) * 4);
-          f[nt][e] = a.scale * pow2(-u);
+          f[nt][e] = row_factor(a, u);
           fr[nt][e] = a.scale_rest * pow2(-u);
           m[nt][e] = -FLT_MAX;
           l[nt][e] = 0.f;
@@ -841,7 +846,7 @@ __global__ void __launch_bounds__(CA_THREADS, NT > 2 ? 1 : 2) cache_attention_we
           const float m = __shfl_sync(0xffffffffu, ml.x, col * 4);
           const bool ok = __shfl_sync(0xffffffffu, there, col * 4);
           const float l = __shfl_sync(0xffffffffu, ml.y, col * 4);
-          f[nt][e] = a.scale * pow2(-u);
+          f[nt][e] = row_factor(a, u);
           fr[nt][e] = a.scale_rest * pow2(-u);
           ref[nt][e] = CA_UP - m;
           inv[nt][e] = 1.f / l;
@@ -948,8 +953,9 @@ lilicorr_status_t ca_launch_rows(const CaArgs& a, const CaPlan& p, cudaStream_t 
     LL_TRY(launch_ca_tc(a, p, st));
     return ca_launch_weights<DP, DIM, 4, 1, __nv_bfloat16>(a, p, st);
   }
-  return p.nt == 1 ? ca_launch<DP, DIM, 1, 1, __nv_bfloat16>(a, p, st)
-                   : ca_launch<DP, DIM, 2, 1, __nv_bfloat16>(a, p, st);
+  return p.nt == 1   ? ca_launch<DP, DIM, 1, 1, __nv_bfloat16>(a, p, st)
+         : p.nt == 2 ? ca_launch<DP, DIM, 2, 1, __nv_bfloat16>(a, p, st)
+                     : ca_launch<DP, DIM, 4, 1, __nv_bfloat16>(a, p, st);
 }
 
 }  // namespace lilicorr

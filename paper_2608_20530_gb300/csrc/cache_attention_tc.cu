@@ -21,14 +21,19 @@ namespace lilicorr {
 namespace {
 using namespace tc;
 
-constexpr int CT_SOFT = 256, CT_EXPAND = 256, CT_THREADS = CT_SOFT + 32 + CT_EXPAND;
 constexpr int CT_KEYS = 128, CT_ROWS = 128;
 constexpr uint32_t CT_CHUNK = 128 * 128;             // 128 rows of 128 bytes
 constexpr uint32_t CT_TMEM = 512;
 constexpr int CT_RAW = 3;                            // tiles of records under way
 
-template <int DP>
+// HALF: blocks of 64 rows or fewer. Q lies in the tile twice, so that scores of all rows lie in tensor memory twice, and
+// each stream has the half whose quarters its warps can read: warps 0 and 1, 2 and 3, a scheduler each, and more
+// registers a thread.
+template <int DP, bool HALF>
 struct CtCfg {
+  static constexpr int QUARTERS = HALF ? 2 : 4, SOFT = 2 * 32 * QUARTERS;      // warps of a stream; threads of both
+  static constexpr int MMA_WARP = SOFT / 32, COPY_WARP = MMA_WARP + 1, FIRST = MMA_WARP + 2;   // FIRST to expand
+  static constexpr int WARPS = FIRST + 9, THREADS = 32 * WARPS;    // (the last one copies, too)
   static constexpr int CH = DP / 64;                 // 64-column chunks of a row
   static constexpr uint32_t TILE = CH * CT_CHUNK;
   static constexpr int NK = 2, NV = 2;
@@ -63,15 +68,30 @@ __device__ __forceinline__ bool elect_one() {        // one lane of a converged 
   asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(r));
   return r != 0;
 }
+// Nothing that uses these registers moves above this point (a load from tensor memory fills them until its wait).
+__device__ __forceinline__ void pin(uint32_t (&r)[32]) {
+#pragma unroll
+  for (int i = 0; i < 32; i += 8)
+    asm volatile("" : "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]),
+                      "+r"(r[i + 5]), "+r"(r[i + 6]), "+r"(r[i + 7]));
+}
 // 2^d of a whole number d <= 0 (0 below the normal range, and for -inf)
 __device__ __forceinline__ float pow2_down(float d) {
   return d < -126.f ? 0.f : __int_as_float((127 + (int)d) << 23);
+}
+// A wait for a phase that lets the warp sleep meanwhile (others of its scheduler work).
+__device__ __forceinline__ bool sleep_wait(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n selp.u32 %0, 1, 0, p;\n}"
+      : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity), "r"(20000) : "memory");
+  return ok != 0;
 }
 // A wait that did not end at once: false after `limit` SM cycles, or when another warp gave up.
 __device__ __noinline__ bool wait_long(uint64_t* bar, uint32_t parity, long long limit,
                                        volatile int* abort_flag) {
   const long long t0 = clock64();
-  while (!mbar_try_wait(bar, parity)) {
+  while (!sleep_wait(bar, parity)) {
     if (*abort_flag) return false;
     if (clock64() - t0 > limit) {
       *abort_flag = 1;
@@ -84,30 +104,34 @@ __device__ __noinline__ bool wait_long(uint64_t* bar, uint32_t parity, long long
 // Half a record at `rec` (or zeros) as row `key` of a tile: DP columns of fp16, zeros past the head's width.
 template <int DP, int DIM>
 __device__ __forceinline__ void expand(const unsigned char* rec, bool there, int d, uint8_t* tile, int key) {
-  const uint32_t zero = there ? 0xFFu : 0u;          // (a scale of 0: codes are finite whatever they are)
+  // everything is read first: the place may be given back while it is expanded
+  uint2 w[DP / 16], b = *reinterpret_cast<const uint2*>(rec + d / 2);
 #pragma unroll
   for (int g = 0; g < DP / 16; ++g) {
-    uint4 v[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
-    if (DIM || g * 16 < d) {
-      const uint2 w = *reinterpret_cast<const uint2*>(rec + g * 8);
-      const uint32_t b = rec[d / 2 + g] & zero, f = scales(b | b << 8);
-      uint32_t r[4];
-      codes(w.x, r);
-      v[0] = make_uint4(mul2(r[0], f), mul2(r[1], f), mul2(r[2], f), mul2(r[3], f));
-      codes(w.y, r);
-      v[1] = make_uint4(mul2(r[0], f), mul2(r[1], f), mul2(r[2], f), mul2(r[3], f));
-    }
+    w[g] = make_uint2(0, 0);
+    if (DIM || g * 16 < d) w[g] = *reinterpret_cast<const uint2*>(rec + g * 8);
+  }
+  // scales of 0 where there is no key (codes are finite whatever they are), or no such group
+  if (!there) b = make_uint2(0, 0);
+  uint8_t* row = tile + key * 128;
+  const int x = key & 7;
+#pragma unroll
+  for (int g = 0; g < DP / 16; ++g) {
+    const uint32_t two = __byte_perm(b.x, b.y, (g & 7) * 0x11), f = scales(DIM || g * 16 < d ? two : 0u);
+    uint32_t r[4];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int p = 2 * g + i;
-      *reinterpret_cast<uint4*>(tile + (p >> 3) * CT_CHUNK + swz(key, p & 7)) = v[i];
+      codes(i ? w[g].y : w[g].x, r);
+      *reinterpret_cast<uint4*>(row + (p >> 3) * CT_CHUNK + (((p & 7) ^ x) << 4)) =
+          make_uint4(mul2(r[0], f), mul2(r[1], f), mul2(r[2], f), mul2(r[3], f));
     }
   }
 }
 
-template <int DP, int DIM>
-__global__ void __launch_bounds__(CT_THREADS, 1) cache_attention_tc_kernel(const CaArgs a) {
-  using Cfg = CtCfg<DP>;
+template <int DP, int DIM, bool HALF>
+__global__ void __launch_bounds__((CtCfg<DP, HALF>::THREADS), 1) cache_attention_tc_kernel(const CaArgs a) {
+  using Cfg = CtCfg<DP, HALF>;
   using E = __nv_bfloat16;
   constexpr int NK = Cfg::NK, NV = Cfg::NV;
   extern __shared__ uint8_t smem_raw[];
@@ -117,7 +141,7 @@ __global__ void __launch_bounds__(CT_THREADS, 1) cache_attention_tc_kernel(const
   uint8_t* sV = sK + NK * Cfg::TILE;
   uint8_t* sR = sV + NV * Cfg::TILE;
   __shared__ __align__(8) uint64_t k_full[NK], k_empty[NK], v_full[NV], v_empty[NV];
-  __shared__ __align__(8) uint64_t s_ready[2], p_ready[2], o_ready[2], drain;
+  __shared__ __align__(8) uint64_t r_full[CT_RAW], r_empty[CT_RAW], s_ready[2], p_ready[2], o_ready[2], drain;
   __shared__ uint32_t tmem_base;
   __shared__ volatile int abort_flag;
   __shared__ float s_factor[CT_ROWS];
@@ -129,18 +153,19 @@ __global__ void __launch_bounds__(CT_THREADS, 1) cache_attention_tc_kernel(const
   if (tid == 0) {
     for (int i = 0; i < NK; ++i) { mbar_init(&k_full[i], 4); mbar_init(&k_empty[i], 1); }
     for (int i = 0; i < NV; ++i) { mbar_init(&v_full[i], 4); mbar_init(&v_empty[i], 1); }
+    for (int i = 0; i < CT_RAW; ++i) { mbar_init(&r_full[i], 64); mbar_init(&r_empty[i], 8); }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&s_ready[i], 1);
-      mbar_init(&p_ready[i], 4);
+      mbar_init(&p_ready[i], Cfg::QUARTERS);
       mbar_init(&o_ready[i], 1);
     }
     mbar_init(&drain, 1);
     abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 8) tmem_alloc(&tmem_base, CT_TMEM);
+  if (warp == Cfg::MMA_WARP) tmem_alloc(&tmem_base, CT_TMEM);
   pdl_wait();
-  CaCursor<CT_KEYS> at;
+  CaCursor<CT_KEYS> at = {};
   uint32_t first = 0, per = 1;
   const uint32_t count = ca_range<CT_KEYS>(a, a.blocks, &at, &first, &per);
   tc_fence_before();
@@ -148,57 +173,77 @@ __global__ void __launch_bounds__(CT_THREADS, 1) cache_attention_tc_kernel(const
   tc_fence_after();
   const uint32_t tmem = tmem_base;
   auto wait = [&](uint64_t* bar, uint32_t parity) {  // for a whole warp: all lanes go on, or none
-    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+    if (__all_sync(0xffffffffu, sleep_wait(bar, parity))) return true;
     return __all_sync(0xffffffffu, wait_long(bar, parity, a.wait_limit, &abort_flag)) != 0;
   };
   uint32_t done = 0;                                 // tiles of the list behind this warp
 
-  if (warp > 8) {
-    // ---- records: copied two tiles ahead, expanded when both their tile and its place are there
-    const int x = tid - CT_SOFT - 32, key = x & 127, is_v = x >> 7;
-    const int vecs = R / 16;
-    CaCursor<CT_KEYS> ahead = at;
-    uint32_t copied = 0;
-    auto copy_next = [&] {
-      if (copied < count) {
-        uint8_t* dst = sR + copied % CT_RAW * Cfg::RAW;
-        const int k0 = ahead.tile * CT_KEYS, there = ahead.len - k0;
-        const unsigned char* src = a.c.at(ahead.n, k0, ahead.h);
-        for (int i = x; i < CT_KEYS * vecs; i += CT_EXPAND) {
-          const int k = i / vecs;
-          if (k < there) copy16(smem_u32(dst + i * 16), src + k * a.c.s[1] + (i - k * vecs) * 16, true);
+  if (warp == Cfg::COPY_WARP || warp == Cfg::WARPS - 1) {
+    // ---- records: CT_RAW tiles ahead, 16 bytes a lane (one bulk copy a record takes 58 clocks each)
+    const int x = lane + (warp == Cfg::COPY_WARP ? 0 : 32), vecs = R / 16;
+    const int step = 64 / vecs, rest = 64 - step * vecs, first_k = x / vecs, first_v = x - first_k * vecs;
+    const int64_t stride = a.c.s[1];
+    uint32_t into = 0, parity = 1;
+    bool ok = true;
+    while (done < count && ok) {
+      const int tile1 = min((uint32_t)at.tiles, at.tile + (count - done));
+      const unsigned char* src = a.c.at(at.n, at.tile * CT_KEYS, at.h);
+      done += tile1 - at.tile;
+      for (; at.tile < tile1 && ok; ++at.tile) {
+        if (!wait(&r_empty[into], parity)) { ok = false; break; }
+        const int there = min(CT_KEYS, at.len - at.tile * CT_KEYS);
+        int k = first_k, v = first_v;
+        const unsigned char* from = src + first_k * stride + first_v * 16;
+        uint32_t to = smem_u32(sR + into * Cfg::RAW) + x * 16;
+#pragma unroll 6
+        for (int i = 0; i < vecs * 2; ++i) {
+          if (k < there) copy16(to, from, true);
+          to += 64 * 16;
+          k += step;
+          v += rest;
+          from += step * stride + rest * 16;
+          if (v >= vecs) {
+            v -= vecs;
+            ++k;
+            from += stride - vecs * 16;
+          }
         }
-        if (++ahead.tile == ahead.tiles && copied + 1 < count) ahead.next(a, a.blocks);
+        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&r_full[into])) : "memory");
+        src += CT_KEYS * stride;
+        if (++into == CT_RAW) { into = 0; parity ^= 1u; }
       }
-      ++copied;
-      copy_commit();
-    };
-    copy_next();
-    copy_next();
+      if (done < count && ok) at.next(a, a.blocks);
+    }
+    copy_commit();
+    copy_wait<0>();
+  } else if (warp >= Cfg::FIRST) {
+    // ---- records expanded, when their tile and its new place are there: four warps keys, four values
+    const int x = tid - 32 * Cfg::FIRST, key = x & 127, is_v = x >> 7;
     uint64_t* full = is_v ? v_full : k_full;
     uint64_t* empty = is_v ? v_empty : k_empty;
     uint8_t* ring = is_v ? sV : sK;
-    uint32_t slot = 0, parity = 1;
-    bool ok = true;
-    for (; done < count; ++done) {
-      copy_wait<1>();
-      named_bar(4, CT_EXPAND);                       // this tile is there for all, the one before it used up
-      copy_next();
-      if (ok && a.test_starve != is_v + 1) {
-        ok = wait(&empty[slot], parity);
-        if (ok) {
-          const unsigned char* rec = sR + done % CT_RAW * Cfg::RAW + key * R + is_v * cache_half_bytes(d);
-          expand<DP, DIM>(rec, at.tile * CT_KEYS + key < at.len, d, ring + slot * Cfg::TILE, key);
-          fence_async_shared();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&full[slot]);
+    uint32_t slot = 0, parity = 1, raw = 0, raw_parity = 0;
+    bool ok = a.test_starve != is_v + 1;
+    while (done < count && ok) {
+      const int tile1 = min((uint32_t)at.tiles, at.tile + (count - done));
+      done += tile1 - at.tile;
+      for (; at.tile < tile1 && ok; ++at.tile) {
+        ok = wait(&r_full[raw], raw_parity) && wait(&empty[slot], parity);
+        if (!ok) break;
+        const unsigned char* rec = sR + raw * Cfg::RAW + key * R + is_v * cache_half_bytes(d);
+        expand<DP, DIM>(rec, at.tile * CT_KEYS + key < at.len, d, ring + slot * Cfg::TILE, key);
+        fence_async_shared();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(&full[slot]);
+          mbar_arrive(&r_empty[raw]);
         }
+        if (++raw == CT_RAW) { raw = 0; raw_parity ^= 1u; }
+        if (++slot == (is_v ? NV : NK)) { slot = 0; parity ^= 1u; }
       }
-      if (++slot == (is_v ? NV : NK)) { slot = 0; parity ^= 1u; }
-      if (++at.tile == at.tiles && done + 1 < count) at.next(a, a.blocks);
+      if (done < count && ok) at.next(a, a.blocks);
     }
-    copy_wait<0>();
-  } else if (warp == 8) {
+  } else if (warp == Cfg::MMA_WARP) {
     // ---- products. The whole warp walks, one lane issues.
     constexpr uint32_t idesc_s = instr_desc_f16(128, 128);
     constexpr uint32_t idesc_o = instr_desc_f16(128, DP) | (1u << 16);      // V MN-major
@@ -209,7 +254,7 @@ __global__ void __launch_bounds__(CT_THREADS, 1) cache_attention_tc_kernel(const
     while (done < count) {
       const uint32_t here = min((uint32_t)(at.tiles - at.tile), count - done);
       const int end = at.len - at.tile * CT_KEYS;    // keys from here on
-      named_bar(1, CT_SOFT + 32);                    // Q is there
+      named_bar(1, Cfg::SOFT + 32);                    // Q is there
       tc_fence_after();
       bool ok = true;
       auto scores = [&](int s) {
@@ -259,7 +304,7 @@ __global__ void __launch_bounds__(CT_THREADS, 1) cache_attention_tc_kernel(const
         sums(s, end - (int)t * CT_KEYS, t < 2, t + 2 >= here);
         if (ok && t + 2 < here) scores(s);
       }
-      named_bar(2, CT_SOFT + 32);                    // the item is done with
+      named_bar(2, Cfg::SOFT + 32);                    // the item is done with
       done += here;
       if (done < count) at.next(a, a.blocks);
     }
@@ -270,7 +315,7 @@ __global__ void __launch_bounds__(CT_THREADS, 1) cache_attention_tc_kernel(const
     }
   } else {
     // ---- the streams: a thread a row
-    const int s = warp >> 2, row = (warp & 3) * 32 + lane;
+    const int s = warp / Cfg::QUARTERS, row = warp % Cfg::QUARTERS * 32 + lane;
     const uint32_t lane_base = tmem + ((uint32_t)((warp & 3) * 32) << 16);
     uint32_t sn = 0, on = 0;                         // scores and outputs met so far
     while (done < count) {
@@ -279,8 +324,8 @@ __global__ void __launch_bounds__(CT_THREADS, 1) cache_attention_tc_kernel(const
       const int tile_rows = min(CT_ROWS, rows - at.rb * CT_ROWS);
       const int r = at.rb * CT_ROWS + row, tok = r / a.rep, hq = at.h * a.rep + (r - tok * a.rep);
       const bool mine = row < tile_rows;
-      // the block's queries: the first stream a row a thread
-      if (s == 0) {
+      // the block's queries, a row a thread: the first stream's, or with HALF either's of its own
+      if (HALF || s == 0) {
         const E* q = static_cast<const E*>(a.q) + at.n * a.q_s[0] + tok * a.q_s[1] + hq * a.q_s[2];
         auto piece = [&](int p) {
           return mine && p * 8 < d ? __ldg(reinterpret_cast<const uint4*>(q + p * 8)) : make_uint4(0, 0, 0, 0);
@@ -303,15 +348,16 @@ __global__ void __launch_bounds__(CT_THREADS, 1) cache_attention_tc_kernel(const
 #pragma unroll
           for (int i = 0; i < 4; ++i)
             w[i] = half2_of(__uint_as_float(w[i] << 16) * by, __uint_as_float(w[i] & 0xFFFF0000u) * by);
-          *reinterpret_cast<uint4*>(sQ + (p >> 3) * CT_CHUNK + swz(row, p & 7)) = make_uint4(w[0], w[1], w[2], w[3]);
+          *reinterpret_cast<uint4*>(sQ + (p >> 3) * CT_CHUNK + swz(HALF ? s * 64 + row : row, p & 7)) = make_uint4(w[0], w[1], w[2], w[3]);
         }
-        s_factor[row] = a.scale * pow2(-up);
+        const float factor = row_factor(a, up);
+        if (s == 0) s_factor[row] = factor;
         fence_async_shared();
-        if (a.scores && mine) a.factors[((size_t)at.n * a.T + tok) * a.Hq + hq] = a.scale * pow2(-up);
+        if (a.scores && s == 0 && mine) a.factors[((size_t)at.n * a.T + tok) * a.Hq + hq] = factor;
       }
-      named_bar(1, CT_SOFT + 32);
+      named_bar(1, Cfg::SOFT + 32);
       const float f = s_factor[row];
-      const bool idle = (warp & 3) * 32 >= tile_rows;
+      const bool idle = warp % Cfg::QUARTERS * 32 >= tile_rows;
       const int lim = mine ? at.len - (a.T - 1 - tok) : 0;     // keys that the row sees
       float m = -INFINITY, l = 0.f;
       bool ok = true;
@@ -325,65 +371,80 @@ __global__ void __launch_bounds__(CT_THREADS, 1) cache_attention_tc_kernel(const
         tc_fence_after();
         const int k0 = (tile0 + (int)t) * CT_KEYS, seen = lim - k0;
         const bool masked = k0 + CT_KEYS > at.len - (a.T - 1);   // some row does not see all of them
-        uint32_t x[32];
-        float mx[2] = {-INFINITY, -INFINITY};
+        auto tile = [&](auto some) {                 // in two copies: the usual one without comparisons
+          constexpr bool MASKED = decltype(some)::value;
+          uint32_t xs[HALF ? 2 : 1][32];               // HALF: the next ones are read while these are worked on
+          tmem_ld32(lane_base + Cfg::S(s), xs[0]);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          tmem_ld32(lane_base + Cfg::S(s) + 32 * c, x);
-          if (masked)
+          for (int c = 0; c < 4; ++c) {                // 32 scores at a time, a step of the reference each
+            if (HALF && c < 3) tmem_ld32_nowait(lane_base + Cfg::S(s) + 32 * (c + 1), xs[HALF ? (c + 1) & 1 : 0]);
+            if (!HALF && c > 0) tmem_ld32(lane_base + Cfg::S(s) + 32 * c, xs[0]);
+            uint32_t (&x)[32] = xs[HALF ? c & 1 : 0];
+            if (MASKED)
 #pragma unroll
-            for (int e = 0; e < 32; ++e)
-              if (32 * c + e >= seen) x[e] = 0xFF800000u;        // -inf
+              for (int e = 0; e < 32; ++e)
+                if (32 * c + e >= seen) x[e] = 0xFF800000u;        // -inf
+            if (a.scores && mine) {                    // for what each key gets: 32 rows of a key side by side
+              float* to = a.scores + (((size_t)at.n * a.c.H + at.h) * a.c.S + k0 + 32 * c) * a.pad + r;
 #pragma unroll
-          for (int e = 0; e < 32; e += 4) {
-            mx[0] = fmaxf(fmaxf(mx[0], __uint_as_float(x[e])), __uint_as_float(x[e + 1]));
-            mx[1] = fmaxf(fmaxf(mx[1], __uint_as_float(x[e + 2])), __uint_as_float(x[e + 3]));
-          }
-          if (a.scores && mine) {                    // for what each key gets: 32 rows of a key side by side
-            float* to = a.scores + (((size_t)at.n * a.c.H + at.h) * a.c.S + k0 + 32 * c) * a.pad + r;
-#pragma unroll
-            for (int e = 0; e < 32; ++e)
-              if (k0 + 32 * c + e < at.len) to[(size_t)e * a.pad] = __uint_as_float(x[e]);
-          }
-        }
-        const float top = fmaxf(mx[0], mx[1]) * f;
-        if (t == (uint32_t)s) {
-          m = ceilf(top);
-        } else if (__any_sync(0xffffffffu, top > m + CA_SLACK)) {
-          // the sums so far to the new reference, by a whole power of two (their product is complete: the
-          // scores came behind it)
-          const float to = fmaxf(m, ceilf(top)), y = pow2_down(m - to);
-          m = to;
-          l *= y;
-#pragma unroll 1
-          for (int c = 0; c < DP / 16; ++c) {
-            uint32_t o[16];
-            tmem_ld16(lane_base + Cfg::O(s) + 16 * c, o);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * y);
-            tmem_st16(lane_base + Cfg::O(s) + 16 * c, o);
-          }
-        }
-        const float base = CA_UP - (m == -INFINITY ? 0.f : m);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          tmem_ld32(lane_base + Cfg::S(s) + 32 * c, x);
-          uint32_t p[16];
-          float sum[2] = {0.f, 0.f};
-#pragma unroll
-          for (int e = 0; e < 32; e += 2) {
-            float p0 = ex2(fmaf(__uint_as_float(x[e]), f, base)), p1 = ex2(fmaf(__uint_as_float(x[e + 1]), f, base));
-            if (masked) {
-              if (32 * c + e >= seen) p0 = 0.f;
-              if (32 * c + e + 1 >= seen) p1 = 0.f;
+              for (int e = 0; e < 32; ++e)
+                if (k0 + 32 * c + e < at.len) to[(size_t)e * a.pad] = __uint_as_float(x[e]);
             }
-            sum[0] += p0;
-            sum[1] += p1;
-            p[e / 2] = half2_of(p0, p1);
+            float mx[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) {
+              mx[0] = fmaxf(fmaxf(mx[0], __uint_as_float(x[e])), __uint_as_float(x[e + 1]));
+              mx[1] = fmaxf(fmaxf(mx[1], __uint_as_float(x[e + 2])), __uint_as_float(x[e + 3]));
+            }
+            const float top = fmaxf(mx[0], mx[1]) * f;
+            if (c == 0 && t == (uint32_t)s) {
+              m = ceilf(top);
+            } else if (__any_sync(0xffffffffu, top > m + CA_SLACK)) {
+              // the sums so far, and this tile's probabilities before these, to the new reference, by a whole
+              // power of two (the product of the sums is complete: the scores came behind it)
+              const float to = fmaxf(m, ceilf(top)), y = pow2_down(m - to);
+              m = to;
+              l *= y;
+              tmem_wait_st();
+              if (t != (uint32_t)s)
+#pragma unroll 1
+                for (int i = 0; i < DP / 16; ++i) {
+                  uint32_t o[16];
+                  tmem_ld16(lane_base + Cfg::O(s) + 16 * i, o);
+#pragma unroll
+                  for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * y);
+                  tmem_st16(lane_base + Cfg::O(s) + 16 * i, o);
+                }
+#pragma unroll 1
+              for (int i = 0; i < c; ++i) {
+                uint32_t o[16];
+                const uint32_t y2 = half2_of(y, y);
+                tmem_ld16(lane_base + Cfg::P(s, 2 * i), o);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[e] = mul2(o[e], y2);
+                tmem_st16(lane_base + Cfg::P(s, 2 * i), o);
+              }
+            }
+            const float base = CA_UP - (m == -INFINITY ? 0.f : m);
+            float sum[2] = {0.f, 0.f};
+            uint32_t p[16];
+#pragma unroll
+            for (int e = 0; e < 32; e += 2) {
+              const float p0 = ex2(fmaf(__uint_as_float(x[e]), f, base)), p1 = ex2(fmaf(__uint_as_float(x[e + 1]), f, base));
+              sum[0] += p0;
+              sum[1] += p1;
+              p[e / 2] = half2_of(p0, p1);
+            }
+            l += sum[0] + sum[1];
+            if (HALF && c < 3) {
+              tmem_wait_ld();
+              pin(xs[HALF ? (c + 1) & 1 : 0]);
+            }
+            tmem_st16(lane_base + Cfg::P(s, 2 * c), p);
           }
-          l += sum[0] + sum[1];
-          tmem_st16(lane_base + Cfg::P(s, 2 * c), p);
-        }
+        };
+        if (masked) tile(std::true_type{});
+        else tile(std::false_type{});
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
@@ -395,9 +456,10 @@ __global__ void __launch_bounds__(CT_THREADS, 1) cache_attention_tc_kernel(const
         tc_fence_after();
       }
       done += here;
-      // ---- the two streams' sums come together: each takes half of the columns
+      // ---- the two streams' sums come together: with HALF the second's come over by the queries' space (every
+      // product with them is done), else each stream takes half of the columns of both
       s_ml[s][row] = make_float2(m, l);
-      named_bar(3, CT_SOFT);
+      named_bar(3, Cfg::SOFT);
       const float2 z0 = s_ml[0][row], z1 = s_ml[1][row];
       const float M = fmaxf(fmaxf(z0.x, z1.x), -FLT_MAX);
       const float f0 = ex2(z0.x - M), f1 = here > 1 ? ex2(z1.x - M) : 0.f, L = z0.y * f0 + z1.y * f1;
@@ -407,7 +469,56 @@ __global__ void __launch_bounds__(CT_THREADS, 1) cache_attention_tc_kernel(const
       auto part = [&](uint32_t team) { return 2 * ((size_t)team * a.team + head) + (team * per < s0); };
       const size_t place = part(blockIdx.x / a.team) * CT_ROWS + row;
       const float by = L == 0.f ? 0.f : a.c.v_unit / L;
-      if (!idle) {
+      auto leave = [&](int c, const float (&y)[16]) {            // 16 columns of the row
+        if (!mine || c * 16 >= d) return;
+        if (complete) {
+          E* out = static_cast<E*>(a.out) + at.n * a.o_s[0] + tok * a.o_s[1] + hq * a.o_s[2] + c * 16;
+#pragma unroll
+          for (int e = 0; e < 16; e += 8)
+            *reinterpret_cast<uint4*>(out + e) =
+                L == 0.f ? make_uint4(0, 0, 0, 0)
+                         : make_uint4(bf16_pack2(y[e] * by, y[e + 1] * by), bf16_pack2(y[e + 2] * by, y[e + 3] * by),
+                                      bf16_pack2(y[e + 4] * by, y[e + 5] * by), bf16_pack2(y[e + 6] * by, y[e + 7] * by));
+        } else {
+          float* po = a.po + place * DP + c * 16;
+#pragma unroll
+          for (int e = 0; e < 16; e += 4) *reinterpret_cast<float4*>(po + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
+        }
+      };
+      if constexpr (HALF) {
+        float4* box = reinterpret_cast<float4*>(sQ) + row * (DP / 4);        // 16-byte pieces, turned by the row
+        if (s == 1 && here > 1 && !idle) {
+#pragma unroll 1
+          for (int c = 0; c < DP / 16; ++c) {
+            uint32_t o[16];
+            tmem_ld16(lane_base + Cfg::O(1) + 16 * c, o);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              box[(4 * c + i) ^ (row & 7)] =
+                  make_float4(__uint_as_float(o[4 * i]) * f1, __uint_as_float(o[4 * i + 1]) * f1,
+                              __uint_as_float(o[4 * i + 2]) * f1, __uint_as_float(o[4 * i + 3]) * f1);
+          }
+        }
+        named_bar(3, Cfg::SOFT);
+        if (s == 0 && !idle) {
+#pragma unroll 1
+          for (int c = 0; c < DP / 16; ++c) {
+            uint32_t o[16];
+            tmem_ld16(lane_base + Cfg::O(0) + 16 * c, o);
+            float y[16];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+              if (here > 1) v = box[(4 * c + i) ^ (row & 7)];
+              y[4 * i] = fmaf(__uint_as_float(o[4 * i]), f0, v.x);
+              y[4 * i + 1] = fmaf(__uint_as_float(o[4 * i + 1]), f0, v.y);
+              y[4 * i + 2] = fmaf(__uint_as_float(o[4 * i + 2]), f0, v.z);
+              y[4 * i + 3] = fmaf(__uint_as_float(o[4 * i + 3]), f0, v.w);
+            }
+            leave(c, y);
+          }
+        }
+      } else if (!idle) {
 #pragma unroll 1
         for (int c = s * (DP / 32); c < (s + 1) * (DP / 32); ++c) {
           uint32_t o[16], o1[16];
@@ -419,20 +530,7 @@ __global__ void __launch_bounds__(CT_THREADS, 1) cache_attention_tc_kernel(const
             y[e] = __uint_as_float(o[e]) * f0;
             if (here > 1) y[e] = fmaf(__uint_as_float(o1[e]), f1, y[e]);
           }
-          if (!mine || c * 16 >= d) continue;
-          if (complete) {
-            E* out = static_cast<E*>(a.out) + at.n * a.o_s[0] + tok * a.o_s[1] + hq * a.o_s[2] + c * 16;
-#pragma unroll
-            for (int e = 0; e < 16; e += 8)
-              *reinterpret_cast<uint4*>(out + e) =
-                  L == 0.f ? make_uint4(0, 0, 0, 0)
-                           : make_uint4(bf16_pack2(y[e] * by, y[e + 1] * by), bf16_pack2(y[e + 2] * by, y[e + 3] * by),
-                                        bf16_pack2(y[e + 4] * by, y[e + 5] * by), bf16_pack2(y[e + 6] * by, y[e + 7] * by));
-          } else {
-            float* po = a.po + place * DP + c * 16;
-#pragma unroll
-            for (int e = 0; e < 16; e += 4) *reinterpret_cast<float4*>(po + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
-          }
+          leave(c, y);
         }
       }
       if (s == 0 && mine) {
@@ -440,7 +538,7 @@ __global__ void __launch_bounds__(CT_THREADS, 1) cache_attention_tc_kernel(const
         else a.ml[place] = make_float2(M, L);
       }
       if (!complete) {
-        named_bar(3, CT_SOFT);
+        named_bar(3, Cfg::SOFT);
         if (tid == 0) {
           __threadfence();
           uint32_t* left = a.left + part(team0);
@@ -448,9 +546,9 @@ __global__ void __launch_bounds__(CT_THREADS, 1) cache_attention_tc_kernel(const
           if (joins) *left = 0;
           __threadfence();
         }
-        named_bar(3, CT_SOFT);
+        named_bar(3, Cfg::SOFT);
         if (joins)
-          for (int i0 = warp * 4; i0 < tile_rows; i0 += 32) {  // four rows a warp, a part of each at a time
+          for (int i0 = warp * 4; i0 < tile_rows; i0 += 4 * (Cfg::SOFT / 32)) {  // four rows a warp, a part of each at a time
             float jm[4], jl[4];
             float4 y[4];
 #pragma unroll
@@ -491,7 +589,7 @@ __global__ void __launch_bounds__(CT_THREADS, 1) cache_attention_tc_kernel(const
           }
       }
       tc_fence_before();
-      named_bar(2, CT_SOFT + 32);
+      named_bar(2, Cfg::SOFT + 32);
       tc_fence_after();
       if (done < count) at.next(a, a.blocks);
     }
@@ -499,26 +597,31 @@ __global__ void __launch_bounds__(CT_THREADS, 1) cache_attention_tc_kernel(const
   tc_fence_before();
   __syncthreads();
   if (abort_flag && tid == 0) set_status(a.status, LILICORR_ERR_TIMEOUT);
-  if (warp == 8) {
+  if (warp == Cfg::MMA_WARP) {
     tc_fence_after();
     tmem_dealloc(tmem, CT_TMEM);
   }
 }
 
-template <int DP, int DIM>
+template <int DP, int DIM, bool HALF>
 lilicorr_status_t launch_tc(const CaArgs& a, const CaPlan& p, cudaStream_t st) {
+  using Cfg = CtCfg<DP, HALF>;
   static bool configured[64] = {false};
-  auto* kernel = cache_attention_tc_kernel<DP, DIM>;
+  auto* kernel = cache_attention_tc_kernel<DP, DIM, HALF>;
   LL_TRY(allow_max_dynamic_smem(kernel, configured));
-  return launch_k(kernel, (unsigned)p.ctas, CT_THREADS, CtCfg<DP>::SMEM, st, a);
+  return launch_k(kernel, (unsigned)p.ctas, Cfg::THREADS, Cfg::SMEM, st, a);
+}
+template <int DP, int DIM>
+lilicorr_status_t launch_rows(const CaArgs& a, const CaPlan& p, cudaStream_t st) {
+  return a.T * a.rep <= 64 ? launch_tc<DP, DIM, true>(a, p, st) : launch_tc<DP, DIM, false>(a, p, st);
 }
 
 }  // namespace
 
 lilicorr_status_t launch_ca_tc(const CaArgs& a, const CaPlan& p, cudaStream_t st) {
-  if (a.c.d == 128) return launch_tc<128, 128>(a, p, st);
-  if (a.c.d == 64) return launch_tc<64, 64>(a, p, st);
-  return a.c.d < 64 ? launch_tc<64, 0>(a, p, st) : launch_tc<128, 0>(a, p, st);
+  if (a.c.d == 128) return launch_rows<128, 128>(a, p, st);
+  if (a.c.d == 64) return launch_rows<64, 64>(a, p, st);
+  return a.c.d < 64 ? launch_rows<64, 0>(a, p, st) : launch_rows<128, 0>(a, p, st);
 }
 
 }  // namespace lilicorr
