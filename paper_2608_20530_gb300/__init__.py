@@ -170,6 +170,11 @@ def _stream() -> int:
     return torch.cuda.current_stream().cuda_stream
 
 
+def _stream_of(dev: int) -> int:
+    """_stream() where the current device is known."""
+    return _raw_stream(dev) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
+
+
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
@@ -853,7 +858,7 @@ def cache_append(cache: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seq_len:
     w = None if weights is None else _cache_weights(weights, x, dev)
     status = lib().lilicorr_cache_append(_CACHE_DESC.pack(*x, k_unit, v_unit), cache.data_ptr(),
                                          _dtype_code(k), T, k.data_ptr(), ks, v.data_ptr(), vs,
-                                         _seq_len(seq_len, x[0], dev), w, _stream())
+                                         _seq_len(seq_len, x[0], dev), w, _stream_of(dev))
     if status:
         _check(status, "cache_append")
     return cache
@@ -875,7 +880,7 @@ def cache_read(cache: torch.Tensor, seq_len: torch.Tensor, tokens: int,
     s = _STRIDES.pack(*k.stride()[:3])
     status = lib().lilicorr_cache_read(_CACHE_DESC.pack(*x, k_unit, v_unit), cache.data_ptr(),
                                        _dtype_code(k), tokens, k.data_ptr(), s, v.data_ptr(), s,
-                                       _seq_len(seq_len, x[0], dev), _stream())
+                                       _seq_len(seq_len, x[0], dev), _stream_of(dev))
     if status:
         _check(status, "cache_read")
     return k, v
@@ -928,7 +933,7 @@ def cache_attention(q: torch.Tensor, cache: torch.Tensor, seq_len: torch.Tensor,
         _here(ws.buf, "ws", dev)
     status = lib().lilicorr_cache_attention(desc, q.data_ptr(), cache.data_ptr(),
                                             _seq_len(seq_len, N, dev), out.data_ptr(), lse.data_ptr(), w,
-                                            ws.buf.data_ptr(), ws.nbytes, _stream())
+                                            ws.buf.data_ptr(), ws.nbytes, _stream_of(dev))
     if status:
         _check(status, "cache_attention")
     return out, lse
@@ -961,7 +966,7 @@ def cache_evict(cache: torch.Tensor, weights: torch.Tensor, seq_len: torch.Tenso
     new_len = torch.empty((x[0],), dtype=torch.int32, device=cache.device)
     status = lib().lilicorr_cache_evict(_CACHE_DESC.pack(*x, 1.0, 1.0), cache.data_ptr(), w,
                                         _seq_len(seq_len, x[0], dev), budget, recent, first, to, to_p, to_w,
-                                        kept.data_ptr(), new_len.data_ptr(), _stream())
+                                        kept.data_ptr(), new_len.data_ptr(), _stream_of(dev))
     if status:
         _check(status, "cache_evict")
     return kept, new_len

@@ -47,6 +47,18 @@ lilicorr_status_t cache_view(const lilicorr_cache_desc* d, const void* cache, bo
 namespace {
 
 // ------------------------------------------------------------------------------- append and read
+// x / d of whole numbers x < 2^31 by a product: with 2^s >= d and m = ceil(2^(31 + s) / d) below 2^32, m x / 2^(31 + s)
+// exceeds x / d by less than 1 / d (Granlund and Montgomery, 1994).
+struct Quotient {
+  uint32_t d, m, s;
+  void set(uint32_t by) {
+    d = by;
+    for (s = 0; (1ull << s) < by; ++s) {}
+    m = (uint32_t)(((1ull << (31 + s)) + by - 1) / by);
+  }
+  __device__ __forceinline__ uint32_t of(uint32_t x) const { return (uint32_t)(((uint64_t)x * m) >> 31) >> s; }
+};
+
 struct CacheTokens {
   const void* k;               // read: written
   const void* v;
@@ -54,6 +66,9 @@ struct CacheTokens {
   int T;
   const int32_t* seq_len;
   float* weights;
+  uint32_t total;              // threads that have work
+  int wide;                    // all groups start at multiples of 32 bytes: a load or store of 32 each
+  Quotient by_row, by_head, by_T;
 };
 
 __device__ __forceinline__ float max_nan(float a, float b) {
@@ -81,38 +96,49 @@ __device__ __forceinline__ float scale_value(uint32_t byte) {
   asm("{\n .reg .b16 lo, hi;\n mov.b32 {lo, hi}, %1;\n cvt.f32.f16 %0, lo;\n}" : "=f"(f) : "r"(r));
   return f;
 }
-// the two codes of a byte
-__device__ __forceinline__ float2 code_values(uint32_t byte) {
-  float2 f;
-  asm("{\n .reg .b8 t;\n .reg .b32 w;\n .reg .b16 lo, hi;\n cvt.u8.u32 t, %2;\n cvt.rn.f16x2.e2m1x2 w, t;\n"
-      " mov.b32 {lo, hi}, w;\n cvt.f32.f16 %0, lo;\n cvt.f32.f16 %1, hi;\n}"
-      : "=f"(f.x), "=f"(f.y) : "r"(byte));
-  return f;
+// the eight codes of a word
+__device__ __forceinline__ void code_values(uint32_t w, float* x) {
+  uint32_t r[4];
+  asm("{\n .reg .b8 a, b, c, d;\n mov.b32 {a, b, c, d}, %4;\n cvt.rn.f16x2.e2m1x2 %0, a;\n"
+      " cvt.rn.f16x2.e2m1x2 %1, b;\n cvt.rn.f16x2.e2m1x2 %2, c;\n cvt.rn.f16x2.e2m1x2 %3, d;\n}"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(w));
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %2;\n cvt.f32.f16 %0, l;\n cvt.f32.f16 %1, h;\n}"
+        : "=f"(x[2 * i]), "=f"(x[2 * i + 1]) : "r"(r[i]));
 }
 
-__device__ __forceinline__ void load16(const __nv_bfloat16* p, float (&x)[16]) {
-  uint4 w[2] = {reinterpret_cast<const uint4*>(p)[0], reinterpret_cast<const uint4*>(p)[1]};
-  const uint32_t* u = reinterpret_cast<const uint32_t*>(w);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    x[2 * i] = __uint_as_float(u[i] << 16);
-    x[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+// 32 bytes, in one piece (a whole sector a lane) or in two
+__device__ __forceinline__ void load32(const void* p, int wide, uint32_t* u) {
+  if (wide) {
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7])
+                 : "l"(p));
+  } else {
+    const uint4 x = __ldcs(static_cast<const uint4*>(p)), y = __ldcs(static_cast<const uint4*>(p) + 1);
+    u[0] = x.x; u[1] = x.y; u[2] = x.z; u[3] = x.w;
+    u[4] = y.x; u[5] = y.y; u[6] = y.z; u[7] = y.w;
   }
 }
-__device__ __forceinline__ void load16(const float* p, float (&x)[16]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) reinterpret_cast<float4*>(x)[i] = reinterpret_cast<const float4*>(p)[i];
+__device__ __forceinline__ void store32(void* p, int wide, const uint32_t* u) {
+  if (wide) {
+    asm volatile("st.global.v8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::"r"(u[0]), "r"(u[1]), "r"(u[2]),
+                 "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]), "l"(p)
+                 : "memory");
+  } else {
+    static_cast<uint4*>(p)[0] = make_uint4(u[0], u[1], u[2], u[3]);
+    static_cast<uint4*>(p)[1] = make_uint4(u[4], u[5], u[6], u[7]);
+  }
 }
-__device__ __forceinline__ void store16(__nv_bfloat16* p, const float (&x)[16]) {
+__device__ __forceinline__ void store16(__nv_bfloat16* p, int wide, const float (&x)[16]) {
   uint32_t u[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) u[i] = bf16_pack2(x[2 * i], x[2 * i + 1]);
-  reinterpret_cast<uint4*>(p)[0] = *reinterpret_cast<uint4*>(u);
-  reinterpret_cast<uint4*>(p)[1] = *reinterpret_cast<uint4*>(u + 4);
+  store32(p, wide, u);
 }
-__device__ __forceinline__ void store16(float* p, const float (&x)[16]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) reinterpret_cast<float4*>(p)[i] = reinterpret_cast<const float4*>(x)[i];
+__device__ __forceinline__ void store16(float* p, int wide, const float (&x)[16]) {
+  store32(p, wide, reinterpret_cast<const uint32_t*>(x));
+  store32(p + 8, wide, reinterpret_cast<const uint32_t*>(x) + 8);
 }
 
 // The byte of the scale nearest to top / (6 unit). The quotient's rounding to fp32 must not put it on the
@@ -152,45 +178,74 @@ __device__ __forceinline__ uint2 group_codes(const float (&x)[16], float su, flo
   return make_uint2(w[0], w[1]);
 }
 
-// A thread has one group of 16 elements; groups in the order (token, head, key or value, group).
-struct CacheGroup { int n, t, h, kv, g, pos; };
+// A thread has a group of 16 elements of the key and of the value; groups in the order (token, head, group).
+struct CacheGroup { int n, t, h, g, pos; };
 __device__ __forceinline__ bool cache_group(const CacheView& c, const CacheTokens& a, CacheGroup* x) {
   uint32_t i = blockIdx.x * blockDim.x + threadIdx.x;
-  const uint32_t G = c.d / 16, per = 2 * G * c.H, total = per * (uint32_t)a.T * (uint32_t)c.N;
-  if (i >= total) return false;
-  const uint32_t row = i / per;
-  i -= row * per;
-  x->n = row / a.T;
+  if (i >= a.total) return false;
+  const uint32_t row = a.by_row.of(i);
+  i -= row * a.by_row.d;
+  x->h = a.by_head.of(i);
+  x->g = i - x->h * a.by_head.d;
+  x->n = a.by_T.of(row);
   x->t = row - x->n * a.T;
-  x->h = i / (2 * G);
-  i -= x->h * 2 * G;
-  x->kv = i >= G;
-  x->g = i - x->kv * G;
   const int len = a.seq_len[x->n];
   x->pos = len < 0 ? -1 : len - a.T + x->t;
   return true;
 }
 
+// A group, and its max |x|: NaN where there is one
+__device__ __forceinline__ void group_load(const __nv_bfloat16* p, int wide, uint32_t (&u)[8]) { load32(p, wide, u); }
+__device__ __forceinline__ void group_load(const float* p, int wide, uint32_t (&u)[16]) {
+  load32(p, wide, u);
+  load32(p + 8, wide, u + 8);
+}
+__device__ __forceinline__ float group_top(const uint32_t (&u)[8], float (&x)[16]) {
+  uint32_t top = u[0] & 0x7FFF7FFFu;                 // two maxima side by side
+#pragma unroll
+  for (int i = 1; i < 8; ++i)
+    asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(top) : "r"(u[i] & 0x7FFF7FFFu));
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    x[2 * i] = __uint_as_float(u[i] << 16);
+    x[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+  }
+  return max_nan(__uint_as_float(top << 16), __uint_as_float(top & 0xFFFF0000u));
+}
+__device__ __forceinline__ float group_top(const uint32_t (&u)[16], float (&x)[16]) {
+  float top = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    x[i] = __uint_as_float(u[i]);
+    top = max_nan(top, fabsf(x[i]));
+  }
+  return top;
+}
+
+// Bytes bound both kernels (bf16: 2.56 bytes an element); what they compute is kept to about 130 (append) and 95
+// (read) instructions a group, most of them on the elements.
 template <typename E>
 __global__ void __launch_bounds__(256) cache_append_kernel(const CacheView c, const CacheTokens a) {
   pdl_wait();
   CacheGroup x;
   if (!cache_group(c, a, &x) || x.pos < 0 || x.pos >= c.S) return;
-  const E* src = static_cast<const E*>(x.kv ? a.v : a.k);
-  const int64_t* s = x.kv ? a.v_s : a.k_s;
-  float e[16];
-  load16(src + (x.n * s[0] + x.t * s[1] + x.h * s[2] + x.g * 16), e);
-  float top = 0.f;
+  uint32_t u[2][4 * sizeof(E)];
+  group_load(static_cast<const E*>(a.k) + (x.n * a.k_s[0] + x.t * a.k_s[1] + x.h * a.k_s[2] + x.g * 16), a.wide, u[0]);
+  group_load(static_cast<const E*>(a.v) + (x.n * a.v_s[0] + x.t * a.v_s[1] + x.h * a.v_s[2] + x.g * 16), a.wide, u[1]);
+  unsigned char* rec = c.at(x.n, x.pos, x.h);
 #pragma unroll
-  for (int i = 0; i < 16; ++i) top = max_nan(top, fabsf(e[i]));
-  const float unit = x.kv ? c.v_unit : c.k_unit;
-  const uint32_t b = group_scale(top, 1.f / unit);
-  unsigned char* rec = c.at(x.n, x.pos, x.h) + x.kv * cache_half_bytes(c.d);
-  *reinterpret_cast<uint2*>(rec + x.g * 8) = group_codes(e, scale_value(b) * unit, E());
-  rec[c.d / 2 + x.g] = (unsigned char)b;
-  if (x.g == 0)                                      // scales that no group has
-    for (int i = c.d / 16; i < 8; ++i) rec[c.d / 2 + i] = 0;
-  if (a.weights && x.g == 0 && !x.kv) a.weights[((size_t)x.n * c.H + x.h) * c.S + x.pos] = 0.f;
+  for (int kv = 0; kv < 2; ++kv) {
+    const float unit = kv ? c.v_unit : c.k_unit;
+    float e[16];
+    const float top = group_top(u[kv], e);
+    const uint32_t b = group_scale(top, 1.f / unit);
+    unsigned char* to = rec + kv * cache_half_bytes(c.d);
+    *reinterpret_cast<uint2*>(to + x.g * 8) = group_codes(e, scale_value(b) * unit, E());
+    to[c.d / 2 + x.g] = (unsigned char)b;
+    if (x.g == 0)                                    // scales that no group has
+      for (int i = c.d / 16; i < 8; ++i) to[c.d / 2 + i] = 0;
+  }
+  if (a.weights && x.g == 0) a.weights[((size_t)x.n * c.H + x.h) * c.S + x.pos] = 0.f;
 }
 
 template <typename E>
@@ -198,23 +253,28 @@ __global__ void __launch_bounds__(256) cache_read_kernel(const CacheView c, cons
   pdl_wait();
   CacheGroup x;
   if (!cache_group(c, a, &x)) return;
-  float e[16];
-#pragma unroll
-  for (int i = 0; i < 16; ++i) e[i] = 0.f;
+  uint2 w[2] = {make_uint2(0, 0), make_uint2(0, 0)};
+  uint32_t b[2] = {0, 0};
   if (x.pos >= 0 && x.pos < c.S) {
-    const unsigned char* rec = c.at(x.n, x.pos, x.h) + x.kv * cache_half_bytes(c.d);
-    const uint2 w = *reinterpret_cast<const uint2*>(rec + x.g * 8);
-    const float su = scale_value(rec[c.d / 2 + x.g]) * (x.kv ? c.v_unit : c.k_unit);
+    const unsigned char* rec = c.at(x.n, x.pos, x.h);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float2 f = code_values(((i < 4 ? w.x : w.y) >> (i % 4 * 8)) & 0xFFu);
-      e[2 * i] = f.x * su;
-      e[2 * i + 1] = f.y * su;
+    for (int kv = 0; kv < 2; ++kv) {
+      w[kv] = *reinterpret_cast<const uint2*>(rec + kv * cache_half_bytes(c.d) + x.g * 8);
+      b[kv] = rec[kv * cache_half_bytes(c.d) + c.d / 2 + x.g];
     }
   }
-  E* dst = static_cast<E*>(const_cast<void*>(x.kv ? a.v : a.k));
-  const int64_t* s = x.kv ? a.v_s : a.k_s;
-  store16(dst + (x.n * s[0] + x.t * s[1] + x.h * s[2] + x.g * 16), e);
+#pragma unroll
+  for (int kv = 0; kv < 2; ++kv) {
+    const float su = scale_value(b[kv]) * (kv ? c.v_unit : c.k_unit);
+    float e[16];
+    code_values(w[kv].x, e);
+    code_values(w[kv].y, e + 8);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) e[i] *= su;
+    E* dst = static_cast<E*>(const_cast<void*>(kv ? a.v : a.k));
+    const int64_t* s = kv ? a.v_s : a.k_s;
+    store16(dst + (x.n * s[0] + x.t * s[1] + x.h * s[2] + x.g * 16), a.wide, e);
+  }
 }
 
 lilicorr_status_t run_tokens(const lilicorr_cache_desc* desc, const void* cache, lilicorr_dtype_t dtype,
@@ -224,7 +284,7 @@ lilicorr_status_t run_tokens(const lilicorr_cache_desc* desc, const void* cache,
   LL_TRY(cache_shape(desc));
   if (dtype != LILICORR_F32 && dtype != LILICORR_BF16) return LILICORR_ERR_DTYPE;
   if (tokens < 0) return LILICORR_ERR_SHAPE;
-  const double groups = (double)desc->sequences * tokens * desc->kv_heads * (desc->head_dim / 8);
+  const double groups = (double)desc->sequences * tokens * desc->kv_heads * (desc->head_dim / 16);
   if (groups >= 2147483648.0) return LILICORR_ERR_SHAPE;
   CacheView c;
   LL_TRY(cache_view(desc, cache, append, &c));
@@ -244,6 +304,13 @@ lilicorr_status_t run_tokens(const lilicorr_cache_desc* desc, const void* cache,
   a.T = tokens;
   a.seq_len = seq_len;
   a.weights = weights;
+  a.total = (uint32_t)groups;
+  const int per32 = 2 * per16;
+  a.wide = !(((uintptr_t)k | (uintptr_t)v) & 31);
+  for (int i = 0; i < 3; ++i) a.wide &= a.k_s[i] % per32 == 0 && a.v_s[i] % per32 == 0;
+  a.by_row.set(c.H * (c.d / 16));
+  a.by_head.set(c.d / 16);
+  a.by_T.set(tokens);
   const unsigned grid = (unsigned)(((int64_t)groups + 255) / 256);
   if (append)
     return dtype == LILICORR_BF16 ? launch_k(cache_append_kernel<__nv_bfloat16>, grid, 256, 0, st, c, a)
