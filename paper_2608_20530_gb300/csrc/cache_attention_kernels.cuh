@@ -61,11 +61,11 @@ struct CaCursor {
   }
 };
 
-// This CTA's part of the list: as many tiles as it returns, from `at` on, which is place `first` of the list. Each
-// warp finds it for itself.
-template <int KEYS>
-__device__ __forceinline__ uint32_t ca_range(const CaArgs& a, int blocks, CaCursor<KEYS>* at, uint32_t* first,
-                                             uint32_t* per) {
+// The list cut over `teams` teams: `per` tiles each. `want` (of `per`) says which place of the list `at` becomes,
+// which head of the team apart; the number of places. Each warp finds it for itself.
+template <int KEYS, typename F>
+__device__ __forceinline__ uint32_t ca_locate(const CaArgs& a, int blocks, uint32_t teams, F want,
+                                              CaCursor<KEYS>* at, uint32_t* per) {
   const int lane = threadIdx.x & 31, N = a.c.N, chunk = (N + 31) / 32;
   const int n0 = min(N, lane * chunk), n1 = min(N, n0 + chunk);
   const uint32_t per_tile = (uint32_t)(a.c.H / a.team) * blocks;
@@ -81,26 +81,37 @@ __device__ __forceinline__ uint32_t ca_range(const CaArgs& a, int blocks, CaCurs
     const uint32_t x = __shfl_up_sync(0xffffffffu, upto, o);
     if (lane >= o) upto += x;
   }
-  const uint32_t total = __shfl_sync(0xffffffffu, upto, 31), g = blockIdx.x / a.team;
-  *per = ca_per_team(total, gridDim.x / a.team);
-  *first = g * *per;
-  if (*first >= total) return 0;
-  const int owner = __ffs(__ballot_sync(0xffffffffu, *first < upto)) - 1;
+  const uint32_t total = __shfl_sync(0xffffffffu, upto, 31);
+  *per = ca_per_team(total, teams);
+  const uint32_t wanted = want(*per);
+  if (wanted >= total) return total;
+  const int owner = __ffs(__ballot_sync(0xffffffffu, wanted < upto)) - 1;
   uint32_t b = upto - mine;
   int n = n0;
   if (lane == owner && chunk > 1)
     while (true) {
       const uint32_t t = ca_tiles<KEYS>(raw, a.c.S) * per_tile;
-      if (*first < b + t) break;
+      if (wanted < b + t) break;
       b += t;
       raw = a.seq_len[++n];
     }
   at->set(a, __shfl_sync(0xffffffffu, n, owner), __shfl_sync(0xffffffffu, raw, owner));
-  const uint32_t place = *first - __shfl_sync(0xffffffffu, b, owner), item = place / at->tiles;
+  const uint32_t place = wanted - __shfl_sync(0xffffffffu, b, owner), item = place / at->tiles;
   at->tile = place - item * at->tiles;
   at->h = item / blocks;
   at->rb = item - at->h * blocks;
-  at->h = at->h * a.team + (blockIdx.x - g * a.team);
+  at->h *= a.team;
+  return total;
+}
+// This CTA's part of the list: as many tiles as it returns, from `at` on, which is place `first` of the list.
+template <int KEYS>
+__device__ __forceinline__ uint32_t ca_range(const CaArgs& a, int blocks, CaCursor<KEYS>* at, uint32_t* first,
+                                             uint32_t* per) {
+  const uint32_t g = blockIdx.x / a.team;
+  const uint32_t total = ca_locate<KEYS>(a, blocks, gridDim.x / a.team, [&](uint32_t p) { return g * p; }, at, per);
+  *first = g * *per;
+  if (*first >= total) return 0;
+  at->h += blockIdx.x - g * a.team;
   return min(*per, total - *first);
 }
 

@@ -104,12 +104,14 @@ __device__ __noinline__ bool wait_long(uint64_t* bar, uint32_t parity, long long
 // Half a record at `rec` (or zeros) as row `key` of a tile: DP columns of fp16, zeros past the head's width.
 template <int DP, int DIM>
 __device__ __forceinline__ void expand(const unsigned char* rec, bool there, int d, uint8_t* tile, int key) {
-  // everything is read first: the place may be given back while it is expanded
+  // Everything is read first: the place may be given back while it is expanded. Records of 144 bytes start at every
+  // second pair of banks, so keys of the upper half of 16 read their groups in another order than the lower.
+  const int turn = DIM ? key >> 3 & 1 : 0;
   uint2 w[DP / 16], b = *reinterpret_cast<const uint2*>(rec + d / 2);
 #pragma unroll
   for (int g = 0; g < DP / 16; ++g) {
     w[g] = make_uint2(0, 0);
-    if (DIM || g * 16 < d) w[g] = *reinterpret_cast<const uint2*>(rec + g * 8);
+    if (DIM || g * 16 < d) w[g] = *reinterpret_cast<const uint2*>(rec + (g ^ turn) * 8);
   }
   // scales of 0 where there is no key (codes are finite whatever they are), or no such group
   if (!there) b = make_uint2(0, 0);
@@ -117,13 +119,13 @@ __device__ __forceinline__ void expand(const unsigned char* rec, bool there, int
   const int x = key & 7;
 #pragma unroll
   for (int g = 0; g < DP / 16; ++g) {
-    const uint32_t two = __byte_perm(b.x, b.y, (g & 7) * 0x11), f = scales(DIM || g * 16 < d ? two : 0u);
+    const uint32_t two = __byte_perm(b.x, b.y, ((g & 7) ^ turn) * 0x11), f = scales(DIM || g * 16 < d ? two : 0u);
     uint32_t r[4];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const int p = 2 * g + i;
+      const int p = 2 * (g ^ turn) + i;
       codes(i ? w[g].y : w[g].x, r);
-      *reinterpret_cast<uint4*>(row + (p >> 3) * CT_CHUNK + (((p & 7) ^ x) << 4)) =
+      *reinterpret_cast<uint4*>(row + (2 * g + i >> 3) * CT_CHUNK + (((p & 7) ^ x) << 4)) =
           make_uint4(mul2(r[0], f), mul2(r[1], f), mul2(r[2], f), mul2(r[3], f));
     }
   }
@@ -146,7 +148,6 @@ __global__ void __launch_bounds__((CtCfg<DP, HALF>::THREADS), 1) cache_attention
   __shared__ volatile int abort_flag;
   __shared__ float s_factor[CT_ROWS];
   __shared__ float2 s_ml[2][CT_ROWS];
-  __shared__ bool joins;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int d = DIM ? DIM : a.c.d, R = cache_record_bytes(d), rows = a.T * a.rep;
@@ -371,80 +372,83 @@ __global__ void __launch_bounds__((CtCfg<DP, HALF>::THREADS), 1) cache_attention
         tc_fence_after();
         const int k0 = (tile0 + (int)t) * CT_KEYS, seen = lim - k0;
         const bool masked = k0 + CT_KEYS > at.len - (a.T - 1);   // some row does not see all of them
-        auto tile = [&](auto some) {                 // in two copies: the usual one without comparisons
-          constexpr bool MASKED = decltype(some)::value;
-          uint32_t xs[HALF ? 2 : 1][32];               // HALF: the next ones are read while these are worked on
-          tmem_ld32(lane_base + Cfg::S(s), xs[0]);
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {                // 32 scores at a time, a step of the reference each
-            if (HALF && c < 3) tmem_ld32_nowait(lane_base + Cfg::S(s) + 32 * (c + 1), xs[HALF ? (c + 1) & 1 : 0]);
-            if (!HALF && c > 0) tmem_ld32(lane_base + Cfg::S(s) + 32 * c, xs[0]);
-            uint32_t (&x)[32] = xs[HALF ? c & 1 : 0];
-            if (MASKED)
-#pragma unroll
-              for (int e = 0; e < 32; ++e)
-                if (32 * c + e >= seen) x[e] = 0xFF800000u;        // -inf
-            if (a.scores && mine) {                    // for what each key gets: 32 rows of a key side by side
-              float* to = a.scores + (((size_t)at.n * a.c.H + at.h) * a.c.S + k0 + 32 * c) * a.pad + r;
-#pragma unroll
-              for (int e = 0; e < 32; ++e)
-                if (k0 + 32 * c + e < at.len) to[(size_t)e * a.pad] = __uint_as_float(x[e]);
-            }
-            float mx[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-            for (int e = 0; e < 32; e += 4) {
-              mx[0] = fmaxf(fmaxf(mx[0], __uint_as_float(x[e])), __uint_as_float(x[e + 1]));
-              mx[1] = fmaxf(fmaxf(mx[1], __uint_as_float(x[e + 2])), __uint_as_float(x[e + 3]));
-            }
-            const float top = fmaxf(mx[0], mx[1]) * f;
-            if (c == 0 && t == (uint32_t)s) {
-              m = ceilf(top);
-            } else if (__any_sync(0xffffffffu, top > m + CA_SLACK)) {
-              // the sums so far, and this tile's probabilities before these, to the new reference, by a whole
-              // power of two (the product of the sums is complete: the scores came behind it)
-              const float to = fmaxf(m, ceilf(top)), y = pow2_down(m - to);
-              m = to;
-              l *= y;
-              tmem_wait_st();
-              if (t != (uint32_t)s)
+        if (masked) {                                // scores of keys that the row does not see: -infinity
 #pragma unroll 1
-                for (int i = 0; i < DP / 16; ++i) {
-                  uint32_t o[16];
-                  tmem_ld16(lane_base + Cfg::O(s) + 16 * i, o);
+          for (int c = 0; c < 4; ++c) {
+            uint32_t x[32];
+            tmem_ld32(lane_base + Cfg::S(s) + 32 * c, x);
 #pragma unroll
-                  for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * y);
-                  tmem_st16(lane_base + Cfg::O(s) + 16 * i, o);
-                }
-#pragma unroll 1
-              for (int i = 0; i < c; ++i) {
-                uint32_t o[16];
-                const uint32_t y2 = half2_of(y, y);
-                tmem_ld16(lane_base + Cfg::P(s, 2 * i), o);
-#pragma unroll
-                for (int e = 0; e < 16; ++e) o[e] = mul2(o[e], y2);
-                tmem_st16(lane_base + Cfg::P(s, 2 * i), o);
-              }
-            }
-            const float base = CA_UP - (m == -INFINITY ? 0.f : m);
-            float sum[2] = {0.f, 0.f};
-            uint32_t p[16];
-#pragma unroll
-            for (int e = 0; e < 32; e += 2) {
-              const float p0 = ex2(fmaf(__uint_as_float(x[e]), f, base)), p1 = ex2(fmaf(__uint_as_float(x[e + 1]), f, base));
-              sum[0] += p0;
-              sum[1] += p1;
-              p[e / 2] = half2_of(p0, p1);
-            }
-            l += sum[0] + sum[1];
-            if (HALF && c < 3) {
-              tmem_wait_ld();
-              pin(xs[HALF ? (c + 1) & 1 : 0]);
-            }
-            tmem_st16(lane_base + Cfg::P(s, 2 * c), p);
+            for (int e = 0; e < 32; ++e)
+              if (32 * c + e >= seen) x[e] = 0xFF800000u;
+            tmem_st32(lane_base + Cfg::S(s) + 32 * c, x);
           }
-        };
-        if (masked) tile(std::true_type{});
-        else tile(std::false_type{});
+          tmem_wait_st();
+        }
+        uint32_t xs[HALF ? 2 : 1][32];               // HALF: the next ones are read while these are worked on
+        tmem_ld32(lane_base + Cfg::S(s), xs[0]);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {                // 32 scores at a time, a step of the reference each
+          if (HALF && c < 3) tmem_ld32_nowait(lane_base + Cfg::S(s) + 32 * (c + 1), xs[HALF ? (c + 1) & 1 : 0]);
+          if (!HALF && c > 0) tmem_ld32(lane_base + Cfg::S(s) + 32 * c, xs[0]);
+          uint32_t (&x)[32] = xs[HALF ? c & 1 : 0];
+          if (a.scores && mine) {                    // for what each key gets: 32 rows of a key side by side
+            float* to = a.scores + (((size_t)at.n * a.c.H + at.h) * a.c.S + k0 + 32 * c) * a.pad + r;
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              if (k0 + 32 * c + e < at.len) to[(size_t)e * a.pad] = __uint_as_float(x[e]);
+          }
+          float mx[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+          for (int e = 0; e < 32; e += 4) {
+            mx[0] = fmaxf(fmaxf(mx[0], __uint_as_float(x[e])), __uint_as_float(x[e + 1]));
+            mx[1] = fmaxf(fmaxf(mx[1], __uint_as_float(x[e + 2])), __uint_as_float(x[e + 3]));
+          }
+          const float top = fmaxf(mx[0], mx[1]) * f;
+          if (c == 0 && t == (uint32_t)s) {
+            m = ceilf(top);
+          } else if (__any_sync(0xffffffffu, top > m + CA_SLACK)) {
+            // the sums so far, and this tile's probabilities before these, to the new reference, by a whole
+            // power of two (the product of the sums is complete: the scores came behind it)
+            const float to = fmaxf(m, ceilf(top)), y = pow2_down(m - to);
+            m = to;
+            l *= y;
+            tmem_wait_st();
+            if (t != (uint32_t)s)
+#pragma unroll 1
+              for (int i = 0; i < DP / 16; ++i) {
+                uint32_t o[16];
+                tmem_ld16(lane_base + Cfg::O(s) + 16 * i, o);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * y);
+                tmem_st16(lane_base + Cfg::O(s) + 16 * i, o);
+              }
+#pragma unroll 1
+            for (int i = 0; i < c; ++i) {
+              uint32_t o[16];
+              const uint32_t y2 = half2_of(y, y);
+              tmem_ld16(lane_base + Cfg::P(s, 2 * i), o);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) o[e] = mul2(o[e], y2);
+              tmem_st16(lane_base + Cfg::P(s, 2 * i), o);
+            }
+          }
+          const float base = CA_UP - (m == -INFINITY ? 0.f : m);
+          float sum[2] = {0.f, 0.f};
+          uint32_t p[16];
+#pragma unroll
+          for (int e = 0; e < 32; e += 2) {
+            const float p0 = ex2(fmaf(__uint_as_float(x[e]), f, base)), p1 = ex2(fmaf(__uint_as_float(x[e + 1]), f, base));
+            sum[0] += p0;
+            sum[1] += p1;
+            p[e / 2] = half2_of(p0, p1);
+          }
+          l += sum[0] + sum[1];
+          if (HALF && c < 3) {
+            tmem_wait_ld();
+            pin(xs[HALF ? (c + 1) & 1 : 0]);
+          }
+          tmem_st16(lane_base + Cfg::P(s, 2 * c), p);
+        }
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
@@ -464,7 +468,7 @@ __global__ void __launch_bounds__((CtCfg<DP, HALF>::THREADS), 1) cache_attention
       const float M = fmaxf(fmaxf(z0.x, z1.x), -FLT_MAX);
       const float f0 = ex2(z0.x - M), f1 = here > 1 ? ex2(z1.x - M) : 0.f, L = z0.y * f0 + z1.y * f1;
       const bool complete = tile0 == 0 && tile1 == at.tiles;
-      const uint32_t s0 = first + done - tile1, team0 = s0 / per, team1 = (s0 + at.tiles - 1) / per;
+      const uint32_t s0 = first + done - tile1;
       const int head = blockIdx.x % a.team;
       auto part = [&](uint32_t team) { return 2 * ((size_t)team * a.team + head) + (team * per < s0); };
       const size_t place = part(blockIdx.x / a.team) * CT_ROWS + row;
@@ -537,57 +541,6 @@ __global__ void __launch_bounds__((CtCfg<DP, HALF>::THREADS), 1) cache_attention
         if (complete) ca_write_row(a, at.n, tok, hq, M, L);
         else a.ml[place] = make_float2(M, L);
       }
-      if (!complete) {
-        named_bar(3, Cfg::SOFT);
-        if (tid == 0) {
-          __threadfence();
-          uint32_t* left = a.left + part(team0);
-          joins = atomicAdd(left, 1u) == team1 - team0;
-          if (joins) *left = 0;
-          __threadfence();
-        }
-        named_bar(3, Cfg::SOFT);
-        if (joins)
-          for (int i0 = warp * 4; i0 < tile_rows; i0 += 4 * (Cfg::SOFT / 32)) {  // four rows a warp, a part of each at a time
-            float jm[4], jl[4];
-            float4 y[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              jm[j] = -FLT_MAX;
-              jl[j] = 0.f;
-              y[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-            }
-#pragma unroll 1
-            for (uint32_t team = team0; team <= team1; ++team) {
-              const size_t at_part = part(team) * CT_ROWS;
-              float2 z[4];
-              float4 v[4];
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                const int i = min(i0 + j, tile_rows - 1);
-                z[j] = __ldcg(&a.ml[at_part + i]);
-                v[j] = lane < DP / 4 ? __ldcg(reinterpret_cast<const float4*>(a.po + (at_part + i) * DP + lane * 4))
-                                     : make_float4(0.f, 0.f, 0.f, 0.f);
-              }
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                const float to = fmaxf(jm[j], z[j].x), x0 = ex2(jm[j] - to), x1 = ex2(z[j].x - to);
-                jm[j] = to;
-                jl[j] = jl[j] * x0 + z[j].y * x1;
-                y[j].x = y[j].x * x0 + v[j].x * x1;
-                y[j].y = y[j].y * x0 + v[j].y * x1;
-                y[j].z = y[j].z * x0 + v[j].z * x1;
-                y[j].w = y[j].w * x0 + v[j].w * x1;
-              }
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              if (i0 + j < tile_rows) {
-                const int rr = at.rb * CT_ROWS + i0 + j, t = rr / a.rep;
-                ca_write<E>(a, at.n, t, at.h * a.rep + (rr - t * a.rep), jm[j], jl[j], y[j], lane);
-              }
-          }
-      }
       tc_fence_before();
       named_bar(2, Cfg::SOFT + 32);
       tc_fence_after();
@@ -603,13 +556,72 @@ __global__ void __launch_bounds__((CtCfg<DP, HALF>::THREADS), 1) cache_attention
   }
 }
 
+// The items that several CTAs have parts of, in a launch of its own: up to 128 rows of 512 bytes a part are too much
+// for the last CTA alone (one sequence of 8,192 keys, 64 rows, 16 parts: 51 us). A block has 16 rows of the item at a
+// border between two teams' parts of the list, if that is the item's first; a warp four of them.
+template <int DP>
+__global__ void __launch_bounds__(128) cache_attention_tc_join_kernel(const CaArgs a, int pieces) {
+  pdl_wait();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const uint32_t id = blockIdx.x / pieces, border = id / a.team;
+  const int head = id - border * a.team, rows = a.T * a.rep;
+  const uint32_t teams = gridDim.x / pieces / a.team + 1;
+  CaCursor<CT_KEYS> at;
+  uint32_t per;
+  const uint32_t total = ca_locate<CT_KEYS>(a, a.blocks, teams, [&](uint32_t p) { return (border + 1) * p; }, &at, &per);
+  const uint32_t x = (border + 1) * per, s0 = x - at.tile;
+  if (x >= total || at.tile == 0 || s0 / per != border) return;
+  const uint32_t last = (s0 + at.tiles - 1) / per;
+  const int i0 = (blockIdx.x - id * pieces) * 16 + warp * 4, tile_rows = min(CT_ROWS, rows - at.rb * CT_ROWS);
+  if (i0 >= tile_rows) return;
+  float m[4], l[4];
+  float4 y[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    m[j] = -FLT_MAX;
+    l[j] = 0.f;
+    y[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+#pragma unroll 2
+  for (uint32_t team = border; team <= last; ++team) {
+    const size_t part = (2 * ((size_t)team * a.team + head) + (team * per < s0)) * CT_ROWS;
+    float2 z[4];
+    float4 v[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const size_t i = part + min(i0 + j, tile_rows - 1);
+      z[j] = a.ml[i];
+      v[j] = lane < DP / 4 ? *reinterpret_cast<const float4*>(a.po + i * DP + lane * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float to = fmaxf(m[j], z[j].x), x0 = ex2(m[j] - to), x1 = ex2(z[j].x - to);
+      m[j] = to;
+      l[j] = l[j] * x0 + z[j].y * x1;
+      y[j].x = y[j].x * x0 + v[j].x * x1;
+      y[j].y = y[j].y * x0 + v[j].y * x1;
+      y[j].z = y[j].z * x0 + v[j].z * x1;
+      y[j].w = y[j].w * x0 + v[j].w * x1;
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (i0 + j < tile_rows) {
+      const int r = at.rb * CT_ROWS + i0 + j, t = r / a.rep;
+      ca_write<__nv_bfloat16>(a, at.n, t, (at.h + head) * a.rep + (r - t * a.rep), m[j], l[j], y[j], lane);
+    }
+}
+
 template <int DP, int DIM, bool HALF>
 lilicorr_status_t launch_tc(const CaArgs& a, const CaPlan& p, cudaStream_t st) {
   using Cfg = CtCfg<DP, HALF>;
   static bool configured[64] = {false};
   auto* kernel = cache_attention_tc_kernel<DP, DIM, HALF>;
   LL_TRY(allow_max_dynamic_smem(kernel, configured));
-  return launch_k(kernel, (unsigned)p.ctas, Cfg::THREADS, Cfg::SMEM, st, a);
+  LL_TRY(launch_k(kernel, (unsigned)p.ctas, Cfg::THREADS, Cfg::SMEM, st, a));
+  if (p.ctas <= a.team) return LILICORR_OK;
+  const int pieces = (min(CT_ROWS, a.T * a.rep) + 15) / 16;
+  return launch_k(cache_attention_tc_join_kernel<DP>, (unsigned)((p.ctas - a.team) * pieces), 128, 0, st, a, pieces);
 }
 template <int DP, int DIM>
 lilicorr_status_t launch_rows(const CaArgs& a, const CaPlan& p, cudaStream_t st) {
