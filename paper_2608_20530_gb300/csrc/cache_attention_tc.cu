@@ -557,10 +557,11 @@ __global__ void __launch_bounds__((CtCfg<DP, HALF>::THREADS), 1) cache_attention
 }
 
 // The items that several CTAs have parts of, in a launch of its own: up to 128 rows of 512 bytes a part are too much
-// for the last CTA alone (one sequence of 8,192 keys, 64 rows, 16 parts: 51 us). A block has 16 rows of the item at a
-// border between two teams' parts of the list, if that is the item's first; a warp four of them.
+// for the last CTA alone. A block has CJ_ROWS rows, a warp each, of the item at a border between two teams' parts of
+// the list, if that is the item's first border.
+constexpr int CJ_ROWS = 8;
 template <int DP>
-__global__ void __launch_bounds__(128) cache_attention_tc_join_kernel(const CaArgs a, int pieces) {
+__global__ void __launch_bounds__(32 * CJ_ROWS) cache_attention_tc_join_kernel(const CaArgs a, int pieces) {
   pdl_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const uint32_t id = blockIdx.x / pieces, border = id / a.team;
@@ -572,44 +573,42 @@ __global__ void __launch_bounds__(128) cache_attention_tc_join_kernel(const CaAr
   const uint32_t x = (border + 1) * per, s0 = x - at.tile;
   if (x >= total || at.tile == 0 || s0 / per != border) return;
   const uint32_t last = (s0 + at.tiles - 1) / per;
-  const int i0 = (blockIdx.x - id * pieces) * 16 + warp * 4, tile_rows = min(CT_ROWS, rows - at.rb * CT_ROWS);
-  if (i0 >= tile_rows) return;
-  float m[4], l[4];
-  float4 y[4];
+  const int i = (blockIdx.x - id * pieces) * CJ_ROWS + warp, r = at.rb * CT_ROWS + i;
+  if (i >= CT_ROWS || r >= rows) return;
+  auto part = [&](uint32_t team) { return (2 * ((size_t)team * a.team + head) + (team * per < s0)) * CT_ROWS + i; };
+  float M = -FLT_MAX, L = 0.f;
+  float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (uint32_t t0 = border; t0 <= last; t0 += 32) { // 32 parts: their references, then their sums, all asked for at once
+    const int parts = min(32u, last - t0 + 1);
+    const float2 z = lane < parts ? a.ml[part(t0 + lane)] : make_float2(-FLT_MAX, 0.f);
+    float4 v[8];
+    auto ask = [&](int j) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    m[j] = -FLT_MAX;
-    l[j] = 0.f;
-    y[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int k = 0; k < 8; ++k)
+        if (j + k < parts && lane < DP / 4)
+          v[k] = *reinterpret_cast<const float4*>(a.po + part(t0 + j + k) * DP + lane * 4);
+    };
+    ask(0);
+    const float to = fmaxf(M, warp_max(z.x)), x0 = ex2(M - to), f = ex2(z.x - to);
+    M = to;
+    L = L * x0 + warp_sum(f * z.y);
+    y.x *= x0; y.y *= x0; y.z *= x0; y.w *= x0;
+    for (int j = 0; j < parts; j += 8) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float g = __shfl_sync(0xffffffffu, f, (j + k) & 31);
+        if (j + k < parts && lane < DP / 4) {
+          y.x = fmaf(g, v[k].x, y.x);
+          y.y = fmaf(g, v[k].y, y.y);
+          y.z = fmaf(g, v[k].z, y.z);
+          y.w = fmaf(g, v[k].w, y.w);
+        }
+      }
+      ask(j + 8);
+    }
   }
-#pragma unroll 2
-  for (uint32_t team = border; team <= last; ++team) {
-    const size_t part = (2 * ((size_t)team * a.team + head) + (team * per < s0)) * CT_ROWS;
-    float2 z[4];
-    float4 v[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const size_t i = part + min(i0 + j, tile_rows - 1);
-      z[j] = a.ml[i];
-      v[j] = lane < DP / 4 ? *reinterpret_cast<const float4*>(a.po + i * DP + lane * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float to = fmaxf(m[j], z[j].x), x0 = ex2(m[j] - to), x1 = ex2(z[j].x - to);
-      m[j] = to;
-      l[j] = l[j] * x0 + z[j].y * x1;
-      y[j].x = y[j].x * x0 + v[j].x * x1;
-      y[j].y = y[j].y * x0 + v[j].y * x1;
-      y[j].z = y[j].z * x0 + v[j].z * x1;
-      y[j].w = y[j].w * x0 + v[j].w * x1;
-    }
-  }
-#pragma unroll
-  for (int j = 0; j < 4; ++j)
-    if (i0 + j < tile_rows) {
-      const int r = at.rb * CT_ROWS + i0 + j, t = r / a.rep;
-      ca_write<__nv_bfloat16>(a, at.n, t, (at.h + head) * a.rep + (r - t * a.rep), m[j], l[j], y[j], lane);
-    }
+  const int t = r / a.rep;
+  ca_write<__nv_bfloat16>(a, at.n, t, (at.h + head) * a.rep + (r - t * a.rep), M, L, y, lane);
 }
 
 template <int DP, int DIM, bool HALF>
@@ -620,8 +619,9 @@ lilicorr_status_t launch_tc(const CaArgs& a, const CaPlan& p, cudaStream_t st) {
   LL_TRY(allow_max_dynamic_smem(kernel, configured));
   LL_TRY(launch_k(kernel, (unsigned)p.ctas, Cfg::THREADS, Cfg::SMEM, st, a));
   if (p.ctas <= a.team) return LILICORR_OK;
-  const int pieces = (min(CT_ROWS, a.T * a.rep) + 15) / 16;
-  return launch_k(cache_attention_tc_join_kernel<DP>, (unsigned)((p.ctas - a.team) * pieces), 128, 0, st, a, pieces);
+  const int pieces = (min(CT_ROWS, a.T * a.rep) + CJ_ROWS - 1) / CJ_ROWS;
+  return launch_k(cache_attention_tc_join_kernel<DP>, (unsigned)((p.ctas - a.team) * pieces),
+                  32 * CJ_ROWS, 0, st, a, pieces);
 }
 template <int DP, int DIM>
 lilicorr_status_t launch_rows(const CaArgs& a, const CaPlan& p, cudaStream_t st) {
