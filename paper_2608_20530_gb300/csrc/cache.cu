@@ -434,8 +434,10 @@ __global__ void __launch_bounds__(EV_THREADS, 2) cache_evict_kernel(const EvictA
     const int p0 = split ? min((int64_t)L, (int64_t)rank * chunk) : 0, p1 = min((int64_t)L, (int64_t)p0 + chunk);
     const int lo = a.first, hi = L - a.recent, c0 = max(p0, lo), c1 = min(p1, hi);
     const bool cached = chunk <= EV_KEYS;
-    if (cached)
+    if (cached) {                                    // (eight loads under way at a time)
+#pragma unroll 8
       for (int i = p0 + tid; i < p1; i += EV_THREADS) x.keys[i - p0] = weight_key(w[i]);
+    }
     auto key = [&](int i) { return cached ? x.keys[i - p0] : weight_key(w[i]); };
     // Larger weights first, then lower positions: the order of weight << 32 | ~position.
     auto order = [&](int i) { return (uint64_t)key(i) << 32 | (uint32_t)~i; };
@@ -458,6 +460,7 @@ __global__ void __launch_bounds__(EV_THREADS, 2) cache_evict_kernel(const EvictA
         const int shift = 64 - 11 * (round + 1) > 0 ? 64 - 11 * (round + 1) : 0;
         const uint64_t known = round == 0 ? 0ull : ~0ull << (64 - 11 * round);
         const uint32_t digits = shift ? 2047 : (1 << (64 - 55)) - 1;
+#pragma unroll 4
         for (int i = c0 + tid; i < c1; i += EV_THREADS) {
           const uint64_t k = order(i);
           if (((k ^ border) & known) == 0)
@@ -537,6 +540,7 @@ __global__ void __launch_bounds__(EV_THREADS, 2) cache_evict_kernel(const EvictA
     int places = 0;                          // before this stretch
     if (split) {
       int m = 0;
+#pragma unroll 4
       for (int i = p0 + tid; i < p1; i += EV_THREADS) m += stays(i);
       m = block_sum(m, x.warp);
       if (tid == 0) x.total = m;

@@ -773,6 +773,18 @@ __global__ void __launch_bounds__(256) cache_attention_spread_kernel(const CaArg
   const int nh = blockIdx.x / pieces, k0 = (blockIdx.x - nh * pieces) * CS_KEYS;
   const int n = nh / a.c.H, h = nh - n * a.c.H, rows = a.T * a.rep, len = cache_len(a.seq_len[n], a.c.S);
   if (k0 >= len) return;
+  const size_t base = ((size_t)n * a.c.H + h) * a.c.S;
+  constexpr int PER = CS_KEYS / 256;
+  float w[PER];
+  float2 s[PER];                                     // the first two rows' products: asked for before the rows' sums
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int k = k0 + i * 256 + threadIdx.x;
+    if (k < len) {
+      w[i] = a.weights[base + k];
+      s[i] = __ldcs(reinterpret_cast<const float2*>(a.scores + (base + k) * a.pad));
+    }
+  }
   if (threadIdx.x < a.pad) {
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
     if (threadIdx.x < rows) {
@@ -787,26 +799,27 @@ __global__ void __launch_bounds__(256) cache_attention_spread_kernel(const CaArg
     row[threadIdx.x] = x;
   }
   __syncthreads();
-  const size_t base = ((size_t)n * a.c.H + h) * a.c.S;
 #pragma unroll
-  for (int i = 0; i < CS_KEYS / 256; ++i) {
+  for (int i = 0; i < PER; ++i) {
     const int k = k0 + i * 256 + threadIdx.x;
     if (k >= len) break;
     float sum = 0.f;
     for (int r = 0; r < a.pad; r += 2) {
-      const float2 s = __ldcs(reinterpret_cast<const float2*>(a.scores + (base + k) * a.pad + r));
+      float2 next = s[i];
+      if (r + 2 < a.pad) next = __ldcs(reinterpret_cast<const float2*>(a.scores + (base + k) * a.pad + r + 2));
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const float4 x = row[r + e];
-        const float v = e ? s.y : s.x;
+        const float v = e ? s[i].y : s[i].x;
         if (x.y > 0.f && v > -INFINITY) {            // (a row that may not see the key has -infinity there)
           float t = x.x;
           if (PIECES > 1) t = fmaf(v, x.w, t);
           sum = fmaf(ex2(fmaf(v, x.z, t)), x.y, sum);
         }
       }
+      s[i] = next;
     }
-    a.weights[base + k] += sum;
+    a.weights[base + k] = w[i] + sum;
   }
 }
 
