@@ -68,6 +68,25 @@ __device__ __forceinline__ bool elect_one() {        // one lane of a converged 
   asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(r));
   return r != 0;
 }
+// packed fp32 pairs: one instruction for both halves
+__device__ __forceinline__ uint64_t pair_of(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void halves(uint64_t v, float& lo, float& hi) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t add_pairs(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
 // Nothing that uses these registers moves above this point (a load from tensor memory fills them until its wait).
 __device__ __forceinline__ void pin(uint32_t (&r)[32]) {
 #pragma unroll
@@ -79,19 +98,11 @@ __device__ __forceinline__ void pin(uint32_t (&r)[32]) {
 __device__ __forceinline__ float pow2_down(float d) {
   return d < -126.f ? 0.f : __int_as_float((127 + (int)d) << 23);
 }
-// A wait for a phase that lets the warp sleep meanwhile (others of its scheduler work).
-__device__ __forceinline__ bool sleep_wait(uint64_t* bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n selp.u32 %0, 1, 0, p;\n}"
-      : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity), "r"(20000) : "memory");
-  return ok != 0;
-}
 // A wait that did not end at once: false after `limit` SM cycles, or when another warp gave up.
 __device__ __noinline__ bool wait_long(uint64_t* bar, uint32_t parity, long long limit,
                                        volatile int* abort_flag) {
   const long long t0 = clock64();
-  while (!sleep_wait(bar, parity)) {
+  while (!mbar_try_wait(bar, parity)) {
     if (*abort_flag) return false;
     if (clock64() - t0 > limit) {
       *abort_flag = 1;
@@ -101,32 +112,41 @@ __device__ __noinline__ bool wait_long(uint64_t* bar, uint32_t parity, long long
   return true;
 }
 
+// shared memory by its address (which ring a pointer is in is not known where it is compiled)
+__device__ __forceinline__ uint2 lds8(uint32_t at) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ void sts16(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+
 // Half a record at `rec` (or zeros) as row `key` of a tile: DP columns of fp16, zeros past the head's width.
 template <int DP, int DIM>
-__device__ __forceinline__ void expand(const unsigned char* rec, bool there, int d, uint8_t* tile, int key) {
+__device__ __forceinline__ void expand(uint32_t rec, bool there, int d, uint32_t tile, int key) {
   // Everything is read first: the place may be given back while it is expanded. Records of 144 bytes start at every
   // second pair of banks, so keys of the upper half of 16 read their groups in another order than the lower.
   const int turn = DIM ? key >> 3 & 1 : 0;
-  uint2 w[DP / 16], b = *reinterpret_cast<const uint2*>(rec + d / 2);
+  uint2 w[DP / 16], b = lds8(rec + d / 2);
 #pragma unroll
   for (int g = 0; g < DP / 16; ++g) {
     w[g] = make_uint2(0, 0);
-    if (DIM || g * 16 < d) w[g] = *reinterpret_cast<const uint2*>(rec + (g ^ turn) * 8);
+    if (DIM || g * 16 < d) w[g] = lds8(rec + (g ^ turn) * 8);
   }
   // scales of 0 where there is no key (codes are finite whatever they are), or no such group
   if (!there) b = make_uint2(0, 0);
-  uint8_t* row = tile + key * 128;
-  const int x = key & 7;
+  const uint32_t row = tile + key * 128, x = key & 7;
 #pragma unroll
   for (int g = 0; g < DP / 16; ++g) {
     const uint32_t two = __byte_perm(b.x, b.y, ((g & 7) ^ turn) * 0x11), f = scales(DIM || g * 16 < d ? two : 0u);
     uint32_t r[4];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const int p = 2 * (g ^ turn) + i;
+      const uint32_t p = 2 * (g ^ turn) + i;
       codes(i ? w[g].y : w[g].x, r);
-      *reinterpret_cast<uint4*>(row + (2 * g + i >> 3) * CT_CHUNK + (((p & 7) ^ x) << 4)) =
-          make_uint4(mul2(r[0], f), mul2(r[1], f), mul2(r[2], f), mul2(r[3], f));
+      sts16(row + (2 * g + i >> 3) * CT_CHUNK + (((p & 7) ^ x) << 4), mul2(r[0], f), mul2(r[1], f), mul2(r[2], f),
+            mul2(r[3], f));
     }
   }
 }
@@ -174,7 +194,7 @@ __global__ void __launch_bounds__((CtCfg<DP, HALF>::THREADS), 1) cache_attention
   tc_fence_after();
   const uint32_t tmem = tmem_base;
   auto wait = [&](uint64_t* bar, uint32_t parity) {  // for a whole warp: all lanes go on, or none
-    if (__all_sync(0xffffffffu, sleep_wait(bar, parity))) return true;
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
     return __all_sync(0xffffffffu, wait_long(bar, parity, a.wait_limit, &abort_flag)) != 0;
   };
   uint32_t done = 0;                                 // tiles of the list behind this warp
@@ -222,7 +242,8 @@ __global__ void __launch_bounds__((CtCfg<DP, HALF>::THREADS), 1) cache_attention
     const int x = tid - 32 * Cfg::FIRST, key = x & 127, is_v = x >> 7;
     uint64_t* full = is_v ? v_full : k_full;
     uint64_t* empty = is_v ? v_empty : k_empty;
-    uint8_t* ring = is_v ? sV : sK;
+    const uint32_t ring = smem_u32(is_v ? sV : sK);
+    const uint32_t source = smem_u32(sR) + key * R + is_v * cache_half_bytes(d);
     uint32_t slot = 0, parity = 1, raw = 0, raw_parity = 0;
     bool ok = a.test_starve != is_v + 1;
     while (done < count && ok) {
@@ -231,8 +252,7 @@ __global__ void __launch_bounds__((CtCfg<DP, HALF>::THREADS), 1) cache_attention
       for (; at.tile < tile1 && ok; ++at.tile) {
         ok = wait(&r_full[raw], raw_parity) && wait(&empty[slot], parity);
         if (!ok) break;
-        const unsigned char* rec = sR + raw * Cfg::RAW + key * R + is_v * cache_half_bytes(d);
-        expand<DP, DIM>(rec, at.tile * CT_KEYS + key < at.len, d, ring + slot * Cfg::TILE, key);
+        expand<DP, DIM>(source + raw * Cfg::RAW, at.tile * CT_KEYS + key < at.len, d, ring + slot * Cfg::TILE, key);
         fence_async_shared();
         __syncwarp();
         if (lane == 0) {
@@ -349,7 +369,7 @@ __global__ void __launch_bounds__((CtCfg<DP, HALF>::THREADS), 1) cache_attention
 #pragma unroll
           for (int i = 0; i < 4; ++i)
             w[i] = half2_of(__uint_as_float(w[i] << 16) * by, __uint_as_float(w[i] & 0xFFFF0000u) * by);
-          *reinterpret_cast<uint4*>(sQ + (p >> 3) * CT_CHUNK + swz(HALF ? s * 64 + row : row, p & 7)) = make_uint4(w[0], w[1], w[2], w[3]);
+          sts16(smem_u32(sQ) + (p >> 3) * CT_CHUNK + swz(HALF ? s * 64 + row : row, p & 7), w[0], w[1], w[2], w[3]);
         }
         const float factor = row_factor(a, up);
         if (s == 0) s_factor[row] = factor;
@@ -384,71 +404,77 @@ __global__ void __launch_bounds__((CtCfg<DP, HALF>::THREADS), 1) cache_attention
           }
           tmem_wait_st();
         }
-        uint32_t xs[HALF ? 2 : 1][32];               // HALF: the next ones are read while these are worked on
-        tmem_ld32(lane_base + Cfg::S(s), xs[0]);
+        // 32 scores at a time; HALF: the next ones are read while these are worked on
+        uint32_t xs[HALF ? 2 : 1][32];
+        auto scores = [&](int c) -> uint32_t (&)[32] {
+          if (HALF) {
+            if (c == 0) tmem_ld32_nowait(lane_base + Cfg::S(s), xs[0]);
+            tmem_wait_ld();
+            pin(xs[HALF ? c & 1 : 0]);
+            if (c < 3) tmem_ld32_nowait(lane_base + Cfg::S(s) + 32 * (c + 1), xs[HALF ? (c + 1) & 1 : 0]);
+          } else {
+            tmem_ld32(lane_base + Cfg::S(s) + 32 * c, xs[0]);
+          }
+          return xs[HALF ? c & 1 : 0];
+        };
+        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {                // 32 scores at a time, a step of the reference each
-          if (HALF && c < 3) tmem_ld32_nowait(lane_base + Cfg::S(s) + 32 * (c + 1), xs[HALF ? (c + 1) & 1 : 0]);
-          if (!HALF && c > 0) tmem_ld32(lane_base + Cfg::S(s) + 32 * c, xs[0]);
-          uint32_t (&x)[32] = xs[HALF ? c & 1 : 0];
+        for (int c = 0; c < 4; ++c) {
+          uint32_t (&x)[32] = scores(c);
           if (a.scores && mine) {                    // for what each key gets: 32 rows of a key side by side
             float* to = a.scores + (((size_t)at.n * a.c.H + at.h) * a.c.S + k0 + 32 * c) * a.pad + r;
 #pragma unroll
             for (int e = 0; e < 32; ++e)
               if (k0 + 32 * c + e < at.len) to[(size_t)e * a.pad] = __uint_as_float(x[e]);
           }
-          float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-          for (int e = 0; e < 32; e += 4) {
-            mx[0] = fmaxf(fmaxf(mx[0], __uint_as_float(x[e])), __uint_as_float(x[e + 1]));
-            mx[1] = fmaxf(fmaxf(mx[1], __uint_as_float(x[e + 2])), __uint_as_float(x[e + 3]));
-          }
-          const float top = fmaxf(mx[0], mx[1]) * f;
-          if (c == 0 && t == (uint32_t)s) {
-            m = ceilf(top);
-          } else if (__any_sync(0xffffffffu, top > m + CA_SLACK)) {
-            // the sums so far, and this tile's probabilities before these, to the new reference, by a whole
-            // power of two (the product of the sums is complete: the scores came behind it)
-            const float to = fmaxf(m, ceilf(top)), y = pow2_down(m - to);
-            m = to;
-            l *= y;
-            tmem_wait_st();
-            if (t != (uint32_t)s)
+          for (int e = 0; e < 32; e += 8)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              mx[i] = fmaxf(fmaxf(mx[i], __uint_as_float(x[e + i])), __uint_as_float(x[e + 4 + i]));
+        }
+        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * f;
+        if (t == (uint32_t)s) {
+          m = ceilf(top);
+        } else if (__any_sync(0xffffffffu, top > m + CA_SLACK)) {
+          // the sums so far to the new reference, by a whole power of two (their product is complete: the
+          // scores came behind it)
+          const float to = fmaxf(m, ceilf(top)), y = pow2_down(m - to);
+          m = to;
+          l *= y;
 #pragma unroll 1
-              for (int i = 0; i < DP / 16; ++i) {
-                uint32_t o[16];
-                tmem_ld16(lane_base + Cfg::O(s) + 16 * i, o);
+          for (int i = 0; i < DP / 16; ++i) {
+            uint32_t o[16];
+            tmem_ld16(lane_base + Cfg::O(s) + 16 * i, o);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * y);
-                tmem_st16(lane_base + Cfg::O(s) + 16 * i, o);
-              }
-#pragma unroll 1
-            for (int i = 0; i < c; ++i) {
-              uint32_t o[16];
-              const uint32_t y2 = half2_of(y, y);
-              tmem_ld16(lane_base + Cfg::P(s, 2 * i), o);
-#pragma unroll
-              for (int e = 0; e < 16; ++e) o[e] = mul2(o[e], y2);
-              tmem_st16(lane_base + Cfg::P(s, 2 * i), o);
-            }
+            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * y);
+            tmem_st16(lane_base + Cfg::O(s) + 16 * i, o);
           }
-          const float base = CA_UP - (m == -INFINITY ? 0.f : m);
-          float sum[2] = {0.f, 0.f};
+        }
+        // once more, for the probabilities: no branch in this pass, so that one's exponentials run beside
+        // another's reads and writes
+        const uint64_t f2 = pair_of(f, f);
+        const float base = CA_UP - (m == -INFINITY ? 0.f : m);
+        const uint64_t base2 = pair_of(base, base);
+        uint64_t sum[2] = {0ull, 0ull};
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          uint32_t (&x)[32] = scores(c);
           uint32_t p[16];
 #pragma unroll
-          for (int e = 0; e < 32; e += 2) {
-            const float p0 = ex2(fmaf(__uint_as_float(x[e]), f, base)), p1 = ex2(fmaf(__uint_as_float(x[e + 1]), f, base));
-            sum[0] += p0;
-            sum[1] += p1;
-            p[e / 2] = half2_of(p0, p1);
-          }
-          l += sum[0] + sum[1];
-          if (HALF && c < 3) {
-            tmem_wait_ld();
-            pin(xs[HALF ? (c + 1) & 1 : 0]);
+          for (int e = 0; e < 16; ++e) {
+            float p0, p1;
+            halves(fma_pair(pair_of(__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1])), f2, base2), p0, p1);
+            p0 = ex2(p0);
+            p1 = ex2(p1);
+            sum[e & 1] = add_pairs(sum[e & 1], pair_of(p0, p1));
+            p[e] = half2_of(p0, p1);
           }
           tmem_st16(lane_base + Cfg::P(s, 2 * c), p);
         }
+        float l0, l1;
+        halves(add_pairs(sum[0], sum[1]), l0, l1);
+        l += l0 + l1;
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
