@@ -492,7 +492,8 @@ lilicorr_status_t lilicorr_cache_read(const lilicorr_cache_desc* desc, const voi
  * q_heads a multiple of kv_heads, 0 < scale * k_unit < 2^100. The cache may overlap itself; out may not, nor
  * may out, lse and weights overlap anything else. Products are exact for F32 queries to 2^-33 and for
  * BF16 ones; softmax and sums are fp32. ws: zero-filled once, at least
- * lilicorr_cache_attention_workspace_bytes(desc) bytes (0: unsupported); its first word is the device status. */
+ * lilicorr_cache_attention_workspace_bytes(desc) bytes (0: unsupported; enough with weights and without); one
+ * workspace serves calls of any shapes. Its first word is the device status. */
 typedef struct {
   lilicorr_cache_desc cache;
   int tokens, q_heads;

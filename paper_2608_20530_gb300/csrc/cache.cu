@@ -47,8 +47,8 @@ lilicorr_status_t cache_view(const lilicorr_cache_desc* d, const void* cache, bo
 namespace {
 
 // ------------------------------------------------------------------------------- append and read
-// x / d of whole numbers x < 2^31 by a product: with 2^s >= d and m = ceil(2^(31 + s) / d) below 2^32, m x / 2^(31 + s)
-// exceeds x / d by less than 1 / d (Granlund and Montgomery, 1994).
+// x / d of whole numbers x < 2^31 by a product: with 2^s >= d and m = ceil(2^(31 + s) / d) below 2^32,
+// m x / 2^(31 + s) exceeds x / d by less than 1 / d (Granlund and Montgomery, 1994).
 struct Quotient {
   uint32_t d, m, s;
   void set(uint32_t by) {
@@ -230,8 +230,10 @@ __global__ void __launch_bounds__(256) cache_append_kernel(const CacheView c, co
   CacheGroup x;
   if (!cache_group(c, a, &x) || x.pos < 0 || x.pos >= c.S) return;
   uint32_t u[2][4 * sizeof(E)];
-  group_load(static_cast<const E*>(a.k) + (x.n * a.k_s[0] + x.t * a.k_s[1] + x.h * a.k_s[2] + x.g * 16), a.wide, u[0]);
-  group_load(static_cast<const E*>(a.v) + (x.n * a.v_s[0] + x.t * a.v_s[1] + x.h * a.v_s[2] + x.g * 16), a.wide, u[1]);
+  group_load(static_cast<const E*>(a.k) + (x.n * a.k_s[0] + x.t * a.k_s[1] + x.h * a.k_s[2] + x.g * 16), a.wide,
+             u[0]);
+  group_load(static_cast<const E*>(a.v) + (x.n * a.v_s[0] + x.t * a.v_s[1] + x.h * a.v_s[2] + x.g * 16), a.wide,
+             u[1]);
   unsigned char* rec = c.at(x.n, x.pos, x.h);
 #pragma unroll
   for (int kv = 0; kv < 2; ++kv) {

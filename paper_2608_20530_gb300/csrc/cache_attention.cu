@@ -25,13 +25,21 @@ lilicorr_status_t ca_plan(const lilicorr_cache_attention_desc* d, CaPlan* p) {
   const int rows = d->tokens * (d->q_heads / c.kv_heads);
   p->dp = c.head_dim <= 32 ? 32 : c.head_dim <= 64 ? 64 : 128;
   p->pieces = d->dtype == LILICORR_BF16 ? 1 : 3;
-  p->tc = p->pieces == 1 && (g_ca_path ? g_ca_path == 1 : rows > 32);
-  p->whole = !p->tc && c.capacity <= 512;
+  // More than 32 rows go to the 5th-generation tensor cores, 128 at a time, fewer to mma.sync, where each 16 keys
+  // cost a matrix instruction for every 8 rows: 32 sequences of 8,192 keys, d = 128, 16 rows a kv head 101 us (on
+  // tcgen05 135), 32 rows 147 (141; d = 64 100 and 115), 48 rows 270 (144), 64 rows 275 (148). Few short contexts
+  // stay on mma.sync: 8 of 384 keys, 64 rows 13 us (25), 64 of 256 69 (46).
+  const int64_t small = (int64_t)c.sequences * c.kv_heads * ((rows + 31) / 32);
+  p->tc = p->pieces == 1 && (g_ca_path ? g_ca_path == 1 : rows > 32 && (c.capacity > 512 || small > num_sms()));
   if (p->tc && p->dp < 64) p->dp = 64;
   p->nt = rows <= 8 ? 1 : rows <= 16 || p->pieces > 1 ? 2 : 4;
   const int per_block = p->tc ? 128 : 8 * p->nt;
   p->blocks = (rows + per_block - 1) / per_block;
   p->items = (size_t)c.sequences * c.kv_heads * p->blocks;
+  // An item a CTA where there is little to share out, or where many items balance by themselves: no list to find
+  // one's place in, no parts to join. 64 items of 640 keys 7.4 us (cut evenly 8.8), of 1,024 8.9 (9.0), of
+  // 2,048 13.9 (11.5); 128 items of 2,048 keys 14.0 (15.9), 512 40.5 (44.0), 2,048 130 (133).
+  p->whole = !p->tc && (c.capacity <= 1024 || (c.capacity <= 2048 && p->items >= (size_t)num_sms() * 3 / 4));
   if ((double)p->items * (c.capacity / 128 + 1) >= 2147483648.0) return LILICORR_ERR_SHAPE;
   // the widest team of at most 16: all heads of a position where there are so few
   p->team = 1;
@@ -41,8 +49,9 @@ lilicorr_status_t ca_plan(const lilicorr_cache_attention_desc* d, CaPlan* p) {
   const size_t parts = p->whole ? 0 : (size_t)2 * p->ctas * per_block;
   p->pad = rows <= 16 ? (rows + 1) / 2 * 2 : 0;
   const size_t keys = (size_t)c.sequences * c.kv_heads * c.capacity;
+  // the counts of parts keep their place in every call's layout: nothing else is ever written there
   p->left_off = 256;
-  p->ml_off = p->left_off + align_up(p->whole ? 0 : (size_t)2 * p->ctas * 4, 256);
+  p->ml_off = p->left_off + align_up((size_t)4 * num_sms() * sizeof(uint32_t), 256);
   p->po_off = p->ml_off + align_up(parts * sizeof(float2), 256);
   p->rows_off = p->po_off + parts * p->dp * sizeof(float);
   p->factors_off = p->rows_off + align_up((size_t)all * sizeof(float2), 256);
@@ -50,7 +59,6 @@ lilicorr_status_t ca_plan(const lilicorr_cache_attention_desc* d, CaPlan* p) {
   p->total = p->scores_off + align_up(keys * p->pad * sizeof(float), 256);
   return LILICORR_OK;
 }
-
 
 lilicorr_status_t run_cache_attention(const lilicorr_cache_attention_desc* desc, const void* q,
                                       const void* cache, const int32_t* seq_len, void* out, float* lse,

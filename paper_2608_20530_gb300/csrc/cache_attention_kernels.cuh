@@ -443,217 +443,217 @@ cache_attention_kernel(const CaArgs a) {
   uint32_t done = 0;
   int place = 0;
   while (true) {
-    {                                                // an item begins
+    // an item begins
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const int r = at.rb * ROWS + nt * 8 + g, t = r / a.rep;
-        const E* q = r < rows ? static_cast<const E*>(a.q) + at.n * a.q_s[0] + t * a.q_s[1] +
-                                    (at.h * a.rep + (r - t * a.rep)) * a.q_s[2]
-                              : nullptr;
-        uint32_t qb[PIECES][KS][2];
-        const int up = load_query<DP, PIECES, E>(q, d, c, qb);
-        if constexpr (Sm::QS) {
-          if (warp == 0)
+    for (int nt = 0; nt < NT; ++nt) {
+      const int r = at.rb * ROWS + nt * 8 + g, t = r / a.rep;
+      const E* q = r < rows ? static_cast<const E*>(a.q) + at.n * a.q_s[0] + t * a.q_s[1] +
+                                  (at.h * a.rep + (r - t * a.rep)) * a.q_s[2]
+                            : nullptr;
+      uint32_t qb[PIECES][KS][2];
+      const int up = load_query<DP, PIECES, E>(q, d, c, qb);
+      if constexpr (Sm::QS) {
+        if (warp == 0)
 #pragma unroll
-            for (int p = 0; p < PIECES; ++p)
+          for (int p = 0; p < PIECES; ++p)
 #pragma unroll
-              for (int i = 0; i < KS; ++i)
-                qs[((nt * PIECES + p) * KS + i) * 32 + lane] = make_uint2(qb[p][i][0], qb[p][i][1]);
-        } else {
+            for (int i = 0; i < KS; ++i)
+              qs[((nt * PIECES + p) * KS + i) * 32 + lane] = make_uint2(qb[p][i][0], qb[p][i][1]);
+      } else {
 #pragma unroll
-          for (int i = 0; i < KS; ++i) { qr[0][i][0] = qb[0][i][0]; qr[0][i][1] = qb[0][i][1]; }
-        }
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {                // this lane's columns
-          const int u = __shfl_sync(0xffffffffu, up, (2 * c + e) * 4);
-          f[nt][e] = row_factor(a, u);
-          fr[nt][e] = a.scale_rest * pow2(-u);
-          m[nt][e] = -FLT_MAX;
-          l[nt][e] = 0.f;
-          const int r = at.rb * ROWS + nt * 8 + 2 * c + e, t = r / a.rep;
-          if (a.scores && warp == 0 && g == 0 && r < rows)
-            a.factors[((size_t)at.n * a.T + t) * a.Hq + at.h * a.rep + (r - t * a.rep)] = f[nt][e];
-        }
+        for (int i = 0; i < KS; ++i) { qr[0][i][0] = qb[0][i][0]; qr[0][i][1] = qb[0][i][1]; }
       }
 #pragma unroll
-      for (int i = 0; i < KS; ++i)
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[i][nt][e] = 0.f;
-      if constexpr (Sm::QS) __syncthreads();
+      for (int e = 0; e < 2; ++e) {                // this lane's columns
+        const int u = __shfl_sync(0xffffffffu, up, (2 * c + e) * 4);
+        f[nt][e] = row_factor(a, u);
+        fr[nt][e] = a.scale_rest * pow2(-u);
+        m[nt][e] = -FLT_MAX;
+        l[nt][e] = 0.f;
+        const int r = at.rb * ROWS + nt * 8 + 2 * c + e, t = r / a.rep;
+        if (a.scores && warp == 0 && g == 0 && r < rows)
+          a.factors[((size_t)at.n * a.T + t) * a.Hq + at.h * a.rep + (r - t * a.rep)] = f[nt][e];
+      }
     }
+#pragma unroll
+    for (int i = 0; i < KS; ++i)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[i][nt][e] = 0.f;
+    if constexpr (Sm::QS) __syncthreads();
     // its tiles here, and the first place in the list behind the last of them
     const int tile0 = at.tile, tile1 = min((uint32_t)at.tiles, tile0 + (count - done));
 #pragma unroll 1
     for (int tile = tile0; tile < tile1; ++tile) {
-    copy_wait<ST - 1>();
-    __syncwarp();
-    const unsigned char* rec = stage + place * Sm::STAGE;
+      copy_wait<ST - 1>();
+      __syncwarp();
+      const unsigned char* rec = stage + place * Sm::STAGE;
 
-    // ---- scores
-    float s[SUB][NT][4];
+      // ---- scores
+      float s[SUB][NT][4];
 #pragma unroll
-    for (int u = 0; u < SUB; ++u) {
+      for (int u = 0; u < SUB; ++u) {
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) s[u][nt][0] = s[u][nt][1] = s[u][nt][2] = s[u][nt][3] = 0.f;
-      CaKeyPart<DP> kp;
-      kp.load(rec + (16 * u + key) * R, R, d, c, kmask);
-      auto step = [&](auto is) {
-        constexpr int i = decltype(is)::value;
-        uint32_t ka[2][4];
-        kp.template operands<i>(ka);
+        for (int nt = 0; nt < NT; ++nt) s[u][nt][0] = s[u][nt][1] = s[u][nt][2] = s[u][nt][3] = 0.f;
+        CaKeyPart<DP> kp;
+        kp.load(rec + (16 * u + key) * R, R, d, c, kmask);
+        auto step = [&](auto is) {
+          constexpr int i = decltype(is)::value;
+          uint32_t ka[2][4];
+          kp.template operands<i>(ka);
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+          for (int j = 0; j < 2; ++j)
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int p = PIECES - 1; p >= 0; --p) {  // the smallest parts first
-              if constexpr (Sm::QS) {
-                const uint2 b = qs[((nt * PIECES + p) * KS + 2 * i + j) * 32 + lane];
-                mma(s[u][nt], ka[j], b.x, b.y);
-              } else {
-                mma(s[u][nt], ka[j], qr[p][2 * i + j][0], qr[p][2 * i + j][1]);
+              for (int p = PIECES - 1; p >= 0; --p) {  // the smallest parts first
+                if constexpr (Sm::QS) {
+                  const uint2 b = qs[((nt * PIECES + p) * KS + 2 * i + j) * 32 + lane];
+                  mma(s[u][nt], ka[j], b.x, b.y);
+                } else {
+                  mma(s[u][nt], ka[j], qr[p][2 * i + j][0], qr[p][2 * i + j][1]);
+                }
               }
+        };
+        steps(step, std::make_integer_sequence<int, KS / 2>{});
+      }
+      const int k0 = tile * KEYS + warp * (16 * SUB);
+      if (k0 + 16 * SUB > at.len - (a.T - 1)) {        // some row may not see all of these keys
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int r = at.rb * ROWS + nt * 8 + 2 * c + e;
+            const int seen = at.len - (a.T - 1 - r / a.rep) - k0 - key;
+#pragma unroll
+            for (int u = 0; u < SUB; ++u) {
+              if (16 * u >= seen) s[u][nt][e] = -INFINITY;
+              if (16 * u + 1 >= seen) s[u][nt][e + 2] = -INFINITY;
             }
-      };
-      steps(step, std::make_integer_sequence<int, KS / 2>{});
-    }
-    const int k0 = tile * KEYS + warp * (16 * SUB);
-    if (k0 + 16 * SUB > at.len - (a.T - 1)) {        // some row may not see all of these keys
+          }
+      }
+      if (a.scores) {                                  // for what each key gets
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+          if (nt * 8 + 2 * c < a.pad)
+#pragma unroll
+            for (int u = 0; u < SUB; ++u)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                const int k = k0 + 16 * u + key + e;
+                if (k < at.len)
+                  *reinterpret_cast<float2*>(a.scores + (((size_t)at.n * a.c.H + at.h) * a.c.S + k) * a.pad +
+                                             nt * 8 + 2 * c) = make_float2(s[u][nt][2 * e], s[u][nt][2 * e + 1]);
+              }
+      }
+      // ---- probabilities: the reference moves when some row of the warp's has left it behind
+      float top[NT][2];
+      bool up = false;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const int r = at.rb * ROWS + nt * 8 + 2 * c + e;
-          const int seen = at.len - (a.T - 1 - r / a.rep) - k0 - key;
+          top[nt][e] = fmaxf(s[0][nt][e], s[0][nt][e + 2]);
 #pragma unroll
-          for (int u = 0; u < SUB; ++u) {
-            if (16 * u >= seen) s[u][nt][e] = -INFINITY;
-            if (16 * u + 1 >= seen) s[u][nt][e + 2] = -INFINITY;
-          }
+          for (int u = 1; u < SUB; ++u) top[nt][e] = fmaxf(top[nt][e], fmaxf(s[u][nt][e], s[u][nt][e + 2]));
+          up |= fmaf(top[nt][e], f[nt][e], -m[nt][e]) > CA_SLACK;
         }
-    }
-    if (a.scores) {                                  // for what each key gets
+      if (__any_sync(0xffffffffu, up)) {
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-        if (nt * 8 + 2 * c < a.pad)
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int u = 0; u < SUB; ++u)
+          for (int e = 0; e < 2; ++e) {
+            float t = top[nt][e];
+            t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 4));
+            t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 8));
+            t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 16));
+            const float to = fmaxf(m[nt][e], fmaf(t, f[nt][e], CA_ROOM)), x = ex2(m[nt][e] - to);
+            m[nt][e] = to;
+            l[nt][e] *= x;
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const int k = k0 + 16 * u + key + e;
-              if (k < at.len)
-                *reinterpret_cast<float2*>(a.scores + (((size_t)at.n * a.c.H + at.h) * a.c.S + k) * a.pad +
-                                           nt * 8 + 2 * c) = make_float2(s[u][nt][2 * e], s[u][nt][2 * e + 1]);
+            for (int i = 0; i < KS; ++i) {
+              o[i][nt][e] *= x;
+              o[i][nt][e + 2] *= x;
             }
-    }
-    // ---- probabilities: the reference moves when some row of the warp's has left it behind
-    float top[NT][2];
-    bool up = false;
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        top[nt][e] = fmaxf(s[0][nt][e], s[0][nt][e + 2]);
-#pragma unroll
-        for (int u = 1; u < SUB; ++u) top[nt][e] = fmaxf(top[nt][e], fmaxf(s[u][nt][e], s[u][nt][e + 2]));
-        up |= fmaf(top[nt][e], f[nt][e], -m[nt][e]) > CA_SLACK;
+          }
       }
-    if (__any_sync(0xffffffffu, up)) {
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+      for (int u = 0; u < SUB; ++u) {
+        uint32_t pb[NT][PIECES][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          float p[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float x = CA_UP - m[nt][e & 1];
+            // (a key that is not seen: no infinity times what the factor lacks, which has either sign)
+            if (PIECES > 1) x = fmaf(fmaxf(s[u][nt][e], -FLT_MAX), fr[nt][e & 1], x);
+            p[e] = ex2(fmaf(s[u][nt][e], f[nt][e & 1], x));
+          }
+          l[nt][0] += p[0] + p[2];
+          l[nt][1] += p[1] + p[3];
+#pragma unroll
+          for (int i = 0; i < PIECES; ++i) {
+            const uint32_t x = half2_of(p[0], p[1]), y = half2_of(p[2], p[3]);
+            pb[nt][i][0] = transpose8(x);
+            pb[nt][i][1] = transpose8(y);
+            if (PIECES > 1) {
+              half2_sub(x, p[0], p[1]);
+              half2_sub(y, p[2], p[3]);
+            }
+          }
+        }
+        // ---- sums of p V: two keys a register, so the codes of two records go together, byte by byte
+        const unsigned char* v = rec + 16 * u * R + half;
+        uint32_t fs[2], w[4][DP / 128 < 1 ? 1 : 2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          float t = top[nt][e];
-          t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 4));
-          t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 8));
-          t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 16));
-          const float to = fmaxf(m[nt][e], fmaf(t, f[nt][e], CA_ROOM)), x = ex2(m[nt][e] - to);
-          m[nt][e] = to;
-          l[nt][e] *= x;
-#pragma unroll
-          for (int i = 0; i < KS; ++i) {
-            o[i][nt][e] *= x;
-            o[i][nt][e + 2] *= x;
+          const unsigned char *pa = v + (va + e) * R, *pb2 = v + (vb + e) * R;
+          if constexpr (DP == 128) {
+            const uint2 x = *reinterpret_cast<const uint2*>(pa + vbyte);
+            const uint2 y = *reinterpret_cast<const uint2*>(pb2 + vbyte);
+            w[2 * e][0] = x.x; w[2 * e][1] = x.y;
+            w[2 * e + 1][0] = y.x; w[2 * e + 1][1] = y.y;
+          } else if constexpr (DP == 64) {
+            w[2 * e][0] = *reinterpret_cast<const uint32_t*>(pa + vbyte);
+            w[2 * e + 1][0] = *reinterpret_cast<const uint32_t*>(pb2 + vbyte);
+          } else {
+            w[2 * e][0] = *reinterpret_cast<const uint16_t*>(pa + vbyte);
+            w[2 * e + 1][0] = *reinterpret_cast<const uint16_t*>(pb2 + vbyte);
           }
+          uint32_t b = pa[d / 2 + vg] | (uint32_t)pb2[d / 2 + vg] << 8;
+          if (!vthere) b = 0;
+          fs[e] = scales(b);
         }
-    }
+        auto step = [&](auto is) {
+          constexpr int i = decltype(is)::value;       // four tiles of 16 elements (DP 32: two)
+          constexpr int tiles = KS < 4 ? KS : 4;
+          uint32_t oa[4][4];
 #pragma unroll
-    for (int u = 0; u < SUB; ++u) {
-      uint32_t pb[NT][PIECES][2];
+          for (int e = 0; e < 2; ++e) {
+            const uint32_t x = w[2 * e][i], y = w[2 * e + 1][i];
+            uint32_t even[4], odd[4];
+            codes((x & 0x0F0F0F0Fu) | ((y << 4) & 0xF0F0F0F0u), even);
+            codes(((x >> 4) & 0x0F0F0F0Fu) | (y & 0xF0F0F0F0u), odd);
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        float p[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float x = CA_UP - m[nt][e & 1];
-          // (a key that is not seen: no infinity times what the factor lacks, which has either sign)
-          if (PIECES > 1) x = fmaf(fmaxf(s[u][nt][e], -FLT_MAX), fr[nt][e & 1], x);
-          p[e] = ex2(fmaf(s[u][nt][e], f[nt][e & 1], x));
-        }
-        l[nt][0] += p[0] + p[2];
-        l[nt][1] += p[1] + p[3];
-#pragma unroll
-        for (int i = 0; i < PIECES; ++i) {
-          const uint32_t x = half2_of(p[0], p[1]), y = half2_of(p[2], p[3]);
-          pb[nt][i][0] = transpose8(x);
-          pb[nt][i][1] = transpose8(y);
-          if (PIECES > 1) {
-            half2_sub(x, p[0], p[1]);
-            half2_sub(y, p[2], p[3]);
+            for (int j = 0; j < tiles; ++j) {
+              oa[j][2 * e] = mul2(even[j], fs[e]);
+              oa[j][2 * e + 1] = mul2(odd[j], fs[e]);
+            }
           }
-        }
+#pragma unroll
+          for (int j = 0; j < tiles; ++j)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int p = PIECES - 1; p >= 0; --p) mma(o[4 * i + j][nt], oa[j], pb[nt][p][0], pb[nt][p][1]);
+        };
+        steps(step, std::make_integer_sequence<int, DP == 128 ? 2 : 1>{});
       }
-      // ---- sums of p V: two keys a register, so the codes of two records go together, byte by byte
-      const unsigned char* v = rec + 16 * u * R + half;
-      uint32_t fs[2], w[4][DP / 128 < 1 ? 1 : 2];
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const unsigned char *pa = v + (va + e) * R, *pb2 = v + (vb + e) * R;
-        if constexpr (DP == 128) {
-          const uint2 x = *reinterpret_cast<const uint2*>(pa + vbyte), y = *reinterpret_cast<const uint2*>(pb2 + vbyte);
-          w[2 * e][0] = x.x; w[2 * e][1] = x.y;
-          w[2 * e + 1][0] = y.x; w[2 * e + 1][1] = y.y;
-        } else if constexpr (DP == 64) {
-          w[2 * e][0] = *reinterpret_cast<const uint32_t*>(pa + vbyte);
-          w[2 * e + 1][0] = *reinterpret_cast<const uint32_t*>(pb2 + vbyte);
-        } else {
-          w[2 * e][0] = *reinterpret_cast<const uint16_t*>(pa + vbyte);
-          w[2 * e + 1][0] = *reinterpret_cast<const uint16_t*>(pb2 + vbyte);
-        }
-        uint32_t b = pa[d / 2 + vg] | (uint32_t)pb2[d / 2 + vg] << 8;
-        if (!vthere) b = 0;
-        fs[e] = scales(b);
-      }
-      auto step = [&](auto is) {
-        constexpr int i = decltype(is)::value;       // four tiles of 16 elements (DP 32: two)
-        constexpr int tiles = KS < 4 ? KS : 4;
-        uint32_t oa[4][4];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const uint32_t x = w[2 * e][i], y = w[2 * e + 1][i];
-          uint32_t even[4], odd[4];
-          codes((x & 0x0F0F0F0Fu) | ((y << 4) & 0xF0F0F0F0u), even);
-          codes(((x >> 4) & 0x0F0F0F0Fu) | (y & 0xF0F0F0F0u), odd);
-#pragma unroll
-          for (int j = 0; j < tiles; ++j) {
-            oa[j][2 * e] = mul2(even[j], fs[e]);
-            oa[j][2 * e + 1] = mul2(odd[j], fs[e]);
-          }
-        }
-#pragma unroll
-        for (int j = 0; j < tiles; ++j)
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int p = PIECES - 1; p >= 0; --p) mma(o[4 * i + j][nt], oa[j], pb[nt][p][0], pb[nt][p][1]);
-      };
-      steps(step, std::make_integer_sequence<int, DP == 128 ? 2 : 1>{});
-    }
-    __syncwarp();                                    // the records' place is free
-    copy_next(place);
-    place = place + 1 == ST ? 0 : place + 1;
+      __syncwarp();                                    // the records' place is free
+      copy_next(place);
+      place = place + 1 == ST ? 0 : place + 1;
     }
     done += tile1 - tile0;
 
@@ -701,7 +701,8 @@ cache_attention_kernel(const CaArgs a) {
           const int t = r / a.rep;
           ca_write<E>(a, at.n, t, at.h * a.rep + (r - t * a.rep), M, L, y, lane);
         } else {
-          const size_t part = ((size_t)2 * blockIdx.x + (tile0 == 0 && done > (uint32_t)tile1)) * ROWS + nt * 8 + warp;
+          const size_t part =
+              ((size_t)2 * blockIdx.x + (tile0 == 0 && done > (uint32_t)tile1)) * ROWS + nt * 8 + warp;
           if (lane == 0) a.ml[part] = make_float2(M, L);
           if (lane < DP / 4) *reinterpret_cast<float4*>(a.po + part * DP + lane * 4) = y;
         }
@@ -962,8 +963,8 @@ lilicorr_status_t ca_launch(const CaArgs& a, const CaPlan& p, cudaStream_t st) {
   static bool configured[64] = {false};
   auto* kernel = cache_attention_kernel<DP, DIM, NT, PIECES, E>;
   LL_TRY(allow_max_dynamic_smem(kernel, configured));
-  LL_TRY(launch_k(kernel, p.whole ? (unsigned)p.items : (unsigned)p.ctas, CA_THREADS, CaSmem<DP, NT, PIECES>::TOTAL, st,
-                  a));
+  LL_TRY(launch_k(kernel, p.whole ? (unsigned)p.items : (unsigned)p.ctas, CA_THREADS,
+                  CaSmem<DP, NT, PIECES>::TOTAL, st, a));
   return ca_launch_weights<DP, DIM, NT, PIECES, E>(a, p, st);
 }
 

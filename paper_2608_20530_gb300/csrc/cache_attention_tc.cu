@@ -26,9 +26,9 @@ constexpr uint32_t CT_CHUNK = 128 * 128;             // 128 rows of 128 bytes
 constexpr uint32_t CT_TMEM = 512;
 constexpr int CT_RAW = 3;                            // tiles of records under way
 
-// HALF: blocks of 64 rows or fewer. Q lies in the tile twice, so that scores of all rows lie in tensor memory twice, and
-// each stream has the half whose quarters its warps can read: warps 0 and 1, 2 and 3, a scheduler each, and more
-// registers a thread.
+// HALF: blocks of 64 rows or fewer. Q lies in the tile twice, so that scores of all rows lie in tensor memory twice,
+// and each stream has the half whose quarters its warps can read: warps 0 and 1, 2 and 3, a scheduler each, and
+// more registers a thread (both streams on the first two quarters: 79 us for 63).
 template <int DP, bool HALF>
 struct CtCfg {
   static constexpr int QUARTERS = HALF ? 2 : 4, SOFT = 2 * 32 * QUARTERS;      // warps of a stream; threads of both
@@ -229,7 +229,8 @@ __global__ void __launch_bounds__((CtCfg<DP, HALF>::THREADS), 1) cache_attention
             from += stride - vecs * 16;
           }
         }
-        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&r_full[into])) : "memory");
+        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&r_full[into]))
+                     : "memory");
         src += CT_KEYS * stride;
         if (++into == CT_RAW) { into = 0; parity ^= 1u; }
       }
@@ -275,7 +276,7 @@ __global__ void __launch_bounds__((CtCfg<DP, HALF>::THREADS), 1) cache_attention
     while (done < count) {
       const uint32_t here = min((uint32_t)(at.tiles - at.tile), count - done);
       const int end = at.len - at.tile * CT_KEYS;    // keys from here on
-      named_bar(1, Cfg::SOFT + 32);                    // Q is there
+      named_bar(1, Cfg::SOFT + 32);                  // Q is there
       tc_fence_after();
       bool ok = true;
       auto scores = [&](int s) {
@@ -325,7 +326,7 @@ __global__ void __launch_bounds__((CtCfg<DP, HALF>::THREADS), 1) cache_attention
         sums(s, end - (int)t * CT_KEYS, t < 2, t + 2 >= here);
         if (ok && t + 2 < here) scores(s);
       }
-      named_bar(2, Cfg::SOFT + 32);                    // the item is done with
+      named_bar(2, Cfg::SOFT + 32);                  // the item is done with
       done += here;
       if (done < count) at.next(a, a.blocks);
     }
@@ -505,14 +506,17 @@ __global__ void __launch_bounds__((CtCfg<DP, HALF>::THREADS), 1) cache_attention
           E* out = static_cast<E*>(a.out) + at.n * a.o_s[0] + tok * a.o_s[1] + hq * a.o_s[2] + c * 16;
 #pragma unroll
           for (int e = 0; e < 16; e += 8)
-            *reinterpret_cast<uint4*>(out + e) =
-                L == 0.f ? make_uint4(0, 0, 0, 0)
-                         : make_uint4(bf16_pack2(y[e] * by, y[e + 1] * by), bf16_pack2(y[e + 2] * by, y[e + 3] * by),
-                                      bf16_pack2(y[e + 4] * by, y[e + 5] * by), bf16_pack2(y[e + 6] * by, y[e + 7] * by));
+            if (L == 0.f)
+              *reinterpret_cast<uint4*>(out + e) = make_uint4(0, 0, 0, 0);
+            else
+              *reinterpret_cast<uint4*>(out + e) =
+                  make_uint4(bf16_pack2(y[e] * by, y[e + 1] * by), bf16_pack2(y[e + 2] * by, y[e + 3] * by),
+                             bf16_pack2(y[e + 4] * by, y[e + 5] * by), bf16_pack2(y[e + 6] * by, y[e + 7] * by));
         } else {
           float* po = a.po + place * DP + c * 16;
 #pragma unroll
-          for (int e = 0; e < 16; e += 4) *reinterpret_cast<float4*>(po + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
+          for (int e = 0; e < 16; e += 4)
+            *reinterpret_cast<float4*>(po + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
         }
       };
       if constexpr (HALF) {
@@ -595,7 +599,8 @@ __global__ void __launch_bounds__(32 * CJ_ROWS) cache_attention_tc_join_kernel(c
   const uint32_t teams = gridDim.x / pieces / a.team + 1;
   CaCursor<CT_KEYS> at;
   uint32_t per;
-  const uint32_t total = ca_locate<CT_KEYS>(a, a.blocks, teams, [&](uint32_t p) { return (border + 1) * p; }, &at, &per);
+  const uint32_t total =
+      ca_locate<CT_KEYS>(a, a.blocks, teams, [&](uint32_t p) { return (border + 1) * p; }, &at, &per);
   const uint32_t x = (border + 1) * per, s0 = x - at.tile;
   if (x >= total || at.tile == 0 || s0 / per != border) return;
   const uint32_t last = (s0 + at.tiles - 1) / per;
@@ -604,7 +609,7 @@ __global__ void __launch_bounds__(32 * CJ_ROWS) cache_attention_tc_join_kernel(c
   auto part = [&](uint32_t team) { return (2 * ((size_t)team * a.team + head) + (team * per < s0)) * CT_ROWS + i; };
   float M = -FLT_MAX, L = 0.f;
   float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (uint32_t t0 = border; t0 <= last; t0 += 32) { // 32 parts: their references, then their sums, all asked for at once
+  for (uint32_t t0 = border; t0 <= last; t0 += 32) { // 32 parts: references and sums are all asked for at once
     const int parts = min(32u, last - t0 + 1);
     const float2 z = lane < parts ? a.ml[part(t0 + lane)] : make_float2(-FLT_MAX, 0.f);
     float4 v[8];
