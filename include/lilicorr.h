@@ -490,8 +490,9 @@ lilicorr_status_t lilicorr_cache_read(const lilicorr_cache_desc* desc, const voi
  *   q, out [sequences, tokens, q_heads, head_dim] of dtype, strides in elements, 16-byte aligned; lse
  *   [sequences, tokens, q_heads] fp32
  * q_heads a multiple of kv_heads, 0 < scale * k_unit < 2^100. The cache may overlap itself; out may not, nor
- * may out, lse and weights overlap anything else. Products are exact for F32 queries to 2^-33 and for
- * BF16 ones; softmax and sums are fp32. ws: zero-filled once, at least
+ * may out, lse and weights overlap anything else. Queries enter exactly, to 2^-38 of their row's
+ * largest element, and so do keys and values; softmax and sums are fp32 (BF16: probabilities are rounded to
+ * fp16 once). ws: zero-filled once, at least
  * lilicorr_cache_attention_workspace_bytes(desc) bytes (0: unsupported; enough with weights and without); one
  * workspace serves calls of any shapes. Its first word is the device status. */
 typedef struct {

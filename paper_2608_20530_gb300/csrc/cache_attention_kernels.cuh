@@ -19,9 +19,9 @@ namespace {
 constexpr int CA_WARPS = 8;                  // of a CTA, each with its own keys of a tile
 constexpr int CA_THREADS = 32 * CA_WARPS;
 // Probabilities are 2^(s - m + CA_UP) with the row's reference m. Only where a score is more than CA_SLACK above
-// it does it move, to CA_ROOM above the largest so far, so that few steps have sums to rescale: at most 2^14,
-// and fp16 numbers of full precision down to 2^-16 of the largest.
-constexpr float CA_UP = 6.f, CA_SLACK = 8.f, CA_ROOM = 4.f;
+// it does it move, to CA_ROOM above the largest so far, so that few steps have sums to rescale. The largest is
+// then between 2^6 and 2^15, and fp16 numbers have their full precision down to 2^-20 of it.
+constexpr float CA_UP = 7.f, CA_SLACK = 8.f, CA_ROOM = 1.f;
 
 // The work is the list of all (sequence, team of kv heads, row block, tile of KEYS keys), in that order, cut
 // evenly over the teams of CTAs: team g takes tiles [g * per, (g + 1) * per), each of its CTAs for its own head.
@@ -945,7 +945,7 @@ __global__ void __launch_bounds__(CA_THREADS, NT > 2 ? 1 : 2) cache_attention_we
 // What each key gets, behind the rows' results.
 template <int DP, int DIM, int NT, int PIECES, typename E>
 lilicorr_status_t ca_launch_weights(const CaArgs& a, const CaPlan& p, cudaStream_t st) {
-  if (!a.weights) return LILICORR_OK;
+  if (!a.weights || a.c.S == 0) return LILICORR_OK;
   if (a.scores) {
     const int pieces = (a.c.S + CS_KEYS - 1) / CS_KEYS;
     return launch_k(cache_attention_spread_kernel<PIECES>, (unsigned)(a.c.N * a.c.H * pieces), 256, 0, st, a, pieces);

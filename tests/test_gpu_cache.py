@@ -343,6 +343,55 @@ def test_nan_query_spoils_its_own_row(dtype, T):
     assert bool(((w1.double() - w.double() - want).abs() <= 2.0 ** -14 * want + 2.0 ** -22 * (1 + want)).all())
 
 
+@pytest.mark.parametrize("T", [1, 16])
+def test_one_large_weight_and_very_many_small_ones(T):
+    """Half of a row's weight on one key, the rest on 2^19 others: what the second product's operand loses of each
+    small one it loses of all of them."""
+    ll = _ll()
+    S, d = (1 << 19) + 77, 16
+    c = _empty(1, S, 1, d, fill=0)
+    c[..., d // 2] = 0x38                            # a scale of 1, elements 0
+    c[..., d + 8] = 0x38
+    g = _gen(5)
+    c[..., d // 2 + 8:d + 8] = torch.randint(0, 256, (1, S, 1, d // 2), generator=g, device="cuda").byte()
+    c[0, 12345, 0, 0] = 0x07                         # one key of 6 along the first element
+    q = torch.zeros((1, T, 4, d), device="cuda").bfloat16()
+    q[..., 0] = torch.linspace(2.1, 2.3, 4, device="cuda")     # exp(6 * 2.2) = 2^19
+    lens = _ints([S])
+    w = torch.zeros((1, 1, S), device="cuda")
+    w1 = w.clone()
+    _check(ll.cache_attention(q, c, lens, scale=1.0, weights=w1), q, c, lens, 1.0, w0=w, w=w1)
+
+
+def test_one_workspace_for_calls_of_any_shapes():
+    """Calls that leave other parts of it written, between calls that need their counts at 0."""
+    ll = _ll()
+    shapes = [(1, 1, 16, 1, 128, 9000), (2, 1, 8, 2, 64, 224), (1, 1, 32, 8, 128, 20000), (2, 16, 32, 4, 128, 1025),
+              (33, 1, 4, 1, 64, 257), (6, 1, 12, 4, 32, 2222)]
+    cases = [_case(ll, *s, "bf16", i) for i, s in enumerate(shapes)]
+    ws = ll.Workspace(max(ll.cache_attention_workspace_bytes(q, c) for q, c, _, _ in cases))
+    for _ in range(2):
+        for q, c, lens, w in cases:
+            w1 = w.clone()
+            _check(ll.cache_attention(q, c, lens, weights=w1, ws=ws), q, c, lens, w0=w, w=w1)
+
+
+def test_caches_without_room():
+    """A capacity of 0: nothing is written, rows see nothing, nothing is evicted."""
+    ll = _ll()
+    c, w = _empty(2, 0, 2, 32), torch.zeros((2, 2, 0), device="cuda")
+    lens = _ints([0, 3])
+    k = torch.ones((2, 1, 2, 32), device="cuda").bfloat16()
+    ll.cache_append(c, k, k, lens, weights=w)
+    assert bool((ll.cache_read(c, lens, 1)[0] == 0).all())
+    for T in (1, 40):
+        q = torch.ones((2, T, 4, 32), device="cuda").bfloat16()
+        out, lse = ll.cache_attention(q, c, lens, weights=w)
+        assert bool((out == 0).all()) and bool((lse == -math.inf).all())
+    kept, new = ll.cache_evict(c, w, lens, 3)
+    assert bool((kept == -1).all()) and new.tolist() == [0, 0]
+
+
 def test_shared_and_strided_caches():
     """Every sequence the same cache (a stride of 0), records with space between them, strided q and out."""
     ll = _ll()
@@ -521,12 +570,13 @@ def test_beams_reorder_a_cache():
     assert torch.equal(cache, want)
 
 
-def test_captured_and_replayed():
+@pytest.mark.parametrize("T,Hq,S", [(2, 8, 600), (2, 8, 3000), (16, 16, 1500)])
+def test_captured_and_replayed(T, Hq, S):
     """The four calls in one graph, on another stream, replayed for other contents and lengths."""
     ll = _ll()
-    N, T, H, Hq, d, S, budget = 2, 2, 2, 8, 128, 600, 400
+    N, H, d, budget = 2, 2, 128, 400
     g = _gen(12)
-    lens = _ints([600, 380])
+    lens = _ints([S, 380])
     cache = _filled(ll, g, N, S, H, d, lens)
     k = torch.randn((N, T, H, d), generator=g, device="cuda").bfloat16()
     v, q = torch.randn_like(k), torch.randn((N, T, Hq, d), generator=g, device="cuda").bfloat16()
@@ -548,7 +598,7 @@ def test_captured_and_replayed():
         torch.cuda.synchronize()
         with torch.cuda.graph(graph, stream=side):
             outs = step()
-    for new in ([600, 380], [0, 1], [-1, 599], [401, 2]):
+    for new in ([S, 380], [0, 1], [-1, 599], [401, 2]):
         lens.copy_(_ints(new))
         cache.copy_(start[0])
         w.copy_(start[1])
