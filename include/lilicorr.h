@@ -444,8 +444,8 @@ lilicorr_status_t lilicorr_prefix_attention(const lilicorr_prefix_attention_desc
  * from 2^-60 to 2^60, the same in every call on a cache: 1, unless the values lie far from 1 (a group's
  * scale is a multiple of 2^-9, and a value is cut at 2688 units).
  * A cache is [sequences, capacity, kv_heads] records, 16-byte aligned, the strides in bytes, multiples of 16
- * and not negative (of positions below 2^28). Where it is written no two of its records may overlap. head_dim is a multiple of 16 up
- * to 128, capacity at most 2^30. Sequence n holds the positions below seq_len[n] (int32, on the device),
+ * and not negative (of positions below 2^28). Where it is written no two of its records may overlap.
+ * head_dim is a multiple of 16 up to 128, capacity at most 2^30. Sequence n holds the positions below seq_len[n] (int32, on the device),
  * clipped to [0, capacity]; below 0 there is no such sequence. What lies behind is not looked at.
  * weights [sequences, kv_heads, capacity] fp32, where there are any, hold what attention each key has
  * gathered: appended at 0, added to by lilicorr_cache_attention, read and moved by lilicorr_cache_evict. */
@@ -464,7 +464,7 @@ size_t lilicorr_cache_record_bytes(int head_dim);
  * that is outside [0, capacity). A group of 16 elements x has the scale nearest to max |x| / (6 unit), at
  * least 2^-9 and at most 448, and the codes nearest to x / (scale unit), at most 6 (ties to the even
  * code; infinities are cut). A group with a NaN becomes NaN. The weights of the new positions become 0
- * (NULL: there are none). */
+ * (NULL: there are none). Fewer than 2^31 groups a call. */
 lilicorr_status_t lilicorr_cache_append(const lilicorr_cache_desc* desc, void* cache,
                                         lilicorr_dtype_t dtype, int tokens, const void* k,
                                         const int64_t host_k_stride[3], const void* v,
@@ -489,7 +489,7 @@ lilicorr_status_t lilicorr_cache_read(const lilicorr_cache_desc* desc, const voi
  * (rows whose lse is not finite add nothing).
  *   q, out [sequences, tokens, q_heads, head_dim] of dtype, strides in elements, 16-byte aligned; lse
  *   [sequences, tokens, q_heads] fp32
- * q_heads a multiple of kv_heads, 0 < scale * k_unit < 2^100. The cache may overlap itself; out may not, nor
+ * q_heads a multiple of kv_heads, sequences * tokens * q_heads at most 2^30, 0 < scale * k_unit < 2^100. The cache may overlap itself; out may not, nor
  * may out, lse and weights overlap anything else. Queries enter exactly, to 2^-38 of their row's
  * largest element, and so do keys and values; softmax and sums are fp32 (BF16: probabilities are rounded to
  * fp16 once). ws: zero-filled once, at least
@@ -517,7 +517,7 @@ lilicorr_status_t lilicorr_cache_attention(const lilicorr_cache_attention_desc* 
  *   kept [sequences, kv_heads, budget] int32: the positions that stayed, in order, then -1
  *   new_len [sequences] int32: min(seq_len, budget) (a negative seq_len as it is); not seq_len itself,
  *   which other layers may still need
- * 1 <= budget, first + recent <= budget. The spans of memory of the two caches, and of their weights,
+ * 1 <= budget <= 2^30, first + recent <= budget. The spans of memory of the two caches, and of their weights,
  * must not overlap. */
 lilicorr_status_t lilicorr_cache_evict(const lilicorr_cache_desc* desc, void* cache, float* weights,
                                        const int32_t* seq_len, int budget, int recent, int first,

@@ -672,7 +672,7 @@ lilicorr_status_t run_evict(const lilicorr_cache_desc* desc, void* cache, float*
                             int32_t* kept, int32_t* new_len, cudaStream_t st) {
   LL_TRY(cache_shape(desc));
   if (budget < 1 || recent < 0 || first < 0 || (int64_t)recent + first > budget) return LILICORR_ERR_ARG;
-  if ((double)desc->sequences * desc->kv_heads * budget >= 9e18) return LILICORR_ERR_SHAPE;
+  if (budget > (1 << 30)) return LILICORR_ERR_SHAPE;           // (places are counted in 32 bits)
   EvictArgs a;
   LL_TRY(cache_view(desc, cache, true, &a.from));
   a.to = a.from;
@@ -689,6 +689,8 @@ lilicorr_status_t run_evict(const lilicorr_cache_desc* desc, void* cache, float*
   if (desc->sequences == 0) return LILICORR_OK;
   if (!seq_len || !kept || !new_len || (desc->capacity && !weights) || (into && !into_weights))
     return LILICORR_ERR_ARG;
+  // every head's CTAs read the lengths
+  if (seq_len < new_len + desc->sequences && new_len < seq_len + desc->sequences) return LILICORR_ERR_ARG;
   if (into && desc->capacity) {
     __int128 lo[2], hi[2];
     span(desc, cache, &lo[0], &hi[0]);

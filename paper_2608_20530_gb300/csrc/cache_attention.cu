@@ -13,7 +13,6 @@ namespace {
 
 int g_ca_path = 0;             // test hook: 1 the tensor-core kernel for all bf16 queries, 2 for none
 
-
 lilicorr_status_t ca_plan(const lilicorr_cache_attention_desc* d, CaPlan* p) {
   if (!d) return LILICORR_ERR_ARG;
   LL_TRY(cache_shape(&d->cache));
@@ -21,7 +20,7 @@ lilicorr_status_t ca_plan(const lilicorr_cache_attention_desc* d, CaPlan* p) {
   const lilicorr_cache_desc& c = d->cache;
   if (d->tokens < 1 || d->q_heads < 1 || d->q_heads % c.kv_heads) return LILICORR_ERR_SHAPE;
   const double all = (double)c.sequences * d->tokens * d->q_heads;
-  if (all >= 2147483648.0) return LILICORR_ERR_SHAPE;
+  if (all > 0x1p30 || (double)d->tokens * d->q_heads > 0x1p30) return LILICORR_ERR_SHAPE;
   const int rows = d->tokens * (d->q_heads / c.kv_heads);
   p->dp = c.head_dim <= 32 ? 32 : c.head_dim <= 64 ? 64 : 128;
   p->pieces = d->dtype == LILICORR_BF16 ? 1 : 3;
@@ -117,7 +116,6 @@ lilicorr_status_t run_cache_attention(const lilicorr_cache_attention_desc* desc,
          : p.dp == 64 ? ca_launch_rows<64, 0>(a, p, stream)
                       : ca_launch_rows<128, 0>(a, p, stream);
 }
-
 
 }  // namespace
 }  // namespace lilicorr

@@ -98,7 +98,7 @@ def test_attention_refuses(ll):
     for shared in OVERLAPPING[:3]:                   # a cache that is read may be shared
         assert _attend(ll, _cache(ll, **shared), ws_bytes=16)[0] == 7, shared
     x = _cache(ll)
-    for bad in (dict(T=0), dict(Hq=0), dict(Hq=7), dict(T=1 << 28, Hq=8)):
+    for bad in (dict(T=0), dict(Hq=0), dict(Hq=7), dict(T=1 << 28, Hq=8), dict(T=(1 << 26) + 1)):
         code, d = _attend(ll, x, **bad)
         assert code == 2, bad
         assert ll.lib().lilicorr_cache_attention_workspace_bytes(ctypes.byref(d)) == 0
@@ -121,7 +121,7 @@ def test_attention_refuses(ll):
 
 
 def _evict(ll, x, budget=50, recent=10, first=2, into=None, cache=P, weights=P, lens=P, into_cache=None,
-           into_weights=None, kept=P, new=P):
+           into_weights=None, kept=P, new=Q):
     return ll.lib().lilicorr_cache_evict(ctypes.byref(x) if x else None, cache, weights, lens, budget, recent,
                                          first, ctypes.byref(into) if into else None, into_cache,
                                          into_weights, kept, new, None)
@@ -139,7 +139,11 @@ def test_evict_refuses(ll):
                 dict(cache=ODD), dict(weights=None), dict(lens=None), dict(kept=None), dict(new=None),
                 dict(into_cache=Q), dict(into_weights=Q)):
         assert _evict(ll, x, **bad) == 1, bad
-    there = dict(into_cache=Q, into_weights=ctypes.c_void_p(1 << 41))
+    # places past 2^30 would pass 32 bits in a stride over them
+    assert _evict(ll, x, budget=(1 << 30) + 1) == 2 and _evict(ll, x, budget=2 ** 31 - 1) == 2
+    # lengths that all heads read, and one of them would write
+    assert _evict(ll, x, new=ctypes.c_void_p(4100)) == 1 and _evict(ll, x, lens=Q, new=Q) == 1
+    there = dict(into_cache=Q, into_weights=ctypes.c_void_p(1 << 41), new=Q)
     for bad in (dict(sequences=3), dict(kv_heads=1), dict(head_dim=80), dict(capacity=49),
                 dict(capacity=-1)):
         assert _evict(ll, x, into=_cache(ll, **bad), **there) == 2, bad
