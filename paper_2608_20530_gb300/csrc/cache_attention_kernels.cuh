@@ -8,6 +8,12 @@
 // Products are turned round: keys (of the second product, elements) are the 16 rows of a matrix instruction,
 // query rows its 8 columns, so the few rows of a decoding step fill it, and what is read from the cache is
 // expanded once, in the registers that the instruction reads, whatever the number of rows.
+//
+// What bounds it: bytes by the cache's rate, 32 sequences of 2,048 to 8,192 positions, 8 heads of 128, 4 rows each:
+// 49.5 us, 3.9 TB/s of records; a key more costs as much as at 5.3 to 6.1 TB/s, and 14 us are start, first bytes,
+// parts and their join. On the way 16 keys cost a warp some 320 instructions, 54 % of all issue slots (alu pipe
+// 45 %: unpacking codes). Tried: 16 warps a CTA that share a tile (a barrier each: 50 -> 66 us), three CTAs
+// an SM at 80 registers (49 -> 54), shorter shares for the CTAs that start last (no better).
 #pragma once
 #include <float.h>
 
@@ -28,10 +34,11 @@ constexpr float CA_UP = 7.f, CA_SLACK = 8.f, CA_ROOM = 1.f;
 // So the heads of a position, which may lie side by side in 64 bytes that memory reads at once, are read
 // at about the same time. An item is one (sequence, kv head, row block). A CTA leaves at most two parts of items
 // that other CTAs have parts of: of its first item (place 2 b) and of its last (2 b + 1). Of the CTAs that have parts
-// of an item, the last to leave its own joins them, in the order of the list.
-constexpr uint32_t CA_MIN_TILES = 1;
+// of an item, the last to leave its own joins them, in the order of the list (a launch of its own for that: 43 us for
+// 41). One head after the other, records of 144 bytes 8 heads apart, read 259 MB for 193 (lines of 128 bytes that
+// two heads share).
 __device__ __forceinline__ uint32_t ca_per_team(uint32_t tiles, uint32_t teams) {
-  return max(CA_MIN_TILES, (tiles + teams - 1) / teams);
+  return max(1u, (tiles + teams - 1) / teams);
 }
 // tiles of a row block of a sequence: one even where there is no key, none where there is no sequence
 template <int KEYS>
@@ -765,7 +772,9 @@ cache_attention_kernel(const CaArgs a) {
 }
 
 // What each key gets, from the scores that the kernel left, against their rows' references and sums; a thread a
-// key, and a block KEYS keys of one kv head.
+// key, and a block CS_KEYS keys of one kv head. Bytes bound it: 4 bytes a row and key written and read again, from L2
+// where they are few, for 8 of the weight itself. 16 sequences of 8,192, 8 heads, 4 rows: 52 us with the attention,
+// which alone takes 41.
 constexpr int CS_KEYS = 512;
 template <int PIECES>
 __global__ void __launch_bounds__(256) cache_attention_spread_kernel(const CaArgs a, int pieces) {
@@ -825,7 +834,8 @@ __global__ void __launch_bounds__(256) cache_attention_spread_kernel(const CaArg
 }
 
 // The same where rows are too many to keep their scores: computed once more, a warp 16 keys; rows go
-// through shared memory 8 NT at a time, and each key's weight is read and written by one lane.
+// through shared memory 8 NT at a time, and each key's weight is read and written by one lane, once for each
+// 8 NT rows.
 template <int DP, int DIM, int NT, int PIECES, typename E>
 __global__ void __launch_bounds__(CA_THREADS, NT > 2 ? 1 : 2) cache_attention_weights_kernel(const CaArgs a) {
   pdl_wait();

@@ -2,18 +2,23 @@
 // matrix instruction has columns (drafted blocks under verification, wide groups of heads), 128 rows at a time
 // against tiles of 128 keys.
 //
-// One CTA an SM. Warps 9-16 copy records to shared memory and expand them, a thread half a record, to fp16 (exact:
-// six significant bits) in the swizzled layout that the tensor cores read: warps 9-12 keys, 13-16 values.
-// Warp 8 issues
+// One CTA an SM. Two warps copy records to shared memory; eight expand them, a thread half a record, to fp16 (exact:
+// six significant bits) in the swizzled layout that the tensor cores read, four of them keys, four values. One warp
+// issues
 //   S = Q K^T   (M 128, N 128)   into tensor memory, and
 //   O += P V    (M 128, N d)     with P read from tensor memory, V as the MN-major operand.
-// Warps 0-3 and 4-7 are two streams, a thread a row, that take the key tiles in turn: while one is at its
+// The first warps are two streams, a thread a row, that take the key tiles in turn: while one is at its
 // exponentials the tensor cores work for the other. Queries are brought to fp16 by a power of two of their row,
 // as on mma.sync (cache_attention_kernels.cuh). Each stream has its own references and sums, whole numbers
 // m that move only when a score passes them by 8; at an item's end the two come together.
 //
-// What bounds it: 1,024 clocks a tile for the two products at d = 128, whatever the number of rows, beside 480 issue
-// slots for the expansion and 64 KB written to and 96 KB read from shared memory.
+// What bounds it: 8 sequences of 4,096 to 16,384 positions, 8 heads of 128, 64 rows: 63.5 us. A tile more costs an SM
+// 0.97 us, some 1,850 clocks: 1,060 of the tensor pipe (its operands are 96 KB of shared memory), 1,900 of a stream's
+// two passes over its scores (128 exponentials a thread are 1,024 of them) and the way from one to the other, for
+// two tiles at a time. None of them alone: half of the matrix work, half of the stores of expanded records, no
+// copies, or no exponentials leave 95, 94, 95 and 94 % of the time. 26 us are start, first tile, a change of item, parts and
+// their join (14 where every CTA has one item). Tried: a thread half of a row's scores of a tile (its softmax in half
+// the time, 63 us for 64), a warp that issues for each stream (65), both (67), half tiles of 64 keys (73).
 #include "cache_attention_kernels.cuh"
 #include "tc_ptx.cuh"
 
