@@ -19,7 +19,8 @@ SOURCES = ["api.cu", "topk_lse.cu", "head_kernels.cu", "pair_walk.cu", "gemm_tc.
            "diagnostics.cu", "gemm_small.cu", "gemm_split.cu", "lm_head.cu",
            "net_cluster.cu", "net_pair.cu", "beam.cu", "prefix_attention.cu",
            "prefix_attention_tc.cu", "cache.cu", "cache_attention.cu",
-           "cache_attention_any.cu", "cache_attention_tc.cu"]
+           "cache_attention_any.cu", "cache_attention_tc.cu",
+           "cache_attention_tc_weights.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr",
          "-I", INCLUDE, "-I", CSRC]

@@ -45,6 +45,8 @@ lilicorr_status_t ca_launch_rows(const CaArgs& a, const CaPlan& p, cudaStream_t 
 
 // bf16 queries on the 5th-generation tensor cores (cache_attention_tc.cu)
 lilicorr_status_t launch_ca_tc(const CaArgs& a, const CaPlan& p, cudaStream_t st);
+// what each key gets from bf16 queries whose scores were not kept (cache_attention_tc_weights.cu)
+lilicorr_status_t launch_ca_tc_weights(const CaArgs& a, const CaPlan& p, cudaStream_t st);
 
 constexpr long long CA_WAIT = 4000000000ll;          // about 2 s
 

@@ -833,13 +833,14 @@ __global__ void __launch_bounds__(256) cache_attention_spread_kernel(const CaArg
   }
 }
 
-// The same where rows are too many to keep their scores: computed once more, a warp 16 keys; rows go
+// The same for more rows of fp32 queries than scores are kept for: computed once more, a warp 16 keys; rows go
 // through shared memory 8 NT at a time, and each key's weight is read and written by one lane, once for each
-// 8 NT rows.
-template <int DP, int DIM, int NT, int PIECES, typename E>
-__global__ void __launch_bounds__(CA_THREADS, NT > 2 ? 1 : 2) cache_attention_weights_kernel(const CaArgs a) {
+// 8 NT rows. (bf16: cache_attention_tc_weights.cu.)
+template <int DP, int DIM>
+__global__ void __launch_bounds__(CA_THREADS, 2) cache_attention_weights_kernel(const CaArgs a) {
   pdl_wait();
-  constexpr int KS = CaCfg<DP>::KS, ST = 4, ROWS = 8 * NT, STAGE = 16 * (DP / 2 + 16), KEYS = 16 * CA_WARPS;
+  using E = float;
+  constexpr int NT = 1, PIECES = 3, KS = CaCfg<DP>::KS, ST = 4, ROWS = 8 * NT, STAGE = 16 * (DP / 2 + 16), KEYS = 16 * CA_WARPS;
   extern __shared__ __align__(16) unsigned char sm[];
   uint2* qs = reinterpret_cast<uint2*>(sm + CA_WARPS * ST * STAGE);      // [NT][PIECES][KS][lane]
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
@@ -953,19 +954,22 @@ __global__ void __launch_bounds__(CA_THREADS, NT > 2 ? 1 : 2) cache_attention_we
 }
 
 // What each key gets, behind the rows' results.
-template <int DP, int DIM, int NT, int PIECES, typename E>
+template <int DP, int DIM, int PIECES>
 lilicorr_status_t ca_launch_weights(const CaArgs& a, const CaPlan& p, cudaStream_t st) {
   if (!a.weights || a.c.S == 0) return LILICORR_OK;
   if (a.scores) {
     const int pieces = (a.c.S + CS_KEYS - 1) / CS_KEYS;
     return launch_k(cache_attention_spread_kernel<PIECES>, (unsigned)(a.c.N * a.c.H * pieces), 256, 0, st, a, pieces);
   }
-  static bool configured_w[64] = {false};
-  constexpr int WT = PIECES > 1 ? 1 : NT;
-  auto* weights = cache_attention_weights_kernel<DP, DIM, WT, PIECES, E>;
-  LL_TRY(allow_max_dynamic_smem(weights, configured_w));
-  const size_t smem = CA_WARPS * 4 * 16 * (DP / 2 + 16) + WT * PIECES * (DP / 16) * 256;
-  return launch_k(weights, (unsigned)(2 * num_sms() / p.team * p.team), CA_THREADS, smem, st, a);
+  if constexpr (PIECES == 1) {
+    return launch_ca_tc_weights(a, p, st);
+  } else {
+    static bool configured[64] = {false};
+    auto* weights = cache_attention_weights_kernel<DP, DIM>;
+    LL_TRY(allow_max_dynamic_smem(weights, configured));
+    const size_t smem = CA_WARPS * 4 * 16 * (DP / 2 + 16) + 3 * (DP / 16) * 256;
+    return launch_k(weights, (unsigned)(2 * num_sms() / p.team * p.team), CA_THREADS, smem, st, a);
+  }
 }
 
 template <int DP, int DIM, int NT, int PIECES, typename E>
@@ -975,7 +979,7 @@ lilicorr_status_t ca_launch(const CaArgs& a, const CaPlan& p, cudaStream_t st) {
   LL_TRY(allow_max_dynamic_smem(kernel, configured));
   LL_TRY(launch_k(kernel, p.whole ? (unsigned)p.items : (unsigned)p.ctas, CA_THREADS,
                   CaSmem<DP, NT, PIECES>::TOTAL, st, a));
-  return ca_launch_weights<DP, DIM, NT, PIECES, E>(a, p, st);
+  return ca_launch_weights<DP, DIM, PIECES>(a, p, st);
 }
 
 }  // namespace
@@ -986,7 +990,7 @@ lilicorr_status_t ca_launch_rows(const CaArgs& a, const CaPlan& p, cudaStream_t 
     return p.nt == 1 ? ca_launch<DP, DIM, 1, 3, float>(a, p, st) : ca_launch<DP, DIM, 2, 3, float>(a, p, st);
   if (p.tc) {
     LL_TRY(launch_ca_tc(a, p, st));
-    return ca_launch_weights<DP, DIM, 4, 1, __nv_bfloat16>(a, p, st);
+    return ca_launch_weights<DP, DIM, 1>(a, p, st);
   }
   return p.nt == 1   ? ca_launch<DP, DIM, 1, 1, __nv_bfloat16>(a, p, st)
          : p.nt == 2 ? ca_launch<DP, DIM, 2, 1, __nv_bfloat16>(a, p, st)
