@@ -115,13 +115,14 @@ int lilicorr_test_attention_path(int mode);
  * the size of its workspace included. Returns the previous mode. */
 int lilicorr_test_cache_attention_path(int mode);
 
-/* lilicorr_cache_attention without weights on its tensor-core kernel, which expands no keys (`which` 1) or
- * values (2) for its products, and a limit as above: the workspace's status word receives LILICORR_ERR_TIMEOUT, the
- * outputs unspecified values. LILICORR_ERR_SHAPE where another kernel takes the call. */
+/* lilicorr_cache_attention whose tensor-core kernels lack operands, and a limit as above: without weights, no keys
+ * (`which` 1) or values (2) are expanded for the attention; with them (3) no keys for what each key gets. The
+ * workspace's status word receives LILICORR_ERR_TIMEOUT, the outputs unspecified values. LILICORR_ERR_SHAPE
+ * where other kernels take the call. */
 lilicorr_status_t lilicorr_test_cache_attention_timeout(const lilicorr_cache_attention_desc* desc, const void* q,
                                                         const void* cache, const int32_t* seq_len, void* out,
-                                                        float* lse, void* ws, size_t ws_bytes,
-                                                        long long wait_cycles, int which,
+                                                        float* lse, float* weights, void* ws,
+                                                        size_t ws_bytes, long long wait_cycles, int which,
                                                         cudaStream_t stream);
 
 #ifdef __cplusplus

@@ -125,7 +125,7 @@ _SIGS = {
     "lilicorr_cache_attention_workspace_bytes": (_S, [_P]),
     "lilicorr_cache_attention": (_I, [_P] * 8 + [_S, _P]),
     "lilicorr_test_cache_attention_path": (_I, [_I]),
-    "lilicorr_test_cache_attention_timeout": (_I, [_P] * 7 + [_S, ctypes.c_longlong, _I, _P]),
+    "lilicorr_test_cache_attention_timeout": (_I, [_P] * 8 + [_S, ctypes.c_longlong, _I, _P]),
     "lilicorr_cache_evict": (_I, [_P] * 4 + [_I] * 3 + [_P] * 6),
     "lilicorr_test_prefix_attention_timeout": (_I, [_P] * 11 + [_S, ctypes.c_longlong, _I, _P]),
     "lilicorr_test_linear": (_I, [_P, _I, _I, _P, _I, _I, _P, _I, _I, _I, _I, _I, _P, _P, _I, _I,
@@ -1072,16 +1072,17 @@ def test_cache_attention_path(mode: int) -> int:
 
 def test_cache_attention_timeout(q: torch.Tensor, cache: torch.Tensor, seq_len: torch.Tensor, ws: Workspace,
                                  wait_cycles: int, which: int) -> None:
-    """Test hook: cache_attention of a dense q on its tensor-core kernel without its keys (``which`` 1) or
-    values (2), so that its bounded waits run out and ``ws`` holds the timeout status."""
+    """Test hook: cache_attention of a dense q on its tensor-core kernels without keys (``which`` 1) or values (2)
+    for the attention or keys (3) for weights, so that bounded waits run out and ``ws`` holds the timeout status."""
     N, S, H, R = cache.shape
     _, T, Hq, d = q.shape
     out, lse = torch.empty_like(q), torch.empty((N, T, Hq), dtype=torch.float32, device=q.device)
+    w = torch.zeros((N, H, S), dtype=torch.float32, device=q.device) if which == 3 else None
     desc = _CA_DESC.pack(N, S, H, d, *cache.stride()[:3], 1.0, 1.0, T, Hq, _dtype_code(q), d ** -0.5,
                          *q.stride()[:3], *out.stride()[:3])
     _check(lib().lilicorr_test_cache_attention_timeout(
-        desc, q.data_ptr(), cache.data_ptr(), seq_len.data_ptr(), out.data_ptr(), lse.data_ptr(), ws.ptr, ws.nbytes,
-        int(wait_cycles), int(which), _stream()), "test_cache_attention_timeout")
+        desc, q.data_ptr(), cache.data_ptr(), seq_len.data_ptr(), out.data_ptr(), lse.data_ptr(), _ptr(w), ws.ptr,
+        ws.nbytes, int(wait_cycles), int(which), _stream()), "test_cache_attention_timeout")
 
 
 def test_attention_path(mode: int) -> int:

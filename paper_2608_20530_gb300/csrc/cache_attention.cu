@@ -79,7 +79,7 @@ lilicorr_status_t run_cache_attention(const lilicorr_cache_attention_desc* desc,
       !cache_rows_ok(desc->out_stride, e, per16, a.c.d, true))
     return LILICORR_ERR_ARG;
   if (ws_bytes < p.total) return LILICORR_ERR_WORKSPACE;
-  if (starve && !p.tc) return LILICORR_ERR_SHAPE;
+  if (starve && (starve == 3 ? p.pieces > 1 || p.pad : !p.tc)) return LILICORR_ERR_SHAPE;
   unsigned char* w = static_cast<unsigned char*>(ws);
   a.q = q;
   a.out = out;
@@ -144,11 +144,12 @@ int lilicorr_test_cache_attention_path(int mode) {
 
 lilicorr_status_t lilicorr_test_cache_attention_timeout(const lilicorr_cache_attention_desc* desc, const void* q,
                                                         const void* cache, const int32_t* seq_len, void* out,
-                                                        float* lse, void* ws, size_t ws_bytes,
-                                                        long long wait_cycles, int which,
+                                                        float* lse, float* weights, void* ws,
+                                                        size_t ws_bytes, long long wait_cycles, int which,
                                                         cudaStream_t stream) {
-  if (wait_cycles < 100000 || wait_cycles > CA_WAIT || which < 1 || which > 2) return LILICORR_ERR_ARG;
-  return run_cache_attention(desc, q, cache, seq_len, out, lse, nullptr, ws, ws_bytes, stream, wait_cycles,
+  if (wait_cycles < 100000 || wait_cycles > CA_WAIT || which < 1 || which > 3 || (which == 3) != (weights != nullptr))
+    return LILICORR_ERR_ARG;
+  return run_cache_attention(desc, q, cache, seq_len, out, lse, weights, ws, ws_bytes, stream, wait_cycles,
                              which);
 }
 

@@ -29,7 +29,7 @@ struct CaArgs {
   int pad;                     // rows, even
   uint32_t* status;
   long long wait_limit;        // SM cycles per bounded wait of the tensor-core kernel
-  int test_starve;             // test hook only: it expands no keys (1) or values (2)
+  int test_starve;             // test hook only: no keys (1), values (2) or keys for the weights (3)
 };
 
 struct CaPlan {

@@ -117,7 +117,7 @@ __global__ void __launch_bounds__(CW_THREADS, 1) cache_attention_tc_weights_kern
   } else if (warp >= CW_FIRST) {
     const int x = tid - 32 * CW_FIRST, key = x & 127;
     const uint32_t mine = x >> 7;                    // of each two tiles
-    bool ok = true;
+    bool ok = a.test_starve != 3;
     walk([&](int tile0, int here, int) {
       for (int t = (g ^ mine) & 1u; t < here && ok; t += 2) {
         const uint32_t i = g + t, raw = i % CW_RAW;
@@ -229,29 +229,33 @@ __global__ void __launch_bounds__(CW_THREADS, 1) cache_attention_tc_weights_kern
         // some row does not see all of them, or may not take their products
         const bool masked = !all || (tile0 + t + 1) * CT_KEYS > at.len - (a.T - 1);
         uint64_t sum[2] = {0ull, 0ull};
+        auto add = [&](auto some) {                  // (some: not all of them)
 #pragma unroll 1
-        for (int c = 0; c < cols; c += 32) {
-          uint32_t x[32];
-          tmem_ld32(scores + c, x);
+          for (int c = 0; c < cols; c += 32) {
+            uint32_t x[32];
+            tmem_ld32(scores + c, x);
 #pragma unroll
-          for (int e = 0; e < 32; e += 4) {          // (columns past the last: queries of 0, 1 / sum of 0)
-            const float4 f = *reinterpret_cast<const float4*>(s_factor + c + e);
-            const float4 b = *reinterpret_cast<const float4*>(s_add + c + e);
-            const float4 y = *reinterpret_cast<const float4*>(s_inv + c + e);
-            float p[4];
-            halves(fma_pair(pair_of(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), pair_of(f.x, f.y),
-                            pair_of(b.x, b.y)), p[0], p[1]);
-            halves(fma_pair(pair_of(__uint_as_float(x[e + 2]), __uint_as_float(x[e + 3])), pair_of(f.z, f.w),
-                            pair_of(b.z, b.w)), p[2], p[3]);
+            for (int e = 0; e < 32; e += 4) {        // (columns past the last: queries of 0, 1 / sum of 0)
+              const float4 f = *reinterpret_cast<const float4*>(s_factor + c + e);
+              const float4 b = *reinterpret_cast<const float4*>(s_add + c + e);
+              const float4 y = *reinterpret_cast<const float4*>(s_inv + c + e);
+              float p[4];
+              halves(fma_pair(pair_of(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), pair_of(f.x, f.y),
+                              pair_of(b.x, b.y)), p[0], p[1]);
+              halves(fma_pair(pair_of(__uint_as_float(x[e + 2]), __uint_as_float(x[e + 3])), pair_of(f.z, f.w),
+                              pair_of(b.z, b.w)), p[2], p[3]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              p[i] = ex2(p[i]);
-              if (masked && k >= s_seen[c + e + i]) p[i] = 0.f;
+              for (int i = 0; i < 4; ++i) {
+                p[i] = ex2(p[i]);
+                if (decltype(some)::value && k >= s_seen[c + e + i]) p[i] = 0.f;
+              }
+              sum[0] = fma_pair(pair_of(p[0], p[1]), pair_of(y.x, y.y), sum[0]);
+              sum[1] = fma_pair(pair_of(p[2], p[3]), pair_of(y.z, y.w), sum[1]);
             }
-            sum[0] = fma_pair(pair_of(p[0], p[1]), pair_of(y.x, y.y), sum[0]);
-            sum[1] = fma_pair(pair_of(p[2], p[3]), pair_of(y.z, y.w), sum[1]);
           }
-        }
+        };
+        if (masked) add(std::true_type{});
+        else add(std::false_type{});
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&s_free[s]);

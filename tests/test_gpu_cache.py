@@ -264,7 +264,7 @@ def test_far_scores_on_tensor_cores(tensor_cores):
         test_nan_query_spoils_its_own_row("bf16", T)
 
 
-@pytest.mark.parametrize("which", [1, 2])
+@pytest.mark.parametrize("which", [1, 2, 3])
 def test_bounded_waits_run_out(tensor_cores, which):
     """Products whose keys or values never come: the waits end, the status says so, the context lives."""
     ll = tensor_cores
@@ -273,7 +273,9 @@ def test_bounded_waits_run_out(tensor_cores, which):
     ll.test_cache_attention_timeout(q, c, lens, ws, 2_000_000, which)
     assert ws.status() == 6
     ws = ll.Workspace(ll.cache_attention_workspace_bytes(q, c))
-    _check(ll.cache_attention(q, c, lens, ws=ws), q, c, lens)
+    w = torch.zeros((2, 2, 700), device="cuda")
+    w1 = w.clone()
+    _check(ll.cache_attention(q, c, lens, weights=w1, ws=ws), q, c, lens, w0=w, w=w1)
     assert ws.status() == 0
 
 
@@ -341,6 +343,36 @@ def test_nan_query_spoils_its_own_row(dtype, T):
     _check((out[:1], lse[:1]), bad[:1], c[:1], lens[:1], w0=w[:1], w=w1[:1])
     want = plain.attention(bad, c, lens, 64 ** -0.5)[2]
     assert bool(((w1.double() - w.double() - want).abs() <= 2.0 ** -14 * want + 2.0 ** -22 * (1 + want)).all())
+
+
+@pytest.mark.parametrize("shape", [
+    (40, 9, 8, 2, 96, 700), (3, 16, 32, 8, 128, 5000), (1, 16, 32, 4, 64, 9000), (2, 70, 16, 2, 128, 900),
+    (300, 5, 32, 8, 128, 130), (2, 17, 1, 1, 16, 20), (5, 33, 12, 3, 48, 400), (1, 129, 2, 1, 80, 1000)])
+def test_weights_of_many_rows(shape):
+    """More rows a kv head than scores are kept for: one block of rows and several, items that begin and end
+    anywhere in a CTA's share."""
+    ll = _ll()
+    q, c, lens, w = _case(ll, *shape, "bf16", 77, heads_first=shape[0] % 2 == 0)
+    w1, w2 = w.clone(), w.clone()
+    _check(ll.cache_attention(q, c, lens, weights=w1), q, c, lens, w0=w, w=w1)
+    ll.cache_attention(q, c, lens, weights=w2)
+    assert torch.equal(w1, w2)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [3, 9, 40])
+def test_keys_that_are_not_finite_add_nothing(dtype, T):
+    """Rows that meet such a key have no finite sum; the other kv heads and sequences do not see it."""
+    ll = _ll()
+    q, c, lens, w = _case(ll, 2, T, 8, 2, 64, 700, dtype, 10, lens=[700, 650])
+    w1, w2 = w.clone(), w.clone()
+    ll.cache_attention(q, c, lens, weights=w1)
+    c[1, 300, 0, 32:40] = 0x7F                       # a key's scales: NaN
+    out, lse = ll.cache_attention(q, c, lens, weights=w2)
+    assert bool(out[1, :, :4].isnan().all()) and bool(lse[1, :, :4].isnan().all())
+    assert torch.equal(w2[1, 0], w[1, 0])
+    assert torch.equal(w2[0], w1[0]) and torch.equal(w2[1, 1], w1[1, 1])
+    assert bool(out[1, :, 4:].isfinite().all()) and bool(out[0].isfinite().all())
 
 
 @pytest.mark.parametrize("T", [1, 16])
