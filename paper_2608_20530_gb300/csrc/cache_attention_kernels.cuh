@@ -358,6 +358,9 @@ __device__ __forceinline__ void store4(E* p, const float4& v) {
   if constexpr (sizeof(E) == 4) *reinterpret_cast<float4*>(p) = v;
   else *reinterpret_cast<uint2*>(p) = make_uint2(bf16_pack2(v.x, v.y), bf16_pack2(v.z, v.w));
 }
+__device__ __forceinline__ void named_barrier(int id, int threads) {
+  asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
 // a row's normaliser from its reference and sum
 __device__ __forceinline__ void ca_write_row(const CaArgs& a, int n, int t, int hq, float m, float l) {
   // the scores were taken in units that their factor's rounding moved
@@ -729,11 +732,14 @@ cache_attention_kernel(const CaArgs a) {
         __threadfence();
       }
       __syncthreads();
-      if (joins)
-        for (int i = warp; i < ROWS && at.rb * ROWS + i < rows; i += CA_WARPS) {
+      if (joins) {
+        // a warp a row, or two where there are so few: then the second has every second four parts
+        const bool two = NT == 1 && rows <= CA_WARPS / 2 && team1 - team0 >= 4;
+        const uint32_t step = two ? 8 : 4;
+        for (int i = two ? warp % (CA_WARPS / 2) : warp; i < ROWS && at.rb * ROWS + i < rows; i += CA_WARPS) {
           float M = -FLT_MAX, L = 0.f;
           float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-          for (uint32_t t0 = team0; t0 <= team1; t0 += 4) {        // four parts at a time
+          for (uint32_t t0 = team0 + (two ? warp & 4 : 0); t0 <= team1; t0 += step) {   // four parts at a time
             float2 z[4];
             float4 v[4];
 #pragma unroll
@@ -760,9 +766,26 @@ cache_attention_kernel(const CaArgs a) {
               y.w = fmaf(x, v[j].w, y.w);
             }
           }
+          if (two) {
+            if (warp & 4) {
+              xm[i] = make_float2(M, L);
+              if (lane < DP / 4) *reinterpret_cast<float4*>(xo + i * Cfg::XL + lane * 4) = y;
+            }
+            named_barrier(1 + i, 64);
+            if (warp & 4) break;
+            const float2 z = xm[i];
+            const float to = fmaxf(M, z.x), x0 = ex2(M - to), x1 = ex2(z.x - to);
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (lane < DP / 4) v = *reinterpret_cast<const float4*>(xo + i * Cfg::XL + lane * 4);
+            M = to;
+            L = fmaf(x1, z.y, L * x0);
+            y = make_float4(fmaf(x1, v.x, y.x * x0), fmaf(x1, v.y, y.y * x0), fmaf(x1, v.z, y.z * x0),
+                            fmaf(x1, v.w, y.w * x0));
+          }
           const int r = at.rb * ROWS + i, t = r / a.rep;
           ca_write<E>(a, at.n, t, at.h * a.rep + (r - t * a.rep), M, L, y, lane);
         }
+      }
     }
     if (done == count) break;
     at.next(a, a.blocks);
