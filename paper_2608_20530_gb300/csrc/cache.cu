@@ -330,7 +330,6 @@ struct EvictArgs {
   float* to_w;                 // [N, H, to.S]
   const int32_t* seq_len;
   int budget, recent, first, in_place;
-  Quotient by_vecs;            // 16-byte pieces of a record
   int32_t* kept;               // [N, H, budget]
   int32_t* new_len;            // [N]
 };
@@ -437,9 +436,6 @@ __global__ void __launch_bounds__(EV_THREADS, 2) cache_evict_kernel(const EvictA
     for (int j = rank * EV_THREADS + tid; j < L; j += C * EV_THREADS) kept[j] = j;
   if (stay == 0 || (all && a.in_place)) return;      // (all CTAs of the cluster)
   const bool whole = L <= EV_KEYS;                   // each CTA has all positions, and the whole list
-  // records of a CTA at a time: up to 455 of 144 bytes, as many for each (found while the weights are under way)
-  const uint32_t at_once = C * a.by_vecs.of(EV_THREADS * EV_VECS), turns = (stay + at_once - 1) / at_once;
-  const int mine = (stay + C * turns - 1) / (C * turns);
   if (!all) {
     const bool split = !whole && C > 1;
     const int chunk = split ? (int)(((int64_t)L + C - 1) / C + EV_THREADS - 1) / EV_THREADS * EV_THREADS : L;
@@ -611,8 +607,13 @@ __global__ void __launch_bounds__(EV_THREADS, 2) cache_evict_kernel(const EvictA
   // its own or a lower position, past all that later ones come from: what is in hand is read by all CTAs before
   // any of it is written.
   const int vecs = cache_record_bytes(a.from.d) / 16;
-  const int step = a.by_vecs.of(EV_THREADS), rest = EV_THREADS - step * vecs;
-  const int jt = a.by_vecs.of(tid), pt = tid - jt * vecs;
+  int mine = EV_THREADS * EV_VECS / vecs;            // records of a CTA at a time: 455 of 144 bytes
+  if (C > 1) {                                       // as many turns, but as many records for each of the cluster
+    const uint32_t turns = (stay + C * mine - 1) / (C * mine);
+    mine = (stay + C * turns - 1) / (C * turns);
+  }
+  const int step = EV_THREADS / vecs, rest = EV_THREADS - step * vecs;
+  const int jt = tid / vecs, pt = tid - jt * vecs;
   const unsigned char* from = a.from.at(n, 0, h);
   unsigned char* to = a.to.at(n, 0, h);
   const uint32_t from_s = (uint32_t)a.from.s[1], to_s = (uint32_t)a.to.s[1];
@@ -716,7 +717,6 @@ lilicorr_status_t run_evict(const lilicorr_cache_desc* desc, void* cache, float*
   a.recent = recent;
   a.first = first;
   a.in_place = into == nullptr;
-  a.by_vecs.set(cache_record_bytes(desc->head_dim) / 16);
   a.kept = kept;
   a.new_len = new_len;
   // as many CTAs an item as keep two an SM busy, up to eight
