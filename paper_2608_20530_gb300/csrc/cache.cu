@@ -346,8 +346,8 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
 // there are few (a barrier of the cluster costs as much as a pass), else each looks at a stretch of them. The
 // records that stay are moved by all of them together.
 // What bounds it is the chain of rounds (count, barriers, prefix sum, barrier), then the records' bytes: 8 heads cut
-// from 2,304 to 2,048 12 us in a graph (one CTA that read weights from memory each round: 55), 256 heads of up to
-// 4,160 to 2,048 41 (records read and written 19 at the copy rate), 16 heads of up to 65,536 to 4,096 33.
+// from 2,304 to 2,048 11.3 us in a graph (one CTA that read weights from memory each round: 55), 256 heads of up to
+// 4,160 to 2,048 40.4 (records read and written 19 at the copy rate), 16 heads of up to 65,536 to 4,096 31.8.
 // CTAs of 1,024 threads, one an SM, took 17 and 58 for the first two's 13 and 36 of then.
 constexpr int EV_THREADS = 512, EV_WARPS = EV_THREADS / 32;
 constexpr int EV_BINS = 2048;  // 11 bits a round

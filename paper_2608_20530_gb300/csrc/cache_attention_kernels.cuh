@@ -10,8 +10,8 @@
 // expanded once, in the registers that the instruction reads, whatever the number of rows.
 //
 // What bounds it: bytes by the cache's rate, 32 sequences of 2,048 to 8,192 positions, 8 heads of 128, 4 rows each:
-// 49.5 us, 3.9 TB/s of records; a key more costs as much as at 5.3 to 6.1 TB/s, and 14 us are start, first bytes,
-// parts and their join. On the way 16 keys cost a warp some 320 instructions, 54 % of all issue slots (alu pipe
+// 49.8 us, 3.9 TB/s of records; one of 131,072: 38.9. A key more costs as much as at 5.3 to 6.1 TB/s, and 12 to 14 us
+// are start, first bytes, parts and their join. On the way 16 keys cost a warp some 320 instructions, 54 % of all issue slots (alu pipe
 // 45 %: unpacking codes). Tried: 16 warps a CTA that share a tile (a barrier each: 50 -> 66 us), three CTAs
 // an SM at 80 registers (49 -> 54), shorter shares for the CTAs that start last (no better).
 #pragma once
@@ -733,7 +733,8 @@ cache_attention_kernel(const CaArgs a) {
       }
       __syncthreads();
       if (joins) {
-        // a warp a row, or two where there are so few: then the second has every second four parts
+        // a warp a row, or two where there are so few: then the second has every second four parts (38 parts of
+        // 131,072 positions: 41.4 -> 39.0 us; eight or more in hand at a time cost the kernel its registers)
         const bool two = NT == 1 && rows <= CA_WARPS / 2 && team1 - team0 >= 4;
         const uint32_t step = two ? 8 : 4;
         for (int i = two ? warp % (CA_WARPS / 2) : warp; i < ROWS && at.rb * ROWS + i < rows; i += CA_WARPS) {
