@@ -6,17 +6,19 @@
 //   weight += sum over rows of 2^(factor s - reference) / sum,
 // the rows' references and sums being those of the attention before. One CTA an SM: two warps copy the keys' half of the
 // records, two times four warps expand them in turn, a thread a key, one issues, and two streams of four warps take
-// the tiles in turn. More than 128 rows come one block after the other, with the keys again.
+// pairs of tiles in turn, so that what a thread reads of a row serves two keys. More than 128 rows come one block
+// after the other, with the keys again.
 //
-// What bounds it: the streams. 64 rows take a warp some 1,500 clocks a tile, most of them the rows' figures from
-// shared memory (12 bytes a row and warp) beside what the products read there. 8 sequences of 16,384, 8 heads of 128: 55 us
-// behind an attention of 82; 32 rows 44 behind 79 (with the few rows' kernel, 32 at a time, 129 and 82).
+// What bounds it: for few rows the way of a tile through copies, expansion and product, for more the rows' figures that
+// the streams read from shared memory (12 bytes a row and warp), beside the products that read there. 8 sequences of
+// 16,384, 8 heads of 128: 64 rows 46.5 us behind an attention of 82, with a tile a stream at a time 55; 32 rows 41.5
+// (on mma.sync, 32 rows at a time, 129 and 82).
 #include "cache_attention_tc.cuh"
 
 namespace lilicorr {
 namespace {
 
-constexpr uint32_t CW_TMEM = 256;
+constexpr uint32_t CW_TMEM = 512;
 constexpr int CW_RAW = 4;                            // tiles of keys under way
 constexpr int CW_SOFT = 256, CW_MMA_WARP = 8, CW_COPY_WARP = 9, CW_FIRST = 11, CW_THREADS = 32 * 19;
 
@@ -70,7 +72,7 @@ __global__ void __launch_bounds__(CW_THREADS, 1) cache_attention_tc_weights_kern
     return __all_sync(0xffffffffu, wait_long(bar, parity, a.wait_limit, &abort_flag)) != 0;
   };
   uint32_t done = 0;                                 // tiles of the list behind this warp
-  uint32_t g = 0;                                    // tiles of all blocks of rows: g % 2 is one's place and stream
+  uint32_t g = 0, pairs = 0;                         // tiles so far, whose place is g % 2; pairs of them: their stream
   // f(tile0, tiles, r0) for each block of rows of each item's tiles here
   auto walk = [&](auto f) {
     while (done < count) {
@@ -78,6 +80,7 @@ __global__ void __launch_bounds__(CW_THREADS, 1) cache_attention_tc_weights_kern
       for (int r0 = 0; r0 < rows; r0 += CT_ROWS) {
         f(at.tile, here, r0);
         g += here;
+        pairs += (here + 1) / 2;
       }
       done += here;
       if (done < count) at.next(a, 1);
@@ -146,20 +149,20 @@ __global__ void __launch_bounds__(CW_THREADS, 1) cache_attention_tc_weights_kern
       named_bar(1, CW_SOFT + 32);                    // Q is there
       tc_fence_after();
       for (int t = 0; t < here && ok; ++t) {
-        const uint32_t i = g + t, s = i & 1u, turn = i >> 1 & 1u;
-        ok = wait(&k_full[s], turn) && wait(&s_free[s], turn ^ 1u);
+        const uint32_t i = g + t, k = i & 1u, pair = pairs + t / 2, s = pair & 1u;
+        ok = wait(&k_full[k], i >> 1 & 1u) && (t & 1 || wait(&s_free[s], (pair >> 1 & 1u) ^ 1u));
         if (!ok) break;
         tc_fence_after();
-        const uint64_t kd = k_desc + s * (Cfg::TILE >> 4);
+        const uint64_t kd = k_desc + k * (Cfg::TILE >> 4);
         if (leader) {
 #pragma unroll
           for (int c = 0; c < Cfg::CH; ++c)
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-              mma_bf16(tmem + s * 128, kd + c * (CT_CHUNK >> 4) + 2 * k, q_desc + c * (CT_CHUNK >> 4) + 2 * k, idesc,
-                       (c | k) > 0);
-          mma_commit(&s_ready[s]);
-          mma_commit(&k_empty[s]);
+            for (int j = 0; j < 4; ++j)
+              mma_bf16(tmem + s * 256 + (t & 1) * 128, kd + c * (CT_CHUNK >> 4) + 2 * j,
+                       q_desc + c * (CT_CHUNK >> 4) + 2 * j, idesc, (c | j) > 0);
+          mma_commit(&k_empty[k]);
+          if (t & 1 || t + 1 == here) mma_commit(&s_ready[s]);
         }
         __syncwarp();
       }
@@ -172,7 +175,7 @@ __global__ void __launch_bounds__(CW_THREADS, 1) cache_attention_tc_weights_kern
   } else {
     const uint32_t s = warp >> 2;
     const int key = (warp & 3) * 32 + lane;
-    const uint32_t scores = tmem + s * 128 + ((uint32_t)((warp & 3) * 32) << 16);
+    const uint32_t scores = tmem + s * 256 + ((uint32_t)((warp & 3) * 32) << 16);
     bool ok = true;
     walk([&](int tile0, int here, int r0) {
       // the block's queries and its rows' figures, a row two threads
@@ -222,39 +225,49 @@ __global__ void __launch_bounds__(CW_THREADS, 1) cache_attention_tc_weights_kern
       bool all = true;
       for (int r = lane; r < cols; r += 32) all &= s_inv[r] > 0.f;
       all = __all_sync(0xffffffffu, all);
-      for (int t = (g ^ s) & 1u; t < here && ok; t += 2) {
-        const uint32_t i = g + t;
-        const int k = (tile0 + t) * CT_KEYS + key;
+      for (int t = 2 * ((pairs ^ s) & 1u); t < here && ok; t += 4) {
+        const uint32_t pair = pairs + t / 2;
+        const int k = (tile0 + t) * CT_KEYS + key;   // and the key 128 behind it
         float* to = a.weights + ((size_t)at.n * a.c.H + at.h) * a.c.S + k;
-        float w = 0.f;
-        if (k < at.len) w = *to;
-        if (!wait(&s_ready[s], i >> 1 & 1u)) { ok = false; break; }
+        float w[2] = {0.f, 0.f};
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          if (t + u < here && k + u * CT_KEYS < at.len) w[u] = to[u * CT_KEYS];
+        if (!wait(&s_ready[s], pair >> 1 & 1u)) { ok = false; break; }
         tc_fence_after();
         // some row does not see all of them, or may not take their products
-        const bool masked = !all || (tile0 + t + 1) * CT_KEYS > at.len - (a.T - 1);
+        const bool masked = !all || (tile0 + t + 2) * CT_KEYS > at.len - (a.T - 1);
         uint64_t sum[2] = {0ull, 0ull};
         auto add = [&](auto some) {                  // (some: not all of them)
 #pragma unroll 1
-          for (int c = 0; c < cols; c += 32) {
-            uint32_t x[32];
-            tmem_ld32(scores + c, x);
+          for (int c = 0; c < cols; c += 16) {
+            uint32_t x[2][16];
+            tmem_ld16_nowait(scores + c, x[0]);
+            tmem_ld16(scores + 128 + c, x[1]);       // (without a second tile: what lies there, for nobody)
 #pragma unroll
-            for (int e = 0; e < 32; e += 4) {        // (columns past the last: queries of 0, 1 / sum of 0)
+            for (int e = 0; e < 16; e += 8)          // nothing that uses the first moves above the second's wait
+              asm volatile("" : "+r"(x[0][e]), "+r"(x[0][e + 1]), "+r"(x[0][e + 2]), "+r"(x[0][e + 3]),
+                                "+r"(x[0][e + 4]), "+r"(x[0][e + 5]), "+r"(x[0][e + 6]), "+r"(x[0][e + 7]));
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {        // (columns past the last: queries of 0, 1 / sum of 0)
               const float4 f = *reinterpret_cast<const float4*>(s_factor + c + e);
               const float4 b = *reinterpret_cast<const float4*>(s_add + c + e);
               const float4 y = *reinterpret_cast<const float4*>(s_inv + c + e);
-              float p[4];
-              halves(fma_pair(pair_of(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), pair_of(f.x, f.y),
-                              pair_of(b.x, b.y)), p[0], p[1]);
-              halves(fma_pair(pair_of(__uint_as_float(x[e + 2]), __uint_as_float(x[e + 3])), pair_of(f.z, f.w),
-                              pair_of(b.z, b.w)), p[2], p[3]);
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                p[i] = ex2(p[i]);
-                if (decltype(some)::value && k >= s_seen[c + e + i]) p[i] = 0.f;
+              for (int u = 0; u < 2; ++u) {
+                float p[4];
+                halves(fma_pair(pair_of(__uint_as_float(x[u][e]), __uint_as_float(x[u][e + 1])), pair_of(f.x, f.y),
+                                pair_of(b.x, b.y)), p[0], p[1]);
+                halves(fma_pair(pair_of(__uint_as_float(x[u][e + 2]), __uint_as_float(x[u][e + 3])),
+                                pair_of(f.z, f.w), pair_of(b.z, b.w)), p[2], p[3]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  p[i] = ex2(p[i]);
+                  if (decltype(some)::value && k + u * CT_KEYS >= s_seen[c + e + i]) p[i] = 0.f;
+                }
+                sum[u] = fma_pair(pair_of(p[0], p[1]), pair_of(y.x, y.y), sum[u]);
+                sum[u] = fma_pair(pair_of(p[2], p[3]), pair_of(y.z, y.w), sum[u]);
               }
-              sum[0] = fma_pair(pair_of(p[0], p[1]), pair_of(y.x, y.y), sum[0]);
-              sum[1] = fma_pair(pair_of(p[2], p[3]), pair_of(y.z, y.w), sum[1]);
             }
           }
         };
@@ -263,10 +276,12 @@ __global__ void __launch_bounds__(CW_THREADS, 1) cache_attention_tc_weights_kern
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&s_free[s]);
-        float y[4];
-        halves(sum[0], y[0], y[1]);
-        halves(sum[1], y[2], y[3]);
-        if (k < at.len) *to = w + ((y[0] + y[1]) + (y[2] + y[3]));
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          float even, odd;
+          halves(sum[u], even, odd);
+          if (t + u < here && k + u * CT_KEYS < at.len) to[u * CT_KEYS] = w[u] + (even + odd);
+        }
       }
       named_bar(3, CW_SOFT);                         // every product with these queries is done
     });
