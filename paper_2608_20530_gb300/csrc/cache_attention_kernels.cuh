@@ -11,8 +11,8 @@
 //
 // What bounds it: bytes by the cache's rate, 32 sequences of 2,048 to 8,192 positions, 8 heads of 128, 4 rows each:
 // 49.8 us, 3.9 TB/s of records; one of 131,072: 38.9. A key more costs as much as at 5.3 to 6.1 TB/s, and 12 to 14 us
-// are start, first bytes, parts and their join. On the way 16 keys cost a warp some 320 instructions, 54 % of all issue slots (alu pipe
-// 45 %: unpacking codes). Tried: 16 warps a CTA that share a tile (a barrier each: 50 -> 66 us), three CTAs
+// are start, first bytes, parts and their join. On the way 16 keys cost a warp some 320 instructions, 54 % of all
+// issue slots (alu pipe 45 %: unpacking codes). Tried: 16 warps a CTA that share a tile (a barrier each: 50 -> 66 us), three CTAs
 // an SM at 80 registers (49 -> 54), shorter shares for the CTAs that start last (no better).
 #pragma once
 #include <float.h>
@@ -864,7 +864,8 @@ template <int DP, int DIM>
 __global__ void __launch_bounds__(CA_THREADS, 2) cache_attention_weights_kernel(const CaArgs a) {
   pdl_wait();
   using E = float;
-  constexpr int NT = 1, PIECES = 3, KS = CaCfg<DP>::KS, ST = 4, ROWS = 8 * NT, STAGE = 16 * (DP / 2 + 16), KEYS = 16 * CA_WARPS;
+  constexpr int NT = 1, PIECES = 3, KS = CaCfg<DP>::KS, ST = 4, ROWS = 8 * NT, STAGE = 16 * (DP / 2 + 16);
+  constexpr int KEYS = 16 * CA_WARPS;
   extern __shared__ __align__(16) unsigned char sm[];
   uint2* qs = reinterpret_cast<uint2*>(sm + CA_WARPS * ST * STAGE);      // [NT][PIECES][KS][lane]
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
