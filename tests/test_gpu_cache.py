@@ -653,6 +653,32 @@ def test_captured_and_replayed(T, Hq, S):
         assert torch.equal(state[0], cache) and torch.equal(state[1], w)
 
 
+def test_calls_at_once_on_two_streams():
+    """Each with a workspace of its own: the few rows' kernel, the many rows', weights and evictions side by side."""
+    ll = _ll()
+    jobs = []
+    for i, (N, T, Hq, H, d, S) in enumerate([(3, 16, 32, 8, 128, 2500), (2, 1, 32, 8, 128, 9000)]):
+        q, c, lens, w = _case(ll, N, T, Hq, H, d, S, "bf16", 40 + i)
+        ws = ll.Workspace(ll.cache_attention_workspace_bytes(q, c))
+
+        def job(q=q, c=c, lens=lens, w=w, ws=ws):
+            w1, c1 = w.clone(), c.clone()
+            got = ll.cache_attention(q, c1, lens, weights=w1, ws=ws)
+            return (*got, w1.clone(), *ll.cache_evict(c1, w1, lens, 700, recent=30, first=2), *ll.cache_read(c1, lens, 5))
+
+        jobs.append((job, job(), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    results = []
+    for _ in range(10):
+        for job, want, stream in jobs:
+            with torch.cuda.stream(stream):
+                results.append((want, job()))
+    torch.cuda.synchronize()
+    for want, got in results:
+        for a, b in zip(want, got):
+            assert torch.equal(a.nan_to_num(7e7), b.nan_to_num(7e7)) if a.is_floating_point() else torch.equal(a, b)
+
+
 def test_offsets_past_32_bits():
     """A cache of more than 2^32 bytes: the last sequence's records lie behind them."""
     ll = _ll()
