@@ -597,8 +597,9 @@ cache_attention_kernel(const CaArgs a) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             float x = CA_UP - m[nt][e & 1];
-            // (a key that is not seen: no infinity times what the factor lacks, which has either sign)
-            if (PIECES > 1) x = fmaf(fmaxf(s[u][nt][e], -FLT_MAX), fr[nt][e & 1], x);
+            // (a key that is not seen has -infinity, which no number of either sign may meet: without one that is
+            // seen the reference is -FLT_MAX, and anything above FLT_MAX would make NaN of it)
+            if (PIECES > 1) x = s[u][nt][e] > -INFINITY ? fmaf(s[u][nt][e], fr[nt][e & 1], x) : x;
             p[e] = ex2(fmaf(s[u][nt][e], f[nt][e & 1], x));
           }
           l[nt][0] += p[0] + p[2];

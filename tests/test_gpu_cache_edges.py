@@ -1,0 +1,84 @@
+"""Calls on 4-bit caches at the edges of what their contract allows, on the GPU, against plain 64-bit forms."""
+import math
+
+import pytest
+import torch
+
+import _cache_plain as plain
+import test_gpu_cache as base
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------------- large fp32 queries
+# The scale's rest (what its rounding to fp32 left) is below 0 for d = 32, 96, 112 and 128, above for 64.
+LARGE = [(32, 1, 130), (112, 9, 130), (128, 1, 3000), (96, 3, 3000), (64, 9, 3000)]
+
+
+def _check_large(got, want, gain, w0, w, X, lse_tol):
+    """X bounds the sum of a score's terms in size. Where a row's probabilities are taken a second time, for the weights,
+    they differ by its way to log2 units: on either side four roundings of 2^-24 X (reference, its difference, the
+    scale's rest, the sum)."""
+    (out, lse), wlse = got, want[1]
+    seen = wlse > -math.inf
+    assert bool(out[seen].isfinite().all()) and bool(lse[seen].isfinite().all())
+    assert bool((out[~seen] == 0).all()) and bool((lse[~seen] == -math.inf).all())
+    over = (lse.double() - wlse).abs() - (2.0 ** -16 + lse_tol)
+    assert bool((over[seen] <= 0).all()), float(over[seen].max())
+    tol = (math.expm1(2.0 ** -21 * X) + 2.0 ** -14) * gain + 2.0 ** -22 * (w0 + gain)
+    over = (w.double() - w0 - gain).abs() - tol
+    assert bool((over <= 0).all()), float(over.max())
+
+
+@pytest.mark.parametrize("d,T,S", LARGE)
+def test_large_fp32_queries_of_one_element(d, T, S):
+    """Keys of few levels along the only element that queries have: the best tie exactly and nothing else counts, so
+    far scores' rounding moves no probability. lse is a reference of a score's size with four roundings (2^-24
+    each) and a product with log 2 (2^-28). Lengths leave some warps without a key that a row sees."""
+    ll, g, N, Hq, H = base._ll(), base._gen(d + T), 4, 8, 2
+    lens = base._ints([1, 100, 129, S])
+    level = torch.tensor([0.0, 1.0, 2.0, 3.0], device="cuda")
+    k = torch.zeros((N, S, H, d), device="cuda")
+    k[..., 0] = level[torch.randint(0, 4, (N, S, H), generator=g, device="cuda")]
+    k[..., 1] = 6.0                                  # the group's largest: a scale of 1, levels exact
+    v = torch.randn((N, S, H, d), generator=g, device="cuda")
+    c = base._empty(N, S, H, d)
+    ll.cache_append(c, k, v, torch.full_like(lens, S))
+    w = torch.rand((N, H, S), generator=g, device="cuda")
+    for size in (65536.0, 98304.0, 131072.0, -114688.0):
+        q = torch.zeros((N, T, Hq, d), device="cuda")
+        q[..., 0] = size
+        w1 = w.clone()
+        got = ll.cache_attention(q, c, lens, weights=w1)
+        want = plain.attention(q, c, lens, d ** -0.5)
+        _check_large(got, want, want[2], w, w1, 3 * abs(size) * d ** -0.5, 2.0 ** -21 * want[1].abs())
+        seen = want[1] > -math.inf
+        over = (got[0].double() - want[0]).abs() - (2.0 ** -15 * want[3] + 2.0 ** -23 * want[0].abs())
+        assert bool((over[seen] <= 0).all()), float(over[seen].max())
+        alone = ll.cache_attention(q, c, lens)
+        assert torch.equal(alone[0], got[0]) and torch.equal(alone[1], got[1])
+
+
+@pytest.mark.parametrize("scale", [None, 8.0e3])
+@pytest.mark.parametrize("d,T,S", LARGE)
+def test_large_fp32_queries(d, T, S, scale):
+    """Queries of 1e4 with one element of 2e5, or of 1 at a large scale. A score's d / 16 * 3 <= 24 matrix steps round
+    by at most 2^-23 X each and its way to log2 units four times by 2^-24 X: in all below 2^-18 X, and lse moves no
+    more than the largest score's error does. Of the weights only the sums are told: a row gives away 1."""
+    ll, g, N, Hq, H = base._ll(), base._gen(d + T), 4, 8, 2
+    lens = base._ints([1, 100, 129, S])
+    c = base._filled(ll, g, N, S, H, d, torch.full_like(lens, S))
+    q = torch.randn((N, T, Hq, d), generator=g, device="cuda")
+    if scale is None:
+        q = 1e4 * q
+        q[..., 5] = 2e5
+    s = d ** -0.5 if scale is None else scale
+    w = torch.zeros((N, H, S), device="cuda")
+    got = ll.cache_attention(q, c, lens, scale=scale, weights=w)
+    want = plain.attention(q, c, lens, s)
+    X = s * torch.einsum("nthrd,njhd->nthrj", q.double().abs().view(N, T, H, Hq // H, d),
+                         plain.values(c[..., :d // 2 + 8]).abs()).amax(4).flatten(2)
+    top = float(X.max())
+    assert top < 2.0 ** 20
+    rows = (want[1] > -math.inf).view(N, T, H, Hq // H).sum((1, 3)).double()             # what each kv head gives away
+    _check_large(got, want, rows, 0.0, w.double().sum(2), top, 2.0 ** -18 * X)
