@@ -481,8 +481,9 @@ lilicorr_status_t lilicorr_cache_read(const lilicorr_cache_desc* desc, const voi
                                       cudaStream_t stream);
 
 /* Attention of each sequence's `tokens` newest tokens, which are in the cache, over its positions:
- *   out[n, t, h] = sum_j softmax_j(scale q[n, t, h] . key_j) value_j,  j < seq_len[n] - (tokens - 1 - t),
- * kv head h / (q_heads / kv_heads); lse[n, t, h] = log sum_j exp(scale q . key_j). A row that sees no key
+ *   out[n, t, h] = sum_j softmax_j(scale q[n, t, h] . key_j) value_j,  j < seq_len[n] - (tokens - 1 - t), j < capacity,
+ * kv head h / (q_heads / kv_heads); lse[n, t, h] = log sum_j exp(scale q . key_j). (Token t has position
+ * seq_len[n] - tokens + t, as in lilicorr_cache_append, past the capacity too.) A row that sees no key
  * gets out 0 and lse -inf; where seq_len[n] < 0 the rows of out and lse are left as they were. A query
  * with a NaN gives its own row NaN, and no other. What the cache holds for the positions has to be finite.
  * weights (may be NULL) [n, kv head, j] += sum of softmax_j over the tokens and the kv head's query heads

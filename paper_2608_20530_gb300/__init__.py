@@ -904,6 +904,7 @@ def cache_attention(q: torch.Tensor, cache: torch.Tensor, seq_len: torch.Tensor,
     """Attention over a cache held in 4 bits: q [N, T, q_heads, d] (fp32 or bf16; the T newest tokens of
     each sequence, which cache_append has put into the cache) over cache [N, S, kv_heads, d + 16], of which
     seq_len [N] int32 positions are held, causal among the T -> (out like q, lse [N, T, q_heads] fp32).
+    Token t has position seq_len[n] - T + t, past the capacity too, and sees what the cache has up to it.
     seq_len < 0: no such sequence, its rows of ``out`` and ``lse`` stay as they are. weights [N,
     kv_heads, S] fp32 gain what attention each position gets, summed over tokens and query heads. scale
     defaults to 1 / sqrt(d)."""

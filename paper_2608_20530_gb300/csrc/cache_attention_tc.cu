@@ -305,7 +305,7 @@ __global__ void __launch_bounds__((CtCfg<DP, HALF>::THREADS), 1) cache_attention
       named_bar(1, Cfg::SOFT + 32);
       const float f = s_factor[row];
       const bool idle = warp % Cfg::QUARTERS * 32 >= tile_rows;
-      const int lim = mine ? at.len - (a.T - 1 - tok) : 0;     // keys that the row sees
+      const int lim = mine ? at.seen(a, tok) : 0;      // keys that the row sees
       float m = -INFINITY, l = 0.f;
       bool ok = true;
       for (uint32_t t = s; t < here; t += 2) {

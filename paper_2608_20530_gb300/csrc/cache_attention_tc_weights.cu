@@ -215,7 +215,7 @@ __global__ void __launch_bounds__(CW_THREADS, 1) cache_attention_tc_weights_kern
           s_factor[row] = there ? row_factor(a, up) : 0.f;
           s_add[row] = there ? CA_UP - ml.x : 0.f;
           s_inv[row] = there ? 1.f / ml.y : 0.f;
-          s_seen[row] = there ? max(0, at.len - (a.T - 1 - tok)) : 0;
+          s_seen[row] = there ? max(0, at.seen(a, tok)) : 0;
         }
         fence_async_shared();
       }

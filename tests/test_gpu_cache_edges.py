@@ -82,3 +82,33 @@ def test_large_fp32_queries(d, T, S, scale):
     assert top < 2.0 ** 20
     rows = (want[1] > -math.inf).view(N, T, H, Hq // H).sum((1, 3)).double()             # what each kv head gives away
     _check_large(got, want, rows, 0.0, w.double().sum(2), top, 2.0 ** -18 * X)
+
+# ------------------------------------------------------------------------------- lengths past the capacity
+@pytest.mark.parametrize("path", [0, 1])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,Hq,H,d,S", [(6, 8, 2, 64, 8), (2, 4, 1, 128, 130), (16, 32, 2, 128, 300), (70, 8, 4, 48, 64),
+                                        (9, 12, 3, 32, 1500), (40, 8, 1, 80, 1300)])
+def test_lengths_past_the_capacity(T, Hq, H, d, S, dtype, path):
+    """Token t has position seq_len - T + t, as in cache_append, wherever the capacity ends: it sees those up to its own
+    that the cache holds."""
+    ll, g = base._ll(), base._gen(T + S)
+    lens = base._ints([S + 1, S + T // 2, S + T - 1, S + T + 5, S, 2 ** 31 - 1])
+    N = len(lens)
+    was = ll.test_cache_attention_path(path)
+    try:
+        c = base._filled(ll, g, N, S, H, d, lens)
+        q = (1.5 * torch.randn((N, T, Hq, d), generator=g, device="cuda")).to(base.DT[dtype])
+        w = torch.rand((N, H, S), generator=g, device="cuda")
+        w1 = w.clone()
+        first = ll.cache_attention(q, c, lens)
+        again = ll.cache_attention(q, c, lens, weights=w1)
+    finally:
+        ll.test_cache_attention_path(was)
+    gain = torch.zeros((N, H, S), dtype=torch.float64, device="cuda")
+    for t in range(T):                               # one token over as many positions as it sees
+        ends = (lens.long() - (T - 1 - t)).clamp(0, S).int()
+        base._check((first[0][:, t:t + 1], first[1][:, t:t + 1]), q[:, t:t + 1], c, ends)
+        gain += plain.attention(q[:, t:t + 1], c, ends, d ** -0.5)[2]
+    assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+    over = (w1.double() - w - gain).abs() - (2.0 ** -14 * gain + 2.0 ** -22 * (w + gain))
+    assert bool((over <= 0).all()), float(over.max())
