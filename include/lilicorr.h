@@ -463,8 +463,9 @@ size_t lilicorr_cache_record_bytes(int head_dim);
  * tokens, rounded into the cache: token t becomes position seq_len[n] - tokens + t, and is left out where
  * that is outside [0, capacity). A group of 16 elements x has the scale nearest to max |x| / (6 unit), at
  * least 2^-9 and at most 448, and the codes nearest to x / (scale unit), at most 6 (ties to the even
- * code; infinities are cut). A group with a NaN becomes NaN. The weights of the new positions become 0
- * (NULL: there are none). Fewer than 2^31 groups a call. */
+ * code; infinities are cut), with the sign of x, that of a zero too. A group with a NaN becomes NaN. Both
+ * types leave the same bytes. The weights of the new positions become 0 (NULL: there are none). Fewer than
+ * 2^31 groups a call. */
 lilicorr_status_t lilicorr_cache_append(const lilicorr_cache_desc* desc, void* cache,
                                         lilicorr_dtype_t dtype, int tokens, const void* k,
                                         const int64_t host_k_stride[3], const void* v,

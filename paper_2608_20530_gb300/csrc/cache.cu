@@ -155,18 +155,30 @@ __device__ __forceinline__ uint32_t group_scale(float top, float inv_unit) {
   return b == 0 ? 1 : b;
 }
 
-// The codes of 16 elements whose scale times the unit is su. In bf16 x / su is a border between two codes or
-// at least 2^-10 away from it, so that the product with the rounded inverse, rounded to multiples of 2^-12,
-// falls on the same side; fp32 elements are compared with the borders, which are exact products.
-__device__ __forceinline__ uint2 group_codes(const float (&x)[16], float su, __nv_bfloat16) {
+// The codes of 16 elements x, whose bits are u and whose scale times the unit is su. In bf16 x / su is a border
+// between two codes or at least 2^-10 away from it, so that the product with the rounded inverse, rounded to
+// multiples of 2^-12, falls on the same side; fp32 elements are compared with the borders, which are exact products.
+// Either way a code has its element's sign, that of a zero too, and codes of a NaN group have nothing else.
+__device__ __forceinline__ uint2 group_codes(const float (&x)[16], const uint32_t (&u)[8], float su) {
   const float inv = 1.f / su, big = 0x1.8p11f;
-  uint32_t w[2] = {0, 0};
+  uint32_t w[2];
 #pragma unroll
-  for (int i = 0; i < 16; i += 2)
-    w[i / 8] |= codes2(fmaf(x[i], inv, big) - big, fmaf(x[i + 1], inv, big) - big) << (i % 8 * 4);
+  for (int j = 0; j < 2; ++j) {
+    w[j] = 0;
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+      const float lo = fmaf(x[8 * j + i], inv, big) - big, hi = fmaf(x[8 * j + i + 1], inv, big) - big;
+      w[j] |= codes2(lo, hi) << (4 * i);
+    }
+    if (!(su == su)) w[j] = 0;
+    // what rounds to zero comes out as +0: the bytes that hold the signs of the even and of the odd elements
+    const uint32_t a = __byte_perm(u[4 * j], u[4 * j + 1], 0x7351), b = __byte_perm(u[4 * j + 2], u[4 * j + 3], 0x7351);
+    const uint32_t even = __byte_perm(a, b, 0x5410), odd = __byte_perm(a, b, 0x7632);
+    w[j] |= (even >> 4 & 0x08080808u) | (odd & 0x80808080u);
+  }
   return make_uint2(w[0], w[1]);
 }
-__device__ __forceinline__ uint2 group_codes(const float (&x)[16], float su, float) {
+__device__ __forceinline__ uint2 group_codes(const float (&x)[16], const uint32_t (&)[16], float su) {
   uint32_t w[2] = {0, 0};
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
@@ -244,7 +256,7 @@ __global__ void __launch_bounds__(256) cache_append_kernel(const CacheView c, co
     const float top = group_top(u[kv], e);
     const uint32_t b = group_scale(top, 1.f / unit);
     unsigned char* to = rec + kv * cache_half_bytes(c.d);
-    *reinterpret_cast<uint2*>(to + x.g * 8) = group_codes(e, scale_value(b) * unit, E());
+    *reinterpret_cast<uint2*>(to + x.g * 8) = group_codes(e, u[kv], scale_value(b) * unit);
     to[c.d / 2 + x.g] = (unsigned char)b;
     if (x.g == 0)                                    // scales that no group has
       for (int i = c.d / 16; i < 8; ++i) to[c.d / 2 + i] = 0;

@@ -112,3 +112,42 @@ def test_lengths_past_the_capacity(T, Hq, H, d, S, dtype, path):
     assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
     over = (w1.double() - w - gain).abs() - (2.0 ** -14 * gain + 2.0 ** -22 * (w + gain))
     assert bool((over <= 0).all()), float(over.max())
+
+# ------------------------------------------------------------------------------- records byte by byte
+def _half_records(x, unit=1.0):
+    """x [..., d] as half records: codes, scales, zeros up to eight of them."""
+    g = x.double().unflatten(-1, (-1, 16)) / unit
+    top = g.abs().amax(-1)
+    scale = plain.nearest(top.clamp(max=1e300) / 6, plain.SCALES[:127]).clamp(min=1)
+    s = torch.tensor(plain.SCALES, dtype=torch.float64, device=x.device)[scale]
+    code = plain.nearest((g.abs() / s[..., None]).nan_to_num(0.0, posinf=9.0), plain.CODES)
+    code = torch.where(top.isnan()[..., None], 0, code)          # of a NaN group, signs alone
+    bits, top_bit = (torch.int32, 31) if x.dtype == torch.float32 else (torch.int16, 15)
+    sign = (x.view(bits).int() >> top_bit & 1).unflatten(-1, (-1, 16))
+    code = (code + 8 * sign).flatten(-2)
+    scales = torch.zeros((*x.shape[:-1], 8), dtype=torch.long, device=x.device)
+    scales[..., :scale.shape[-1]] = torch.where(top.isnan(), 127, scale)
+    return torch.cat([code[..., ::2] + 16 * code[..., 1::2], scales], -1).byte()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [16, 48, 80, 112, 128])
+def test_records_byte_by_byte(d, dtype):
+    """Codes, scales and the rest of a record are the same bytes for both types: zeros keep their sign, negative
+    elements that round to zero too, and a NaN group has signs alone."""
+    ll, g, N, T, H = base._ll(), base._gen(d), 3, 50, 2
+    x = torch.randn((N, T, H, d // 16, 16), generator=g, device="cuda")
+    pick = torch.randint(0, 8, x.shape, generator=g, device="cuda")
+    for i, to in enumerate((0.0, -0.0, 2.0 ** -16, -2.0 ** -16, -2.0 ** -100)):
+        x = torch.where(pick == i, torch.tensor(to, device="cuda"), x)
+    x[0, 0] = -0.0
+    x[0, 1, :, :, 3] = -math.inf
+    x[0, 2, :, :, 5] = math.nan
+    x[0, 3, :, :, 1] = -math.nan
+    x = x * torch.exp2(torch.randint(-12, 8, (N, T, H, d // 16, 1), generator=g, device="cuda").float())
+    x = x.flatten(3).to(base.DT[dtype]).contiguous()
+    lens = base._ints([T] * N)
+    for unit in (1.0, 2.0 ** -9):
+        c = base._empty(N, T, H, d)
+        ll.cache_append(c, x, -x, lens, k_unit=unit)
+        assert torch.equal(c, torch.cat([_half_records(x, unit), _half_records(-x)], -1)), unit
