@@ -515,9 +515,10 @@ lilicorr_status_t lilicorr_cache_attention(const lilicorr_cache_attention_desc* 
  * ones by lower position; -0 equals +0, NaN counts as less than anything). Records and weights of what
  * stays move, in the order of their positions, to positions 0, 1, ..., in place or, with `into` (of the
  * same sequences, kv_heads and head_dim, capacity at least budget, units of `desc`), to another cache and
- * its weights, to which shorter sequences are copied whole. Positions behind keep what they held.
+ * its weights, to which shorter sequences are copied whole (the first cache is then only read, and may
+ * overlap itself). Positions behind keep what they held.
  *   kept [sequences, kv_heads, budget] int32: the positions that stayed, in order, then -1
- *   new_len [sequences] int32: min(seq_len, budget) (a negative seq_len as it is); not seq_len itself,
+ *   new_len [sequences] int32: min(seq_len, capacity, budget) (a negative seq_len as it is); not seq_len itself,
  *   which other layers may still need
  * 1 <= budget <= 2^30, first + recent <= budget. The spans of memory of the two caches, and of their weights,
  * must not overlap. */

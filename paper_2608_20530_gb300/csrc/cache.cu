@@ -696,7 +696,7 @@ lilicorr_status_t run_evict(const lilicorr_cache_desc* desc, void* cache, float*
   if (budget < 1 || recent < 0 || first < 0 || (int64_t)recent + first > budget) return LILICORR_ERR_ARG;
   if (budget > (1 << 30)) return LILICORR_ERR_SHAPE;           // (places are counted in 32 bits)
   EvictArgs a;
-  LL_TRY(cache_view(desc, cache, true, &a.from));
+  LL_TRY(cache_view(desc, cache, into == nullptr, &a.from));   // in place it is written
   a.to = a.from;
   if (into) {
     LL_TRY(cache_shape(into));

@@ -151,3 +151,23 @@ def test_records_byte_by_byte(d, dtype):
         c = base._empty(N, T, H, d)
         ll.cache_append(c, x, -x, lens, k_unit=unit)
         assert torch.equal(c, torch.cat([_half_records(x, unit), _half_records(-x)], -1)), unit
+
+# ------------------------------------------------------------------------------- eviction
+def test_evict_a_shared_cache_into_others():
+    """One prompt's records stand for all sequences (a stride of 0): read, they may, and each gets its own choice."""
+    ll, N, S, H, d, budget = base._ll(), 3, 200, 2, 64, 50
+    c, w, lens = base._evict_case(N, S, H, d, [200, 150, 40], 5)
+    one = c[:1].clone()
+    shared = one.expand(N, S, H, d + 16)
+    want, new = plain.evict(w.cpu(), lens.tolist(), budget, 10, 2)
+    to, to_w = base._empty(N, 64, H, d), torch.full((N, H, 64), 5.0, device="cuda")
+    kept, new_len = ll.cache_evict(shared, w, lens, budget, recent=10, first=2, into=to, into_weights=to_w)
+    assert torch.equal(kept.cpu(), want) and torch.equal(new_len.cpu(), new)
+    there, at, h = kept >= 0, kept.clamp(min=0).long(), torch.arange(H, device="cuda")[:, None]
+    assert torch.equal(to[:, :budget].transpose(1, 2), torch.where(there[..., None], one[0][at, h], 0x7F))
+    assert base._same(to_w[..., :budget].contiguous(), torch.where(there, torch.gather(w, 2, at), 5.0))
+    # written, it may not: in place, and as what is written into
+    with pytest.raises(ll.LilicorrError):
+        ll.cache_evict(shared, w, lens, budget)
+    with pytest.raises(ll.LilicorrError):
+        ll.cache_evict(c, w, lens, budget, into=shared, into_weights=w.clone())
