@@ -171,3 +171,19 @@ def test_evict_a_shared_cache_into_others():
         ll.cache_evict(shared, w, lens, budget)
     with pytest.raises(ll.LilicorrError):
         ll.cache_evict(c, w, lens, budget, into=shared, into_weights=w.clone())
+
+
+@pytest.mark.parametrize("weights", ["spread", "ties", "nan"])
+@pytest.mark.parametrize("case", [
+    # N, S, H, d, lengths, budget, recent, first: on 152 SMs clusters of 4, 2, 1 CTAs an item, ...
+    (10, 900, 4, 128, [900 - 37 * i for i in range(10)], 600, 50, 3),
+    (20, 700, 4, 80, [700 - 30 * i for i in range(20)], 333, 20, 0),
+    (100, 1300, 2, 128, [1300 - 7 * i for i in range(100)], 1000, 100, 4),
+    (200, 90, 1, 16, [90 - i % 60 for i in range(200)], 44, 3, 1),
+    # ... of 4 with a stretch of 2,500 each, of 2 with more than are kept in shared memory, and one CTA with as many
+    (10, 10000, 4, 32, [10000 - 100 * i for i in range(10)], 700, 64, 4),
+    (40, 17000, 2, 16, [17000 - 50 * i for i in range(40)], 9000, 64, 4),
+    (160, 9000, 1, 16, [9000 - 10 * i for i in range(160)], 8500, 100, 2),
+])
+def test_evict_clusters_of_every_size(case, weights):
+    base.test_evict(case, weights)
