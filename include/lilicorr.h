@@ -494,7 +494,8 @@ lilicorr_status_t lilicorr_cache_read(const lilicorr_cache_desc* desc, const voi
  * q_heads a multiple of kv_heads, sequences * tokens * q_heads at most 2^30, 0 < scale * k_unit < 2^100. The cache may overlap itself; out may not, nor
  * may out, lse and weights overlap anything else. Queries enter exactly, to 2^-38 of their row's
  * largest element, and so do keys and values; softmax and sums are fp32 (BF16: probabilities are rounded to
- * fp16 once). ws: zero-filled once, at least
+ * fp16 once). Scores (the sums of their terms' sizes) have to stay below 2^23: fp32 does not tell larger ones
+ * apart, and their rows may become infinite, NaN or 0. ws: zero-filled once, at least
  * lilicorr_cache_attention_workspace_bytes(desc) bytes (0: unsupported; enough with weights and without); one
  * workspace serves calls of any shapes. Its first word is the device status. */
 typedef struct {

@@ -907,7 +907,7 @@ def cache_attention(q: torch.Tensor, cache: torch.Tensor, seq_len: torch.Tensor,
     Token t has position seq_len[n] - T + t, past the capacity too, and sees what the cache has up to it.
     seq_len < 0: no such sequence, its rows of ``out`` and ``lse`` stay as they are. weights [N,
     kv_heads, S] fp32 gain what attention each position gets, summed over tokens and query heads. scale
-    defaults to 1 / sqrt(d)."""
+    defaults to 1 / sqrt(d); scores have to stay below 2^23 (see lilicorr.h)."""
     dev, dt = torch.cuda.current_device(), q.dtype
     x = _cache(cache, dev)
     if q.dim() != 4:

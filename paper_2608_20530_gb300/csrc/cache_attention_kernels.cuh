@@ -26,7 +26,8 @@ constexpr int CA_WARPS = 8;                  // of a CTA, each with its own keys
 constexpr int CA_THREADS = 32 * CA_WARPS;
 // Probabilities are 2^(s - m + CA_UP) with the row's reference m. Only where a score is more than CA_SLACK above
 // it does it move, to CA_ROOM above the largest so far, so that few steps have sums to rescale. The largest is
-// then between 2^6 and 2^15, and fp16 numbers have their full precision down to 2^-20 of it.
+// then between 2^6 and 2^15, and fp16 numbers have their full precision down to 2^-20 of it. (Up to scores of 2^24 in
+// log2 units: their sums with the reference round by at most 1/2 there, and 2^15.5 is still an fp16 number.)
 constexpr float CA_UP = 7.f, CA_SLACK = 8.f, CA_ROOM = 1.f;
 
 // The work is the list of all (sequence, team of kv heads, row block, tile of KEYS keys), in that order, cut

@@ -187,3 +187,40 @@ def test_evict_a_shared_cache_into_others():
 ])
 def test_evict_clusters_of_every_size(case, weights):
     base.test_evict(case, weights)
+
+
+# ------------------------------------------------------------------------------- far scores
+@pytest.mark.parametrize("path", [0, 1])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d,T,S", [(64, 1, 400), (128, 4, 3000), (32, 20, 3000), (96, 9, 700)])
+def test_far_scores_that_lie_close(d, T, S, dtype, path):
+    """Scores of nearly 2^23, the largest that the contract has, some a few units apart, in any order: rows keep finite
+    numbers. X, terms and tolerance as in test_large_fp32_queries; bf16 has a third of its matrix steps."""
+    ll, g, N, Hq, H = base._ll(), base._gen(d + T), 3, 8, 2
+    lens = base._ints([129, 100, S])
+    k = torch.zeros((N, S, H, d), device="cuda")
+    k[..., 0] = torch.tensor([2.0, 3.0], device="cuda")[(torch.rand((N, S, H), generator=g, device="cuda") < 0.7).long()]
+    k[..., 1] = 6.0                                  # the group's largest: a scale of 1
+    k[..., 2] = torch.randint(0, 5, (N, S, H), generator=g, device="cuda").float()       # (half steps: rounded)
+    v = torch.randn((N, S, H, d), generator=g, device="cuda")
+    c = base._empty(N, S, H, d)
+    ll.cache_append(c, k, v, torch.full_like(lens, S))
+    s = d ** -0.5
+    q = torch.zeros((N, T, Hq, d), device="cuda")
+    q[..., 0] = 0.98 * 2.0 ** 23 / (3 * s)
+    q[..., 2] = torch.rand((N, T, Hq), generator=g, device="cuda") * 2 / s
+    q = q.to(base.DT[dtype])
+    was = ll.test_cache_attention_path(path)
+    try:
+        out, lse = ll.cache_attention(q, c, lens)
+    finally:
+        ll.test_cache_attention_path(was)
+    want, wlse, _, _ = plain.attention(q, c, lens, s)
+    X = s * (3 * q[..., 0].double() + 4 * q[..., 2].double())
+    assert float(X.max()) < 2.0 ** 23
+    seen = wlse > -math.inf
+    assert bool(out[seen].isfinite().all()) and bool((out[~seen] == 0).all())
+    assert bool((out[seen].abs().float() <= 1.01 * plain.values(c[..., d // 2 + 8:]).abs().max()).all())
+    over = (lse.double() - wlse).abs() - (2.0 ** -16 + 2.0 ** -18 * X)
+    assert bool((over[seen] <= 0).all()), float(over[seen].max())
+    assert bool((lse[~seen] == -math.inf).all())
