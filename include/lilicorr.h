@@ -445,8 +445,9 @@ lilicorr_status_t lilicorr_prefix_attention(const lilicorr_prefix_attention_desc
  * scale is a multiple of 2^-9, and a value is cut at 2688 units).
  * A cache is [sequences, capacity, kv_heads] records, 16-byte aligned, the strides in bytes, multiples of 16
  * and not negative (of positions below 2^28). Where it is written no two of its records may overlap.
- * head_dim is a multiple of 16 up to 128, capacity at most 2^30. Sequence n holds the positions below seq_len[n] (int32, on the device),
- * clipped to [0, capacity]; below 0 there is no such sequence. What lies behind is not looked at.
+ * head_dim is a multiple of 16 up to 128, capacity at most 2^30. Sequence n holds the positions below seq_len[n]
+ * (int32, on the device), clipped to [0, capacity]; below 0 there is no such sequence. What lies behind is not
+ * looked at.
  * weights [sequences, kv_heads, capacity] fp32, where there are any, hold what attention each key has
  * gathered: appended at 0, added to by lilicorr_cache_attention, read and moved by lilicorr_cache_evict. */
 typedef struct {
@@ -482,22 +483,24 @@ lilicorr_status_t lilicorr_cache_read(const lilicorr_cache_desc* desc, const voi
                                       cudaStream_t stream);
 
 /* Attention of each sequence's `tokens` newest tokens, which are in the cache, over its positions:
- *   out[n, t, h] = sum_j softmax_j(scale q[n, t, h] . key_j) value_j,  j < seq_len[n] - (tokens - 1 - t), j < capacity,
- * kv head h / (q_heads / kv_heads); lse[n, t, h] = log sum_j exp(scale q . key_j). (Token t has position
- * seq_len[n] - tokens + t, as in lilicorr_cache_append, past the capacity too.) A row that sees no key
- * gets out 0 and lse -inf; where seq_len[n] < 0 the rows of out and lse are left as they were. A query
- * with a NaN gives its own row NaN, and no other. What the cache holds for the positions has to be finite.
+ *   out[n, t, h] = sum_j softmax_j(scale q[n, t, h] . key_j) value_j,
+ *   j < seq_len[n] - (tokens - 1 - t) and j < capacity, kv head h / (q_heads / kv_heads);
+ *   lse[n, t, h] = log sum_j exp(scale q . key_j)
+ * (token t has position seq_len[n] - tokens + t, as in lilicorr_cache_append, past the capacity too). A row
+ * that sees no key gets out 0 and lse -inf; where seq_len[n] < 0 the rows of out and lse are left as they
+ * were. A query with a NaN gives its own row NaN, and no other. What the cache holds for the positions has
+ * to be finite.
  * weights (may be NULL) [n, kv head, j] += sum of softmax_j over the tokens and the kv head's query heads
  * (rows whose lse is not finite add nothing).
  *   q, out [sequences, tokens, q_heads, head_dim] of dtype, strides in elements, 16-byte aligned; lse
  *   [sequences, tokens, q_heads] fp32
- * q_heads a multiple of kv_heads, sequences * tokens * q_heads at most 2^30, 0 < scale * k_unit < 2^100. The cache may overlap itself; out may not, nor
- * may out, lse and weights overlap anything else. Queries enter exactly, to 2^-38 of their row's
- * largest element, and so do keys and values; softmax and sums are fp32 (BF16: probabilities are rounded to
- * fp16 once). Scores (the sums of their terms' sizes) have to stay below 2^23: fp32 does not tell larger ones
- * apart, and their rows may become infinite, NaN or 0. ws: zero-filled once, at least
- * lilicorr_cache_attention_workspace_bytes(desc) bytes (0: unsupported; enough with weights and without); one
- * workspace serves calls of any shapes. Its first word is the device status. */
+ * q_heads a multiple of kv_heads, sequences * tokens * q_heads at most 2^30, 0 < scale * k_unit < 2^100.
+ * The cache may overlap itself; out may not, nor may out, lse and weights overlap anything else. Queries
+ * enter exactly, to 2^-38 of their row's largest element, and so do keys and values; softmax and sums are
+ * fp32 (BF16: probabilities are rounded to fp16 once). Scores (the sums of their terms' sizes) have to stay
+ * below 2^23: fp32 does not tell larger ones apart, and their rows may become infinite, NaN or 0. ws:
+ * zero-filled once, at least lilicorr_cache_attention_workspace_bytes(desc) bytes (0: unsupported; enough with
+ * weights and without); one workspace serves calls of any shapes. Its first word is the device status. */
 typedef struct {
   lilicorr_cache_desc cache;
   int tokens, q_heads;

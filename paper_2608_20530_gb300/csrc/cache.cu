@@ -234,10 +234,11 @@ __device__ __forceinline__ float group_top(const uint32_t (&u)[16], float (&x)[1
   return top;
 }
 
-// Bytes should bound both kernels (bf16: 2.56 an element), and issue comes near: about 160 (append) and 110 (read)
-// instructions a thread's group of the key and of the value. Up to 8,192 tokens of four sequences, 8 heads of 128:
-// append and read together 51.6 us in a graph, 260 MB at 5.0 TB/s. Loads and stores of 32 bytes, a whole sector a
-// lane, and products for the divisions took them there from 72.
+// Bytes should bound both kernels (bf16: 2.56 an element); neither they (DRAM 48 and 50 % under a profiler) nor issue
+// (67 and 56 % of the slots; about 160 and 110 instructions a thread's group of the key and of the value) do: what is
+// left is the way of a thread's two loads, all that it has under way. Up to 8,192 tokens of four sequences, 8 heads
+// of 128: append and read together 51.5 us in a graph, 260 MB at 5.0 TB/s (under the profiler 29.2 and 25.8). Loads and
+// stores of 32 bytes, a whole sector a lane, and products for the divisions took them there from 72.
 template <typename E>
 __global__ void __launch_bounds__(256) cache_append_kernel(const CacheView c, const CacheTokens a) {
   pdl_wait();
@@ -357,9 +358,11 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
 // A cluster of CTAs has one (sequence, kv head). Which positions stay is found by each of them for itself where
 // there are few (a barrier of the cluster costs as much as a pass), else each looks at a stretch of them. The
 // records that stay are moved by all of them together.
-// What bounds it is the chain of rounds (count, barriers, prefix sum, barrier), then the records' bytes: 8 heads cut
-// from 2,304 to 2,048 11.3 us in a graph (one CTA that read weights from memory each round: 55), 256 heads of up to
-// 4,160 to 2,048 40.4 (records read and written 19 at the copy rate), 16 heads of up to 65,536 to 4,096 31.8.
+// What bounds it: for one sequence its chain, of 22 thousand clocks 10 in the move (one turn's loads and stores), 2.6 a
+// round (count, barriers, prefix sum, barrier), 3 each for the ranking and the places; for many the rounds, then the
+// records, a turn after the other (DRAM 27 %, waits for loads). 8 heads cut from 2,304 to 2,048 11.3 us in a graph
+// (one CTA that read weights from memory each round: 55), 256 heads of up to 4,160 to 2,048 40.4 (records read and
+// written 19 at the copy rate), 16 heads of up to 65,536 to 4,096 31.8.
 // CTAs of 1,024 threads, one an SM, took 17 and 58 for the first two's 13 and 36 of then.
 constexpr int EV_THREADS = 512, EV_WARPS = EV_THREADS / 32;
 constexpr int EV_BINS = 2048;  // 11 bits a round

@@ -40,7 +40,9 @@ lilicorr_status_t ca_plan(const lilicorr_cache_attention_desc* d, CaPlan* p) {
   // 2,048 13.9 (11.5); 128 items of 2,048 keys 14.0 (15.9), 512 40.5 (44.0), 2,048 130 (133).
   p->whole = !p->tc && (c.capacity <= 1024 || (c.capacity <= 2048 && p->items >= (size_t)num_sms() * 3 / 4));
   if ((double)p->items * (c.capacity / 128 + 1) >= 2147483648.0) return LILICORR_ERR_SHAPE;
-  // the widest team of at most 16: all heads of a position where there are so few
+  // the widest team of at most 16: all heads of a position where there are so few. Measured for 8 heads whose records
+  // lie side by side (32 sequences of 8,192: 193 MB read for 259 one head after the other); caches by head, where heads
+  // share no line, and 11 or more heads, which leave up to 9 SMs without a CTA, take the same rule unmeasured.
   p->team = 1;
   for (int i = 2; i <= 16; ++i)
     if (c.kv_heads % i == 0) p->team = i;
